@@ -318,6 +318,105 @@ eat_status eat_selftest_bounded_wait(int64_t limit_ns, uint32_t* status_out);
  * EAT_ERR_STATE until eat_reset_accounts.  No fault, trap or hang is involved. */
 eat_status eat_selftest_expire_wait(eat_handle* h, int64_t limit_ns, void* stream);
 
+/* ---- Operators around the layer: norm, vocabulary head, balance loss --------------------------
+ * They need no layer handle.  Errors are reported through eat_last_error(NULL). */
+
+/* h = x + residual; y = h / sqrt(mean(h^2) + eps) * gamma, row by row: what stands before an EAT
+ * layer (its x is y) and after it (its y is the next call's x, h the next call's residual).
+ * x, residual, h [T, d] in xdtype (EAT_F32 or EAT_BF16); gamma [d] fp32; residual may be NULL: then
+ * h = x and the h argument is not written (it may be NULL).  h may alias x or residual.
+ *  - ydtype == xdtype: y [T, d]; y_scale is ignored.
+ *  - ydtype == EAT_FP8_E4M3: y [T, d] e4m3 bytes and y_scale [T] fp32, row t being
+ *    y_scale[t] * (its bytes): y_scale[t] = max |row| / 448 (1 for an all-zero row), the format of
+ *    the library's e4m3 weights and of an e4m3 head's hidden states.
+ * h is rounded to xdtype when it is stored; y is computed from the unrounded fp32 sum.
+ * T >= 1, 1 <= d <= 65536, eps > 0.  Any alignment of the element types is accepted. */
+eat_status eat_rms_norm(const void* x, const void* residual, int32_t T, int32_t d, int32_t xdtype,
+                        const float* gamma, double eps, void* h, void* y, int32_t ydtype,
+                        float* y_scale, void* stream);
+
+/* Gradient of eat_rms_norm at the stored sum h [T, d] (xdtype).  dy [T, d]: gradient of y (with an
+ * e4m3 output: of the values it stands for); dres [T, d] or NULL: gradient that reaches h from
+ * elsewhere (the residual stream).  With n = h / sqrt(mean(h^2) + eps):
+ *   dx [T, d] (xdtype) = dres + (gamma dy - n mean(gamma dy n)) / sqrt(mean(h^2) + eps), which is the
+ *   gradient of x and of the residual alike;  dgamma [d] fp32 = sum over rows of dy n, in a fixed
+ *   order (the same inputs give the same bits).
+ * dx may alias dy or dres.  work: eat_rms_norm_grad_workspace(T, d) bytes of device memory, 16-byte
+ * aligned, whose contents do not matter; the call may use it until it has finished on `stream`. */
+eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int32_t xdtype,
+                             const float* gamma, double eps, const void* dy, const void* dres,
+                             void* dx, float* dgamma, void* work, void* stream);
+int64_t eat_rms_norm_grad_workspace(int32_t T, int32_t d);
+
+/* Load-balancing loss of a router and per-expert counts.  logits [T, E] fp32 (before the softmax,
+ * after any temperature); idx [T, K] int32 as eat_route writes it (entries outside [0, E), such as
+ * the -1 after the k-th, select nothing); mask [T] bytes or NULL: tokens whose byte is 0 do not
+ * count, whatever their logits and idx hold.  Over the n counted tokens:
+ *   counts[e] = number of entries of idx equal to e;  f_e = counts[e] / sum counts;
+ *   loss = E sum_e f_e (1/n) sum_t softmax(logits_t)_e   (1 for a uniform router, 0 when no token
+ *   counts or none selects an expert).
+ * Outputs on the device: loss [1] fp32, counts [E] int32, n_tokens [1] int32 (= n).  Sums have a
+ * fixed order.  T >= 1, 1 <= E <= 256, 1 <= K <= 16.  work: eat_balance_workspace(T, E) bytes, as
+ * above. */
+eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E, int32_t K,
+                            const int32_t* idx, const uint8_t* mask, float* loss, int32_t* counts,
+                            int32_t* n_tokens, void* work, void* stream);
+int64_t eat_balance_workspace(int32_t T, int32_t E);
+
+/* Gradient of eat_balance_loss to the logits, f held constant (counts have no gradient):
+ *   dlogits_te = g E / n p_te (f_e - sum_j f_j p_tj), 0 for tokens that do not count.
+ * counts and n_tokens: eat_balance_loss's outputs; g: device [1] fp32, the gradient of the loss.
+ * dlogits [T, E] fp32 may alias logits. */
+eat_status eat_balance_grad(const float* logits, int32_t T, int32_t E, const uint8_t* mask,
+                            const int32_t* counts, const int32_t* n_tokens, const float* g,
+                            float* dlogits, void* stream);
+
+/* A vocabulary head: logits l_tv = <x_t, w_v>, and the softmax cross entropy of their targets,
+ * computed in pieces so that the T x vocab logits are never held in memory.  The nll of a window of
+ * tokens is what eat_ppl_update takes.
+ * w [vocab, d_model] in dtype: EAT_BF16, or EAT_FP8_E4M3 with w_scale [vocab] fp32 (row v is
+ * w_scale[v] * its bytes).  The hidden states of a call have the same dtype.  The caller keeps w
+ * (and w_scale) alive; w may be updated in place between calls (in stream order).
+ * with_grad != 0 (EAT_BF16 only): the handle also holds the workspace of eat_head_nll_grad.
+ * Supported: d_model a multiple of 64 up to 16384; 1 <= vocab <= 2^20; 1 <= max_tokens <= 65536; w
+ * 16-byte aligned.  fp32 heads are not: their products would not run on the tensor cores. */
+typedef struct eat_head_desc {
+  int32_t d_model, vocab, max_tokens, dtype, with_grad;
+  const void* w;
+  const float* w_scale;
+} eat_head_desc;
+
+typedef struct eat_head eat_head;
+
+/* As eat_create / eat_destroy: validates, allocates the workspace (no call allocates afterwards),
+ * synchronous; a failure leaves *out NULL.  One handle serves one stream at a time. */
+eat_status eat_head_create(const eat_head_desc* desc, eat_head** out);
+eat_status eat_head_destroy(eat_head* h);
+
+/* Loss of T tokens, 1 <= T <= max_tokens: x [T, d_model] (dtype, 16-byte aligned); x_scale [T] fp32
+ * for an e4m3 head (token t is x_scale[t] * its bytes), else ignored; target [T] int32.
+ *   lse[t] = log sum_v exp l_tv;  nll[t] = lse[t] - l_t,target[t]   (fp32)
+ * A token whose target is negative is ignored: nll = lse = 0, whatever its x holds.  One whose
+ * target is >= vocab gets nll = lse = NaN.  nll keeps its relative accuracy for confident tokens
+ * (it is summed as log(1 + sum over the other v of exp(l_v - l_target))).  lse may be NULL. */
+eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_t T,
+                        const int32_t* target, float* nll, float* lse, void* stream);
+
+/* The loss as eat_head_nll and, in the same call, the gradients of sum_t g[t] nll[t] (g [T] fp32,
+ * e.g. 1 / number of tokens): with P_tv = g[t] (exp(l_tv - lse[t]) - [v = target[t]]),
+ *   dx [T, d_model] = P w,  dw [vocab, d_model] = P^T x, both bf16, rounded from fp32 sums.
+ * P enters the products as bf16.  Ignored tokens, and tokens whose target is >= vocab, give a zero
+ * row of dx and add nothing to dw, whatever their x holds (NaN among it).  dx must not alias x.
+ * dx and dw 16-byte aligned.  Needs a handle created with with_grad. */
+eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_t* target,
+                             const float* g, float* nll, float* lse, void* dx, void* dw,
+                             void* stream);
+
+/* A kernel of the head that gave up on a bounded wait (see EAT_ERR_STATE) makes the nll of its call
+ * NaN, and later calls on the handle fail with EAT_ERR_STATE until eat_head_reset, which
+ * synchronises `stream`. */
+eat_status eat_head_reset(eat_head* h, void* stream);
+
 /* Last error on the handle (never NULL), or a generic text for a NULL handle. */
 const char* eat_last_error(const eat_handle* h);
 const char* eat_status_string(eat_status s);

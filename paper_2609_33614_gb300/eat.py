@@ -41,6 +41,11 @@ class eat_layer_desc(ctypes.Structure):
                                     "ws_gate_scale", "ws_up_scale", "ws_down_scale")]
 
 
+class eat_head_desc(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("d_model", "vocab", "max_tokens", "dtype", "with_grad")] + \
+               [("w", c_vp), ("w_scale", c_vp)]
+
+
 class EatError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{status_string(status)}: {msg}")
@@ -75,6 +80,20 @@ _SIGS = {
     "eat_ffn_backend": (c_i32, [c_vp]),
     "eat_selftest_bounded_wait": (c_i32, [c_i64, ctypes.POINTER(ctypes.c_uint32)]),
     "eat_selftest_expire_wait": (c_i32, [c_vp, c_i64, c_vp]),
+    "eat_rms_norm": (c_i32, [c_vp, c_vp, c_i32, c_i32, c_i32, c_vp, c_dbl, c_vp, c_vp, c_i32, c_vp,
+                             c_vp]),
+    "eat_rms_norm_grad": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_dbl, c_vp, c_vp, c_vp, c_vp,
+                                  c_vp, c_vp]),
+    "eat_rms_norm_grad_workspace": (c_i64, [c_i32, c_i32]),
+    "eat_balance_loss": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                 c_vp]),
+    "eat_balance_workspace": (c_i64, [c_i32, c_i32]),
+    "eat_balance_grad": (c_i32, [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "eat_head_create": (c_i32, [ctypes.POINTER(eat_head_desc), ctypes.POINTER(c_vp)]),
+    "eat_head_destroy": (c_i32, [c_vp]),
+    "eat_head_nll": (c_i32, [c_vp, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp]),
+    "eat_head_nll_grad": (c_i32, [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "eat_head_reset": (c_i32, [c_vp, c_vp]),
     "eat_last_error": (ctypes.c_char_p, [c_vp]),
     "eat_status_string": (ctypes.c_char_p, [c_i32]),
 }
@@ -244,6 +263,215 @@ def eat_selftest_bounded_wait(limit_ns: int) -> int:
 
 def eat_selftest_expire_wait(h, limit_ns: int, stream=None):
     _check(lib().eat_selftest_expire_wait(h, limit_ns, _stream(stream)), h)
+
+
+def eat_rms_norm(x, residual, T, d, xdtype, gamma, eps, h, y, ydtype, y_scale=None, stream=None):
+    _check(lib().eat_rms_norm(_ptr(x), _ptr(residual), T, d, xdtype, _ptr(gamma), eps, _ptr(h),
+                              _ptr(y), ydtype, _ptr(y_scale), _stream(stream)))
+
+
+def eat_rms_norm_grad(h, T, d, xdtype, gamma, eps, dy, dres, dx, dgamma, work, stream=None):
+    _check(lib().eat_rms_norm_grad(_ptr(h), T, d, xdtype, _ptr(gamma), eps, _ptr(dy), _ptr(dres),
+                                   _ptr(dx), _ptr(dgamma), _ptr(work), _stream(stream)))
+
+
+def eat_rms_norm_grad_workspace(T, d) -> int:
+    return lib().eat_rms_norm_grad_workspace(T, d)
+
+
+def eat_balance_loss(logits, T, E, K, idx, mask, loss, counts, n_tokens, work, stream=None):
+    _check(lib().eat_balance_loss(_ptr(logits), T, E, K, _ptr(idx), _ptr(mask), _ptr(loss),
+                                  _ptr(counts), _ptr(n_tokens), _ptr(work), _stream(stream)))
+
+
+def eat_balance_workspace(T, E) -> int:
+    return lib().eat_balance_workspace(T, E)
+
+
+def eat_balance_grad(logits, T, E, mask, counts, n_tokens, g, dlogits, stream=None):
+    _check(lib().eat_balance_grad(_ptr(logits), T, E, _ptr(mask), _ptr(counts), _ptr(n_tokens),
+                                  _ptr(g), _ptr(dlogits), _stream(stream)))
+
+
+def eat_head_create(desc: eat_head_desc) -> int:
+    h = c_vp()
+    _check(lib().eat_head_create(ctypes.byref(desc), ctypes.byref(h)))
+    return h.value
+
+
+def eat_head_destroy(h):
+    _check(lib().eat_head_destroy(h))
+
+
+def eat_head_nll(h, x, x_scale, T, target, nll, lse=None, stream=None):
+    _check(lib().eat_head_nll(h, _ptr(x), _ptr(x_scale), T, _ptr(target), _ptr(nll), _ptr(lse),
+                              _stream(stream)))
+
+
+def eat_head_nll_grad(h, x, T, target, g, nll, lse, dx, dw, stream=None):
+    _check(lib().eat_head_nll_grad(h, _ptr(x), T, _ptr(target), _ptr(g), _ptr(nll), _ptr(lse),
+                                   _ptr(dx), _ptr(dw), _stream(stream)))
+
+
+def eat_head_reset(h, stream=None):
+    _check(lib().eat_head_reset(h, _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------------
+# The operators around the layer on torch tensors (still only marshalling).  Tensors are CUDA,
+# contiguous and of the stated type; outputs are new tensors, and calls go to the current stream.
+# ------------------------------------------------------------------------------------------------
+def _take(name, t, shape, *dtypes):
+    """Raise unless tensor t has this shape and one of the types, contiguous on the GPU."""
+    if tuple(t.shape) != tuple(shape) or t.dtype not in dtypes:
+        raise ValueError(f"{name}: need {tuple(shape)} of {dtypes}, got {tuple(t.shape)} {t.dtype}")
+    if not (t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{name}: need a contiguous CUDA tensor")
+
+
+def _xdtype(x):
+    import torch
+    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"need [T, d] fp32 or bf16 rows, got {tuple(x.shape)} {x.dtype}")
+    return EAT_BF16 if x.dtype == torch.bfloat16 else EAT_F32
+
+
+def _norm_args(x, gamma, residual):
+    import torch
+    code = _xdtype(x)
+    _take("x", x, x.shape, x.dtype)
+    _take("gamma", gamma, x.shape[1:], torch.float32)
+    if residual is None:
+        return code, x
+    _take("residual", residual, x.shape, x.dtype)
+    return code, torch.empty_like(x)
+
+
+def rms_norm(x, gamma, eps=1e-6, residual=None):
+    """(y, h): h = x + residual, y = RMS norm of h times gamma, both in x's type (x, residual [T, d]
+    fp32 or bf16; gamma [d] fp32).  Without a residual h is x itself."""
+    import torch
+    code, h = _norm_args(x, gamma, residual)
+    y = torch.empty_like(x)
+    eat_rms_norm(x, residual, x.shape[0], x.shape[1], code, gamma, eps, h, y, code)
+    return y, h
+
+
+def rms_norm_fp8(x, gamma, eps=1e-6, residual=None):
+    """(q, scale, h): rms_norm with y as torch.float8_e4m3fn rows q and their fp32 scales [T]."""
+    import torch
+    code, h = _norm_args(x, gamma, residual)
+    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    eat_rms_norm(x, residual, x.shape[0], x.shape[1], code, gamma, eps, h, q, EAT_FP8_E4M3, scale)
+    return q, scale, h
+
+
+def rms_norm_grad(h, gamma, eps, dy, dres=None):
+    """(dx, dgamma) of rms_norm at its stored sum h: dx is the gradient of x and of the residual,
+    dres the gradient that reaches h from the residual stream."""
+    import torch
+    code = _xdtype(h)
+    T, d = h.shape
+    _take("h", h, h.shape, h.dtype)
+    _take("gamma", gamma, (d,), torch.float32)
+    _take("dy", dy, h.shape, h.dtype)
+    if dres is not None:
+        _take("dres", dres, h.shape, h.dtype)
+    dx = torch.empty_like(h)
+    dgamma = torch.empty(d, dtype=torch.float32, device=h.device)
+    work = torch.empty(eat_rms_norm_grad_workspace(T, d), dtype=torch.uint8, device=h.device)
+    eat_rms_norm_grad(h, T, d, code, gamma, eps, dy, dres, dx, dgamma, work)
+    return dx, dgamma
+
+
+def balance_loss(logits, idx, mask=None):
+    """(loss [1], counts [E] int32, n_tokens [1] int32) of router logits [T, E] fp32 and the selected
+    experts idx [T, K] int32 of EatLayer.route or forward; mask [T] bool: tokens that count."""
+    import torch
+    _take("logits", logits, logits.shape[:2], torch.float32)
+    T, E = logits.shape
+    _take("idx", idx, (T, idx.shape[-1]), torch.int32)
+    if mask is not None:
+        _take("mask", mask, (T,), torch.bool, torch.uint8)
+    dev = logits.device
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    counts = torch.empty(E, dtype=torch.int32, device=dev)
+    n = torch.empty(1, dtype=torch.int32, device=dev)
+    work = torch.empty(eat_balance_workspace(T, E), dtype=torch.uint8, device=dev)
+    eat_balance_loss(logits, T, E, idx.shape[1], idx, mask, loss, counts, n, work)
+    return loss, counts, n
+
+
+def balance_grad(logits, counts, n_tokens, g, mask=None):
+    """Gradient of balance_loss to the logits, times g (fp32 [1] on the device)."""
+    import torch
+    _take("logits", logits, logits.shape[:2], torch.float32)
+    T, E = logits.shape
+    _take("counts", counts, (E,), torch.int32)
+    _take("n_tokens", n_tokens, (1,), torch.int32)
+    _take("g", g, (1,), torch.float32)
+    if mask is not None:
+        _take("mask", mask, (T,), torch.bool, torch.uint8)
+    dlogits = torch.empty_like(logits)
+    eat_balance_grad(logits, T, E, mask, counts, n_tokens, g, dlogits)
+    return dlogits
+
+
+class EatHead:
+    """Owns an eat_head for one vocabulary matrix w [vocab, d] (bf16, or torch.float8_e4m3fn with
+    w_scale [vocab] fp32), kept referenced; grad=True (bf16) for nll_grad."""
+
+    def __init__(self, w, max_tokens, w_scale=None, grad=False):
+        import torch
+        _take("w", w, w.shape[:2], torch.bfloat16, torch.float8_e4m3fn)
+        self.V, self.d = w.shape
+        self.dtype = w.dtype
+        if w.dtype == torch.float8_e4m3fn:
+            _take("w_scale", w_scale, (self.V,), torch.float32)
+        self._keep = [w, w_scale]
+        code = EAT_BF16 if w.dtype == torch.bfloat16 else EAT_FP8_E4M3
+        self.h = eat_head_create(eat_head_desc(self.d, self.V, max_tokens, code, int(grad), _ptr(w),
+                                               _ptr(w_scale)))
+
+    def _call(self, x, target):
+        import torch
+        T = target.shape[0]
+        _take("x", x, (T, self.d), self.dtype)
+        _take("target", target, (T,), torch.int32)
+        return T, torch.empty(T, dtype=torch.float32, device=x.device), \
+            torch.empty(T, dtype=torch.float32, device=x.device)
+
+    def nll(self, x, target, x_scale=None):
+        """(nll, lse) [T] fp32 of hidden states x [T, d] and targets [T] int32 (negative: ignored);
+        x_scale [T] fp32 with an e4m3 head (rms_norm_fp8 makes both)."""
+        import torch
+        T, nll, lse = self._call(x, target)
+        if self.dtype == torch.float8_e4m3fn:
+            _take("x_scale", x_scale, (T,), torch.float32)
+        eat_head_nll(self.h, x, x_scale, T, target, nll, lse)
+        return nll, lse
+
+    def nll_grad(self, x, target, g):
+        """(nll, lse, dx, dw): the loss, and the gradients of sum(g * nll) to x and w (g [T] fp32)."""
+        import torch
+        T, nll, lse = self._call(x, target)
+        _take("g", g, (T,), torch.float32)
+        dx = torch.empty_like(x)
+        dw = torch.empty_like(self._keep[0])
+        eat_head_nll_grad(self.h, x, T, target, g, nll, lse, dx, dw)
+        return nll, lse, dx, dw
+
+    def close(self):
+        if getattr(self, "h", None):
+            eat_head_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # ------------------------------------------------------------------------------------------------
