@@ -1,221 +1,345 @@
-// Vocabulary head: softmax cross entropy of hidden states against a vocabulary matrix, in pieces
-// of the vocabulary, without holding the logits; and its gradient.
+// Vocabulary head: softmax cross entropy of hidden states against a vocabulary matrix, in pieces,
+// without holding the logits; and its gradient.  Host side and the kernels around the products of
+// head_tc.cu.
 //   l_tv = s_t s_v <x_t, w_v>;  r = log sum_{v != y} exp l_v - l_y;  nll = log(1 + exp r)
-//   lse = l_y + nll;  P_tv = g_t (exp(l_tv - lse_t) - [v = y_t]);  dx = P w;  dw = P^T x
-#include "eat_internal.cuh"
+//   (the target is left out of the sum, so that nll keeps its relative accuracy when it is small);
+//   lse = l_y + nll;  P_tv = g_t (exp(l_tv - lse_t) - [v = y_t]);  dx = P w;  dw = P^T x.
+// The gradient takes the counted tokens (target in [0, vocab)) in pieces of at most kPieceBytes of
+// exponentials, and each product once:
+//   E_tv = exp(l_tv - l_ty), stored as bf16 while its sum over v != y, Z', is taken in fp32;
+//   then E_ty := -q with q = bf16(Z'), f_t = g_t / (1 + Z') (Z' / q), and
+//   dx_t = f_t sum_v E_tv w_v (f in fp32),  dw = E^T X', X'_t = bf16(f_t x_t).
+// P enters as f E: its target entry is exact in dx, as f_t q = g_t (1 - p_y); the other entries carry
+// one bf16 rounding of E and that of q.  A second pass that computed the logits again, now with lse at
+// hand, would spend 8 instead of 6 T V d flops and round P once as well.
+#include "head_tc.cuh"
 
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <cstring>
 #include <new>
 #include <string>
 
 struct eat_head {
   eat_head_desc desc;
+  bool w8 = false;
+  int num_sms = 0, max_pairs = 1;
   char* mem = nullptr;
-  float2* part = nullptr;          // [vocabulary tiles][max_tokens] {max, sum of exp}
-  float* ly = nullptr;             // [max_tokens] target logits
-  float* lse = nullptr;            // [max_tokens]
-  __nv_bfloat16* p = nullptr;      // [max_tokens, piece] P of a piece of the vocabulary
-  float* dx = nullptr;             // [max_tokens, d] dx over the pieces so far
-  int piece = 0;
+  eat::HeadStatus st{};
+  unsigned int* mirror_host = nullptr;
+  bool failed = false;
+  CUtensorMap w128, w64, w16, x64, e64;
+  float2* part = nullptr;      // small calls [ctas][n]; larger ones [128-row pieces][T]
+  float* ly = nullptr;         // [max_tokens] base-2 target logits
+  // gradient
+  int cap = 0, ld = 0;         // tokens of a piece, columns of E
+  int32_t* n_counted = nullptr;
+  int32_t* rows = nullptr;     // [tokens] counted tokens, ascending
+  int32_t* ytok = nullptr;     // [tokens] their targets
+  float* f = nullptr;          // [tokens]
+  uint32_t* row_max = nullptr;
+  int32_t* far = nullptr;
+  __nv_bfloat16* xc = nullptr;  // [tokens, d] their hidden states, then X'
+  __nv_bfloat16* e = nullptr;   // [cap, ld]
+  float* dw_sum = nullptr;
 };
 
 namespace eat {
 
 namespace {
 
-constexpr int kTile = 64, kStep = 16;
-constexpr int kPieceBytes = 64 << 20;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr size_t kPieceBytes = 512u << 20;
 
-__device__ __forceinline__ float val(const __nv_bfloat16* p, size_t i) {
-  return __bfloat162float(p[i]);
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
-__device__ __forceinline__ float val(const __nv_fp8_e4m3* p, size_t i) { return (float)p[i]; }
 
-// acc = 64 x 64 tile of A B^T at (m0, n0): A(m, k) = a[m am + k ak] for m < M, B(n, k) = b[n bn + k
-// bk] for n < N, summed over k < K; thread (tx, ty) holds rows ty + 16 i and columns tx + 16 j.
-template <typename TA, typename TB>
-__device__ void tile_product(const TA* a, size_t am, size_t ak, int M, int m0, const TB* b,
-                             size_t bn, size_t bk, int N, int n0, int K, float (&acc)[4][4]) {
-  __shared__ float sa[kStep][kTile + 1], sb[kStep][kTile + 1];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-  for (int k0 = 0; k0 < K; k0 += kStep) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kTile * kStep; i += 256) {
-      const int ka = ak == 1 ? i % kStep : i / kTile, ma = ak == 1 ? i / kStep : i % kTile;
-      const int kb = bk == 1 ? i % kStep : i / kTile, nb = bk == 1 ? i / kStep : i % kTile;
-      sa[ka][ma] = m0 + ma < M && k0 + ka < K ? val(a, (m0 + ma) * am + (k0 + ka) * ak) : 0.f;
-      sb[kb][nb] = n0 + nb < N && k0 + kb < K ? val(b, (n0 + nb) * bn + (k0 + kb) * bk) : 0.f;
+// 16 bytes of a row as floats: 8 bf16 or 16 e4m3
+template <bool W8>
+struct Vec {
+  static constexpr int kN = W8 ? 16 : 8;
+  float v[kN];
+  __device__ explicit Vec(uint4 u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (W8) {
+        __nv_fp8x4_e4m3 q;
+        q.__x = w[i];
+        const float4 f = (float4)q;
+        v[4 * i] = f.x;
+        v[4 * i + 1] = f.y;
+        v[4 * i + 2] = f.z;
+        v[4 * i + 3] = f.w;
+      } else {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
     }
-    __syncthreads();
+  }
+};
+template <bool W8>
+__device__ __forceinline__ float dot16(uint4 a, uint4 b, float s) {
+  const Vec<W8> x(a), w(b);
 #pragma unroll
-    for (int k = 0; k < kStep; ++k)
+  for (int i = 0; i < Vec<W8>::kN; ++i) s = fmaf(x.v[i], w.v[i], s);
+  return s;
+}
+
+// nll and lse of a token from the base-2 target logit and the sum of the others' exp2 relative to m
+__device__ __forceinline__ float2 token_loss(float m, float s, float ly) {
+  const float r = (m - ly + log2f(s)) * kLn2;
+  float a = fmaxf(r, 0.f) + log1pf(expf(-fabsf(r)));
+  if (isnan(r)) a = r;
+  return make_float2(a, fmaf(ly, kLn2, a));
+}
+
+// Joins the CTAs' partial sums of a small call; a block per token.  The target's logit is a sum of
+// its own in fp32.
+template <bool W8>
+__global__ void __launch_bounds__(128)
+small_join_kernel(const float2* __restrict__ part, int ctas, int n, const uint4* __restrict__ x,
+                  const uint4* __restrict__ w, int row_vecs, const float* __restrict__ xs,
+                  const float* __restrict__ ws, int V, const int32_t* __restrict__ target,
+                  float* __restrict__ nll, float* __restrict__ lse,
+                  const unsigned int* __restrict__ err) {
+  __shared__ float s_m[4], s_s[4], s_d[4];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int t = blockIdx.x, y = target[t];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (y < 0 || y >= V) {
+    if (threadIdx.x == 0) {
+      nll[t] = y < 0 ? 0.f : NAN;
+      if (lse) lse[t] = y < 0 ? 0.f : NAN;
+    }
+    return;
+  }
+  float d = 0.f;
+  for (int i = threadIdx.x; i < row_vecs; i += 128)
+    d = dot16<W8>(x[(size_t)t * row_vecs + i], w[(size_t)y * row_vecs + i], d);
+  float m = kHeadLow, s = 0.f;
+  for (int i = threadIdx.x; i < ctas; i += 128) {
+    const float2 q = part[(size_t)i * n + t];
+    const float k = fmaxf(m, q.x);
+    s = s * exp2f(m - k) + q.y * exp2f(q.x - k);
+    m = k;
+  }
+  d = warp_sum(d);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += sa[k][ty + 16 * i] * sb[k][tx + 16 * j];
+  for (int o = 16; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
+    const float k = fmaxf(m, m2);
+    s = s * exp2f(m - k) + s2 * exp2f(m2 - k);
+    m = k;
+  }
+  if (lane == 0) {
+    s_m[warp] = m;
+    s_s[warp] = s;
+    s_d[warp] = d;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 4; ++i) {
+      const float k = fmaxf(m, s_m[i]);
+      s = s * exp2f(m - k) + s_s[i] * exp2f(s_m[i] - k);
+      m = k;
+      d += s_d[i];
+    }
+    if (W8) d *= xs[t] * ws[y];
+    float2 r = token_loss(m, s, d * kLog2e);
+    if (*err) r = make_float2(NAN, NAN);
+    nll[t] = r.x;
+    if (lse) lse[t] = r.y;
   }
 }
 
-// part[v tile][t]: maximum and sum of exp over the tile's rows other than the target
-template <typename E>
-__global__ void __launch_bounds__(256)
-head_part_kernel(const E* __restrict__ x, const float* __restrict__ xs, const E* __restrict__ w,
-                 const float* __restrict__ ws, int T, int V, int d,
-                 const int32_t* __restrict__ target, float2* __restrict__ part,
-                 float* __restrict__ ly) {
+// The same for larger calls: 32 tokens per block, its warps over the pieces of the vocabulary.
+constexpr int kJoinWarps = 16;
+__global__ void __launch_bounds__(32 * kJoinWarps)
+join_kernel(const float2* __restrict__ part, int pieces, const float* __restrict__ ly, int T,
+            int V, const int32_t* __restrict__ target, float* __restrict__ nll,
+            float* __restrict__ lse, const unsigned int* __restrict__ err) {
+  __shared__ float2 s_p[kJoinWarps][32];
   pdl_wait();
   pdl_launch_dependents();
-  const int v0 = blockIdx.x * kTile, t0 = blockIdx.y * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4];
-  tile_product(x, d, 1, T, t0, w, d, 1, V, v0, d, acc);
-  for (int i = 0; i < 4; ++i) {
-    const int t = t0 + ty + 16 * i;
-    const int y = t < T ? target[t] : -1;
-    const float st = xs && t < T ? xs[t] : 1.f;
-    float m = -INFINITY, s = 0.f;
-    for (int j = 0; j < 4; ++j) {
-      const int v = v0 + tx + 16 * j;
-      if (v < V) acc[i][j] *= st * (ws ? ws[v] : 1.f);
-      if (v < V && v == y) ly[t] = acc[i][j];
-      if (v >= V || v == y) acc[i][j] = -INFINITY;
-      m = fmaxf(m, acc[i][j]);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int t = blockIdx.x * 32 + lane;
+  float m = kHeadLow, s = 0.f;
+  if (t < T) {
+#pragma unroll 4
+    for (int i = warp; i < pieces; i += kJoinWarps) {
+      const float2 q = part[(size_t)i * T + t];
+      const float k = fmaxf(m, q.x);
+      s = s * exp2f(m - k) + q.y * exp2f(q.x - k);
+      m = k;
     }
-    for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    for (int j = 0; j < 4; ++j) s += acc[i][j] == -INFINITY ? 0.f : expf(acc[i][j] - m);
-    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (tx == 0 && t < T) part[(size_t)blockIdx.x * T + t] = make_float2(m, s);
   }
-}
-
-__global__ void __launch_bounds__(256)
-head_join_kernel(const float2* __restrict__ part, int tiles, const float* __restrict__ ly, int T,
-                 int V, const int32_t* __restrict__ target, float* __restrict__ nll,
-                 float* __restrict__ lse, float* __restrict__ lse_opt) {
-  pdl_wait();
-  pdl_launch_dependents();
-  const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= T) return;
-  float m = -INFINITY, s = 0.f;
-  for (int i = 0; i < tiles; ++i) {
-    const float2 q = part[(size_t)i * T + t];
-    const float n = fmaxf(m, q.x);
-    if (!(n == -INFINITY)) s = s * expf(m - n) + q.y * expf(q.x - n);
-    m = n;
+  s_p[warp][lane] = make_float2(m, s);
+  __syncthreads();
+  if (warp != 0 || t >= T) return;
+  for (int i = 1; i < kJoinWarps; ++i) {
+    const float2 q = s_p[i][lane];
+    const float k = fmaxf(m, q.x);
+    s = s * exp2f(m - k) + q.y * exp2f(q.x - k);
+    m = k;
   }
   const int y = target[t];
-  float a = 0.f, b = 0.f;
-  if (y >= V) {
-    a = b = NAN;
-  } else if (y >= 0) {
-    const float r = m + logf(s) - ly[t];
-    a = fmaxf(r, 0.f) + log1pf(expf(-fabsf(r)));
-    if (isnan(r)) a = r;
-    b = ly[t] + a;
-  }
-  nll[t] = a;
-  lse[t] = b;
-  if (lse_opt) lse_opt[t] = b;
+  float2 r = make_float2(0.f, 0.f);
+  if (y >= V || *err) r = make_float2(NAN, NAN);
+  else if (y >= 0) r = token_loss(m, s, ly[t]);
+  if (y < 0) r = make_float2(0.f, 0.f);
+  nll[t] = r.x;
+  if (lse) lse[t] = r.y;
 }
 
-// P of the vocabulary rows [vp, vp + n) (columns of p), as bf16
-__global__ void __launch_bounds__(256)
-head_p_kernel(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ w, int T,
-              int V, int d, int vp, int n, const int32_t* __restrict__ target,
-              const float* __restrict__ lse, const float* __restrict__ g,
-              __nv_bfloat16* __restrict__ p, int ld) {
+// ------------------------------------------------------------------------------- gradient
+// The counted tokens in order, by one block; the launch's per-call words are cleared.
+__global__ void __launch_bounds__(1024)
+count_kernel(const int32_t* __restrict__ target, int T, int V, int tiles,
+             int32_t* __restrict__ rows, int32_t* __restrict__ ytok, int32_t* __restrict__ n_counted,
+             int32_t* __restrict__ far) {
+  __shared__ int s_w[32];
   pdl_wait();
   pdl_launch_dependents();
-  const int c0 = blockIdx.x * kTile, t0 = blockIdx.y * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4];
-  tile_product(x, d, 1, T, t0, w + (size_t)vp * d, d, 1, n, c0, d, acc);
-  for (int i = 0; i < 4; ++i) {
-    const int t = t0 + ty + 16 * i;
-    if (t >= T) continue;
-    const int y = target[t];
-    for (int j = 0; j < 4; ++j) {
-      const int c = c0 + tx + 16 * j;
-      if (c >= n) continue;
-      float v = 0.f;
-      if (y >= 0 && y < V) v = g[t] * (expf(acc[i][j] - lse[t]) - (vp + c == y ? 1.f : 0.f));
-      p[(size_t)t * ld + c] = __float2bfloat16_rn(v);
-    }
-  }
-}
-
-// dx (+)= P w[vp ...]; the last piece writes the rounded result
-__global__ void __launch_bounds__(256)
-head_dx_kernel(const __nv_bfloat16* __restrict__ p, int ld, int n,
-               const __nv_bfloat16* __restrict__ w, int T, int d, int first, int last,
-               float* __restrict__ sum, __nv_bfloat16* __restrict__ dx) {
-  pdl_wait();
-  pdl_launch_dependents();
-  const int c0 = blockIdx.x * kTile, t0 = blockIdx.y * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4];
-  tile_product(p, ld, 1, T, t0, w, 1, d, d, c0, n, acc);
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int t = t0 + ty + 16 * i, c = c0 + tx + 16 * j;
-      if (t >= T || c >= d) continue;
-      const size_t o = (size_t)t * d + c;
-      const float v = acc[i][j] + (first ? 0.f : sum[o]);
-      if (last) dx[o] = __float2bfloat16_rn(v);
-      else sum[o] = v;
-    }
-}
-
-// The hidden states with zero rows for the tokens that carry no loss
-struct Rows {
-  const __nv_bfloat16* x;
-  const int32_t* target;
-  int V, d;
-};
-__device__ __forceinline__ float val(const Rows r, size_t i) {
-  const int y = r.target[i / r.d];
-  return y >= 0 && y < r.V ? __bfloat162float(r.x[i]) : 0.f;
-}
-
-__global__ void __launch_bounds__(256)
-head_dw_kernel(const __nv_bfloat16* __restrict__ p, int ld, int n,
-               const __nv_bfloat16* __restrict__ x, const int32_t* __restrict__ target, int T,
-               int V, int d, __nv_bfloat16* __restrict__ dw) {
-  pdl_wait();
-  pdl_launch_dependents();
-  const int c0 = blockIdx.x * kTile, v0 = blockIdx.y * kTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4];
-  __shared__ float sa[kStep][kTile + 1], sb[kStep][kTile + 1];
-  const Rows r{x, target, V, d};
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-  for (int k0 = 0; k0 < T; k0 += kStep) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < tiles; i += 1024) far[i] = 0;
+  int base = 0;
+  for (int t0 = 0; t0 < T; t0 += 1024) {
+    const int t = t0 + threadIdx.x;
+    const int y = t < T ? target[t] : -1;
+    const bool on = y >= 0 && y < V;
+    const unsigned b = __ballot_sync(0xffffffffu, on);
+    if (lane == 0) s_w[warp] = __popc(b);
     __syncthreads();
-    for (int i = threadIdx.x; i < kTile * kStep; i += 256) {
-      const int k = i / kTile, m = i % kTile;
-      sa[k][m] = v0 + m < n && k0 + k < T ? val(p, (size_t)(k0 + k) * ld + v0 + m) : 0.f;
-      sb[k][m] = c0 + m < d && k0 + k < T ? val(r, (size_t)(k0 + k) * d + c0 + m) : 0.f;
+    int before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      before += i < warp ? s_w[i] : 0;
+      all += s_w[i];
     }
+    if (on) {
+      const int at = base + before + __popc(b & ((1u << lane) - 1u));
+      rows[at] = t;
+      ytok[at] = y;
+    }
+    base += all;
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kStep; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += sa[k][ty + 16 * i] * sb[k][tx + 16 * j];
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int v = v0 + ty + 16 * i, c = c0 + tx + 16 * j;
-      if (v < n && c < d) dw[(size_t)v * d + c] = __float2bfloat16_rn(acc[i][j]);
-    }
+  if (threadIdx.x == 0) *n_counted = base;
 }
 
+// A warp per row i: the i-th counted token's hidden state into xc (zeros up to the end of the last
+// tile) and its base-2 target logit; and for token i, if it does not count, its outputs.
+__global__ void __launch_bounds__(256)
+gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_vecs, int T, int V,
+              const int32_t* __restrict__ target, const int32_t* __restrict__ rows,
+              const int32_t* __restrict__ n_counted, uint4* __restrict__ xc,
+              float* __restrict__ ly, uint32_t* __restrict__ row_max, uint4* __restrict__ dx,
+              float* __restrict__ nll, float* __restrict__ lse) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, i = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int n = *n_counted;
+  if (i < n) {
+    const int t = rows[i];
+    const uint4* a = x + (size_t)t * row_vecs;
+    const uint4* b = w + (size_t)target[t] * row_vecs;
+    float d = 0.f;
+#pragma unroll 4
+    for (int c = lane; c < row_vecs; c += 32) {
+      const uint4 v = a[c];
+      xc[(size_t)i * row_vecs + c] = v;
+      d = dot16<false>(v, b[c], d);
+    }
+    d = warp_sum(d);
+    if (lane == 0) {
+      ly[i] = d * kLog2e;
+      row_max[i] = 0;
+    }
+  } else if (i < (n + kHeadTile - 1) / kHeadTile * kHeadTile) {
+    for (int c = lane; c < row_vecs; c += 32) xc[(size_t)i * row_vecs + c] = make_uint4(0, 0, 0, 0);
+  }
+  if (i < T) {
+    const int y = target[i];
+    if (y < 0 || y >= V) {
+      for (int c = lane; c < row_vecs; c += 32) dx[(size_t)i * row_vecs + c] = make_uint4(0, 0, 0, 0);
+      if (lane == 0) {
+        nll[i] = y < 0 ? 0.f : NAN;
+        if (lse) lse[i] = y < 0 ? 0.f : NAN;
+      }
+    }
+  }
+}
+
+// After a piece's exponentials, 32 counted tokens per block: their sums, losses and factors; the
+// target entries of E; X' in place of x.
+__global__ void __launch_bounds__(256)
+finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
+              const int32_t* __restrict__ n_counted, const int32_t* __restrict__ rows,
+              const int32_t* __restrict__ ytok, const float* __restrict__ ly,
+              const uint32_t* __restrict__ row_max, const float* __restrict__ g,
+              __nv_bfloat16* __restrict__ e, int ld, float* __restrict__ f,
+              uint4* __restrict__ xc, int row_vecs, float* __restrict__ nll,
+              float* __restrict__ lse, const unsigned int* __restrict__ err) {
+  __shared__ float s_p[8][32];
+  __shared__ float s_f[32];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r0 = blockIdx.x * 32, n = min(cap, *n_counted - t0);
+  if (r0 >= n) return;
+  const int r = r0 + lane;  // row of the piece
+  float s = 0.f;
+  if (r < n) {
+#pragma unroll 4
+    for (int i = warp; i < pieces; i += 8) s += part[(size_t)i * cap + r];
+  }
+  s_p[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && r < n) {
+    for (int i = 1; i < 8; ++i) s += s_p[i][lane];
+    const int t = rows[t0 + r];
+    const float l2 = ly[t0 + r], ref = head_ref(l2, row_max[t0 + r]);
+    float2 a = token_loss(ref, s, l2);
+    const __nv_bfloat16 q = __float2bfloat16_rn(s);
+    const float qf = __bfloat162float(q);
+    float k = g[t] / (s + exp2f(l2 - ref));
+    if (qf > 0.f) k *= s / qf;
+    if (*err) {
+      a = make_float2(NAN, NAN);
+      k = NAN;
+    }
+    e[(size_t)r * ld + ytok[t0 + r]] = __float2bfloat16_rn(-qf);
+    f[t0 + r] = k;
+    s_f[lane] = k;
+    nll[t] = a.x;
+    if (lse) lse[t] = a.y;
+  }
+  __syncthreads();
+  for (int j = warp; j < min(32, n - r0); j += 8) {
+    const float k = s_f[j];
+    uint4* row = xc + (size_t)(t0 + r0 + j) * row_vecs;
+#pragma unroll 4
+    for (int c = lane; c < row_vecs; c += 32) {
+      const Vec<false> v(row[c]);
+      uint32_t b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(v.v[2 * i] * k, v.v[2 * i + 1] * k);
+        b[i] = *(const uint32_t*)&p;
+      }
+      row[c] = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+  }
+}
+
+// -------------------------------------------------------------------------------- host side
 eat_status fail(eat_status s, const std::string& msg) {
   set_thread_error(msg.c_str());
   return s;
@@ -223,14 +347,15 @@ eat_status fail(eat_status s, const std::string& msg) {
 
 void free_head(eat_head* h) {
   if (!h) return;
+  if (h->mirror_host) cudaFreeHost(h->mirror_host);
   if (h->mem) cudaFree(h->mem);
   delete h;
 }
 
-int tiles(int n) { return (n + kTile - 1) / kTile; }
+int up(int n, int m) { return (n + m - 1) / m * m; }
 
 eat_status check_call(const char* fn, eat_head* h, const void* x, int32_t T,
-                      const int32_t* target, const float* nll) {
+                      const int32_t* target, const float* nll, const float* lse) {
   const std::string f(fn);
   if (!h) return fail(EAT_ERR_INVALID_ARG, f + ": null handle");
   if (!x || !target || !nll)
@@ -238,29 +363,95 @@ eat_status check_call(const char* fn, eat_head* h, const void* x, int32_t T,
   if (T < 1 || T > h->desc.max_tokens)
     return fail(EAT_ERR_INVALID_ARG, f + ": T outside [1, max_tokens]");
   if ((uintptr_t)x & 15) return fail(EAT_ERR_INVALID_ARG, f + ": x must be 16-byte aligned");
-  if (((uintptr_t)target | (uintptr_t)nll) & 3)
+  if (((uintptr_t)target | (uintptr_t)nll | (uintptr_t)lse) & 3)
     return fail(EAT_ERR_INVALID_ARG, f + ": misaligned pointer");
+  if (!h->failed && *(volatile unsigned int*)h->mirror_host) h->failed = true;
+  if (h->failed)
+    return fail(EAT_ERR_STATE, f + ": a kernel of an earlier call gave up on a bounded wait; "
+                                   "eat_head_reset clears the state");
   return EAT_OK;
 }
 
-cudaError_t run_nll(eat_head* h, const void* x, const float* xs, int T, const int32_t* target,
-                    float* nll, float* lse_opt, cudaStream_t st) {
-  const int V = h->desc.vocab, d = h->desc.d_model;
-  const dim3 grid(tiles(V), tiles(T));
-  cudaError_t e;
-  if (h->desc.dtype == EAT_BF16)
-    e = launch_pdl(head_part_kernel<__nv_bfloat16>, grid, dim3(256), 0, st,
-                   (const __nv_bfloat16*)x, (const float*)nullptr,
-                   (const __nv_bfloat16*)h->desc.w, (const float*)nullptr, T, V, d, target,
-                   h->part, h->ly);
-  else
-    e = launch_pdl(head_part_kernel<__nv_fp8_e4m3>, grid, dim3(256), 0, st,
-                   (const __nv_fp8_e4m3*)x, xs, (const __nv_fp8_e4m3*)h->desc.w, h->desc.w_scale,
-                   T, V, d, target, h->part, h->ly);
+cudaError_t run_small(eat_head* h, const void* x, const float* xs, int T, const int32_t* target,
+                      float* nll, float* lse, cudaStream_t st) {
+  const int V = h->desc.vocab, d = h->desc.d_model, n = head_small_n(T);
+  CUtensorMap mx;
+  if (!head_encode(&mx, h->w8, x, T, d, n)) return cudaErrorInvalidValue;
+  const int ctas = head_small_ctas(h->num_sms, V), kb = h->w8 ? 128 : 64;
+  const HeadSmallArgs a{T, V, (d + kb - 1) / kb, target, xs, h->desc.w_scale, h->part, h->st};
+  const cudaError_t e = head_launch_small(h->w8, h->w128, h->w16, mx, a, ctas, st);
   if (e != cudaSuccess) return e;
-  return launch_pdl(head_join_kernel, dim3((T + 255) / 256), dim3(256), 0, st,
-                    (const float2*)h->part, tiles(V), (const float*)h->ly, T, V, target, nll,
-                    h->lse, lse_opt);
+  return launch_pdl(h->w8 ? small_join_kernel<true> : small_join_kernel<false>, dim3(T), dim3(128),
+                    0, st, (const float2*)h->part, ctas, n, (const uint4*)x,
+                    (const uint4*)h->desc.w, d * (h->w8 ? 1 : 2) / 16, xs, h->desc.w_scale, V,
+                    target, nll, lse, (const unsigned int*)h->st.err);
+}
+
+cudaError_t run_pair(eat_head* h, const void* x, const float* xs, int T, const int32_t* target,
+                     float* nll, float* lse, cudaStream_t st) {
+  const int V = h->desc.vocab, d = h->desc.d_model, kb = h->w8 ? 128 : 64;
+  CUtensorMap mx;
+  if (!head_encode(&mx, h->w8, x, T, d, 64)) return cudaErrorInvalidValue;
+  HeadPairArgs a{};
+  a.T = T;
+  a.V = V;
+  a.kblocks = (d + kb - 1) / kb;
+  a.target = target;
+  a.xs = xs;
+  a.ws = h->desc.w_scale;
+  a.part2 = h->part;
+  a.ly = h->ly;
+  a.st = h->st;
+  const cudaError_t e = head_launch_pair(h->w8, false, mx, h->w64, a, h->max_pairs, st);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(join_kernel, dim3((T + 31) / 32), dim3(32 * kJoinWarps), 0, st,
+                    (const float2*)h->part, up(V, kHeadTile) / 128, (const float*)h->ly, T, V,
+                    target, nll, lse, (const unsigned int*)h->st.err);
+}
+
+cudaError_t run_grad(eat_head* h, const void* x, int T, const int32_t* target, const float* g,
+                     float* nll, float* lse, void* dx, void* dw, cudaStream_t st) {
+  const int V = h->desc.vocab, d = h->desc.d_model, row_vecs = d / 8;
+  const int t_pad = up(T, kHeadTile);
+  cudaError_t e = launch_pdl(count_kernel, dim3(1), dim3(1024), 0, st, target, T, V,
+                             t_pad / kHeadTile, h->rows, h->ytok, h->n_counted, h->far);
+  if (e == cudaSuccess)
+    e = launch_pdl(gather_kernel, dim3(t_pad / 8), dim3(256), 0, st, (const uint4*)x,
+                   (const uint4*)h->desc.w, row_vecs, T, V, target, (const int32_t*)h->rows,
+                   (const int32_t*)h->n_counted, (uint4*)h->xc, h->ly, h->row_max, (uint4*)dx, nll,
+                   lse);
+  for (int t0 = 0; t0 < T && e == cudaSuccess; t0 += h->cap) {
+    const int cap = std::min(h->cap, t_pad - t0);
+    HeadPairArgs a{};
+    a.V = V;
+    a.kblocks = d / 64;
+    a.target = h->ytok;
+    a.n_counted = h->n_counted;
+    a.t0 = t0;
+    a.cap = cap;
+    a.ld = h->ld;
+    a.ref = h->ly;
+    a.row_max = h->row_max;
+    a.far = h->far;
+    a.part = (float*)h->part;
+    a.e = h->e;
+    a.st = h->st;
+    e = head_launch_pair(false, true, h->x64, h->w64, a, h->max_pairs, st);
+    if (e != cudaSuccess) break;
+    a.redo = 1;
+    e = head_launch_pair(false, true, h->x64, h->w64, a, h->max_pairs, st);
+    if (e != cudaSuccess) break;
+    e = launch_pdl(finish_kernel, dim3(cap / 32), dim3(256), 0, st, (const float*)h->part,
+                   up(V, kHeadTile) / 128, t0, cap, (const int32_t*)h->n_counted,
+                   (const int32_t*)h->rows, (const int32_t*)h->ytok, (const float*)h->ly,
+                   (const uint32_t*)h->row_max, g, h->e, h->ld, h->f, (uint4*)h->xc, row_vecs, nll,
+                   lse, (const unsigned int*)h->st.err);
+    if (e != cudaSuccess) break;
+    const HeadGradArgs b{V,      d,       h->n_counted, t0, cap, h->f, h->rows, (__nv_bfloat16*)dx,
+                         (__nv_bfloat16*)dw, h->dw_sum, h->st};
+    e = head_launch_grad(h->e64, h->w64, h->x64, b, h->max_pairs, st);
+  }
+  return e;
 }
 
 }  // namespace
@@ -289,30 +480,88 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
     return fail(EAT_ERR_INVALID_ARG, "an e4m3 head needs w_scale, 4-byte aligned");
   if (D.with_grad && D.dtype != EAT_BF16)
     return fail(EAT_ERR_UNSUPPORTED, "gradients need a BF16 head");
+
+  int dev = 0;
+  cudaDeviceProp prop;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaGetDeviceProperties(&prop, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return fail(EAT_ERR_CUDA, "no CUDA device");
+  }
+  if (prop.major != 10 || prop.minor != 3)
+    return fail(EAT_ERR_UNSUPPORTED, "the tensor-core kernels are built for sm_103a (GB300)");
   eat_head* h = new (std::nothrow) eat_head();
   if (!h) return fail(EAT_ERR_OOM, "host allocation failed");
   h->desc = D;
-  const size_t T = (size_t)D.max_tokens;
-  h->piece = (int)std::min<size_t>((size_t)tiles(D.vocab) * kTile,
-                                   std::max<size_t>(kPieceBytes / 2 / T / kTile * kTile, kTile));
-  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-  const size_t n_part = up(sizeof(float2) * tiles(D.vocab) * T), n_t = up(4 * T);
-  const size_t n_p = D.with_grad ? up(2 * T * h->piece) : 0;
-  const size_t n_dx = D.with_grad ? up(4 * T * D.d_model) : 0;
-  const size_t total = n_part + 2 * n_t + n_p + n_dx;
-  const cudaError_t e = cudaMalloc((void**)&h->mem, total);
+  h->w8 = D.dtype == EAT_FP8_E4M3;
+  h->num_sms = prop.multiProcessorCount;
+  cudaError_t e = head_configure(h->num_sms, &h->max_pairs);
+  if (e != cudaSuccess) {
+    free_head(h);
+    return fail(EAT_ERR_CUDA, std::string("head kernels: ") + cudaGetErrorString(e));
+  }
+
+  const int V = D.vocab, t_pad = up(D.max_tokens, kHeadTile), pieces = up(V, kHeadTile) / 128;
+  const size_t tokens = (size_t)t_pad;
+  h->ld = up(V, kHeadTile);
+  h->cap = (int)std::min<size_t>(
+      tokens, std::max<size_t>(kPieceBytes / 2 / h->ld / kHeadTile * kHeadTile, kHeadTile));
+  const size_t small_part = sizeof(float2) * (size_t)head_small_ctas(h->num_sms, V) * kHeadSmallT;
+  const size_t large_part =
+      D.max_tokens > kHeadSmallT ? sizeof(float2) * (size_t)pieces * D.max_tokens : 0;
+  const size_t grad_part = D.with_grad ? sizeof(float) * (size_t)pieces * h->cap : 0;
+  struct Part { void** p; size_t bytes; };
+  Part parts[16];
+  int np = 0;
+  auto add = [&](void* p, size_t bytes) { parts[np++] = {(void**)p, bytes}; };
+  add(&h->st.err, 16);
+  add(&h->part, std::max({small_part, large_part, grad_part}));
+  add(&h->ly, 4 * tokens);
+  if (D.with_grad) {
+    add(&h->n_counted, 4);
+    add(&h->rows, 4 * tokens);
+    add(&h->ytok, 4 * tokens);
+    add(&h->f, 4 * tokens);
+    add(&h->row_max, 4 * tokens);
+    add(&h->far, 4 * (tokens / kHeadTile));
+    add(&h->xc, 2 * tokens * D.d_model);
+    add(&h->e, 2 * (size_t)h->cap * h->ld);
+    if (h->cap < t_pad) add(&h->dw_sum, 4 * (size_t)V * D.d_model);
+  }
+  size_t total = 0;
+  for (int i = 0; i < np; ++i) total += (parts[i].bytes + 255) / 256 * 256;
+  e = cudaMalloc((void**)&h->mem, total);
+  if (e == cudaSuccess) e = cudaHostAlloc((void**)&h->mirror_host, 16, cudaHostAllocMapped);
+  if (e == cudaSuccess) {
+    std::memset(h->mirror_host, 0, 16);
+    e = cudaHostGetDevicePointer((void**)&h->st.mirror, h->mirror_host, 0);
+  }
   if (e != cudaSuccess) {
     cudaGetLastError();  // a failed allocation leaves the context usable: clear its error
     free_head(h);
-    return fail(EAT_ERR_OOM, "cudaMalloc of " + std::to_string(total) + " bytes failed: " +
+    return fail(EAT_ERR_OOM, "head workspace of " + std::to_string(total) + " bytes: " +
                                  cudaGetErrorString(e));
   }
   char* at = h->mem;
-  h->part = (float2*)at;
-  h->ly = (float*)(at += n_part);
-  h->lse = (float*)(at += n_t);
-  h->p = (__nv_bfloat16*)(at += n_t);
-  h->dx = (float*)(at += n_p);
+  for (int i = 0; i < np; ++i) {
+    *parts[i].p = at;
+    at += (parts[i].bytes + 255) / 256 * 256;
+  }
+  e = cudaMemset(h->st.err, 0, 16);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) {
+    free_head(h);
+    return fail(EAT_ERR_CUDA, std::string("head workspace: ") + cudaGetErrorString(e));
+  }
+  bool ok = head_encode(&h->w128, h->w8, D.w, V, D.d_model, 128) &&
+            head_encode(&h->w64, h->w8, D.w, V, D.d_model, 64) &&
+            head_encode(&h->w16, h->w8, D.w, V, D.d_model, 16);
+  if (ok && D.with_grad)
+    ok = head_encode(&h->x64, false, h->xc, t_pad, D.d_model, 64) &&
+         head_encode(&h->e64, false, h->e, h->cap, h->ld, 64);
+  if (!ok) {
+    free_head(h);
+    return fail(EAT_ERR_CUDA, "cuTensorMapEncodeTiled rejected a head tensor");
+  }
   *out = h;
   return EAT_OK;
 }
@@ -326,19 +575,24 @@ eat_status eat_head_destroy(eat_head* h) {
 
 eat_status eat_head_reset(eat_head* h, void* stream) {
   if (!h) return fail(EAT_ERR_INVALID_ARG, "eat_head_reset: null handle");
-  const cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
+  cudaError_t e = cudaMemsetAsync(h->st.err, 0, 16, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
   if (e != cudaSuccess)
     return fail(EAT_ERR_CUDA, std::string("eat_head_reset: ") + cudaGetErrorString(e));
+  *(volatile unsigned int*)h->mirror_host = 0u;
+  h->failed = false;
   return EAT_OK;
 }
 
 eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_t T,
                         const int32_t* target, float* nll, float* lse, void* stream) {
-  const eat_status s = check_call("eat_head_nll", h, x, T, target, nll);
+  const eat_status s = check_call("eat_head_nll", h, x, T, target, nll, lse);
   if (s != EAT_OK) return s;
-  if (h->desc.dtype == EAT_FP8_E4M3 && (!x_scale || ((uintptr_t)x_scale & 3)))
+  if (h->w8 && (!x_scale || ((uintptr_t)x_scale & 3)))
     return fail(EAT_ERR_INVALID_ARG, "eat_head_nll: an e4m3 head needs x_scale, 4-byte aligned");
-  const cudaError_t e = run_nll(h, x, x_scale, T, target, nll, lse, (cudaStream_t)stream);
+  const cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = T <= kHeadSmallT ? run_small(h, x, x_scale, T, target, nll, lse, st)
+                                         : run_pair(h, x, x_scale, T, target, nll, lse, st);
   if (e != cudaSuccess)
     return fail(EAT_ERR_CUDA, std::string("eat_head_nll launch: ") + cudaGetErrorString(e));
   return EAT_OK;
@@ -347,33 +601,16 @@ eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_
 eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_t* target,
                              const float* g, float* nll, float* lse, void* dx, void* dw,
                              void* stream) {
-  const eat_status s = check_call("eat_head_nll_grad", h, x, T, target, nll);
+  const eat_status s = check_call("eat_head_nll_grad", h, x, T, target, nll, lse);
   if (s != EAT_OK) return s;
   if (!h->desc.with_grad)
     return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: the handle was created without with_grad");
   if (!g || !dx || !dw)
     return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: g, dx and dw must be non-NULL");
-  if (((uintptr_t)dx | (uintptr_t)dw) & 15)
+  if ((((uintptr_t)dx | (uintptr_t)dw) & 15) || ((uintptr_t)g & 3))
     return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: dx and dw must be 16-byte aligned");
   if (dx == x) return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: dx must not alias x");
-  const cudaStream_t st = (cudaStream_t)stream;
-  const int V = h->desc.vocab, d = h->desc.d_model;
-  const __nv_bfloat16* w = (const __nv_bfloat16*)h->desc.w;
-  cudaError_t e = run_nll(h, x, nullptr, T, target, nll, lse, st);
-  for (int vp = 0; vp < V && e == cudaSuccess; vp += h->piece) {
-    const int n = std::min(h->piece, V - vp);
-    e = launch_pdl(head_p_kernel, dim3(tiles(n), tiles(T)), dim3(256), 0, st,
-                   (const __nv_bfloat16*)x, w, T, V, d, vp, n, target, (const float*)h->lse, g,
-                   h->p, h->piece);
-    if (e == cudaSuccess)
-      e = launch_pdl(head_dx_kernel, dim3(tiles(d), tiles(T)), dim3(256), 0, st,
-                     (const __nv_bfloat16*)h->p, h->piece, n, w + (size_t)vp * d, T, d, vp == 0,
-                     vp + n == V, h->dx, (__nv_bfloat16*)dx);
-    if (e == cudaSuccess)
-      e = launch_pdl(head_dw_kernel, dim3(tiles(d), tiles(n)), dim3(256), 0, st,
-                     (const __nv_bfloat16*)h->p, h->piece, n, (const __nv_bfloat16*)x, target, T,
-                     V, d, (__nv_bfloat16*)dw + (size_t)vp * d);
-  }
+  const cudaError_t e = run_grad(h, x, T, target, g, nll, lse, dx, dw, (cudaStream_t)stream);
   if (e != cudaSuccess)
     return fail(EAT_ERR_CUDA, std::string("eat_head_nll_grad launch: ") + cudaGetErrorString(e));
   return EAT_OK;

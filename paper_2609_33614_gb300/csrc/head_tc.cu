@@ -1,0 +1,871 @@
+// Tensor-core kernels of the vocabulary head: logits l_tv = <x_t, w_v> that live in TMEM only.
+//
+//  small_kernel (loss, up to 128 tokens): a tile is 128 vocabulary rows (M) x the call's tokens (N =
+//      16 .. 128), so a decode call streams the vocabulary matrix once and its MMAs stay below that.
+//      Bound: HBM.  Each CTA takes an equal run of 16-row groups; a thread owns a vocabulary row of
+//      the tile and keeps a running maximum and sum of exponentials per token, joined across the
+//      CTA once at its end.  The k-blocks of a tile go to up to four accumulators, added in fp32: a
+//      tensor-core sum truncates at every step, and shorter sums keep a decode token's loss within
+//      a few 1e-6.
+//  pair_kernel: 256 tokens (M, on an SM pair, cta_group::2) x 256 vocabulary rows (N).  A thread
+//      owns a token's row of the tile, so sums over the vocabulary stay within a thread.  Bound:
+//      tensor pipe.  kNll: running maximum and sum; kExp: exponentials relative to the target's
+//      logit, stored as bf16 for the gradient's products, and their sums; kGrad: dx = f (E W) and
+//      dW = E^T X, operands taken from the row-major matrices as they are (K-major or MN-major).
+// Warp roles as in the expert kernels: warp 0 one elected lane issues TMA, warp 1 owns TMEM and one
+// elected lane issues MMAs, the others drain TMEM (double-buffered accumulators).  Every wait is
+// bounded; on expiry the kernel records it, lets copies and MMAs land, frees TMEM and returns.
+#include "head_tc.cuh"
+
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "tc_ptx.cuh"
+
+namespace eat {
+
+namespace {
+
+using namespace ptx;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kRowBytes = 128;             // bytes of a k-block's row: 64 bf16 or 128 e4m3
+constexpr int kOperand = 128 * kRowBytes;  // 128 rows of a k-block
+constexpr int kBoxBytes = 64 * kRowBytes;  // a box of 64 rows
+
+__device__ __forceinline__ void report(const HeadStatus& st, volatile int* abort_flag) {
+  if (*abort_flag) *(volatile unsigned int*)st.mirror = *(volatile unsigned int*)st.err;
+}
+
+// (m, s) += (m2, s2): sums of exp2 relative to their maxima
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+  const float n = fmaxf(m, m2);
+  s = s * ex2(m - n) + s2 * ex2(m2 - n);
+  m = n;
+}
+
+// ------------------------------------------------------------------------------ small calls
+template <int N>
+struct SmallCfg {
+  static constexpr int kKps = 2;                                 // k-blocks per stage
+  static constexpr int kSub = kOperand + N * kRowBytes;
+  static constexpr int kStage = kKps * kSub;
+  static constexpr int kStagesRaw = (220 * 1024 - 1024) / kStage;
+  static constexpr int kStages = kStagesRaw > 6 ? 6 : kStagesRaw;
+  static constexpr int kSmem = 1024 + kStages * kStage;
+  static constexpr int kSplits = 256 / N < 4 ? 256 / N : 4;      // accumulators of a tile
+  static constexpr int kAccCols = kSplits * N;
+  static constexpr int kTmemCols = 2 * kAccCols;
+  static constexpr int kCols = N < 64 ? N : 64;                  // token columns of a thread
+  static constexpr int kEpiWarps = 4 * (N / kCols);
+  static constexpr int kThreads = 64 + 32 * kEpiWarps;
+};
+
+// The first k-block of accumulator s.
+__device__ __forceinline__ int split_begin(int s, int splits, int kblocks) {
+  return (int)((long long)kblocks * s / splits);
+}
+
+template <int N, bool W8>
+__global__ void __launch_bounds__(SmallCfg<N>::kThreads, 1)
+small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant__ CUtensorMap map_w16,
+             const __grid_constant__ CUtensorMap map_x, const HeadSmallArgs a) {
+  using C = SmallCfg<N>;
+  constexpr int S = C::kStages;
+  constexpr int kElems = W8 ? 128 : 64;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  __shared__ uint64_t full[S], empty[S], tfull[2], tempty[2], mma_done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  __shared__ int32_t s_target[N];
+  __shared__ float s_xs[N];
+  __shared__ float2 s_fin[4][N];
+  volatile int* abort_flag = &abort_word;
+  const WaitCtx wc{abort_flag, a.st.err};
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], C::kEpiWarps);
+    }
+    mbar_init(&mma_done, 1);
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&map_w128);
+    prefetch_map(&map_x);
+  }
+  if (warp == 1) tmem_alloc<false>(&tmem_slot, C::kTmemCols);
+  pdl_wait();
+  pdl_launch_dependents();
+  for (int i = threadIdx.x; i < N; i += C::kThreads) {
+    s_target[i] = i < a.T ? a.target[i] : -1;
+    s_xs[i] = kLog2e * (W8 && i < a.T ? a.xs[i] : 1.0f);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+
+  // this CTA's vocabulary rows
+  const long long groups = (a.V + 15) / 16;
+  const int row0 = 16 * (int)(groups * blockIdx.x / gridDim.x);
+  const int row1 = min(a.V, 16 * (int)(groups * (blockIdx.x + 1) / gridDim.x));
+  const int splits = min(C::kSplits, a.kblocks);
+
+  if (warp == 0) {
+    if (elect_one()) {
+      const uint64_t once = policy_evict_first();
+      int stage = 0;
+      uint32_t phase = 0;
+      long long issued = 0;
+      bool ok = true;
+      for (int r = row0; r < row1 && ok; r += 128) {
+        const int boxes = min(8, (row1 - r + 15) / 16);  // 16-row boxes of the tile
+        for (int kb = 0; kb < a.kblocks; kb += C::kKps) {
+          const int nk = min(C::kKps, a.kblocks - kb);
+          if (!mbar_wait(&empty[stage], phase ^ 1u, wc, 1u)) {
+            ok = false;
+            break;
+          }
+          uint8_t* st = smem + stage * C::kStage;
+          mbar_expect_tx(&full[stage], nk * (boxes * 16 * kRowBytes + N * kRowBytes));
+#pragma unroll
+          for (int j = 0; j < C::kKps; ++j) {
+            if (j >= nk) break;
+            uint8_t* sj = st + j * C::kSub;
+            const int kx = (kb + j) * kElems;
+            if (boxes == 8) {
+              tma_load_hint(sj, &map_w128, &full[stage], kx, r, once);
+            } else {
+              for (int b = 0; b < boxes; ++b)
+                tma_load_hint(sj + b * 16 * kRowBytes, &map_w16, &full[stage], kx, r + 16 * b,
+                              once);
+            }
+            tma_load(sj + kOperand, &map_x, &full[stage], kx, 0);
+          }
+          ++issued;
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      // copies in flight land before the CTA may exit
+      for (long long i = issued > S ? issued - S : 0; i < issued; ++i)
+        mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), wc, 2u, false);
+    }
+  } else if (warp == 1) {
+    if (elect_one()) {
+      constexpr uint32_t id = idesc(W8, 128, N);
+      int stage = 0, local = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int r = row0; r < row1 && ok; r += 128, ++local) {
+        const int buf = local & 1;
+        if (!mbar_wait(&tempty[buf], ((local >> 1) & 1) ^ 1u, wc, 4u)) break;
+        tc_fence_after();
+        int split = 0, next = split_begin(1, splits, a.kblocks);
+        uint32_t acc = 0;
+        for (int kb = 0; kb < a.kblocks; kb += C::kKps) {
+          if (!mbar_wait(&full[stage], phase, wc, 8u)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+#pragma unroll
+          for (int j = 0; j < C::kKps; ++j) {
+            if (kb + j >= a.kblocks) break;
+            if (kb + j == next) {
+              ++split;
+              next = split_begin(split + 1, splits, a.kblocks);
+              acc = 0;
+            }
+            const uint32_t d = tmem_base + (uint32_t)(buf * C::kAccCols + split * N);
+            const uint32_t sa = smem_u32(smem + stage * C::kStage + j * C::kSub);
+            const uint64_t da = sdesc_k(sa), db = sdesc_k(sa + kOperand);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              mma<false, W8>(d, da + 2 * k, db + 2 * k, id, acc);
+              acc = 1;
+            }
+          }
+          mma_commit<false>(&empty[stage]);
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        if (ok) mma_commit<false>(&tfull[buf]);
+      }
+      mma_commit<false>(&mma_done);  // no MMA may run when TMEM is freed
+    }
+    if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+  } else {
+    // a thread: vocabulary row 32 q + lane of the tile, columns [col0, col0 + kCols)
+    const int q = warp & 3, half = (warp - 2) >> 2, col0 = half * C::kCols;
+    float m[C::kCols], s[C::kCols];
+#pragma unroll
+    for (int c = 0; c < C::kCols; ++c) {
+      m[c] = kHeadLow;
+      s[c] = 0.f;
+    }
+    int local = 0;
+    for (int r = row0; r < row1; r += 128, ++local) {
+      const int buf = local & 1;
+      if (!warp_wait(&tfull[buf], (local >> 1) & 1, wc, 32u)) break;
+      tc_fence_after();
+      const int v = r + 32 * q + lane;
+      const bool live = v < row1;
+      const float sv = W8 && live ? a.ws[v] : 1.0f;
+      // does a token of these columns have its target among the warp's rows?
+      bool hit = false;
+      for (int c = lane; c < C::kCols; c += 32) {
+        const int o = s_target[col0 + c] - (r + 32 * q);
+        hit |= o >= 0 && o < 32;
+      }
+      hit = __any_sync(0xffffffffu, hit);
+      const uint32_t t0 = tmem_base + ((uint32_t)(32 * q) << 16) +
+                          (uint32_t)(buf * C::kAccCols + col0);
+#pragma unroll
+      for (int c0 = 0; c0 < C::kCols; c0 += 16) {
+        uint32_t w[16], w2[16];
+        __syncwarp();
+        tmem_ld16(t0 + c0, w);
+#pragma unroll
+        for (int i = 1; i < C::kSplits; ++i) {
+          if (i < splits) {
+            tmem_ld16(t0 + i * N + c0, w2);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              w[j] = __float_as_uint(__uint_as_float(w[j]) + __uint_as_float(w2[j]));
+          }
+        }
+        tmem_wait_ld();
+        if (live) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int c = c0 + j;
+            const float l = __uint_as_float(w[j]) * (W8 ? sv * s_xs[col0 + c] : kLog2e);
+            if (hit && s_target[col0 + c] == v) continue;
+            const float dl = l - m[c], e = ex2(-fabsf(dl));
+            s[c] = dl > 0.f ? fmaf(s[c], e, 1.0f) : s[c] + e;
+            m[c] = fmaxf(m[c], l);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&tempty[buf]);
+    }
+    // over the warp's rows, then the four warps
+#pragma unroll
+    for (int c = 0; c < C::kCols; ++c) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m[c], o);
+        const float s2 = __shfl_xor_sync(0xffffffffu, s[c], o);
+        join(m[c], s[c], m2, s2);
+      }
+      if (lane == 0) s_fin[q][col0 + c] = make_float2(m[c], s[c]);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc<false>(tmem_base, C::kTmemCols);
+  for (int c = threadIdx.x; c < a.T; c += C::kThreads) {
+    float2 f = s_fin[0][c];
+    for (int i = 1; i < 4; ++i) join(f.x, f.y, s_fin[i][c].x, s_fin[i][c].y);
+    a.part[(size_t)blockIdx.x * N + c] = f;
+  }
+  if (threadIdx.x == 0) report(a.st, abort_flag);
+}
+
+// --------------------------------------------------------------------------------- SM pairs
+enum : int { kNll = 0, kExp = 1, kGrad = 2 };
+
+struct PairCfg {
+  static constexpr int kKps = 2;
+  static constexpr int kSub = 2 * kOperand;  // one CTA's 128 rows of A and of B
+  static constexpr int kStage = kKps * kSub;
+  static constexpr int kStages = 3;
+  static constexpr int kSmem = 1024 + kStages * kStage;
+  static constexpr int kEpiWarps = 8;
+  static constexpr int kThreads = 64 + 32 * kEpiWarps;
+  static constexpr int kAccCols = 256;
+};
+
+struct PairParams {
+  HeadPairArgs p;
+  HeadGradArgs g;
+};
+
+// One tile of a launch: 256 rows of A from m0, 256 rows of B from n0, kb k-blocks.
+struct Tile {
+  int m0, n0, kb;
+  bool dw;  // kGrad: a tile of dW
+};
+
+// The gradient's tiles in the order in which equal workers would take them: first the product with
+// the longer sums (n1 tiles of k1 k-blocks each, dealt round), then the other one (n2 tiles of k2),
+// whose j-th tile of a worker is the one that it would reach in time order.
+struct GradTiles {
+  int n1, k1, n2, k2, pairs, pair;
+  bool dw_first;
+  __device__ int first_count() const { return n1 / pairs + (pair < n1 % pairs ? 1 : 0); }
+  // the i-th tile of this pair: its number, and in `second` whether it is of the second product;
+  // -1 when there is none
+  __device__ int at(int i, bool& second) const {
+    const int own = first_count();
+    second = i >= own;
+    if (!second) return i * pairs + pair;
+    const int j = i - own, r = n1 % pairs;
+    long long t;
+    if (r == 0) {
+      t = (long long)j * pairs + pair;
+    } else if (pair >= r) {  // free one tile of the first product earlier
+      const long long ahead = (long long)j * k2 - k1;  // time after the others begin
+      t = (long long)j * (pairs - r) + (pair - r) + (ahead > 0 ? (ahead + k2 - 1) / k2 * r : 0);
+    } else {
+      t = (long long)j * r + pair + (long long)(j + k1 / max(k2, 1) + 1) * (pairs - r);
+    }
+    return t < n2 ? (int)t : -1;
+  }
+};
+
+template <int MODE, bool W8>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg::kThreads, 1)
+pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+            const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PairParams prm) {
+  using C = PairCfg;
+  constexpr int S = C::kStages;
+  constexpr int kElems = W8 ? 128 : 64;
+  const HeadPairArgs& p = prm.p;
+  const HeadGradArgs& g = prm.g;
+  const HeadStatus status = MODE == kGrad ? g.st : p.st;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  __shared__ uint64_t full[S], empty[S], tfull[2], tempty[2], mma_done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  __shared__ float s_ws[W8 ? C::kEpiWarps : 1][W8 ? 128 : 1];
+  volatile int* abort_flag = &abort_word;
+  const WaitCtx wc{abort_flag, status.err};
+
+  const uint32_t rank = cluster_rank();
+  const bool leader = rank == 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], 2 * C::kEpiWarps);  // the epilogue warps of both CTAs (rank 0's)
+    }
+    mbar_init(&mma_done, 1);
+    abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&map_a);
+    prefetch_map(&map_b);
+    if (MODE == kGrad) prefetch_map(&map_x);
+  }
+  if (warp == 1) tmem_alloc<true>(&tmem_slot, 512);
+  tc_fence_before();
+  cluster_sync_all();  // both CTAs' barriers exist before either signals the other
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  // the launch's tokens (kNll), or the counted ones of its piece
+  int rows = p.T, n_counted = 0;
+  if (MODE != kNll) {
+    n_counted = MODE == kGrad ? *g.n_counted : *p.n_counted;
+    const int t0 = MODE == kGrad ? g.t0 : p.t0, cap = MODE == kGrad ? g.cap : p.cap;
+    rows = max(0, min(cap, n_counted - t0));
+  }
+  const int row_tiles = (rows + kHeadTile - 1) / kHeadTile;
+  const int V = MODE == kGrad ? g.V : p.V;
+  const int v_tiles = (V + kHeadTile - 1) / kHeadTile;
+  const int units = row_tiles * v_tiles;
+  GradTiles gt{};
+  const int d_tiles = MODE == kGrad ? (g.d + kHeadTile - 1) / kHeadTile : 1;
+  if (MODE == kGrad) {
+    const int nx = row_tiles * d_tiles, kx = (V + 63) / 64;
+    // a piece without tokens adds nothing, but the first one still writes dW
+    const int nw = rows > 0 || g.t0 == 0 ? v_tiles * d_tiles : 0, kw = (rows + 63) / 64;
+    gt.dw_first = kw > kx;
+    gt.n1 = gt.dw_first ? nw : nx;
+    gt.k1 = gt.dw_first ? kw : kx;
+    gt.n2 = gt.dw_first ? nx : nw;
+    gt.k2 = gt.dw_first ? kx : kw;
+    gt.pairs = n_pairs;
+    gt.pair = pair;
+  }
+  // the next tile of this pair after step i (i is left at the step that follows it)
+  auto next_tile = [&](int& i, Tile& t) -> bool {
+    if (MODE == kGrad) {
+      bool second;
+      const int n = gt.at(i, second);
+      if (n < 0 || (!second && n >= gt.n1)) return false;
+      ++i;
+      t.dw = second != gt.dw_first;
+      t.m0 = n / d_tiles * kHeadTile;
+      t.n0 = n % d_tiles * kHeadTile;
+      t.kb = second ? gt.k2 : gt.k1;
+      return true;
+    }
+    for (;;) {
+      const long long u = (long long)i * n_pairs + pair;
+      if (u >= units) return false;
+      ++i;
+      const int rt = (int)(u % row_tiles);
+      if (MODE == kExp && p.redo && !p.far[(p.t0 / kHeadTile) + rt]) continue;
+      t.dw = false;
+      t.m0 = rt * kHeadTile;
+      t.n0 = (int)(u / row_tiles) * kHeadTile;
+      t.kb = p.kblocks;
+      return true;
+    }
+  };
+  const uint32_t full0 = map_rank(smem_u32(full), 0);
+  const uint32_t tempty0 = map_rank(smem_u32(tempty), 0);
+
+  if (warp == 0) {
+    if (elect_one()) {
+      int stage = 0, i = 0;
+      uint32_t phase = 0;
+      long long issued = 0;
+      bool ok = true;
+      Tile t;
+      while (ok && next_tile(i, t)) {
+        // dX: A = E (K-major), B = W (MN-major); dW: A = E, B = X (both MN-major); scores: A = X,
+        // B = W (both K-major)
+        const CUtensorMap* mb = MODE == kGrad && t.dw ? &map_x : &map_b;
+        const int ra = t.m0 + (int)rank * 128 + (MODE == kExp ? p.t0 : 0);
+        const int rb = t.n0 + (int)rank * 128;
+        for (int kb = 0; kb < t.kb; kb += C::kKps) {
+          const int nk = min(C::kKps, t.kb - kb);
+          if (!mbar_wait(&empty[stage], phase ^ 1u, wc, 1u)) {
+            ok = false;
+            break;
+          }
+          uint8_t* st = smem + stage * C::kStage;
+          const uint32_t fb = full0 + 8u * (uint32_t)stage;
+          if (leader) mbar_expect_tx(&full[stage], 2 * nk * C::kSub);
+#pragma unroll
+          for (int j = 0; j < C::kKps; ++j) {
+            if (j >= nk) break;
+            uint8_t* sa = st + j * C::kSub;
+            uint8_t* sb = sa + kOperand;
+            const int kx = (kb + j) * kElems;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              if (MODE == kGrad) {
+                if (t.dw) tma_load_pair(sa + b * kBoxBytes, &map_a, fb, ra + 64 * b, kx);
+                else tma_load_pair(sa + b * kBoxBytes, &map_a, fb, kx, ra + 64 * b);
+                tma_load_pair(sb + b * kBoxBytes, mb, fb, rb + 64 * b, kx + (t.dw ? g.t0 : 0));
+              } else {
+                tma_load_pair(sa + b * kBoxBytes, &map_a, fb, kx, ra + 64 * b);
+                tma_load_pair(sb + b * kBoxBytes, mb, fb, kx, rb + 64 * b);
+              }
+            }
+          }
+          ++issued;
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      // rank 0: the copies of both CTAs still in flight land before the pair may exit
+      if (leader)
+        for (long long n = issued > S ? issued - S : 0; n < issued; ++n)
+          mbar_wait(&full[n % S], (uint32_t)((n / S) & 1), wc, 2u, false);
+    }
+  } else if (warp == 1) {
+    if (leader && elect_one()) {
+      int stage = 0, i = 0, local = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      Tile t;
+      for (; ok && next_tile(i, t); ++local) {
+        const int buf = local & 1;
+        if (!mbar_wait(&tempty[buf], ((local >> 1) & 1) ^ 1u, wc, 4u)) break;
+        tc_fence_after();
+        const uint32_t d0 = tmem_base + (uint32_t)(buf * C::kAccCols);
+        const uint32_t id = idesc(W8, 256, 256, MODE == kGrad && t.dw, MODE == kGrad);
+        uint32_t acc = 0;
+        for (int kb = 0; kb < t.kb; kb += C::kKps) {
+          const int nk = min(C::kKps, t.kb - kb);
+          if (!mbar_wait(&full[stage], phase, wc, 8u)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+#pragma unroll
+          for (int j = 0; j < C::kKps; ++j) {
+            if (j >= nk) break;
+            const uint32_t sa = smem_u32(smem + stage * C::kStage + j * C::kSub);
+            const bool a_mn = MODE == kGrad && t.dw;
+            const uint64_t da = a_mn ? sdesc_mn(sa) : sdesc_k(sa);
+            const uint64_t db =
+                MODE == kGrad ? sdesc_mn(sa + kOperand) : sdesc_k(sa + kOperand);
+            const int step_a = a_mn ? 128 : 2, step_b = MODE == kGrad ? 128 : 2;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              mma<true, W8>(d0, da + k * step_a, db + k * step_b, id, acc);
+              acc = 1;
+            }
+          }
+          mma_commit<true>(&empty[stage]);
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
+          }
+        }
+        if (ok) mma_commit<true>(&tfull[buf]);
+      }
+      mma_commit<true>(&mma_done);
+    }
+    if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+  } else {
+    // a thread: row 128 rank + 32 q + lane of the tile, columns [128 ch, 128 ch + 128)
+    const int q = warp & 3, ch = (warp - 2) >> 2;
+    const int my_row = (int)rank * 128 + 32 * q + lane;
+    int i = 0, local = 0;
+    Tile t;
+    for (; next_tile(i, t); ++local) {
+      const int buf = local & 1;
+      const int row = t.m0 + my_row, n0 = t.n0 + 128 * ch;
+      // what the rows and columns need, loaded while the MMAs run
+      int y = -1;
+      float xs = kLog2e, ref = INFINITY;
+      if (MODE != kGrad && row < rows) {
+        y = p.target[(MODE == kExp ? p.t0 : 0) + row];
+        if (W8) xs *= p.xs[row];
+        if (MODE == kExp) {
+          ref = p.ref[p.t0 + row];
+          if (p.redo) ref = head_ref(ref, p.row_max[p.t0 + row]);
+        }
+      }
+      if (W8) {
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) {
+          const int v = n0 + c + lane;
+          s_ws[W8 ? warp - 2 : 0][c + lane] = v < V ? p.ws[v] : 0.f;
+        }
+        __syncwarp();
+      }
+      if (!warp_wait(&tfull[buf], (local >> 1) & 1, wc, 32u)) break;
+      tc_fence_after();
+      const uint32_t tb =
+          tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * C::kAccCols + 128 * ch);
+      float m = kHeadLow, s = 0.f;
+      float factor = 1.f;
+      __nv_bfloat16* out = nullptr;
+      float* sum = nullptr;
+      bool add = false, stores = false;
+      if (MODE == kGrad) {
+        if (t.dw) {
+          stores = row < V;
+          out = g.dw + (size_t)row * g.d;
+          const bool last = g.t0 + g.cap >= n_counted;
+          add = g.t0 > 0;
+          if (add || !last) sum = g.dw_sum + (size_t)row * g.d;
+          if (!last) out = nullptr;
+        } else if (row < rows) {
+          stores = true;
+          factor = g.f[g.t0 + row];
+          out = g.dx + (size_t)g.rows[g.t0 + row] * g.d;
+        }
+      }
+#pragma unroll 1
+      for (int c0 = 0; c0 < 128; c0 += 32) {
+        uint32_t w[32];
+        __syncwarp();
+        tmem_ld16(tb + c0, w);
+        tmem_ld16(tb + c0 + 16, w + 16);
+        tmem_wait_ld();
+        const int nc = n0 + c0;
+        if (MODE == kGrad) {
+          if (nc >= g.d || !stores) continue;
+          if (t.kb == 0) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w[j] = 0;
+          }
+          if (t.dw) {
+            if (add) {
+#pragma unroll
+              for (int j = 0; j < 32; j += 4) {
+                const float4 o = *(const float4*)(sum + nc + j);
+                w[j] = __float_as_uint(__uint_as_float(w[j]) + o.x);
+                w[j + 1] = __float_as_uint(__uint_as_float(w[j + 1]) + o.y);
+                w[j + 2] = __float_as_uint(__uint_as_float(w[j + 2]) + o.z);
+                w[j + 3] = __float_as_uint(__uint_as_float(w[j + 3]) + o.w);
+              }
+            }
+            if (!out) {
+#pragma unroll
+              for (int j = 0; j < 32; j += 4)
+                *(uint4*)(sum + nc + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+              continue;
+            }
+          }
+          uint32_t b[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(w[2 * j]) * factor,
+                                                           __uint_as_float(w[2 * j + 1]) * factor);
+            b[j] = *(const uint32_t*)&v;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *(uint4*)(out + nc + 8 * j) = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
+          continue;
+        }
+        // scores: base-2 logits
+        float l[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float sc = W8 ? xs * s_ws[W8 ? warp - 2 : 0][c0 + j] : kLog2e;
+          l[j] = MODE == kExp ? __uint_as_float(w[j]) : __uint_as_float(w[j]) * sc;
+        }
+        const int hit = y - nc;  // the target's column, if among these
+        if (MODE == kNll) {
+          if (hit >= 0 && hit < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j == hit) {
+                p.ly[row] = l[j];
+                l[j] = kHeadLow;
+              }
+          }
+          if (nc + 32 > V) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (nc + j >= V) l[j] = kHeadLow;
+          }
+          float n = m;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) n = fmaxf(n, l[j]);
+          float s0 = s * ex2(m - n), s1 = 0.f;
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            s0 += ex2(l[j] - n);
+            s1 += ex2(l[j + 1] - n);
+          }
+          s = s0 + s1;
+          m = n;
+        } else {
+          float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) m = fmaxf(m, l[j]);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) l[j] = ex2(fmaf(l[j], kLog2e, -ref));
+          if (hit >= 0 && hit < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j == hit) l[j] = 0.f;
+          }
+          if (nc + 32 > V) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (nc + j >= V) l[j] = 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            s0 += l[j];
+            s1 += l[j + 1];
+          }
+          s += s0 + s1;
+          uint32_t b[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(l[2 * j], l[2 * j + 1]);
+            b[j] = *(const uint32_t*)&v;
+          }
+          __nv_bfloat16* e = p.e + (size_t)row * p.ld + nc;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
+                             e + 16 * j),
+                         "r"(b[8 * j]), "r"(b[8 * j + 1]), "r"(b[8 * j + 2]), "r"(b[8 * j + 3]),
+                         "r"(b[8 * j + 4]), "r"(b[8 * j + 5]), "r"(b[8 * j + 6]),
+                         "r"(b[8 * j + 7])
+                         : "memory");
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (leader) mbar_arrive(&tempty[buf]);
+        else mbar_arrive_cluster(tempty0 + 8u * (uint32_t)buf);
+      }
+      if (MODE == kNll && row < rows)
+        p.part2[(size_t)(n0 / 128) * p.T + row] = make_float2(m, s);
+      if (MODE == kExp) {
+        p.part[(size_t)(n0 / 128) * p.cap + row] = s;
+        if (!p.redo && row < rows && m * kLog2e > ref + kHeadFar) {
+          atomicMax(&p.row_max[p.t0 + row], ordered_bits(m * kLog2e));
+          p.far[(p.t0 + row) / kHeadTile] = 1;
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // neither CTA leaves while the other may still signal it
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc<true>(tmem_base, 512);
+  if (threadIdx.x == 0) report(status, abort_flag);
+}
+
+// -------------------------------------------------------------------------------- host side
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = (PFN_cuTensorMapEncodeTiled_v12000)p;
+  });
+  return fn;
+}
+
+template <int N, bool W8>
+cudaError_t launch_small(const CUtensorMap& w128, const CUtensorMap& w16, const CUtensorMap& x,
+                         const HeadSmallArgs& a, int ctas, cudaStream_t st) {
+  return launch_pdl(small_kernel<N, W8>, dim3(ctas), dim3(SmallCfg<N>::kThreads),
+                    SmallCfg<N>::kSmem, st, w128, w16, x, a);
+}
+template <bool W8>
+cudaError_t launch_small_n(const CUtensorMap& w128, const CUtensorMap& w16, const CUtensorMap& x,
+                           const HeadSmallArgs& a, int ctas, cudaStream_t st) {
+  switch (head_small_n(a.T)) {
+    case 16: return launch_small<16, W8>(w128, w16, x, a, ctas, st);
+    case 32: return launch_small<32, W8>(w128, w16, x, a, ctas, st);
+    case 64: return launch_small<64, W8>(w128, w16, x, a, ctas, st);
+    default: return launch_small<128, W8>(w128, w16, x, a, ctas, st);
+  }
+}
+template <int MODE, bool W8>
+cudaError_t launch_pair(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& x,
+                        const PairParams& p, int pairs, cudaStream_t st) {
+  return launch_pdl(pair_kernel<MODE, W8>, dim3(2 * pairs), dim3(PairCfg::kThreads),
+                    PairCfg::kSmem, st, a, b, x, p);
+}
+
+template <typename K>
+cudaError_t limit(K kernel, int smem) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+}
+template <bool W8>
+cudaError_t configure_small() {
+  cudaError_t e = limit(small_kernel<16, W8>, SmallCfg<16>::kSmem);
+  if (e == cudaSuccess) e = limit(small_kernel<32, W8>, SmallCfg<32>::kSmem);
+  if (e == cudaSuccess) e = limit(small_kernel<64, W8>, SmallCfg<64>::kSmem);
+  if (e == cudaSuccess) e = limit(small_kernel<128, W8>, SmallCfg<128>::kSmem);
+  return e;
+}
+template <int MODE, bool W8>
+cudaError_t configure_pair(int num_sms, int* max_pairs) {
+  const cudaError_t e = limit(pair_kernel<MODE, W8>, PairCfg::kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(num_sms & ~1);
+  cfg.blockDim = dim3(PairCfg::kThreads);
+  cfg.dynamicSmemBytes = PairCfg::kSmem;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, pair_kernel<MODE, W8>, &cfg) != cudaSuccess || n <= 0) {
+    cudaGetLastError();
+    n = num_sms / 2;
+  }
+  *max_pairs = std::max(1, std::min(*max_pairs, n));
+  return cudaSuccess;
+}
+
+}  // namespace
+
+int head_small_n(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
+int head_small_ctas(int num_sms, int V) { return std::min(num_sms, (V + 15) / 16); }
+
+cudaError_t head_launch_small(bool w8, const CUtensorMap& w128, const CUtensorMap& w16,
+                              const CUtensorMap& x, const HeadSmallArgs& a, int ctas,
+                              cudaStream_t st) {
+  return w8 ? launch_small_n<true>(w128, w16, x, a, ctas, st)
+            : launch_small_n<false>(w128, w16, x, a, ctas, st);
+}
+
+cudaError_t head_launch_pair(bool w8, bool exp, const CUtensorMap& x, const CUtensorMap& w,
+                             const HeadPairArgs& a, int max_pairs, cudaStream_t st) {
+  PairParams p{};
+  p.p = a;
+  const long long tokens = exp ? a.cap : a.T;
+  const long long units =
+      (tokens + kHeadTile - 1) / kHeadTile * ((a.V + kHeadTile - 1) / kHeadTile);
+  const int pairs = (int)std::min<long long>(max_pairs, units);
+  if (exp) return launch_pair<kExp, false>(x, w, w, p, pairs, st);
+  return w8 ? launch_pair<kNll, true>(x, w, w, p, pairs, st)
+            : launch_pair<kNll, false>(x, w, w, p, pairs, st);
+}
+
+cudaError_t head_launch_grad(const CUtensorMap& e, const CUtensorMap& w, const CUtensorMap& x,
+                             const HeadGradArgs& a, int max_pairs, cudaStream_t st) {
+  PairParams p{};
+  p.g = a;
+  const long long units = ((a.cap + kHeadTile - 1) / kHeadTile + (a.V + kHeadTile - 1) / kHeadTile) *
+                          (long long)((a.d + kHeadTile - 1) / kHeadTile);
+  const int pairs = (int)std::min<long long>(max_pairs, units);
+  return launch_pair<kGrad, false>(e, w, x, p, pairs, st);
+}
+
+cudaError_t head_configure(int num_sms, int* max_pairs) {
+  *max_pairs = std::max(1, num_sms / 2);
+  cudaError_t e = configure_small<false>();
+  if (e == cudaSuccess) e = configure_small<true>();
+  if (e == cudaSuccess) e = configure_pair<kNll, false>(num_sms, max_pairs);
+  if (e == cudaSuccess) e = configure_pair<kNll, true>(num_sms, max_pairs);
+  if (e == cudaSuccess) e = configure_pair<kExp, false>(num_sms, max_pairs);
+  if (e == cudaSuccess) e = configure_pair<kGrad, false>(num_sms, max_pairs);
+  return e;
+}
+
+bool head_encode(CUtensorMap* m, bool w8, const void* ptr, long long rows, long long cols,
+                 int box_rows) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)cols * (w8 ? 1 : 2)};
+  cuuint32_t box[2] = {(cuuint32_t)(w8 ? 128 : 64), (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(m, w8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+            const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace eat

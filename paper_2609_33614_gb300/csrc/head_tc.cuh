@@ -1,0 +1,99 @@
+// Tensor-core kernels of the vocabulary head (head_tc.cu) and what its host side (head.cu) calls.
+#pragma once
+
+#include "eat_internal.cuh"
+
+#include <cuda.h>
+
+namespace eat {
+
+constexpr int kHeadSmallT = 128;  // calls of up to this many tokens stream the vocabulary once
+constexpr int kHeadTile = 256;    // tokens, vocabulary rows and columns of an SM pair's tile
+// a partial maximum that no logit has set; finite, so that differences of it are not NaN
+constexpr float kHeadLow = -3.0e38f;
+// Exponentials of the gradient's pass are taken relative to the token's target logit.  A token with
+// a logit more than this many powers of two above it is taken again, relative to its largest logit.
+constexpr float kHeadFar = 40.0f;
+
+struct HeadStatus {
+  unsigned int* err;     // device status word
+  unsigned int* mirror;  // device address of its host-mapped copy
+};
+
+// Loss of up to kHeadSmallT tokens: part[cta][n] = {max, sum of exp2 relative to it} of the base-2
+// logits of the CTA's vocabulary rows, without the targets; n = small_n(T) columns.
+struct HeadSmallArgs {
+  int T, V, kblocks;
+  const int32_t* target;
+  const float* xs;  // e4m3: [T]
+  const float* ws;  // e4m3: [V]
+  float2* part;
+  HeadStatus st;
+};
+int head_small_n(int T);
+int head_small_ctas(int num_sms, int V);
+cudaError_t head_launch_small(bool w8, const CUtensorMap& w128, const CUtensorMap& w16,
+                              const CUtensorMap& x, const HeadSmallArgs& a, int ctas,
+                              cudaStream_t st);
+
+// Loss of more tokens (exp == false): part2[128-row piece of the vocabulary][T] as above, ly[t] the
+// base-2 target logit.  Gradient's first pass (exp == true): e[row][v] = exp2(l - ref) as bf16 (0 in
+// the target's column, beyond V and in rows beyond the counted tokens), part[piece][cap] its sums.
+struct HeadPairArgs {
+  int T, V, kblocks;
+  const int32_t* target;
+  const float* xs;
+  const float* ws;
+  float2* part2;
+  float* ly;
+  // gradient's first pass, over the counted tokens [t0, t0 + cap)
+  const int32_t* n_counted;  // device
+  int t0, cap, ld;
+  const float* ref;          // [tokens] base-2 target logits
+  uint32_t* row_max;         // [tokens] ordered bits of a far token's largest base-2 logit, or 0
+  int32_t* far;              // [tiles] a token of the tile is far
+  int redo;                  // only the tiles with far tokens, relative to their largest logits
+  float* part;
+  __nv_bfloat16* e;
+  HeadStatus st;
+};
+cudaError_t head_launch_pair(bool w8, bool exp, const CUtensorMap& x, const CUtensorMap& w,
+                             const HeadPairArgs& a, int max_pairs, cudaStream_t st);
+
+// dx = f (E W) and dW = E^T X of the counted tokens [t0, t0 + cap): both products' tiles in one
+// launch.  Pieces of tokens after the first add to dw_sum; the last one rounds.
+struct HeadGradArgs {
+  int V, d;
+  const int32_t* n_counted;
+  int t0, cap;
+  const float* f;        // [tokens] factors of the rows of dx
+  const int32_t* rows;   // [tokens] rows of dx
+  __nv_bfloat16* dx;
+  __nv_bfloat16* dw;
+  float* dw_sum;         // [V, d], or null when one piece holds every token
+  HeadStatus st;
+};
+cudaError_t head_launch_grad(const CUtensorMap& e, const CUtensorMap& w, const CUtensorMap& x,
+                             const HeadGradArgs& a, int max_pairs, cudaStream_t st);
+
+// The kernels' shared-memory limits on the current device, and the SM pairs that can be resident.
+cudaError_t head_configure(int num_sms, int* max_pairs);
+// Row-major [rows, cols] matrix in boxes of box_rows rows of 128 bytes, 128-byte swizzle, zeros
+// outside.
+bool head_encode(CUtensorMap* m, bool w8, const void* ptr, long long rows, long long cols,
+                 int box_rows);
+
+// Ordered bits of a float: larger floats have larger bits, and no float has 0 (other than NaNs).
+__device__ __forceinline__ uint32_t ordered_bits(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) {
+  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+// What a token's exponentials are relative to.
+__device__ __forceinline__ float head_ref(float ref, uint32_t row_max) {
+  return row_max ? from_ordered(row_max) : ref;
+}
+
+}  // namespace eat
