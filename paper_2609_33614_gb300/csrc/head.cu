@@ -14,8 +14,6 @@
 // hand, would spend 8 instead of 6 T V d flops and round P once as well.
 #include "head_tc.cuh"
 
-#include <cuda_fp8.h>
-
 #include <algorithm>
 #include <cstring>
 #include <new>
@@ -57,38 +55,6 @@ __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
-}
-
-// 16 bytes of a row as floats: 8 bf16 or 16 e4m3
-template <bool W8>
-struct Vec {
-  static constexpr int kN = W8 ? 16 : 8;
-  float v[kN];
-  __device__ explicit Vec(uint4 u) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (W8) {
-        __nv_fp8x4_e4m3 q;
-        q.__x = w[i];
-        const float4 f = (float4)q;
-        v[4 * i] = f.x;
-        v[4 * i + 1] = f.y;
-        v[4 * i + 2] = f.z;
-        v[4 * i + 3] = f.w;
-      } else {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
-  }
-};
-template <bool W8>
-__device__ __forceinline__ float dot16(uint4 a, uint4 b, float s) {
-  const Vec<W8> x(a), w(b);
-#pragma unroll
-  for (int i = 0; i < Vec<W8>::kN; ++i) s = fmaf(x.v[i], w.v[i], s);
-  return s;
 }
 
 // nll and lse of a token from the base-2 target logit and the sum of the others' exp2 relative to m
@@ -395,8 +361,11 @@ cudaError_t run_pair(eat_head* h, const void* x, const float* xs, int T, const i
   HeadPairArgs a{};
   a.T = T;
   a.V = V;
+  a.d = d;
   a.kblocks = (d + kb - 1) / kb;
   a.target = target;
+  a.x = x;
+  a.w = h->desc.w;
   a.xs = xs;
   a.ws = h->desc.w_scale;
   a.part2 = h->part;

@@ -293,6 +293,7 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
 // --------------------------------------------------------------------------------- SM pairs
 enum : int { kNll = 0, kExp = 1, kGrad = 2 };
 
+template <int MODE>
 struct PairCfg {
   static constexpr int kKps = 2;
   static constexpr int kSub = 2 * kOperand;  // one CTA's 128 rows of A and of B
@@ -300,7 +301,8 @@ struct PairCfg {
   static constexpr int kStages = 3;
   static constexpr int kSmem = 1024 + kStages * kStage;
   static constexpr int kEpiWarps = 8;
-  static constexpr int kThreads = 64 + 32 * kEpiWarps;
+  static constexpr int kDotWarp = 2 + kEpiWarps;  // kNll: the target logits
+  static constexpr int kThreads = 64 + 32 * kEpiWarps + (MODE == kNll ? 32 : 0);
   static constexpr int kAccCols = 256;
 };
 
@@ -343,10 +345,10 @@ struct GradTiles {
 };
 
 template <int MODE, bool W8>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg::kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE>::kThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
             const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PairParams prm) {
-  using C = PairCfg;
+  using C = PairCfg<MODE>;
   constexpr int S = C::kStages;
   constexpr int kElems = W8 ? 128 : 64;
   const HeadPairArgs& p = prm.p;
@@ -541,6 +543,23 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       mma_commit<true>(&mma_done);
     }
     if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+  } else if (MODE == kNll && warp == C::kDotWarp) {
+    // the target logits as fp32 sums of their own, beside the MMAs: a tensor-core sum truncates at
+    // every step, which a logit that grows steadily, as a target's does, shows most
+    constexpr int kVec = W8 ? 16 : 8;  // elements of 16 bytes
+    const int vecs = p.d / kVec;
+    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
+      const int y = p.target[t];
+      if (y < 0 || y >= V) continue;
+      const uint4* x = (const uint4*)p.x + (size_t)t * vecs;
+      const uint4* w = (const uint4*)p.w + (size_t)y * vecs;
+      float d = 0.f;
+#pragma unroll 4
+      for (int c = lane; c < vecs; c += 32) d = dot16<W8>(x[c], w[c], d);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+      if (lane == 0) p.ly[t] = d * kLog2e * (W8 ? p.xs[t] * p.ws[y] : 1.0f);
+    }
   } else {
     // a thread: row 128 rank + 32 q + lane of the tile, columns [128 ch, 128 ch + 128)
     const int q = warp & 3, ch = (warp - 2) >> 2;
@@ -649,10 +668,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           if (hit >= 0 && hit < 32) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (j == hit) {
-                p.ly[row] = l[j];
-                l[j] = kHeadLow;
-              }
+              if (j == hit) l[j] = kHeadLow;
           }
           if (nc + 32 > V) {
 #pragma unroll
@@ -768,8 +784,8 @@ cudaError_t launch_small_n(const CUtensorMap& w128, const CUtensorMap& w16, cons
 template <int MODE, bool W8>
 cudaError_t launch_pair(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& x,
                         const PairParams& p, int pairs, cudaStream_t st) {
-  return launch_pdl(pair_kernel<MODE, W8>, dim3(2 * pairs), dim3(PairCfg::kThreads),
-                    PairCfg::kSmem, st, a, b, x, p);
+  return launch_pdl(pair_kernel<MODE, W8>, dim3(2 * pairs), dim3(PairCfg<MODE>::kThreads),
+                    PairCfg<MODE>::kSmem, st, a, b, x, p);
 }
 
 template <typename K>
@@ -786,12 +802,12 @@ cudaError_t configure_small() {
 }
 template <int MODE, bool W8>
 cudaError_t configure_pair(int num_sms, int* max_pairs) {
-  const cudaError_t e = limit(pair_kernel<MODE, W8>, PairCfg::kSmem);
+  const cudaError_t e = limit(pair_kernel<MODE, W8>, PairCfg<MODE>::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(num_sms & ~1);
-  cfg.blockDim = dim3(PairCfg::kThreads);
-  cfg.dynamicSmemBytes = PairCfg::kSmem;
+  cfg.blockDim = dim3(PairCfg<MODE>::kThreads);
+  cfg.dynamicSmemBytes = PairCfg<MODE>::kSmem;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = 2;

@@ -4,6 +4,7 @@
 #include "eat_internal.cuh"
 
 #include <cuda.h>
+#include <cuda_fp8.h>
 
 namespace eat {
 
@@ -40,8 +41,10 @@ cudaError_t head_launch_small(bool w8, const CUtensorMap& w128, const CUtensorMa
 // base-2 target logit.  Gradient's first pass (exp == true): e[row][v] = exp2(l - ref) as bf16 (0 in
 // the target's column, beyond V and in rows beyond the counted tokens), part[piece][cap] its sums.
 struct HeadPairArgs {
-  int T, V, kblocks;
+  int T, V, d, kblocks;
   const int32_t* target;
+  const void* x;  // exp == false: the matrices themselves, for the target logits
+  const void* w;
   const float* xs;
   const float* ws;
   float2* part2;
@@ -82,6 +85,38 @@ cudaError_t head_configure(int num_sms, int* max_pairs);
 // outside.
 bool head_encode(CUtensorMap* m, bool w8, const void* ptr, long long rows, long long cols,
                  int box_rows);
+
+// 16 bytes of a row as floats: 8 bf16 or 16 e4m3
+template <bool W8>
+struct Vec {
+  static constexpr int kN = W8 ? 16 : 8;
+  float v[kN];
+  __device__ explicit Vec(uint4 u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (W8) {
+        __nv_fp8x4_e4m3 q;
+        q.__x = w[i];
+        const float4 f = (float4)q;
+        v[4 * i] = f.x;
+        v[4 * i + 1] = f.y;
+        v[4 * i + 2] = f.z;
+        v[4 * i + 3] = f.w;
+      } else {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
+};
+template <bool W8>
+__device__ __forceinline__ float dot16(uint4 a, uint4 b, float s) {
+  const Vec<W8> x(a), w(b);
+#pragma unroll
+  for (int i = 0; i < Vec<W8>::kN; ++i) s = fmaf(x.v[i], w.v[i], s);
+  return s;
+}
 
 // Ordered bits of a float: larger floats have larger bits, and no float has 0 (other than NaNs).
 __device__ __forceinline__ uint32_t ordered_bits(float v) {

@@ -10,6 +10,8 @@ from __future__ import annotations
 import ctypes
 import os
 
+import torch
+
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libeat.so")
 
@@ -128,14 +130,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     """The stream's handle; None: torch's current stream.  The raw query saves most of what building
     a Stream object costs the host on each call (a small call is bound by the host)."""
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is not None:
-            return raw(torch.cuda.current_device())
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream
 
@@ -320,101 +323,108 @@ def eat_head_reset(h, stream=None):
 # ------------------------------------------------------------------------------------------------
 # The operators around the layer on torch tensors (still only marshalling).  Tensors are CUDA,
 # contiguous and of the stated type; outputs are new tensors, and calls go to the current stream.
+# A small call is bound by the host, so these check and marshal with as few Python calls as they can.
 # ------------------------------------------------------------------------------------------------
-def _take(name, t, shape, *dtypes):
-    """Raise unless tensor t has this shape and one of the types, contiguous on the GPU."""
-    if tuple(t.shape) != tuple(shape) or t.dtype not in dtypes:
-        raise ValueError(f"{name}: need {tuple(shape)} of {dtypes}, got {tuple(t.shape)} {t.dtype}")
+def _take(name, t, shape, dtype):
+    """Raise unless tensor t has this shape and type, contiguous on the GPU; its address."""
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name}: need {tuple(shape)} {dtype}, got {tuple(t.shape)} {t.dtype}")
     if not (t.is_cuda and t.is_contiguous()):
         raise ValueError(f"{name}: need a contiguous CUDA tensor")
+    return t.data_ptr()
 
 
-def _xdtype(x):
-    import torch
-    if x.dim() != 2 or x.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"need [T, d] fp32 or bf16 rows, got {tuple(x.shape)} {x.dtype}")
-    return EAT_BF16 if x.dtype == torch.bfloat16 else EAT_F32
+def _take_mask(mask, T):
+    if mask is None:
+        return None
+    return _take("mask", mask, (T,), torch.uint8 if mask.dtype is torch.uint8 else torch.bool)
 
 
-def _norm_args(x, gamma, residual):
-    import torch
-    code = _xdtype(x)
-    _take("x", x, x.shape, x.dtype)
-    _take("gamma", gamma, x.shape[1:], torch.float32)
-    if residual is None:
-        return code, x
-    _take("residual", residual, x.shape, x.dtype)
-    return code, torch.empty_like(x)
+def _rows(name, x):
+    """(T, d, type code, address) of fp32 or bf16 rows [T, d]."""
+    dt = x.dtype
+    if x.dim() != 2 or (dt is not torch.bfloat16 and dt is not torch.float32):
+        raise ValueError(f"{name}: need [T, d] fp32 or bf16 rows, got {tuple(x.shape)} {dt}")
+    T, d = x.shape
+    return T, d, EAT_BF16 if dt is torch.bfloat16 else EAT_F32, _take(name, x, (T, d), dt)
+
+
+def _norm(x, gamma, eps, residual, fp8):
+    T, d, code, px = _rows("x", x)
+    pg = _take("gamma", gamma, (d,), torch.float32)
+    h, pr, ph = x, None, None
+    if residual is not None:
+        pr = _take("residual", residual, (T, d), x.dtype)
+        h = torch.empty_like(x)
+        ph = h.data_ptr()
+    if fp8:
+        y = torch.empty_like(x, dtype=torch.float8_e4m3fn)
+        scale = gamma.new_empty(T)
+        ps, ycode = scale.data_ptr(), EAT_FP8_E4M3
+    else:
+        y = torch.empty_like(x)
+        scale, ps, ycode = None, None, code
+    _check(lib().eat_rms_norm(px, pr, T, d, code, pg, eps, ph, y.data_ptr(), ycode, ps,
+                              _stream(None)))
+    return y, scale, h
 
 
 def rms_norm(x, gamma, eps=1e-6, residual=None):
     """(y, h): h = x + residual, y = RMS norm of h times gamma, both in x's type (x, residual [T, d]
     fp32 or bf16; gamma [d] fp32).  Without a residual h is x itself."""
-    import torch
-    code, h = _norm_args(x, gamma, residual)
-    y = torch.empty_like(x)
-    eat_rms_norm(x, residual, x.shape[0], x.shape[1], code, gamma, eps, h, y, code)
+    y, _, h = _norm(x, gamma, eps, residual, False)
     return y, h
 
 
 def rms_norm_fp8(x, gamma, eps=1e-6, residual=None):
     """(q, scale, h): rms_norm with y as torch.float8_e4m3fn rows q and their fp32 scales [T]."""
-    import torch
-    code, h = _norm_args(x, gamma, residual)
-    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-    scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    eat_rms_norm(x, residual, x.shape[0], x.shape[1], code, gamma, eps, h, q, EAT_FP8_E4M3, scale)
-    return q, scale, h
+    return _norm(x, gamma, eps, residual, True)
 
 
 def rms_norm_grad(h, gamma, eps, dy, dres=None):
     """(dx, dgamma) of rms_norm at its stored sum h: dx is the gradient of x and of the residual,
     dres the gradient that reaches h from the residual stream."""
-    import torch
-    code = _xdtype(h)
-    T, d = h.shape
-    _take("h", h, h.shape, h.dtype)
-    _take("gamma", gamma, (d,), torch.float32)
-    _take("dy", dy, h.shape, h.dtype)
-    if dres is not None:
-        _take("dres", dres, h.shape, h.dtype)
+    T, d, code, ph = _rows("h", h)
+    pg = _take("gamma", gamma, (d,), torch.float32)
+    py = _take("dy", dy, (T, d), h.dtype)
+    pr = None if dres is None else _take("dres", dres, (T, d), h.dtype)
+    L = lib()
     dx = torch.empty_like(h)
-    dgamma = torch.empty(d, dtype=torch.float32, device=h.device)
-    work = torch.empty(eat_rms_norm_grad_workspace(T, d), dtype=torch.uint8, device=h.device)
-    eat_rms_norm_grad(h, T, d, code, gamma, eps, dy, dres, dx, dgamma, work)
+    dgamma = torch.empty_like(gamma)
+    work = gamma.new_empty(L.eat_rms_norm_grad_workspace(T, d), dtype=torch.uint8)
+    _check(L.eat_rms_norm_grad(ph, T, d, code, pg, eps, py, pr, dx.data_ptr(), dgamma.data_ptr(),
+                               work.data_ptr(), _stream(None)))
     return dx, dgamma
 
 
 def balance_loss(logits, idx, mask=None):
     """(loss [1], counts [E] int32, n_tokens [1] int32) of router logits [T, E] fp32 and the selected
     experts idx [T, K] int32 of EatLayer.route or forward; mask [T] bool: tokens that count."""
-    import torch
-    _take("logits", logits, logits.shape[:2], torch.float32)
     T, E = logits.shape
-    _take("idx", idx, (T, idx.shape[-1]), torch.int32)
-    if mask is not None:
-        _take("mask", mask, (T,), torch.bool, torch.uint8)
-    dev = logits.device
-    loss = torch.empty(1, dtype=torch.float32, device=dev)
-    counts = torch.empty(E, dtype=torch.int32, device=dev)
-    n = torch.empty(1, dtype=torch.int32, device=dev)
-    work = torch.empty(eat_balance_workspace(T, E), dtype=torch.uint8, device=dev)
-    eat_balance_loss(logits, T, E, idx.shape[1], idx, mask, loss, counts, n, work)
+    K = idx.shape[-1]
+    pl = _take("logits", logits, (T, E), torch.float32)
+    pi = _take("idx", idx, (T, K), torch.int32)
+    pm = _take_mask(mask, T)
+    L = lib()
+    loss = logits.new_empty(1)
+    counts = idx.new_empty(E)
+    n = idx.new_empty(1)
+    work = idx.new_empty(L.eat_balance_workspace(T, E), dtype=torch.uint8)
+    _check(L.eat_balance_loss(pl, T, E, K, pi, pm, loss.data_ptr(), counts.data_ptr(),
+                              n.data_ptr(), work.data_ptr(), _stream(None)))
     return loss, counts, n
 
 
 def balance_grad(logits, counts, n_tokens, g, mask=None):
     """Gradient of balance_loss to the logits, times g (fp32 [1] on the device)."""
-    import torch
-    _take("logits", logits, logits.shape[:2], torch.float32)
     T, E = logits.shape
-    _take("counts", counts, (E,), torch.int32)
-    _take("n_tokens", n_tokens, (1,), torch.int32)
-    _take("g", g, (1,), torch.float32)
-    if mask is not None:
-        _take("mask", mask, (T,), torch.bool, torch.uint8)
+    pl = _take("logits", logits, (T, E), torch.float32)
+    pc = _take("counts", counts, (E,), torch.int32)
+    pn = _take("n_tokens", n_tokens, (1,), torch.int32)
+    pg = _take("g", g, (1,), torch.float32)
+    pm = _take_mask(mask, T)
     dlogits = torch.empty_like(logits)
-    eat_balance_grad(logits, T, E, mask, counts, n_tokens, g, dlogits)
+    _check(lib().eat_balance_grad(pl, T, E, pm, pc, pn, pg, dlogits.data_ptr(), _stream(None)))
     return dlogits
 
 
@@ -423,43 +433,41 @@ class EatHead:
     w_scale [vocab] fp32), kept referenced; grad=True (bf16) for nll_grad."""
 
     def __init__(self, w, max_tokens, w_scale=None, grad=False):
-        import torch
-        _take("w", w, w.shape[:2], torch.bfloat16, torch.float8_e4m3fn)
+        fp8 = w.dtype is torch.float8_e4m3fn
         self.V, self.d = w.shape
-        self.dtype = w.dtype
-        if w.dtype == torch.float8_e4m3fn:
-            _take("w_scale", w_scale, (self.V,), torch.float32)
+        self.dtype = torch.float8_e4m3fn if fp8 else torch.bfloat16
+        pw = _take("w", w, (self.V, self.d), self.dtype)
+        ps = _take("w_scale", w_scale, (self.V,), torch.float32) if fp8 else None
         self._keep = [w, w_scale]
-        code = EAT_BF16 if w.dtype == torch.bfloat16 else EAT_FP8_E4M3
-        self.h = eat_head_create(eat_head_desc(self.d, self.V, max_tokens, code, int(grad), _ptr(w),
-                                               _ptr(w_scale)))
-
-    def _call(self, x, target):
-        import torch
-        T = target.shape[0]
-        _take("x", x, (T, self.d), self.dtype)
-        _take("target", target, (T,), torch.int32)
-        return T, torch.empty(T, dtype=torch.float32, device=x.device), \
-            torch.empty(T, dtype=torch.float32, device=x.device)
+        self.h = eat_head_create(eat_head_desc(self.d, self.V, max_tokens,
+                                               EAT_FP8_E4M3 if fp8 else EAT_BF16, int(grad), pw, ps))
 
     def nll(self, x, target, x_scale=None):
         """(nll, lse) [T] fp32 of hidden states x [T, d] and targets [T] int32 (negative: ignored);
         x_scale [T] fp32 with an e4m3 head (rms_norm_fp8 makes both)."""
-        import torch
-        T, nll, lse = self._call(x, target)
-        if self.dtype == torch.float8_e4m3fn:
-            _take("x_scale", x_scale, (T,), torch.float32)
-        eat_head_nll(self.h, x, x_scale, T, target, nll, lse)
+        T = target.shape[0]
+        px = _take("x", x, (T, self.d), self.dtype)
+        pt = _take("target", target, (T,), torch.int32)
+        ps = None
+        if self.dtype is torch.float8_e4m3fn:
+            ps = _take("x_scale", x_scale, (T,), torch.float32)
+        nll = torch.empty_like(target, dtype=torch.float32)
+        lse = torch.empty_like(nll)
+        _check(lib().eat_head_nll(self.h, px, ps, T, pt, nll.data_ptr(), lse.data_ptr(),
+                                  _stream(None)))
         return nll, lse
 
     def nll_grad(self, x, target, g):
         """(nll, lse, dx, dw): the loss, and the gradients of sum(g * nll) to x and w (g [T] fp32)."""
-        import torch
-        T, nll, lse = self._call(x, target)
-        _take("g", g, (T,), torch.float32)
+        T = target.shape[0]
+        px = _take("x", x, (T, self.d), self.dtype)
+        pt = _take("target", target, (T,), torch.int32)
+        pg = _take("g", g, (T,), torch.float32)
+        nll, lse = torch.empty_like(g), torch.empty_like(g)
         dx = torch.empty_like(x)
         dw = torch.empty_like(self._keep[0])
-        eat_head_nll_grad(self.h, x, T, target, g, nll, lse, dx, dw)
+        _check(lib().eat_head_nll_grad(self.h, px, T, pt, pg, nll.data_ptr(), lse.data_ptr(),
+                                       dx.data_ptr(), dw.data_ptr(), _stream(None)))
         return nll, lse, dx, dw
 
     def close(self):
@@ -485,7 +493,6 @@ class EatLayer:
         """Expert weights fp32, bf16, or torch.float8_e4m3fn with ``scales`` = dict of the fp32
         per-row scale tensors (w_gate_scale, w_up_scale, w_down_scale and, with shared experts,
         ws_gate_scale, ws_up_scale, ws_down_scale)."""
-        import torch
         scales = scales or {}
         self._keep = [w_router, b_router, w_gate, w_up, w_down, ws_gate, ws_up, ws_down,
                       opd_scale] + list(scales.values())
@@ -531,7 +538,6 @@ class EatLayer:
             pass
 
     def forward(self, x, ppl_sign=0, with_routing=False):
-        import torch
         T = x.shape[0]
         y = torch.empty_like(x)
         if with_routing:
@@ -544,7 +550,6 @@ class EatLayer:
         return y
 
     def route(self, x, ppl_sign=0):
-        import torch
         T = x.shape[0]
         idx = torch.empty(T, self.K, dtype=torch.int32, device=x.device)
         w = torch.empty(T, self.K, dtype=torch.float32, device=x.device)
@@ -553,7 +558,6 @@ class EatLayer:
         return idx, w, k
 
     def accounts(self):
-        import torch
         N = torch.empty(self.E, dtype=torch.int64, device="cuda")
         P = torch.empty(self.E, dtype=torch.float64, device="cuda")
         C = torch.empty(self.E, dtype=torch.float64, device="cuda")
@@ -564,7 +568,6 @@ class EatLayer:
         eat_set_accounts(self.h, N.contiguous(), P.contiguous(), C.contiguous())
 
     def call_stats(self):
-        import torch
         n = torch.empty(self.E, dtype=torch.int32, device="cuda")
         sp = torch.empty(self.E, dtype=torch.float64, device="cuda")
         sn = torch.empty(self.E, dtype=torch.float64, device="cuda")
