@@ -327,8 +327,8 @@ eat_status eat_selftest_expire_wait(eat_handle* h, int64_t limit_ns, void* strea
  * h = x and the h argument is not written (it may be NULL).  h may alias x or residual.
  *  - ydtype == xdtype: y [T, d]; y_scale is ignored.
  *  - ydtype == EAT_FP8_E4M3: y [T, d] e4m3 bytes and y_scale [T] fp32, row t being
- *    y_scale[t] * (its bytes): y_scale[t] = max |row| / 448 (1 for an all-zero row), the format of
- *    the library's e4m3 weights and of an e4m3 head's hidden states.
+ *    y_scale[t] * (its bytes): y_scale[t] = max |row| / 448 (1, and bytes 0, where that maximum is
+ *    not above 1e-35), the format of the library's e4m3 weights and of an e4m3 head's hidden states.
  * h is rounded to xdtype when it is stored; y is computed from the unrounded fp32 sum.
  * T >= 1, 1 <= d <= 65536, eps > 0.  Any alignment of the element types is accepted. */
 eat_status eat_rms_norm(const void* x, const void* residual, int32_t T, int32_t d, int32_t xdtype,
@@ -357,7 +357,7 @@ int64_t eat_rms_norm_grad_workspace(int32_t T, int32_t d);
  *   counts or none selects an expert).
  * Outputs on the device: loss [1] fp32, counts [E] int32, n_tokens [1] int32 (= n).  Sums have a
  * fixed order.  T >= 1, 1 <= E <= 256, 1 <= K <= 16.  work: eat_balance_workspace(T, E) bytes, as
- * above. */
+ * above (calls of up to 512 tokens leave it untouched). */
 eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E, int32_t K,
                             const int32_t* idx, const uint8_t* mask, float* loss, int32_t* counts,
                             int32_t* n_tokens, void* work, void* stream);

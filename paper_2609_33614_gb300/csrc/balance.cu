@@ -1,158 +1,251 @@
 // Load-balancing loss of a router with per-expert counts, and its gradient to the logits.
 //   counts[e] = entries of idx equal to e;  f_e = counts[e] / sum counts;  p_t = softmax(logits_t)
 //   loss = E sum_e f_e (1/n) sum_t p_te;   dlogits_te = g E / n p_te (f_e - sum_j f_j p_tj)
+// Bound: latency (a router's logits are a few MB at most, which L2 holds).  A warp takes kTok tokens
+// at a time, lane l the experts l, l + 32, ..., so that the tokens' loads and shuffles overlap.
+// Counts are integers (shared-memory atomics, any order gives the same); probabilities are summed in
+// fp32 in a fixed order: a lane over its warp's tokens, the block's warps, then the blocks.
 #include "eat_internal.cuh"
 
+#include <algorithm>
 #include <string>
+#include <type_traits>
 
 namespace eat {
 
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kPer = kMaxExperts / 32;  // experts per lane
+constexpr int kTok = 4;
 constexpr int kMaxBlocks = 304;
+constexpr int kWarps = 8;       // of a block of several
+constexpr int kOneWarps = 32;   // of a block that takes the whole call
+// Calls of up to this many tokens run in one block, without partial sums in memory: 4.0 us of device
+// time at 64 x 8 and 512 x 64, where two launches took 7 and one launch less saves the host 1.6.
+constexpr int kOneBlockT = 512;
 
 __device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ float warp_max(float v) {
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
+
+// softmax of the tokens t0 .. t0 + kTok - 1 (those for which on[k]; others: all zeros)
+template <int PER>
+__device__ __forceinline__ void softmax_rows(const float* logits, long long t0, int E, int lane,
+                                             const bool (&on)[kTok], float (&p)[kTok][PER]) {
+#pragma unroll
+  for (int k = 0; k < kTok; ++k)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = i * 32 + lane;
+      p[k][i] = on[k] && e < E ? logits[(t0 + k) * E + e] : -INFINITY;
+    }
+  float m[kTok], s[kTok];
+#pragma unroll
+  for (int k = 0; k < kTok; ++k) {
+    m[k] = p[k][0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) m[k] = fmaxf(m[k], p[k][i]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) m[k] = fmaxf(m[k], __shfl_xor_sync(0xffffffffu, m[k], o));
+#pragma unroll
+  for (int k = 0; k < kTok; ++k) {
+    s[k] = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      p[k][i] = on[k] && i * 32 + lane < E ? __expf(p[k][i] - m[k]) : 0.f;
+      s[k] += p[k][i];
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+#pragma unroll
+  for (int k = 0; k < kTok; ++k) {
+    s[k] = on[k] ? 1.0f / s[k] : 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) p[k][i] *= s[k];
+  }
 }
 
-// softmax of a row of E logits; lane l holds the experts l, l + 32, ... (0 beyond E)
-__device__ __forceinline__ void row_softmax(const float* z, int E, int lane, float (&p)[kPer]) {
-  float m = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    p[i] = i * 32 + lane < E ? z[i * 32 + lane] : -INFINITY;
-    m = fmaxf(m, p[i]);
+// loss, counts and the number of counted tokens from the sums of a block's threads: thread e < E
+// has expert e's sum of p and count, n the counted tokens
+__device__ void write_loss(float s, int c, int n, int E, float2* red, float* loss, int32_t* counts,
+                           int32_t* n_tokens) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if ((int)threadIdx.x < E) counts[threadIdx.x] = c;
+  const float a = warp_sum(s * (float)c), b = warp_sum((float)c);
+  if (lane == 0) red[warp] = make_float2(a, b);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float x = 0.f, y = 0.f;
+    for (int i = 0; i < kMaxExperts / 32; ++i) {
+      x += red[i].x;
+      y += red[i].y;
+    }
+    *loss = y > 0.f ? (float)E * x / (y * (float)n) : 0.f;
+    *n_tokens = n;
   }
-  m = warp_max(m);
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    p[i] = i * 32 + lane < E ? __expf(p[i] - m) : 0.f;
-    s += p[i];
-  }
-  s = 1.0f / warp_sum(s);
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) p[i] *= s;
 }
 
-// A warp per token; part[b][e] = {sum of p, count} of block b, its last entry the tokens counted.
-__global__ void __launch_bounds__(kThreads)
-balance_part_kernel(const float* __restrict__ logits, int T, int E, int K,
-                    const int32_t* __restrict__ idx, const uint8_t* __restrict__ mask,
-                    float* __restrict__ psum, int32_t* __restrict__ cnt) {
+// With WARPS = kOneWarps one block does the whole call; else block b leaves its sums in psum[b][E]
+// and cnt[b][E + 1] (the last: the tokens counted).
+template <int PER, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS)
+balance_sum_kernel(const float* __restrict__ logits, int T, int E, int K,
+                   const int32_t* __restrict__ idx, const uint8_t* __restrict__ mask,
+                   float* __restrict__ psum, int32_t* __restrict__ cnt, float* __restrict__ loss,
+                   int32_t* __restrict__ counts, int32_t* __restrict__ n_tokens) {
   __shared__ int s_cnt[kMaxExperts + 1];
-  __shared__ float s_p[kWarps][kMaxExperts];
+  __shared__ float s_p[WARPS][32 * PER];
+  __shared__ float2 red[WARPS];
   pdl_wait();
   pdl_launch_dependents();
-  for (int i = threadIdx.x; i <= E; i += kThreads) s_cnt[i] = 0;
+  for (int i = threadIdx.x; i <= E; i += 32 * WARPS) s_cnt[i] = 0;
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float acc[kPer] = {};
-  for (int t = blockIdx.x * kWarps + warp; t < T; t += gridDim.x * kWarps) {
-    if (mask && !mask[t]) continue;
-    float p[kPer];
-    row_softmax(logits + (size_t)t * E, E, lane, p);
+  float acc[PER] = {};
+  for (long long t0 = (long long)(blockIdx.x * WARPS + warp) * kTok; t0 < T;
+       t0 += (long long)gridDim.x * WARPS * kTok) {
+    bool on[kTok];
+    int e[kTok];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] += p[i];
-    if (lane < K) {
-      const int e = idx[(size_t)t * K + lane];
-      if (e >= 0 && e < E) atomicAdd(&s_cnt[e], 1);
+    for (int k = 0; k < kTok; ++k) {
+      on[k] = t0 + k < T && !(mask && !mask[t0 + k]);
+      e[k] = on[k] && lane < K ? idx[(t0 + k) * K + lane] : -1;
     }
-    if (lane == 0) atomicAdd(&s_cnt[E], 1);
+    float p[kTok][PER];
+    softmax_rows<PER>(logits, t0, E, lane, on, p);
+#pragma unroll
+    for (int k = 0; k < kTok; ++k) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) acc[i] += p[k][i];
+      if (e[k] >= 0 && e[k] < E) atomicAdd(&s_cnt[e[k]], 1);
+    }
+    if (lane == 0) atomicAdd(&s_cnt[E], (int)on[0] + (int)on[1] + (int)on[2] + (int)on[3]);
   }
 #pragma unroll
-  for (int i = 0; i < kPer; ++i)
-    if (i * 32 + lane < E) s_p[warp][i * 32 + lane] = acc[i];
+  for (int i = 0; i < PER; ++i) s_p[warp][i * 32 + lane] = acc[i];
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += kThreads) {
-    float s = 0.f;
-    for (int w = 0; w < kWarps; ++w) s += s_p[w][e];
-    psum[(size_t)blockIdx.x * E + e] = s;
+  const int e = threadIdx.x;
+  float s = 0.f;
+  if (e < E) {
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) s += s_p[w][e];
   }
-  for (int e = threadIdx.x; e <= E; e += kThreads)
-    cnt[(size_t)blockIdx.x * (E + 1) + e] = s_cnt[e];
+  if (WARPS == kOneWarps) {
+    write_loss(s, e < E ? s_cnt[e] : 0, s_cnt[E], E, red, loss, counts, n_tokens);
+  } else {
+    if (e < E) psum[(size_t)blockIdx.x * E + e] = s;
+    for (int i = e; i <= E; i += 32 * WARPS) cnt[(size_t)blockIdx.x * (E + 1) + i] = s_cnt[i];
+  }
 }
 
-__global__ void __launch_bounds__(kThreads)
+// The blocks' sums joined: a warp takes every 32nd block, its lanes the experts.
+template <int PER>
+__global__ void __launch_bounds__(32 * kOneWarps)
 balance_join_kernel(const float* __restrict__ psum, const int32_t* __restrict__ cnt, int parts,
                     int E, float* __restrict__ loss, int32_t* __restrict__ counts,
                     int32_t* __restrict__ n_tokens) {
-  __shared__ float red[kThreads];
-  __shared__ float red_c[kThreads];
-  __shared__ int s_n;
+  __shared__ float s_p[kOneWarps][32 * PER];
+  __shared__ int s_cnt[32 * PER], s_n;
+  __shared__ float2 red[kOneWarps];
   pdl_wait();
-  float s = 0.f;
-  int c = 0;
-  const int e = threadIdx.x;
-  if (e < E) {
-    for (int b = 0; b < parts; ++b) {
-      s += psum[(size_t)b * E + e];
-      c += cnt[(size_t)b * (E + 1) + e];
-    }
-    counts[e] = c;
-  }
-  if (threadIdx.x == 0) {
-    int n = 0;
-    for (int b = 0; b < parts; ++b) n += cnt[(size_t)b * (E + 1) + E];
-    s_n = n;
-    *n_tokens = n;
-  }
-  red[threadIdx.x] = s * (float)c;
-  red_c[threadIdx.x] = (float)c;
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x < 32 * PER) s_cnt[threadIdx.x] = 0;
+  if (threadIdx.x == 0) s_n = 0;
   __syncthreads();
-  for (int w = kThreads / 2; w > 0; w >>= 1) {
-    if (threadIdx.x < w) {
-      red[threadIdx.x] += red[threadIdx.x + w];
-      red_c[threadIdx.x] += red_c[threadIdx.x + w];
+  float s[PER] = {};
+  int c[PER] = {}, n = 0;
+#pragma unroll 4
+  for (int b = warp; b < parts; b += kOneWarps) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = i * 32 + lane;
+      if (e < E) {
+        s[i] += psum[(size_t)b * E + e];
+        c[i] += cnt[(size_t)b * (E + 1) + e];
+      }
     }
-    __syncthreads();
+    if (lane == 0) n += cnt[(size_t)b * (E + 1) + E];
   }
-  if (threadIdx.x == 0)
-    *loss = red_c[0] > 0.f ? (float)E * red[0] / (red_c[0] * (float)s_n) : 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    s_p[warp][i * 32 + lane] = s[i];
+    if (c[i]) atomicAdd(&s_cnt[i * 32 + lane], c[i]);
+  }
+  if (lane == 0) atomicAdd(&s_n, n);
+  __syncthreads();
+  float sum = 0.f;
+  if ((int)threadIdx.x < E) {
+#pragma unroll
+    for (int w = 0; w < kOneWarps; ++w) sum += s_p[w][threadIdx.x];
+  }
+  write_loss(sum, (int)threadIdx.x < E ? s_cnt[threadIdx.x] : 0, s_n, E, red, loss, counts,
+             n_tokens);
 }
 
-__global__ void __launch_bounds__(kThreads)
+template <int PER>
+__global__ void __launch_bounds__(32 * kWarps)
 balance_grad_kernel(const float* logits, int T, int E, const uint8_t* __restrict__ mask,
                     const int32_t* __restrict__ counts, const int32_t* __restrict__ n_tokens,
                     const float* __restrict__ g, float* dlogits) {
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float f[kPer], total = 0.f;
+  float f[PER], total = 0.f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     f[i] = i * 32 + lane < E ? (float)counts[i * 32 + lane] : 0.f;
     total += f[i];
   }
   total = warp_sum(total);
-  const float scale = total > 0.f ? *g * (float)E / ((float)*n_tokens) : 0.f;
+  const float scale = total > 0.f ? *g * (float)E / (float)*n_tokens : 0.f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) f[i] = total > 0.f ? f[i] / total : 0.f;
-  for (int t = blockIdx.x * kWarps + warp; t < T; t += gridDim.x * kWarps) {
-    const bool on = total > 0.f && !(mask && !mask[t]);
-    float p[kPer], dot = 0.f;
-    row_softmax(logits + (size_t)t * E, E, lane, p);
+  for (int i = 0; i < PER; ++i) f[i] = total > 0.f ? f[i] / total : 0.f;
+  for (long long t0 = (long long)(blockIdx.x * kWarps + warp) * kTok; t0 < T;
+       t0 += (long long)gridDim.x * kWarps * kTok) {
+    bool on[kTok];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) dot += f[i] * p[i];
-    dot = warp_sum(dot);
+    for (int k = 0; k < kTok; ++k)
+      on[k] = t0 + k < T && total > 0.f && !(mask && !mask[t0 + k]);
+    float p[kTok][PER], dot[kTok];
+    softmax_rows<PER>(logits, t0, E, lane, on, p);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (i * 32 + lane < E)
-        dlogits[(size_t)t * E + i * 32 + lane] = on ? scale * p[i] * (f[i] - dot) : 0.f;
+    for (int k = 0; k < kTok; ++k) {
+      dot[k] = 0.f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) dot[k] = fmaf(f[i], p[k][i], dot[k]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < kTok; ++k) dot[k] += __shfl_xor_sync(0xffffffffu, dot[k], o);
+#pragma unroll
+    for (int k = 0; k < kTok; ++k)
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (t0 + k < T && i * 32 + lane < E)
+          dlogits[(t0 + k) * E + i * 32 + lane] = on[k] ? scale * p[k][i] * (f[i] - dot[k]) : 0.f;
   }
 }
 
-int part_blocks(int T) {
-  const int b = (T + kWarps - 1) / kWarps;
-  return b < kMaxBlocks ? b : kMaxBlocks;
+int sum_blocks(int T) {
+  return std::min((int)(((long long)T + kWarps * kTok - 1) / (kWarps * kTok)), kMaxBlocks);
+}
+
+// go(PER): experts per lane
+template <typename F>
+cudaError_t pick_per(int E, F&& go) {
+  if (E <= 32) return go(std::integral_constant<int, 1>());
+  if (E <= 64) return go(std::integral_constant<int, 2>());
+  if (E <= 128) return go(std::integral_constant<int, 4>());
+  return go(std::integral_constant<int, 8>());
 }
 
 eat_status bad(const char* fn, const char* what) {
@@ -172,7 +265,8 @@ bool misaligned(const void* p, int n) { return ((uintptr_t)p & (uintptr_t)(n - 1
 using namespace eat;
 
 extern "C" int64_t eat_balance_workspace(int32_t T, int32_t E) {
-  return T < 1 || E < 1 ? 0 : (int64_t)part_blocks(T) * (2 * E + 1) * 4;
+  if (T < 1 || E < 1) return 0;
+  return T <= kOneBlockT ? 16 : (int64_t)sum_blocks(T) * (2 * E + 1) * 4;
 }
 
 extern "C" eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E, int32_t K,
@@ -188,15 +282,24 @@ extern "C" eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E
       misaligned(counts, 4) || misaligned(n_tokens, 4) || misaligned(work, 16))
     return bad(fn, "misaligned pointer");
   const cudaStream_t st = (cudaStream_t)stream;
-  const int parts = part_blocks(T);
+  if (T <= kOneBlockT)
+    return launched(fn, pick_per(E, [&](auto per) {
+      return launch_pdl(balance_sum_kernel<decltype(per)::value, kOneWarps>, dim3(1),
+                        dim3(32 * kOneWarps), 0, st, logits, T, E, K, idx, mask, (float*)nullptr,
+                        (int32_t*)nullptr, loss, counts, n_tokens);
+    }));
+  const int parts = sum_blocks(T);
   float* psum = (float*)work;
   int32_t* cnt = (int32_t*)(psum + (size_t)parts * E);
-  cudaError_t e = launch_pdl(balance_part_kernel, dim3(parts), dim3(kThreads), 0, st, logits, T, E,
-                             K, idx, mask, psum, cnt);
-  if (e == cudaSuccess)
-    e = launch_pdl(balance_join_kernel, dim3(1), dim3(kThreads), 0, st, (const float*)psum,
-                   (const int32_t*)cnt, parts, E, loss, counts, n_tokens);
-  return launched(fn, e);
+  return launched(fn, pick_per(E, [&](auto per) {
+    constexpr int PER = decltype(per)::value;
+    const cudaError_t e =
+        launch_pdl(balance_sum_kernel<PER, kWarps>, dim3(parts), dim3(32 * kWarps), 0, st, logits,
+                   T, E, K, idx, mask, psum, cnt, loss, counts, n_tokens);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(balance_join_kernel<PER>, dim3(1), dim3(32 * kOneWarps), 0, st,
+                      (const float*)psum, (const int32_t*)cnt, parts, E, loss, counts, n_tokens);
+  }));
 }
 
 extern "C" eat_status eat_balance_grad(const float* logits, int32_t T, int32_t E,
@@ -210,7 +313,9 @@ extern "C" eat_status eat_balance_grad(const float* logits, int32_t T, int32_t E
   if (misaligned(logits, 4) || misaligned(counts, 4) || misaligned(n_tokens, 4) ||
       misaligned(g, 4) || misaligned(dlogits, 4))
     return bad(fn, "misaligned pointer");
-  return launched(fn, launch_pdl(balance_grad_kernel, dim3(part_blocks(T)), dim3(kThreads), 0,
-                                 (cudaStream_t)stream, logits, T, E, mask, counts, n_tokens, g,
-                                 dlogits));
+  return launched(fn, pick_per(E, [&](auto per) {
+    return launch_pdl(balance_grad_kernel<decltype(per)::value>, dim3(sum_blocks(T)),
+                      dim3(32 * kWarps), 0, (cudaStream_t)stream, logits, T, E, mask, counts,
+                      n_tokens, g, dlogits);
+  }));
 }

@@ -2,120 +2,436 @@
 // and its gradient.
 //   h = x + r;  rstd = 1 / sqrt(sum h^2 / d + eps);  y = h rstd gamma
 //   e4m3: s = max |y| / 448, q = round(y / s).  max |y| = rstd max |h gamma|, so the row's sum of
-//   squares and its maximum come out of one reduction and y / s = (h gamma) (448 / max |h gamma|).
+//   squares and its maximum come out of one reduction and y / s = (h gamma) (rstd / s).
 //   gradient, n = h rstd:  dx = dres + rstd (gamma dy - n mean(gamma dy n));  dgamma = sum_t dy n
+// Bound: HBM (a row is read once and kept in registers between the reduction and the outputs).
+// A thread holds NV vectors of 16 bytes of a row; a row is taken by a warp (up to 128 vectors) or by
+// a block of 256 threads.  Rows whose length is no multiple of a vector begin at any element: their
+// vectors are the aligned ones of memory, and the first and the last of a row are partial.  All
+// sums are fp32; a value is rounded once, when it is stored.
 #include "eat_internal.cuh"
 
 #include <cuda_fp8.h>
 
+#include <algorithm>
 #include <string>
+#include <type_traits>
 
 namespace eat {
 
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+// e4m3 rows whose largest value is not above this get the scale 1 (and bytes 0): max / 448 and its
+// reciprocal stay away from fp32's ends
+constexpr float kTiny = 1e-35f;
 
 template <typename T>
-__device__ __forceinline__ float to_f(T v);
+struct Elem;
 template <>
-__device__ __forceinline__ float to_f(float v) { return v; }
+struct Elem<float> {
+  static constexpr int kN = 4;  // elements of 16 bytes
+  static __device__ __forceinline__ float get(float v) { return v; }
+  static __device__ __forceinline__ float put(float v) { return v; }
+  static __device__ __forceinline__ void unpack(uint4 u, float* v) {
+    v[0] = __uint_as_float(u.x);
+    v[1] = __uint_as_float(u.y);
+    v[2] = __uint_as_float(u.z);
+    v[3] = __uint_as_float(u.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float* v) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                      __float_as_uint(v[3]));
+  }
+};
 template <>
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <typename T>
-__device__ __forceinline__ T from_f(float v);
-template <>
-__device__ __forceinline__ float from_f(float v) { return v; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
+struct Elem<__nv_bfloat16> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+  static __device__ __forceinline__ void unpack(uint4 u, float* v) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float* v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *(const uint32_t*)&b;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
 
-// Sum and maximum over the block, in every thread.
-__device__ float2 block_sum_max(float s, float m) {
-  __shared__ float2 red[kThreads / 32];
-  for (int o = 16; o > 0; o >>= 1) {
-    s += __shfl_xor_sync(0xffffffffu, s, o);
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+// Elements [c, c + kN) of a row of d elements as they lie in memory; with ALIGNED the row begins at
+// a vector and c never leaves it, else elements outside the row are 0.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ uint4 load_vec(const T* row, int c, int d) {
+  constexpr int N = Elem<T>::kN;
+  if (ALIGNED || (c >= 0 && c + N <= d)) return *(const uint4*)(row + c);
+  union {
+    uint4 u;
+    T e[N];
+  } v;
+  v.u = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (c + j >= 0 && c + j < d) v.e[j] = row[c + j];
+  return v.u;
+}
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void store_vec(T* row, int c, int d, const float* v) {
+  constexpr int N = Elem<T>::kN;
+  if (ALIGNED || (c >= 0 && c + N <= d)) {
+    *(uint4*)(row + c) = Elem<T>::pack(v);
+    return;
   }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_float2(s, m);
-  __syncthreads();
-  s = 0.f;
-  m = 0.f;
-  for (int i = 0; i < kThreads / 32; ++i) {
-    s += red[i].x;
-    m = fmaxf(m, red[i].y);
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (c + j >= 0 && c + j < d) row[c + j] = Elem<T>::put(v[j]);
+}
+template <int N, bool ALIGNED>
+__device__ __forceinline__ void load_gamma(const float* g, int c, int d, float* v) {
+  if (ALIGNED) {
+#pragma unroll
+    for (int j = 0; j < N; j += 4) *(float4*)(v + j) = __ldg((const float4*)(g + c + j));
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = c + j >= 0 && c + j < d ? __ldg(g + c + j) : 0.f;
   }
-  return make_float2(s, m);
 }
 
-// One block per row.
-template <typename T, bool F8>
+// Sums (or maxima) over the threads of a row, in every one of them.  ROW threads: 32 or the block;
+// `red` alternates between two buffers, so one barrier per row is enough.
+template <int ROW, bool MAX>
+__device__ __forceinline__ float2 row_reduce(float a, float b, float2 (*red)[kWarps], int turn) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a += __shfl_xor_sync(0xffffffffu, a, o);
+    const float b2 = __shfl_xor_sync(0xffffffffu, b, o);
+    b = MAX ? fmaxf(b, b2) : b + b2;
+  }
+  if (ROW == 32) return make_float2(a, b);
+  if ((threadIdx.x & 31) == 0) red[turn & 1][threadIdx.x >> 5] = make_float2(a, b);
+  __syncthreads();
+  float2 s = red[turn & 1][0];
+#pragma unroll
+  for (int i = 1; i < kWarps; ++i) {
+    const float2 q = red[turn & 1][i];
+    s.x += q.x;
+    s.y = MAX ? fmaxf(s.y, q.y) : s.y + q.y;
+  }
+  return s;
+}
+
+template <typename T, bool F8, int ROW, int NV, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads)
-rms_norm_kernel(const T* __restrict__ x, const T* r, int d, const float* __restrict__ gamma,
-                float eps, T* h, void* y, float* __restrict__ y_scale) {
+rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict__ gamma, float eps,
+                T* h, void* y, float* __restrict__ y_scale) {
+  constexpr int N = Elem<T>::kN;
+  __shared__ float2 red[2][kWarps];
   pdl_wait();
   pdl_launch_dependents();
-  const size_t row = (size_t)blockIdx.x * d;
-  float ss = 0.f, mx = 0.f;
-  for (int c = threadIdx.x; c < d; c += kThreads) {
-    const float v = to_f(x[row + c]) + (r ? to_f(r[row + c]) : 0.f);
-    ss += v * v;
-    mx = fmaxf(mx, fabsf(v * gamma[c]));
+  const int t = ROW == 32 ? blockIdx.x * kWarps + (threadIdx.x >> 5) : blockIdx.x;
+  if (t >= rows) return;
+  const int lane = ROW == 32 ? threadIdx.x & 31 : threadIdx.x;
+  const size_t at = (size_t)t * d;
+  const int shift = ALIGNED ? 0 : (int)(at % N);
+  uint4 ux[NV], ur[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (lane + i * ROW) * N - shift;
+    if (c < d) {
+      ux[i] = load_vec<T, ALIGNED>(x + at, c, d);
+      if (r) ur[i] = load_vec<T, ALIGNED>(r + at, c, d);
+    }
   }
-  const float2 a = block_sum_max(ss, mx);
+  float v[NV][N];
+  float ss = 0.f, top = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (lane + i * ROW) * N - shift;
+    if (c < d) {
+      Elem<T>::unpack(ux[i], v[i]);
+      if (r) {
+        float w[N];
+        Elem<T>::unpack(ur[i], w);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[i][j] += w[j];
+        store_vec<T, ALIGNED>(h + at, c, d, v[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+      float g[N];
+      load_gamma<N, ALIGNED>(gamma, c, d, g);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        v[i][j] *= g[j];
+        if (F8) top = fmaxf(top, fabsf(v[i][j]));
+      }
+    }
+  }
+  const float2 a = row_reduce<ROW, true>(ss, top, red, 0);
   const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
-  const float top = a.y * rstd;
-  const float scale = top > 0.f ? top / 448.0f : 1.0f;
-  for (int c = threadIdx.x; c < d; c += kThreads) {
-    const float v = to_f(x[row + c]) + (r ? to_f(r[row + c]) : 0.f);
-    if (r) h[row + c] = from_f<T>(v);
-    const float o = v * rstd * gamma[c];
-    if (F8) ((__nv_fp8_e4m3*)y)[row + c] = __nv_fp8_e4m3(o / scale);
-    else ((T*)y)[row + c] = from_f<T>(o);
+  float k = rstd;
+  if (F8) {
+    const float m = a.y * rstd, scale = m > kTiny ? m / 448.0f : 1.0f;
+    k = rstd / scale;
+    if (lane == 0) y_scale[t] = scale;
   }
-  if (F8 && threadIdx.x == 0) y_scale[blockIdx.x] = scale;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (lane + i * ROW) * N - shift;
+    if (c < d) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[i][j] *= k;
+      if (!F8) {
+        store_vec<T, ALIGNED>((T*)y + at, c, d, v[i]);
+      } else {
+        uint32_t q[N / 4];
+#pragma unroll
+        for (int j = 0; j < N; j += 4)
+          q[j / 4] = __nv_fp8x4_e4m3(make_float4(v[i][j], v[i][j + 1], v[i][j + 2], v[i][j + 3])).__x;
+        uint8_t* o = (uint8_t*)y + at + c;
+        if (ALIGNED && N == 8) {
+          *(uint2*)o = make_uint2(q[0], q[N / 4 - 1]);
+        } else if (ALIGNED) {
+          *(uint32_t*)o = q[0];
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (c + j >= 0 && c + j < d) o[j] = (uint8_t)(q[j / 4] >> (8 * (j & 3)));
+        }
+      }
+    }
+  }
 }
 
-// Block b takes rows b, b + gridDim.x, ...: dx of each row, and the block's part of dgamma
-// (part[b], every column of which belongs to one thread).
-template <typename T>
+// Group b of threads (a warp or the block) takes rows b, b + groups, ... (the number of groups is a
+// multiple of a vector's elements, so these rows begin alike): dx, and in registers the group's sum of
+// dy n, which the block adds up and leaves in part[block].
+template <typename T, int ROW, int NV, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads)
 rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __restrict__ gamma,
                      float eps, const T* dy, const T* dres, T* dx, float* __restrict__ part) {
+  constexpr int N = Elem<T>::kN;
+  constexpr int kGroups = kThreads / ROW;  // per block
+  __shared__ float2 red[2][kWarps];
+  extern __shared__ float s_part[];        // warps' sums: [kWarps][d] (ROW == 32)
   pdl_wait();
   pdl_launch_dependents();
-  float* mine = part + (size_t)blockIdx.x * d;
-  for (int t = blockIdx.x; t < rows; t += gridDim.x) {
-    const size_t row = (size_t)t * d;
-    float ss = 0.f, dot = 0.f;
-    for (int c = threadIdx.x; c < d; c += kThreads) {
-      const float v = to_f(h[row + c]);
-      ss += v * v;
-      dot += gamma[c] * to_f(dy[row + c]) * v;
+  const int lane = ROW == 32 ? threadIdx.x & 31 : threadIdx.x;
+  const int t0 = blockIdx.x * kGroups + (ROW == 32 ? threadIdx.x >> 5 : 0);
+  const int step = gridDim.x * kGroups;
+  const int shift = ALIGNED ? 0 : (int)((size_t)t0 * d % N);
+  float acc[NV][N];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
+  int turn = 0;
+  for (int t = t0; t < rows; t += step, ++turn) {
+    const size_t at = (size_t)t * d;
+    uint4 uh[NV], ug[NV], ur[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * ROW) * N - shift;
+      if (c < d) {
+        uh[i] = load_vec<T, ALIGNED>(h + at, c, d);
+        ug[i] = load_vec<T, ALIGNED>(dy + at, c, d);
+        if (dres) ur[i] = load_vec<T, ALIGNED>(dres + at, c, d);
+      }
     }
-    const float rstd = 1.0f / sqrtf(block_sum_max(ss, 0.f).x / (float)d + eps);
-    const float m = block_sum_max(dot, 0.f).x * rstd / (float)d;
+    float ss = 0.f, dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * ROW) * N - shift;
+      if (c < d) {
+        float v[N], w[N], g[N];
+        Elem<T>::unpack(uh[i], v);
+        Elem<T>::unpack(ug[i], w);
+        load_gamma<N, ALIGNED>(gamma, c, d, g);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          ss = fmaf(v[j], v[j], ss);
+          dot = fmaf(g[j] * w[j], v[j], dot);
+        }
+      }
+    }
+    const float2 a = row_reduce<ROW, false>(ss, dot, red, turn);
+    const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
+    const float m = a.y * rstd / (float)d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * ROW) * N - shift;
+      if (c < d) {
+        float v[N], w[N], g[N], o[N];
+        Elem<T>::unpack(uh[i], v);
+        Elem<T>::unpack(ug[i], w);
+        load_gamma<N, ALIGNED>(gamma, c, d, g);
+        if (dres) Elem<T>::unpack(ur[i], o);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float n = v[j] * rstd;
+          acc[i][j] = fmaf(w[j], n, acc[i][j]);
+          const float k = rstd * (g[j] * w[j] - n * m);
+          o[j] = dres ? o[j] + k : k;
+        }
+        store_vec<T, ALIGNED>(dx + at, c, d, o);
+      }
+    }
+  }
+  float* mine = part + (size_t)blockIdx.x * d;
+  if (ROW == 32) {
+    float* w = s_part + (threadIdx.x >> 5) * d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int c = (lane + i * ROW) * N - shift + j;
+        if (c >= 0 && c < d) w[c] = acc[i][j];
+      }
+    __syncthreads();
     for (int c = threadIdx.x; c < d; c += kThreads) {
-      const float n = to_f(h[row + c]) * rstd, g = to_f(dy[row + c]);
-      mine[c] = (t == (int)blockIdx.x ? 0.f : mine[c]) + g * n;
-      const float v = rstd * (gamma[c] * g - n * m);
-      dx[row + c] = from_f<T>(v + (dres ? to_f(dres[row + c]) : 0.f));
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) s += s_part[i * d + c];
+      mine[c] = s;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * ROW) * N - shift;
+      if (ALIGNED) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4)
+          if (c < d) *(uint4*)(mine + c + j) = Elem<float>::pack(acc[i] + j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (c + j >= 0 && c + j < d) mine[c + j] = acc[i][j];
+      }
     }
   }
 }
 
+// Rows that no vector kernel takes: a block per row, element by element, reading the row twice.
+template <typename T, bool F8>
 __global__ void __launch_bounds__(kThreads)
-rms_norm_dgamma_kernel(const float* __restrict__ part, int n_parts, int d,
-                       float* __restrict__ dgamma) {
+rms_norm_any_kernel(const T* x, const T* r, int d, const float* __restrict__ gamma, float eps, T* h,
+                    void* y, float* __restrict__ y_scale) {
+  __shared__ float2 red[2][kWarps];
   pdl_wait();
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= d) return;
-  float s = 0.f;
-  for (int i = 0; i < n_parts; ++i) s += part[(size_t)i * d + c];
-  dgamma[c] = s;
+  pdl_launch_dependents();
+  const size_t row = (size_t)blockIdx.x * d;
+  auto sum = [&](int c) {
+    return Elem<T>::get(x[row + c]) + (r ? Elem<T>::get(r[row + c]) : 0.f);
+  };
+  float ss = 0.f, top = 0.f;
+  for (int c = threadIdx.x; c < d; c += kThreads) {
+    const float v = sum(c);
+    ss = fmaf(v, v, ss);
+    top = fmaxf(top, fabsf(v * gamma[c]));
+  }
+  const float2 a = row_reduce<kThreads, true>(ss, top, red, 0);
+  const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
+  const float m = a.y * rstd, scale = m > kTiny ? m / 448.0f : 1.0f;
+  const float k = F8 ? rstd / scale : rstd;
+  for (int c = threadIdx.x; c < d; c += kThreads) {
+    const float v = sum(c);
+    if (r) h[row + c] = Elem<T>::put(v);
+    const float o = v * gamma[c] * k;
+    if (F8) ((__nv_fp8_e4m3*)y)[row + c] = __nv_fp8_e4m3(o);
+    else ((T*)y)[row + c] = Elem<T>::put(o);
+  }
+  if (F8 && threadIdx.x == 0) y_scale[blockIdx.x] = scale;
+}
+// Block b takes rows b, b + gridDim.x, ...; every column of part[b] belongs to one thread.
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+rms_norm_grad_any_kernel(const T* __restrict__ h, int rows, int d, const float* __restrict__ gamma,
+                         float eps, const T* dy, const T* dres, T* dx, float* __restrict__ part) {
+  __shared__ float2 red[2][kWarps];
+  pdl_wait();
+  pdl_launch_dependents();
+  float* mine = part + (size_t)blockIdx.x * d;
+  int turn = 0;
+  for (int t = blockIdx.x; t < rows; t += gridDim.x, ++turn) {
+    const size_t row = (size_t)t * d;
+    float ss = 0.f, dot = 0.f;
+    for (int c = threadIdx.x; c < d; c += kThreads) {
+      const float v = Elem<T>::get(h[row + c]);
+      ss = fmaf(v, v, ss);
+      dot = fmaf(gamma[c] * Elem<T>::get(dy[row + c]), v, dot);
+    }
+    const float2 a = row_reduce<kThreads, false>(ss, dot, red, turn);
+    const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
+    const float m = a.y * rstd / (float)d;
+    for (int c = threadIdx.x; c < d; c += kThreads) {
+      const float n = Elem<T>::get(h[row + c]) * rstd, g = Elem<T>::get(dy[row + c]);
+      mine[c] = fmaf(g, n, turn ? mine[c] : 0.f);
+      const float v = rstd * (gamma[c] * g - n * m);
+      dx[row + c] = Elem<T>::put(dres ? Elem<T>::get(dres[row + c]) + v : v);
+    }
+  }
 }
 
-int grad_blocks(int T) { return T < 608 ? T : 608; }
+// dgamma: 32 columns per block, its warps over the blocks' sums, added in a fixed order.
+__global__ void __launch_bounds__(1024)
+rms_norm_dgamma_kernel(const float* __restrict__ part, int n_parts, int d,
+                       float* __restrict__ dgamma) {
+  __shared__ float s_w[32][33];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int c = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < d) {
+#pragma unroll 8
+    for (int i = warp; i < n_parts; i += 32) s += part[(size_t)i * d + c];
+  }
+  s_w[warp][lane] = s;
+  __syncthreads();
+  s = s_w[lane][warp];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0 && blockIdx.x * 32 + warp < d) dgamma[blockIdx.x * 32 + warp] = s;
+}
+
+// Blocks of the gradient's first kernel: at most four per SM of this chip (152), a multiple of a
+// vector's elements unless every group has one row.
+constexpr int kGradBlocks = 608;
+int grad_blocks(int T, int groups) { return std::min((T + groups - 1) / groups, kGradBlocks); }
+
+// The kernel for rows of d elements of type E in memory aligned to vectors: pick(ROW, NV, ALIGNED)
+// with the constants as types; false when no vector kernel takes the row.
+template <typename E, typename F>
+bool pick_rows(int d, F&& pick) {
+  constexpr int N = Elem<E>::kN;
+  const bool aligned = d % N == 0;
+  const int vecs = aligned ? d / N : (d + 2 * N - 2) / N;  // of a row that begins anywhere
+  auto go = [&](auto row, auto nv) {
+    if (aligned) pick(row, nv, std::true_type());
+    else pick(row, nv, std::false_type());
+    return true;
+  };
+  using R32 = std::integral_constant<int, 32>;
+  using R256 = std::integral_constant<int, kThreads>;
+  if (vecs <= 32) return go(R32(), std::integral_constant<int, 1>());
+  if (vecs <= 64) return go(R32(), std::integral_constant<int, 2>());
+  if (vecs <= 128) return go(R32(), std::integral_constant<int, 4>());
+  if (vecs <= 256) return go(R256(), std::integral_constant<int, 1>());
+  if (vecs <= 512) return go(R256(), std::integral_constant<int, 2>());
+  if (vecs <= 1024) return go(R256(), std::integral_constant<int, 4>());
+  if (vecs <= 2048) return go(R256(), std::integral_constant<int, 8>());
+  return false;
+}
 
 eat_status bad(const char* fn, const char* what) {
   set_thread_error((std::string(fn) + ": " + what).c_str());
@@ -149,23 +465,36 @@ extern "C" eat_status eat_rms_norm(const void* x, const void* residual, int32_t 
   if (misaligned(x, al) || misaligned(residual, al) || (residual && misaligned(h, al)) ||
       misaligned(gamma, 4) || (ydtype == EAT_FP8_E4M3 ? misaligned(y_scale, 4) : misaligned(y, al)))
     return bad(fn, "misaligned pointer");
+  const bool vec = !(misaligned(x, 16) || misaligned(residual, 16) || misaligned(gamma, 16) ||
+                     misaligned(y, 16) || (residual && misaligned(h, 16)));
+  const cudaStream_t st = (cudaStream_t)stream;
   auto run = [&](auto* tag, auto f8) {
     using E = std::remove_pointer_t<decltype(tag)>;
-    return launch_pdl(rms_norm_kernel<E, decltype(f8)::value>, dim3(T), dim3(kThreads), 0,
-                      (cudaStream_t)stream, (const E*)x, (const E*)residual, d, gamma, (float)eps,
-                      (E*)h, y, y_scale);
+    constexpr bool F8 = decltype(f8)::value;
+    cudaError_t e = cudaSuccess;
+    if (vec && pick_rows<E>(d, [&](auto row, auto nv, auto al) {
+          constexpr int ROW = decltype(row)::value;
+          const unsigned blocks = ROW == 32 ? ((unsigned)T + kWarps - 1) / kWarps : (unsigned)T;
+          e = launch_pdl(rms_norm_kernel<E, F8, ROW, decltype(nv)::value, decltype(al)::value>,
+                         dim3(blocks), dim3(kThreads), 0, st, (const E*)x, (const E*)residual, T, d,
+                         gamma, (float)eps, (E*)h, y, y_scale);
+        }))
+      return e;
+    return launch_pdl(rms_norm_any_kernel<E, F8>, dim3(T), dim3(kThreads), 0, st, (const E*)x,
+                      (const E*)residual, d, gamma, (float)eps, (E*)h, y, y_scale);
   };
   const bool f8 = ydtype == EAT_FP8_E4M3;
   cudaError_t e;
   if (xdtype == EAT_BF16)
-    e = f8 ? run((__nv_bfloat16*)nullptr, std::true_type()) : run((__nv_bfloat16*)nullptr, std::false_type());
+    e = f8 ? run((__nv_bfloat16*)nullptr, std::true_type())
+           : run((__nv_bfloat16*)nullptr, std::false_type());
   else
     e = f8 ? run((float*)nullptr, std::true_type()) : run((float*)nullptr, std::false_type());
   return launched(fn, e);
 }
 
 extern "C" int64_t eat_rms_norm_grad_workspace(int32_t T, int32_t d) {
-  return T < 1 || d < 1 ? 0 : (int64_t)grad_blocks(T) * d * 4;
+  return T < 1 || d < 1 ? 0 : (int64_t)grad_blocks(T, 1) * d * 4;
 }
 
 extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int32_t xdtype,
@@ -183,15 +512,25 @@ extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int
       misaligned(gamma, 4) || misaligned(dgamma, 4) || misaligned(work, 16))
     return bad(fn, "misaligned pointer");
   const cudaStream_t st = (cudaStream_t)stream;
+  const bool vec = !(misaligned(h, 16) || misaligned(dy, 16) || misaligned(dres, 16) ||
+                     misaligned(dx, 16) || misaligned(gamma, 16));
   auto run = [&](auto* tag) {
     using E = std::remove_pointer_t<decltype(tag)>;
-    const int blocks = grad_blocks(T);
-    cudaError_t e = launch_pdl(rms_norm_grad_kernel<E>, dim3(blocks), dim3(kThreads), 0, st,
-                               (const E*)h, T, d, gamma, (float)eps, (const E*)dy, (const E*)dres,
-                               (E*)dx, (float*)work);
+    cudaError_t e = cudaSuccess;
+    int blocks = grad_blocks(T, 1);
+    if (!(vec && pick_rows<E>(d, [&](auto row, auto nv, auto al) {
+            constexpr int ROW = decltype(row)::value;
+            blocks = grad_blocks(T, kThreads / ROW);
+            e = launch_pdl(rms_norm_grad_kernel<E, ROW, decltype(nv)::value, decltype(al)::value>,
+                           dim3(blocks), dim3(kThreads), ROW == 32 ? (size_t)kWarps * d * 4 : 0, st,
+                           (const E*)h, T, d, gamma, (float)eps, (const E*)dy, (const E*)dres,
+                           (E*)dx, (float*)work);
+          })))
+      e = launch_pdl(rms_norm_grad_any_kernel<E>, dim3(blocks), dim3(kThreads), 0, st, (const E*)h,
+                     T, d, gamma, (float)eps, (const E*)dy, (const E*)dres, (E*)dx, (float*)work);
     if (e != cudaSuccess) return e;
-    return launch_pdl(rms_norm_dgamma_kernel, dim3((d + kThreads - 1) / kThreads), dim3(kThreads),
-                      0, st, (const float*)work, blocks, d, dgamma);
+    return launch_pdl(rms_norm_dgamma_kernel, dim3((d + 31) / 32), dim3(1024), 0, st,
+                      (const float*)work, blocks, d, dgamma);
   };
   return launched(fn, xdtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr));
 }

@@ -409,7 +409,8 @@ def balance_loss(logits, idx, mask=None):
     loss = logits.new_empty(1)
     counts = idx.new_empty(E)
     n = idx.new_empty(1)
-    work = idx.new_empty(L.eat_balance_workspace(T, E), dtype=torch.uint8)
+    # (a small call leaves its workspace untouched: any address does)
+    work = counts if T <= 512 else idx.new_empty(L.eat_balance_workspace(T, E), dtype=torch.uint8)
     _check(L.eat_balance_loss(pl, T, E, K, pi, pm, loss.data_ptr(), counts.data_ptr(),
                               n.data_ptr(), work.data_ptr(), _stream(None)))
     return loss, counts, n
