@@ -41,6 +41,7 @@ struct eat_head {
   __nv_bfloat16* xc = nullptr;  // [tokens, d] their hidden states, then X'
   __nv_bfloat16* e = nullptr;   // [cap, ld]
   float* dw_sum = nullptr;
+  float* dx_part = nullptr;     // slices of dx's sums over the vocabulary
 };
 
 namespace eat {
@@ -165,63 +166,70 @@ join_kernel(const float2* __restrict__ part, int pieces, const float* __restrict
 }
 
 // ------------------------------------------------------------------------------- gradient
-// The counted tokens in order, by one block; the launch's per-call words are cleared.
+// 32 rows per block, a warp each: the i-th counted token's hidden state into xc (zeros up to the end
+// of the last tile) and its base-2 target logit; and for token i, if it does not count, its outputs.
+// Every block finds its tokens itself: each thread counts a run of the targets (1 / 1024 of them),
+// and the runs' prefix sums say which hold the block's rows.  (A launch of its own for the list took
+// 14 us of 8192 tokens on one SM, and 3.5 us of any call.)
 __global__ void __launch_bounds__(1024)
-count_kernel(const int32_t* __restrict__ target, int T, int V, int tiles,
-             int32_t* __restrict__ rows, int32_t* __restrict__ ytok, int32_t* __restrict__ n_counted,
-             int32_t* __restrict__ far) {
-  __shared__ int s_w[32];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < tiles; i += 1024) far[i] = 0;
-  int base = 0;
-  for (int t0 = 0; t0 < T; t0 += 1024) {
-    const int t = t0 + threadIdx.x;
-    const int y = t < T ? target[t] : -1;
-    const bool on = y >= 0 && y < V;
-    const unsigned b = __ballot_sync(0xffffffffu, on);
-    if (lane == 0) s_w[warp] = __popc(b);
-    __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      before += i < warp ? s_w[i] : 0;
-      all += s_w[i];
-    }
-    if (on) {
-      const int at = base + before + __popc(b & ((1u << lane) - 1u));
-      rows[at] = t;
-      ytok[at] = y;
-    }
-    base += all;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) *n_counted = base;
-}
-
-// A warp per row i: the i-th counted token's hidden state into xc (zeros up to the end of the last
-// tile) and its base-2 target logit; and for token i, if it does not count, its outputs.
-__global__ void __launch_bounds__(256)
 gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_vecs, int T, int V,
-              const int32_t* __restrict__ target, const int32_t* __restrict__ rows,
-              const int32_t* __restrict__ n_counted, uint4* __restrict__ xc,
-              float* __restrict__ ly, uint32_t* __restrict__ row_max, uint4* __restrict__ dx,
-              float* __restrict__ nll, float* __restrict__ lse) {
+              const int32_t* __restrict__ target, int32_t* __restrict__ rows,
+              int32_t* __restrict__ ytok, int32_t* __restrict__ n_counted, uint4* __restrict__ xc,
+              float* __restrict__ ly, uint32_t* __restrict__ row_max, int32_t* __restrict__ far,
+              uint4* __restrict__ dx, float* __restrict__ nll, float* __restrict__ lse) {
+  __shared__ int s_w[32], s_row[32];
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, i = blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int n = *n_counted;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i0 = blockIdx.x * 32;
+  const int run = (T + 1023) / 1024, a = threadIdx.x * run, b = min(T, a + run);
+  int mine = 0;
+#pragma unroll 4
+  for (int t = a; t < b; ++t) {
+    const int y = target[t];
+    mine += y >= 0 && y < V;
+  }
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) s_w[warp] = incl;
+  __syncthreads();
+  int before = 0, n = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    before += i < warp ? s_w[i] : 0;
+    n += s_w[i];
+  }
+  int rank = before + incl - mine;  // of the run's first counted token
+  if (rank < i0 + 32 && rank + mine > i0) {
+    for (int t = a; t < b; ++t) {
+      const int y = target[t];
+      if (y >= 0 && y < V) {
+        if (rank >= i0 && rank < i0 + 32) {
+          s_row[rank - i0] = t;
+          rows[rank] = t;
+          ytok[rank] = y;
+        }
+        ++rank;
+      }
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *n_counted = n;
+  if (threadIdx.x == 0 && i0 % kHeadTile == 0) far[i0 / kHeadTile] = 0;
+  __syncthreads();
+  const int i = i0 + warp;
   if (i < n) {
-    const int t = rows[i];
-    const uint4* a = x + (size_t)t * row_vecs;
-    const uint4* b = w + (size_t)target[t] * row_vecs;
+    const int t = s_row[warp];
+    const uint4* p = x + (size_t)t * row_vecs;
+    const uint4* q = w + (size_t)target[t] * row_vecs;
     float d = 0.f;
 #pragma unroll 4
     for (int c = lane; c < row_vecs; c += 32) {
-      const uint4 v = a[c];
+      const uint4 v = p[c];
       xc[(size_t)i * row_vecs + c] = v;
-      d = dot16<false>(v, b[c], d);
+      d = dot16<false>(v, q[c], d);
     }
     d = warp_sum(d);
     if (lane == 0) {
@@ -245,7 +253,7 @@ gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_
 
 // After a piece's exponentials, 32 counted tokens per block: their sums, losses and factors; the
 // target entries of E; X' in place of x.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
               const int32_t* __restrict__ n_counted, const int32_t* __restrict__ rows,
               const int32_t* __restrict__ ytok, const float* __restrict__ ly,
@@ -253,7 +261,7 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
               __nv_bfloat16* __restrict__ e, int ld, float* __restrict__ f,
               uint4* __restrict__ xc, int row_vecs, float* __restrict__ nll,
               float* __restrict__ lse, const unsigned int* __restrict__ err) {
-  __shared__ float s_p[8][32];
+  __shared__ float s_p[32][33];
   __shared__ float s_f[32];
   pdl_wait();
   pdl_launch_dependents();
@@ -264,12 +272,17 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
   float s = 0.f;
   if (r < n) {
 #pragma unroll 4
-    for (int i = warp; i < pieces; i += 8) s += part[(size_t)i * cap + r];
+    for (int i = warp; i < pieces; i += 32) s += part[(size_t)i * cap + r];
   }
   s_p[warp][lane] = s;
   __syncthreads();
+  // warp j: token j's sum
+  const float all = warp_sum(s_p[lane][warp]);
+  __syncthreads();
+  if (lane == 0) s_f[warp] = all;
+  __syncthreads();
   if (warp == 0 && r < n) {
-    for (int i = 1; i < 8; ++i) s += s_p[i][lane];
+    s = s_f[lane];
     const int t = rows[t0 + r];
     const float l2 = ly[t0 + r], ref = head_ref(l2, row_max[t0 + r]);
     float2 a = token_loss(ref, s, l2);
@@ -288,9 +301,9 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
     if (lse) lse[t] = a.y;
   }
   __syncthreads();
-  for (int j = warp; j < min(32, n - r0); j += 8) {
-    const float k = s_f[j];
-    uint4* row = xc + (size_t)(t0 + r0 + j) * row_vecs;
+  if (r0 + warp < n) {
+    const float k = s_f[warp];
+    uint4* row = xc + (size_t)(t0 + r0 + warp) * row_vecs;
 #pragma unroll 4
     for (int c = lane; c < row_vecs; c += 32) {
       const Vec<false> v(row[c]);
@@ -303,6 +316,39 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
       row[c] = make_uint4(b[0], b[1], b[2], b[3]);
     }
   }
+}
+
+// dx from the slices of its split sums: a warp per counted token and 256 columns.
+__global__ void __launch_bounds__(256)
+dx_join_kernel(const float* __restrict__ part, int slices, int t0, int cap, int d,
+               const int32_t* __restrict__ n_counted, const int32_t* __restrict__ rows,
+               const float* __restrict__ f, __nv_bfloat16* __restrict__ dx) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int r = blockIdx.y * 8 + (threadIdx.x >> 5), c = blockIdx.x * 256 + (threadIdx.x & 31) * 8;
+  if (r >= min(cap, *n_counted - t0) || c >= d) return;
+  float s[8] = {};
+#pragma unroll 4
+  for (int i = 0; i < slices; ++i) {
+    const float4* p = (const float4*)(part + ((size_t)i * cap + r) * d + c);
+    const float4 a = p[0], b = p[1];
+    s[0] += a.x;
+    s[1] += a.y;
+    s[2] += a.z;
+    s[3] += a.w;
+    s[4] += b.x;
+    s[5] += b.y;
+    s[6] += b.z;
+    s[7] += b.w;
+  }
+  const float k = f[t0 + r];
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(s[2 * i] * k, s[2 * i + 1] * k);
+    o[i] = *(const uint32_t*)&v;
+  }
+  *(uint4*)(dx + (size_t)rows[t0 + r] * d + c) = make_uint4(o[0], o[1], o[2], o[3]);
 }
 
 // -------------------------------------------------------------------------------- host side
@@ -382,13 +428,10 @@ cudaError_t run_grad(eat_head* h, const void* x, int T, const int32_t* target, c
                      float* nll, float* lse, void* dx, void* dw, cudaStream_t st) {
   const int V = h->desc.vocab, d = h->desc.d_model, row_vecs = d / 8;
   const int t_pad = up(T, kHeadTile);
-  cudaError_t e = launch_pdl(count_kernel, dim3(1), dim3(1024), 0, st, target, T, V,
-                             t_pad / kHeadTile, h->rows, h->ytok, h->n_counted, h->far);
-  if (e == cudaSuccess)
-    e = launch_pdl(gather_kernel, dim3(t_pad / 8), dim3(256), 0, st, (const uint4*)x,
-                   (const uint4*)h->desc.w, row_vecs, T, V, target, (const int32_t*)h->rows,
-                   (const int32_t*)h->n_counted, (uint4*)h->xc, h->ly, h->row_max, (uint4*)dx, nll,
-                   lse);
+  cudaError_t e =
+      launch_pdl(gather_kernel, dim3(t_pad / 32), dim3(1024), 0, st, (const uint4*)x,
+                 (const uint4*)h->desc.w, row_vecs, T, V, target, h->rows, h->ytok, h->n_counted,
+                 (uint4*)h->xc, h->ly, h->row_max, h->far, (uint4*)dx, nll, lse);
   for (int t0 = 0; t0 < T && e == cudaSuccess; t0 += h->cap) {
     const int cap = std::min(h->cap, t_pad - t0);
     HeadPairArgs a{};
@@ -410,15 +453,20 @@ cudaError_t run_grad(eat_head* h, const void* x, int T, const int32_t* target, c
     a.redo = 1;
     e = head_launch_pair(false, true, h->x64, h->w64, a, h->max_pairs, st);
     if (e != cudaSuccess) break;
-    e = launch_pdl(finish_kernel, dim3(cap / 32), dim3(256), 0, st, (const float*)h->part,
+    e = launch_pdl(finish_kernel, dim3(cap / 32), dim3(1024), 0, st, (const float*)h->part,
                    up(V, kHeadTile) / 128, t0, cap, (const int32_t*)h->n_counted,
                    (const int32_t*)h->rows, (const int32_t*)h->ytok, (const float*)h->ly,
                    (const uint32_t*)h->row_max, g, h->e, h->ld, h->f, (uint4*)h->xc, row_vecs, nll,
                    lse, (const unsigned int*)h->st.err);
     if (e != cudaSuccess) break;
-    const HeadGradArgs b{V,      d,       h->n_counted, t0, cap, h->f, h->rows, (__nv_bfloat16*)dx,
-                         (__nv_bfloat16*)dw, h->dw_sum, h->st};
+    const int slices = head_dx_slices(cap, V, d, h->max_pairs);
+    const HeadGradArgs b{V, d, h->n_counted, t0, cap, h->f, h->rows, (__nv_bfloat16*)dx,
+                         (__nv_bfloat16*)dw, h->dw_sum, slices, h->dx_part, h->st};
     e = head_launch_grad(h->e64, h->w64, h->x64, b, h->max_pairs, st);
+    if (e == cudaSuccess && slices > 1)
+      e = launch_pdl(dx_join_kernel, dim3((d + 255) / 256, (cap + 7) / 8), dim3(256), 0, st,
+                     (const float*)h->dx_part, slices, t0, cap, d, (const int32_t*)h->n_counted,
+                     (const int32_t*)h->rows, (const float*)h->f, (__nv_bfloat16*)dx);
   }
   return e;
 }
@@ -479,7 +527,7 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
       D.max_tokens > kHeadSmallT ? sizeof(float2) * (size_t)pieces * D.max_tokens : 0;
   const size_t grad_part = D.with_grad ? sizeof(float) * (size_t)pieces * h->cap : 0;
   struct Part { void** p; size_t bytes; };
-  Part parts[16];
+  Part parts[20];
   int np = 0;
   auto add = [&](void* p, size_t bytes) { parts[np++] = {(void**)p, bytes}; };
   add(&h->st.err, 16);
@@ -495,6 +543,13 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
     add(&h->xc, 2 * tokens * D.d_model);
     add(&h->e, 2 * (size_t)h->cap * h->ld);
     if (h->cap < t_pad) add(&h->dw_sum, 4 * (size_t)V * D.d_model);
+    // a call's last piece may be as short as one tile
+    size_t most = 0;
+    for (int c = kHeadTile; c <= h->cap; c += kHeadTile) {
+      const int n = head_dx_slices(c, V, D.d_model, h->max_pairs);
+      if (n > 1) most = std::max(most, 4 * (size_t)n * c * D.d_model);
+    }
+    if (most) add(&h->dx_part, most);
   }
   size_t total = 0;
   for (int i = 0; i < np; ++i) total += (parts[i].bytes + 255) / 256 * 256;

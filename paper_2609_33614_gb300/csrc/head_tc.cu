@@ -314,6 +314,7 @@ struct PairParams {
 // One tile of a launch: 256 rows of A from m0, 256 rows of B from n0, kb k-blocks.
 struct Tile {
   int m0, n0, kb;
+  int k0;   // first k-block
   bool dw;  // kGrad: a tile of dW
 };
 
@@ -344,6 +345,11 @@ struct GradTiles {
   }
 };
 
+// k-blocks of a slice of the vocabulary
+__host__ __device__ __forceinline__ int slice_blocks(int V, int slices) {
+  return ((V + 63) / 64 + slices - 1) / slices;
+}
+
 template <int MODE, bool W8>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE>::kThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -366,6 +372,13 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (MODE == kExp && p.redo) {  // as a rule no token is far: the launch ends here
+    pdl_wait();
+    int any = 0;
+    for (int i = threadIdx.x; i < p.cap / kHeadTile; i += C::kThreads)
+      any |= p.far[p.t0 / kHeadTile + i];
+    if (!__syncthreads_or(any)) return;
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(&full[s], 1);
@@ -405,7 +418,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   GradTiles gt{};
   const int d_tiles = MODE == kGrad ? (g.d + kHeadTile - 1) / kHeadTile : 1;
   if (MODE == kGrad) {
-    const int nx = row_tiles * d_tiles, kx = (V + 63) / 64;
+    const int nx = row_tiles * d_tiles * g.slices, kx = slice_blocks(V, g.slices);
     // a piece without tokens adds nothing, but the first one still writes dW
     const int nw = rows > 0 || g.t0 == 0 ? v_tiles * d_tiles : 0, kw = (rows + 63) / 64;
     gt.dw_first = kw > kx;
@@ -424,9 +437,18 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       if (n < 0 || (!second && n >= gt.n1)) return false;
       ++i;
       t.dw = second != gt.dw_first;
-      t.m0 = n / d_tiles * kHeadTile;
       t.n0 = n % d_tiles * kHeadTile;
-      t.kb = second ? gt.k2 : gt.k1;
+      const int r = n / d_tiles;
+      if (t.dw) {
+        t.m0 = r * kHeadTile;
+        t.k0 = 0;
+        t.kb = second ? gt.k2 : gt.k1;
+      } else {
+        const int per = slice_blocks(V, g.slices), all = (V + 63) / 64;
+        t.m0 = r % row_tiles * kHeadTile;
+        t.k0 = r / row_tiles * per;
+        t.kb = max(0, min(per, all - t.k0));
+      }
       return true;
     }
     for (;;) {
@@ -438,6 +460,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       t.dw = false;
       t.m0 = rt * kHeadTile;
       t.n0 = (int)(u / row_tiles) * kHeadTile;
+      t.k0 = 0;
       t.kb = p.kblocks;
       return true;
     }
@@ -472,7 +495,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             if (j >= nk) break;
             uint8_t* sa = st + j * C::kSub;
             uint8_t* sb = sa + kOperand;
-            const int kx = (kb + j) * kElems;
+            const int kx = (t.k0 + kb + j) * kElems;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
               if (MODE == kGrad) {
@@ -606,6 +629,9 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           add = g.t0 > 0;
           if (add || !last) sum = g.dw_sum + (size_t)row * g.d;
           if (!last) out = nullptr;
+        } else if (row < rows && g.slices > 1) {
+          stores = true;
+          sum = g.dx_part + ((size_t)(t.k0 / slice_blocks(V, g.slices)) * g.cap + row) * g.d;
         } else if (row < rows) {
           stores = true;
           factor = g.f[g.t0 + row];
@@ -626,23 +652,21 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 #pragma unroll
             for (int j = 0; j < 32; ++j) w[j] = 0;
           }
-          if (t.dw) {
-            if (add) {
+          if (add) {
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const float4 o = *(const float4*)(sum + nc + j);
-                w[j] = __float_as_uint(__uint_as_float(w[j]) + o.x);
-                w[j + 1] = __float_as_uint(__uint_as_float(w[j + 1]) + o.y);
-                w[j + 2] = __float_as_uint(__uint_as_float(w[j + 2]) + o.z);
-                w[j + 3] = __float_as_uint(__uint_as_float(w[j + 3]) + o.w);
-              }
+            for (int j = 0; j < 32; j += 4) {
+              const float4 o = *(const float4*)(sum + nc + j);
+              w[j] = __float_as_uint(__uint_as_float(w[j]) + o.x);
+              w[j + 1] = __float_as_uint(__uint_as_float(w[j + 1]) + o.y);
+              w[j + 2] = __float_as_uint(__uint_as_float(w[j + 2]) + o.z);
+              w[j + 3] = __float_as_uint(__uint_as_float(w[j + 3]) + o.w);
             }
-            if (!out) {
+          }
+          if (!out) {
 #pragma unroll
-              for (int j = 0; j < 32; j += 4)
-                *(uint4*)(sum + nc + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
-              continue;
-            }
+            for (int j = 0; j < 32; j += 4)
+              *(uint4*)(sum + nc + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+            continue;
           }
           uint32_t b[16];
 #pragma unroll
@@ -849,12 +873,29 @@ cudaError_t head_launch_pair(bool w8, bool exp, const CUtensorMap& x, const CUte
             : launch_pair<kNll, false>(x, w, w, p, pairs, st);
 }
 
+// A piece whose tiles of dx are few, and whose sums run over the whole vocabulary, would leave most
+// SM pairs waiting for them: the sums are cut so that a slice takes at most half of what every pair
+// has to do anyway, but not below 8 k-blocks (a tile's cost besides its k-blocks, about 12 of them,
+// would outweigh what is gained).  Slices are added by a kernel of their own, in order.
+int head_dx_slices(int cap, int V, int d, int max_pairs) {
+  const long long dt = (d + kHeadTile - 1) / kHeadTile, kx = (V + 63) / 64, kw = (cap + 63) / 64;
+  const long long nx = cap / kHeadTile * dt, nw = (V + kHeadTile - 1) / kHeadTile * dt, fix = 12;
+  if (nx >= 2LL * max_pairs) return 1;
+  const long long share = (nx * (kx + fix) + nw * (kw + fix)) / max_pairs;
+  const long long len = std::max(8LL, share / 2);
+  const long long n = std::min((kx + len - 1) / len, 2LL * max_pairs / nx + 1);
+  // (no slice is empty)
+  const long long per = (kx + n - 1) / n;
+  return (int)((kx + per - 1) / per);
+}
+
 cudaError_t head_launch_grad(const CUtensorMap& e, const CUtensorMap& w, const CUtensorMap& x,
                              const HeadGradArgs& a, int max_pairs, cudaStream_t st) {
   PairParams p{};
   p.g = a;
-  const long long units = ((a.cap + kHeadTile - 1) / kHeadTile + (a.V + kHeadTile - 1) / kHeadTile) *
-                          (long long)((a.d + kHeadTile - 1) / kHeadTile);
+  const long long units =
+      ((long long)a.cap / kHeadTile * a.slices + (a.V + kHeadTile - 1) / kHeadTile) *
+      ((a.d + kHeadTile - 1) / kHeadTile);
   const int pairs = (int)std::min<long long>(max_pairs, units);
   return launch_pair<kGrad, false>(e, w, x, p, pairs, st);
 }

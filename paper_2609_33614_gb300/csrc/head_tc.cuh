@@ -74,8 +74,12 @@ struct HeadGradArgs {
   __nv_bfloat16* dx;
   __nv_bfloat16* dw;
   float* dw_sum;         // [V, d], or null when one piece holds every token
+  int slices;            // of dx's sums over the vocabulary
+  float* dx_part;        // slices > 1: [slice][cap][d] unscaled sums instead of dx
   HeadStatus st;
 };
+// Slices of dx's sums for a piece of cap tokens (a multiple of kHeadTile).
+int head_dx_slices(int cap, int V, int d, int max_pairs);
 cudaError_t head_launch_grad(const CUtensorMap& e, const CUtensorMap& w, const CUtensorMap& x,
                              const HeadGradArgs& a, int max_pairs, cudaStream_t st);
 

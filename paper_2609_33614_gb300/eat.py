@@ -359,7 +359,7 @@ def _norm(x, gamma, eps, residual, fp8):
         ph = h.data_ptr()
     if fp8:
         y = torch.empty_like(x, dtype=torch.float8_e4m3fn)
-        scale = gamma.new_empty(T)
+        scale = torch.empty(T, dtype=torch.float32, device=x.device)
         ps, ycode = scale.data_ptr(), EAT_FP8_E4M3
     else:
         y = torch.empty_like(x)
@@ -391,7 +391,7 @@ def rms_norm_grad(h, gamma, eps, dy, dres=None):
     L = lib()
     dx = torch.empty_like(h)
     dgamma = torch.empty_like(gamma)
-    work = gamma.new_empty(L.eat_rms_norm_grad_workspace(T, d), dtype=torch.uint8)
+    work = torch.empty(L.eat_rms_norm_grad_workspace(T, d), dtype=torch.uint8, device=h.device)
     _check(L.eat_rms_norm_grad(ph, T, d, code, pg, eps, py, pr, dx.data_ptr(), dgamma.data_ptr(),
                                work.data_ptr(), _stream(None)))
     return dx, dgamma
@@ -406,11 +406,13 @@ def balance_loss(logits, idx, mask=None):
     pi = _take("idx", idx, (T, K), torch.int32)
     pm = _take_mask(mask, T)
     L = lib()
-    loss = logits.new_empty(1)
-    counts = idx.new_empty(E)
-    n = idx.new_empty(1)
+    dev = logits.device
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    counts = torch.empty(E, dtype=torch.int32, device=dev)
+    n = torch.empty(1, dtype=torch.int32, device=dev)
     # (a small call leaves its workspace untouched: any address does)
-    work = counts if T <= 512 else idx.new_empty(L.eat_balance_workspace(T, E), dtype=torch.uint8)
+    work = counts if T <= 512 else \
+        torch.empty(L.eat_balance_workspace(T, E), dtype=torch.uint8, device=dev)
     _check(L.eat_balance_loss(pl, T, E, K, pi, pm, loss.data_ptr(), counts.data_ptr(),
                               n.data_ptr(), work.data_ptr(), _stream(None)))
     return loss, counts, n
