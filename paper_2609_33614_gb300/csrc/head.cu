@@ -126,32 +126,40 @@ small_join_kernel(const float2* __restrict__ part, int ctas, int n, const uint4*
   }
 }
 
-// The same for larger calls: 32 tokens per block, its warps over the pieces of the vocabulary.
-constexpr int kJoinWarps = 16;
-__global__ void __launch_bounds__(32 * kJoinWarps)
+// The same for larger calls: 8 tokens per block, 64 threads each over the pieces of the vocabulary.
+constexpr int kJoinT = 8;
+__global__ void __launch_bounds__(512)
 join_kernel(const float2* __restrict__ part, int pieces, const float* __restrict__ ly, int T,
             int V, const int32_t* __restrict__ target, float* __restrict__ nll,
             float* __restrict__ lse, const unsigned int* __restrict__ err) {
-  __shared__ float2 s_p[kJoinWarps][32];
+  __shared__ float2 s_p[16][kJoinT];
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int t = blockIdx.x * 32 + lane;
+  const int t = blockIdx.x * kJoinT + (lane & 7);
   float m = kHeadLow, s = 0.f;
   if (t < T) {
-#pragma unroll 4
-    for (int i = warp; i < pieces; i += kJoinWarps) {
+#pragma unroll 8
+    for (int i = warp * 4 + (lane >> 3); i < pieces; i += 64) {
       const float2 q = part[(size_t)i * T + t];
       const float k = fmaxf(m, q.x);
       s = s * exp2f(m - k) + q.y * exp2f(q.x - k);
       m = k;
     }
   }
-  s_p[warp][lane] = make_float2(m, s);
+#pragma unroll
+  for (int o = 8; o < 32; o <<= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
+    const float k = fmaxf(m, m2);
+    s = s * exp2f(m - k) + s2 * exp2f(m2 - k);
+    m = k;
+  }
+  if (lane < kJoinT) s_p[warp][lane] = make_float2(m, s);
   __syncthreads();
-  if (warp != 0 || t >= T) return;
-  for (int i = 1; i < kJoinWarps; ++i) {
-    const float2 q = s_p[i][lane];
+  if (threadIdx.x >= kJoinT || t >= T) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) {
+    const float2 q = s_p[i][threadIdx.x];
     const float k = fmaxf(m, q.x);
     s = s * exp2f(m - k) + q.y * exp2f(q.x - k);
     m = k;
@@ -419,7 +427,7 @@ cudaError_t run_pair(eat_head* h, const void* x, const float* xs, int T, const i
   a.st = h->st;
   const cudaError_t e = head_launch_pair(h->w8, false, mx, h->w64, a, h->max_pairs, st);
   if (e != cudaSuccess) return e;
-  return launch_pdl(join_kernel, dim3((T + 31) / 32), dim3(32 * kJoinWarps), 0, st,
+  return launch_pdl(join_kernel, dim3((T + kJoinT - 1) / kJoinT), dim3(512), 0, st,
                     (const float2*)h->part, up(V, kHeadTile) / 128, (const float*)h->ly, T, V,
                     target, nll, lse, (const unsigned int*)h->st.err);
 }
