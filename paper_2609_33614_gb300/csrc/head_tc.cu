@@ -791,7 +791,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       __syncwarp();
       if (lane == 0) {
         if (leader) mbar_arrive(&tempty[buf]);
-        else mbar_arrive_cluster(tempty0 + 8u * (uint32_t)buf);
+        else mbar_arrive_remote(tempty0 + 8u * (uint32_t)buf);
       }
       if (MODE == kNll && row < rows)
         p.part2[(size_t)(n0 / 128) * p.T + row] = make_float2(m, s);
