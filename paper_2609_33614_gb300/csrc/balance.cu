@@ -7,6 +7,8 @@
 // fp32 in a fixed order: a lane over its warp's tokens, the block's warps, then the blocks.
 #include "eat_internal.cuh"
 
+#include <cooperative_groups.h>
+
 #include <algorithm>
 #include <string>
 #include <type_traits>
@@ -16,12 +18,16 @@ namespace eat {
 namespace {
 
 constexpr int kTok = 4;
-constexpr int kMaxBlocks = 304;
-constexpr int kWarps = 8;       // of a block of several
-constexpr int kOneWarps = 32;   // of a block that takes the whole call
-// Calls of up to this many tokens run in one block, without partial sums in memory: 4.0 us of device
-// time at 64 x 8 and 512 x 64, where two launches took 7 and one launch less saves the host 1.6.
-constexpr int kOneBlockT = 512;
+constexpr int kWarps = 16;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kCluster = 8;
+// Calls of up to kOneBlockT tokens run in one block and up to kOneClusterT in one cluster, whose
+// blocks add up in shared memory: one launch and no sums in memory, which saves the host 4 us a call
+// (15 instead of 19) while the device takes less than that (2000 x 64: 9.4 us, in two launches 4.7).
+// Larger ones are joined by a second launch (16384 x 64: 8.6 us; in clusters, joined twice, 12.0).
+constexpr int kOneBlockT = kWarps * kTok;
+constexpr int kOneClusterT = 2048;
+constexpr int kMaxBlocks = 304;  // two per SM
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -74,12 +80,13 @@ __device__ __forceinline__ void softmax_rows(const float* logits, long long t0, 
 
 // loss, counts and the number of counted tokens from the sums of a block's threads: thread e < E
 // has expert e's sum of p and count, n the counted tokens
-__device__ void write_loss(float s, int c, int n, int E, float2* red, float* loss, int32_t* counts,
+__device__ void write_loss(float s, int c, int n, int E, float* loss, int32_t* counts,
                            int32_t* n_tokens) {
+  __shared__ float2 red[kMaxExperts / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if ((int)threadIdx.x < E) counts[threadIdx.x] = c;
   const float a = warp_sum(s * (float)c), b = warp_sum((float)c);
-  if (lane == 0) red[warp] = make_float2(a, b);
+  if (lane == 0 && warp < kMaxExperts / 32) red[warp] = make_float2(a, b);
   __syncthreads();
   if (threadIdx.x == 0) {
     float x = 0.f, y = 0.f;
@@ -92,25 +99,28 @@ __device__ void write_loss(float s, int c, int n, int E, float2* red, float* los
   }
 }
 
-// With WARPS = kOneWarps one block does the whole call; else block b leaves its sums in psum[b][E]
-// and cnt[b][E + 1] (the last: the tokens counted).
-template <int PER, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS)
+// A launch of one cluster writes the call's results; with blocks of their own, block b leaves its sums
+// in psum[b][E] and cnt[b][E + 1] (the last: the tokens counted).
+template <int PER>
+__global__ void __launch_bounds__(kThreads)
 balance_sum_kernel(const float* __restrict__ logits, int T, int E, int K,
                    const int32_t* __restrict__ idx, const uint8_t* __restrict__ mask,
                    float* __restrict__ psum, int32_t* __restrict__ cnt, float* __restrict__ loss,
                    int32_t* __restrict__ counts, int32_t* __restrict__ n_tokens) {
+  namespace cg = cooperative_groups;
   __shared__ int s_cnt[kMaxExperts + 1];
-  __shared__ float s_p[WARPS][32 * PER];
-  __shared__ float2 red[WARPS];
+  __shared__ float s_p[kWarps][32 * PER];
+  __shared__ float s_sum[32 * PER];
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int blocks = (int)cluster.num_blocks();
   pdl_wait();
   pdl_launch_dependents();
-  for (int i = threadIdx.x; i <= E; i += 32 * WARPS) s_cnt[i] = 0;
+  for (int i = threadIdx.x; i <= E; i += kThreads) s_cnt[i] = 0;
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float acc[PER] = {};
-  for (long long t0 = (long long)(blockIdx.x * WARPS + warp) * kTok; t0 < T;
-       t0 += (long long)gridDim.x * WARPS * kTok) {
+  for (long long t0 = (long long)(blockIdx.x * kWarps + warp) * kTok; t0 < T;
+       t0 += (long long)gridDim.x * kWarps * kTok) {
     bool on[kTok];
     int e[kTok];
 #pragma unroll
@@ -132,28 +142,48 @@ balance_sum_kernel(const float* __restrict__ logits, int T, int E, int K,
   for (int i = 0; i < PER; ++i) s_p[warp][i * 32 + lane] = acc[i];
   __syncthreads();
   const int e = threadIdx.x;
-  float s = 0.f;
-  if (e < E) {
+  if (e < 32 * PER) {
+    float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) s += s_p[w][e];
+    for (int w = 0; w < kWarps; ++w) s += s_p[w][e];
+    s_sum[e] = s;
   }
-  if (WARPS == kOneWarps) {
-    write_loss(s, e < E ? s_cnt[e] : 0, s_cnt[E], E, red, loss, counts, n_tokens);
-  } else {
-    if (e < E) psum[(size_t)blockIdx.x * E + e] = s;
-    for (int i = e; i <= E; i += 32 * WARPS) cnt[(size_t)blockIdx.x * (E + 1) + i] = s_cnt[i];
+  cluster.sync();
+  if (cluster.block_rank() == 0) {
+    float s = 0.f;
+    int c = 0, n = 0;
+#pragma unroll
+    for (int r = 0; r < kCluster; ++r) {
+      if (r >= blocks) break;
+      const int* rc = cluster.map_shared_rank(s_cnt, r);
+      if (e < E) {
+        s += cluster.map_shared_rank(s_sum, r)[e];
+        c += rc[e];
+      }
+      n += rc[E];
+    }
+    if ((int)gridDim.x == blocks) {
+      write_loss(s, c, n, E, loss, counts, n_tokens);
+    } else {
+      if (e < E) {
+        psum[(size_t)blockIdx.x * E + e] = s;
+        cnt[(size_t)blockIdx.x * (E + 1) + e] = c;
+      }
+      if (e == 0) cnt[(size_t)blockIdx.x * (E + 1) + E] = n;
+    }
   }
+  cluster.sync();  // no block leaves while another reads its sums
 }
 
 // The blocks' sums joined: a warp takes every 32nd block, its lanes the experts.
+constexpr int kJoinWarps = 32;
 template <int PER>
-__global__ void __launch_bounds__(32 * kOneWarps)
+__global__ void __launch_bounds__(32 * kJoinWarps)
 balance_join_kernel(const float* __restrict__ psum, const int32_t* __restrict__ cnt, int parts,
                     int E, float* __restrict__ loss, int32_t* __restrict__ counts,
                     int32_t* __restrict__ n_tokens) {
-  __shared__ float s_p[kOneWarps][32 * PER];
+  __shared__ float s_p[kJoinWarps][32 * PER];
   __shared__ int s_cnt[32 * PER], s_n;
-  __shared__ float2 red[kOneWarps];
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -162,8 +192,8 @@ balance_join_kernel(const float* __restrict__ psum, const int32_t* __restrict__ 
   __syncthreads();
   float s[PER] = {};
   int c[PER] = {}, n = 0;
-#pragma unroll 4
-  for (int b = warp; b < parts; b += kOneWarps) {
+#pragma unroll 5
+  for (int b = warp; b < parts; b += kJoinWarps) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int e = i * 32 + lane;
@@ -184,14 +214,13 @@ balance_join_kernel(const float* __restrict__ psum, const int32_t* __restrict__ 
   float sum = 0.f;
   if ((int)threadIdx.x < E) {
 #pragma unroll
-    for (int w = 0; w < kOneWarps; ++w) sum += s_p[w][threadIdx.x];
+    for (int w = 0; w < kJoinWarps; ++w) sum += s_p[w][threadIdx.x];
   }
-  write_loss(sum, (int)threadIdx.x < E ? s_cnt[threadIdx.x] : 0, s_n, E, red, loss, counts,
-             n_tokens);
+  write_loss(sum, (int)threadIdx.x < E ? s_cnt[threadIdx.x] : 0, s_n, E, loss, counts, n_tokens);
 }
 
 template <int PER>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(kThreads)
 balance_grad_kernel(const float* logits, int T, int E, const uint8_t* __restrict__ mask,
                     const int32_t* __restrict__ counts, const int32_t* __restrict__ n_tokens,
                     const float* __restrict__ g, float* dlogits) {
@@ -235,8 +264,8 @@ balance_grad_kernel(const float* logits, int T, int E, const uint8_t* __restrict
   }
 }
 
-int sum_blocks(int T) {
-  return std::min((int)(((long long)T + kWarps * kTok - 1) / (kWarps * kTok)), kMaxBlocks);
+int blocks_for(int T) {
+  return (int)std::min(((long long)T + kOneBlockT - 1) / kOneBlockT, (long long)kMaxBlocks);
 }
 
 // go(PER): experts per lane
@@ -266,7 +295,7 @@ using namespace eat;
 
 extern "C" int64_t eat_balance_workspace(int32_t T, int32_t E) {
   if (T < 1 || E < 1) return 0;
-  return T <= kOneBlockT ? 16 : (int64_t)sum_blocks(T) * (2 * E + 1) * 4;
+  return T <= kOneClusterT ? 16 : (int64_t)blocks_for(T) * (2 * E + 1) * 4;
 }
 
 extern "C" eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E, int32_t K,
@@ -282,23 +311,18 @@ extern "C" eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E
       misaligned(counts, 4) || misaligned(n_tokens, 4) || misaligned(work, 16))
     return bad(fn, "misaligned pointer");
   const cudaStream_t st = (cudaStream_t)stream;
-  if (T <= kOneBlockT)
-    return launched(fn, pick_per(E, [&](auto per) {
-      return launch_pdl(balance_sum_kernel<decltype(per)::value, kOneWarps>, dim3(1),
-                        dim3(32 * kOneWarps), 0, st, logits, T, E, K, idx, mask, (float*)nullptr,
-                        (int32_t*)nullptr, loss, counts, n_tokens);
-    }));
-  const int parts = sum_blocks(T);
+  const bool one = T <= kOneClusterT;
+  const int cluster = one && T > kOneBlockT ? kCluster : 1, blocks = one ? cluster : blocks_for(T);
   float* psum = (float*)work;
-  int32_t* cnt = (int32_t*)(psum + (size_t)parts * E);
+  int32_t* cnt = (int32_t*)(psum + (size_t)blocks * E);
   return launched(fn, pick_per(E, [&](auto per) {
     constexpr int PER = decltype(per)::value;
     const cudaError_t e =
-        launch_pdl(balance_sum_kernel<PER, kWarps>, dim3(parts), dim3(32 * kWarps), 0, st, logits,
-                   T, E, K, idx, mask, psum, cnt, loss, counts, n_tokens);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(balance_join_kernel<PER>, dim3(1), dim3(32 * kOneWarps), 0, st,
-                      (const float*)psum, (const int32_t*)cnt, parts, E, loss, counts, n_tokens);
+        launch_pdl_cluster(balance_sum_kernel<PER>, dim3(blocks), cluster, dim3(kThreads), 0, st,
+                           logits, T, E, K, idx, mask, psum, cnt, loss, counts, n_tokens);
+    if (e != cudaSuccess || one) return e;
+    return launch_pdl(balance_join_kernel<PER>, dim3(1), dim3(32 * kJoinWarps), 0, st,
+                      (const float*)psum, (const int32_t*)cnt, blocks, E, loss, counts, n_tokens);
   }));
 }
 
@@ -314,8 +338,8 @@ extern "C" eat_status eat_balance_grad(const float* logits, int32_t T, int32_t E
       misaligned(g, 4) || misaligned(dlogits, 4))
     return bad(fn, "misaligned pointer");
   return launched(fn, pick_per(E, [&](auto per) {
-    return launch_pdl(balance_grad_kernel<decltype(per)::value>, dim3(sum_blocks(T)),
-                      dim3(32 * kWarps), 0, (cudaStream_t)stream, logits, T, E, mask, counts,
-                      n_tokens, g, dlogits);
+    return launch_pdl(balance_grad_kernel<decltype(per)::value>, dim3(blocks_for(T)),
+                      dim3(kThreads), 0, (cudaStream_t)stream, logits, T, E, mask, counts, n_tokens,
+                      g, dlogits);
   }));
 }

@@ -5,8 +5,8 @@
 //   squares and its maximum come out of one reduction and y / s = (h gamma) (rstd / s).
 //   gradient, n = h rstd:  dx = dres + rstd (gamma dy - n mean(gamma dy n));  dgamma = sum_t dy n
 // Bound: HBM (a row is read once and kept in registers between the reduction and the outputs).
-// A thread holds NV vectors of 16 bytes of a row; a row is taken by a warp (up to 128 vectors) or by
-// a block of 256 threads.  Rows whose length is no multiple of a vector begin at any element: their
+// A thread holds NV vectors of 16 bytes of a row; a row is taken by a warp (up to 64 vectors) or by a
+// block of as many warps as it needs.  Rows whose length is no multiple of a vector begin at any element: their
 // vectors are the aligned ones of memory, and the first and the last of a row are partial.  All
 // sums are fp32; a value is rounded once, when it is stored.
 #include "eat_internal.cuh"
@@ -21,8 +21,10 @@ namespace eat {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;  // of a block whose warps take a row each, and of the plain kernels
 constexpr int kWarps = kThreads / 32;
+constexpr int kMaxThreads = 512;  // of a block that takes a row
+constexpr int kMaxWarps = kMaxThreads / 32;
 // e4m3 rows whose largest value is not above this get the scale 1 (and bytes 0): max / 448 and its
 // reciprocal stay away from fp32's ends
 constexpr float kTiny = 1e-35f;
@@ -96,33 +98,49 @@ __device__ __forceinline__ void store_vec(T* row, int c, int d, const float* v) 
   for (int j = 0; j < N; ++j)
     if (c + j >= 0 && c + j < d) row[c + j] = Elem<T>::put(v[j]);
 }
+// Elements [c, c + N) of gamma.  A row that begins anywhere has c anywhere, but the same remainder of
+// four in all its threads: whole vectors around the elements are loaded, and shifted by it.  (Loads
+// element by element made 16384 rows of 2047 take twice the time of 2048.)
 template <int N, bool ALIGNED>
 __device__ __forceinline__ void load_gamma(const float* g, int c, int d, float* v) {
   if (ALIGNED) {
 #pragma unroll
     for (int j = 0; j < N; j += 4) *(float4*)(v + j) = __ldg((const float4*)(g + c + j));
+    return;
+  }
+  const int a = c & 3;
+  if (c - a >= 0 && c - a + N + 4 <= d) {
+    float w[N + 4];
+#pragma unroll
+    for (int j = 0; j < N + 4; j += 4) *(float4*)(w + j) = __ldg((const float4*)(g + c - a + j));
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      v[j] = a == 0 ? w[j] : a == 1 ? w[j + 1] : a == 2 ? w[j + 2] : w[j + 3];
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = c + j >= 0 && c + j < d ? __ldg(g + c + j) : 0.f;
   }
 }
 
-// Sums (or maxima) over the threads of a row, in every one of them.  ROW threads: 32 or the block;
-// `red` alternates between two buffers, so one barrier per row is enough.
-template <int ROW, bool MAX>
-__device__ __forceinline__ float2 row_reduce(float a, float b, float2 (*red)[kWarps], int turn) {
+// Sums (or maxima) over the threads of a row, in every one of them: a warp, or the whole block; `red`
+// alternates between two buffers, so one barrier per row is enough.
+template <bool WARP, bool MAX>
+__device__ __forceinline__ float2 row_reduce(float a, float b, float2 (*red)[kMaxWarps],
+                                             int turn) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     a += __shfl_xor_sync(0xffffffffu, a, o);
     const float b2 = __shfl_xor_sync(0xffffffffu, b, o);
     b = MAX ? fmaxf(b, b2) : b + b2;
   }
-  if (ROW == 32) return make_float2(a, b);
+  if (WARP) return make_float2(a, b);
   if ((threadIdx.x & 31) == 0) red[turn & 1][threadIdx.x >> 5] = make_float2(a, b);
   __syncthreads();
+  const int warps = blockDim.x >> 5;
   float2 s = red[turn & 1][0];
 #pragma unroll
-  for (int i = 1; i < kWarps; ++i) {
+  for (int i = 1; i < kMaxWarps; ++i) {
+    if (i >= warps) break;
     const float2 q = red[turn & 1][i];
     s.x += q.x;
     s.y = MAX ? fmaxf(s.y, q.y) : s.y + q.y;
@@ -130,17 +148,17 @@ __device__ __forceinline__ float2 row_reduce(float a, float b, float2 (*red)[kWa
   return s;
 }
 
-template <typename T, bool F8, int ROW, int NV, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, bool F8, bool WARP, int NV, bool ALIGNED>
+__global__ void __launch_bounds__(kMaxThreads)
 rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict__ gamma, float eps,
                 T* h, void* y, float* __restrict__ y_scale) {
   constexpr int N = Elem<T>::kN;
-  __shared__ float2 red[2][kWarps];
+  __shared__ float2 red[2][kMaxWarps];
   pdl_wait();
   pdl_launch_dependents();
-  const int t = ROW == 32 ? blockIdx.x * kWarps + (threadIdx.x >> 5) : blockIdx.x;
+  const int t = WARP ? blockIdx.x * kWarps + (threadIdx.x >> 5) : blockIdx.x;
   if (t >= rows) return;
-  const int lane = ROW == 32 ? threadIdx.x & 31 : threadIdx.x;
+  const int lane = WARP ? threadIdx.x & 31 : threadIdx.x, ROW = WARP ? 32 : blockDim.x;
   const size_t at = (size_t)t * d;
   const int shift = ALIGNED ? 0 : (int)(at % N);
   uint4 ux[NV], ur[NV];
@@ -177,7 +195,7 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
       }
     }
   }
-  const float2 a = row_reduce<ROW, true>(ss, top, red, 0);
+  const float2 a = row_reduce<WARP, true>(ss, top, red, 0);
   const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
   float k = rstd;
   if (F8) {
@@ -213,21 +231,32 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
   }
 }
 
+// Threads of the gradient's blocks at most, and blocks that are to fit an SM.
+__host__ __device__ constexpr int grad_threads(bool warp, int nv) {
+  return warp || nv == 2 ? kThreads : kMaxThreads;
+}
+__host__ __device__ constexpr int grad_resident(bool warp, int nv) {
+  return warp || nv == 2 ? 2 : 1;
+}
+
 // Group b of threads (a warp or the block) takes rows b, b + groups, ... (the number of groups is a
 // multiple of a vector's elements, so these rows begin alike): dx, and in registers the group's sum of
 // dy n, which the block adds up and leaves in part[block].
-template <typename T, int ROW, int NV, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads)
+// A row's loads are issued before the row ahead of it is reduced (up to two vectors a thread, so that
+// two rows fit the registers of two blocks per SM).
+template <typename T, bool WARP, int NV, bool ALIGNED>
+__global__ void __launch_bounds__(grad_threads(WARP, NV), grad_resident(WARP, NV))
 rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __restrict__ gamma,
                      float eps, const T* dy, const T* dres, T* dx, float* __restrict__ part) {
   constexpr int N = Elem<T>::kN;
-  constexpr int kGroups = kThreads / ROW;  // per block
-  __shared__ float2 red[2][kWarps];
-  extern __shared__ float s_part[];        // warps' sums: [kWarps][d] (ROW == 32)
+  constexpr int kGroups = WARP ? kWarps : 1;  // per block
+  constexpr bool kAhead = NV <= 2;
+  __shared__ float2 red[2][kMaxWarps];
+  extern __shared__ float s_part[];        // warps' sums: [kWarps][d] (WARP)
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = ROW == 32 ? threadIdx.x & 31 : threadIdx.x;
-  const int t0 = blockIdx.x * kGroups + (ROW == 32 ? threadIdx.x >> 5 : 0);
+  const int lane = WARP ? threadIdx.x & 31 : threadIdx.x, ROW = WARP ? 32 : blockDim.x;
+  const int t0 = blockIdx.x * kGroups + (WARP ? threadIdx.x >> 5 : 0);
   const int step = gridDim.x * kGroups;
   const int shift = ALIGNED ? 0 : (int)((size_t)t0 * d % N);
   float acc[NV][N];
@@ -235,18 +264,44 @@ rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __re
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
-  int turn = 0;
-  for (int t = t0; t < rows; t += step, ++turn) {
+  uint4 uh[NV], ug[NV], ur[NV];
+  auto load = [&](int t, uint4 (&a)[NV], uint4 (&b)[NV], uint4 (&r)[NV]) {
     const size_t at = (size_t)t * d;
-    uint4 uh[NV], ug[NV], ur[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (lane + i * ROW) * N - shift;
       if (c < d) {
-        uh[i] = load_vec<T, ALIGNED>(h + at, c, d);
-        ug[i] = load_vec<T, ALIGNED>(dy + at, c, d);
-        if (dres) ur[i] = load_vec<T, ALIGNED>(dres + at, c, d);
+        a[i] = load_vec<T, ALIGNED>(h + at, c, d);
+        b[i] = load_vec<T, ALIGNED>(dy + at, c, d);
+        if (dres) r[i] = load_vec<T, ALIGNED>(dres + at, c, d);
       }
+    }
+  };
+  if (kAhead && t0 < rows) load(t0, uh, ug, ur);
+  float gm[kAhead ? NV : 1][N];  // gamma, alike for all rows
+  if constexpr (kAhead) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * ROW) * N - shift;
+      if (c < d) load_gamma<N, ALIGNED>(gamma, c, d, gm[i]);
+    }
+  }
+  auto get_gamma = [&](int i, int c, float (&g)[N]) {
+    if constexpr (kAhead) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) g[j] = gm[i][j];
+    } else {
+      load_gamma<N, ALIGNED>(gamma, c, d, g);
+    }
+  };
+  int turn = 0;
+  for (int t = t0; t < rows; t += step, ++turn) {
+    const size_t at = (size_t)t * d;
+    uint4 nh[kAhead ? NV : 1], ng[kAhead ? NV : 1], nr[kAhead ? NV : 1];
+    if constexpr (kAhead) {
+      if (t + step < rows) load(t + step, nh, ng, nr);
+    } else {
+      load(t, uh, ug, ur);
     }
     float ss = 0.f, dot = 0.f;
 #pragma unroll
@@ -256,7 +311,7 @@ rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __re
         float v[N], w[N], g[N];
         Elem<T>::unpack(uh[i], v);
         Elem<T>::unpack(ug[i], w);
-        load_gamma<N, ALIGNED>(gamma, c, d, g);
+        get_gamma(i, c, g);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           ss = fmaf(v[j], v[j], ss);
@@ -264,7 +319,7 @@ rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __re
         }
       }
     }
-    const float2 a = row_reduce<ROW, false>(ss, dot, red, turn);
+    const float2 a = row_reduce<WARP, false>(ss, dot, red, turn);
     const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
     const float m = a.y * rstd / (float)d;
 #pragma unroll
@@ -274,7 +329,7 @@ rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __re
         float v[N], w[N], g[N], o[N];
         Elem<T>::unpack(uh[i], v);
         Elem<T>::unpack(ug[i], w);
-        load_gamma<N, ALIGNED>(gamma, c, d, g);
+        get_gamma(i, c, g);
         if (dres) Elem<T>::unpack(ur[i], o);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -286,9 +341,17 @@ rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __re
         store_vec<T, ALIGNED>(dx + at, c, d, o);
       }
     }
+    if constexpr (kAhead) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        uh[i] = nh[i];
+        ug[i] = ng[i];
+        ur[i] = nr[i];
+      }
+    }
   }
   float* mine = part + (size_t)blockIdx.x * d;
-  if (ROW == 32) {
+  if (WARP) {
     float* w = s_part + (threadIdx.x >> 5) * d;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -326,7 +389,7 @@ template <typename T, bool F8>
 __global__ void __launch_bounds__(kThreads)
 rms_norm_any_kernel(const T* x, const T* r, int d, const float* __restrict__ gamma, float eps, T* h,
                     void* y, float* __restrict__ y_scale) {
-  __shared__ float2 red[2][kWarps];
+  __shared__ float2 red[2][kMaxWarps];
   pdl_wait();
   pdl_launch_dependents();
   const size_t row = (size_t)blockIdx.x * d;
@@ -339,7 +402,7 @@ rms_norm_any_kernel(const T* x, const T* r, int d, const float* __restrict__ gam
     ss = fmaf(v, v, ss);
     top = fmaxf(top, fabsf(v * gamma[c]));
   }
-  const float2 a = row_reduce<kThreads, true>(ss, top, red, 0);
+  const float2 a = row_reduce<false, true>(ss, top, red, 0);
   const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
   const float m = a.y * rstd, scale = m > kTiny ? m / 448.0f : 1.0f;
   const float k = F8 ? rstd / scale : rstd;
@@ -357,7 +420,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads)
 rms_norm_grad_any_kernel(const T* __restrict__ h, int rows, int d, const float* __restrict__ gamma,
                          float eps, const T* dy, const T* dres, T* dx, float* __restrict__ part) {
-  __shared__ float2 red[2][kWarps];
+  __shared__ float2 red[2][kMaxWarps];
   pdl_wait();
   pdl_launch_dependents();
   float* mine = part + (size_t)blockIdx.x * d;
@@ -370,7 +433,7 @@ rms_norm_grad_any_kernel(const T* __restrict__ h, int rows, int d, const float* 
       ss = fmaf(v, v, ss);
       dot = fmaf(gamma[c] * Elem<T>::get(dy[row + c]), v, dot);
     }
-    const float2 a = row_reduce<kThreads, false>(ss, dot, red, turn);
+    const float2 a = row_reduce<false, false>(ss, dot, red, turn);
     const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
     const float m = a.y * rstd / (float)d;
     for (int c = threadIdx.x; c < d; c += kThreads) {
@@ -404,32 +467,40 @@ rms_norm_dgamma_kernel(const float* __restrict__ part, int n_parts, int d,
   if (lane == 0 && blockIdx.x * 32 + warp < d) dgamma[blockIdx.x * 32 + warp] = s;
 }
 
-// Blocks of the gradient's first kernel: at most four per SM of this chip (152), a multiple of a
-// vector's elements unless every group has one row.
-constexpr int kGradBlocks = 608;
-int grad_blocks(int T, int groups) { return std::min((T + groups - 1) / groups, kGradBlocks); }
+// Blocks of the gradient's first kernel: at most as many as fit this chip's 152 SMs with 512 threads of
+// 128 registers each, a multiple of a vector's elements unless every group has one row.
+constexpr int kGradBlocks = 1216;
+int grad_blocks(int T, int groups, int threads) {
+  return std::min((T + groups - 1) / groups, 152 * std::max(1, std::min(8, 512 / threads)));
+}
 
-// The kernel for rows of d elements of type E in memory aligned to vectors: pick(ROW, NV, ALIGNED)
-// with the constants as types; false when no vector kernel takes the row.
-template <typename E, typename F>
+// The kernel for rows of d elements of type E in memory aligned to vectors: pick(WARP, NV, ALIGNED,
+// threads) with the first three as types; false when no vector kernel takes the row.  The gradient
+// takes two vectors a thread where the norm takes one: it holds three matrices' rows and a barrier
+// per row, and blocks of half the threads overlap better (16384 x 2048: 81 -> 51 us).
+template <typename E, bool GRAD, typename F>
 bool pick_rows(int d, F&& pick) {
   constexpr int N = Elem<E>::kN;
   const bool aligned = d % N == 0;
   const int vecs = aligned ? d / N : (d + 2 * N - 2) / N;  // of a row that begins anywhere
-  auto go = [&](auto row, auto nv) {
-    if (aligned) pick(row, nv, std::true_type());
-    else pick(row, nv, std::false_type());
+  auto go = [&](auto warp, auto nv) {
+    constexpr int NV = decltype(nv)::value;
+    const int threads =
+        decltype(warp)::value ? kThreads : ((vecs + NV - 1) / NV + 31) / 32 * 32;
+    if (aligned) pick(warp, nv, std::true_type(), threads);
+    else pick(warp, nv, std::false_type(), threads);
     return true;
   };
-  using R32 = std::integral_constant<int, 32>;
-  using R256 = std::integral_constant<int, kThreads>;
-  if (vecs <= 32) return go(R32(), std::integral_constant<int, 1>());
-  if (vecs <= 64) return go(R32(), std::integral_constant<int, 2>());
-  if (vecs <= 128) return go(R32(), std::integral_constant<int, 4>());
-  if (vecs <= 256) return go(R256(), std::integral_constant<int, 1>());
-  if (vecs <= 512) return go(R256(), std::integral_constant<int, 2>());
-  if (vecs <= 1024) return go(R256(), std::integral_constant<int, 4>());
-  if (vecs <= 2048) return go(R256(), std::integral_constant<int, 8>());
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  using Four = std::integral_constant<int, 4>;
+  if (vecs <= 32) return go(std::true_type(), One());
+  if (vecs <= 64) return go(std::true_type(), Two());
+  if constexpr (!GRAD) {
+    if (vecs <= 320) return go(std::false_type(), One());
+  }
+  if (vecs <= 512) return go(std::false_type(), Two());
+  if (vecs <= 4 * kMaxThreads) return go(std::false_type(), Four());
   return false;
 }
 
@@ -472,11 +543,11 @@ extern "C" eat_status eat_rms_norm(const void* x, const void* residual, int32_t 
     using E = std::remove_pointer_t<decltype(tag)>;
     constexpr bool F8 = decltype(f8)::value;
     cudaError_t e = cudaSuccess;
-    if (vec && pick_rows<E>(d, [&](auto row, auto nv, auto al) {
-          constexpr int ROW = decltype(row)::value;
-          const unsigned blocks = ROW == 32 ? ((unsigned)T + kWarps - 1) / kWarps : (unsigned)T;
-          e = launch_pdl(rms_norm_kernel<E, F8, ROW, decltype(nv)::value, decltype(al)::value>,
-                         dim3(blocks), dim3(kThreads), 0, st, (const E*)x, (const E*)residual, T, d,
+    if (vec && pick_rows<E, false>(d, [&](auto warp, auto nv, auto al, int threads) {
+          constexpr bool WARP = decltype(warp)::value;
+          const unsigned blocks = WARP ? ((unsigned)T + kWarps - 1) / kWarps : (unsigned)T;
+          e = launch_pdl(rms_norm_kernel<E, F8, WARP, decltype(nv)::value, decltype(al)::value>,
+                         dim3(blocks), dim3(threads), 0, st, (const E*)x, (const E*)residual, T, d,
                          gamma, (float)eps, (E*)h, y, y_scale);
         }))
       return e;
@@ -494,7 +565,7 @@ extern "C" eat_status eat_rms_norm(const void* x, const void* residual, int32_t 
 }
 
 extern "C" int64_t eat_rms_norm_grad_workspace(int32_t T, int32_t d) {
-  return T < 1 || d < 1 ? 0 : (int64_t)grad_blocks(T, 1) * d * 4;
+  return T < 1 || d < 1 ? 0 : (int64_t)std::min(T, kGradBlocks) * d * 4;
 }
 
 extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int32_t xdtype,
@@ -517,12 +588,12 @@ extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int
   auto run = [&](auto* tag) {
     using E = std::remove_pointer_t<decltype(tag)>;
     cudaError_t e = cudaSuccess;
-    int blocks = grad_blocks(T, 1);
-    if (!(vec && pick_rows<E>(d, [&](auto row, auto nv, auto al) {
-            constexpr int ROW = decltype(row)::value;
-            blocks = grad_blocks(T, kThreads / ROW);
-            e = launch_pdl(rms_norm_grad_kernel<E, ROW, decltype(nv)::value, decltype(al)::value>,
-                           dim3(blocks), dim3(kThreads), ROW == 32 ? (size_t)kWarps * d * 4 : 0, st,
+    int blocks = grad_blocks(T, 1, kThreads);
+    if (!(vec && pick_rows<E, true>(d, [&](auto warp, auto nv, auto al, int threads) {
+            constexpr bool WARP = decltype(warp)::value;
+            blocks = grad_blocks(T, WARP ? kWarps : 1, threads);
+            e = launch_pdl(rms_norm_grad_kernel<E, WARP, decltype(nv)::value, decltype(al)::value>,
+                           dim3(blocks), dim3(threads), WARP ? (size_t)kWarps * d * 4 : 0, st,
                            (const E*)h, T, d, gamma, (float)eps, (const E*)dy, (const E*)dres,
                            (E*)dx, (float*)work);
           })))

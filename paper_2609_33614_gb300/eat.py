@@ -411,7 +411,7 @@ def balance_loss(logits, idx, mask=None):
     counts = torch.empty(E, dtype=torch.int32, device=dev)
     n = torch.empty(1, dtype=torch.int32, device=dev)
     # (a small call leaves its workspace untouched: any address does)
-    work = counts if T <= 512 else \
+    work = counts if T <= 2048 else \
         torch.empty(L.eat_balance_workspace(T, E), dtype=torch.uint8, device=dev)
     _check(L.eat_balance_loss(pl, T, E, K, pi, pm, loss.data_ptr(), counts.data_ptr(),
                               n.data_ptr(), work.data_ptr(), _stream(None)))
