@@ -30,6 +30,7 @@ struct eat_head {
   CUtensorMap w128, w64, w16, x64, e64;
   float2* part = nullptr;      // small calls [ctas][n]; larger ones [128-row pieces][T]
   float* ly = nullptr;         // [max_tokens] base-2 target logits
+  unsigned int* tickets = nullptr;  // small calls (0 between calls)
   // gradient
   int cap = 0, ld = 0;         // tokens of a piece, columns of E
   int32_t* n_counted = nullptr;
@@ -48,8 +49,6 @@ namespace eat {
 
 namespace {
 
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr size_t kPieceBytes = 512u << 20;
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -58,79 +57,11 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// nll and lse of a token from the base-2 target logit and the sum of the others' exp2 relative to m
-__device__ __forceinline__ float2 token_loss(float m, float s, float ly) {
-  const float r = (m - ly + log2f(s)) * kLn2;
-  float a = fmaxf(r, 0.f) + log1pf(expf(-fabsf(r)));
-  if (isnan(r)) a = r;
-  return make_float2(a, fmaf(ly, kLn2, a));
-}
-
-// Joins the CTAs' partial sums of a small call; a block per token.  The target's logit is a sum of
-// its own in fp32.
-template <bool W8>
-__global__ void __launch_bounds__(128)
-small_join_kernel(const float2* __restrict__ part, int ctas, int n, const uint4* __restrict__ x,
-                  const uint4* __restrict__ w, int row_vecs, const float* __restrict__ xs,
-                  const float* __restrict__ ws, int V, const int32_t* __restrict__ target,
-                  float* __restrict__ nll, float* __restrict__ lse,
-                  const unsigned int* __restrict__ err) {
-  __shared__ float s_m[4], s_s[4], s_d[4];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int t = blockIdx.x, y = target[t];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (y < 0 || y >= V) {
-    if (threadIdx.x == 0) {
-      nll[t] = y < 0 ? 0.f : NAN;
-      if (lse) lse[t] = y < 0 ? 0.f : NAN;
-    }
-    return;
-  }
-  float d = 0.f;
-  for (int i = threadIdx.x; i < row_vecs; i += 128)
-    d = dot16<W8>(x[(size_t)t * row_vecs + i], w[(size_t)y * row_vecs + i], d);
-  float m = kHeadLow, s = 0.f;
-  for (int i = threadIdx.x; i < ctas; i += 128) {
-    const float2 q = part[(size_t)i * n + t];
-    const float k = fmaxf(m, q.x);
-    s = s * exp2f(m - k) + q.y * exp2f(q.x - k);
-    m = k;
-  }
-  d = warp_sum(d);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-    const float k = fmaxf(m, m2);
-    s = s * exp2f(m - k) + s2 * exp2f(m2 - k);
-    m = k;
-  }
-  if (lane == 0) {
-    s_m[warp] = m;
-    s_s[warp] = s;
-    s_d[warp] = d;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < 4; ++i) {
-      const float k = fmaxf(m, s_m[i]);
-      s = s * exp2f(m - k) + s_s[i] * exp2f(s_m[i] - k);
-      m = k;
-      d += s_d[i];
-    }
-    if (W8) d *= xs[t] * ws[y];
-    float2 r = token_loss(m, s, d * kLog2e);
-    if (*err) r = make_float2(NAN, NAN);
-    nll[t] = r.x;
-    if (lse) lse[t] = r.y;
-  }
-}
-
-// The same for larger calls: 8 tokens per block, 64 threads each over the pieces of the vocabulary.
+// Joins the pieces' (or a small call's CTAs') sums of a loss, part[piece][stride]: 8 tokens per block, 64 threads each over the pieces of the vocabulary.
 constexpr int kJoinT = 8;
 __global__ void __launch_bounds__(512)
-join_kernel(const float2* __restrict__ part, int pieces, const float* __restrict__ ly, int T,
-            int V, const int32_t* __restrict__ target, float* __restrict__ nll,
+join_kernel(const float2* __restrict__ part, int pieces, int stride,
+            const float* __restrict__ ly, int T, int V, const int32_t* __restrict__ target, float* __restrict__ nll,
             float* __restrict__ lse, const unsigned int* __restrict__ err) {
   __shared__ float2 s_p[16][kJoinT];
   pdl_wait();
@@ -141,7 +72,7 @@ join_kernel(const float2* __restrict__ part, int pieces, const float* __restrict
   if (t < T) {
 #pragma unroll 8
     for (int i = warp * 4 + (lane >> 3); i < pieces; i += 64) {
-      const float2 q = part[(size_t)i * T + t];
+      const float2 q = part[(size_t)i * stride + t];
       const float k = fmaxf(m, q.x);
       s = s * exp2f(m - k) + q.y * exp2f(q.x - k);
       m = k;
@@ -398,13 +329,27 @@ cudaError_t run_small(eat_head* h, const void* x, const float* xs, int T, const 
   CUtensorMap mx;
   if (!head_encode(&mx, h->w8, x, T, d, n)) return cudaErrorInvalidValue;
   const int ctas = head_small_ctas(h->num_sms, V), kb = h->w8 ? 128 : 64;
-  const HeadSmallArgs a{T, V, (d + kb - 1) / kb, target, xs, h->desc.w_scale, h->part, h->st};
+  HeadSmallArgs a{};
+  a.T = T;
+  a.V = V;
+  a.d = d;
+  a.kblocks = (d + kb - 1) / kb;
+  a.target = target;
+  a.x = x;
+  a.w = h->desc.w;
+  a.xs = xs;
+  a.ws = h->desc.w_scale;
+  a.part = h->part;
+  a.ly = h->ly;
+  a.tickets = h->tickets;
+  a.nll = nll;
+  a.lse = lse;
+  a.st = h->st;
   const cudaError_t e = head_launch_small(h->w8, h->w128, h->w16, mx, a, ctas, st);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(h->w8 ? small_join_kernel<true> : small_join_kernel<false>, dim3(T), dim3(128),
-                    0, st, (const float2*)h->part, ctas, n, (const uint4*)x,
-                    (const uint4*)h->desc.w, d * (h->w8 ? 1 : 2) / 16, xs, h->desc.w_scale, V,
-                    target, nll, lse, (const unsigned int*)h->st.err);
+  if (e != cudaSuccess || head_small_joins(n)) return e;
+  return launch_pdl(join_kernel, dim3((T + kJoinT - 1) / kJoinT), dim3(512), 0, st,
+                    (const float2*)h->part, ctas, n, (const float*)h->ly, T, V, target, nll, lse,
+                    (const unsigned int*)h->st.err);
 }
 
 cudaError_t run_pair(eat_head* h, const void* x, const float* xs, int T, const int32_t* target,
@@ -428,7 +373,7 @@ cudaError_t run_pair(eat_head* h, const void* x, const float* xs, int T, const i
   const cudaError_t e = head_launch_pair(h->w8, false, mx, h->w64, a, h->max_pairs, st);
   if (e != cudaSuccess) return e;
   return launch_pdl(join_kernel, dim3((T + kJoinT - 1) / kJoinT), dim3(512), 0, st,
-                    (const float2*)h->part, up(V, kHeadTile) / 128, (const float*)h->ly, T, V,
+                    (const float2*)h->part, up(V, kHeadTile) / 128, T, (const float*)h->ly, T, V,
                     target, nll, lse, (const unsigned int*)h->st.err);
 }
 
@@ -578,6 +523,7 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
     *parts[i].p = at;
     at += (parts[i].bytes + 255) / 256 * 256;
   }
+  h->tickets = h->st.err + 1;
   e = cudaMemset(h->st.err, 0, 16);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {

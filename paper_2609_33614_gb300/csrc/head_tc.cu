@@ -1,10 +1,11 @@
 // Tensor-core kernels of the vocabulary head: logits l_tv = <x_t, w_v> that live in TMEM only.
 //
-//  small_kernel (loss, up to 128 tokens): a tile is 128 vocabulary rows (M) x the call's tokens (N =
-//      16 .. 128), so a decode call streams the vocabulary matrix once and its MMAs stay below that.
-//      Bound: HBM.  Each CTA takes an equal run of 16-row groups; a thread owns a vocabulary row of
-//      the tile and keeps a running maximum and sum of exponentials per token, joined across the
-//      CTA once at its end.  The k-blocks of a tile go to up to four accumulators, added in fp32: a
+//  small_kernel (loss, up to 128 tokens): a tile is 256 vocabulary rows (two MMAs of M = 128) x the
+//      call's tokens (N = 16 .. 128), so a decode call streams the vocabulary matrix once, the tokens
+//      (which every CTA reads again for each tile, from L2) half as often, and its MMAs stay below that.
+//      Bound: HBM.  Each CTA takes an equal run of 16-row groups, in tiles of equal heights; its warps
+//      keep a running maximum and sum of exponentials per token, joined across the CTA at its end,
+//      and across the CTAs by the one that finishes last.  The k-blocks of a tile go to up to four accumulators, added in fp32: a
 //      tensor-core sum truncates at every step, and shorter sums keep a decode token's loss within
 //      a few 1e-6.
 //  pair_kernel: 256 tokens (M, on an SM pair, cta_group::2) x 256 vocabulary rows (N).  A thread
@@ -30,7 +31,6 @@ namespace {
 
 using namespace ptx;
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowBytes = 128;             // bytes of a k-block's row: 64 bf16 or 128 e4m3
 constexpr int kOperand = 128 * kRowBytes;  // 128 rows of a k-block
 constexpr int kBoxBytes = 64 * kRowBytes;  // a box of 64 rows
@@ -46,21 +46,63 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
   m = n;
 }
 
+// A warp: the target logits of tokens t0, t0 + step, ... as fp32 sums of their own.  A tensor-core sum
+// truncates at every step, which a logit that grows steadily, as a target's does, shows most.
+template <bool W8, typename Args>
+__device__ __forceinline__ void target_logits(const Args& a, int t0, int step, int lane) {
+  const int vecs = a.d / (W8 ? 16 : 8);  // 16-byte pieces of a row
+  for (int t = t0; t < a.T; t += step) {
+    const int y = a.target[t];
+    if (y < 0 || y >= a.V) continue;
+    const uint4* x = (const uint4*)a.x + (size_t)t * vecs;
+    const uint4* w = (const uint4*)a.w + (size_t)y * vecs;
+    float d = 0.f;
+#pragma unroll 4
+    for (int c = lane; c < vecs; c += 32) d = dot16<W8>(x[c], w[c], d);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    if (lane == 0) a.ly[t] = d * kLog2e * (W8 ? a.xs[t] * a.ws[y] : 1.0f);
+  }
+}
+
+// Sums of W values a lane over the warp's lanes: lane l gets the sum of the l % W-th values.  Lanes
+// exchange the halves that they do not keep, so W values take W - 1 shuffles (and one more for 16).
+template <int W>
+__device__ __forceinline__ float column_sums(float (&v)[W], int lane) {
+#pragma unroll
+  for (int h = W / 2; h > 0; h >>= 1) {
+    const bool upper = lane & h;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const float give = upper ? v[i] : v[i + h], keep = upper ? v[i + h] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, h);
+    }
+  }
+  if (W == 16) v[0] += __shfl_xor_sync(0xffffffffu, v[0], 16);
+  return v[0];
+}
+
 // ------------------------------------------------------------------------------ small calls
+constexpr int kSmallRows = 256;  // vocabulary rows of a tile at most: two M = 128 halves
+// The ring of stages of a small call: as many k-blocks of its tiles as fit, up to kSmallStages.
+constexpr int kSmallStages = 16;
+constexpr int kSmallRing = 216 * 1024;
+constexpr int kSmallStageBytes = 40 * 1024;  // of a stage at most, unless one k-block is larger
 template <int N>
 struct SmallCfg {
-  static constexpr int kKps = 2;                                 // k-blocks per stage
-  static constexpr int kSub = kOperand + N * kRowBytes;
-  static constexpr int kStage = kKps * kSub;
-  static constexpr int kStagesRaw = (220 * 1024 - 1024) / kStage;
-  static constexpr int kStages = kStagesRaw > 6 ? 6 : kStagesRaw;
-  static constexpr int kSmem = 1024 + kStages * kStage;
-  static constexpr int kSplits = 256 / N < 4 ? 256 / N : 4;      // accumulators of a tile
-  static constexpr int kAccCols = kSplits * N;
+  static constexpr int kSmem = 1024 + kSmallRing;
+  static constexpr int kSplits = 128 / N < 4 ? 128 / N : 4;      // accumulators of a half tile
+  static constexpr int kHalfCols = kSplits * N;
+  static constexpr int kAccCols = 2 * kHalfCols;
   static constexpr int kTmemCols = 2 * kAccCols;
-  static constexpr int kCols = N < 64 ? N : 64;                  // token columns of a thread
+  static constexpr int kCols = N < 64 ? N : 64;                  // token columns of a warp
+  static constexpr int kChunk = N < 32 ? N : 32;                 // of them at a time
   static constexpr int kEpiWarps = 4 * (N / kCols);
-  static constexpr int kThreads = 64 + 32 * kEpiWarps;
+  static constexpr int kDotWarp = 2 + kEpiWarps;  // the target logits
+  static constexpr int kThreads = 32 * (kDotWarp + 1);
+  // Up to 32 columns the CTA that finishes last joins the sums of all; of more, a kernel of its own
+  // (64 columns: 2 us less of device time, 128: 5; 16: none, and the host saves a launch).
+  static constexpr bool kJoins = N <= 32;  // (head_small_joins)
 };
 
 // The first k-block of accumulator s.
@@ -73,22 +115,23 @@ __global__ void __launch_bounds__(SmallCfg<N>::kThreads, 1)
 small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant__ CUtensorMap map_w16,
              const __grid_constant__ CUtensorMap map_x, const HeadSmallArgs a) {
   using C = SmallCfg<N>;
-  constexpr int S = C::kStages;
   constexpr int kElems = W8 ? 128 : 64;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  __shared__ uint64_t full[S], empty[S], tfull[2], tempty[2], mma_done;
+  __shared__ uint64_t full[kSmallStages], empty[kSmallStages], tfull[2], tempty[2], mma_done;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   __shared__ int32_t s_target[N];
   __shared__ float s_xs[N];
-  __shared__ float2 s_fin[4][N];
+  __shared__ float2 s_fin[4][N], s_join[128 / N][N];
+  __shared__ float s_max[C::kEpiWarps][C::kChunk];
+  __shared__ int s_last;
   volatile int* abort_flag = &abort_word;
   const WaitCtx wc{abort_flag, a.st.err};
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S; ++s) {
+    for (int s = 0; s < kSmallStages; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
@@ -119,6 +162,16 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
   const int row0 = 16 * (int)(groups * blockIdx.x / gridDim.x);
   const int row1 = min(a.V, 16 * (int)(groups * (blockIdx.x + 1) / gridDim.x));
   const int splits = min(C::kSplits, a.kblocks);
+  // in tiles of equal heights, whose stages hold no more than they need: a call is bound by the bytes
+  // in flight
+  const int rows = row1 - row0, tiles = (rows + kSmallRows - 1) / kSmallRows;
+  const int height = ((rows + tiles - 1) / tiles + 15) / 16 * 16;
+  const int a_bytes = height * kRowBytes, sub_bytes = a_bytes + N * kRowBytes;
+  // k-blocks of a stage: a stage costs a round of barriers however little it holds
+  const int kps = max(1, min(8, kSmallStageBytes / sub_bytes)), stage_bytes = kps * sub_bytes;
+  // (an MMA reads its 128 rows whole: the last k-block's reach past a low tile stays inside the ring)
+  const int reach = (height > 128 ? 2 : 1) * kOperand;
+  const int S = min(kSmallStages, (kSmallRing - max(0, reach - sub_bytes)) / stage_bytes);
 
   if (warp == 0) {
     if (elect_one()) {
@@ -127,29 +180,25 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
       uint32_t phase = 0;
       long long issued = 0;
       bool ok = true;
-      for (int r = row0; r < row1 && ok; r += 128) {
-        const int boxes = min(8, (row1 - r + 15) / 16);  // 16-row boxes of the tile
-        for (int kb = 0; kb < a.kblocks; kb += C::kKps) {
-          const int nk = min(C::kKps, a.kblocks - kb);
+      for (int r = row0; r < row1 && ok; r += height) {
+        const int boxes = min(height, row1 - r + 15) / 16;  // 16-row boxes of the tile
+        for (int kb = 0; kb < a.kblocks; kb += kps) {
+          const int nk = min(kps, a.kblocks - kb);
           if (!mbar_wait(&empty[stage], phase ^ 1u, wc, 1u)) {
             ok = false;
             break;
           }
-          uint8_t* st = smem + stage * C::kStage;
-          mbar_expect_tx(&full[stage], nk * (boxes * 16 * kRowBytes + N * kRowBytes));
-#pragma unroll
-          for (int j = 0; j < C::kKps; ++j) {
-            if (j >= nk) break;
-            uint8_t* sj = st + j * C::kSub;
+          mbar_expect_tx(&full[stage], nk * (boxes * 16 + N) * kRowBytes);
+          for (int j = 0; j < nk; ++j) {
+            uint8_t* st = smem + stage * stage_bytes + j * sub_bytes;
             const int kx = (kb + j) * kElems;
-            if (boxes == 8) {
-              tma_load_hint(sj, &map_w128, &full[stage], kx, r, once);
-            } else {
-              for (int b = 0; b < boxes; ++b)
-                tma_load_hint(sj + b * 16 * kRowBytes, &map_w16, &full[stage], kx, r + 16 * b,
-                              once);
-            }
-            tma_load(sj + kOperand, &map_x, &full[stage], kx, 0);
+            tma_load(st + a_bytes, &map_x, &full[stage], kx, 0);
+            int b = 0;
+            for (; b + 8 <= boxes; b += 8)
+              tma_load_hint(st + b * 16 * kRowBytes, &map_w128, &full[stage], kx, r + 16 * b,
+                            once);
+            for (; b < boxes; ++b)
+              tma_load_hint(st + b * 16 * kRowBytes, &map_w16, &full[stage], kx, r + 16 * b, once);
           }
           ++issued;
           if (++stage == S) {
@@ -168,34 +217,37 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
       int stage = 0, local = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int r = row0; r < row1 && ok; r += 128, ++local) {
+      for (int r = row0; r < row1 && ok; r += height, ++local) {
         const int buf = local & 1;
         if (!mbar_wait(&tempty[buf], ((local >> 1) & 1) ^ 1u, wc, 4u)) break;
         tc_fence_after();
+        const bool two = min(height, row1 - r) > 128;
         int split = 0, next = split_begin(1, splits, a.kblocks);
         uint32_t acc = 0;
-        for (int kb = 0; kb < a.kblocks; kb += C::kKps) {
+        for (int kb = 0; kb < a.kblocks; kb += kps) {
+          const int nk = min(kps, a.kblocks - kb);
           if (!mbar_wait(&full[stage], phase, wc, 8u)) {
             ok = false;
             break;
           }
           tc_fence_after();
-#pragma unroll
-          for (int j = 0; j < C::kKps; ++j) {
-            if (kb + j >= a.kblocks) break;
+          for (int j = 0; j < nk; ++j) {
             if (kb + j == next) {
               ++split;
               next = split_begin(split + 1, splits, a.kblocks);
               acc = 0;
             }
             const uint32_t d = tmem_base + (uint32_t)(buf * C::kAccCols + split * N);
-            const uint32_t sa = smem_u32(smem + stage * C::kStage + j * C::kSub);
-            const uint64_t da = sdesc_k(sa), db = sdesc_k(sa + kOperand);
+            const uint32_t sa = smem_u32(smem + stage * stage_bytes + j * sub_bytes);
+            const uint64_t da = sdesc_k(sa), d2 = sdesc_k(sa + kOperand);
+            const uint64_t db = sdesc_k(sa + a_bytes);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              mma<false, W8>(d, da + 2 * k, db + 2 * k, id, acc);
-              acc = 1;
+              mma<false, W8>(d, da + 2 * k, db + 2 * k, id, acc | (uint32_t)k);
+              if (two)
+                mma<false, W8>(d + C::kHalfCols, d2 + 2 * k, db + 2 * k, id, acc | (uint32_t)k);
             }
+            acc = 1;
           }
           mma_commit<false>(&empty[stage]);
           if (++stage == S) {
@@ -208,74 +260,80 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
       mma_commit<false>(&mma_done);  // no MMA may run when TMEM is freed
     }
     if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+  } else if (warp == C::kDotWarp) {
+    target_logits<W8>(a, blockIdx.x, gridDim.x, lane);  // beside the MMAs
   } else {
-    // a thread: vocabulary row 32 q + lane of the tile, columns [col0, col0 + kCols)
+    // A lane has vocabulary row 32 q + lane of each half of the tile; per kChunk token columns the warp
+    // takes their maximum and the sum of exponentials over its rows, which lane l then joins to the
+    // l-th column's so far.  (State in registers, a lane per row, needs the columns unrolled: code
+    // that is fetched once per call for 10 us of 64 columns.)
+    constexpr int W = C::kChunk;
     const int q = warp & 3, half = (warp - 2) >> 2, col0 = half * C::kCols;
-    float m[C::kCols], s[C::kCols];
-#pragma unroll
-    for (int c = 0; c < C::kCols; ++c) {
-      m[c] = kHeadLow;
-      s[c] = 0.f;
-    }
+    float2* const state = s_fin[q] + col0;
+    float* const s_m = s_max[warp - 2];
+    for (int c = lane; c < C::kCols; c += 32) state[c] = make_float2(kHeadLow, 0.f);
     int local = 0;
-    for (int r = row0; r < row1; r += 128, ++local) {
+    for (int r = row0; r < row1; r += height, ++local) {
       const int buf = local & 1;
       if (!warp_wait(&tfull[buf], (local >> 1) & 1, wc, 32u)) break;
       tc_fence_after();
-      const int v = r + 32 * q + lane;
-      const bool live = v < row1;
-      const float sv = W8 && live ? a.ws[v] : 1.0f;
-      // does a token of these columns have its target among the warp's rows?
-      bool hit = false;
-      for (int c = lane; c < C::kCols; c += 32) {
-        const int o = s_target[col0 + c] - (r + 32 * q);
-        hit |= o >= 0 && o < 32;
-      }
-      hit = __any_sync(0xffffffffu, hit);
-      const uint32_t t0 = tmem_base + ((uint32_t)(32 * q) << 16) +
-                          (uint32_t)(buf * C::kAccCols + col0);
+#pragma unroll 1
+      for (int p = 0; p < 2 && 128 * p < min(height, row1 - r); ++p) {
+        const int v = r + 128 * p + 32 * q + lane;
+        const bool live = v < min(r + height, row1);
+        const float sv = W8 && live ? a.ws[v] : 1.0f;
+        const uint32_t t0 = tmem_base + ((uint32_t)(32 * q) << 16) +
+                            (uint32_t)(buf * C::kAccCols + p * C::kHalfCols + col0);
+#pragma unroll 1
+        for (int c0 = 0; c0 < C::kCols; c0 += W) {
+          uint32_t w[W];
+          __syncwarp();
 #pragma unroll
-      for (int c0 = 0; c0 < C::kCols; c0 += 16) {
-        uint32_t w[16], w2[16];
-        __syncwarp();
-        tmem_ld16(t0 + c0, w);
+          for (int j = 0; j < W; j += 16) tmem_ld16(t0 + c0 + j, w + j);
+          tmem_wait_ld();
+#pragma unroll 1
+          for (int i = 1; i < splits; ++i) {
+            uint32_t w2[W];
 #pragma unroll
-        for (int i = 1; i < C::kSplits; ++i) {
-          if (i < splits) {
-            tmem_ld16(t0 + i * N + c0, w2);
+            for (int j = 0; j < W; j += 16) tmem_ld16(t0 + i * N + c0 + j, w2 + j);
             tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+            for (int j = 0; j < W; ++j)
               w[j] = __float_as_uint(__uint_as_float(w[j]) + __uint_as_float(w2[j]));
           }
-        }
-        tmem_wait_ld();
-        if (live) {
+          float l[W];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int c = c0 + j;
-            const float l = __uint_as_float(w[j]) * (W8 ? sv * s_xs[col0 + c] : kLog2e);
-            if (hit && s_target[col0 + c] == v) continue;
-            const float dl = l - m[c], e = ex2(-fabsf(dl));
-            s[c] = dl > 0.f ? fmaf(s[c], e, 1.0f) : s[c] + e;
-            m[c] = fmaxf(m[c], l);
+          for (int j = 0; j < W; ++j) {
+            l[j] = __uint_as_float(w[j]) * (W8 ? sv * s_xs[col0 + c0 + j] : kLog2e);
+            if (!live) l[j] = kHeadLow;
+          }
+          // a column whose target is one of the warp's rows leaves that row out
+          const int o = lane < W ? s_target[col0 + c0 + lane] - (v - lane) : -1;
+          unsigned hits = __ballot_sync(0xffffffffu, o >= 0 && o < 32);
+          if (hits) {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+              if ((hits >> j & 1u) && s_target[col0 + c0 + j] == v) l[j] = kHeadLow;
+          }
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            const float m = warp_max(l[j]);
+            l[j] = ex2(l[j] - m);
+            if (lane == 0) s_m[j] = m;
+          }
+          const float s = column_sums<W>(l, lane);
+          __syncwarp();
+          if (lane < W) {
+            float2 f = state[c0 + lane];
+            join(f.x, f.y, s_m[lane], s);
+            state[c0 + lane] = f;
           }
         }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&tempty[buf]);
-    }
-    // over the warp's rows, then the four warps
-#pragma unroll
-    for (int c = 0; c < C::kCols; ++c) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, m[c], o);
-        const float s2 = __shfl_xor_sync(0xffffffffu, s[c], o);
-        join(m[c], s[c], m2, s2);
-      }
-      if (lane == 0) s_fin[q][col0 + c] = make_float2(m[c], s[c]);
     }
   }
   tc_fence_before();
@@ -287,7 +345,48 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
     for (int i = 1; i < 4; ++i) join(f.x, f.y, s_fin[i][c].x, s_fin[i][c].y);
     a.part[(size_t)blockIdx.x * N + c] = f;
   }
-  if (threadIdx.x == 0) report(a.st, abort_flag);
+  if (!C::kJoins) {
+    if (threadIdx.x == 0) report(a.st, abort_flag);
+    return;
+  }
+  // the CTA that finishes last joins the sums of all (in their order, whichever CTA it is)
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    report(a.st, abort_flag);
+    s_last = atomicInc(a.tickets, gridDim.x - 1) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  // columns c of group k: the CTAs k, k + kGroups, ...
+  constexpr int kGroups = 128 / N;
+  const int c = threadIdx.x % N, k = threadIdx.x / N;
+  if (threadIdx.x < 128) {
+    float m = kHeadLow, s = 0.f;
+    if (c < a.T) {
+#pragma unroll 8
+      for (int i = k; i < (int)gridDim.x; i += kGroups) {
+        const float2 q = __ldcg(a.part + (size_t)i * N + c);
+        join(m, s, q.x, q.y);
+      }
+    }
+    s_join[k][c] = make_float2(m, s);
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < a.T) {
+    const int t = threadIdx.x;
+    float2 f = s_join[0][t];
+#pragma unroll
+    for (int i = 1; i < kGroups; ++i) join(f.x, f.y, s_join[i][t].x, s_join[i][t].y);
+    const int y = s_target[t];
+    float2 r = make_float2(0.f, 0.f);
+    if (y >= a.V) r = make_float2(NAN, NAN);
+    else if (y >= 0) r = token_loss(f.x, f.y, __ldcg(a.ly + t));
+    if (y >= 0 && __ldcg(a.st.err)) r = make_float2(NAN, NAN);
+    a.nll[t] = r.x;
+    if (a.lse) a.lse[t] = r.y;
+  }
 }
 
 // --------------------------------------------------------------------------------- SM pairs
@@ -295,10 +394,10 @@ enum : int { kNll = 0, kExp = 1, kGrad = 2 };
 
 template <int MODE>
 struct PairCfg {
-  static constexpr int kKps = 2;
-  static constexpr int kSub = 2 * kOperand;  // one CTA's 128 rows of A and of B
-  static constexpr int kStage = kKps * kSub;
-  static constexpr int kStages = 3;
+  // a stage is one k-block: 128 rows of A and of B of each CTA (six stages of 32 KB; three of two
+  // k-blocks measured 0 to 2 % slower from 12 to 8192 tokens)
+  static constexpr int kStage = 2 * kOperand;
+  static constexpr int kStages = 6;
   // kExp, kGrad: 32 rows of 64 bytes per epilogue warp, on their way to memory
   static constexpr int kOut = MODE == kNll ? 0 : 8 * 32 * 64;
   static constexpr int kSmem = 1024 + kStages * kStage + kOut;
@@ -503,31 +602,25 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const CUtensorMap* mb = MODE == kGrad && t.dw ? &map_x : &map_b;
         const int ra = t.m0 + (int)rank * 128 + (MODE == kExp ? p.t0 : 0);
         const int rb = t.n0 + (int)rank * 128;
-        for (int kb = 0; kb < t.kb; kb += C::kKps) {
-          const int nk = min(C::kKps, t.kb - kb);
+        for (int kb = 0; kb < t.kb; ++kb) {
           if (!mbar_wait(&empty[stage], phase ^ 1u, wc, 1u)) {
             ok = false;
             break;
           }
-          uint8_t* st = smem + stage * C::kStage;
+          uint8_t* sa = smem + stage * C::kStage;
+          uint8_t* sb = sa + kOperand;
           const uint32_t fb = full0 + 8u * (uint32_t)stage;
-          if (leader) mbar_expect_tx(&full[stage], 2 * nk * C::kSub);
+          if (leader) mbar_expect_tx(&full[stage], 2 * C::kStage);
+          const int kx = (t.k0 + kb) * kElems;
 #pragma unroll
-          for (int j = 0; j < C::kKps; ++j) {
-            if (j >= nk) break;
-            uint8_t* sa = st + j * C::kSub;
-            uint8_t* sb = sa + kOperand;
-            const int kx = (t.k0 + kb + j) * kElems;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              if (MODE == kGrad) {
-                if (t.dw) tma_load_pair(sa + b * kBoxBytes, &map_a, fb, ra + 64 * b, kx);
-                else tma_load_pair(sa + b * kBoxBytes, &map_a, fb, kx, ra + 64 * b);
-                tma_load_pair(sb + b * kBoxBytes, mb, fb, rb + 64 * b, kx + (t.dw ? g.t0 : 0));
-              } else {
-                tma_load_pair(sa + b * kBoxBytes, &map_a, fb, kx, ra + 64 * b);
-                tma_load_pair(sb + b * kBoxBytes, mb, fb, kx, rb + 64 * b);
-              }
+          for (int b = 0; b < 2; ++b) {
+            if (MODE == kGrad) {
+              if (t.dw) tma_load_pair(sa + b * kBoxBytes, &map_a, fb, ra + 64 * b, kx);
+              else tma_load_pair(sa + b * kBoxBytes, &map_a, fb, kx, ra + 64 * b);
+              tma_load_pair(sb + b * kBoxBytes, mb, fb, rb + 64 * b, kx + (t.dw ? g.t0 : 0));
+            } else {
+              tma_load_pair(sa + b * kBoxBytes, &map_a, fb, kx, ra + 64 * b);
+              tma_load_pair(sb + b * kBoxBytes, mb, fb, kx, rb + 64 * b);
             }
           }
           ++issued;
@@ -554,29 +647,20 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         tc_fence_after();
         const uint32_t d0 = tmem_base + (uint32_t)(buf * C::kAccCols);
         const uint32_t id = idesc(W8, 256, 256, MODE == kGrad && t.dw, MODE == kGrad);
-        uint32_t acc = 0;
-        for (int kb = 0; kb < t.kb; kb += C::kKps) {
-          const int nk = min(C::kKps, t.kb - kb);
+        const bool a_mn = MODE == kGrad && t.dw;
+        const int step_a = a_mn ? 128 : 2, step_b = MODE == kGrad ? 128 : 2;
+        for (int kb = 0; kb < t.kb; ++kb) {
           if (!mbar_wait(&full[stage], phase, wc, 8u)) {
             ok = false;
             break;
           }
           tc_fence_after();
+          const uint32_t sa = smem_u32(smem + stage * C::kStage);
+          const uint64_t da = a_mn ? sdesc_mn(sa) : sdesc_k(sa);
+          const uint64_t db = MODE == kGrad ? sdesc_mn(sa + kOperand) : sdesc_k(sa + kOperand);
 #pragma unroll
-          for (int j = 0; j < C::kKps; ++j) {
-            if (j >= nk) break;
-            const uint32_t sa = smem_u32(smem + stage * C::kStage + j * C::kSub);
-            const bool a_mn = MODE == kGrad && t.dw;
-            const uint64_t da = a_mn ? sdesc_mn(sa) : sdesc_k(sa);
-            const uint64_t db =
-                MODE == kGrad ? sdesc_mn(sa + kOperand) : sdesc_k(sa + kOperand);
-            const int step_a = a_mn ? 128 : 2, step_b = MODE == kGrad ? 128 : 2;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              mma<true, W8>(d0, da + k * step_a, db + k * step_b, id, acc);
-              acc = 1;
-            }
-          }
+          for (int k = 0; k < 4; ++k)
+            mma<true, W8>(d0, da + k * step_a, db + k * step_b, id, kb > 0 || k > 0);
           mma_commit<true>(&empty[stage]);
           if (++stage == S) {
             stage = 0;
@@ -589,22 +673,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
     if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
   } else if (MODE == kNll && warp == C::kDotWarp) {
-    // the target logits as fp32 sums of their own, beside the MMAs: a tensor-core sum truncates at
-    // every step, which a logit that grows steadily, as a target's does, shows most
-    constexpr int kVec = W8 ? 16 : 8;  // elements of 16 bytes
-    const int vecs = p.d / kVec;
-    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
-      const int y = p.target[t];
-      if (y < 0 || y >= V) continue;
-      const uint4* x = (const uint4*)p.x + (size_t)t * vecs;
-      const uint4* w = (const uint4*)p.w + (size_t)y * vecs;
-      float d = 0.f;
-#pragma unroll 4
-      for (int c = lane; c < vecs; c += 32) d = dot16<W8>(x[c], w[c], d);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-      if (lane == 0) p.ly[t] = d * kLog2e * (W8 ? p.xs[t] * p.ws[y] : 1.0f);
-    }
+    target_logits<W8>(p, blockIdx.x, gridDim.x, lane);  // beside the MMAs
   } else {
     // a thread: row 128 rank + 32 q + lane of the tile, columns [128 ch, 128 ch + 128)
     const int q = warp & 3, ch = (warp - 2) >> 2;
@@ -889,6 +958,7 @@ cudaError_t configure_pair(int num_sms, int* max_pairs) {
 }  // namespace
 
 int head_small_n(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
+bool head_small_joins(int n) { return n <= 32; }
 int head_small_ctas(int num_sms, int V) { return std::min(num_sms, (V + 15) / 16); }
 
 cudaError_t head_launch_small(bool w8, const CUtensorMap& w128, const CUtensorMap& w16,

@@ -21,17 +21,25 @@ struct HeadStatus {
   unsigned int* mirror;  // device address of its host-mapped copy
 };
 
-// Loss of up to kHeadSmallT tokens: part[cta][n] = {max, sum of exp2 relative to it} of the base-2
-// logits of the CTA's vocabulary rows, without the targets; n = small_n(T) columns.
+// Loss of up to kHeadSmallT tokens.  part[cta][n]: maximum and sum of exp2 relative to it of the base-2
+// logits of the CTA's vocabulary rows, without the targets; ly[t] the base-2 target logit.  With few
+// columns the CTA that takes the last ticket joins them (tickets: a word that is 0 between calls).
 struct HeadSmallArgs {
-  int T, V, kblocks;
+  int T, V, d, kblocks;
   const int32_t* target;
+  const void* x;    // the matrices themselves, for the target logits
+  const void* w;
   const float* xs;  // e4m3: [T]
   const float* ws;  // e4m3: [V]
   float2* part;
+  float* ly;
+  unsigned int* tickets;
+  float* nll;
+  float* lse;       // or null
   HeadStatus st;
 };
 int head_small_n(int T);
+bool head_small_joins(int n);  // the kernel of n columns writes nll and lse itself
 int head_small_ctas(int num_sms, int V);
 cudaError_t head_launch_small(bool w8, const CUtensorMap& w128, const CUtensorMap& w16,
                               const CUtensorMap& x, const HeadSmallArgs& a, int ctas,
@@ -120,6 +128,17 @@ __device__ __forceinline__ float dot16(uint4 a, uint4 b, float s) {
 #pragma unroll
   for (int i = 0; i < Vec<W8>::kN; ++i) s = fmaf(x.v[i], w.v[i], s);
   return s;
+}
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// nll and lse of a token from the base-2 target logit and the sum of the others' exp2 relative to m
+__device__ __forceinline__ float2 token_loss(float m, float s, float ly) {
+  const float r = (m - ly + log2f(s)) * kLn2;
+  float a = fmaxf(r, 0.f) + log1pf(expf(-fabsf(r)));
+  if (isnan(r)) a = r;
+  return make_float2(a, fmaf(ly, kLn2, a));
 }
 
 // Ordered bits of a float: larger floats have larger bits, and no float has 0 (other than NaNs).
