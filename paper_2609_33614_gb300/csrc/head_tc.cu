@@ -87,7 +87,7 @@ constexpr int kSmallRows = 256;  // vocabulary rows of a tile at most: two M = 1
 // The ring of stages of a small call: as many k-blocks of its tiles as fit, up to kSmallStages.
 constexpr int kSmallStages = 16;
 constexpr int kSmallRing = 216 * 1024;
-constexpr int kSmallStageBytes = 40 * 1024;  // of a stage at most, unless one k-block is larger
+constexpr int kSmallStageBytes = 50 * 1024;  // of a stage at most, unless one k-block is larger
 template <int N>
 struct SmallCfg {
   static constexpr int kSmem = 1024 + kSmallRing;
@@ -975,22 +975,24 @@ cudaError_t head_launch_pair(bool w8, bool exp, const CUtensorMap& x, const CUte
   const long long tokens = exp ? a.cap : a.T;
   const long long units =
       (tokens + kHeadTile - 1) / kHeadTile * ((a.V + kHeadTile - 1) / kHeadTile);
-  const int pairs = (int)std::min<long long>(max_pairs, units);
-  if (exp) return launch_pair<kExp, false>(x, w, w, p, pairs, st);
+  if (exp)
+    return launch_pair<kExp, false>(x, w, w, p, (int)std::min<long long>(max_pairs, units), st);
+  // (a small vocabulary leaves pairs without tiles, but with target logits: 16 tokens a pair)
+  const int pairs = (int)std::min<long long>(max_pairs, std::max<long long>(units, a.T / 16));
   return w8 ? launch_pair<kNll, true>(x, w, w, p, pairs, st)
             : launch_pair<kNll, false>(x, w, w, p, pairs, st);
 }
 
 // A piece whose tiles of dx are few, and whose sums run over the whole vocabulary, would leave most
 // SM pairs waiting for them: the sums are cut so that a slice takes at most half of what every pair
-// has to do anyway, but not below 8 k-blocks (a tile's cost besides its k-blocks, about 12 of them,
-// would outweigh what is gained).  Slices are added by a kernel of their own, in order.
+// has to do anyway (a tile costs about 12 k-blocks besides its own), and not below 12 k-blocks, about
+// what the launch that adds the slices, in order, costs.
 int head_dx_slices(int cap, int V, int d, int max_pairs) {
   const long long dt = (d + kHeadTile - 1) / kHeadTile, kx = (V + 63) / 64, kw = (cap + 63) / 64;
   const long long nx = cap / kHeadTile * dt, nw = (V + kHeadTile - 1) / kHeadTile * dt, fix = 12;
   if (nx >= 2LL * max_pairs) return 1;
   const long long share = (nx * (kx + fix) + nw * (kw + fix)) / max_pairs;
-  const long long len = std::max(8LL, share / 2);
+  const long long len = std::max(12LL, share / 2);
   const long long n = std::min((kx + len - 1) / len, 2LL * max_pairs / nx + 1);
   // (no slice is empty)
   const long long per = (kx + n - 1) / n;
