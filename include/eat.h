@@ -330,7 +330,7 @@ eat_status eat_selftest_expire_wait(eat_handle* h, int64_t limit_ns, void* strea
  *    y_scale[t] * (its bytes): y_scale[t] = max |row| / 448 (1, and bytes 0, where that maximum is
  *    not above 1e-35), the format of the library's e4m3 weights and of an e4m3 head's hidden states.
  * h is rounded to xdtype when it is stored; y is computed from the unrounded fp32 sum.
- * T >= 1, 1 <= d <= 65536, eps > 0.  Any alignment of the element types is accepted. */
+ * 1 <= T <= 2^30, 1 <= d <= 65536, eps > 0.  Any alignment of the element types is accepted. */
 eat_status eat_rms_norm(const void* x, const void* residual, int32_t T, int32_t d, int32_t xdtype,
                         const float* gamma, double eps, void* h, void* y, int32_t ydtype,
                         float* y_scale, void* stream);
@@ -356,7 +356,7 @@ int64_t eat_rms_norm_grad_workspace(int32_t T, int32_t d);
  *   loss = E sum_e f_e (1/n) sum_t softmax(logits_t)_e   (1 for a uniform router, 0 when no token
  *   counts or none selects an expert).
  * Outputs on the device: loss [1] fp32, counts [E] int32, n_tokens [1] int32 (= n).  Sums have a
- * fixed order.  T >= 1, 1 <= E <= 256, 1 <= K <= 16.  work: eat_balance_workspace(T, E) bytes, as
+ * fixed order.  1 <= T <= 2^26, 1 <= E <= 256, 1 <= K <= 16.  work: eat_balance_workspace(T, E) bytes, as
  * above (calls of up to 2048 tokens leave it untouched). */
 eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E, int32_t K,
                             const int32_t* idx, const uint8_t* mask, float* loss, int32_t* counts,

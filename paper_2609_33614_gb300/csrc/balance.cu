@@ -17,6 +17,7 @@ namespace eat {
 
 namespace {
 
+constexpr int kMaxTokens = 1 << 26;  // times 16 selections: counts stay within an int
 constexpr int kTok = 4;
 constexpr int kWarps = 16;
 constexpr int kThreads = 32 * kWarps;
@@ -305,8 +306,8 @@ extern "C" eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E
   const char* fn = "eat_balance_loss";
   if (!logits || !idx || !loss || !counts || !n_tokens || !work)
     return bad(fn, "logits, idx, loss, counts, n_tokens and work must be non-NULL");
-  if (T < 1 || E < 1 || E > kMaxExperts || K < 1 || K > kMaxK)
-    return bad(fn, "need T >= 1, 1 <= E <= 256 and 1 <= K <= 16");
+  if (T < 1 || T > kMaxTokens || E < 1 || E > kMaxExperts || K < 1 || K > kMaxK)
+    return bad(fn, "need T >= 1, T <= 2^26, 1 <= E <= 256 and 1 <= K <= 16");
   if (misaligned(logits, 4) || misaligned(idx, 4) || misaligned(loss, 4) ||
       misaligned(counts, 4) || misaligned(n_tokens, 4) || misaligned(work, 16))
     return bad(fn, "misaligned pointer");
@@ -333,7 +334,8 @@ extern "C" eat_status eat_balance_grad(const float* logits, int32_t T, int32_t E
   const char* fn = "eat_balance_grad";
   if (!logits || !counts || !n_tokens || !g || !dlogits)
     return bad(fn, "logits, counts, n_tokens, g and dlogits must be non-NULL");
-  if (T < 1 || E < 1 || E > kMaxExperts) return bad(fn, "need T >= 1 and 1 <= E <= 256");
+  if (T < 1 || T > kMaxTokens || E < 1 || E > kMaxExperts)
+    return bad(fn, "need T >= 1, T <= 2^26 and 1 <= E <= 256");
   if (misaligned(logits, 4) || misaligned(counts, 4) || misaligned(n_tokens, 4) ||
       misaligned(g, 4) || misaligned(dlogits, 4))
     return bad(fn, "misaligned pointer");

@@ -6,9 +6,10 @@
 //   gradient, n = h rstd:  dx = dres + rstd (gamma dy - n mean(gamma dy n));  dgamma = sum_t dy n
 // Bound: HBM (a row is read once and kept in registers between the reduction and the outputs).
 // A thread holds NV vectors of 16 bytes of a row; a row is taken by a warp (up to 64 vectors) or by a
-// block of as many warps as it needs.  Rows whose length is no multiple of a vector begin at any element: their
-// vectors are the aligned ones of memory, and the first and the last of a row are partial.  All
-// sums are fp32; a value is rounded once, when it is stored.
+// block of as many warps as it needs.  Rows whose length is no multiple of a vector begin at any
+// element: their vectors are the aligned ones of memory, and the first and the last of a row are
+// shared with its neighbours (read whole, masked, and stored element by element).  All sums are
+// fp32; a value is rounded once, when it is stored.
 #include "eat_internal.cuh"
 
 #include <cuda_fp8.h>
@@ -23,6 +24,7 @@ namespace {
 
 constexpr int kThreads = 256;  // of a block whose warps take a row each, and of the plain kernels
 constexpr int kWarps = kThreads / 32;
+constexpr int kMaxRows = 1 << 30;  // row numbers and their strides ahead stay within an int
 constexpr int kMaxThreads = 512;  // of a block that takes a row
 constexpr int kMaxWarps = kMaxThreads / 32;
 // e4m3 rows whose largest value is not above this get the scale 1 (and bytes 0): max / 448 and its
@@ -71,12 +73,13 @@ struct Elem<__nv_bfloat16> {
   }
 };
 
-// Elements [c, c + kN) of a row of d elements as they lie in memory; with ALIGNED the row begins at
-// a vector and c never leaves it, else elements outside the row are 0.
+// Elements [c, c + kN) of a row as they lie in memory.  With ALIGNED the row begins at a vector and c
+// never leaves it; else the vector may begin in the row before and end in the one behind (their
+// elements are there to be masked), and `left` elements from the row's begin on are the matrix's.
 template <typename T, bool ALIGNED>
-__device__ __forceinline__ uint4 load_vec(const T* row, int c, int d) {
+__device__ __forceinline__ uint4 load_vec(const T* row, int c, long long left) {
   constexpr int N = Elem<T>::kN;
-  if (ALIGNED || (c >= 0 && c + N <= d)) return *(const uint4*)(row + c);
+  if (ALIGNED || c + N <= left) return *(const uint4*)(row + c);
   union {
     uint4 u;
     T e[N];
@@ -84,8 +87,16 @@ __device__ __forceinline__ uint4 load_vec(const T* row, int c, int d) {
   v.u = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    if (c + j >= 0 && c + j < d) v.e[j] = row[c + j];
+    if (c + j < left) v.e[j] = row[c + j];
   return v.u;
+}
+// The elements outside the row become 0.
+template <int N, bool ALIGNED>
+__device__ __forceinline__ void mask_vec(float (&v)[N], int c, int d) {
+  if (ALIGNED || (c >= 0 && c + N <= d)) return;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (c + j < 0 || c + j >= d) v[j] = 0.f;
 }
 template <typename T, bool ALIGNED>
 __device__ __forceinline__ void store_vec(T* row, int c, int d, const float* v) {
@@ -161,13 +172,14 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
   const int lane = WARP ? threadIdx.x & 31 : threadIdx.x, ROW = WARP ? 32 : blockDim.x;
   const size_t at = (size_t)t * d;
   const int shift = ALIGNED ? 0 : (int)(at % N);
+  const long long left = (long long)(rows - t) * d;
   uint4 ux[NV], ur[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (lane + i * ROW) * N - shift;
     if (c < d) {
-      ux[i] = load_vec<T, ALIGNED>(x + at, c, d);
-      if (r) ur[i] = load_vec<T, ALIGNED>(r + at, c, d);
+      ux[i] = load_vec<T, ALIGNED>(x + at, c, left);
+      if (r) ur[i] = load_vec<T, ALIGNED>(r + at, c, left);
     }
   }
   float v[NV][N];
@@ -184,6 +196,7 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
         for (int j = 0; j < N; ++j) v[i][j] += w[j];
         store_vec<T, ALIGNED>(h + at, c, d, v[i]);
       }
+      mask_vec<N, ALIGNED>(v[i], c, d);
 #pragma unroll
       for (int j = 0; j < N; ++j) ss = fmaf(v[i][j], v[i][j], ss);
       float g[N];
@@ -216,11 +229,11 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
 #pragma unroll
         for (int j = 0; j < N; j += 4)
           q[j / 4] = __nv_fp8x4_e4m3(make_float4(v[i][j], v[i][j + 1], v[i][j + 2], v[i][j + 3])).__x;
+        // (at + c is a multiple of N in either case)
         uint8_t* o = (uint8_t*)y + at + c;
-        if (ALIGNED && N == 8) {
-          *(uint2*)o = make_uint2(q[0], q[N / 4 - 1]);
-        } else if (ALIGNED) {
-          *(uint32_t*)o = q[0];
+        if (ALIGNED || (c >= 0 && c + N <= d)) {
+          if (N == 8) *(uint2*)o = make_uint2(q[0], q[N / 4 - 1]);
+          else *(uint32_t*)o = q[0];
         } else {
 #pragma unroll
           for (int j = 0; j < N; ++j)
@@ -232,90 +245,84 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
 }
 
 // Threads of the gradient's blocks at most, and blocks that are to fit an SM.
-__host__ __device__ constexpr int grad_threads(bool warp, int nv) {
-  return warp || nv == 2 ? kThreads : kMaxThreads;
-}
-__host__ __device__ constexpr int grad_resident(bool warp, int nv) {
-  return warp || nv == 2 ? 2 : 1;
-}
+__host__ __device__ constexpr int grad_threads(int nv) { return nv <= 2 ? kThreads : kMaxThreads; }
+// Rows of a group on their way or at work: 24 KB each of h, dy and dres at 256 threads and two vectors.
+__host__ __device__ constexpr int grad_stages(int nv) { return nv <= 2 ? 4 : 2; }
 
 // Group b of threads (a warp or the block) takes rows b, b + groups, ... (the number of groups is a
 // multiple of a vector's elements, so these rows begin alike): dx, and in registers the group's sum of
 // dy n, which the block adds up and leaves in part[block].
-// A row's loads are issued before the row ahead of it is reduced (up to two vectors a thread, so that
-// two rows fit the registers of two blocks per SM).
+// Rows are copied ahead into shared memory; each thread waits for, and reads, its own vectors only.
+// (Rows ahead in registers reach one row: 4095 x 4096 with a residual's gradient 31 us, so 22.)
 template <typename T, bool WARP, int NV, bool ALIGNED>
-__global__ void __launch_bounds__(grad_threads(WARP, NV), grad_resident(WARP, NV))
+__global__ void __launch_bounds__(grad_threads(NV), NV <= 2 ? 2 : 1)
 rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __restrict__ gamma,
                      float eps, const T* dy, const T* dres, T* dx, float* __restrict__ part) {
-  constexpr int N = Elem<T>::kN;
+  constexpr int N = Elem<T>::kN, S = grad_stages(NV);
   constexpr int kGroups = WARP ? kWarps : 1;  // per block
-  constexpr bool kAhead = NV <= 2;
   __shared__ float2 red[2][kMaxWarps];
-  extern __shared__ float s_part[];        // warps' sums: [kWarps][d] (WARP)
+  extern __shared__ uint4 ring[];  // [stage][h, dy, dres][NV][thread]; at the end the warps' sums (WARP)
   pdl_wait();
   pdl_launch_dependents();
   const int lane = WARP ? threadIdx.x & 31 : threadIdx.x, ROW = WARP ? 32 : blockDim.x;
   const int t0 = blockIdx.x * kGroups + (WARP ? threadIdx.x >> 5 : 0);
   const int step = gridDim.x * kGroups;
   const int shift = ALIGNED ? 0 : (int)((size_t)t0 * d % N);
-  float acc[NV][N];
+  auto slot = [&](int stage, int a, int i) {
+    return ring + ((stage * 3 + a) * NV + i) * blockDim.x + threadIdx.x;
+  };
+  auto copy = [&](const T* m, int t, int a, int stage) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * ROW) * N - shift;
+      if (c >= d) continue;
+      const T* row = m + (size_t)t * d;
+      uint4* to = slot(stage, a, i);
+      const long long left = (long long)(rows - t) * d;
+      if (ALIGNED || c + N <= left)
+        cp_async16((uint32_t)__cvta_generic_to_shared(to), row + c);
+      else
+        *to = load_vec<T, ALIGNED>(row, c, left);
+    }
+  };
+  auto fetch = [&](int t, int stage) {
+    if (t < rows) {
+      copy(h, t, 0, stage);
+      copy(dy, t, 1, stage);
+      if (dres) copy(dres, t, 2, stage);
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int k = 0; k < S - 1; ++k) fetch(t0 + k * step, k);
+  float acc[NV][N], gm[NV][N];  // sums of dy n; gamma, alike for all rows
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (lane + i * ROW) * N - shift;
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
-  uint4 uh[NV], ug[NV], ur[NV];
-  auto load = [&](int t, uint4 (&a)[NV], uint4 (&b)[NV], uint4 (&r)[NV]) {
-    const size_t at = (size_t)t * d;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * ROW) * N - shift;
-      if (c < d) {
-        a[i] = load_vec<T, ALIGNED>(h + at, c, d);
-        b[i] = load_vec<T, ALIGNED>(dy + at, c, d);
-        if (dres) r[i] = load_vec<T, ALIGNED>(dres + at, c, d);
-      }
-    }
-  };
-  if (kAhead && t0 < rows) load(t0, uh, ug, ur);
-  float gm[kAhead ? NV : 1][N];  // gamma, alike for all rows
-  if constexpr (kAhead) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * ROW) * N - shift;
-      if (c < d) load_gamma<N, ALIGNED>(gamma, c, d, gm[i]);
-    }
+    if (c < d) load_gamma<N, ALIGNED>(gamma, c, d, gm[i]);
   }
-  auto get_gamma = [&](int i, int c, float (&g)[N]) {
-    if constexpr (kAhead) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) g[j] = gm[i][j];
-    } else {
-      load_gamma<N, ALIGNED>(gamma, c, d, g);
-    }
-  };
   int turn = 0;
   for (int t = t0; t < rows; t += step, ++turn) {
     const size_t at = (size_t)t * d;
-    uint4 nh[kAhead ? NV : 1], ng[kAhead ? NV : 1], nr[kAhead ? NV : 1];
-    if constexpr (kAhead) {
-      if (t + step < rows) load(t + step, nh, ng, nr);
-    } else {
-      load(t, uh, ug, ur);
-    }
+    const int stage = turn % S;
+    fetch(t + (S - 1) * step, (turn + S - 1) % S);
+    cp_async_wait<S - 1>();
     float ss = 0.f, dot = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (lane + i * ROW) * N - shift;
       if (c < d) {
-        float v[N], w[N], g[N];
-        Elem<T>::unpack(uh[i], v);
-        Elem<T>::unpack(ug[i], w);
-        get_gamma(i, c, g);
+        float v[N], w[N];
+        Elem<T>::unpack(*slot(stage, 0, i), v);
+        Elem<T>::unpack(*slot(stage, 1, i), w);
+        mask_vec<N, ALIGNED>(v, c, d);
+        mask_vec<N, ALIGNED>(w, c, d);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           ss = fmaf(v[j], v[j], ss);
-          dot = fmaf(g[j] * w[j], v[j], dot);
+          dot = fmaf(gm[i][j] * w[j], v[j], dot);
         }
       }
     }
@@ -326,32 +333,28 @@ rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __re
     for (int i = 0; i < NV; ++i) {
       const int c = (lane + i * ROW) * N - shift;
       if (c < d) {
-        float v[N], w[N], g[N], o[N];
-        Elem<T>::unpack(uh[i], v);
-        Elem<T>::unpack(ug[i], w);
-        get_gamma(i, c, g);
-        if (dres) Elem<T>::unpack(ur[i], o);
+        float v[N], w[N], o[N];
+        Elem<T>::unpack(*slot(stage, 0, i), v);
+        Elem<T>::unpack(*slot(stage, 1, i), w);
+        mask_vec<N, ALIGNED>(v, c, d);
+        mask_vec<N, ALIGNED>(w, c, d);
+        if (dres) Elem<T>::unpack(*slot(stage, 2, i), o);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           const float n = v[j] * rstd;
           acc[i][j] = fmaf(w[j], n, acc[i][j]);
-          const float k = rstd * (g[j] * w[j] - n * m);
+          const float k = rstd * (gm[i][j] * w[j] - n * m);
           o[j] = dres ? o[j] + k : k;
         }
         store_vec<T, ALIGNED>(dx + at, c, d, o);
       }
     }
-    if constexpr (kAhead) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        uh[i] = nh[i];
-        ug[i] = ng[i];
-        ur[i] = nr[i];
-      }
-    }
   }
+  cp_async_wait<0>();
   float* mine = part + (size_t)blockIdx.x * d;
   if (WARP) {
+    float* const s_part = (float*)ring;  // [kWarps][d]
+    __syncthreads();
     float* w = s_part + (threadIdx.x >> 5) * d;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -467,8 +470,8 @@ rms_norm_dgamma_kernel(const float* __restrict__ part, int n_parts, int d,
   if (lane == 0 && blockIdx.x * 32 + warp < d) dgamma[blockIdx.x * 32 + warp] = s;
 }
 
-// Blocks of the gradient's first kernel: at most as many as fit this chip's 152 SMs with 512 threads of
-// 128 registers each, a multiple of a vector's elements unless every group has one row.
+// Blocks of the gradient's first kernel: as many as fit this chip's 152 SMs (512 threads each) at most,
+// a multiple of a vector's elements unless every group has one row.
 constexpr int kGradBlocks = 1216;
 int grad_blocks(int T, int groups, int threads) {
   return std::min((T + groups - 1) / groups, 152 * std::max(1, std::min(8, 512 / threads)));
@@ -526,7 +529,8 @@ extern "C" eat_status eat_rms_norm(const void* x, const void* residual, int32_t 
   const char* fn = "eat_rms_norm";
   if (!x || !gamma || !y) return bad(fn, "x, gamma and y must be non-NULL");
   if (residual && !h) return bad(fn, "a residual needs h");
-  if (T < 1 || d < 1 || d > 65536) return bad(fn, "need T >= 1 and 1 <= d <= 65536");
+  if (T < 1 || T > kMaxRows || d < 1 || d > 65536)
+    return bad(fn, "need T >= 1, T <= 2^30 and 1 <= d <= 65536");
   if (xdtype != EAT_F32 && xdtype != EAT_BF16) return bad(fn, "xdtype must be F32 or BF16");
   if (ydtype != xdtype && ydtype != EAT_FP8_E4M3)
     return bad(fn, "ydtype must be xdtype or FP8_E4M3");
@@ -575,7 +579,8 @@ extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int
   const char* fn = "eat_rms_norm_grad";
   if (!h || !gamma || !dy || !dx || !dgamma || !work)
     return bad(fn, "h, gamma, dy, dx, dgamma and work must be non-NULL");
-  if (T < 1 || d < 1 || d > 65536) return bad(fn, "need T >= 1 and 1 <= d <= 65536");
+  if (T < 1 || T > kMaxRows || d < 1 || d > 65536)
+    return bad(fn, "need T >= 1, T <= 2^30 and 1 <= d <= 65536");
   if (xdtype != EAT_F32 && xdtype != EAT_BF16) return bad(fn, "xdtype must be F32 or BF16");
   if (!((float)eps > 0.0f) || !(eps <= 1e30)) return bad(fn, "eps must be positive");
   const int al = xdtype == EAT_BF16 ? 2 : 4;
@@ -591,11 +596,22 @@ extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int
     int blocks = grad_blocks(T, 1, kThreads);
     if (!(vec && pick_rows<E, true>(d, [&](auto warp, auto nv, auto al, int threads) {
             constexpr bool WARP = decltype(warp)::value;
+            constexpr int NV = decltype(nv)::value;
             blocks = grad_blocks(T, WARP ? kWarps : 1, threads);
-            e = launch_pdl(rms_norm_grad_kernel<E, WARP, decltype(nv)::value, decltype(al)::value>,
-                           dim3(blocks), dim3(threads), WARP ? (size_t)kWarps * d * 4 : 0, st,
-                           (const E*)h, T, d, gamma, (float)eps, (const E*)dy, (const E*)dres,
-                           (E*)dx, (float*)work);
+            // a group with one row needs one stage
+            const bool one = (long long)blocks * (WARP ? kWarps : 1) >= T;
+            const size_t stage = (size_t)3 * NV * threads * 16;
+            const size_t smem = std::max(one ? stage : grad_stages(NV) * stage,
+                                         WARP ? (size_t)kWarps * d * 4 : 0);
+            auto* kernel = rms_norm_grad_kernel<E, WARP, NV, decltype(al)::value>;
+            // (per call: it holds for the current device and context, and takes less than a launch)
+            if (smem > 47 * 1024)
+              e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)smem);
+            if (e == cudaSuccess)
+              e = launch_pdl(kernel, dim3(blocks), dim3(threads), smem, st, (const E*)h, T, d,
+                             gamma, (float)eps, (const E*)dy, (const E*)dres, (E*)dx,
+                             (float*)work);
           })))
       e = launch_pdl(rms_norm_grad_any_kernel<E>, dim3(blocks), dim3(kThreads), 0, st, (const E*)h,
                      T, d, gamma, (float)eps, (const E*)dy, (const E*)dres, (E*)dx, (float*)work);
