@@ -412,10 +412,14 @@ eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_
                              const float* g, float* nll, float* lse, void* dx, void* dw,
                              void* stream);
 
-/* A kernel of the head that gave up on a bounded wait (see EAT_ERR_STATE) makes the nll of its call
- * NaN, and later calls on the handle fail with EAT_ERR_STATE until eat_head_reset, which
- * synchronises `stream`. */
+/* A kernel of the head that gave up on a bounded wait (see EAT_ERR_STATE) makes the nll, dx and dw of
+ * its call NaN (dx and dw alone are incomplete when it was one of their products), and later calls on
+ * the handle fail with EAT_ERR_STATE until eat_head_reset, which synchronises `stream`. */
 eat_status eat_head_reset(eat_head* h, void* stream);
+
+/* Diagnostic of the head's failure state, as eat_selftest_expire_wait: a bounded wait on a barrier
+ * nothing arrives on gives up after limit_ns (1 us .. 1 s) and sets the head's device status word. */
+eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* stream);
 
 /* Last error on the handle (never NULL), or a generic text for a NULL handle. */
 const char* eat_last_error(const eat_handle* h);

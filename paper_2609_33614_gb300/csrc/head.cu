@@ -14,6 +14,8 @@
 // hand, would spend 8 instead of 6 T V d flops and round P once as well.
 #include "head_tc.cuh"
 
+#include "ffn_tc.cuh"
+
 #include <algorithm>
 #include <cstring>
 #include <new>
@@ -62,10 +64,12 @@ constexpr int kJoinT = 8;
 __global__ void __launch_bounds__(512)
 join_kernel(const float2* __restrict__ part, int pieces, int stride,
             const float* __restrict__ ly, int T, int V, const int32_t* __restrict__ target, float* __restrict__ nll,
-            float* __restrict__ lse, const unsigned int* __restrict__ err) {
+            float* __restrict__ lse, const HeadStatus st) {
   __shared__ float2 s_p[16][kJoinT];
   pdl_wait();
   pdl_launch_dependents();
+  const unsigned int err = *st.err;
+  if (err && blockIdx.x == 0 && threadIdx.x == 0) *st.mirror = err;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int t = blockIdx.x * kJoinT + (lane & 7);
   float m = kHeadLow, s = 0.f;
@@ -97,7 +101,7 @@ join_kernel(const float2* __restrict__ part, int pieces, int stride,
   }
   const int y = target[t];
   float2 r = make_float2(0.f, 0.f);
-  if (y >= V || *err) r = make_float2(NAN, NAN);
+  if (y >= V || err) r = make_float2(NAN, NAN);
   else if (y >= 0) r = token_loss(m, s, ly[t]);
   if (y < 0) r = make_float2(0.f, 0.f);
   nll[t] = r.x;
@@ -199,11 +203,13 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
               const uint32_t* __restrict__ row_max, const float* __restrict__ g,
               __nv_bfloat16* __restrict__ e, int ld, float* __restrict__ f,
               uint4* __restrict__ xc, int row_vecs, float* __restrict__ nll,
-              float* __restrict__ lse, const unsigned int* __restrict__ err) {
+              float* __restrict__ lse, const HeadStatus st) {
   __shared__ float s_p[32][33];
   __shared__ float s_f[32];
   pdl_wait();
   pdl_launch_dependents();
+  const unsigned int err = *st.err;
+  if (err && blockIdx.x == 0 && threadIdx.x == 0) *st.mirror = err;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r0 = blockIdx.x * 32, n = min(cap, *n_counted - t0);
   if (r0 >= n) return;
@@ -229,7 +235,7 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
     const float qf = __bfloat162float(q);
     float k = g[t] / (s + exp2f(l2 - ref));
     if (qf > 0.f) k *= s / qf;
-    if (*err) {
+    if (err) {
       a = make_float2(NAN, NAN);
       k = NAN;
     }
@@ -349,7 +355,7 @@ cudaError_t run_small(eat_head* h, const void* x, const float* xs, int T, const 
   if (e != cudaSuccess || head_small_joins(n)) return e;
   return launch_pdl(join_kernel, dim3((T + kJoinT - 1) / kJoinT), dim3(512), 0, st,
                     (const float2*)h->part, ctas, n, (const float*)h->ly, T, V, target, nll, lse,
-                    (const unsigned int*)h->st.err);
+                    h->st);
 }
 
 cudaError_t run_pair(eat_head* h, const void* x, const float* xs, int T, const int32_t* target,
@@ -374,7 +380,7 @@ cudaError_t run_pair(eat_head* h, const void* x, const float* xs, int T, const i
   if (e != cudaSuccess) return e;
   return launch_pdl(join_kernel, dim3((T + kJoinT - 1) / kJoinT), dim3(512), 0, st,
                     (const float2*)h->part, up(V, kHeadTile) / 128, T, (const float*)h->ly, T, V,
-                    target, nll, lse, (const unsigned int*)h->st.err);
+                    target, nll, lse, h->st);
 }
 
 cudaError_t run_grad(eat_head* h, const void* x, int T, const int32_t* target, const float* g,
@@ -410,7 +416,7 @@ cudaError_t run_grad(eat_head* h, const void* x, int T, const int32_t* target, c
                    up(V, kHeadTile) / 128, t0, cap, (const int32_t*)h->n_counted,
                    (const int32_t*)h->rows, (const int32_t*)h->ytok, (const float*)h->ly,
                    (const uint32_t*)h->row_max, g, h->e, h->ld, h->f, (uint4*)h->xc, row_vecs, nll,
-                   lse, (const unsigned int*)h->st.err);
+                   lse, h->st);
     if (e != cudaSuccess) break;
     const int slices = head_dx_slices(cap, V, d, h->max_pairs);
     const HeadGradArgs b{V, d, h->n_counted, t0, cap, h->f, h->rows, (__nv_bfloat16*)dx,
@@ -559,6 +565,18 @@ eat_status eat_head_reset(eat_head* h, void* stream) {
     return fail(EAT_ERR_CUDA, std::string("eat_head_reset: ") + cudaGetErrorString(e));
   *(volatile unsigned int*)h->mirror_host = 0u;
   h->failed = false;
+  return EAT_OK;
+}
+
+eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* stream) {
+  if (!h) return fail(EAT_ERR_INVALID_ARG, "eat_head_selftest_expire_wait: null handle");
+  if (limit_ns < 1000 || limit_ns > 1000000000LL)
+    return fail(EAT_ERR_INVALID_ARG, "eat_head_selftest_expire_wait: need 1 us <= limit_ns <= 1 s");
+  const cudaError_t e = tc_selftest_bounded_wait((unsigned long long)limit_ns, h->st.err,
+                                                 (cudaStream_t)stream);
+  if (e != cudaSuccess)
+    return fail(EAT_ERR_CUDA, std::string("eat_head_selftest_expire_wait launch: ") +
+                                  cudaGetErrorString(e));
   return EAT_OK;
 }
 

@@ -383,7 +383,9 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
     float2 r = make_float2(0.f, 0.f);
     if (y >= a.V) r = make_float2(NAN, NAN);
     else if (y >= 0) r = token_loss(f.x, f.y, __ldcg(a.ly + t));
-    if (y >= 0 && __ldcg(a.st.err)) r = make_float2(NAN, NAN);
+    const unsigned int err = __ldcg(a.st.err);
+    if (y >= 0 && err) r = make_float2(NAN, NAN);
+    if (err && t == 0) *a.st.mirror = err;
     a.nll[t] = r.x;
     if (a.lse) a.lse[t] = r.y;
   }

@@ -96,6 +96,7 @@ _SIGS = {
     "eat_head_nll": (c_i32, [c_vp, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp]),
     "eat_head_nll_grad": (c_i32, [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
     "eat_head_reset": (c_i32, [c_vp, c_vp]),
+    "eat_head_selftest_expire_wait": (c_i32, [c_vp, c_i64, c_vp]),
     "eat_last_error": (ctypes.c_char_p, [c_vp]),
     "eat_status_string": (ctypes.c_char_p, [c_i32]),
 }
@@ -318,6 +319,10 @@ def eat_head_nll_grad(h, x, T, target, g, nll, lse, dx, dw, stream=None):
 
 def eat_head_reset(h, stream=None):
     _check(lib().eat_head_reset(h, _stream(stream)))
+
+
+def eat_head_selftest_expire_wait(h, limit_ns: int, stream=None):
+    _check(lib().eat_head_selftest_expire_wait(h, limit_ns, _stream(stream)))
 
 
 # ------------------------------------------------------------------------------------------------
