@@ -5,12 +5,11 @@
 // at a time, lane l the experts l, l + 32, ..., so that the tokens' loads and shuffles overlap.
 // Counts are integers (shared-memory atomics, any order gives the same); probabilities are summed in
 // fp32 in a fixed order: a lane over its warp's tokens, the block's warps, then the blocks.
-#include "eat_internal.cuh"
+#include "op_checks.cuh"
 
 #include <cooperative_groups.h>
 
 #include <algorithm>
-#include <string>
 #include <type_traits>
 
 namespace eat {
@@ -278,17 +277,6 @@ cudaError_t pick_per(int E, F&& go) {
   return go(std::integral_constant<int, 8>());
 }
 
-eat_status bad(const char* fn, const char* what) {
-  set_thread_error((std::string(fn) + ": " + what).c_str());
-  return EAT_ERR_INVALID_ARG;
-}
-eat_status launched(const char* fn, cudaError_t e) {
-  if (e == cudaSuccess) return EAT_OK;
-  set_thread_error((std::string(fn) + " launch: " + cudaGetErrorString(e)).c_str());
-  return EAT_ERR_CUDA;
-}
-bool misaligned(const void* p, int n) { return ((uintptr_t)p & (uintptr_t)(n - 1)) != 0; }
-
 }  // namespace
 }  // namespace eat
 
@@ -305,12 +293,12 @@ extern "C" eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E
                                        void* stream) {
   const char* fn = "eat_balance_loss";
   if (!logits || !idx || !loss || !counts || !n_tokens || !work)
-    return bad(fn, "logits, idx, loss, counts, n_tokens and work must be non-NULL");
+    return bad_arg(fn, "logits, idx, loss, counts, n_tokens and work must be non-NULL");
   if (T < 1 || T > kMaxTokens || E < 1 || E > kMaxExperts || K < 1 || K > kMaxK)
-    return bad(fn, "need T >= 1, T <= 2^26, 1 <= E <= 256 and 1 <= K <= 16");
+    return bad_arg(fn, "need T >= 1, T <= 2^26, 1 <= E <= 256 and 1 <= K <= 16");
   if (misaligned(logits, 4) || misaligned(idx, 4) || misaligned(loss, 4) ||
       misaligned(counts, 4) || misaligned(n_tokens, 4) || misaligned(work, 16))
-    return bad(fn, "misaligned pointer");
+    return bad_arg(fn, "misaligned pointer");
   const cudaStream_t st = (cudaStream_t)stream;
   const bool one = T <= kOneClusterT;
   const int cluster = one && T > kOneBlockT ? kCluster : 1, blocks = one ? cluster : blocks_for(T);
@@ -333,12 +321,12 @@ extern "C" eat_status eat_balance_grad(const float* logits, int32_t T, int32_t E
                                        void* stream) {
   const char* fn = "eat_balance_grad";
   if (!logits || !counts || !n_tokens || !g || !dlogits)
-    return bad(fn, "logits, counts, n_tokens, g and dlogits must be non-NULL");
+    return bad_arg(fn, "logits, counts, n_tokens, g and dlogits must be non-NULL");
   if (T < 1 || T > kMaxTokens || E < 1 || E > kMaxExperts)
-    return bad(fn, "need T >= 1, T <= 2^26 and 1 <= E <= 256");
+    return bad_arg(fn, "need T >= 1, T <= 2^26 and 1 <= E <= 256");
   if (misaligned(logits, 4) || misaligned(counts, 4) || misaligned(n_tokens, 4) ||
       misaligned(g, 4) || misaligned(dlogits, 4))
-    return bad(fn, "misaligned pointer");
+    return bad_arg(fn, "misaligned pointer");
   return launched(fn, pick_per(E, [&](auto per) {
     return launch_pdl(balance_grad_kernel<decltype(per)::value>, dim3(blocks_for(T)),
                       dim3(kThreads), 0, (cudaStream_t)stream, logits, T, E, mask, counts, n_tokens,

@@ -8,6 +8,7 @@
 #include "ffn_tc.cuh"
 
 #include <algorithm>
+#include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -909,6 +910,18 @@ const char* eat_status_string(eat_status s) {
 
 namespace eat {
 void set_thread_error(const char* msg) { g_err = msg ? msg : ""; }
+eat_status thread_fail(eat_status s, const char* format, ...) noexcept {
+  char msg[256];
+  va_list args;
+  va_start(args, format);
+  vsnprintf(msg, sizeof msg, format, args);
+  va_end(args);
+  try {
+    set_thread_error(msg);
+  } catch (...) {  // no memory for the text: the status says what it can
+  }
+  return s;
+}
 }  // namespace eat
 
 namespace eat {

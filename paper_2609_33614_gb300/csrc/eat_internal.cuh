@@ -242,5 +242,7 @@ cudaError_t launch_ppl_update(const float* nll, int n, double* state, int32_t* s
 // Records msg as the text eat_last_error(NULL) returns on this thread (entry points without a
 // handle).
 void set_thread_error(const char* msg);
+// The same with a printf format; returns s.  Throws nothing.
+eat_status thread_fail(eat_status s, const char* format, ...) noexcept;
 
 }  // namespace eat

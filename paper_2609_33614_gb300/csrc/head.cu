@@ -15,11 +15,11 @@
 #include "head_tc.cuh"
 
 #include "ffn_tc.cuh"
+#include "op_checks.cuh"
 
 #include <algorithm>
 #include <cstring>
 #include <new>
-#include <string>
 
 struct eat_head {
   eat_head_desc desc;
@@ -297,11 +297,6 @@ dx_join_kernel(const float* __restrict__ part, int slices, int t0, int cap, int 
 }
 
 // -------------------------------------------------------------------------------- host side
-eat_status fail(eat_status s, const std::string& msg) {
-  set_thread_error(msg.c_str());
-  return s;
-}
-
 void free_head(eat_head* h) {
   if (!h) return;
   if (h->mirror_host) cudaFreeHost(h->mirror_host);
@@ -313,19 +308,17 @@ int up(int n, int m) { return (n + m - 1) / m * m; }
 
 eat_status check_call(const char* fn, eat_head* h, const void* x, int32_t T,
                       const int32_t* target, const float* nll, const float* lse) {
-  const std::string f(fn);
-  if (!h) return fail(EAT_ERR_INVALID_ARG, f + ": null handle");
-  if (!x || !target || !nll)
-    return fail(EAT_ERR_INVALID_ARG, f + ": x, target and nll must be non-NULL");
-  if (T < 1 || T > h->desc.max_tokens)
-    return fail(EAT_ERR_INVALID_ARG, f + ": T outside [1, max_tokens]");
-  if ((uintptr_t)x & 15) return fail(EAT_ERR_INVALID_ARG, f + ": x must be 16-byte aligned");
-  if (((uintptr_t)target | (uintptr_t)nll | (uintptr_t)lse) & 3)
-    return fail(EAT_ERR_INVALID_ARG, f + ": misaligned pointer");
+  if (!h) return bad_arg(fn, "null handle");
+  if (!x || !target || !nll) return bad_arg(fn, "x, target and nll must be non-NULL");
+  if (T < 1 || T > h->desc.max_tokens) return bad_arg(fn, "T outside [1, max_tokens]");
+  if (misaligned(x, 16)) return bad_arg(fn, "x must be 16-byte aligned");
+  if (misaligned(target, 4) || misaligned(nll, 4) || misaligned(lse, 4))
+    return bad_arg(fn, "misaligned pointer");
   if (!h->failed && *(volatile unsigned int*)h->mirror_host) h->failed = true;
   if (h->failed)
-    return fail(EAT_ERR_STATE, f + ": a kernel of an earlier call gave up on a bounded wait; "
-                                   "eat_head_reset clears the state");
+    return thread_fail(EAT_ERR_STATE,
+                       "%s: a kernel of an earlier call gave up on a bounded wait; eat_head_reset "
+                       "clears the state", fn);
   return EAT_OK;
 }
 
@@ -438,42 +431,42 @@ using namespace eat;
 extern "C" {
 
 eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
-  if (!out) return fail(EAT_ERR_INVALID_ARG, "out is NULL");
+  if (!out) return bad_arg("eat_head_create", "out is NULL");
   *out = nullptr;
-  if (!desc) return fail(EAT_ERR_INVALID_ARG, "desc is NULL");
+  if (!desc) return bad_arg("eat_head_create", "desc is NULL");
   const eat_head_desc& D = *desc;
   if (D.dtype != EAT_BF16 && D.dtype != EAT_FP8_E4M3)
-    return fail(EAT_ERR_UNSUPPORTED, "head dtype must be BF16 or FP8_E4M3");
+    return thread_fail(EAT_ERR_UNSUPPORTED, "head dtype must be BF16 or FP8_E4M3");
   if (D.d_model < 64 || D.d_model % 64 || D.d_model > 16384)
-    return fail(EAT_ERR_UNSUPPORTED, "d_model must be a multiple of 64 up to 16384");
+    return thread_fail(EAT_ERR_UNSUPPORTED, "d_model must be a multiple of 64 up to 16384");
   if (D.vocab < 1 || D.vocab > (1 << 20))
-    return fail(EAT_ERR_UNSUPPORTED, "vocab must be in [1, 2^20]");
+    return thread_fail(EAT_ERR_UNSUPPORTED, "vocab must be in [1, 2^20]");
   if (D.max_tokens < 1 || D.max_tokens > 65536)
-    return fail(EAT_ERR_INVALID_ARG, "max_tokens must be in [1, 65536]");
-  if (!D.w) return fail(EAT_ERR_INVALID_ARG, "w is NULL");
-  if ((uintptr_t)D.w & 15) return fail(EAT_ERR_INVALID_ARG, "w must be 16-byte aligned");
+    return thread_fail(EAT_ERR_INVALID_ARG, "max_tokens must be in [1, 65536]");
+  if (!D.w) return thread_fail(EAT_ERR_INVALID_ARG, "w is NULL");
+  if ((uintptr_t)D.w & 15) return thread_fail(EAT_ERR_INVALID_ARG, "w must be 16-byte aligned");
   if (D.dtype == EAT_FP8_E4M3 && (!D.w_scale || ((uintptr_t)D.w_scale & 3)))
-    return fail(EAT_ERR_INVALID_ARG, "an e4m3 head needs w_scale, 4-byte aligned");
+    return thread_fail(EAT_ERR_INVALID_ARG, "an e4m3 head needs w_scale, 4-byte aligned");
   if (D.with_grad && D.dtype != EAT_BF16)
-    return fail(EAT_ERR_UNSUPPORTED, "gradients need a BF16 head");
+    return thread_fail(EAT_ERR_UNSUPPORTED, "gradients need a BF16 head");
 
   int dev = 0;
   cudaDeviceProp prop;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaGetDeviceProperties(&prop, dev) != cudaSuccess) {
     cudaGetLastError();
-    return fail(EAT_ERR_CUDA, "no CUDA device");
+    return thread_fail(EAT_ERR_CUDA, "no CUDA device");
   }
   if (prop.major != 10 || prop.minor != 3)
-    return fail(EAT_ERR_UNSUPPORTED, "the tensor-core kernels are built for sm_103a (GB300)");
+    return thread_fail(EAT_ERR_UNSUPPORTED, "the tensor-core kernels are built for sm_103a (GB300)");
   eat_head* h = new (std::nothrow) eat_head();
-  if (!h) return fail(EAT_ERR_OOM, "host allocation failed");
+  if (!h) return thread_fail(EAT_ERR_OOM, "host allocation failed");
   h->desc = D;
   h->w8 = D.dtype == EAT_FP8_E4M3;
   h->num_sms = prop.multiProcessorCount;
   cudaError_t e = head_configure(h->num_sms, &h->max_pairs);
   if (e != cudaSuccess) {
     free_head(h);
-    return fail(EAT_ERR_CUDA, std::string("head kernels: ") + cudaGetErrorString(e));
+    return thread_fail(EAT_ERR_CUDA, "head kernels: %s", cudaGetErrorString(e));
   }
 
   const int V = D.vocab, t_pad = up(D.max_tokens, kHeadTile), pieces = up(V, kHeadTile) / 128;
@@ -521,8 +514,8 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
   if (e != cudaSuccess) {
     cudaGetLastError();  // a failed allocation leaves the context usable: clear its error
     free_head(h);
-    return fail(EAT_ERR_OOM, "head workspace of " + std::to_string(total) + " bytes: " +
-                                 cudaGetErrorString(e));
+    return thread_fail(EAT_ERR_OOM, "head workspace of %zu bytes: %s", total,
+                       cudaGetErrorString(e));
   }
   char* at = h->mem;
   for (int i = 0; i < np; ++i) {
@@ -534,7 +527,7 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
     free_head(h);
-    return fail(EAT_ERR_CUDA, std::string("head workspace: ") + cudaGetErrorString(e));
+    return thread_fail(EAT_ERR_CUDA, "head workspace: %s", cudaGetErrorString(e));
   }
   bool ok = head_encode(&h->w128, h->w8, D.w, V, D.d_model, 128) &&
             head_encode(&h->w64, h->w8, D.w, V, D.d_model, 64) &&
@@ -544,7 +537,7 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
          head_encode(&h->e64, false, h->e, h->cap, h->ld, 64);
   if (!ok) {
     free_head(h);
-    return fail(EAT_ERR_CUDA, "cuTensorMapEncodeTiled rejected a head tensor");
+    return thread_fail(EAT_ERR_CUDA, "cuTensorMapEncodeTiled rejected a head tensor");
   }
   *out = h;
   return EAT_OK;
@@ -558,58 +551,49 @@ eat_status eat_head_destroy(eat_head* h) {
 }
 
 eat_status eat_head_reset(eat_head* h, void* stream) {
-  if (!h) return fail(EAT_ERR_INVALID_ARG, "eat_head_reset: null handle");
+  const char* fn = "eat_head_reset";
+  if (!h) return bad_arg(fn, "null handle");
   cudaError_t e = cudaMemsetAsync(h->st.err, 0, 16, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
-  if (e != cudaSuccess)
-    return fail(EAT_ERR_CUDA, std::string("eat_head_reset: ") + cudaGetErrorString(e));
+  if (e != cudaSuccess) return thread_fail(EAT_ERR_CUDA, "%s: %s", fn, cudaGetErrorString(e));
   *(volatile unsigned int*)h->mirror_host = 0u;
   h->failed = false;
   return EAT_OK;
 }
 
 eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* stream) {
-  if (!h) return fail(EAT_ERR_INVALID_ARG, "eat_head_selftest_expire_wait: null handle");
+  const char* fn = "eat_head_selftest_expire_wait";
+  if (!h) return bad_arg(fn, "null handle");
   if (limit_ns < 1000 || limit_ns > 1000000000LL)
-    return fail(EAT_ERR_INVALID_ARG, "eat_head_selftest_expire_wait: need 1 us <= limit_ns <= 1 s");
-  const cudaError_t e = tc_selftest_bounded_wait((unsigned long long)limit_ns, h->st.err,
-                                                 (cudaStream_t)stream);
-  if (e != cudaSuccess)
-    return fail(EAT_ERR_CUDA, std::string("eat_head_selftest_expire_wait launch: ") +
-                                  cudaGetErrorString(e));
-  return EAT_OK;
+    return bad_arg(fn, "need 1 us <= limit_ns <= 1 s");
+  return launched(fn, tc_selftest_bounded_wait((unsigned long long)limit_ns, h->st.err,
+                                               (cudaStream_t)stream));
 }
 
 eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_t T,
                         const int32_t* target, float* nll, float* lse, void* stream) {
-  const eat_status s = check_call("eat_head_nll", h, x, T, target, nll, lse);
+  const char* fn = "eat_head_nll";
+  const eat_status s = check_call(fn, h, x, T, target, nll, lse);
   if (s != EAT_OK) return s;
-  if (h->w8 && (!x_scale || ((uintptr_t)x_scale & 3)))
-    return fail(EAT_ERR_INVALID_ARG, "eat_head_nll: an e4m3 head needs x_scale, 4-byte aligned");
+  if (h->w8 && (!x_scale || misaligned(x_scale, 4)))
+    return bad_arg(fn, "an e4m3 head needs x_scale, 4-byte aligned");
   const cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = T <= kHeadSmallT ? run_small(h, x, x_scale, T, target, nll, lse, st)
-                                         : run_pair(h, x, x_scale, T, target, nll, lse, st);
-  if (e != cudaSuccess)
-    return fail(EAT_ERR_CUDA, std::string("eat_head_nll launch: ") + cudaGetErrorString(e));
-  return EAT_OK;
+  return launched(fn, T <= kHeadSmallT ? run_small(h, x, x_scale, T, target, nll, lse, st)
+                                       : run_pair(h, x, x_scale, T, target, nll, lse, st));
 }
 
 eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_t* target,
                              const float* g, float* nll, float* lse, void* dx, void* dw,
                              void* stream) {
-  const eat_status s = check_call("eat_head_nll_grad", h, x, T, target, nll, lse);
+  const char* fn = "eat_head_nll_grad";
+  const eat_status s = check_call(fn, h, x, T, target, nll, lse);
   if (s != EAT_OK) return s;
-  if (!h->desc.with_grad)
-    return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: the handle was created without with_grad");
-  if (!g || !dx || !dw)
-    return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: g, dx and dw must be non-NULL");
-  if ((((uintptr_t)dx | (uintptr_t)dw) & 15) || ((uintptr_t)g & 3))
-    return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: dx and dw must be 16-byte aligned");
-  if (dx == x) return fail(EAT_ERR_INVALID_ARG, "eat_head_nll_grad: dx must not alias x");
-  const cudaError_t e = run_grad(h, x, T, target, g, nll, lse, dx, dw, (cudaStream_t)stream);
-  if (e != cudaSuccess)
-    return fail(EAT_ERR_CUDA, std::string("eat_head_nll_grad launch: ") + cudaGetErrorString(e));
-  return EAT_OK;
+  if (!h->desc.with_grad) return bad_arg(fn, "the handle was created without with_grad");
+  if (!g || !dx || !dw) return bad_arg(fn, "g, dx and dw must be non-NULL");
+  if (misaligned(dx, 16) || misaligned(dw, 16) || misaligned(g, 4))
+    return bad_arg(fn, "dx and dw must be 16-byte aligned");
+  if (dx == x) return bad_arg(fn, "dx must not alias x");
+  return launched(fn, run_grad(h, x, T, target, g, nll, lse, dx, dw, (cudaStream_t)stream));
 }
 
 }  // extern "C"

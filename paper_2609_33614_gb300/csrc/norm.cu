@@ -10,12 +10,11 @@
 // element: their vectors are the aligned ones of memory, and the first and the last of a row are
 // shared with its neighbours (read whole, masked, and stored element by element).  All sums are
 // fp32; a value is rounded once, when it is stored.
-#include "eat_internal.cuh"
+#include "op_checks.cuh"
 
 #include <cuda_fp8.h>
 
 #include <algorithm>
-#include <string>
 #include <type_traits>
 
 namespace eat {
@@ -507,17 +506,6 @@ bool pick_rows(int d, F&& pick) {
   return false;
 }
 
-eat_status bad(const char* fn, const char* what) {
-  set_thread_error((std::string(fn) + ": " + what).c_str());
-  return EAT_ERR_INVALID_ARG;
-}
-eat_status launched(const char* fn, cudaError_t e) {
-  if (e == cudaSuccess) return EAT_OK;
-  set_thread_error((std::string(fn) + " launch: " + cudaGetErrorString(e)).c_str());
-  return EAT_ERR_CUDA;
-}
-bool misaligned(const void* p, int n) { return ((uintptr_t)p & (uintptr_t)(n - 1)) != 0; }
-
 }  // namespace
 }  // namespace eat
 
@@ -527,19 +515,19 @@ extern "C" eat_status eat_rms_norm(const void* x, const void* residual, int32_t 
                                    int32_t xdtype, const float* gamma, double eps, void* h,
                                    void* y, int32_t ydtype, float* y_scale, void* stream) {
   const char* fn = "eat_rms_norm";
-  if (!x || !gamma || !y) return bad(fn, "x, gamma and y must be non-NULL");
-  if (residual && !h) return bad(fn, "a residual needs h");
+  if (!x || !gamma || !y) return bad_arg(fn, "x, gamma and y must be non-NULL");
+  if (residual && !h) return bad_arg(fn, "a residual needs h");
   if (T < 1 || T > kMaxRows || d < 1 || d > 65536)
-    return bad(fn, "need T >= 1, T <= 2^30 and 1 <= d <= 65536");
-  if (xdtype != EAT_F32 && xdtype != EAT_BF16) return bad(fn, "xdtype must be F32 or BF16");
+    return bad_arg(fn, "need T >= 1, T <= 2^30 and 1 <= d <= 65536");
+  if (xdtype != EAT_F32 && xdtype != EAT_BF16) return bad_arg(fn, "xdtype must be F32 or BF16");
   if (ydtype != xdtype && ydtype != EAT_FP8_E4M3)
-    return bad(fn, "ydtype must be xdtype or FP8_E4M3");
-  if (ydtype == EAT_FP8_E4M3 && !y_scale) return bad(fn, "an e4m3 output needs y_scale");
-  if (!((float)eps > 0.0f) || !(eps <= 1e30)) return bad(fn, "eps must be positive");
+    return bad_arg(fn, "ydtype must be xdtype or FP8_E4M3");
+  if (ydtype == EAT_FP8_E4M3 && !y_scale) return bad_arg(fn, "an e4m3 output needs y_scale");
+  if (!((float)eps > 0.0f) || !(eps <= 1e30)) return bad_arg(fn, "eps must be positive");
   const int al = xdtype == EAT_BF16 ? 2 : 4;
   if (misaligned(x, al) || misaligned(residual, al) || (residual && misaligned(h, al)) ||
       misaligned(gamma, 4) || (ydtype == EAT_FP8_E4M3 ? misaligned(y_scale, 4) : misaligned(y, al)))
-    return bad(fn, "misaligned pointer");
+    return bad_arg(fn, "misaligned pointer");
   const bool vec = !(misaligned(x, 16) || misaligned(residual, 16) || misaligned(gamma, 16) ||
                      misaligned(y, 16) || (residual && misaligned(h, 16)));
   const cudaStream_t st = (cudaStream_t)stream;
@@ -578,15 +566,15 @@ extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int
                                         void* stream) {
   const char* fn = "eat_rms_norm_grad";
   if (!h || !gamma || !dy || !dx || !dgamma || !work)
-    return bad(fn, "h, gamma, dy, dx, dgamma and work must be non-NULL");
+    return bad_arg(fn, "h, gamma, dy, dx, dgamma and work must be non-NULL");
   if (T < 1 || T > kMaxRows || d < 1 || d > 65536)
-    return bad(fn, "need T >= 1, T <= 2^30 and 1 <= d <= 65536");
-  if (xdtype != EAT_F32 && xdtype != EAT_BF16) return bad(fn, "xdtype must be F32 or BF16");
-  if (!((float)eps > 0.0f) || !(eps <= 1e30)) return bad(fn, "eps must be positive");
+    return bad_arg(fn, "need T >= 1, T <= 2^30 and 1 <= d <= 65536");
+  if (xdtype != EAT_F32 && xdtype != EAT_BF16) return bad_arg(fn, "xdtype must be F32 or BF16");
+  if (!((float)eps > 0.0f) || !(eps <= 1e30)) return bad_arg(fn, "eps must be positive");
   const int al = xdtype == EAT_BF16 ? 2 : 4;
   if (misaligned(h, al) || misaligned(dy, al) || misaligned(dres, al) || misaligned(dx, al) ||
       misaligned(gamma, 4) || misaligned(dgamma, 4) || misaligned(work, 16))
-    return bad(fn, "misaligned pointer");
+    return bad_arg(fn, "misaligned pointer");
   const cudaStream_t st = (cudaStream_t)stream;
   const bool vec = !(misaligned(h, 16) || misaligned(dy, 16) || misaligned(dres, 16) ||
                      misaligned(dx, 16) || misaligned(gamma, 16));
