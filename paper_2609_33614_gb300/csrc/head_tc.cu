@@ -150,16 +150,12 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
     prefetch_map(&map_x);
   }
   if (warp == 1) tmem_alloc<false>(&tmem_slot, C::kTmemCols);
-  pdl_wait();
-  pdl_launch_dependents();
-  for (int i = threadIdx.x; i < N; i += C::kThreads) {
-    s_target[i] = i < a.T ? a.target[i] : -1;
-    s_xs[i] = kLog2e * (W8 && i < a.T ? a.xs[i] : 1.0f);
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
 
   // this CTA's vocabulary rows
   const long long groups = (a.V + 15) / 16;
@@ -276,6 +272,12 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
     float2* const state = s_fin[q] + col0;
     float* const s_m = s_max[warp - 2];
     for (int c = lane; c < C::kCols; c += 32) state[c] = make_float2(kHeadLow, 0.f);
+    // (by these warps alone: the loads of the vocabulary do not wait for the targets)
+    for (int i = threadIdx.x - 64; i < N; i += 32 * C::kEpiWarps) {
+      s_target[i] = i < a.T ? a.target[i] : -1;
+      s_xs[i] = kLog2e * (W8 && i < a.T ? a.xs[i] : 1.0f);
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * C::kEpiWarps) : "memory");
     int local = 0;
     for (int r = row0; r < row1; r += height, ++local) {
       const int buf = local & 1;
