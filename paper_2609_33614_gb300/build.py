@@ -1,5 +1,6 @@
 """Build libeat.so in-tree for sm_103a (GB300): one nvcc call per translation unit, in parallel,
-then one link.  Rebuilds only when a source, header or flag changed (content hash stamp)."""
+then one link; and beside it _eatops.so, the Python binding of the operators on torch tensors.
+Rebuilds only when a source, header or flag changed (content hash stamp)."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -8,12 +9,14 @@ import hashlib
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libeat.so")
+BINDING = os.path.join(PKG, "_eatops.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xptxas", "-warn-spills",
@@ -85,8 +88,51 @@ def ffn_source_hash() -> str:
     return h.hexdigest()
 
 
+def _build_binding(force: bool = False) -> str:
+    """Compile and link _eatops.so against the installed torch and libeat.so (found beside it)."""
+    import torch
+    src = os.path.join(CSRC, "binding.cpp")
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(ROOT, "include"), os.path.join(root, "include"),
+           os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))), "include"),
+           sysconfig.get_paths()["include"]]
+    flags = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    h = hashlib.sha256(" ".join(flags + inc + [torch.__version__]).encode())
+    for f in (src, os.path.join(ROOT, "include", "eat.h")):
+        with open(f, "rb") as fh:
+            h.update(fh.read())
+    stamp_file = os.path.join(BUILD, "eatops.stamp")
+    if not force and os.path.exists(BINDING) and os.path.exists(stamp_file):
+        with open(stamp_file) as fh:
+            if fh.read().strip() == h.hexdigest():
+                return BINDING
+    obj = os.path.join(BUILD, "binding.o")
+    tmp = BINDING + ".tmp"
+    cxx = os.environ.get("CXX", "g++")
+    # (torch's libraries are loaded before it; libeat.so is found in its own directory)
+    libs = ["-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+            "-L" + PKG, "-l:libeat.so", "-Wl,-rpath,$ORIGIN"]
+    for cmd in ([cxx] + flags + ["-I" + i for i in inc] + ["-c", src, "-o", obj],
+                [cxx, "-shared", "-o", tmp, obj] + libs):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"{' '.join(cmd[:2])} failed on {src}:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BINDING)
+    with open(stamp_file, "w") as fh:
+        fh.write(h.hexdigest())
+    return BINDING
+
+
 def build(verbose: bool = False, force: bool = False) -> str:
-    """Compile and link libeat.so; returns its path."""
+    """Compile and link libeat.so and its Python binding; returns the library's path."""
+    path = _build_library(verbose, force)
+    _build_binding(force)
+    return path
+
+
+def _build_library(verbose: bool, force: bool) -> str:
     os.makedirs(BUILD, exist_ok=True)
     stamp_file = os.path.join(BUILD, "libeat.stamp")
     stamp = _stamp()

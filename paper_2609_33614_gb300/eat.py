@@ -1,4 +1,5 @@
-"""Thin ctypes binding of libeat.so (include/eat.h), same names as the C ABI.
+"""Thin ctypes binding of libeat.so (include/eat.h), same names as the C ABI; the operators around the
+layer also as functions of torch tensors, through _eatops.so.
 
 Argument marshalling only: every step of the layer runs in the CUDA library.  torch tensors are
 used for device memory and streams; pointers are passed as ``tensor.data_ptr()`` and the stream
@@ -326,114 +327,58 @@ def eat_head_selftest_expire_wait(h, limit_ns: int, stream=None):
 
 
 # ------------------------------------------------------------------------------------------------
-# The operators around the layer on torch tensors (still only marshalling).  Tensors are CUDA,
-# contiguous and of the stated type; outputs are new tensors, and calls go to the current stream.
-# A small call is bound by the host, so these check and marshal with as few Python calls as they can.
+# The operators around the layer on torch tensors.  Tensors are CUDA, contiguous and of the stated
+# type (ValueError otherwise); outputs are new tensors, and calls go to the current stream of the
+# inputs' device.  A small call is bound by the host, so _eatops.so (csrc/binding.cpp) checks,
+# allocates and calls the library.
 # ------------------------------------------------------------------------------------------------
-def _take(name, t, shape, dtype):
-    """Raise unless tensor t has this shape and type, contiguous on the GPU; its address."""
-    if t.shape != shape or t.dtype is not dtype:
-        raise ValueError(f"{name}: need {tuple(shape)} {dtype}, got {tuple(t.shape)} {t.dtype}")
-    if not (t.is_cuda and t.is_contiguous()):
-        raise ValueError(f"{name}: need a contiguous CUDA tensor")
-    return t.data_ptr()
+_eatops = None
 
 
-def _take_mask(mask, T):
-    if mask is None:
-        return None
-    return _take("mask", mask, (T,), torch.uint8 if mask.dtype is torch.uint8 else torch.bool)
-
-
-def _rows(name, x):
-    """(T, d, type code, address) of fp32 or bf16 rows [T, d]."""
-    dt = x.dtype
-    if x.dim() != 2 or (dt is not torch.bfloat16 and dt is not torch.float32):
-        raise ValueError(f"{name}: need [T, d] fp32 or bf16 rows, got {tuple(x.shape)} {dt}")
-    T, d = x.shape
-    return T, d, EAT_BF16 if dt is torch.bfloat16 else EAT_F32, _take(name, x, (T, d), dt)
-
-
-def _norm(x, gamma, eps, residual, fp8):
-    T, d, code, px = _rows("x", x)
-    pg = _take("gamma", gamma, (d,), torch.float32)
-    h, pr, ph = x, None, None
-    if residual is not None:
-        pr = _take("residual", residual, (T, d), x.dtype)
-        h = torch.empty_like(x)
-        ph = h.data_ptr()
-    if fp8:
-        y = torch.empty_like(x, dtype=torch.float8_e4m3fn)
-        scale = torch.empty(T, dtype=torch.float32, device=x.device)
-        ps, ycode = scale.data_ptr(), EAT_FP8_E4M3
-    else:
-        y = torch.empty_like(x)
-        scale, ps, ycode = None, None, code
-    _check(lib().eat_rms_norm(px, pr, T, d, code, pg, eps, ph, y.data_ptr(), ycode, ps,
-                              _stream(None)))
-    return y, scale, h
+def _ops():
+    global _eatops
+    if _eatops is None:
+        path = os.path.join(PKG, "_eatops.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it first "
+                               "(python -c 'import __graft_entry__ as g; g.build()')")
+        lib()
+        import importlib.util
+        spec = importlib.util.spec_from_file_location("_eatops", path)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        m.set_error(EatError)
+        _eatops = m
+    return _eatops
 
 
 def rms_norm(x, gamma, eps=1e-6, residual=None):
     """(y, h): h = x + residual, y = RMS norm of h times gamma, both in x's type (x, residual [T, d]
     fp32 or bf16; gamma [d] fp32).  Without a residual h is x itself."""
-    y, _, h = _norm(x, gamma, eps, residual, False)
+    y, _, h = (_eatops or _ops()).norm(x, gamma, eps, residual, False)
     return y, h
 
 
 def rms_norm_fp8(x, gamma, eps=1e-6, residual=None):
     """(q, scale, h): rms_norm with y as torch.float8_e4m3fn rows q and their fp32 scales [T]."""
-    return _norm(x, gamma, eps, residual, True)
+    return (_eatops or _ops()).norm(x, gamma, eps, residual, True)
 
 
 def rms_norm_grad(h, gamma, eps, dy, dres=None):
     """(dx, dgamma) of rms_norm at its stored sum h: dx is the gradient of x and of the residual,
     dres the gradient that reaches h from the residual stream."""
-    T, d, code, ph = _rows("h", h)
-    pg = _take("gamma", gamma, (d,), torch.float32)
-    py = _take("dy", dy, (T, d), h.dtype)
-    pr = None if dres is None else _take("dres", dres, (T, d), h.dtype)
-    L = lib()
-    dx = torch.empty_like(h)
-    dgamma = torch.empty_like(gamma)
-    work = torch.empty(L.eat_rms_norm_grad_workspace(T, d), dtype=torch.uint8, device=h.device)
-    _check(L.eat_rms_norm_grad(ph, T, d, code, pg, eps, py, pr, dx.data_ptr(), dgamma.data_ptr(),
-                               work.data_ptr(), _stream(None)))
-    return dx, dgamma
+    return (_eatops or _ops()).norm_grad(h, gamma, eps, dy, dres)
 
 
 def balance_loss(logits, idx, mask=None):
     """(loss [1], counts [E] int32, n_tokens [1] int32) of router logits [T, E] fp32 and the selected
     experts idx [T, K] int32 of EatLayer.route or forward; mask [T] bool: tokens that count."""
-    T, E = logits.shape
-    K = idx.shape[-1]
-    pl = _take("logits", logits, (T, E), torch.float32)
-    pi = _take("idx", idx, (T, K), torch.int32)
-    pm = _take_mask(mask, T)
-    L = lib()
-    dev = logits.device
-    loss = torch.empty(1, dtype=torch.float32, device=dev)
-    counts = torch.empty(E, dtype=torch.int32, device=dev)
-    n = torch.empty(1, dtype=torch.int32, device=dev)
-    # (a small call leaves its workspace untouched: any address does)
-    work = counts if T <= 2048 else \
-        torch.empty(L.eat_balance_workspace(T, E), dtype=torch.uint8, device=dev)
-    _check(L.eat_balance_loss(pl, T, E, K, pi, pm, loss.data_ptr(), counts.data_ptr(),
-                              n.data_ptr(), work.data_ptr(), _stream(None)))
-    return loss, counts, n
+    return (_eatops or _ops()).balance_loss(logits, idx, mask)
 
 
 def balance_grad(logits, counts, n_tokens, g, mask=None):
     """Gradient of balance_loss to the logits, times g (fp32 [1] on the device)."""
-    T, E = logits.shape
-    pl = _take("logits", logits, (T, E), torch.float32)
-    pc = _take("counts", counts, (E,), torch.int32)
-    pn = _take("n_tokens", n_tokens, (1,), torch.int32)
-    pg = _take("g", g, (1,), torch.float32)
-    pm = _take_mask(mask, T)
-    dlogits = torch.empty_like(logits)
-    _check(lib().eat_balance_grad(pl, T, E, pm, pc, pn, pg, dlogits.data_ptr(), _stream(None)))
-    return dlogits
+    return (_eatops or _ops()).balance_grad(logits, counts, n_tokens, g, mask)
 
 
 class EatHead:
@@ -442,41 +387,27 @@ class EatHead:
 
     def __init__(self, w, max_tokens, w_scale=None, grad=False):
         fp8 = w.dtype is torch.float8_e4m3fn
+        if w.dim() != 2 or not (fp8 or w.dtype is torch.bfloat16) or not w.is_cuda \
+                or not w.is_contiguous():
+            raise ValueError("w: need a contiguous CUDA matrix, bf16 or float8_e4m3fn")
         self.V, self.d = w.shape
-        self.dtype = torch.float8_e4m3fn if fp8 else torch.bfloat16
-        pw = _take("w", w, (self.V, self.d), self.dtype)
-        ps = _take("w_scale", w_scale, (self.V,), torch.float32) if fp8 else None
-        self._keep = [w, w_scale]
+        if fp8 and (w_scale is None or w_scale.shape != (self.V,) or
+                    w_scale.dtype is not torch.float32 or not w_scale.is_cuda
+                    or not w_scale.is_contiguous()):
+            raise ValueError("w_scale: need one fp32 scale per row of w, contiguous, on the GPU")
+        self.w, self.w_scale, self.dtype = w, w_scale, w.dtype
         self.h = eat_head_create(eat_head_desc(self.d, self.V, max_tokens,
-                                               EAT_FP8_E4M3 if fp8 else EAT_BF16, int(grad), pw, ps))
+                                               EAT_FP8_E4M3 if fp8 else EAT_BF16, int(grad),
+                                               _ptr(w), _ptr(w_scale) if fp8 else None))
 
     def nll(self, x, target, x_scale=None):
         """(nll, lse) [T] fp32 of hidden states x [T, d] and targets [T] int32 (negative: ignored);
         x_scale [T] fp32 with an e4m3 head (rms_norm_fp8 makes both)."""
-        T = target.shape[0]
-        px = _take("x", x, (T, self.d), self.dtype)
-        pt = _take("target", target, (T,), torch.int32)
-        ps = None
-        if self.dtype is torch.float8_e4m3fn:
-            ps = _take("x_scale", x_scale, (T,), torch.float32)
-        nll = torch.empty_like(target, dtype=torch.float32)
-        lse = torch.empty_like(nll)
-        _check(lib().eat_head_nll(self.h, px, ps, T, pt, nll.data_ptr(), lse.data_ptr(),
-                                  _stream(None)))
-        return nll, lse
+        return (_eatops or _ops()).head_nll(self.h, self.w, x, target, x_scale)
 
     def nll_grad(self, x, target, g):
         """(nll, lse, dx, dw): the loss, and the gradients of sum(g * nll) to x and w (g [T] fp32)."""
-        T = target.shape[0]
-        px = _take("x", x, (T, self.d), self.dtype)
-        pt = _take("target", target, (T,), torch.int32)
-        pg = _take("g", g, (T,), torch.float32)
-        nll, lse = torch.empty_like(g), torch.empty_like(g)
-        dx = torch.empty_like(x)
-        dw = torch.empty_like(self._keep[0])
-        _check(lib().eat_head_nll_grad(self.h, px, T, pt, pg, nll.data_ptr(), lse.data_ptr(),
-                                       dx.data_ptr(), dw.data_ptr(), _stream(None)))
-        return nll, lse, dx, dw
+        return (_eatops or _ops()).head_nll_grad(self.h, self.w, x, target, g)
 
     def close(self):
         if getattr(self, "h", None):
