@@ -357,7 +357,7 @@ int64_t eat_rms_norm_grad_workspace(int32_t T, int32_t d);
  *   counts or none selects an expert).
  * Outputs on the device: loss [1] fp32, counts [E] int32, n_tokens [1] int32 (= n).  Sums have a
  * fixed order.  1 <= T <= 2^26, 1 <= E <= 256, 1 <= K <= 16.  work: eat_balance_workspace(T, E) bytes, as
- * above (calls of up to 2048 tokens leave it untouched). */
+ * above (calls of up to 1024 tokens leave it untouched). */
 eat_status eat_balance_loss(const float* logits, int32_t T, int32_t E, int32_t K,
                             const int32_t* idx, const uint8_t* mask, float* loss, int32_t* counts,
                             int32_t* n_tokens, void* work, void* stream);

@@ -22,11 +22,11 @@ constexpr int kWarps = 16;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kCluster = 8;
 // Calls of up to kOneBlockT tokens run in one block and up to kOneClusterT in one cluster, whose
-// blocks add up in shared memory: one launch and no sums in memory, which saves the host 4 us a call
-// (15 instead of 19) while the device takes less than that (2000 x 64: 9.4 us, in two launches 4.7).
-// Larger ones are joined by a second launch (16384 x 64: 8.6 us; in clusters, joined twice, 12.0).
+// blocks add up in shared memory: one launch and no sums in memory, 6.4 us of the host a call, as long
+// as the device takes no more (512 x 64: 4.7 us; 2000 x 64: 9.4).  Larger ones are joined by a second
+// launch: 8.4 us of the host (device: 2000 x 64 4.7, 16384 x 64 8.6; in clusters, joined twice, 12.0).
 constexpr int kOneBlockT = kWarps * kTok;
-constexpr int kOneClusterT = 2048;
+constexpr int kOneClusterT = 1024;
 constexpr int kMaxBlocks = 304;  // two per SM
 
 __device__ __forceinline__ float warp_sum(float v) {

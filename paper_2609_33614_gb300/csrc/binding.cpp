@@ -1,7 +1,7 @@
 // Python binding of the operators around the layer (norm, balance loss, vocabulary head) on torch
 // tensors: checks, output allocation and the call into libeat.so, nothing else.  A small call is
 // bound by the host, and ctypes with Python-level allocations took most of it (RMS norm of one row:
-// 13 us a call, here 5).
+// 13 us a call, here 4.4; its gradient 20 and 7.4; balance loss 15 and 6.5).
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>

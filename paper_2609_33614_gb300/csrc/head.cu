@@ -10,7 +10,8 @@
 //   then E_ty := -q with q = bf16(Z'), f_t = g_t / (1 + Z') (Z' / q), and
 //   dx_t = f_t sum_v E_tv w_v (f in fp32),  dw = E^T X', X'_t = bf16(f_t x_t).
 // P enters as f E: its target entry is exact in dx, as f_t q = g_t (1 - p_y); the other entries carry
-// one bf16 rounding of E and that of q.  A second pass that computed the logits again, now with lse at
+// one bf16 rounding of E and that of q.  With up to 128 counted tokens X' has two bf16 parts (head_lo),
+// and with them dw's target terms are exact too; with more they carry the rounding of X'.  A second pass that computed the logits again, now with lse at
 // hand, would spend 8 instead of 6 T V d flops and round P once as well.
 #include "head_tc.cuh"
 
@@ -110,7 +111,8 @@ join_kernel(const float2* __restrict__ part, int pieces, int stride,
 
 // ------------------------------------------------------------------------------- gradient
 // 32 rows per block, a warp each: the i-th counted token's hidden state into xc (zeros up to the end
-// of the last tile) and its base-2 target logit; and for token i, if it does not count, its outputs.
+// of the last tile) and its base-2 target logit, of few tokens twice (head_lo); and for token i, if it
+// does not count, its outputs.
 // Every block finds its tokens itself: each thread counts a run of the targets (1 / 1024 of them),
 // and the runs' prefix sums say which hold the block's rows.  (A launch of its own for the list took
 // 14 us of 8192 tokens on one SM, and 3.5 us of any call.)
@@ -146,14 +148,17 @@ gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_
     n += s_w[i];
   }
   int rank = before + incl - mine;  // of the run's first counted token
-  if (rank < i0 + 32 && rank + mine > i0) {
+  const int lo = head_lo(n);        // where the tokens' rows come a second time, or 0
+  if ((rank < i0 + 32 && rank + mine > i0) ||
+      (lo && rank + lo < i0 + 32 && rank + lo + mine > i0)) {
     for (int t = a; t < b; ++t) {
       const int y = target[t];
       if (y >= 0 && y < V) {
-        if (rank >= i0 && rank < i0 + 32) {
-          s_row[rank - i0] = t;
-          rows[rank] = t;
-          ytok[rank] = y;
+        for (int at = rank; at <= rank + lo; at += max(lo, 1)) {
+          if (at < i0 || at >= i0 + 32) continue;
+          s_row[at - i0] = t;
+          rows[at] = t;
+          ytok[at] = y;
         }
         ++rank;
       }
@@ -163,7 +168,7 @@ gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_
   if (threadIdx.x == 0 && i0 % kHeadTile == 0) far[i0 / kHeadTile] = 0;
   __syncthreads();
   const int i = i0 + warp;
-  if (i < n) {
+  if (i < n || (lo && i >= lo && i < lo + n)) {
     const int t = s_row[warp];
     const uint4* p = x + (size_t)t * row_vecs;
     const uint4* q = w + (size_t)target[t] * row_vecs;
@@ -181,6 +186,11 @@ gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_
     }
   } else if (i < (n + kHeadTile - 1) / kHeadTile * kHeadTile) {
     for (int c = lane; c < row_vecs; c += 32) xc[(size_t)i * row_vecs + c] = make_uint4(0, 0, 0, 0);
+    if (lane == 0) {  // (between the two)
+      ly[i] = INFINITY;
+      row_max[i] = 0;
+      ytok[i] = -1;
+    }
   }
   if (i < T) {
     const int y = target[i];
@@ -213,6 +223,7 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r0 = blockIdx.x * 32, n = min(cap, *n_counted - t0);
   if (r0 >= n) return;
+  const int lo = head_lo(*n_counted);
   const int r = r0 + lane;  // row of the piece
   float s = 0.f;
   if (r < n) {
@@ -240,6 +251,7 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
       k = NAN;
     }
     e[(size_t)r * ld + ytok[t0 + r]] = __float2bfloat16_rn(-qf);
+    if (lo) e[(size_t)(r + lo) * ld + ytok[t0 + r]] = __float2bfloat16_rn(-qf);
     f[t0 + r] = k;
     s_f[lane] = k;
     nll[t] = a.x;
@@ -252,13 +264,17 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
 #pragma unroll 4
     for (int c = lane; c < row_vecs; c += 32) {
       const Vec<false> v(row[c]);
-      uint32_t b[4];
+      uint32_t b[4], left[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(v.v[2 * i] * k, v.v[2 * i + 1] * k);
+        const float u = v.v[2 * i] * k, w = v.v[2 * i + 1] * k;
+        const __nv_bfloat162 p = __floats2bfloat162_rn(u, w);
+        const __nv_bfloat162 q = __floats2bfloat162_rn(u - __low2float(p), w - __high2float(p));
         b[i] = *(const uint32_t*)&p;
+        left[i] = *(const uint32_t*)&q;
       }
       row[c] = make_uint4(b[0], b[1], b[2], b[3]);
+      if (lo) row[(size_t)lo * row_vecs + c] = make_uint4(left[0], left[1], left[2], left[3]);
     }
   }
 }

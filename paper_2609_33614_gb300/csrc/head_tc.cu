@@ -534,11 +534,11 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
   // the launch's tokens (kNll), or the counted ones of its piece
-  int rows = p.T, n_counted = 0;
+  int rows = p.T, n_counted = 0;  // (rows: those of E; n_counted: those of dx)
   if (MODE != kNll) {
     n_counted = MODE == kGrad ? *g.n_counted : *p.n_counted;
     const int t0 = MODE == kGrad ? g.t0 : p.t0, cap = MODE == kGrad ? g.cap : p.cap;
-    rows = max(0, min(cap, n_counted - t0));
+    rows = max(0, min(cap, head_rows(n_counted) - t0));
   }
   const int row_tiles = (rows + kHeadTile - 1) / kHeadTile;
   const int V = MODE == kGrad ? g.V : p.V;
@@ -725,7 +725,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       int dst[4], limit = 0;  // rows of the destination, -1: none
       uint4* const box = (uint4*)(smem + S * C::kStage) + (warp - 2) * 128;
       if (MODE == kGrad) {
-        limit = t.dw ? V : rows;
+        limit = t.dw ? V : min(rows, n_counted - g.t0);
         if (t.dw) {
           const bool last = g.t0 + g.cap >= n_counted;
           add = g.t0 > 0;
@@ -735,7 +735,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           sum = g.dx_part + (size_t)(t.k0 / slice_blocks(V, g.slices)) * g.cap * g.d;
         } else {
           out = g.dx;
-          if (row < rows) factor = g.f[g.t0 + row];
+          if (row < limit) factor = g.f[g.t0 + row];
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {

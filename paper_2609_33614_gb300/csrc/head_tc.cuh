@@ -16,6 +16,15 @@ constexpr float kHeadLow = -3.0e38f;
 // a logit more than this many powers of two above it is taken again, relative to its largest logit.
 constexpr float kHeadFar = 40.0f;
 
+// A gradient over n counted tokens, 1 <= n <= 128, multiplies X' in two bf16 parts: the tokens' rows
+// come a second time head_lo(n) rows further, where X' holds what its first part left over.  (A row of
+// dW often is one token's; with one part it would carry two roundings, and the second costs nothing
+// where a tile of 256 rows, and for 32 tokens a k-block of 64, is there anyway.)
+__host__ __device__ __forceinline__ int head_lo(int n) {
+  return n < 1 || n > 128 ? 0 : n <= 32 ? 32 : n <= 64 ? 64 : 128;
+}
+__host__ __device__ __forceinline__ int head_rows(int n) { return n + head_lo(n); }
+
 struct HeadStatus {
   unsigned int* err;     // device status word
   unsigned int* mirror;  // device address of its host-mapped copy

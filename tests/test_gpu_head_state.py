@@ -78,3 +78,21 @@ def test_vocabulary_updated_in_place():
     b = head.nll(x, y)[0]
     assert not torch.equal(a, b)
     assert torch.equal(eat.EatHead(w.clone(), 40).nll(x, y)[0], b)
+
+
+@pytest.mark.parametrize("T,times", [(1, 1.3), (4, 1.3), (32, 1.3), (33, 1.3), (64, 1.3), (65, 1.3),
+                                     (128, 1.3), (129, 1.9), (700, 1.9)])
+def test_gradients_are_little_more_than_rounded_once(T, times):
+    """The error of dx and dw beside that of rounding the exact gradients to bf16 once.  dx's target
+    terms are exact, and dw's with up to 128 tokens; with more they carry one rounding of their own
+    (1.41 where both are as large on average; mantissas shift it)."""
+    x, w, y = _case(T, 6000, 256, 31)
+    g = torch.rand(T, generator=torch.Generator("cuda").manual_seed(5), device="cuda") / T
+    _, _, dx, dw = eat.EatHead(w, T, grad=True).nll_grad(x, y, g)
+    x64, w64 = x.double(), w.double()
+    p = torch.softmax(x64 @ w64.T, 1)
+    p[torch.arange(T, device="cuda"), y.long()] -= 1.0
+    p *= g.double()[:, None]
+    for got, want, k in ((dx, p @ w64, 1.3), (dw, p.T @ x64, times)):
+        once = (want.bfloat16().double() - want).norm()
+        assert (got.double() - want).norm() <= k * once
