@@ -8,15 +8,15 @@
 //      and across the CTAs by the one that finishes last.  The k-blocks of a tile go to up to four
 //      accumulators, added in fp32: a tensor-core sum truncates at every step (at 4096 terms a logit
 //      is off by 6e-6, biased towards zero), and shorter sums keep a decode token's loss within 1e-6.
-//      One token, 50257 x 2048 bf16: 40 us a call, 5.1 TB/s; 16 tokens, 100000 x 4096: 129 us,
-//      6.4 TB/s; 64 tokens, 100003 x 4096 e4m3: 69 us, 5.9 TB/s.
+//      One token, 50257 x 2048 bf16: 37 us a call, 5.6 TB/s; 16 tokens, 100000 x 4096: 129 us,
+//      6.4 TB/s; 64 tokens, 100003 x 4096 e4m3: 65 us, 6.3 TB/s.
 //  pair_kernel: 256 tokens (M, on an SM pair, cta_group::2) x 256 vocabulary rows (N).  A thread
 //      owns a token's row of the tile, so sums over the vocabulary stay within a thread.  Bound:
 //      tensor pipe.  kNll: running maximum and sum; kExp: exponentials relative to the target's
 //      logit, stored as bf16 for the gradient's products, and their sums; kGrad: dx = f (E W) and
 //      dW = E^T X, operands taken from the row-major matrices as they are (K-major or MN-major).
-//      8192 tokens, 65536 x 2048: kExp 1.95, kGrad 1.88 PFLOP/s, 3.88 ms the whole call; e4m3 loss of
-//      4096 tokens, 65536 x 4096: 3.5 PFLOP/s.
+//      8192 tokens, 65536 x 2048: kExp 1.95, kGrad 1.88 PFLOP/s, 3.83 ms the whole call; e4m3 loss of
+//      4096 tokens, 65536 x 4096: 649 us, 3.4 PFLOP/s.
 // Warp roles as in the expert kernels: warp 0 one elected lane issues TMA, warp 1 owns TMEM and one
 // elected lane issues MMAs, the others drain TMEM (double-buffered accumulators).  Every wait is
 // bounded; on expiry the kernel records it, lets copies and MMAs land, frees TMEM and returns.
