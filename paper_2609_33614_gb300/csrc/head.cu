@@ -173,7 +173,7 @@ gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_
     const uint4* p = x + (size_t)t * row_vecs;
     const uint4* q = w + (size_t)target[t] * row_vecs;
     float d = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int c = lane; c < row_vecs; c += 32) {
       const uint4 v = p[c];
       xc[(size_t)i * row_vecs + c] = v;
@@ -204,8 +204,10 @@ gather_kernel(const uint4* __restrict__ x, const uint4* __restrict__ w, int row_
   }
 }
 
-// After a piece's exponentials, 32 counted tokens per block: their sums, losses and factors; the
-// target entries of E; X' in place of x.
+// After a piece's exponentials, kFinishT counted tokens per block: their sums, losses and factors; the
+// target entries of E; X' in place of x.  (128 threads a token: with 32 tokens per block a call of a few
+// tokens spent 11 to 16 us here, on one SM.)
+constexpr int kFinishT = 8;
 __global__ void __launch_bounds__(1024)
 finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
               const int32_t* __restrict__ n_counted, const int32_t* __restrict__ rows,
@@ -214,68 +216,66 @@ finish_kernel(const float* __restrict__ part, int pieces, int t0, int cap,
               __nv_bfloat16* __restrict__ e, int ld, float* __restrict__ f,
               uint4* __restrict__ xc, int row_vecs, float* __restrict__ nll,
               float* __restrict__ lse, const HeadStatus st) {
-  __shared__ float s_p[32][33];
-  __shared__ float s_f[32];
+  __shared__ float s_p[32][kFinishT], s_f[kFinishT];
   pdl_wait();
   pdl_launch_dependents();
   const unsigned int err = *st.err;
   if (err && blockIdx.x == 0 && threadIdx.x == 0) *st.mirror = err;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r0 = blockIdx.x * 32, n = min(cap, *n_counted - t0);
+  const int counted = *n_counted, n = min(cap, counted - t0), r0 = blockIdx.x * kFinishT;
   if (r0 >= n) return;
-  const int lo = head_lo(*n_counted);
-  const int r = r0 + lane;  // row of the piece
+  const int lo = head_lo(counted);
+  const int r = r0 + (lane & 7);  // row of the piece
   float s = 0.f;
   if (r < n) {
 #pragma unroll 4
-    for (int i = warp; i < pieces; i += 32) s += part[(size_t)i * cap + r];
+    for (int i = warp * 4 + (lane >> 3); i < pieces; i += 128) s += part[(size_t)i * cap + r];
   }
-  s_p[warp][lane] = s;
+  s += __shfl_xor_sync(0xffffffffu, s, 8);
+  s += __shfl_xor_sync(0xffffffffu, s, 16);
+  if (lane < kFinishT) s_p[warp][lane] = s;
   __syncthreads();
-  // warp j: token j's sum
-  const float all = warp_sum(s_p[lane][warp]);
-  __syncthreads();
-  if (lane == 0) s_f[warp] = all;
-  __syncthreads();
-  if (warp == 0 && r < n) {
-    s = s_f[lane];
-    const int t = rows[t0 + r];
-    const float l2 = ly[t0 + r], ref = head_ref(l2, row_max[t0 + r]);
-    float2 a = token_loss(ref, s, l2);
-    const __nv_bfloat16 q = __float2bfloat16_rn(s);
-    const float qf = __bfloat162float(q);
-    float k = g[t] / (s + exp2f(l2 - ref));
-    if (qf > 0.f) k *= s / qf;
-    if (err) {
-      a = make_float2(NAN, NAN);
-      k = NAN;
-    }
-    e[(size_t)r * ld + ytok[t0 + r]] = __float2bfloat16_rn(-qf);
-    if (lo) e[(size_t)(r + lo) * ld + ytok[t0 + r]] = __float2bfloat16_rn(-qf);
-    f[t0 + r] = k;
-    s_f[lane] = k;
-    nll[t] = a.x;
-    if (lse) lse[t] = a.y;
-  }
-  __syncthreads();
-  if (r0 + warp < n) {
-    const float k = s_f[warp];
-    uint4* row = xc + (size_t)(t0 + r0 + warp) * row_vecs;
-#pragma unroll 4
-    for (int c = lane; c < row_vecs; c += 32) {
-      const Vec<false> v(row[c]);
-      uint32_t b[4], left[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float u = v.v[2 * i] * k, w = v.v[2 * i + 1] * k;
-        const __nv_bfloat162 p = __floats2bfloat162_rn(u, w);
-        const __nv_bfloat162 q = __floats2bfloat162_rn(u - __low2float(p), w - __high2float(p));
-        b[i] = *(const uint32_t*)&p;
-        left[i] = *(const uint32_t*)&q;
+  if (warp < kFinishT && r0 + warp < n) {  // warp j: token j
+    const float sum = warp_sum(s_p[lane][warp]);
+    if (lane == 0) {
+      const int i = t0 + r0 + warp, t = rows[i], y = ytok[i];
+      const float l2 = ly[i], ref = head_ref(l2, row_max[i]);
+      float2 a = token_loss(ref, sum, l2);
+      const float qf = __bfloat162float(__float2bfloat16_rn(sum));
+      float k = g[t] / (sum + exp2f(l2 - ref));
+      if (qf > 0.f) k *= sum / qf;
+      if (err) {
+        a = make_float2(NAN, NAN);
+        k = NAN;
       }
-      row[c] = make_uint4(b[0], b[1], b[2], b[3]);
-      if (lo) row[(size_t)lo * row_vecs + c] = make_uint4(left[0], left[1], left[2], left[3]);
+      __nv_bfloat16* to = e + (size_t)(r0 + warp) * ld + y;
+      to[0] = __float2bfloat16_rn(-qf);
+      if (lo) to[(size_t)lo * ld] = __float2bfloat16_rn(-qf);
+      f[i] = k;
+      s_f[warp] = k;
+      nll[t] = a.x;
+      if (lse) lse[t] = a.y;
     }
+  }
+  __syncthreads();
+  const int j = warp >> 2;  // four warps a token
+  if (r0 + j >= n) return;
+  const float k = s_f[j];
+  uint4* row = xc + (size_t)(t0 + r0 + j) * row_vecs;
+#pragma unroll 4
+  for (int c = (warp & 3) * 32 + lane; c < row_vecs; c += 128) {
+    const Vec<false> v(row[c]);
+    uint32_t b[4], left[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float u = v.v[2 * i] * k, w = v.v[2 * i + 1] * k;
+      const __nv_bfloat162 p = __floats2bfloat162_rn(u, w);
+      const __nv_bfloat162 q = __floats2bfloat162_rn(u - __low2float(p), w - __high2float(p));
+      b[i] = *(const uint32_t*)&p;
+      left[i] = *(const uint32_t*)&q;
+    }
+    row[c] = make_uint4(b[0], b[1], b[2], b[3]);
+    if (lo) row[(size_t)lo * row_vecs + c] = make_uint4(left[0], left[1], left[2], left[3]);
   }
 }
 
@@ -421,7 +421,7 @@ cudaError_t run_grad(eat_head* h, const void* x, int T, const int32_t* target, c
     a.redo = 1;
     e = head_launch_pair(false, true, h->x64, h->w64, a, h->max_pairs, st);
     if (e != cudaSuccess) break;
-    e = launch_pdl(finish_kernel, dim3(cap / 32), dim3(1024), 0, st, (const float*)h->part,
+    e = launch_pdl(finish_kernel, dim3(cap / kFinishT), dim3(1024), 0, st, (const float*)h->part,
                    up(V, kHeadTile) / 128, t0, cap, (const int32_t*)h->n_counted,
                    (const int32_t*)h->rows, (const int32_t*)h->ytok, (const float*)h->ly,
                    (const uint32_t*)h->row_max, g, h->e, h->ld, h->f, (uint4*)h->xc, row_vecs, nll,
