@@ -96,3 +96,33 @@ def test_gradients_are_little_more_than_rounded_once(T, times):
     for got, want, k in ((dx, p @ w64, 1.3), (dw, p.T @ x64, times)):
         once = (want.bfloat16().double() - want).norm()
         assert (got.double() - want).norm() <= k * once
+
+
+@pytest.mark.parametrize("ignored", [0.1, 0.6, 0.97])
+def test_gradient_in_pieces_of_tokens(ignored):
+    """A vocabulary of 2^20 rows takes 256 tokens at a time (512 MB of exponentials): sums of dw that
+    go on over pieces, a last piece with few tokens, pieces without any."""
+    T, V, d = 700, 1 << 20, 64
+    x, w, y = _case(T, V, d, 41)
+    gen = torch.Generator("cuda").manual_seed(42)
+    drop = torch.rand(T, generator=gen, device="cuda") < ignored
+    x[drop] = float("nan")
+    y = torch.where(drop, -1, y)
+    g = torch.rand(T, generator=gen, device="cuda") / T
+    head = eat.EatHead(w, T, grad=True)
+    nll, lse, dx, dw = head.nll_grad(x, y, g)
+    on = ~drop
+    x64, w64 = x[on].double(), w.double()
+    logits = x64 @ w64.T
+    want = torch.logsumexp(logits, 1)
+    assert ((lse[on].double() - want).abs() <= 1e-5 * want.abs()).all()
+    p = logits.sub_(want[:, None]).exp_()
+    p[torch.arange(int(on.sum()), device="cuda"), y[on].long()] -= 1.0
+    p *= g[on].double()[:, None]
+    ref = p @ w64
+    assert (dx[on].double() - ref).norm() <= 2.0 ** -8 * ref.norm()
+    assert (dx[drop] == 0).all() and (nll[drop] == 0).all()
+    ref = p.T @ x64
+    del p, logits
+    assert (dw.double() - ref).norm() <= 2.0 ** -8 * ref.norm()
+    head.close()
