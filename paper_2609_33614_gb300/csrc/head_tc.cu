@@ -5,8 +5,8 @@
 //      (which every CTA reads again for each tile, from L2) half as often, and its MMAs stay below that.
 //      Bound: HBM.  Each CTA takes an equal run of 16-row groups, in tiles of equal heights; its warps
 //      keep a running maximum and sum of exponentials per token, joined across the CTA at its end,
-//      and across the CTAs by the one that finishes last.  The k-blocks of a tile go to up to four
-//      accumulators, added in fp32: a tensor-core sum truncates at every step (at 4096 terms a logit
+//      and across the CTAs by the one that finishes last.  The steps of a k-block go to up to four
+//      accumulators in turn, added in fp32: a tensor-core sum truncates at every step (at 4096 terms a logit
 //      is off by 6e-6, biased towards zero), and shorter sums keep a decode token's loss within 1e-6.
 //      One token, 50257 x 2048 bf16: 37 us a call, 5.6 TB/s; 16 tokens, 100000 x 4096: 129 us,
 //      6.4 TB/s; 64 tokens, 100003 x 4096 e4m3: 65 us, 6.3 TB/s.
@@ -87,6 +87,7 @@ __device__ __forceinline__ float column_sums(float (&v)[W], int lane) {
 }
 
 // ------------------------------------------------------------------------------ small calls
+constexpr int kSmallCtas = 160;  // at most (the last one's lanes take five each)
 constexpr int kSmallRows = 256;  // vocabulary rows of a tile at most: two M = 128 halves
 // The ring of stages of a small call: as many k-blocks of its tiles as fit, up to kSmallStages.
 constexpr int kSmallStages = 16;
@@ -109,11 +110,6 @@ struct SmallCfg {
   static constexpr bool kJoins = N <= 32;  // (head_small_joins)
 };
 
-// The first k-block of accumulator s.
-__device__ __forceinline__ int split_begin(int s, int splits, int kblocks) {
-  return (int)((long long)kblocks * s / splits);
-}
-
 template <int N, bool W8>
 __global__ void __launch_bounds__(SmallCfg<N>::kThreads, 1)
 small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant__ CUtensorMap map_w16,
@@ -127,7 +123,7 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
   __shared__ int abort_word;
   __shared__ int32_t s_target[N];
   __shared__ float s_xs[N];
-  __shared__ float2 s_fin[4][N], s_join[128 / N][N];
+  __shared__ float2 s_fin[4][N];
   __shared__ float s_max[C::kEpiWarps][C::kChunk];
   __shared__ int s_last;
   volatile int* abort_flag = &abort_word;
@@ -150,18 +146,10 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
     prefetch_map(&map_x);
   }
   if (warp == 1) tmem_alloc<false>(&tmem_slot, C::kTmemCols);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem_base = tmem_slot;
-  pdl_wait();
-  pdl_launch_dependents();
-
-  // this CTA's vocabulary rows
-  const long long groups = (a.V + 15) / 16;
+  // this CTA's vocabulary rows (worked out before the wait: the divisions take 0.5 us)
+  const unsigned groups = (unsigned)(a.V + 15) / 16;
   const int row0 = 16 * (int)(groups * blockIdx.x / gridDim.x);
   const int row1 = min(a.V, 16 * (int)(groups * (blockIdx.x + 1) / gridDim.x));
-  const int splits = min(C::kSplits, a.kblocks);
   // in tiles of equal heights, whose stages hold no more than they need: a call is bound by the bytes
   // in flight
   const int rows = row1 - row0, tiles = (rows + kSmallRows - 1) / kSmallRows;
@@ -172,6 +160,12 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
   // (an MMA reads its 128 rows whole: the last k-block's reach past a low tile stays inside the ring)
   const int reach = (height > 128 ? 2 : 1) * kOperand;
   const int S = min(kSmallStages, (kSmallRing - max(0, reach - sub_bytes)) / stage_bytes);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
 
   if (warp == 0) {
     if (elect_one()) {
@@ -222,8 +216,6 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
         if (!mbar_wait(&tempty[buf], ((local >> 1) & 1) ^ 1u, wc, 4u)) break;
         tc_fence_after();
         const bool two = min(height, row1 - r) > 128;
-        int split = 0, next = split_begin(1, splits, a.kblocks);
-        uint32_t acc = 0;
         for (int kb = 0; kb < a.kblocks; kb += kps) {
           const int nk = min(kps, a.kblocks - kb);
           if (!mbar_wait(&full[stage], phase, wc, 8u)) {
@@ -232,22 +224,18 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
           }
           tc_fence_after();
           for (int j = 0; j < nk; ++j) {
-            if (kb + j == next) {
-              ++split;
-              next = split_begin(split + 1, splits, a.kblocks);
-              acc = 0;
-            }
-            const uint32_t d = tmem_base + (uint32_t)(buf * C::kAccCols + split * N);
+            const uint32_t d = tmem_base + (uint32_t)(buf * C::kAccCols);
             const uint32_t sa = smem_u32(smem + stage * stage_bytes + j * sub_bytes);
             const uint64_t da = sdesc_k(sa), d2 = sdesc_k(sa + kOperand);
             const uint64_t db = sdesc_k(sa + a_bytes);
+            // (an accumulator's first step is among the first k-block's four)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              mma<false, W8>(d, da + 2 * k, db + 2 * k, id, acc | (uint32_t)k);
-              if (two)
-                mma<false, W8>(d + C::kHalfCols, d2 + 2 * k, db + 2 * k, id, acc | (uint32_t)k);
+              const uint32_t dk = d + (k % C::kSplits) * N;
+              const uint32_t acc = kb + j > 0 || k >= C::kSplits;
+              mma<false, W8>(dk, da + 2 * k, db + 2 * k, id, acc);
+              if (two) mma<false, W8>(dk + C::kHalfCols, d2 + 2 * k, db + 2 * k, id, acc);
             }
-            acc = 1;
           }
           mma_commit<false>(&empty[stage]);
           if (++stage == S) {
@@ -298,7 +286,7 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
           for (int j = 0; j < W; j += 16) tmem_ld16(t0 + c0 + j, w + j);
           tmem_wait_ld();
 #pragma unroll 1
-          for (int i = 1; i < splits; ++i) {
+          for (int i = 1; i < C::kSplits; ++i) {
             uint32_t w2[W];
 #pragma unroll
             for (int j = 0; j < W; j += 16) tmem_ld16(t0 + i * N + c0 + j, w2 + j);
@@ -349,51 +337,65 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
   for (int c = threadIdx.x; c < a.T; c += C::kThreads) {
     float2 f = s_fin[0][c];
     for (int i = 1; i < 4; ++i) join(f.x, f.y, s_fin[i][c].x, s_fin[i][c].y);
-    a.part[(size_t)blockIdx.x * N + c] = f;
+    // [CTA][column] for the kernel that joins them, [column][CTA] for the last CTA's warps
+    a.part[C::kJoins ? (size_t)c * gridDim.x + blockIdx.x : (size_t)blockIdx.x * N + c] = f;
   }
-  if (!C::kJoins) {
-    if (threadIdx.x == 0) report(a.st, abort_flag);
-    return;
-  }
+  if (threadIdx.x == 0) report(a.st, abort_flag);
+  if (!C::kJoins) return;
   // the CTA that finishes last joins the sums of all (in their order, whichever CTA it is)
-  __threadfence();
   __syncthreads();
   if (threadIdx.x == 0) {
-    report(a.st, abort_flag);
-    s_last = atomicInc(a.tickets, gridDim.x - 1) == gridDim.x - 1;
+    // releases what the CTA wrote (the barrier above orders it), and acquires what the others did
+    unsigned int old;
+    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;"
+                 : "=r"(old)
+                 : "l"(a.tickets), "r"(gridDim.x - 1)
+                 : "memory");
+    s_last = old == gridDim.x - 1;
   }
   __syncthreads();
   if (!s_last) return;
-  __threadfence();
-  // columns c of group k: the CTAs k, k + kGroups, ...
-  constexpr int kGroups = 128 / N;
-  const int c = threadIdx.x % N, k = threadIdx.x / N;
-  if (threadIdx.x < 128) {
-    float m = kHeadLow, s = 0.f;
-    if (c < a.T) {
-#pragma unroll 8
-      for (int i = k; i < (int)gridDim.x; i += kGroups) {
-        const float2 q = __ldcg(a.part + (size_t)i * N + c);
-        join(m, s, q.x, q.y);
-      }
-    }
-    s_join[k][c] = make_float2(m, s);
-  }
-  __syncthreads();
-  if ((int)threadIdx.x < a.T) {
-    const int t = threadIdx.x;
-    float2 f = s_join[0][t];
+  // a warp takes every kWarps-th token, all of its loads first
+  constexpr int kWarps = C::kThreads / 32, kTok = (N + kWarps - 1) / kWarps;
+  constexpr int kLoads = kSmallCtas / 32;
+  float2 v[kTok][kLoads];
+  float ly[kTok];
+  const unsigned int err = __ldcg(a.st.err);
 #pragma unroll
-    for (int i = 1; i < kGroups; ++i) join(f.x, f.y, s_join[i][t].x, s_join[i][t].y);
-    const int y = s_target[t];
-    float2 r = make_float2(0.f, 0.f);
-    if (y >= a.V) r = make_float2(NAN, NAN);
-    else if (y >= 0) r = token_loss(f.x, f.y, __ldcg(a.ly + t));
-    const unsigned int err = __ldcg(a.st.err);
-    if (y >= 0 && err) r = make_float2(NAN, NAN);
-    if (err && t == 0) *a.st.mirror = err;
-    a.nll[t] = r.x;
-    if (a.lse) a.lse[t] = r.y;
+  for (int i = 0; i < kTok; ++i) {
+    const int t = warp + i * kWarps;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int cta = k * 32 + lane;
+      v[i][k] = make_float2(kHeadLow, 0.f);
+      if (t < a.T && cta < (int)gridDim.x)
+        v[i][k] = __ldcg(a.part + (size_t)t * gridDim.x + cta);
+    }
+    ly[i] = t < a.T ? __ldcg(a.ly + t) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < kTok; ++i) {
+    const int t = warp + i * kWarps;
+    if (t >= a.T) break;
+    float2 f = v[i][0];
+#pragma unroll
+    for (int k = 1; k < kLoads; ++k) join(f.x, f.y, v[i][k].x, v[i][k].y);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float m = __shfl_xor_sync(0xffffffffu, f.x, o);
+      const float s = __shfl_xor_sync(0xffffffffu, f.y, o);
+      join(f.x, f.y, m, s);
+    }
+    if (lane == 0) {
+      const int y = s_target[t];
+      float2 r = make_float2(0.f, 0.f);
+      if (y >= a.V) r = make_float2(NAN, NAN);
+      else if (y >= 0) r = token_loss(f.x, f.y, ly[i]);
+      if (y >= 0 && err) r = make_float2(NAN, NAN);
+      if (err && t == 0) *a.st.mirror = err;
+      a.nll[t] = r.x;
+      if (a.lse) a.lse[t] = r.y;
+    }
   }
 }
 
@@ -967,7 +969,9 @@ cudaError_t configure_pair(int num_sms, int* max_pairs) {
 
 int head_small_n(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
 bool head_small_joins(int n) { return n <= 32; }
-int head_small_ctas(int num_sms, int V) { return std::min(num_sms, (V + 15) / 16); }
+int head_small_ctas(int num_sms, int V) {
+  return std::min(std::min(num_sms, kSmallCtas), (V + 15) / 16);
+}
 
 cudaError_t head_launch_small(bool w8, const CUtensorMap& w128, const CUtensorMap& w16,
                               const CUtensorMap& x, const HeadSmallArgs& a, int ctas,

@@ -30,9 +30,10 @@ struct HeadStatus {
   unsigned int* mirror;  // device address of its host-mapped copy
 };
 
-// Loss of up to kHeadSmallT tokens.  part[cta][n]: maximum and sum of exp2 relative to it of the base-2
-// logits of the CTA's vocabulary rows, without the targets; ly[t] the base-2 target logit.  With few
-// columns the CTA that takes the last ticket joins them (tickets: a word that is 0 between calls).
+// Loss of up to kHeadSmallT tokens.  part: each CTA's maximum and sum of exp2 relative to it of the base-2
+// logits of its vocabulary rows, without the targets, per column; ly[t] the base-2 target logit.  With
+// few columns the CTA that takes the last ticket joins them (tickets: a word that is 0 between calls),
+// else part is [CTA][column] for the kernel that does.
 struct HeadSmallArgs {
   int T, V, d, kblocks;
   const int32_t* target;
