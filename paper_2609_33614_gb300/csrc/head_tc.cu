@@ -8,14 +8,14 @@
 //      and across the CTAs by the one that finishes last.  The steps of a k-block go to up to four
 //      accumulators in turn, added in fp32: a tensor-core sum truncates at every step (at 4096 terms a logit
 //      is off by 6e-6, biased towards zero), and shorter sums keep a decode token's loss within 1e-6.
-//      One token, 50257 x 2048 bf16: 37 us a call, 5.6 TB/s; 16 tokens, 100000 x 4096: 129 us,
-//      6.4 TB/s; 64 tokens, 100003 x 4096 e4m3: 65 us, 6.3 TB/s.
+//      One token, 50257 x 2048 bf16: 35 us a call, 5.9 TB/s; 16 tokens, 100000 x 4096: 126 us,
+//      6.5 TB/s; 64 tokens, 100003 x 4096 e4m3: 65 us, 6.3 TB/s.
 //  pair_kernel: 256 tokens (M, on an SM pair, cta_group::2) x 256 vocabulary rows (N).  A thread
 //      owns a token's row of the tile, so sums over the vocabulary stay within a thread.  Bound:
 //      tensor pipe.  kNll: running maximum and sum; kExp: exponentials relative to the target's
 //      logit, stored as bf16 for the gradient's products, and their sums; kGrad: dx = f (E W) and
 //      dW = E^T X, operands taken from the row-major matrices as they are (K-major or MN-major).
-//      8192 tokens, 65536 x 2048: kExp 1.95, kGrad 1.88 PFLOP/s, 3.83 ms the whole call; e4m3 loss of
+//      8192 tokens, 65536 x 2048: kExp 1.95, kGrad 1.88 PFLOP/s, 3.86 ms the whole call; e4m3 loss of
 //      4096 tokens, 65536 x 4096: 649 us, 3.4 PFLOP/s.
 // Warp roles as in the expert kernels: warp 0 one elected lane issues TMA, warp 1 owns TMEM and one
 // elected lane issues MMAs, the others drain TMEM (double-buffered accumulators).  Every wait is
@@ -106,7 +106,8 @@ struct SmallCfg {
   static constexpr int kDotWarp = 2 + kEpiWarps;  // the target logits
   static constexpr int kThreads = 32 * (kDotWarp + 1);
   // Up to 32 columns the CTA that finishes last joins the sums of all; of more, a kernel of its own
-  // (64 columns: 2 us less of device time, 128: 5; 16: none, and the host saves a launch).
+  // (40 tokens, 20000 x 1024: 16.0 us that way, 17.8 with the last CTA; 128 columns: 5 us less;
+  // 16: no less, and the host saves a launch)
   static constexpr bool kJoins = N <= 32;  // (head_small_joins)
 };
 
