@@ -313,7 +313,7 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < W; ++j) {
-            const float m = warp_max(l[j]);
+            const float m = fmaxf(warp_max(l[j]), kHeadLow);  // (finite where all are -inf)
             l[j] = ex2(l[j] - m);
             if (lane == 0) s_m[j] = m;
           }

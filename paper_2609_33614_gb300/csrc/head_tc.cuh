@@ -148,7 +148,8 @@ __device__ __forceinline__ float2 token_loss(float m, float s, float ly) {
   const float r = (m - ly + log2f(s)) * kLn2;
   float a = fmaxf(r, 0.f) + log1pf(expf(-fabsf(r)));
   if (isnan(r)) a = r;
-  return make_float2(a, fmaf(ly, kLn2, a));
+  // (a target of logit -inf: the others' sum alone)
+  return make_float2(a, ly == -INFINITY ? (m + log2f(s)) * kLn2 : fmaf(ly, kLn2, a));
 }
 
 // Ordered bits of a float: larger floats have larger bits, and no float has 0 (other than NaNs).

@@ -353,6 +353,29 @@ def test_head_nll_confident_and_hopeless_tokens():
     _check_nll(x.double(), w.double(), y.to(torch.int32), nll, lse)
 
 
+@pytest.mark.parametrize("V", [900, 20000])
+@pytest.mark.parametrize("T", [2, 20, 50, 100, 300])
+def test_head_nll_rows_without_probability(T, V):
+    """Vocabulary rows whose logit is -inf add nothing; as a target they cost infinitely much."""
+    d, dead = 128, slice(100, 2 * V // 3)
+    x, w, target = _head_case(T, V, d, 81, ignored=0.0)
+    x[:, 0] = x[:, 0].abs() + 0.5
+    x[1] = x[0]
+    x, w = x.bfloat16(), w.bfloat16()
+    live = torch.ones(V, dtype=torch.bool, device="cuda")
+    live[dead] = False
+    to_live = torch.cumsum(live, 0).to(torch.int32) - 1
+    w[~live, 0] = -math.inf
+    target = torch.where(live[target.long()], target, target % 100)
+    target[1] = 300
+    nll, lse = eat.EatHead(w, T).nll(x, target)
+    on = torch.arange(T, device="cuda") != 1
+    x64, w64 = x.double(), w[live].double()
+    _check_nll(x64[on], w64, to_live[target[on].long()], nll[on], lse[on])
+    assert float(nll[1]) == math.inf
+    _check_nll(x64[:1], w64, to_live[target[:1].long()], nll[:1], lse[1:2])
+
+
 def _grads64(x, w, target, g):
     V = w.shape[0]
     on = (target >= 0) & (target < V)
