@@ -834,6 +834,12 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           m = n;
         } else {
           float s0 = 0.f, s1 = 0.f;
+          // (columns past the vocabulary, which loads fill with zeros, are no logits)
+          if (nc + 32 > V) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (nc + j >= V) l[j] = kHeadLow;
+          }
 #pragma unroll
           for (int j = 0; j < 32; ++j) m = fmaxf(m, l[j]);
 #pragma unroll

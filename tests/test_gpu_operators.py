@@ -459,6 +459,25 @@ def test_head_grad_far_tokens():
     _check_grads(x.double(), w.double(), target, g.double(), (dx, dw), 4 * dl)
 
 
+@pytest.mark.parametrize("T,V", [(5, 300), (200, 300), (5, 512)])
+def test_head_grad_all_logits_low(T, V):
+    """Every logit of a token near -150: what the vocabulary's last tile pads counts as no row."""
+    d = 128
+    x, w, target = _head_case(T, V, d, 97)
+    x, w = 0.1 * x, 0.02 * w
+    x[::2, 0], w[:, 0] = -15.0, 10.0
+    x, w = x.bfloat16(), w.bfloat16()
+    g = _randn(98, T)
+    nll, lse, dx, dw = eat.EatHead(w, T, grad=True).nll_grad(x, target, g)
+    x64, w64 = x.double(), w.double()
+    _check_nll(x64, w64, target, nll, lse)
+    dl = (d / 16 + 4) * U32 * float((x64.abs() @ w64.abs().T).max())
+    dx64, dw64, ax, aw = _grads64(x64, w64, target, g.double())
+    for have, want, mag in ((dx, dx64, ax), (dw, dw64, aw)):  # (entry by entry: dx[:, 0] cancels)
+        bound = (2 * U16 + 4 * dl) * mag * 1.01 + U16 * want.abs() + 1e-30
+        assert ((have.double() - want).abs() <= bound).all()
+
+
 def test_head_grad_against_differences():
     T, V, d = 60, 400, 128
     x, w, target = _head_case(T, V, d, 101, ignored=0.3)
