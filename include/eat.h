@@ -398,7 +398,8 @@ eat_status eat_head_destroy(eat_head* h);
  *   lse[t] = log sum_v exp l_tv;  nll[t] = lse[t] - l_t,target[t]   (fp32)
  * A token whose target is negative is ignored: nll = lse = 0, whatever its x holds.  One whose
  * target is >= vocab gets nll = lse = NaN.  nll keeps its relative accuracy for confident tokens
- * (it is summed as log(1 + sum over the other v of exp(l_v - l_target))).  lse may be NULL. */
+ * (it is summed as log(1 + sum over the other v of exp(l_v - l_target))).  A vocabulary row of logit
+ * -inf adds nothing, and nll is inf where it is the target.  lse may be NULL. */
 eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_t T,
                         const int32_t* target, float* nll, float* lse, void* stream);
 
