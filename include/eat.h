@@ -407,7 +407,9 @@ eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_
  * e.g. 1 / number of tokens): with P_tv = g[t] (exp(l_tv - lse[t]) - [v = target[t]]),
  *   dx [T, d_model] = P w,  dw [vocab, d_model] = P^T x, both bf16, rounded from fp32 sums.
  * P enters the products as bf16.  Ignored tokens, and tokens whose target is >= vocab, give a zero
- * row of dx and add nothing to dw, whatever their x holds (NaN among it).  dx must not alias x.
+ * row of dx and add nothing to dw, whatever their x holds (NaN among it).  A vocabulary row of logit
+ * -inf has P = 0 and adds nothing to dw; in dx, P w is NaN where w itself is infinite.  dx must not
+ * alias x.
  * dx and dw 16-byte aligned.  Needs a handle created with with_grad. */
 eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_t* target,
                              const float* g, float* nll, float* lse, void* dx, void* dw,

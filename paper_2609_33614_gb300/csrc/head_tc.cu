@@ -844,6 +844,12 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           for (int j = 0; j < 32; ++j) m = fmaxf(m, l[j]);
 #pragma unroll
           for (int j = 0; j < 32; ++j) l[j] = ex2(fmaf(l[j], kLog2e, -ref));
+          // (a row that stands for no token has x = 0, and with a vocabulary row that holds an
+          // infinity a logit of NaN, which X' = 0 would not take out of dW)
+          if (y < 0) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) l[j] = 0.f;
+          }
           if (hit >= 0 && hit < 32) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
