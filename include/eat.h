@@ -399,7 +399,8 @@ eat_status eat_head_destroy(eat_head* h);
  * A token whose target is negative is ignored: nll = lse = 0, whatever its x holds.  One whose
  * target is >= vocab gets nll = lse = NaN.  nll keeps its relative accuracy for confident tokens
  * (it is summed as log(1 + sum over the other v of exp(l_v - l_target))).  A vocabulary row of logit
- * -inf adds nothing, and nll is inf where it is the target.  lse may be NULL. */
+ * -inf adds nothing, and nll is inf where it is the target; one of logit +inf makes nll and lse inf
+ * (where it is the target, nll is the sum's limit: 0, or NaN beside another +inf).  lse may be NULL. */
 eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_t T,
                         const int32_t* target, float* nll, float* lse, void* stream);
 
@@ -408,8 +409,8 @@ eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_
  *   dx [T, d_model] = P w,  dw [vocab, d_model] = P^T x, both bf16, rounded from fp32 sums.
  * P enters the products as bf16.  Ignored tokens, and tokens whose target is >= vocab, give a zero
  * row of dx and add nothing to dw, whatever their x holds (NaN among it).  A vocabulary row of logit
- * -inf has P = 0 and adds nothing to dw; in dx, P w is NaN where w itself is infinite.  dx must not
- * alias x.
+ * -inf has P = 0 and adds nothing to dw; in dx, P w is NaN where w itself is infinite.  A counted
+ * token with a logit of +inf makes its row of dx, and dw, NaN.  dx must not alias x.
  * dx and dw 16-byte aligned.  Needs a handle created with with_grad. */
 eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_t* target,
                              const float* g, float* nll, float* lse, void* dx, void* dw,

@@ -313,7 +313,8 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < W; ++j) {
-            const float m = fmaxf(warp_max(l[j]), kHeadLow);  // (finite where all are -inf)
+            // (finite where all are -inf, or one is +inf)
+            const float m = fminf(fmaxf(warp_max(l[j]), kHeadLow), kHeadHigh);
             l[j] = ex2(l[j] - m);
             if (lane == 0) s_m[j] = m;
           }
@@ -824,6 +825,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           float n = m;
 #pragma unroll
           for (int j = 0; j < 32; ++j) n = fmaxf(n, l[j]);
+          n = fminf(n, kHeadHigh);
           float s0 = s * ex2(m - n), s1 = 0.f;
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
@@ -890,7 +892,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       if (MODE == kExp) {
         p.part[(size_t)(n0 / 128) * p.cap + row] = s;
         if (!p.redo && row < rows && m * kLog2e > ref + kHeadFar) {
-          atomicMax(&p.row_max[p.t0 + row], ordered_bits(m * kLog2e));
+          atomicMax(&p.row_max[p.t0 + row], ordered_bits(fminf(m * kLog2e, kHeadHigh)));
           p.far[(p.t0 + row) / kHeadTile] = 1;
         }
       }

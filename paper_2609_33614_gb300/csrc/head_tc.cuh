@@ -12,6 +12,8 @@ constexpr int kHeadSmallT = 128;  // calls of up to this many tokens stream the 
 constexpr int kHeadTile = 256;    // tokens, vocabulary rows and columns of an SM pair's tile
 // a partial maximum that no logit has set; finite, so that differences of it are not NaN
 constexpr float kHeadLow = -3.0e38f;
+// what a maximum is held to, so that a logit of +inf minus it is +inf and not NaN
+constexpr float kHeadHigh = 3.402823466e38f;
 // Exponentials of the gradient's pass are taken relative to the token's target logit.  A token with
 // a logit more than this many powers of two above it is taken again, relative to its largest logit.
 constexpr float kHeadFar = 40.0f;

@@ -74,3 +74,28 @@ def test_gradient_with_rows_without_probability(T, V):
     # (column 0 of w holds -inf, and 0 times that is NaN)
     ref, mag = p @ w64[:, 1:], p.abs() @ w64[:, 1:].abs()
     assert ((dx[:, 1:].double() - ref).abs() <= 1.01 * k * mag + U16 * ref.abs() + 1e-30).all()
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("V", [900, 20000])
+@pytest.mark.parametrize("T", [2, 20, 50, 100, 300])
+def test_a_logit_of_plus_infinity_costs_infinitely_much(T, V, grad):
+    """nll and lse of a token with a logit of +inf beside its target's are inf; the others', for whom
+    the row's logit is -inf, are those of the other rows."""
+    d, row = 128, V // 2
+    x, w, y, g = _case(T, V, d, 7)
+    x[::2, 0] = -x[::2, 0]
+    w[row, 0] = math.inf
+    y = torch.where(y == row, row + 1, y)
+    head = eat.EatHead(w, T, grad=grad)
+    nll, lse = head.nll_grad(x, y, g)[:2] if grad else head.nll(x, y)
+    assert (nll[1::2] == math.inf).all() and (lse[1::2] == math.inf).all()
+    x64, w64 = x[::2].double(), w.double()
+    w64[row] = 0.0
+    logits = x64 @ w64.T
+    logits[:, row] = -math.inf
+    z = torch.logsumexp(logits, 1)
+    want = z - logits.gather(1, y[::2, None].long())[:, 0]
+    dl = (d / 16 + 2) * U32 * float((x64.abs() @ w64.abs().T).max()) + 64 * U32
+    assert ((lse[::2].double() - z).abs() <= 2 * dl).all()
+    assert ((nll[::2].double() - want).abs() <= 2 * dl).all()
