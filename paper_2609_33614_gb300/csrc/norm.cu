@@ -30,6 +30,13 @@ constexpr int kMaxWarps = kMaxThreads / 32;
 // reciprocal stay away from fp32's ends
 constexpr float kTiny = 1e-35f;
 
+// What the products h gamma are multiplied by for an e4m3 row, one after the other: rstd / scale and 1,
+// or, where that quotient (448 / max |h gamma|) is beyond fp32, rstd and 1 / scale.
+__device__ __forceinline__ float2 e4m3_factors(float rstd, float scale) {
+  const float k = rstd / scale;
+  return isinf(k) ? make_float2(rstd, 1.0f / scale) : make_float2(k, 1.0f);
+}
+
 template <typename T>
 struct Elem;
 template <>
@@ -209,10 +216,10 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
   }
   const float2 a = row_reduce<WARP, true>(ss, top, red, 0);
   const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
-  float k = rstd;
+  float2 k = make_float2(rstd, 1.0f);
   if (F8) {
     const float m = a.y * rstd, scale = m > kTiny ? m / 448.0f : 1.0f;
-    k = rstd / scale;
+    k = e4m3_factors(rstd, scale);
     if (lane == 0) y_scale[t] = scale;
   }
 #pragma unroll
@@ -220,7 +227,7 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
     const int c = (lane + i * ROW) * N - shift;
     if (c < d) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[i][j] *= k;
+      for (int j = 0; j < N; ++j) v[i][j] = F8 ? v[i][j] * k.x * k.y : v[i][j] * k.x;
       if (!F8) {
         store_vec<T, ALIGNED>((T*)y + at, c, d, v[i]);
       } else {
@@ -407,11 +414,11 @@ rms_norm_any_kernel(const T* x, const T* r, int d, const float* __restrict__ gam
   const float2 a = row_reduce<false, true>(ss, top, red, 0);
   const float rstd = 1.0f / sqrtf(a.x / (float)d + eps);
   const float m = a.y * rstd, scale = m > kTiny ? m / 448.0f : 1.0f;
-  const float k = F8 ? rstd / scale : rstd;
+  const float2 k = F8 ? e4m3_factors(rstd, scale) : make_float2(rstd, 1.0f);
   for (int c = threadIdx.x; c < d; c += kThreads) {
     const float v = sum(c);
     if (r) h[row + c] = Elem<T>::put(v);
-    const float o = v * gamma[c] * k;
+    const float o = v * gamma[c] * k.x * k.y;
     if (F8) ((__nv_fp8_e4m3*)y)[row + c] = __nv_fp8_e4m3(o);
     else ((T*)y)[row + c] = Elem<T>::put(o);
   }
