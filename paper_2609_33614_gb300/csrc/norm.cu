@@ -252,8 +252,14 @@ rms_norm_kernel(const T* x, const T* r, int rows, int d, const float* __restrict
 
 // Threads of the gradient's blocks at most, and blocks that are to fit an SM.
 __host__ __device__ constexpr int grad_threads(int nv) { return nv <= 2 ? kThreads : kMaxThreads; }
-// Rows of a group on their way or at work: 24 KB each of h, dy and dres at 256 threads and two vectors.
+// Rows of a group on their way or at work: 32 KB each of h, dy and dres (24 KB of it on the way) at 256
+// threads and two vectors, 96 KB a block.
 __host__ __device__ constexpr int grad_stages(int nv) { return nv <= 2 ? 4 : 2; }
+
+// Dynamic shared memory of a block at most: all stages (a warp's sums take less, kWarps rows of up to 64
+// vectors of bf16).
+constexpr int grad_smem_limit(int nv) { return grad_stages(nv) * 3 * nv * grad_threads(nv) * 16; }
+static_assert(kWarps * 64 * 8 * 4 <= grad_smem_limit(1), "the warps' sums fit the stages");
 
 // Group b of threads (a warp or the block) takes rows b, b + groups, ... (the number of groups is a
 // multiple of a vector's elements, so these rows begin alike): dx, and in registers the group's sum of
@@ -599,10 +605,12 @@ extern "C" eat_status eat_rms_norm_grad(const void* h, int32_t T, int32_t d, int
             const size_t smem = std::max(one ? stage : grad_stages(NV) * stage,
                                          WARP ? (size_t)kWarps * d * 4 : 0);
             auto* kernel = rms_norm_grad_kernel<E, WARP, NV, decltype(al)::value>;
-            // (per call: it holds for the current device and context, and takes less than a launch)
+            // (per call: it holds for the current device and context, and takes less than a launch.  The
+            // limit is the function's, not the call's: the largest that any of its calls needs, so
+            // that calls of other threads cannot lower it before the launch)
             if (smem > 47 * 1024)
               e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)smem);
+                                       grad_smem_limit(NV));
             if (e == cudaSuccess)
               e = launch_pdl(kernel, dim3(blocks), dim3(threads), smem, st, (const E*)h, T, d,
                              gamma, (float)eps, (const E*)dy, (const E*)dres, (E*)dx,
