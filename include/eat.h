@@ -389,7 +389,9 @@ typedef struct eat_head_desc {
 typedef struct eat_head eat_head;
 
 /* As eat_create / eat_destroy: validates, allocates the workspace (no call allocates afterwards),
- * synchronous; a failure leaves *out NULL.  One handle serves one stream at a time. */
+ * synchronous; a failure leaves *out NULL.  One handle serves one stream at a time.  It belongs to the
+ * device that is current at its creation: calls with another one current (destroying it apart) are
+ * refused with EAT_ERR_INVALID_ARG. */
 eat_status eat_head_create(const eat_head_desc* desc, eat_head** out);
 eat_status eat_head_destroy(eat_head* h);
 

@@ -35,9 +35,10 @@ const at::Tensor& tensor(const char* name, PyObject* o) {
   return THPVariable_Unpack(o);
 }
 
-// Fails unless t has this type and shape, contiguous on the GPU.
+// Fails unless t has this type and shape, contiguous on the GPU, and lies where `like` (the call's first
+// tensor, or null for it) does.
 const at::Tensor& check(const char* name, const at::Tensor& t, at::ScalarType type,
-                        at::IntArrayRef shape) {
+                        at::IntArrayRef shape, const at::Tensor* like) {
   if (t.scalar_type() != type || t.sizes() != shape) {
     std::ostringstream s;
     s << name << ": need " << shape << " " << type << ", got " << t.sizes() << " "
@@ -46,15 +47,20 @@ const at::Tensor& check(const char* name, const at::Tensor& t, at::ScalarType ty
   }
   if (!t.is_cuda() || !t.is_contiguous())
     value_error(std::string(name) + ": need a contiguous CUDA tensor");
+  if (like && t.device() != like->device()) {
+    std::ostringstream s;
+    s << name << ": need a tensor on " << like->device() << ", got one on " << t.device();
+    value_error(s.str());
+  }
   return t;
 }
 const at::Tensor& take(const char* name, PyObject* o, at::ScalarType type,
-                       std::initializer_list<int64_t> shape) {
-  return check(name, tensor(name, o), type, at::IntArrayRef(shape.begin(), shape.size()));
+                       std::initializer_list<int64_t> shape, const at::Tensor& like) {
+  return check(name, tensor(name, o), type, at::IntArrayRef(shape.begin(), shape.size()), &like);
 }
 const void* take_or_null(const char* name, PyObject* o, at::ScalarType type,
-                         std::initializer_list<int64_t> shape) {
-  return o == Py_None ? nullptr : take(name, o, type, shape).const_data_ptr();
+                         std::initializer_list<int64_t> shape, const at::Tensor& like) {
+  return o == Py_None ? nullptr : take(name, o, type, shape, like).const_data_ptr();
 }
 
 // fp32 or bf16 rows [T, d]
@@ -62,18 +68,19 @@ const at::Tensor& rows(const char* name, PyObject* o) {
   const at::Tensor& t = tensor(name, o);
   if (t.dim() != 2 || (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16))
     value_error(std::string(name) + ": need [T, d] fp32 or bf16 rows");
-  return check(name, t, t.scalar_type(), t.sizes());
+  return check(name, t, t.scalar_type(), t.sizes(), nullptr);
 }
-const at::Tensor& matrix(const char* name, PyObject* o, at::ScalarType type) {
+const at::Tensor& matrix(const char* name, PyObject* o, at::ScalarType type,
+                         const at::Tensor* like = nullptr) {
   const at::Tensor& t = tensor(name, o);
   if (t.dim() != 2) value_error(std::string(name) + ": need a matrix");
-  return check(name, t, type, t.sizes());
+  return check(name, t, type, t.sizes(), like);
 }
-const uint8_t* take_mask(PyObject* o, int64_t T) {
+const uint8_t* take_mask(PyObject* o, int64_t T, const at::Tensor& like) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor("mask", o);
   const at::ScalarType type = t.scalar_type() == at::kByte ? at::kByte : at::kBool;
-  return (const uint8_t*)take("mask", o, type, {T}).const_data_ptr();
+  return (const uint8_t*)take("mask", o, type, {T}, like).const_data_ptr();
 }
 
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
@@ -148,8 +155,8 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return entry("norm", n, 5, [&] {
     const at::Tensor& x = rows("x", a[0]);
     const int64_t T = x.size(0), d = x.size(1);
-    const at::Tensor& gamma = take("gamma", a[1], at::kFloat, {d});
-    const void* residual = take_or_null("residual", a[3], x.scalar_type(), {T, d});
+    const at::Tensor& gamma = take("gamma", a[1], at::kFloat, {d}, x);
+    const void* residual = take_or_null("residual", a[3], x.scalar_type(), {T, d}, x);
     const bool fp8 = a[4] == Py_True;
     const c10::cuda::CUDAGuard guard(x.device());
     at::Tensor h = residual ? empty(x.sizes(), x.scalar_type(), x) : x;
@@ -169,9 +176,9 @@ PyObject* norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return entry("norm_grad", n, 5, [&] {
     const at::Tensor& h = rows("h", a[0]);
     const int64_t T = h.size(0), d = h.size(1);
-    const at::Tensor& gamma = take("gamma", a[1], at::kFloat, {d});
-    const at::Tensor& dy = take("dy", a[3], h.scalar_type(), {T, d});
-    const void* dres = take_or_null("dres", a[4], h.scalar_type(), {T, d});
+    const at::Tensor& gamma = take("gamma", a[1], at::kFloat, {d}, h);
+    const at::Tensor& dy = take("dy", a[3], h.scalar_type(), {T, d}, h);
+    const void* dres = take_or_null("dres", a[4], h.scalar_type(), {T, d}, h);
     const c10::cuda::CUDAGuard guard(h.device());
     at::Tensor dx = empty(h.sizes(), h.scalar_type(), h), dgamma = empty({d}, at::kFloat, h);
     const int32_t T32 = to_i32("T", T), d32 = to_i32("d", d);
@@ -188,10 +195,10 @@ PyObject* norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* balance_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return entry("balance_loss", n, 3, [&] {
     const at::Tensor& logits = matrix("logits", a[0], at::kFloat);
-    const at::Tensor& idx = matrix("idx", a[1], at::kInt);
+    const at::Tensor& idx = matrix("idx", a[1], at::kInt, &logits);
     const int64_t T = logits.size(0), E = logits.size(1), K = idx.size(1);
-    check("idx", idx, at::kInt, {T, K});
-    const uint8_t* mask = take_mask(a[2], T);
+    check("idx", idx, at::kInt, {T, K}, &logits);
+    const uint8_t* mask = take_mask(a[2], T, logits);
     const c10::cuda::CUDAGuard guard(logits.device());
     at::Tensor loss = empty({1}, at::kFloat, logits), counts = empty({E}, at::kInt, logits);
     at::Tensor count = empty({1}, at::kInt, logits);
@@ -210,10 +217,10 @@ PyObject* balance_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return entry("balance_grad", n, 5, [&] {
     const at::Tensor& logits = matrix("logits", a[0], at::kFloat);
     const int64_t T = logits.size(0), E = logits.size(1);
-    const at::Tensor& counts = take("counts", a[1], at::kInt, {E});
-    const at::Tensor& count = take("n_tokens", a[2], at::kInt, {1});
-    const at::Tensor& g = take("g", a[3], at::kFloat, {1});
-    const uint8_t* mask = take_mask(a[4], T);
+    const at::Tensor& counts = take("counts", a[1], at::kInt, {E}, logits);
+    const at::Tensor& count = take("n_tokens", a[2], at::kInt, {1}, logits);
+    const at::Tensor& g = take("g", a[3], at::kFloat, {1}, logits);
+    const uint8_t* mask = take_mask(a[4], T, logits);
     const c10::cuda::CUDAGuard guard(logits.device());
     at::Tensor d = empty(logits.sizes(), at::kFloat, logits);
     ok(eat_balance_grad((const float*)logits.const_data_ptr(), to_i32("T", T), to_i32("E", E),
@@ -229,11 +236,11 @@ PyObject* head_nll(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return entry("head_nll", n, 5, [&] {
     const at::Tensor &w = tensor("w", a[1]), &target = tensor("target", a[3]);
     const int64_t T = target.numel();
-    const at::Tensor& x = take("x", a[2], w.scalar_type(), {T, w.size(1)});
-    check("target", target, at::kInt, {T});
+    const at::Tensor& x = take("x", a[2], w.scalar_type(), {T, w.size(1)}, w);
+    check("target", target, at::kInt, {T}, &w);
     const void* xs = nullptr;
     if (w.scalar_type() == at::kFloat8_e4m3fn)
-      xs = take("x_scale", a[4], at::kFloat, {T}).const_data_ptr();
+      xs = take("x_scale", a[4], at::kFloat, {T}, w).const_data_ptr();
     const c10::cuda::CUDAGuard guard(x.device());
     at::Tensor nll = empty({T}, at::kFloat, x), lse = empty({T}, at::kFloat, x);
     ok(eat_head_nll(handle(a[0]), x.const_data_ptr(), (const float*)xs, to_i32("T", T),
@@ -248,9 +255,9 @@ PyObject* head_nll_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return entry("head_nll_grad", n, 5, [&] {
     const at::Tensor &w = tensor("w", a[1]), &target = tensor("target", a[3]);
     const int64_t T = target.numel();
-    const at::Tensor& x = take("x", a[2], w.scalar_type(), {T, w.size(1)});
-    check("target", target, at::kInt, {T});
-    const at::Tensor& g = take("g", a[4], at::kFloat, {T});
+    const at::Tensor& x = take("x", a[2], w.scalar_type(), {T, w.size(1)}, w);
+    check("target", target, at::kInt, {T}, &w);
+    const at::Tensor& g = take("g", a[4], at::kFloat, {T}, w);
     const c10::cuda::CUDAGuard guard(x.device());
     at::Tensor nll = empty({T}, at::kFloat, x), lse = empty({T}, at::kFloat, x);
     at::Tensor dx = empty(x.sizes(), x.scalar_type(), x), dw = empty(w.sizes(), w.scalar_type(), x);

@@ -25,7 +25,7 @@
 struct eat_head {
   eat_head_desc desc;
   bool w8 = false;
-  int num_sms = 0, max_pairs = 1;
+  int device = 0, num_sms = 0, max_pairs = 1;
   char* mem = nullptr;
   eat::HeadStatus st{};
   unsigned int* mirror_host = nullptr;
@@ -322,6 +322,15 @@ void free_head(eat_head* h) {
 
 int up(int n, int m) { return (n + m - 1) / m * m; }
 
+// The handle's workspace and its kernels' shared-memory limits belong to the device it was created on.
+eat_status check_device(const char* fn, const eat_head* h) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev != h->device)
+    return thread_fail(EAT_ERR_INVALID_ARG, "%s: the handle is of device %d, the current one is %d",
+                       fn, h->device, dev);
+  return EAT_OK;
+}
+
 eat_status check_call(const char* fn, eat_head* h, const void* x, int32_t T,
                       const int32_t* target, const float* nll, const float* lse) {
   if (!h) return bad_arg(fn, "null handle");
@@ -330,6 +339,8 @@ eat_status check_call(const char* fn, eat_head* h, const void* x, int32_t T,
   if (misaligned(x, 16)) return bad_arg(fn, "x must be 16-byte aligned");
   if (misaligned(target, 4) || misaligned(nll, 4) || misaligned(lse, 4))
     return bad_arg(fn, "misaligned pointer");
+  const eat_status on_device = check_device(fn, h);
+  if (on_device != EAT_OK) return on_device;
   if (!h->failed && *(volatile unsigned int*)h->mirror_host) h->failed = true;
   if (h->failed)
     return thread_fail(EAT_ERR_STATE,
@@ -477,6 +488,7 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
   eat_head* h = new (std::nothrow) eat_head();
   if (!h) return thread_fail(EAT_ERR_OOM, "host allocation failed");
   h->desc = D;
+  h->device = dev;
   h->w8 = D.dtype == EAT_FP8_E4M3;
   h->num_sms = prop.multiProcessorCount;
   cudaError_t e = head_configure(h->num_sms, &h->max_pairs);
@@ -561,7 +573,11 @@ eat_status eat_head_create(const eat_head_desc* desc, eat_head** out) {
 
 eat_status eat_head_destroy(eat_head* h) {
   if (!h) return EAT_OK;
+  int dev = h->device;
+  cudaGetDevice(&dev);
+  if (dev != h->device) cudaSetDevice(h->device);
   cudaDeviceSynchronize();
+  if (dev != h->device) cudaSetDevice(dev);
   free_head(h);
   return EAT_OK;
 }
@@ -569,6 +585,8 @@ eat_status eat_head_destroy(eat_head* h) {
 eat_status eat_head_reset(eat_head* h, void* stream) {
   const char* fn = "eat_head_reset";
   if (!h) return bad_arg(fn, "null handle");
+  const eat_status on_device = check_device(fn, h);
+  if (on_device != EAT_OK) return on_device;
   cudaError_t e = cudaMemsetAsync(h->st.err, 0, 16, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
   if (e != cudaSuccess) return thread_fail(EAT_ERR_CUDA, "%s: %s", fn, cudaGetErrorString(e));
@@ -582,6 +600,8 @@ eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* st
   if (!h) return bad_arg(fn, "null handle");
   if (limit_ns < 1000 || limit_ns > 1000000000LL)
     return bad_arg(fn, "need 1 us <= limit_ns <= 1 s");
+  const eat_status on_device = check_device(fn, h);
+  if (on_device != EAT_OK) return on_device;
   return launched(fn, tc_selftest_bounded_wait((unsigned long long)limit_ns, h->st.err,
                                                (cudaStream_t)stream));
 }

@@ -327,9 +327,9 @@ def eat_head_selftest_expire_wait(h, limit_ns: int, stream=None):
 
 
 # ------------------------------------------------------------------------------------------------
-# The operators around the layer on torch tensors.  Tensors are CUDA, contiguous and of the stated
-# type (ValueError otherwise); outputs are new tensors, and calls go to the current stream of the
-# inputs' device.  A small call is bound by the host, so _eatops.so (csrc/binding.cpp) checks,
+# The operators around the layer on torch tensors.  Tensors are CUDA, contiguous, of the stated
+# type and all on one device (ValueError otherwise); outputs are new tensors, and calls go to the
+# current stream of the inputs' device.  A small call is bound by the host, so _eatops.so (csrc/binding.cpp) checks,
 # allocates and calls the library.
 # ------------------------------------------------------------------------------------------------
 _eatops = None
@@ -395,10 +395,13 @@ class EatHead:
                     w_scale.dtype is not torch.float32 or not w_scale.is_cuda
                     or not w_scale.is_contiguous()):
             raise ValueError("w_scale: need one fp32 scale per row of w, contiguous, on the GPU")
+        if fp8 and w_scale.device != w.device:
+            raise ValueError(f"w_scale: need a tensor on {w.device}, got one on {w_scale.device}")
         self.w, self.w_scale, self.dtype = w, w_scale, w.dtype
-        self.h = eat_head_create(eat_head_desc(self.d, self.V, max_tokens,
-                                               EAT_FP8_E4M3 if fp8 else EAT_BF16, int(grad),
-                                               _ptr(w), _ptr(w_scale) if fp8 else None))
+        desc = eat_head_desc(self.d, self.V, max_tokens, EAT_FP8_E4M3 if fp8 else EAT_BF16, int(grad),
+                             _ptr(w), _ptr(w_scale) if fp8 else None)
+        with torch.cuda.device(w.device):  # the handle's: its calls run there
+            self.h = eat_head_create(desc)
 
     def nll(self, x, target, x_scale=None):
         """(nll, lse) [T] fp32 of hidden states x [T, d] and targets [T] int32 (negative: ignored);
