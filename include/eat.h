@@ -412,7 +412,8 @@ eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_
  * P enters the products as bf16.  Ignored tokens, and tokens whose target is >= vocab, give a zero
  * row of dx and add nothing to dw, whatever their x holds (NaN among it).  A vocabulary row of logit
  * -inf has P = 0 and adds nothing to dw; in dx, P w is NaN where w itself is infinite.  A counted
- * token with a logit of +inf makes its row of dx, and dw, NaN.  dx must not alias x.
+ * token with a logit of +inf makes its row of dx, and dw, NaN.  dx and dw overlap
+ * neither x nor w nor each other (EAT_ERR_INVALID_ARG).
  * dx and dw 16-byte aligned.  Needs a handle created with with_grad. */
 eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_t* target,
                              const float* g, float* nll, float* lse, void* dx, void* dw,

@@ -628,7 +628,13 @@ eat_status eat_head_nll_grad(eat_head* h, const void* x, int32_t T, const int32_
   if (!g || !dx || !dw) return bad_arg(fn, "g, dx and dw must be non-NULL");
   if (misaligned(dx, 16) || misaligned(dw, 16) || misaligned(g, 4))
     return bad_arg(fn, "dx and dw must be 16-byte aligned");
-  if (dx == x) return bad_arg(fn, "dx must not alias x");
+  // (x and w are read while dx and dw are written)
+  const size_t row = 2 * (size_t)h->desc.d_model, tokens = T * row, vocab = h->desc.vocab * row;
+  if (overlap(dx, tokens, x, tokens) || overlap(dx, tokens, h->desc.w, vocab))
+    return bad_arg(fn, "dx must not overlap x or w");
+  if (overlap(dw, vocab, x, tokens) || overlap(dw, vocab, h->desc.w, vocab) ||
+      overlap(dw, vocab, dx, tokens))
+    return bad_arg(fn, "dw must not overlap x, w or dx");
   return launched(fn, run_grad(h, x, T, target, g, nll, lse, dx, dw, (cudaStream_t)stream));
 }
 
