@@ -52,6 +52,7 @@ class Model:
         self.layers = []
         self.make_layers()
         self.head = eat.EatHead(self.head_w, BATCH, grad=True)  # w may change in place
+        self.head8, self.trained = None, False
 
     def make_layers(self):
         """Layer handles for the present routers (a handle's weights do not change while it lives);
@@ -81,17 +82,23 @@ class Model:
 
     def score(self, tokens, targets):
         """Token NLLs through the e4m3 head, and the perplexity signal of this window."""
-        if not hasattr(self, "head8"):
-            self.head8 = eat.EatHead(*self._e4m3())
+        self.update_head8()
         x, h, _ = self.body(tokens)
         q, scale, _ = eat.rms_norm_fp8(x, self.gamma_out, EPS, residual=h)
         nll, _ = self.head8.nll(q, targets, x_scale=scale)
         eat.eat_ppl_update(nll, nll.numel(), self.ppl, self.sign)
         return nll
 
-    def _e4m3(self):
-        q, scale = e4m3_rows(self.head_w)
-        return q, BATCH, scale
+    def update_head8(self):
+        """The e4m3 head of the present vocabulary matrix; after a training step its rows are written
+        in place (a handle's w may change between calls)."""
+        if self.head8 is None:
+            self.w8, self.w8_scale = e4m3_rows(self.head_w)
+            self.head8 = eat.EatHead(self.w8, BATCH, w_scale=self.w8_scale)
+        elif self.trained:
+            for mine, now in zip((self.w8, self.w8_scale), e4m3_rows(self.head_w)):
+                mine.copy_(now)
+        self.trained = False
 
     def train_step(self, tokens, targets, mask, lr=0.5, balance=0.05):
         """One step on the tokens that count; (mean NLL, balance losses, expert counts)."""
@@ -113,6 +120,7 @@ class Model:
             all_counts.append(counts)
         self.gamma_out -= lr * dgamma
         self.head_w -= lr * dw
+        self.trained = True
         self.make_layers()
         return (nll * g).sum(), losses, all_counts
 
@@ -120,7 +128,7 @@ class Model:
         for layer in self.layers:
             layer.close()
         self.head.close()
-        if hasattr(self, "head8"):
+        if self.head8 is not None:
             self.head8.close()
 
 
