@@ -11,8 +11,6 @@ from __future__ import annotations
 import ctypes
 import os
 
-import torch
-
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libeat.so")
 
@@ -132,16 +130,27 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_stream = None  # torch's current stream of the current device, once asked for
+
+
+def _torch_stream():
+    """How to ask torch for its current stream's handle.  The raw query saves most of what building a
+    Stream object costs the host on each call (a small call is bound by the host)."""
+    global _current_stream
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        _current_stream = lambda: torch.cuda.current_stream().cuda_stream
+    else:
+        device = torch.cuda.current_device
+        _current_stream = lambda: raw(device())
+    return _current_stream
 
 
 def _stream(stream):
-    """The stream's handle; None: torch's current stream.  The raw query saves most of what building
-    a Stream object costs the host on each call (a small call is bound by the host)."""
+    """The stream's handle; None: torch's current stream (torch is imported by the first such call)."""
     if stream is None:
-        if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream
+        return (_current_stream or _torch_stream())()
     return stream
 
 
@@ -386,6 +395,7 @@ class EatHead:
     w_scale [vocab] fp32), kept referenced; grad=True (bf16) for nll_grad."""
 
     def __init__(self, w, max_tokens, w_scale=None, grad=False):
+        import torch
         fp8 = w.dtype is torch.float8_e4m3fn
         if w.dim() != 2 or not (fp8 or w.dtype is torch.bfloat16) or not w.is_cuda \
                 or not w.is_contiguous():
@@ -435,6 +445,7 @@ class EatLayer:
         """Expert weights fp32, bf16, or torch.float8_e4m3fn with ``scales`` = dict of the fp32
         per-row scale tensors (w_gate_scale, w_up_scale, w_down_scale and, with shared experts,
         ws_gate_scale, ws_up_scale, ws_down_scale)."""
+        import torch
         scales = scales or {}
         self._keep = [w_router, b_router, w_gate, w_up, w_down, ws_gate, ws_up, ws_down,
                       opd_scale] + list(scales.values())
@@ -480,6 +491,7 @@ class EatLayer:
             pass
 
     def forward(self, x, ppl_sign=0, with_routing=False):
+        import torch
         T = x.shape[0]
         y = torch.empty_like(x)
         if with_routing:
@@ -492,6 +504,7 @@ class EatLayer:
         return y
 
     def route(self, x, ppl_sign=0):
+        import torch
         T = x.shape[0]
         idx = torch.empty(T, self.K, dtype=torch.int32, device=x.device)
         w = torch.empty(T, self.K, dtype=torch.float32, device=x.device)
@@ -500,6 +513,7 @@ class EatLayer:
         return idx, w, k
 
     def accounts(self):
+        import torch
         N = torch.empty(self.E, dtype=torch.int64, device="cuda")
         P = torch.empty(self.E, dtype=torch.float64, device="cuda")
         C = torch.empty(self.E, dtype=torch.float64, device="cuda")
@@ -510,6 +524,7 @@ class EatLayer:
         eat_set_accounts(self.h, N.contiguous(), P.contiguous(), C.contiguous())
 
     def call_stats(self):
+        import torch
         n = torch.empty(self.E, dtype=torch.int32, device="cuda")
         sp = torch.empty(self.E, dtype=torch.float64, device="cuda")
         sn = torch.empty(self.E, dtype=torch.float64, device="cuda")
