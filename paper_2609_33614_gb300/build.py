@@ -10,6 +10,7 @@ import os
 import shutil
 import subprocess
 import sysconfig
+import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -88,15 +89,34 @@ def ffn_source_hash() -> str:
     return h.hexdigest()
 
 
-def _build_binding(force: bool = False) -> str:
-    """Compile and link _eatops.so against the installed torch and libeat.so (found beside it)."""
-    import torch
-    src = os.path.join(CSRC, "binding.cpp")
+def _binding_needs():
+    """(include directories, library directory, compiler) of the binding; RuntimeError with what is
+    missing.  libeat.so needs none of it."""
+    try:
+        import torch
+    except ImportError as e:
+        raise RuntimeError(f"torch cannot be imported ({e})") from None
     root = os.path.dirname(torch.__file__)
+    python = sysconfig.get_paths()["include"]
     inc = [os.path.join(ROOT, "include"), os.path.join(root, "include"),
            os.path.join(root, "include", "torch", "csrc", "api", "include"),
            os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))), "include"),
-           sysconfig.get_paths()["include"]]
+           python]
+    for f in (os.path.join(root, "include", "ATen", "core", "Tensor.h"),
+              os.path.join(python, "Python.h")):
+        if not os.path.exists(f):
+            raise RuntimeError(f"{f} is missing")
+    cxx = os.environ.get("CXX", "g++")
+    if not shutil.which(cxx.split()[0]):
+        raise RuntimeError(f"no C++ compiler ({cxx})")
+    return inc, os.path.join(root, "lib"), cxx.split()
+
+
+def _build_binding(force: bool = False) -> str:
+    """Compile and link _eatops.so against the installed torch and libeat.so (found beside it)."""
+    inc, lib, cxx = _binding_needs()
+    import torch
+    src = os.path.join(CSRC, "binding.cpp")
     flags = ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
     h = hashlib.sha256(" ".join(flags + inc + [torch.__version__]).encode())
@@ -110,12 +130,11 @@ def _build_binding(force: bool = False) -> str:
                 return BINDING
     obj = os.path.join(BUILD, "binding.o")
     tmp = BINDING + ".tmp"
-    cxx = os.environ.get("CXX", "g++")
     # (torch's libraries are loaded before it; libeat.so is found in its own directory)
-    libs = ["-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+    libs = ["-L" + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
             "-L" + PKG, "-l:libeat.so", "-Wl,-rpath,$ORIGIN"]
-    for cmd in ([cxx] + flags + ["-I" + i for i in inc] + ["-c", src, "-o", obj],
-                [cxx, "-shared", "-o", tmp, obj] + libs):
+    for cmd in (cxx + flags + ["-I" + i for i in inc] + ["-c", src, "-o", obj],
+                cxx + ["-shared", "-o", tmp, obj] + libs):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"{' '.join(cmd[:2])} failed on {src}:\n{r.stdout}\n{r.stderr}")
@@ -126,8 +145,17 @@ def _build_binding(force: bool = False) -> str:
 
 
 def build(verbose: bool = False, force: bool = False) -> str:
-    """Compile and link libeat.so and its Python binding; returns the library's path."""
+    """Compile and link libeat.so and its Python binding; returns the library's path.  Where torch, its
+    headers, Python's or a C++ compiler are missing, the library is built alone, with a warning: the
+    C ABI and the ctypes functions work, and the functions of torch tensors say what they lack."""
     path = _build_library(verbose, force)
+    try:
+        _binding_needs()
+    except RuntimeError as e:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)  # of another library, as a rule
+        warnings.warn(f"_eatops.so is not built: {e}")
+        return path
     _build_binding(force)
     return path
 
