@@ -409,7 +409,9 @@ eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_
 /* The loss as eat_head_nll and, in the same call, the gradients of sum_t g[t] nll[t] (g [T] fp32,
  * e.g. 1 / number of tokens): with P_tv = g[t] (exp(l_tv - lse[t]) - [v = target[t]]),
  *   dx [T, d_model] = P w,  dw [vocab, d_model] = P^T x, both bf16, rounded from fp32 sums.
- * P enters the products as bf16.  Ignored tokens, and tokens whose target is >= vocab, give a zero
+ * P enters the products as bf16: exp(l_tv - l_t,target) is rounded once, beside it a row factor g[t] /
+ * sum, in fp32 for dx; for dw, the factor times x is rounded once more with over 128 counted tokens
+ * (with fewer it has two bf16 parts).  Ignored tokens, and tokens whose target is >= vocab, give a zero
  * row of dx and add nothing to dw, whatever their x holds (NaN among it).  A vocabulary row of logit
  * -inf has P = 0 and adds nothing to dw; in dx, P w is NaN where w itself is infinite.  A counted
  * token with a logit of +inf makes its row of dx, and dw, NaN.  dx and dw overlap

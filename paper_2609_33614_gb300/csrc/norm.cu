@@ -399,7 +399,10 @@ rms_norm_grad_kernel(const T* __restrict__ h, int rows, int d, const float* __re
   }
 }
 
-// Rows that no vector kernel takes: a block per row, element by element, reading the row twice.
+// Rows that no vector kernel takes (longer than 16384 bf16 or 8192 fp32, or in memory that is not aligned
+// to vectors, such as a view one element in): a block per row, element by element, reading the row twice.
+// With a residual, bf16: 4096 x 20000 261 us, 2.5 TB/s; 4096 x 4096 one element in 36 us, where aligned
+// rows take 21.
 template <typename T, bool F8>
 __global__ void __launch_bounds__(kThreads)
 rms_norm_any_kernel(const T* x, const T* r, int d, const float* __restrict__ gamma, float eps, T* h,
@@ -430,7 +433,9 @@ rms_norm_any_kernel(const T* x, const T* r, int d, const float* __restrict__ gam
   }
   if (F8 && threadIdx.x == 0) y_scale[blockIdx.x] = scale;
 }
-// Block b takes rows b, b + gridDim.x, ...; every column of part[b] belongs to one thread.
+// Block b takes rows b, b + gridDim.x, ...; every column of part[b] belongs to one thread, which adds each
+// row's term to it in memory.  Bound by that: 4096 x 20000 1215 us, 0.5 TB/s; 4096 x 4096 one element in
+// 219 us, where aligned rows take 28.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 rms_norm_grad_any_kernel(const T* __restrict__ h, int rows, int d, const float* __restrict__ gamma,
