@@ -354,14 +354,12 @@ def _own_mm(st):
 def _own_linear(st):
     from paper_2609_33614_gb300 import eat
     offsets = st.offsets if st.case["experts"] else None
-    wq, ws, wtq, wts = eat.quant_tiles(st.w, transposed=True)
-    xq, xs = eat.quant_rows(st.x)
+    wq, ws = eat.quant_tiles(st.w)
+    xq, xs, xcq, xcs = eat.quant_rows_columns(st.x, offsets=offsets)
     y = eat.block_mm(xq, xs, wq, ws, offsets=offsets)
-    gq, gs = eat.quant_rows(st.dy)
-    dx = eat.block_mm(gq, gs, wtq, wts, offsets=offsets)
-    gtq, gts = eat.quant_columns(st.dy, offsets=offsets)
-    xtq, xts = eat.quant_columns(st.x, offsets=offsets)
-    dw = eat.block_mm_grad(gtq, gts, xtq, xts, offsets=offsets)
+    gq, gs, gcq, gcs = eat.quant_rows_columns(st.dy, offsets=offsets)
+    dx = eat.block_mm(gq, gs, wq, ws, offsets=offsets, transposed=True)
+    dw = eat.block_mm_grad(gcq, gcs, xcq, xcs, offsets=offsets)
     return {"y": y, "dx": dx, "dw": dw}
 
 
