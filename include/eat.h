@@ -430,6 +430,99 @@ eat_status eat_head_reset(eat_head* h, void* stream);
  * nothing arrives on gives up after limit_ns (1 us .. 1 s) and sets the head's device status word. */
 eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* stream);
 
+/* ---- Experts of a router's choice: tokens sorted by expert and back, products in e4m3 -----------
+ * What serving and training experts outside a layer handle takes, on the idx and w that eat_route
+ * writes.  No handle; errors through eat_last_error(NULL).  Every output is a function of the inputs
+ * alone: the same inputs give the same bits.  1 <= K <= 16, 1 <= E <= 256, T K <= 2^30, 1 <= d <= 65536. */
+
+/* Sorts the selections of idx [T, K] by expert.  Entries outside [0, E), and those of tokens whose mask
+ * byte is 0 (mask [T] or NULL), select nothing.  offsets [E + 1]: offsets[e] is the number of
+ * selections of experts below e; slot [T, K]: the row of selection (t, k) among the sorted ones (those
+ * of an expert in the order of t, then k), or -1.  A token may select an expert more than once.
+ * work: eat_expert_sort_workspace(T, K, E) bytes of device memory, 16-byte aligned, whose contents do
+ * not matter; the call may use it until it has finished on `stream`. */
+eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, int32_t E, const uint8_t* mask,
+                           int32_t* offsets, int32_t* slot, void* work, void* stream);
+int64_t eat_expert_sort_workspace(int32_t T, int32_t K, int32_t E);
+
+/* rows[slot[t][k]] = x[t], and zeros behind row offsets[E].  x [T, d] fp32 or bf16 (dtype); rows
+ * [T K, d] in dtype, or e4m3 (EAT_FP8_E4M3) with scale [ceil(d / 128)][T K] fp32: see eat_quant_rows
+ * (rows of zeros have the scale 1). */
+eat_status eat_expert_gather(const void* x, int32_t T, int32_t K, int32_t E, int32_t d, int32_t dtype,
+                             const int32_t* slot, const int32_t* offsets, void* rows,
+                             int32_t rows_dtype, float* scale, void* stream);
+
+/* y[t] = sum_k w[t][k] rows[slot[t][k]], over the selections that have a row (0 where none has,
+ * whatever the other rows and weights hold).  rows [T K, d], y [T, d] fp32 or bf16 (dtype); w [T, K]
+ * fp32, or NULL for ones: then y is the gradient of x in eat_expert_gather. */
+eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K, int32_t d, int32_t dtype,
+                              const int32_t* slot, const float* w, void* y, void* stream);
+
+/* Gradients of eat_expert_combine: drows[slot[t][k]] = w[t][k] dy[t], and zeros behind row offsets[E];
+ * dw[t][k] = <dy[t], rows[slot[t][k]]>, 0 where there is no row.  drows overlaps neither rows nor dy. */
+eat_status eat_expert_combine_grad(const void* dy, const void* rows, int32_t T, int32_t K, int32_t E,
+                                   int32_t d, int32_t dtype, const int32_t* slot,
+                                   const int32_t* offsets, const float* w, void* drows, float* dw,
+                                   void* stream);
+
+/* e4m3 with a scale for each 128 elements of a row.  x [M, K] fp32 or bf16 (dtype); q [M, K] bytes;
+ * scale [ceil(K / 128)][M] fp32: element k of row r is scale[k / 128][r] * (its byte), and the scale is
+ * the largest magnitude / 448 (1, and bytes 0, where that is not above 1e-35).  A block that holds an
+ * infinity reads as NaN; a NaN leaves the others of its block as they are.
+ * 1 <= M <= 2^30, 1 <= K <= 65536. */
+eat_status eat_quant_rows(const void* x, int32_t M, int32_t K, int32_t dtype, void* q, float* scale,
+                          void* stream);
+
+/* e4m3 with a scale for each 128 rows of a column, for sums over an expert's rows (eat_block_mm_grad).
+ * x [M, K]; offsets [E + 1] of rows sorted by expert, or NULL with E = 1: one expert with all rows.
+ * cq [eat_quant_columns_rows(M, E), K] bytes: expert e's rows begin where those of the experts below it
+ * end, each with its count rounded up to a multiple of 32 (zeros behind its last).
+ * cscale [eat_quant_columns_blocks(M, E)][K] fp32: expert e's blocks of 128 rows begin behind those of
+ * the experts below it; element k of an expert's row i is cscale[its block i / 128][k] * (its byte).
+ * What lies behind the last expert's rows and blocks is not written.
+ * q and scale, both or neither (NULL): eat_quant_rows of the same x beside it, for one read of x; rows
+ * from offsets[E] on are then zeros with the scale 1, whatever x holds there. */
+eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int32_t dtype,
+                             const int32_t* offsets, int32_t E, void* q, float* scale, void* cq,
+                             float* cscale, void* stream);
+int64_t eat_quant_columns_rows(int32_t M, int32_t E);
+int64_t eat_quant_columns_blocks(int32_t M, int32_t E);
+
+/* e4m3 with a scale for each 128 x 128 tile: w [E, N, K] fp32 or bf16 (dtype), q [E, N, K] bytes, scale
+ * [E][ceil(N / 128)][ceil(K / 128)] fp32. */
+eat_status eat_quant_tiles(const void* w, int32_t E, int32_t N, int32_t K, int32_t dtype, void* q,
+                           float* scale, void* stream);
+
+/* y = x w^T (or, transposed != 0, x w) of operands as eat_quant_rows and eat_quant_tiles make them, w
+ * [E, N, K]: rows offsets[e] .. offsets[e + 1] - 1 of x by matrix e, zeros in the rows from offsets[E]
+ * on; offsets NULL with E = 1: one matrix for all rows.
+ *   x [M, K], xs [ceil(K / 128)][M], y [M, N]; transposed: x [M, N], xs [ceil(N / 128)][M], y [M, K].
+ * y in ydtype, EAT_BF16 or EAT_F32.  Sums are fp32: those of a block of 128 on the tensor cores, scaled
+ * and added to each other in order.  Rows of x behind an expert's own never reach its outputs.
+ * K, and with transposed N, are multiples of 16 (EAT_ERR_UNSUPPORTED otherwise); N, K <= 65536; xq and
+ * wq 16-byte aligned.  y overlaps no input. */
+eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const float* ws,
+                        const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
+                        int32_t transposed, void* y, int32_t ydtype, void* stream);
+
+/* dw [E, N, K] (dtype: EAT_BF16 or EAT_F32) = for each expert the sum over its rows of g^T x, of
+ * operands as eat_quant_columns makes them with the same offsets: gq [rows, N], gs [blocks][N], xq
+ * [rows, K], xs [blocks][K], rows and blocks being eat_quant_columns_rows and _blocks.  Zeros for an
+ * expert without rows.  offsets NULL with E = 1: one expert with `rows` rows (those that pad add
+ * nothing).  N and K are multiples of 16; gq and xq 16-byte aligned. */
+eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq, const float* xs,
+                             const int32_t* offsets, int32_t E, int32_t rows, int32_t blocks,
+                             int32_t N, int32_t K, void* dw, int32_t dtype, void* stream);
+
+/* The gated activation between an expert's two products: rows gu [R, 2 F] = [gate | up], fp32 or bf16
+ * (dtype): h = gate / (1 + exp(-gate)) * up, in dtype, or (h_dtype EAT_FP8_E4M3) e4m3 with scale
+ * [ceil(F / 128)][R] as eat_quant_rows makes it of the unrounded h.  1 <= R <= 2^30, 1 <= F <= 65536. */
+eat_status eat_swiglu(const void* gu, int32_t R, int32_t F, int32_t dtype, void* h, int32_t h_dtype,
+                      float* scale, void* stream);
+/* Its gradient: dgu [R, 2 F] of dh [R, F], all in dtype.  dgu may be gu. */
+eat_status eat_swiglu_grad(const void* gu, const void* dh, int32_t R, int32_t F, int32_t dtype,
+                           void* dgu, void* stream);
+
 /* Last error on the handle (never NULL), or a generic text for a NULL handle. */
 const char* eat_last_error(const eat_handle* h);
 const char* eat_status_string(eat_status s);

@@ -10,9 +10,8 @@
 // element: their vectors are the aligned ones of memory, and the first and the last of a row are
 // shared with its neighbours (read whole, masked, and stored element by element).  All sums are
 // fp32; a value is rounded once, when it is stored.
+#include "elem.cuh"
 #include "op_checks.cuh"
-
-#include <cuda_fp8.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -26,9 +25,6 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kMaxRows = 1 << 30;  // row numbers and their strides ahead stay within an int
 constexpr int kMaxThreads = 512;  // of a block that takes a row
 constexpr int kMaxWarps = kMaxThreads / 32;
-// e4m3 rows whose largest value is not above this get the scale 1 (and bytes 0): max / 448 and its
-// reciprocal stay away from fp32's ends
-constexpr float kTiny = 1e-35f;
 
 // What the products h gamma are multiplied by for an e4m3 row, one after the other: rstd / scale and 1,
 // or, where that quotient (448 / max |h gamma|) is beyond fp32, rstd and 1 / scale.
@@ -36,48 +32,6 @@ __device__ __forceinline__ float2 e4m3_factors(float rstd, float scale) {
   const float k = rstd / scale;
   return isinf(k) ? make_float2(rstd, 1.0f / scale) : make_float2(k, 1.0f);
 }
-
-template <typename T>
-struct Elem;
-template <>
-struct Elem<float> {
-  static constexpr int kN = 4;  // elements of 16 bytes
-  static __device__ __forceinline__ float get(float v) { return v; }
-  static __device__ __forceinline__ float put(float v) { return v; }
-  static __device__ __forceinline__ void unpack(uint4 u, float* v) {
-    v[0] = __uint_as_float(u.x);
-    v[1] = __uint_as_float(u.y);
-    v[2] = __uint_as_float(u.z);
-    v[3] = __uint_as_float(u.w);
-  }
-  static __device__ __forceinline__ uint4 pack(const float* v) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-                      __float_as_uint(v[3]));
-  }
-};
-template <>
-struct Elem<__nv_bfloat16> {
-  static constexpr int kN = 8;
-  static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
-  static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
-  static __device__ __forceinline__ void unpack(uint4 u, float* v) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ uint4 pack(const float* v) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = *(const uint32_t*)&b;
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
-};
 
 // Elements [c, c + kN) of a row as they lie in memory.  With ALIGNED the row begins at a vector and c
 // never leaves it; else the vector may begin in the row before and end in the one behind (their

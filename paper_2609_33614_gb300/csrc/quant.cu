@@ -1,0 +1,432 @@
+// e4m3 operands with a scale for each block of 128 (block_mm.cu multiplies them), and the gated
+// activation between two such products.
+//   rows:    a scale for each 128 elements of a row, [ceil(K / 128)][M]
+//   columns: a scale for each 128 rows of a column, [blocks][K]: what the weights' gradient, a sum over
+//            an expert's rows, reads.  Each expert's rows begin at a multiple of 32 (what one MMA
+//            sums), zeros behind its last.
+//   tiles:   weights, a scale for each 128 x 128 tile, so one copy serves both directions
+//   swiglu:  h = gate up / (1 + exp(-gate)) of rows [gate | up]; its gradient:
+//            s = 1 / (1 + exp(-gate)):  dgate = dh up s (1 + gate (1 - s)),  dup = dh gate s
+// Bound: HBM; each input is read once and kept in registers between a block's maximum and its bytes.
+// swiglu's e4m3 form takes the maximum of the unrounded fp32 values.
+#include "elem.cuh"
+#include "op_checks.cuh"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace eat {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+// 1 / (1 + exp(-g)): within 3 2^-23 + |g| 2^-24 of itself, far below what bf16 or e4m3 keep of it.
+__device__ __forceinline__ float sigmoid(float g) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-g)));
+  return r;
+}
+
+// ------------------------------------------------------------------------------------- rows
+constexpr int kRows = 8;  // rows of a unit: their scales fill a sector of [blocks][M]
+
+// A unit is kRows rows of one block of 128 columns, taken by as many lanes as the block has 16-byte
+// vectors.  GLU: the values are swiglu of rows of twice the length.
+template <typename T, bool VEC, bool GLU>
+__global__ void __launch_bounds__(kThreads)
+quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __restrict__ q,
+                  float* __restrict__ scale) {
+  constexpr int N = Elem<T>::kN, G = kBlock / N, U = GLU ? 4 : kRows;
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) / G;
+  const int kb = (int)(unit % blocks), l = threadIdx.x % G;
+  const long long r0 = unit / blocks * kRows;
+  const int c = kb * kBlock + l * N, left = K - c;
+  const size_t pitch = GLU ? 2 * (size_t)K : (size_t)K;
+  float s = 1.0f;  // lane l: of the l-th row
+#pragma unroll
+  for (int i0 = 0; i0 < kRows; i0 += U) {
+    float v[U][N], u[GLU ? U : 1][N];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const long long r = r0 + i0 + i;
+      if (r < M && left > 0) {
+        load_elems<T, N, VEC>(x + r * pitch + c, left, v[i]);
+        if (GLU) load_elems<T, N, VEC>(x + r * pitch + K + c, left, u[GLU ? i : 0]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const long long r = r0 + i0 + i;
+      float top = 0.f;
+      if (r < M && left > 0) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          if (GLU) v[i][j] = v[i][j] * sigmoid(v[i][j]) * u[GLU ? i : 0][j];
+          if (VEC || j < left) top = fmaxf(top, fabsf(v[i][j]));
+        }
+      }
+      top = group_max<G>(top);
+      if (r < M && left > 0)
+        store_e4m3<N, VEC>(q + (size_t)r * K + c, left, v[i], block_factor(top));
+      if (l == i0 + i) s = block_scale(top);
+    }
+  }
+  if (l < kRows && r0 + l < M) scale[(size_t)kb * M + r0 + l] = s;
+}
+
+// ---------------------------------------------------------------------------------- columns
+// Block b of the experts' blocks of 128 rows: its rows in x, and where they go in the padded order.
+struct RowBlock {
+  int row, n, padded;  // first row, number (0: none), first padded row
+};
+// By a full warp; the same in all lanes.  Offsets are held to [0, M].  Blocks past the experts' last
+// take the rows behind it: n is 0, and row the first of their 128 (M where there is none).
+__device__ RowBlock find_block(const int32_t* offsets, int E, int M, int b) {
+  const int lane = threadIdx.x & 31;
+  int blocks = 0, padded = 0, end = 0;  // of the experts so far
+  for (int e0 = 0; e0 < E; e0 += 32) {
+    const int e = e0 + lane;
+    const int lo = e < E ? max(0, min(offsets ? offsets[e] : 0, M)) : 0;
+    const int hi = e < E ? max(lo, min(offsets ? offsets[e + 1] : M, M)) : 0;
+    const int c = (hi - lo + kBlock - 1) / kBlock, p = (hi - lo + 31) & ~31;
+    int vc = c, vp = p;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int uc = __shfl_up_sync(0xffffffffu, vc, o), up = __shfl_up_sync(0xffffffffu, vp, o);
+      if (lane >= o) {
+        vc += uc;
+        vp += up;
+      }
+    }
+    const int at = b - (blocks + vc - c);
+    const unsigned who = __ballot_sync(0xffffffffu, at >= 0 && at < c);
+    if (who) {
+      const int src = __ffs(who) - 1;
+      const RowBlock r{lo + at * kBlock, min(kBlock, hi - lo - at * kBlock),
+                       padded + vp - p + at * kBlock};
+      return RowBlock{__shfl_sync(0xffffffffu, r.row, src), __shfl_sync(0xffffffffu, r.n, src),
+                      __shfl_sync(0xffffffffu, r.padded, src)};
+    }
+    blocks += __shfl_sync(0xffffffffu, vc, 31);
+    padded += __shfl_sync(0xffffffffu, vp, 31);
+    end = max(end, (int)__reduce_max_sync(0xffffffffu, (unsigned)hi));
+  }
+  return RowBlock{(int)min((long long)M, end + (long long)(b - blocks) * kBlock), 0, 0};
+}
+
+// A tile of 128 rows and 128 columns at a time: thread (l, r) holds a vector of kSpan consecutive rows.
+// ROWS: the rows' own blocks as well (q, scale), which the same tile holds whole.
+template <typename T, bool VEC, bool ROWS>
+__global__ void __launch_bounds__(kThreads)
+quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __restrict__ offsets,
+                     int E, int padded_rows, int blocks, int tiles, uint8_t* __restrict__ q,
+                     float* __restrict__ scale, uint8_t* __restrict__ cq,
+                     float* __restrict__ cscale) {
+  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kThreads;
+  __shared__ float s_top[kWarps][kBlock];
+  __shared__ float s_factor[kBlock];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int b = blockIdx.x;
+  const RowBlock rb = find_block(offsets, E, M, b);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int l = threadIdx.x % L, r = threadIdx.x / L * R;
+  const int out_rows = (rb.n + 31) & ~31;
+  if (rb.n > 0 && (b >= blocks || rb.padded + out_rows > padded_rows)) return;  // no such offsets
+  if (rb.n == 0) {  // rows behind the last expert's
+    if (ROWS)
+      for (int i = blockIdx.y; i < tiles; i += gridDim.y) {
+        const int c = i * kBlock + l * N, left = K - c;
+        const float zero[N] = {};
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          const int row = rb.row + r + k;
+          if (row >= M) break;
+          if (left > 0) store_e4m3<N, VEC>(q + (size_t)row * K + c, left, zero, 0.f);
+          if (l == 0) scale[(size_t)i * M + row] = 1.0f;
+        }
+      }
+    return;
+  }
+  for (int i = blockIdx.y; i < tiles; i += gridDim.y) {
+    const int c = i * kBlock + l * N, left = K - c;
+    float v[R][N], top[N] = {};
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (r + k < rb.n && left > 0) {
+        load_elems<T, N, VEC>(x + (size_t)(rb.row + r + k) * K + c, left, v[k]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[k][j] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) top[j] = fmaxf(top[j], fabsf(v[k][j]));
+#pragma unroll
+      for (int o = 16; o >= L; o >>= 1)
+        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
+      if (lane < L) s_top[warp][lane * N + j] = top[j];
+    }
+    if (ROWS) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        float t = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) t = fmaxf(t, fabsf(v[k][j]));
+        t = group_max<L>(t);
+        if (r + k >= rb.n) continue;
+        const size_t row = rb.row + r + k;
+        if (left > 0) store_e4m3<N, VEC>(q + row * K + c, left, v[k], block_factor(t));
+        if (l == 0) scale[(size_t)i * M + row] = block_scale(t);
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x < kBlock) {
+      float t = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) t = fmaxf(t, s_top[k][threadIdx.x]);
+      s_factor[threadIdx.x] = block_factor(t);
+      const int col = i * kBlock + threadIdx.x;
+      if (col < K) cscale[(size_t)b * K + col] = block_scale(t);
+    }
+    __syncthreads();
+    float f[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = s_factor[l * N + j];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (r + k >= out_rows || left <= 0) continue;
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[k][j] *= f[j];
+      store_e4m3<N, VEC>(cq + (size_t)(rb.padded + r + k) * K + c, left, v[k], 1.0f);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------ tiles
+// A block takes a tile; thread: N columns of R consecutive rows.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads)
+quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restrict__ q,
+                   float* __restrict__ scale) {
+  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kThreads;
+  __shared__ float s_top[kWarps];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int kb = blockIdx.x, blocks = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n_blocks = (n_rows + kBlock - 1) / kBlock, nb = blockIdx.y;
+  const size_t e = blockIdx.z, at = e * n_rows * K;
+  const int l = threadIdx.x % L, r = threadIdx.x / L * R;
+  const int c = kb * kBlock + l * N, left = K - c, row0 = nb * kBlock + r;
+  float v[R][N], top = 0.f;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (row0 + k < n_rows && left > 0) {
+      load_elems<T, N, VEC>(w + at + (size_t)(row0 + k) * K + c, left, v[k]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[k][j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[k][j]));
+  top = group_max<32>(top);
+  if (lane == 0) s_top[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kWarps; ++k) top = fmaxf(top, s_top[k]);
+  if (threadIdx.x == 0) scale[(e * n_blocks + nb) * blocks + kb] = block_scale(top);
+  const float f = block_factor(top);
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+    if (row0 + k < n_rows && left > 0)
+      store_e4m3<N, VEC>(q + at + (size_t)(row0 + k) * K + c, left, v[k], f);
+}
+
+// ----------------------------------------------------------------------------------- swiglu
+// N elements a thread (a 16-byte vector, or one).
+template <typename T, int N, bool GRAD>
+__global__ void __launch_bounds__(kThreads)
+swiglu_kernel(const T* __restrict__ gu, const T* __restrict__ dh, long long n, int F,
+              T* __restrict__ out) {
+  constexpr bool VEC = N > 1;
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long at = ((long long)blockIdx.x * kThreads + threadIdx.x) * N;
+  if (at >= n) return;
+  const long long r = at / F;
+  const int c = (int)(at - r * F);
+  const size_t g0 = (size_t)r * 2 * F + c;
+  float g[N], u[N], o[N];
+  load_elems<T, N, VEC>(gu + g0, N, g);
+  load_elems<T, N, VEC>(gu + g0 + F, N, u);
+  if (!GRAD) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = g[j] * sigmoid(g[j]) * u[j];
+    store_elems<T, N, VEC>(out + at, N, o);
+    return;
+  }
+  float d[N], du[N];
+  load_elems<T, N, VEC>(dh + at, N, d);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float s = sigmoid(g[j]);
+    o[j] = d[j] * u[j] * s * fmaf(g[j], 1.0f - s, 1.0f);
+    du[j] = d[j] * g[j] * s;
+  }
+  store_elems<T, N, VEC>(out + g0, N, o);
+  store_elems<T, N, VEC>(out + g0 + F, N, du);
+}
+
+const char* bad_matrix(int32_t M, int32_t K, int32_t dtype) {
+  if (M < 1 || M > 1 << 30) return "need between 1 and 2^30 rows";
+  if (K < 1 || K > 65536) return "need between 1 and 65536 columns";
+  if (dtype != EAT_F32 && dtype != EAT_BF16) return "dtype must be F32 or BF16";
+  return nullptr;
+}
+int elem_bytes(int32_t dtype) { return dtype == EAT_BF16 ? 2 : 4; }
+
+template <typename F>
+cudaError_t by_type(int32_t dtype, F&& run) {
+  return dtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr);
+}
+
+template <bool GLU>
+cudaError_t quant_rows(const void* x, int M, int K, int dtype, void* q, float* scale,
+                       cudaStream_t st) {
+  return by_type(dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    constexpr int N = Elem<T>::kN;
+    const int blocks = (K + kBlock - 1) / kBlock;
+    const long long units = (long long)((M + kRows - 1) / kRows) * blocks;
+    const bool vec = K % N == 0 && !misaligned(x, 16) && !misaligned(q, N);
+    const long long threads = units * (kBlock / N);
+    return launch_pdl(vec ? quant_rows_kernel<T, true, GLU> : quant_rows_kernel<T, false, GLU>,
+                      dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st,
+                      (const T*)x, M, K, blocks, (uint8_t*)q, scale);
+  });
+}
+
+}  // namespace
+}  // namespace eat
+
+using namespace eat;
+
+extern "C" eat_status eat_quant_rows(const void* x, int32_t M, int32_t K, int32_t dtype, void* q,
+                                     float* scale, void* stream) {
+  const char* fn = "eat_quant_rows";
+  if (!x || !q || !scale) return bad_arg(fn, "x, q and scale must be non-NULL");
+  if (const char* why = bad_matrix(M, K, dtype)) return bad_arg(fn, why);
+  if (misaligned(x, elem_bytes(dtype)) || misaligned(scale, 4)) return bad_arg(fn, "misaligned pointer");
+  return launched(fn, quant_rows<false>(x, M, K, dtype, q, scale, (cudaStream_t)stream));
+}
+
+extern "C" int64_t eat_quant_columns_rows(int32_t M, int32_t E) {
+  if (M < 1 || M > 1 << 30 || E < 1 || E > kMaxExperts) return 0;
+  // (an expert lacks at most 31 rows, and one without rows takes none)
+  return std::min(((long long)M + 31 * E) / 32, (long long)M) * 32;
+}
+extern "C" int64_t eat_quant_columns_blocks(int32_t M, int32_t E) {
+  if (M < 1 || M > 1 << 30 || E < 1 || E > kMaxExperts) return 0;
+  return std::min(((long long)M + 127 * E) / kBlock, (long long)M);
+}
+
+extern "C" eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int32_t dtype,
+                                        const int32_t* offsets, int32_t E, void* q, float* scale,
+                                        void* cq, float* cscale, void* stream) {
+  const char* fn = "eat_quant_columns";
+  if (!x || !cq || !cscale) return bad_arg(fn, "x, cq and cscale must be non-NULL");
+  if (!q != !scale) return bad_arg(fn, "q and scale come together");
+  if (const char* why = bad_matrix(M, K, dtype)) return bad_arg(fn, why);
+  if (E < 1 || E > kMaxExperts) return bad_arg(fn, "need 1 <= E <= 256");
+  if (!offsets && E != 1) return bad_arg(fn, "several experts need offsets");
+  if (misaligned(x, elem_bytes(dtype)) || misaligned(scale, 4) || misaligned(cscale, 4) ||
+      misaligned(offsets, 4))
+    return bad_arg(fn, "misaligned pointer");
+  const long long padded = eat_quant_columns_rows(M, E);
+  const int blocks = (int)eat_quant_columns_blocks(M, E), tiles = (K + kBlock - 1) / kBlock;
+  if (padded > 1 << 30) return bad_arg(fn, "need at most 2^30 padded rows");
+  return launched(fn, by_type(dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    constexpr int N = Elem<T>::kN;
+    const bool vec =
+        K % N == 0 && !misaligned(x, 16) && !misaligned(cq, N) && !(q && misaligned(q, N));
+    auto* kernel = q ? (vec ? quant_columns_kernel<T, true, true> : quant_columns_kernel<T, false, true>)
+                     : (vec ? quant_columns_kernel<T, true, false>
+                            : quant_columns_kernel<T, false, false>);
+    // (one more block than the experts can have: the rows behind them)
+    return launch_pdl(kernel, dim3(blocks + 1, std::min(tiles, 65535)), dim3(kThreads), 0,
+                      (cudaStream_t)stream, (const T*)x, M, K, offsets, E, (int)padded, blocks, tiles,
+                      (uint8_t*)q, scale, (uint8_t*)cq, cscale);
+  }));
+}
+
+extern "C" eat_status eat_quant_tiles(const void* w, int32_t E, int32_t N, int32_t K, int32_t dtype,
+                                      void* q, float* scale, void* stream) {
+  const char* fn = "eat_quant_tiles";
+  if (!w || !q || !scale) return bad_arg(fn, "w, q and scale must be non-NULL");
+  if (E < 1 || E > kMaxExperts) return bad_arg(fn, "need 1 <= E <= 256");
+  if (N < 1 || N > 65536) return bad_arg(fn, "need 1 <= N <= 65536");
+  if (const char* why = bad_matrix(N, K, dtype)) return bad_arg(fn, why);
+  if (misaligned(w, elem_bytes(dtype)) || misaligned(scale, 4)) return bad_arg(fn, "misaligned pointer");
+  return launched(fn, by_type(dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    constexpr int V = Elem<T>::kN;
+    const bool vec = K % V == 0 && !misaligned(w, 16) && !misaligned(q, V);
+    return launch_pdl(vec ? quant_tiles_kernel<T, true> : quant_tiles_kernel<T, false>,
+                      dim3((K + kBlock - 1) / kBlock, (N + kBlock - 1) / kBlock, E), dim3(kThreads),
+                      0, (cudaStream_t)stream, (const T*)w, N, K, (uint8_t*)q, scale);
+  }));
+}
+
+extern "C" eat_status eat_swiglu(const void* gu, int32_t R, int32_t F, int32_t dtype, void* h,
+                                 int32_t h_dtype, float* scale, void* stream) {
+  const char* fn = "eat_swiglu";
+  if (!gu || !h) return bad_arg(fn, "gu and h must be non-NULL");
+  if (const char* why = bad_matrix(R, F, dtype)) return bad_arg(fn, why);
+  if (h_dtype != dtype && h_dtype != EAT_FP8_E4M3)
+    return bad_arg(fn, "h_dtype must be dtype or FP8_E4M3");
+  const bool fp8 = h_dtype == EAT_FP8_E4M3;
+  if (fp8 && !scale) return bad_arg(fn, "an e4m3 output needs scale");
+  const int eb = elem_bytes(dtype);
+  if (misaligned(gu, eb) || misaligned(h, fp8 ? 1 : eb) || (fp8 && misaligned(scale, 4)))
+    return bad_arg(fn, "misaligned pointer");
+  const cudaStream_t st = (cudaStream_t)stream;
+  if (fp8) return launched(fn, quant_rows<true>(gu, R, F, dtype, h, scale, st));
+  return launched(fn, by_type(dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    constexpr int N = Elem<T>::kN;
+    const bool vec = F % N == 0 && !misaligned(gu, 16) && !misaligned(h, 16);
+    const long long n = (long long)R * F, per = (long long)kThreads * (vec ? N : 1);
+    return launch_pdl(vec ? swiglu_kernel<T, N, false> : swiglu_kernel<T, 1, false>,
+                      dim3((unsigned)((n + per - 1) / per)), dim3(kThreads), 0, st, (const T*)gu,
+                      (const T*)nullptr, n, F, (T*)h);
+  }));
+}
+
+extern "C" eat_status eat_swiglu_grad(const void* gu, const void* dh, int32_t R, int32_t F,
+                                      int32_t dtype, void* dgu, void* stream) {
+  const char* fn = "eat_swiglu_grad";
+  if (!gu || !dh || !dgu) return bad_arg(fn, "gu, dh and dgu must be non-NULL");
+  if (const char* why = bad_matrix(R, F, dtype)) return bad_arg(fn, why);
+  const int eb = elem_bytes(dtype);
+  if (misaligned(gu, eb) || misaligned(dh, eb) || misaligned(dgu, eb))
+    return bad_arg(fn, "misaligned pointer");
+  return launched(fn, by_type(dtype, [&](auto* tag) {
+    using T = std::remove_pointer_t<decltype(tag)>;
+    constexpr int N = Elem<T>::kN;
+    const bool vec = F % N == 0 && !misaligned(gu, 16) && !misaligned(dh, 16) && !misaligned(dgu, 16);
+    const long long n = (long long)R * F, per = (long long)kThreads * (vec ? N : 1);
+    return launch_pdl(vec ? swiglu_kernel<T, N, true> : swiglu_kernel<T, 1, true>,
+                      dim3((unsigned)((n + per - 1) / per)), dim3(kThreads), 0, (cudaStream_t)stream,
+                      (const T*)gu, (const T*)dh, n, F, (T*)dgu);
+  }));
+}

@@ -1,0 +1,463 @@
+// Tokens sorted by expert and back (what a layer's experts read and what becomes of their rows), and
+// the gradients of both.
+//   sort:    offsets[e] = number of selections of experts below e; slot[t][k] = the row of selection
+//            (t, k), rows of an expert in the selections' order (t, then k); -1 where there is none
+//   gather:  rows[slot[t][k]] = x[t], in x's type or in e4m3 with a scale for each 128 elements
+//   combine: y[t] = sum_k w[t][k] rows[slot[t][k]]  (w = 1: the gradient of gather)
+//   combine's gradient: drows[slot[t][k]] = w[t][k] dy[t];  dw[t][k] = <dy[t], rows[slot[t][k]]>
+// Bound: HBM; the sort itself: latency.  The copies go by token: a row of x (or dy) is read once and
+// written to all of its slots.  Rows behind the last selection are written as zeros by the same warps:
+// token t takes the t-th of them and every T-th further, at most K.  All sums are fp32, in the order of
+// k and of the lanes, so the same inputs give the same bits; a value is rounded when it is stored.
+#include "elem.cuh"
+#include "op_checks.cuh"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace eat {
+
+namespace {
+
+// ------------------------------------------------------------------------------------- sort
+// A block sorts a chunk of consecutive selections; a warp takes kPer times 32 of them in order and
+// counts per expert as it goes (lanes of the same expert find each other by __match_any_sync), so a
+// selection's row is its expert's first + the chunks' and warps' before + its rank in the warp.
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kPer = 8;
+constexpr int kChunkLen = kSortThreads * kPer;
+
+enum : int { kWhole = 0, kCount = 1, kAssign = 2 };
+
+// chunk[c][e]: kCount writes the chunks' counts, kAssign reads the sums of the chunks before, and total[e].
+template <int MODE>
+__global__ void __launch_bounds__(kSortThreads)
+sort_kernel(const int32_t* __restrict__ idx, int n, int K, int E, const uint8_t* __restrict__ mask,
+            int32_t* chunk, const int32_t* __restrict__ total, int32_t* __restrict__ offsets,
+            int32_t* __restrict__ slot) {
+  extern __shared__ int s_cnt[];  // [warps][E], then [E] first rows
+  int* const s_base = s_cnt + kSortWarps * E;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  for (int i = tid; i < kSortWarps * E; i += kSortThreads) s_cnt[i] = 0;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int first = blockIdx.x * kChunkLen + warp * 32 * kPer + lane;
+  int ex[kPer], rank[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int at = first + 32 * i;
+    int e = at < n ? idx[at] : -1;
+    if (mask && at < n && !mask[at / K]) e = -1;
+    ex[i] = e >= 0 && e < E ? e : -1;
+  }
+  __syncthreads();
+  int* const mine = s_cnt + warp * E;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const unsigned same = __match_any_sync(0xffffffffu, ex[i]);
+    const int below = __popc(same & ((1u << lane) - 1u));
+    int c = 0;
+    if (ex[i] >= 0) c = mine[ex[i]];
+    rank[i] = c + below;
+    __syncwarp();
+    if (ex[i] >= 0 && below == 0) mine[ex[i]] = c + __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int e = tid; e < E; e += kSortThreads) {
+    int sum = 0;
+    for (int w = 0; w < kSortWarps; ++w) {
+      const int c = s_cnt[w * E + e];
+      s_cnt[w * E + e] = sum;
+      sum += c;
+    }
+    if (MODE == kCount) chunk[(size_t)blockIdx.x * E + e] = sum;
+    s_base[e] = MODE == kAssign ? total[e] : sum;
+  }
+  if (MODE == kCount) return;
+  __syncthreads();
+  if (warp == 0) {  // first rows of the experts
+    int before = 0;
+    for (int b = 0; b < E; b += 32) {
+      const int c = b + lane < E ? s_base[b + lane] : 0;
+      int v = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+      }
+      if (b + lane < E) {
+        s_base[b + lane] = before + v - c;
+        if (blockIdx.x == 0) offsets[b + lane] = before + v - c;
+      }
+      before += __shfl_sync(0xffffffffu, v, 31);
+    }
+    if (blockIdx.x == 0 && lane == 0) offsets[E] = before;
+  }
+  __syncthreads();
+  if (MODE == kAssign) {
+    for (int e = tid; e < E; e += kSortThreads) s_base[e] += chunk[(size_t)blockIdx.x * E + e];
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int at = first + 32 * i;
+    if (at < n) slot[at] = ex[i] < 0 ? -1 : s_base[ex[i]] + mine[ex[i]] + rank[i];
+  }
+}
+
+// A warp per expert: chunk[c][e] becomes the sum of the chunks before c, total[e] the sum of all.
+__global__ void __launch_bounds__(32) sort_scan_kernel(int32_t* chunk, int chunks, int E,
+                                                       int32_t* __restrict__ total) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int e = blockIdx.x, lane = threadIdx.x;
+  int before = 0;
+  for (int b = 0; b < chunks; b += 32) {
+    const int at = b + lane;
+    const int c = at < chunks ? chunk[(size_t)at * E + e] : 0;
+    int v = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
+    }
+    if (at < chunks) chunk[(size_t)at * E + e] = before + v - c;
+    before += __shfl_sync(0xffffffffu, v, 31);
+  }
+  if (lane == 0) total[e] = before;
+}
+
+// ------------------------------------------------------------------------------ there and back
+constexpr int kWarps = 8;  // of a block whose warps take pieces of tokens
+constexpr int kLoads = 4;  // vectors of a lane at a time
+
+// Rows behind the last selection, as offsets says (any value is held to the buffer).
+__device__ __forceinline__ int rows_used(const int32_t* offsets, int E, int rows) {
+  return max(0, min(offsets[E], rows));
+}
+
+// V: what a row is copied in (16 bytes where the rows begin at multiples of it, else less).
+template <typename V>
+__global__ void __launch_bounds__(32 * kWarps)
+gather_kernel(const V* __restrict__ x, const int32_t* __restrict__ slot,
+              const int32_t* __restrict__ offsets, int T, int K, int E, int len, int pieces,
+              V* __restrict__ rows) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, t = (int)(w / pieces), c0 = (int)(w % pieces) * 32 * kLoads;
+  if (t >= T) return;
+  const int M = T * K, used = rows_used(offsets, E, M);
+  const int mine = lane < K ? slot[(size_t)t * K + lane] : -1;
+  V v[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int c = c0 + 32 * i + lane;
+    if (c < len) v[i] = x[(size_t)t * len + c];
+  }
+  for (int k = 0; k < K; ++k) {
+    const int r = __shfl_sync(0xffffffffu, mine, k);
+    if (r < 0 || r >= M) continue;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = c0 + 32 * i + lane;
+      if (c < len) rows[(size_t)r * len + c] = v[i];
+    }
+  }
+  for (long long r = (long long)used + t; r < M; r += T) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = c0 + 32 * i + lane;
+      if (c < len) rows[(size_t)r * len + c] = V{};
+    }
+  }
+}
+
+// The same in e4m3: a block of 128 elements is taken by as many lanes as it has 16-byte vectors.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(32 * kWarps)
+gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
+                  const int32_t* __restrict__ offsets, int tokens, int K, int E, int d, int pieces,
+                  uint8_t* __restrict__ q, float* __restrict__ scale) {
+  constexpr int N = Elem<T>::kN, G = kBlock / N, U = 2;
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, t = (int)(w / pieces);
+  const int c0 = (int)(w % pieces) * 32 * N * U + lane * N;
+  if (t >= tokens) return;
+  const int M = tokens * K, used = rows_used(offsets, E, M);
+  const int mine = lane < K ? slot[(size_t)t * K + lane] : -1;
+  float v[U][N], f[U], s[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int c = c0 + 32 * N * i;
+    float top = 0.f;
+    if (c < d) load_elems<T, N, VEC>(x + (size_t)t * d + c, d - c, v[i]);
+    if (c < d)
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[i][j]));
+    top = group_max<G>(top);
+    f[i] = block_factor(top);
+    s[i] = block_scale(top);
+  }
+  for (int k = 0; k < K; ++k) {
+    const int r = __shfl_sync(0xffffffffu, mine, k);
+    if (r < 0 || r >= M) continue;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int c = c0 + 32 * N * i;
+      if (c >= d) continue;
+      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, v[i], f[i]);
+      if (lane % G == 0) scale[(size_t)(c / kBlock) * M + r] = s[i];
+    }
+  }
+  const float zero[N] = {};
+  for (long long r = (long long)used + t; r < M; r += tokens) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int c = c0 + 32 * N * i;
+      if (c >= d) continue;
+      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, zero, 0.f);
+      if (lane % G == 0) scale[(size_t)(c / kBlock) * M + r] = 1.0f;
+    }
+  }
+}
+
+// y[t]: a warp takes N elements a lane of one token, all of its rows' loads before their use.
+template <typename T, int N>
+__global__ void __launch_bounds__(32 * kWarps)
+combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
+               const float* __restrict__ weight, int tokens, int K, int d, int pieces,
+               T* __restrict__ y) {
+  constexpr bool VEC = N > 1;
+  constexpr int kAhead = 8;  // rows
+  pdl_wait();
+  pdl_launch_dependents();
+  const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, t = (int)(w / pieces);
+  const int c = ((int)(w % pieces) * 32 + lane) * N;
+  if (t >= tokens) return;
+  const int M = tokens * K;
+  int mine = lane < K ? slot[(size_t)t * K + lane] : -1;
+  if (mine >= M) mine = -1;
+  const float wt = lane < K && weight ? weight[(size_t)t * K + lane] : 1.0f;
+  float sum[N] = {};
+  for (int k0 = 0; k0 < K; k0 += kAhead) {
+    float v[kAhead][N];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+      if (r >= 0 && c < d) load_elems<T, N, VEC>(rows + (size_t)r * d + c, d - c, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+      const float f = __shfl_sync(0xffffffffu, wt, (k0 + k) & 31);
+      if (r < 0) continue;
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[j] = fmaf(f, v[k][j], sum[j]);
+    }
+  }
+  if (c < d) store_elems<T, N, VEC>(y + (size_t)t * d + c, d - c, sum);
+}
+
+// A block takes a token: its warps share the row, and add their parts of dw in their order.
+template <typename T, int N>
+__global__ void __launch_bounds__(32 * kWarps)
+combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
+                    const int32_t* __restrict__ slot, const int32_t* __restrict__ offsets,
+                    const float* __restrict__ weight, int tokens, int K, int E, int d,
+                    T* __restrict__ drows, float* __restrict__ dw) {
+  constexpr bool VEC = N > 1;
+  __shared__ float s_part[kWarps][kMaxK];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int t = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int M = tokens * K, used = rows_used(offsets, E, M);
+  int mine = lane < K ? slot[(size_t)t * K + lane] : -1;
+  if (mine >= M) mine = -1;
+  const float wt = lane < K ? weight[(size_t)t * K + lane] : 0.f;
+  float part = 0.f;  // lane k's: the warp's part of dw[t][k]
+  for (int c = threadIdx.x * N; c - lane * N < d; c += blockDim.x * N) {
+    float g[N];
+    const bool in = c < d;
+    if (in) load_elems<T, N, VEC>(dy + (size_t)t * d + c, d - c, g);
+    for (int k = 0; k < K; ++k) {
+      const int r = __shfl_sync(0xffffffffu, mine, k);
+      const float f = __shfl_sync(0xffffffffu, wt, k);
+      if (r < 0) continue;
+      float dot = 0.f;
+      if (in) {
+        float v[N], o[N];
+        load_elems<T, N, VEC>(rows + (size_t)r * d + c, d - c, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          dot = fmaf(g[j], v[j], dot);
+          o[j] = f * g[j];
+        }
+        store_elems<T, N, VEC>(drows + (size_t)r * d + c, d - c, o);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      if (lane == k) part += dot;
+    }
+    const float zero[N] = {};
+    if (in)
+      for (long long r = (long long)used + t; r < M; r += tokens)
+        store_elems<T, N, VEC>(drows + (size_t)r * d + c, d - c, zero);
+  }
+  if (lane < K) s_part[warp][lane] = part;
+  __syncthreads();
+  if (threadIdx.x < K) {
+    float s = 0.f;
+    for (int i = 0; i < (int)blockDim.x / 32; ++i) s += s_part[i][threadIdx.x];
+    dw[(size_t)t * K + threadIdx.x] = s;
+  }
+}
+
+int sort_chunks(int n) { return (n + kChunkLen - 1) / kChunkLen; }
+dim3 warp_grid(long long warps) { return dim3((unsigned)((warps + kWarps - 1) / kWarps)); }
+
+// What the calls on sorted rows have in common; empty when they may go on.
+const char* bad_rows(int32_t T, int32_t K, int32_t E, int32_t d, int32_t dtype) {
+  if (T < 1 || K < 1 || K > kMaxK || (long long)T * K > 1 << 30)
+    return "need T >= 1, 1 <= K <= 16 and T K <= 2^30";
+  if (E < 1 || E > kMaxExperts) return "need 1 <= E <= 256";
+  if (d < 1 || d > 65536) return "need 1 <= d <= 65536";
+  if (dtype != EAT_F32 && dtype != EAT_BF16) return "dtype must be F32 or BF16";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace eat
+
+using namespace eat;
+
+extern "C" int64_t eat_expert_sort_workspace(int32_t T, int32_t K, int32_t E) {
+  if (T < 1 || K < 1 || K > kMaxK || E < 1 || E > kMaxExperts || (long long)T * K > 1 << 30) return 0;
+  return (int64_t)(sort_chunks(T * K) + 1) * E * 4;
+}
+
+extern "C" eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, int32_t E,
+                                      const uint8_t* mask, int32_t* offsets, int32_t* slot,
+                                      void* work, void* stream) {
+  const char* fn = "eat_expert_sort";
+  if (!idx || !offsets || !slot || !work)
+    return bad_arg(fn, "idx, offsets, slot and work must be non-NULL");
+  if (const char* why = bad_rows(T, K, E, 1, EAT_F32)) return bad_arg(fn, why);
+  if (misaligned(idx, 4) || misaligned(offsets, 4) || misaligned(slot, 4) || misaligned(work, 16))
+    return bad_arg(fn, "misaligned pointer");
+  const cudaStream_t st = (cudaStream_t)stream;
+  const int n = T * K, chunks = sort_chunks(n);
+  const size_t smem = (size_t)(kSortWarps + 1) * E * 4;  // at most 33 KB
+  if (chunks == 1)
+    return launched(fn, launch_pdl(sort_kernel<kWhole>, dim3(1), dim3(kSortThreads), smem, st, idx,
+                                   n, K, E, mask, (int32_t*)nullptr, (const int32_t*)nullptr,
+                                   offsets, slot));
+  int32_t *chunk = (int32_t*)work, *total = chunk + (size_t)chunks * E;
+  cudaError_t e = launch_pdl(sort_kernel<kCount>, dim3(chunks), dim3(kSortThreads), smem, st, idx, n,
+                             K, E, mask, chunk, (const int32_t*)nullptr, (int32_t*)nullptr,
+                             (int32_t*)nullptr);
+  if (e == cudaSuccess)
+    e = launch_pdl(sort_scan_kernel, dim3(E), dim3(32), 0, st, chunk, chunks, E, total);
+  if (e == cudaSuccess)
+    e = launch_pdl(sort_kernel<kAssign>, dim3(chunks), dim3(kSortThreads), smem, st, idx, n, K, E,
+                   mask, chunk, (const int32_t*)total, offsets, slot);
+  return launched(fn, e);
+}
+
+extern "C" eat_status eat_expert_gather(const void* x, int32_t T, int32_t K, int32_t E, int32_t d,
+                                        int32_t dtype, const int32_t* slot, const int32_t* offsets,
+                                        void* rows, int32_t rows_dtype, float* scale,
+                                        void* stream) {
+  const char* fn = "eat_expert_gather";
+  if (!x || !slot || !offsets || !rows)
+    return bad_arg(fn, "x, slot, offsets and rows must be non-NULL");
+  if (const char* why = bad_rows(T, K, E, d, dtype)) return bad_arg(fn, why);
+  if (rows_dtype != dtype && rows_dtype != EAT_FP8_E4M3)
+    return bad_arg(fn, "rows_dtype must be dtype or FP8_E4M3");
+  const bool fp8 = rows_dtype == EAT_FP8_E4M3;
+  if (fp8 && !scale) return bad_arg(fn, "e4m3 rows need scale");
+  const int eb = dtype == EAT_BF16 ? 2 : 4;
+  if (misaligned(x, eb) || misaligned(rows, fp8 ? 1 : eb) || misaligned(slot, 4) ||
+      misaligned(offsets, 4) || (fp8 && misaligned(scale, 4)))
+    return bad_arg(fn, "misaligned pointer");
+  const cudaStream_t st = (cudaStream_t)stream;
+  if (fp8) {
+    auto run = [&](auto* tag) {
+      using X = std::remove_pointer_t<decltype(tag)>;
+      constexpr int N = Elem<X>::kN;
+      const int pieces = (d + 64 * N - 1) / (64 * N);
+      const bool vec = d % N == 0 && !misaligned(x, 16) && !misaligned(rows, N);
+      return launch_pdl(vec ? gather_fp8_kernel<X, true> : gather_fp8_kernel<X, false>,
+                        warp_grid((long long)T * pieces), dim3(32 * kWarps), 0, st, (const X*)x,
+                        slot, offsets, T, K, E, d, pieces, (uint8_t*)rows, scale);
+    };
+    return launched(fn, dtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr));
+  }
+  auto run = [&](auto* tag) {
+    using V = std::remove_pointer_t<decltype(tag)>;
+    const int len = (int)((long long)d * eb / (int)sizeof(V));
+    const int pieces = (len + 32 * kLoads - 1) / (32 * kLoads);
+    return launch_pdl(gather_kernel<V>, warp_grid((long long)T * pieces), dim3(32 * kWarps), 0, st,
+                      (const V*)x, slot, offsets, T, K, E, len, pieces, (V*)rows);
+  };
+  auto fits = [&](int n) { return (long long)d * eb % n == 0 && !misaligned(x, n) && !misaligned(rows, n); };
+  return launched(fn, fits(16)  ? run((uint4*)nullptr)
+                      : fits(4) ? run((uint32_t*)nullptr)
+                                : run((uint16_t*)nullptr));
+}
+
+extern "C" eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K, int32_t d,
+                                         int32_t dtype, const int32_t* slot, const float* w, void* y,
+                                         void* stream) {
+  const char* fn = "eat_expert_combine";
+  if (!rows || !slot || !y) return bad_arg(fn, "rows, slot and y must be non-NULL");
+  if (const char* why = bad_rows(T, K, 1, d, dtype)) return bad_arg(fn, why);
+  const int eb = dtype == EAT_BF16 ? 2 : 4;
+  if (misaligned(rows, eb) || misaligned(y, eb) || misaligned(slot, 4) || misaligned(w, 4))
+    return bad_arg(fn, "misaligned pointer");
+  if (overlap(rows, (size_t)T * K * d * eb, y, (size_t)T * d * eb))
+    return bad_arg(fn, "y overlaps rows");
+  auto run = [&](auto* tag) {
+    using X = std::remove_pointer_t<decltype(tag)>;
+    constexpr int N = Elem<X>::kN;
+    const bool vec = d % N == 0 && !misaligned(rows, 16) && !misaligned(y, 16);
+    const int n = vec ? N : 1, pieces = (d + 32 * n - 1) / (32 * n);
+    return launch_pdl(vec ? combine_kernel<X, N> : combine_kernel<X, 1>,
+                      warp_grid((long long)T * pieces), dim3(32 * kWarps), 0, (cudaStream_t)stream,
+                      (const X*)rows, slot, w, T, K, d, pieces, (X*)y);
+  };
+  return launched(fn, dtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr));
+}
+
+extern "C" eat_status eat_expert_combine_grad(const void* dy, const void* rows, int32_t T, int32_t K,
+                                              int32_t E, int32_t d, int32_t dtype,
+                                              const int32_t* slot, const int32_t* offsets,
+                                              const float* w, void* drows, float* dw, void* stream) {
+  const char* fn = "eat_expert_combine_grad";
+  if (!dy || !rows || !slot || !offsets || !w || !drows || !dw)
+    return bad_arg(fn, "dy, rows, slot, offsets, w, drows and dw must be non-NULL");
+  if (const char* why = bad_rows(T, K, E, d, dtype)) return bad_arg(fn, why);
+  const int eb = dtype == EAT_BF16 ? 2 : 4;
+  if (misaligned(dy, eb) || misaligned(rows, eb) || misaligned(drows, eb) || misaligned(slot, 4) ||
+      misaligned(offsets, 4) || misaligned(w, 4) || misaligned(dw, 4))
+    return bad_arg(fn, "misaligned pointer");
+  const size_t n = (size_t)T * K * d * eb;
+  if (overlap(drows, n, rows, n) || overlap(drows, n, dy, n / K))
+    return bad_arg(fn, "drows overlaps rows or dy");
+  auto run = [&](auto* tag) {
+    using X = std::remove_pointer_t<decltype(tag)>;
+    constexpr int N = Elem<X>::kN;
+    const bool vec =
+        d % N == 0 && !misaligned(dy, 16) && !misaligned(rows, 16) && !misaligned(drows, 16);
+    const int per = vec ? N : 1, warps = std::min(kWarps, (d + 32 * per - 1) / (32 * per));
+    return launch_pdl(vec ? combine_grad_kernel<X, N> : combine_grad_kernel<X, 1>, dim3(T),
+                      dim3(32 * warps), 0, (cudaStream_t)stream, (const X*)dy, (const X*)rows, slot,
+                      offsets, w, T, K, E, d, (X*)drows, dw);
+  };
+  return launched(fn, dtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr));
+}

@@ -96,6 +96,25 @@ _SIGS = {
     "eat_head_nll_grad": (c_i32, [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
     "eat_head_reset": (c_i32, [c_vp, c_vp]),
     "eat_head_selftest_expire_wait": (c_i32, [c_vp, c_i64, c_vp]),
+    "eat_expert_sort": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "eat_expert_sort_workspace": (c_i64, [c_i32, c_i32, c_i32]),
+    "eat_expert_gather": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32,
+                                  c_vp, c_vp]),
+    "eat_expert_combine": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp]),
+    "eat_expert_combine_grad": (c_i32, [c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp,
+                                        c_vp, c_vp, c_vp, c_vp]),
+    "eat_quant_rows": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp]),
+    "eat_quant_columns": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp,
+                                  c_vp]),
+    "eat_quant_columns_rows": (c_i64, [c_i32, c_i32]),
+    "eat_quant_columns_blocks": (c_i64, [c_i32, c_i32]),
+    "eat_quant_tiles": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp]),
+    "eat_block_mm": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp,
+                             c_i32, c_vp]),
+    "eat_block_mm_grad": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                  c_vp, c_i32, c_vp]),
+    "eat_swiglu": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_i32, c_vp, c_vp]),
+    "eat_swiglu_grad": (c_i32, [c_vp, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp]),
     "eat_last_error": (ctypes.c_char_p, [c_vp]),
     "eat_status_string": (ctypes.c_char_p, [c_i32]),
 }
@@ -335,6 +354,70 @@ def eat_head_selftest_expire_wait(h, limit_ns: int, stream=None):
     _check(lib().eat_head_selftest_expire_wait(h, limit_ns, _stream(stream)))
 
 
+def eat_expert_sort(idx, T, K, E, mask, offsets, slot, work, stream=None):
+    _check(lib().eat_expert_sort(_ptr(idx), T, K, E, _ptr(mask), _ptr(offsets), _ptr(slot),
+                                 _ptr(work), _stream(stream)))
+
+
+def eat_expert_sort_workspace(T, K, E) -> int:
+    return lib().eat_expert_sort_workspace(T, K, E)
+
+
+def eat_expert_gather(x, T, K, E, d, dtype, slot, offsets, rows, rows_dtype, scale=None, stream=None):
+    _check(lib().eat_expert_gather(_ptr(x), T, K, E, d, dtype, _ptr(slot), _ptr(offsets), _ptr(rows),
+                                   rows_dtype, _ptr(scale), _stream(stream)))
+
+
+def eat_expert_combine(rows, T, K, d, dtype, slot, w, y, stream=None):
+    _check(lib().eat_expert_combine(_ptr(rows), T, K, d, dtype, _ptr(slot), _ptr(w), _ptr(y),
+                                    _stream(stream)))
+
+
+def eat_expert_combine_grad(dy, rows, T, K, E, d, dtype, slot, offsets, w, drows, dw, stream=None):
+    _check(lib().eat_expert_combine_grad(_ptr(dy), _ptr(rows), T, K, E, d, dtype, _ptr(slot),
+                                         _ptr(offsets), _ptr(w), _ptr(drows), _ptr(dw),
+                                         _stream(stream)))
+
+
+def eat_quant_rows(x, M, K, dtype, q, scale, stream=None):
+    _check(lib().eat_quant_rows(_ptr(x), M, K, dtype, _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def eat_quant_columns(x, M, K, dtype, offsets, E, q, scale, cq, cscale, stream=None):
+    _check(lib().eat_quant_columns(_ptr(x), M, K, dtype, _ptr(offsets), E, _ptr(q), _ptr(scale),
+                                   _ptr(cq), _ptr(cscale), _stream(stream)))
+
+
+def eat_quant_columns_rows(M, E) -> int:
+    return lib().eat_quant_columns_rows(M, E)
+
+
+def eat_quant_columns_blocks(M, E) -> int:
+    return lib().eat_quant_columns_blocks(M, E)
+
+
+def eat_quant_tiles(w, E, N, K, dtype, q, scale, stream=None):
+    _check(lib().eat_quant_tiles(_ptr(w), E, N, K, dtype, _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def eat_block_mm(xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, stream=None):
+    _check(lib().eat_block_mm(_ptr(xq), _ptr(xs), _ptr(wq), _ptr(ws), _ptr(offsets), E, M, N, K,
+                              int(transposed), _ptr(y), ydtype, _stream(stream)))
+
+
+def eat_block_mm_grad(gq, gs, xq, xs, offsets, E, rows, blocks, N, K, dw, dtype, stream=None):
+    _check(lib().eat_block_mm_grad(_ptr(gq), _ptr(gs), _ptr(xq), _ptr(xs), _ptr(offsets), E, rows,
+                                   blocks, N, K, _ptr(dw), dtype, _stream(stream)))
+
+
+def eat_swiglu(gu, R, F, dtype, h, h_dtype, scale=None, stream=None):
+    _check(lib().eat_swiglu(_ptr(gu), R, F, dtype, _ptr(h), h_dtype, _ptr(scale), _stream(stream)))
+
+
+def eat_swiglu_grad(gu, dh, R, F, dtype, dgu, stream=None):
+    _check(lib().eat_swiglu_grad(_ptr(gu), _ptr(dh), R, F, dtype, _ptr(dgu), _stream(stream)))
+
+
 # ------------------------------------------------------------------------------------------------
 # The operators around the layer on torch tensors.  Tensors are CUDA, contiguous, of the stated
 # type and all on one device (ValueError otherwise); outputs are new tensors, and calls go to the
@@ -388,6 +471,86 @@ def balance_loss(logits, idx, mask=None):
 def balance_grad(logits, counts, n_tokens, g, mask=None):
     """Gradient of balance_loss to the logits, times g (fp32 [1] on the device)."""
     return (_eatops or _ops()).balance_grad(logits, counts, n_tokens, g, mask)
+
+
+def expert_sort(idx, n_experts, mask=None):
+    """(offsets [E + 1], slot [T, K]) int32 of selected experts idx [T, K] int32 (EatLayer.route's):
+    experts' first rows once the selections are sorted by expert, and each selection's row (-1: none);
+    mask [T] bool: tokens that count."""
+    return (_eatops or _ops()).expert_sort(idx, n_experts, mask)
+
+
+def expert_gather(x, slot, offsets):
+    """rows [T K, d] with rows[slot[t, k]] = x[t], zeros behind the last (x [T, d] fp32 or bf16)."""
+    return (_eatops or _ops()).expert_gather(x, slot, offsets, False)[0]
+
+
+def expert_gather_fp8(x, slot, offsets):
+    """(q, scale) of expert_gather's rows, as quant_rows gives them."""
+    return (_eatops or _ops()).expert_gather(x, slot, offsets, True)
+
+
+def expert_combine(rows, slot, w=None):
+    """y [T, d] = sum over k of w[t, k] rows[slot[t, k]]; without w, the gradient of expert_gather."""
+    return (_eatops or _ops()).expert_combine(rows, slot, w)
+
+
+def expert_combine_grad(dy, rows, slot, offsets, w):
+    """(drows, dw): the gradients of expert_combine to its rows and to w."""
+    return (_eatops or _ops()).expert_combine_grad(dy, rows, slot, offsets, w)
+
+
+def quant_rows(x):
+    """(q, scale): x [M, K] fp32 or bf16 as torch.float8_e4m3fn, with a scale for each 128 elements of a
+    row, [ceil(K / 128), M] fp32."""
+    return (_eatops or _ops()).quant_rows(x)
+
+
+def quant_columns(x, offsets=None):
+    """(cq, cscale): e4m3 with a scale for each 128 rows of a column, each expert's rows beginning at a
+    multiple of 32 and its blocks at its first row (see eat_quant_columns): block_mm_grad's operands.
+    offsets [E + 1] int32 of rows sorted by expert; None: all rows are one expert's."""
+    return (_eatops or _ops()).quant_columns(x, offsets, False)[2:]
+
+
+def quant_rows_columns(x, offsets=None):
+    """(q, scale, cq, cscale): quant_rows and quant_columns with one read of x.  Rows from offsets[E] on
+    are zeros in q."""
+    return (_eatops or _ops()).quant_columns(x, offsets, True)
+
+
+def quant_tiles(w):
+    """(q, scale): weights w [N, K] or [E, N, K], fp32 or bf16, as e4m3 with a scale for each 128 x 128
+    tile, [E, ceil(N / 128), ceil(K / 128)] fp32 (no E for a matrix)."""
+    return (_eatops or _ops()).quant_tiles(w)
+
+
+def block_mm(xq, xs, wq, ws, offsets=None, transposed=False, dtype=None):
+    """y = x w^T (transposed: x w) of quant_rows' x and quant_tiles' w: a matrix for all rows, or (w
+    [E, N, K]) expert e's for rows offsets[e] .. offsets[e + 1], zeros behind offsets[E].  dtype:
+    torch.bfloat16 (None) or torch.float32."""
+    return (_eatops or _ops()).block_mm(xq, xs, wq, ws, offsets, transposed, dtype)
+
+
+def block_mm_grad(gq, gs, xq, xs, offsets=None, dtype=None):
+    """dw [N, K] = g^T x of quant_columns' g [., N] and x [., K]; with offsets [E + 1] the experts',
+    [E, N, K].  dtype as in block_mm."""
+    return (_eatops or _ops()).block_mm_grad(gq, gs, xq, xs, offsets, dtype)
+
+
+def swiglu(gu):
+    """h [R, F] = silu(gate) * up of rows gu [R, 2 F] = [gate | up], fp32 or bf16."""
+    return (_eatops or _ops()).swiglu(gu, False)[0]
+
+
+def swiglu_fp8(gu):
+    """(q, scale) of swiglu's rows, as quant_rows gives them (from the unrounded values)."""
+    return (_eatops or _ops()).swiglu(gu, True)
+
+
+def swiglu_grad(gu, dh):
+    """dgu [R, 2 F]: the gradient of swiglu to its rows."""
+    return (_eatops or _ops()).swiglu_grad(gu, dh)
 
 
 class EatHead:
