@@ -3,134 +3,594 @@
 //   y[r][n]  = sum_b xs[b][r] ws[n / 128][b] sum_{k in b} x[r][k] w[n][k]
 //   y[r][k]  = the same with w as it lies, summed over n (transposed: the gradient to x)
 //   dw[n][k] = sum_b gs[b][n] xs[b][k] sum_{r in b} g[r][n] x[r][k], b the blocks of 128 rows of an expert
-// All sums are fp32; each block's sum is scaled and added once; a value is rounded when it is stored.
+//
+// A tile of the output is up to NT of its rows x 128 of its columns, as the transposed product: the 128
+// columns (w's; dw: x's) are the MMA's M, the rows (x's; dw: g's) its N.  So a matrix is read once for up
+// to NT rows of x, however few there are, and an expert's rows are cut into tiles of equal heights.
+// A k-block of 128 is four MMAs into an accumulator of its own in TMEM; the epilogue's warps read it,
+// multiply by the block's scales and add it to fp32 sums in registers while the next k-blocks run.  In
+// the 16x256b layout a thread has two neighbouring rows of the output for each of its columns, so a
+// scale's pair is one load and each packed multiply-add takes two elements.
+// Operands come by TMA as they lie (K-major, or MN-major where the sum runs over their rows): w serves
+// both directions, and the gradient reads both operands by rows.
+// Warps: 0 issues TMA, 1 owns TMEM and issues MMAs, 2 copies the blocks' scales into a ring and clears
+// the rows behind the last expert's, the others drain TMEM.  Every wait is bounded; where one expires
+// the CTA's tiles that are not done become NaN, copies and MMAs land, TMEM is freed and the kernel ends.
 #include "elem.cuh"
 #include "op_checks.cuh"
+#include "tc_ptx.cuh"
+
+#include <algorithm>
+
+#include "tensor_map.cuh"
 
 namespace eat {
 
 namespace {
 
+using namespace ptx;
+
 enum : int { kForward = 0, kBack = 1, kGrad = 2 };
 
-// out[i][j] = sum_k rows[i][k] cols[j][k]: rows are x's (of an expert), or dw's n; cols are what is left.
 struct Args {
-  const uint8_t *a, *w;      // rows' and columns' operand
-  const float *as, *ws;
-  const int32_t* offsets;    // or null: one expert with every row
-  int E, M, N, K;            // N, K: w's shape; M: x's rows (kGrad: the operands' padded rows)
-  int blocks;                // kGrad: rows of the scales
+  const float *xs, *ws;  // kGrad: g's and x's
+  const int32_t* offsets;
+  int E, M, N, K;  // N, K: w's shape; M: x's rows (kGrad: the operands' padded rows)
+  int blocks;      // kGrad: rows of the scales
   void* out;
+  int vec;         // rows of the output begin at multiples of 16 bytes
 };
 
-constexpr int kTile = 64, kStep = 32, kThreads = 256;
+constexpr int kOperand = kBlock * kBlock;  // bytes of 128 rows of a k-block
+constexpr int kSlots = 6;                  // of the ring of scales
+constexpr int kFirstEpi = 3;               // warps before the epilogue's
 
-__device__ __forceinline__ float e4m3(uint8_t v) {
-  __nv_fp8_e4m3 q;
-  q.__x = v;
-  return (float)q;
+template <int NT>
+struct Cfg {
+  static constexpr int kEpiWarps = NT >= 64 ? 8 : 4;
+  static constexpr int kCols = NT >= 64 ? NT / 2 : NT;  // of the accumulator, for a warp
+  static constexpr int kChunk = kCols < 32 ? kCols : 32;  // of them at a time
+  static constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
+  static constexpr int kBufs = NT == 256 ? 2 : NT == 128 ? 4 : 8;  // accumulators
+  static constexpr int kTmemCols = NT * kBufs;
+  static constexpr int kStage = kOperand + NT * kBlock;
+  static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 8 : 10;
+  static constexpr int kBox = NT < 64 ? NT : 64;  // rows of x that a copy takes
+  static constexpr int kSlotFloats = NT + kBlock;
+  static constexpr int kOut = kEpiWarps * 32 * 64;  // 32 rows of 64 bytes per warp
+  static constexpr int kSmem =
+      1024 + kStages * kStage + kOut + kSlots * kSlotFloats * 4;
+};
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0,
+                                            int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+// 16 lanes x 8 G columns: registers 4 g .. 4 g + 3 of lane l hold columns 8 g + 2 (l % 4), + 1 of lane
+// l / 4, and the same columns of lane l / 4 + 8.
+__device__ __forceinline__ void tmem_ld_pairs(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "
+      "%12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+// MN-major e4m3, 128-byte swizzle: a row of 128 bytes holds 128 consecutive M (or N) elements of one k;
+// groups of 8 k lie 1024 B apart (stride offset), the next 128 elements 16384 B further (leading offset);
+// 32 k further is + 256.
+__device__ __forceinline__ uint64_t sdesc_mn8(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFF) >> 4) | (uint64_t)(kOperand >> 4) << 16 |
+         (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
-template <int MODE, typename T>
-__global__ void __launch_bounds__(kThreads) block_mm_kernel(const Args a) {
-  __shared__ float s_a[kStep][kTile + 1], s_b[kStep][kTile + 1];
+// Pairs of floats
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, float b) {
+  uint64_t r;
+  asm("{\n .reg .b64 t;\n mov.b64 t, {%2, %2};\n mul.rn.f32x2 %0, %1, t;\n}\n"
+      : "=l"(r)
+      : "l"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 floats(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t bf16x2(uint64_t v) {
+  const float2 f = floats(v);
+  const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+  return *(const uint32_t*)&b;
+}
+// Four 8 x 8 matrices of 16-bit values whose fragments the lanes hold, transposed into rows of 16 bytes.
+__device__ __forceinline__ void stmatrix_t(uint32_t dst, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(dst),
+               "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
+
+// The experts of a call, in shared memory: rows row[e] .. end[e] - 1 (held to [0, M]) and the row tiles of
+// the experts below e; kGrad: first padded row, number of rows, first block.
+struct Experts {
+  int row[kMaxExperts], end[kMaxExperts], tile0[kMaxExperts + 1];
+};
+// One tile: `rows` output rows from row0 (x's rows, or dw's n), columns c0 .. c0 + 127 of expert e, nkb
+// k-blocks (the last of `tail` k; kGrad: from padded row k0, block b0).
+struct Tile {
+  int e, row0, rows, c0, nkb, k0, b0, sums;
+};
+
+template <int MODE, int NT, typename Out>
+__global__ void __launch_bounds__(Cfg<NT>::kThreads, 1)
+block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                const Args a) {
+  using C = Cfg<NT>;
+  static_assert(MODE != kGrad || NT % kBlock == 0, "columns of 128 bytes");
+  constexpr int S = C::kStages, B = C::kBufs;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* const s_out = smem + S * C::kStage;
+  float* const s_scale = (float*)(s_out + C::kOut);
+  __shared__ uint64_t full[S], empty[S], tfull[B], tempty[B], sfull[kSlots], sempty[kSlots], mma_done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  __shared__ unsigned int err_word;
+  __shared__ Experts ex;
+  volatile int* const abort_flag = &abort_word;
+  const WaitCtx wc{abort_flag, &err_word};
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < B; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], C::kEpiWarps);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&sfull[s], 32);
+      mbar_init(&sempty[s], C::kEpiWarps);
+    }
+    mbar_init(&mma_done, 1);
+    abort_word = 0;
+    err_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&map_a);
+    prefetch_map(&map_b);
+  }
+  if (warp == 1) tmem_alloc<false>(&tmem_slot, C::kTmemCols);
   pdl_wait();
   pdl_launch_dependents();
-  const int e = blockIdx.z, c0 = blockIdx.x * kTile, i0 = blockIdx.y * kTile;
-  const int nb = (a.N + kBlock - 1) / kBlock, kb = (a.K + kBlock - 1) / kBlock;
-  const int cols = MODE == kForward ? a.N : a.K, inner = MODE == kForward ? a.K : a.N;
-  int lo = 0, hi = a.M, block0 = 0, padded0 = 0;
-  if (a.offsets) {
-    int end = 0;
-    for (int f = 0; f <= e && f < a.E; ++f) {
-      const int cap = MODE == kGrad ? 1 << 30 : a.M;
-      if (MODE == kGrad && f > 0) {
-        block0 += (hi - lo + kBlock - 1) / kBlock;
-        padded0 += (hi - lo + 31) & ~31;
+  if (warp == 0) {
+    // prefix sums over the experts; what follows the last one is in [E]
+    int tiles = 0, padded = 0, blocks = 0;
+    const int cap = MODE == kGrad ? 1 << 30 : a.M;
+    for (int e0 = 0; e0 < a.E; e0 += 32) {
+      const int e = e0 + lane;
+      int lo = 0, hi = 0;
+      if (e < a.E) {
+        lo = a.offsets ? max(0, min(a.offsets[e], cap)) : 0;
+        hi = a.offsets ? max(lo, min(a.offsets[e + 1], cap)) : a.M;
       }
-      lo = max(0, min(a.offsets[f], cap));
-      hi = max(lo, min(a.offsets[f + 1], cap));
-      end = max(end, hi);
-    }
-    if (e == a.E) lo = end, hi = a.M;  // rows behind the last
-  }
-  const bool zero = e == a.E;
-  int sums = inner, limit = hi - lo;
-  size_t out0 = lo;
-  if (MODE == kGrad) {
-    sums = hi - lo;
-    if (block0 + (sums + kBlock - 1) / kBlock > a.blocks || padded0 + sums > a.M) sums = 0;
-    limit = a.N;
-    out0 = (size_t)e * a.N;
-  }
-  if (zero) sums = 0;
-  if (i0 >= limit) return;
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float acc[4][4] = {};
-  for (int b = 0; b * kBlock < sums; ++b) {
-    float p[4][4] = {};
-    for (int k0 = b * kBlock; k0 < min(sums, (b + 1) * kBlock); k0 += kStep) {
-      __syncthreads();
-      for (int t = threadIdx.x; t < kStep * kTile; t += kThreads) {
-        float va = 0.f, vb = 0.f;
+      const int n = hi - lo;
+      int vt = (n + NT - 1) / NT, vp = (n + 31) & ~31, vb = (n + kBlock - 1) / kBlock;
+      const int t = vt, p = vp, b = vb;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int ut = __shfl_up_sync(0xffffffffu, vt, o), up = __shfl_up_sync(0xffffffffu, vp, o),
+                  ub = __shfl_up_sync(0xffffffffu, vb, o);
+        if (lane >= o) {
+          vt += ut;
+          vp += up;
+          vb += ub;
+        }
+      }
+      if (e < a.E) {
         if (MODE == kGrad) {
-          const int i = t % kTile, k = t / kTile;
-          const size_t r = padded0 + k0 + k;
-          if (k0 + k < sums && i0 + i < a.N) va = e4m3(a.a[r * a.N + i0 + i]);
-          if (k0 + k < sums && c0 + i < a.K) vb = e4m3(a.w[r * a.K + c0 + i]);
-          s_a[k][i] = va;
-          s_b[k][i] = vb;
+          // (offsets that are not those of the operands reach nothing outside of them)
+          const int k0 = padded + vp - p, b0 = blocks + vb - b;
+          const bool fits = k0 >= 0 && b0 >= 0 && (long long)k0 + p <= a.M && (long long)b0 + b <= a.blocks;
+          ex.row[e] = k0;
+          ex.end[e] = fits ? n : 0;
+          ex.tile0[e] = b0;
         } else {
-          const int k = t % kStep, i = t / kStep;
-          if (k0 + k < inner && i0 + i < limit)
-            va = e4m3(a.a[(out0 + i0 + i) * (size_t)inner + k0 + k]);
-          s_a[k][i] = va;
-          if (MODE == kForward) {
-            if (k0 + k < inner && c0 + i < cols)
-              vb = e4m3(a.w[((size_t)e * a.N + c0 + i) * a.K + k0 + k]);
-            s_b[k][i] = vb;
+          ex.row[e] = lo;
+          ex.end[e] = hi;
+          ex.tile0[e] = tiles + vt - t;
+        }
+      }
+      tiles += __shfl_sync(0xffffffffu, vt, 31);
+      padded += __shfl_sync(0xffffffffu, vp, 31);
+      blocks += __shfl_sync(0xffffffffu, vb, 31);
+    }
+    if (lane == 0) ex.tile0[a.E] = tiles;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+
+  const int cols = MODE == kForward ? a.N : a.K, inner = MODE == kForward ? a.K : a.N;
+  const int col_tiles = (cols + kBlock - 1) / kBlock;
+  const int n_tiles = (a.N + NT - 1) / NT;  // kGrad
+  const long long units = (long long)(MODE == kGrad ? a.E * n_tiles : ex.tile0[a.E]) * col_tiles;
+  // Tiles in the order (expert, columns, rows): those that read the same part of a matrix follow each other.
+  auto tile_at = [&](long long u) {
+    Tile t;
+    if (MODE == kGrad) {
+      const int per = n_tiles * col_tiles;
+      t.e = (int)(u / per);
+      const int v = (int)(u - (long long)t.e * per);
+      const int h = ((a.N + n_tiles - 1) / n_tiles + 15) & ~15;
+      t.row0 = v % n_tiles * h;
+      t.rows = max(0, min(h, a.N - t.row0));
+      t.c0 = v / n_tiles * kBlock;
+      t.sums = ex.end[t.e];
+      t.k0 = ex.row[t.e];
+      t.b0 = ex.tile0[t.e];
+    } else {
+      int lo = 0, hi = a.E;  // the last expert whose tiles begin at or before u
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((long long)ex.tile0[mid] * col_tiles <= u) lo = mid;
+        else hi = mid;
+      }
+      t.e = lo;
+      const int n = ex.end[lo] - ex.row[lo], count = ex.tile0[lo + 1] - ex.tile0[lo];
+      const int v = (int)(u - (long long)ex.tile0[lo] * col_tiles);
+      const int h = ((n + count - 1) / count + 15) & ~15;
+      const int i = v % count;
+      t.row0 = ex.row[lo] + i * h;
+      t.rows = min(h, n - i * h);
+      t.c0 = v / count * kBlock;
+      t.sums = inner;
+      t.k0 = t.b0 = 0;
+    }
+    t.nkb = (t.sums + kBlock - 1) / kBlock;
+    return t;
+  };
+
+  if (warp == 0) {
+    if (elect_one()) {
+      int stage = 0;
+      uint32_t phase = 0;
+      long long issued = 0;
+      bool ok = true;
+      for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Tile t = tile_at(u);
+        for (int kb = 0; kb < t.nkb; ++kb) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, wc, 1u)) {
+            ok = false;
+            break;
+          }
+          uint8_t* const sa = smem + stage * C::kStage;
+          uint8_t* const sb = sa + kOperand;
+          uint64_t* const bar = &full[stage];
+          if (MODE == kGrad) {
+            const int k = t.k0 + kb * kBlock, boxes = (min(kBlock, t.sums - kb * kBlock) + 31) / 32;
+            const int chunks = (t.rows + kBlock - 1) / kBlock;
+            mbar_expect_tx(bar, (1 + chunks) * boxes * 32 * kBlock);
+            for (int i = 0; i < boxes; ++i) {
+              tma_load(sa + i * 32 * kBlock, &map_a, bar, t.c0, k + 32 * i);
+              for (int c = 0; c < chunks; ++c)
+                tma_load(sb + c * kOperand + i * 32 * kBlock, &map_b, bar, t.row0 + c * kBlock, k + 32 * i);
+            }
           } else {
-            const int j = t % kTile, kk = t / kTile;
-            if (k0 + kk < inner && c0 + j < cols)
-              vb = e4m3(a.w[((size_t)e * a.N + k0 + kk) * a.K + c0 + j]);
-            s_b[kk][j] = vb;
+            const int k = kb * kBlock, boxes = (t.rows + C::kBox - 1) / C::kBox;
+            mbar_expect_tx(bar, kOperand + boxes * C::kBox * kBlock);
+            if (MODE == kForward) tma_load_3d(sa, &map_a, bar, k, t.c0, t.e);
+            else tma_load_3d(sa, &map_a, bar, t.c0, k, t.e);
+            for (int i = 0; i < boxes; ++i)
+              tma_load(sb + i * C::kBox * kBlock, &map_b, bar, k, t.row0 + i * C::kBox);
+          }
+          ++issued;
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
           }
         }
       }
-      __syncthreads();
-      for (int k = 0; k < kStep; ++k)
-        for (int i = 0; i < 4; ++i)
-          for (int j = 0; j < 4; ++j) p[i][j] = fmaf(s_a[k][ty * 4 + i], s_b[k][tx * 4 + j], p[i][j]);
+      // copies in flight land before the CTA may exit
+      for (long long i = issued > S ? issued - S : 0; i < issued; ++i)
+        mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), wc, 2u, false);
     }
-    for (int i = 0; i < 4; ++i)
-      for (int j = 0; j < 4; ++j) {
-        const int row = i0 + ty * 4 + i, c = c0 + tx * 4 + j;
-        if (row >= limit || c >= cols) continue;
-        float s;
-        if (MODE == kGrad)
-          s = a.as[(size_t)(block0 + b) * a.N + row] * a.ws[(size_t)(block0 + b) * a.K + c];
-        else
-          s = a.as[(size_t)b * a.M + out0 + row] *
-              a.ws[((size_t)e * nb + (MODE == kForward ? c / kBlock : b)) * kb +
-                   (MODE == kForward ? b : c / kBlock)];
-        acc[i][j] = fmaf(p[i][j], s, acc[i][j]);
+  } else if (warp == 1) {
+    if (elect_one()) {
+      int stage = 0, buf = 0;
+      uint32_t phase = 0, bphase = 0;
+      bool ok = true;
+      for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        const Tile t = tile_at(u);
+        const uint32_t id = idesc(true, kBlock, (t.rows + 15) & ~15, MODE != kForward, MODE == kGrad);
+        for (int kb = 0; kb < t.nkb; ++kb) {
+          if (!mbar_wait(&tempty[buf], bphase ^ 1u, wc, 4u) || !mbar_wait(&full[stage], phase, wc, 8u)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t sa = smem_u32(smem + stage * C::kStage);
+          const uint64_t da = MODE == kForward ? sdesc_k(sa) : sdesc_mn8(sa);
+          const uint64_t db = MODE == kGrad ? sdesc_mn8(sa + kOperand) : sdesc_k(sa + kOperand);
+          const uint32_t d = tmem_base + (uint32_t)(buf * NT);
+          const int steps = (min(kBlock, t.sums - kb * kBlock) + 31) / 32;
+          for (int k = 0; k < steps; ++k)
+            mma<false, true>(d, da + k * (MODE == kForward ? 2 : 256), db + k * (MODE == kGrad ? 256 : 2),
+                             id, k > 0);
+          mma_commit<false>(&empty[stage]);
+          mma_commit<false>(&tfull[buf]);
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1u;
+          }
+          if (++buf == B) {
+            buf = 0;
+            bphase ^= 1u;
+          }
+        }
       }
-  }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int row = i0 + ty * 4 + i, c = c0 + tx * 4 + j;
-      if (row < limit && c < cols) ((T*)a.out)[(out0 + row) * cols + c] = Elem<T>::put(acc[i][j]);
+      mma_commit<false>(&mma_done);  // no MMA may run when TMEM is freed
     }
+    if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+  } else if (warp == 2) {
+    // The rows behind the last expert's, in pieces of 512 bytes of which every CTA takes its share.
+    uint4* zero = nullptr;
+    long long pieces = 0, piece = blockIdx.x;
+    if (MODE != kGrad && a.offsets) {
+      int end = 0;
+      for (int e = lane; e < a.E; e += 32) end = max(end, ex.end[e]);
+      end = (int)__reduce_max_sync(0xffffffffu, (unsigned)end);
+      Out* const first = (Out*)a.out + (size_t)end * cols;
+      Out* const last = (Out*)a.out + (size_t)a.M * cols;
+      zero = (uint4*)(((uintptr_t)first + 15) & ~(uintptr_t)15);
+      uint4* const stop = (uint4*)((uintptr_t)last & ~(uintptr_t)15);
+      pieces = stop > zero ? ((long long)(stop - zero) + 31) / 32 : 0;
+      if (blockIdx.x == 0) {  // what lies before and behind whole vectors
+        const long long n = last - first, head = min(n, (long long)((Out*)zero - first));
+        if (lane < head) first[lane] = Elem<Out>::put(0.f);
+        const long long tail = stop >= zero ? last - (Out*)stop : 0;
+        if (lane < tail) last[-1 - lane] = Elem<Out>::put(0.f);
+      }
+      zero += lane;
+      if (pieces > 0 && zero + (pieces - 1) * 32 >= stop) --pieces;  // this lane has none in the last
+    }
+    auto clear = [&](int n) {
+      for (; n > 0 && piece < pieces; --n, piece += gridDim.x) zero[piece * 32] = make_uint4(0, 0, 0, 0);
+    };
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Tile t = tile_at(u);
+      const int nb = (a.N + kBlock - 1) / kBlock, kbs = (a.K + kBlock - 1) / kBlock;
+      for (int kb = 0; kb < t.nkb; ++kb) {
+        if (!warp_wait(&sempty[slot], phase ^ 1u, wc, 64u)) {
+          ok = false;
+          break;
+        }
+        const uint32_t dst = smem_u32(s_scale + slot * C::kSlotFloats);
+        const float* rs = MODE == kGrad ? a.xs + (size_t)(t.b0 + kb) * a.N : a.xs + (size_t)kb * a.M;
+        for (int i = lane; i < t.rows; i += 32) cp_async4(dst + i * 4, rs + t.row0 + i);
+        if (MODE == kGrad) {
+          const float* cs = a.ws + (size_t)(t.b0 + kb) * a.K;
+#pragma unroll
+          for (int i = 0; i < kBlock; i += 32)
+            cp_async4(dst + (NT + i + lane) * 4, cs + min(t.c0 + i + lane, a.K - 1));
+        } else if (lane == 0) {
+          const size_t at = MODE == kForward ? ((size_t)t.e * nb + t.c0 / kBlock) * kbs + kb
+                                             : ((size_t)t.e * nb + kb) * kbs + t.c0 / kBlock;
+          cp_async4(dst + NT * 4, a.ws + at);
+        }
+        cp_async_arrive(&sfull[slot]);
+        clear(8);
+        if (++slot == kSlots) {
+          slot = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    clear(1 << 30);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else {
+    const int q = warp & 3, ch = (warp - kFirstEpi) >> 2;  // quarter of the columns, half of the rows
+    const uint32_t tq = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(ch * C::kCols);
+    uint4* const box = (uint4*)(s_out + (warp - kFirstEpi) * 32 * 64);
+    int slot = 0, buf = 0;
+    uint32_t sphase = 0, bphase = 0;
+    bool ok = true;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+      const Tile t = tile_at(u);
+      // acc[g][2 h + p]: rows 8 g + 2 (lane % 4), + 1, column 16 h + 8 p + lane / 4 of the warp's
+      uint64_t acc[C::kCols / 8][4];
+#pragma unroll
+      for (int g = 0; g < C::kCols / 8; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[g][i] = 0;
+      const int live = t.rows - ch * C::kCols;  // rows of this warp
+      for (int kb = 0; ok && kb < t.nkb; ++kb) {
+        if (!warp_wait(&sfull[slot], sphase, wc, 32u) || !warp_wait(&tfull[buf], bphase, wc, 32u)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const float* const sc = s_scale + slot * C::kSlotFloats;
+        float f[4];  // of the thread's columns
+        if (MODE == kGrad) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] = sc[NT + 32 * q + 8 * i + (lane >> 2)];
+        } else {
+          f[0] = sc[NT];
+        }
+#pragma unroll
+        for (int c0 = 0; c0 < C::kCols; c0 += C::kChunk) {
+          if (c0 >= live) break;
+          uint32_t w[2][C::kChunk / 2];
+          __syncwarp();
+          tmem_ld_pairs(tq + (uint32_t)(buf * NT + c0), w[0]);
+          tmem_ld_pairs(tq + (uint32_t)(buf * NT + c0) + (16u << 16), w[1]);
+          uint64_t s[C::kChunk / 8];
+#pragma unroll
+          for (int g = 0; g < C::kChunk / 8; ++g) {
+            s[g] = *(const uint64_t*)(sc + ch * C::kCols + c0 + 8 * g + 2 * (lane & 3));
+            if (MODE != kGrad) s[g] = mul2(s[g], f[0]);
+          }
+          tmem_wait_ld();
+#pragma unroll
+          for (int g = 0; g < C::kChunk / 8; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint64_t p = pair(w[i >> 1][4 * g + 2 * (i & 1)], w[i >> 1][4 * g + 2 * (i & 1) + 1]);
+              uint64_t& d = acc[c0 / 8 + g][i];
+              d = fma2(p, MODE == kGrad ? mul2(s[g], f[i]) : s[g], d);
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&tempty[buf]);
+          mbar_arrive(&sempty[slot]);
+        }
+        if (++slot == kSlots) {
+          slot = 0;
+          sphase ^= 1u;
+        }
+        if (++buf == B) {
+          buf = 0;
+          bphase ^= 1u;
+        }
+      }
+      if (!ok) {
+#pragma unroll
+        for (int g = 0; g < C::kCols / 8; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[g][i] = pair(0x7fc00000u, 0x7fc00000u);
+      }
+      // out[row][column]: rows of 32 columns of this warp
+      const size_t row0 = (MODE == kGrad ? (size_t)t.e * a.N : 0) + t.row0 + ch * C::kCols;
+      const int col = t.c0 + 32 * q;
+      Out* const out = (Out*)a.out + row0 * cols + col;
+      if (sizeof(Out) == 4) {
+        // eight lanes with the same lane % 4 store a sector of a row
+#pragma unroll
+        for (int g = 0; g < C::kCols / 8; ++g)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 v = floats(acc[g][i]);
+            const int r = 8 * g + 2 * (lane & 3), c = 8 * i + (lane >> 2);
+            if (col + c < cols) {
+              if (r < live) out[(size_t)r * cols + c] = Elem<Out>::put(v.x);
+              if (r + 1 < live) out[(size_t)(r + 1) * cols + c] = Elem<Out>::put(v.y);
+            }
+          }
+      } else {
+        // 32 rows at a time through shared memory, whose pieces of 16 bytes are exchanged by row
+        constexpr int kRows = C::kChunk;
+#pragma unroll
+        for (int r0 = 0; r0 < C::kCols; r0 += kRows) {
+          if (r0 >= live) break;
+          __syncwarp();
+#pragma unroll
+          for (int g = 0; g < kRows / 8; ++g) {
+            const int r = 8 * g + (lane & 7), piece = lane >> 3;
+            const uint64_t(&v)[4] = acc[r0 / 8 + g];
+            stmatrix_t(smem_u32(box + r * 4 + (piece ^ ((r >> 1) & 3))), bf16x2(v[0]), bf16x2(v[1]),
+                       bf16x2(v[2]), bf16x2(v[3]));
+          }
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < kRows / 8; ++k) {
+            const int r = 8 * k + (lane >> 2), piece = lane & 3, c = 8 * piece;
+            const uint4 v = box[r * 4 + (piece ^ ((r >> 1) & 3))];
+            if (r0 + r >= live || col + c >= cols) continue;
+            Out* const p = out + (size_t)(r0 + r) * cols + c;
+            if (a.vec && col + c + 8 <= cols) {
+              *(uint4*)p = v;
+            } else {
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (col + c + j < cols) ((uint16_t*)p)[j] = (uint16_t)(w[j / 2] >> 16 * (j & 1));
+            }
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc<false>(tmem_base, C::kTmemCols);
+}
+
+// -------------------------------------------------------------------------------- host side
+template <int MODE, int NT>
+cudaError_t run_nt(const CUtensorMap& ma, const CUtensorMap& mb, const Args& a, int out_dtype, int ctas,
+                   cudaStream_t st) {
+  auto go = [&](auto* kernel) {
+    // (the kernel's own limit, whatever the call: it cannot be lowered between this and the launch)
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<NT>::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kernel, dim3(ctas), dim3(Cfg<NT>::kThreads), Cfg<NT>::kSmem, st, ma, mb, a);
+  };
+  return out_dtype == EAT_BF16 ? go(block_mm_kernel<MODE, NT, __nv_bfloat16>)
+                               : go(block_mm_kernel<MODE, NT, float>);
 }
 
 template <int MODE>
-cudaError_t run(const Args& a, int out_dtype, cudaStream_t st) {
-  const int cols = MODE == kForward ? a.N : a.K, rows = MODE == kGrad ? a.N : a.M;
-  const dim3 grid((cols + kTile - 1) / kTile, (rows + kTile - 1) / kTile,
-                  a.E + (MODE == kGrad || !a.offsets ? 0 : 1));
-  return launch_pdl(out_dtype == EAT_BF16 ? block_mm_kernel<MODE, __nv_bfloat16>
-                                          : block_mm_kernel<MODE, float>,
-                    grid, dim3(kThreads), 0, st, a);
+eat_status run(const char* fn, const void* x, const void* w, const Args& a, int out_dtype,
+               cudaStream_t st) {
+  int device = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  if (e != cudaSuccess) return launched(fn, e);
+  // rows of a tile at most: what an expert has on average, with room
+  const int rows = MODE == kGrad ? a.N : (a.M + a.E - 1) / a.E;
+  int nt = rows <= 16 ? 32 : rows <= 32 ? 64 : rows <= 64 ? 128 : 256;
+  if (MODE == kGrad) nt = rows <= kBlock ? 128 : 256;  // (its operands come in columns of 128)
+  const int box = MODE == kGrad ? 32 : std::min(nt, 64);
+  CUtensorMap ma, mb;
+  bool ok;
+  if (MODE == kGrad)
+    ok = encode_bytes(&ma, 2, w, a.K, a.M, 1, box) && encode_bytes(&mb, 2, x, a.N, a.M, 1, box);
+  else
+    ok = encode_bytes(&ma, 3, w, a.K, a.N, a.E, kBlock) &&
+         encode_bytes(&mb, 2, x, MODE == kForward ? a.K : a.N, a.M, 1, box);
+  if (!ok) return thread_fail(EAT_ERR_CUDA, "%s: tensor map", fn);
+  const int cols = MODE == kForward ? a.N : a.K, col_tiles = (cols + kBlock - 1) / kBlock;
+  const long long tiles =
+      (MODE == kGrad ? (long long)a.E * ((a.N + nt - 1) / nt)
+                     : (long long)std::min((long long)a.M, (a.M + (long long)a.E * (nt - 1)) / nt)) *
+      col_tiles;
+  const int ctas = (int)std::min<long long>(sms, tiles);
+  if (nt == 256) e = run_nt<MODE, 256>(ma, mb, a, out_dtype, ctas, st);
+  else if (nt == 128) e = run_nt<MODE, 128>(ma, mb, a, out_dtype, ctas, st);
+  else if constexpr (MODE != kGrad)
+    e = nt == 64 ? run_nt<MODE, 64>(ma, mb, a, out_dtype, ctas, st)
+                 : run_nt<MODE, 32>(ma, mb, a, out_dtype, ctas, st);
+  return launched(fn, e);
 }
 
 const char* bad_shape(int32_t E, int32_t M, int32_t N, int32_t K, const void* offsets,
@@ -159,9 +619,10 @@ extern "C" eat_status eat_block_mm(const void* xq, const float* xs, const void* 
   if (misaligned(xq, 16) || misaligned(wq, 16) || misaligned(xs, 4) || misaligned(ws, 4) ||
       misaligned(offsets, 4) || misaligned(y, ydtype == EAT_BF16 ? 2 : 4))
     return bad_arg(fn, "misaligned pointer");
-  const Args a{(const uint8_t*)xq, (const uint8_t*)wq, xs, ws, offsets, E, M, N, K, 0, y};
+  const int vec = !misaligned(y, 16) && (transposed ? K : N) % 8 == 0;
+  const Args a{xs, ws, offsets, E, M, N, K, 0, y, vec};
   const cudaStream_t st = (cudaStream_t)stream;
-  return launched(fn, transposed ? run<kBack>(a, ydtype, st) : run<kForward>(a, ydtype, st));
+  return transposed ? run<kBack>(fn, xq, wq, a, ydtype, st) : run<kForward>(fn, xq, wq, a, ydtype, st);
 }
 
 extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq,
@@ -177,6 +638,6 @@ extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const v
   if (misaligned(gq, 16) || misaligned(xq, 16) || misaligned(gs, 4) || misaligned(xs, 4) ||
       misaligned(offsets, 4) || misaligned(dw, dtype == EAT_BF16 ? 2 : 4))
     return bad_arg(fn, "misaligned pointer");
-  const Args a{(const uint8_t*)gq, (const uint8_t*)xq, gs, xs, offsets, E, rows, N, K, blocks, dw};
-  return launched(fn, run<kGrad>(a, dtype, (cudaStream_t)stream));
+  const Args a{gs, xs, offsets, E, rows, N, K, blocks, dw, !misaligned(dw, 16)};
+  return run<kGrad>(fn, gq, xq, a, dtype, (cudaStream_t)stream);
 }

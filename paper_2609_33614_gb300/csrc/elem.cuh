@@ -83,24 +83,36 @@ __device__ __forceinline__ void store_elems(T* p, int left, const float* v) {
 // leaves the others as they are.
 constexpr int kBlock = 128;  // elements of a block along its axis
 
-__device__ __forceinline__ float block_scale(float top) { return top > kTiny ? top / 448.0f : 1.0f; }
-// What a block's values are multiplied by (within 2^-23 of the quotient by the scale; a multiplication
-// where a division would cost ten instructions an element).
-__device__ __forceinline__ float block_factor(float top) {
-  return top > kTiny ? 1.0f / (top / 448.0f) : 0.0f;
+// (within 2^-23 of the quotient)
+__device__ __forceinline__ float block_scale(float top) {
+  return top > kTiny ? top * (1.0f / 448.0f) : 1.0f;
 }
+// What a block's values are divided by: its scale, and the scale's rounded reciprocal.  With both, a
+// product and two fused steps give the rounded quotient (Markstein, IBM J. R&D 34, 1990), where a
+// division would cost ten instructions an element, and a product alone would take values that lie between
+// two e4m3 values, which quotients of bf16 values often do, to the wrong side.
+struct BlockDiv {
+  float scale, recip;
+  __device__ __forceinline__ explicit BlockDiv(float top)
+      : scale(block_scale(top)), recip(top > kTiny ? 1.0f / scale : 0.0f) {}
+  __device__ __forceinline__ BlockDiv(float s, float r) : scale(s), recip(r) {}
+  __device__ __forceinline__ float operator()(float v) const {
+    const float t = v * recip;
+    return fmaf(fmaf(-t, scale, v), recip, t);
+  }
+};
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ uint32_t e4m3x4(const float* v, float f) {
-  return e4m3x2(v[0] * f, v[1] * f) | e4m3x2(v[2] * f, v[3] * f) << 16;
+__device__ __forceinline__ uint32_t e4m3x4(const float* v) {
+  return e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
 }
-// N = 4 or 8 bytes of a row.
+// N = 4 or 8 bytes of a row, of quotients.
 template <int N, bool VEC>
-__device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v, float f) {
+__device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v) {
   uint32_t w[N / 4];
 #pragma unroll
-  for (int j = 0; j < N / 4; ++j) w[j] = e4m3x4(v + 4 * j, f);
+  for (int j = 0; j < N / 4; ++j) w[j] = e4m3x4(v + 4 * j);
   if (VEC) {
     if (N == 8) *(uint2*)p = make_uint2(w[0], w[N / 4 - 1]);
     else *(uint32_t*)p = w[0];
@@ -109,6 +121,13 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v,
     for (int j = 0; j < N; ++j)
       if (j < left) p[j] = (uint8_t)(w[j / 4] >> 8 * (j % 4));
   }
+}
+template <int N, bool VEC>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v, const BlockDiv& div) {
+  float t[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) t[j] = div(v[j]);
+  store_e4m3<N, VEC>(p, left, t);
 }
 // The largest magnitude over groups of G lanes, in all of them.
 template <int G>

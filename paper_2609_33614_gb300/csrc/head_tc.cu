@@ -28,6 +28,7 @@
 #include <mutex>
 
 #include "tc_ptx.cuh"
+#include "tensor_map.cuh"
 
 namespace eat {
 
@@ -1046,6 +1047,19 @@ cudaError_t head_configure(int num_sms, int* max_pairs) {
   if (e == cudaSuccess) e = configure_pair<kExp, false>(num_sms, max_pairs);
   if (e == cudaSuccess) e = configure_pair<kGrad, false>(num_sms, max_pairs);
   return e;
+}
+
+bool encode_bytes(CUtensorMap* m, int rank, const void* ptr, long long cols, long long rows,
+                  long long planes, int box_rows) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+  cuuint64_t strides[2] = {(cuuint64_t)cols, (cuuint64_t)cols * (cuuint64_t)rows};
+  cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void*>(ptr), dims, strides,
+            box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool head_encode(CUtensorMap* m, bool w8, const void* ptr, long long rows, long long cols,

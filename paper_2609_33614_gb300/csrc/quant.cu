@@ -70,9 +70,9 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
         }
       }
       top = group_max<G>(top);
-      if (r < M && left > 0)
-        store_e4m3<N, VEC>(q + (size_t)r * K + c, left, v[i], block_factor(top));
-      if (l == i0 + i) s = block_scale(top);
+      const BlockDiv div(top);
+      if (r < M && left > 0) store_e4m3<N, VEC>(q + (size_t)r * K + c, left, v[i], div);
+      if (l == i0 + i) s = div.scale;
     }
   }
   if (l < kRows && r0 + l < M) scale[(size_t)kb * M + r0 + l] = s;
@@ -128,7 +128,7 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
                      float* __restrict__ cscale) {
   constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kThreads;
   __shared__ float s_top[kWarps][kBlock];
-  __shared__ float s_factor[kBlock];
+  __shared__ float s_scale[kBlock], s_recip[kBlock];
   pdl_wait();
   pdl_launch_dependents();
   const int b = blockIdx.x;
@@ -146,7 +146,7 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
         for (int k = 0; k < R; ++k) {
           const int row = rb.row + r + k;
           if (row >= M) break;
-          if (left > 0) store_e4m3<N, VEC>(q + (size_t)row * K + c, left, zero, 0.f);
+          if (left > 0) store_e4m3<N, VEC>(q + (size_t)row * K + c, left, zero);
           if (l == 0) scale[(size_t)i * M + row] = 1.0f;
         }
       }
@@ -182,8 +182,9 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
         t = group_max<L>(t);
         if (r + k >= rb.n) continue;
         const size_t row = rb.row + r + k;
-        if (left > 0) store_e4m3<N, VEC>(q + row * K + c, left, v[k], block_factor(t));
-        if (l == 0) scale[(size_t)i * M + row] = block_scale(t);
+        const BlockDiv div(t);
+        if (left > 0) store_e4m3<N, VEC>(q + row * K + c, left, v[k], div);
+        if (l == 0) scale[(size_t)i * M + row] = div.scale;
       }
     }
     __syncthreads();
@@ -191,20 +192,25 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
       float t = 0.f;
 #pragma unroll
       for (int k = 0; k < kWarps; ++k) t = fmaxf(t, s_top[k][threadIdx.x]);
-      s_factor[threadIdx.x] = block_factor(t);
+      const BlockDiv div(t);
+      s_scale[threadIdx.x] = div.scale;
+      s_recip[threadIdx.x] = div.recip;
       const int col = i * kBlock + threadIdx.x;
-      if (col < K) cscale[(size_t)b * K + col] = block_scale(t);
+      if (col < K) cscale[(size_t)b * K + col] = div.scale;
     }
     __syncthreads();
-    float f[N];
+    float fs[N], fr[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) f[j] = s_factor[l * N + j];
+    for (int j = 0; j < N; ++j) {
+      fs[j] = s_scale[l * N + j];
+      fr[j] = s_recip[l * N + j];
+    }
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       if (r + k >= out_rows || left <= 0) continue;
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[k][j] *= f[j];
-      store_e4m3<N, VEC>(cq + (size_t)(rb.padded + r + k) * K + c, left, v[k], 1.0f);
+      for (int j = 0; j < N; ++j) v[k][j] = BlockDiv(fs[j], fr[j])(v[k][j]);
+      store_e4m3<N, VEC>(cq + (size_t)(rb.padded + r + k) * K + c, left, v[k]);
     }
   }
 }
@@ -243,12 +249,12 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kWarps; ++k) top = fmaxf(top, s_top[k]);
-  if (threadIdx.x == 0) scale[(e * n_blocks + nb) * blocks + kb] = block_scale(top);
-  const float f = block_factor(top);
+  const BlockDiv div(top);
+  if (threadIdx.x == 0) scale[(e * n_blocks + nb) * blocks + kb] = div.scale;
 #pragma unroll
   for (int k = 0; k < R; ++k)
     if (row0 + k < n_rows && left > 0)
-      store_e4m3<N, VEC>(q + at + (size_t)(row0 + k) * K + c, left, v[k], f);
+      store_e4m3<N, VEC>(q + at + (size_t)(row0 + k) * K + c, left, v[k], div);
 }
 
 // ----------------------------------------------------------------------------------- swiglu

@@ -190,7 +190,7 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
   if (t >= tokens) return;
   const int M = tokens * K, used = rows_used(offsets, E, M);
   const int mine = lane < K ? slot[(size_t)t * K + lane] : -1;
-  float v[U][N], f[U], s[U];
+  float v[U][N], s[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const int c = c0 + 32 * N * i;
@@ -200,8 +200,10 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[i][j]));
     top = group_max<G>(top);
-    f[i] = block_factor(top);
-    s[i] = block_scale(top);
+    const BlockDiv div(top);
+    s[i] = div.scale;
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[i][j] = div(v[i][j]);
   }
   for (int k = 0; k < K; ++k) {
     const int r = __shfl_sync(0xffffffffu, mine, k);
@@ -210,7 +212,7 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
     for (int i = 0; i < U; ++i) {
       const int c = c0 + 32 * N * i;
       if (c >= d) continue;
-      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, v[i], f[i]);
+      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, v[i]);
       if (lane % G == 0) scale[(size_t)(c / kBlock) * M + r] = s[i];
     }
   }
@@ -220,7 +222,7 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
     for (int i = 0; i < U; ++i) {
       const int c = c0 + 32 * N * i;
       if (c >= d) continue;
-      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, zero, 0.f);
+      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, zero);
       if (lane % G == 0) scale[(size_t)(c / kBlock) * M + r] = 1.0f;
     }
   }

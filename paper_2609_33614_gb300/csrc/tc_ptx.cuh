@@ -1,4 +1,4 @@
-// PTX wrappers of the vocabulary head's tensor-core kernels: mbarriers with bounded waits, TMA loads,
+// PTX wrappers of the head's and the block-scaled products' tensor-core kernels: mbarriers with bounded waits, TMA loads,
 // TMEM, tcgen05.mma on one SM and on SM pairs, and their shared-memory and instruction descriptors.
 #pragma once
 
@@ -53,7 +53,7 @@ struct WaitCtx {
 // Bounded wait on the phase with the given parity; false when it gave up: because another role
 // raised the abort flag (check_abort), or after kWaitLimitNs (then it raises the flag itself and
 // records `code`).  The first polls are inlined; only a longer wait pays for the call and the clock.
-__device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, WaitCtx c,
+static __device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, WaitCtx c,
                                             unsigned int code, bool check_abort) {
   unsigned long long t0, t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));

@@ -182,7 +182,7 @@ def _blocked(v, dim):
 
 
 def _check_bytes(q, v, scale):
-    """q are the e4m3 values of v / scale, rounded (the factor 1 / scale is off by 2^-23)."""
+    """q are the e4m3 values of v / scale, rounded (the quotient is rounded to fp32 first)."""
     t = v / scale
     step = torch.maximum(t.abs() * 2.0 ** -4, torch.full_like(t, 2.0 ** -10))
     assert ((q.double() - t).abs() <= step + 4 * U32 * t.abs()).all()
@@ -216,6 +216,18 @@ def _values(seed, M, K, dtype):
 def test_quant_rows(M, K, off, dtype):
     x = _offset(_values(12, M, K, dtype), off)
     _check_rows(x, *eat.quant_rows(x))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_quotients_are_rounded_once(dtype):
+    """Values half way between two e4m3 values, which bf16 quotients often are, go where the fp32 quotient
+    goes."""
+    x = _offset(_randn(17, 512, 2048).to(dtype), 0)
+    q, scale = eat.quant_rows(x)
+    s = _blocked(x.double(), 1).abs().amax(2) / 448.0
+    assert ((scale.t() - s).abs() <= 2 * U32 * s).all()
+    want = (x.float() / scale.t().repeat_interleave(128, 1)).to(E4M3)
+    assert torch.equal(q.view(torch.uint8), want.view(torch.uint8))
 
 
 def test_quant_rows_special():
