@@ -42,24 +42,28 @@ struct Args {
 };
 
 constexpr int kOperand = kBlock * kBlock;  // bytes of 128 rows of a k-block
-constexpr int kSlots = 6;                  // of the ring of scales
-constexpr int kFirstEpi = 3;               // warps before the epilogue's
+constexpr int kAhead = 4;                  // k-blocks whose scales are on their way
+constexpr int kFirstEpi = 4;               // warps before the epilogue's
 
 template <int NT>
 struct Cfg {
   static constexpr int kEpiWarps = NT >= 64 ? 8 : 4;
   static constexpr int kCols = NT >= 64 ? NT / 2 : NT;  // of the accumulator, for a warp
-  static constexpr int kChunk = kCols < 32 ? kCols : 32;  // of them at a time
+  static constexpr int kChunks = kCols / 16;  // of 16, which the warp reads at a time
   static constexpr int kThreads = 32 * (kFirstEpi + kEpiWarps);
   static constexpr int kBufs = NT == 256 ? 2 : NT == 128 ? 4 : 8;  // accumulators
   static constexpr int kTmemCols = NT * kBufs;
   static constexpr int kStage = kOperand + NT * kBlock;
   static constexpr int kStages = NT == 256 ? 4 : NT == 128 ? 6 : NT == 64 ? 8 : 10;
   static constexpr int kBox = NT < 64 ? NT : 64;  // rows of x that a copy takes
+  static constexpr int kSlots = kAhead + kBufs;  // of the ring of scales
   static constexpr int kSlotFloats = NT + kBlock;
   static constexpr int kOut = kEpiWarps * 32 * 64;  // 32 rows of 64 bytes per warp
   static constexpr int kSmem =
       1024 + kStages * kStage + kOut + kSlots * kSlotFloats * 4;
+  // Registers of the first four warps and of the epilogue's once they are shared out (NT = 256: 168 a thread
+  // at launch, 384 (168) = 128 (88) + 256 (208)); 0: as launched.
+  static constexpr int kFewRegs = NT == 256 ? 88 : 0, kManyRegs = NT == 256 ? 208 : 0;
 };
 
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0,
@@ -70,15 +74,13 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, u
       "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
-// 16 lanes x 8 G columns: registers 4 g .. 4 g + 3 of lane l hold columns 8 g + 2 (l % 4), + 1 of lane
+// 16 lanes x 16 columns: registers 4 g .. 4 g + 3 of lane l hold columns 8 g + 2 (l % 4), + 1 of lane
 // l / 4, and the same columns of lane l / 4 + 8.
-__device__ __forceinline__ void tmem_ld_pairs(uint32_t taddr, uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_ld_pairs(uint32_t taddr, uint32_t (&r)[8]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "
-      "%12, %13, %14, %15}, [%16];"
+      "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15])
+        "=r"(r[7])
       : "r"(taddr));
 }
 // MN-major e4m3, 128-byte swizzle: a row of 128 bytes holds 128 consecutive M (or N) elements of one k;
@@ -90,9 +92,6 @@ __device__ __forceinline__ uint64_t sdesc_mn8(uint32_t saddr) {
 }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
 // Pairs of floats
@@ -152,7 +151,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* const s_out = smem + S * C::kStage;
   float* const s_scale = (float*)(s_out + C::kOut);
-  __shared__ uint64_t full[S], empty[S], tfull[B], tempty[B], sfull[kSlots], sempty[kSlots], mma_done;
+  __shared__ uint64_t full[S], empty[S], tfull[B], tempty[B], mma_done;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   __shared__ unsigned int err_word;
@@ -167,12 +166,8 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       mbar_init(&empty[s], 1);
     }
     for (int b = 0; b < B; ++b) {
-      mbar_init(&tfull[b], 1);
+      mbar_init(&tfull[b], 2);  // the products and the scales
       mbar_init(&tempty[b], C::kEpiWarps);
-    }
-    for (int s = 0; s < kSlots; ++s) {
-      mbar_init(&sfull[s], 32);
-      mbar_init(&sempty[s], C::kEpiWarps);
     }
     mbar_init(&mma_done, 1);
     abort_word = 0;
@@ -273,6 +268,9 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     return t;
   };
 
+  if (warp < kFirstEpi) {
+  if constexpr (C::kFewRegs > 0)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kFewRegs));
   if (warp == 0) {
     if (elect_one()) {
       int stage = 0;
@@ -379,46 +377,71 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     auto clear = [&](int n) {
       for (; n > 0 && piece < pieces; --n, piece += gridDim.x) zero[piece * 32] = make_uint4(0, 0, 0, 0);
     };
-    int slot = 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Tile t = tile_at(u);
-      const int nb = (a.N + kBlock - 1) / kBlock, kbs = (a.K + kBlock - 1) / kBlock;
-      for (int kb = 0; kb < t.nkb; ++kb) {
-        if (!warp_wait(&sempty[slot], phase ^ 1u, wc, 64u)) {
-          ok = false;
-          break;
+    // The copies of k-block i are issued kAhead before those of i - kAhead are handed over, which is once
+    // the accumulator that goes with them is free: then so is the slot that comes kBufs before it.
+    long long u = blockIdx.x;
+    Tile t{};
+    int kb = 0, copy = 0, buf = 0;
+    uint32_t bphase = 0;
+    auto next = [&] {  // the tile of the next k-block to copy; false behind the last
+      while (kb == t.nkb) {
+        if (u >= units) return false;
+        t = tile_at(u);
+        u += gridDim.x;
+        kb = 0;
+      }
+      return true;
+    };
+    const int nb = (a.N + kBlock - 1) / kBlock, kbs = (a.K + kBlock - 1) / kBlock;
+    int pending = 0;
+    for (int i = 0;; ++i) {
+      if (i >= kAhead) {
+        if (pending == 0) break;
+        cp_async_wait<kAhead - 1>();
+        __syncwarp();
+        if (!warp_wait(&tempty[buf], bphase ^ 1u, wc, 64u)) break;
+        if (lane == 0) mbar_arrive(&tfull[buf]);
+        --pending;
+        if (++buf == B) {
+          buf = 0;
+          bphase ^= 1u;
         }
-        const uint32_t dst = smem_u32(s_scale + slot * C::kSlotFloats);
-        const float* rs = MODE == kGrad ? a.xs + (size_t)(t.b0 + kb) * a.N : a.xs + (size_t)kb * a.M;
-        for (int i = lane; i < t.rows; i += 32) cp_async4(dst + i * 4, rs + t.row0 + i);
+      }
+      if (next()) {
+        const uint32_t dst = smem_u32(s_scale + copy * C::kSlotFloats);
+        const float* rs =
+            (MODE == kGrad ? a.xs + (size_t)(t.b0 + kb) * a.N : a.xs + (size_t)kb * a.M) + t.row0;
+#pragma unroll
+        for (int j = 0; j < NT; j += 32)
+          if (j + lane < t.rows) cp_async4(dst + (j + lane) * 4, rs + j + lane);
         if (MODE == kGrad) {
           const float* cs = a.ws + (size_t)(t.b0 + kb) * a.K;
 #pragma unroll
-          for (int i = 0; i < kBlock; i += 32)
-            cp_async4(dst + (NT + i + lane) * 4, cs + min(t.c0 + i + lane, a.K - 1));
+          for (int j = 0; j < kBlock; j += 32)
+            cp_async4(dst + (NT + j + lane) * 4, cs + min(t.c0 + j + lane, a.K - 1));
         } else if (lane == 0) {
           const size_t at = MODE == kForward ? ((size_t)t.e * nb + t.c0 / kBlock) * kbs + kb
                                              : ((size_t)t.e * nb + kb) * kbs + t.c0 / kBlock;
           cp_async4(dst + NT * 4, a.ws + at);
         }
-        cp_async_arrive(&sfull[slot]);
-        clear(8);
-        if (++slot == kSlots) {
-          slot = 0;
-          phase ^= 1u;
-        }
+        ++kb;
+        ++pending;
+        if (++copy == C::kSlots) copy = 0;
       }
+      cp_async_commit();  // (one group an iteration, whether it holds a copy or not)
+      clear(8);
     }
     clear(1 << 30);
     asm volatile("cp.async.wait_all;" ::: "memory");
+  }
   } else {
+    if constexpr (C::kManyRegs > 0)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kManyRegs));
     const int q = warp & 3, ch = (warp - kFirstEpi) >> 2;  // quarter of the columns, half of the rows
     const uint32_t tq = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(ch * C::kCols);
     uint4* const box = (uint4*)(s_out + (warp - kFirstEpi) * 32 * 64);
     int slot = 0, buf = 0;
-    uint32_t sphase = 0, bphase = 0;
+    uint32_t bphase = 0;
     bool ok = true;
     for (long long u = blockIdx.x; u < units; u += gridDim.x) {
       const Tile t = tile_at(u);
@@ -430,12 +453,13 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         for (int i = 0; i < 4; ++i) acc[g][i] = 0;
       const int live = t.rows - ch * C::kCols;  // rows of this warp
       for (int kb = 0; ok && kb < t.nkb; ++kb) {
-        if (!warp_wait(&sfull[slot], sphase, wc, 32u) || !warp_wait(&tfull[buf], bphase, wc, 32u)) {
+        if (!__all_sync(0xffffffffu, mbar_wait_inline(&tfull[buf], bphase, wc, 32u))) {
           ok = false;
           break;
         }
         tc_fence_after();
         const float* const sc = s_scale + slot * C::kSlotFloats;
+        const uint32_t tb = tq + (uint32_t)(buf * NT);
         float f[4];  // of the thread's columns
         if (MODE == kGrad) {
 #pragma unroll
@@ -443,39 +467,38 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         } else {
           f[0] = sc[NT];
         }
+        // a chunk's loads run while the one before it is added
+        uint32_t w[2][2][8];
+        tmem_ld_pairs(tb, w[0][0]);
+        tmem_ld_pairs(tb + (16u << 16), w[0][1]);
 #pragma unroll
-        for (int c0 = 0; c0 < C::kCols; c0 += C::kChunk) {
-          if (c0 >= live) break;
-          uint32_t w[2][C::kChunk / 2];
-          __syncwarp();
-          tmem_ld_pairs(tq + (uint32_t)(buf * NT + c0), w[0]);
-          tmem_ld_pairs(tq + (uint32_t)(buf * NT + c0) + (16u << 16), w[1]);
-          uint64_t s[C::kChunk / 8];
+        for (int c = 0; c < C::kChunks; ++c) {
+          uint64_t s[2];
 #pragma unroll
-          for (int g = 0; g < C::kChunk / 8; ++g) {
-            s[g] = *(const uint64_t*)(sc + ch * C::kCols + c0 + 8 * g + 2 * (lane & 3));
+          for (int g = 0; g < 2; ++g) {
+            s[g] = *(const uint64_t*)(sc + ch * C::kCols + 16 * c + 8 * g + 2 * (lane & 3));
             if (MODE != kGrad) s[g] = mul2(s[g], f[0]);
           }
           tmem_wait_ld();
+          if (c + 1 < C::kChunks) {
+            tmem_ld_pairs(tb + (uint32_t)(16 * (c + 1)), w[(c + 1) & 1][0]);
+            tmem_ld_pairs(tb + (uint32_t)(16 * (c + 1)) + (16u << 16), w[(c + 1) & 1][1]);
+          }
 #pragma unroll
-          for (int g = 0; g < C::kChunk / 8; ++g)
+          for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint64_t p = pair(w[i >> 1][4 * g + 2 * (i & 1)], w[i >> 1][4 * g + 2 * (i & 1) + 1]);
-              uint64_t& d = acc[c0 / 8 + g][i];
-              d = fma2(p, MODE == kGrad ? mul2(s[g], f[i]) : s[g], d);
+              const uint32_t* const v = &w[c & 1][i >> 1][4 * g + 2 * (i & 1)];
+              uint64_t& d = acc[2 * c + g][i];
+              d = fma2(pair(v[0], v[1]), MODE == kGrad ? mul2(s[g], f[i]) : s[g], d);
             }
+          if (16 * (c + 1) >= live) break;
         }
+        tmem_wait_ld();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&tempty[buf]);
-          mbar_arrive(&sempty[slot]);
-        }
-        if (++slot == kSlots) {
-          slot = 0;
-          sphase ^= 1u;
-        }
+        if (lane == 0) mbar_arrive(&tempty[buf]);
+        if (++slot == C::kSlots) slot = 0;
         if (++buf == B) {
           buf = 0;
           bphase ^= 1u;
@@ -506,7 +529,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           }
       } else {
         // 32 rows at a time through shared memory, whose pieces of 16 bytes are exchanged by row
-        constexpr int kRows = C::kChunk;
+        constexpr int kRows = C::kCols < 32 ? C::kCols : 32;
 #pragma unroll
         for (int r0 = 0; r0 < C::kCols; r0 += kRows) {
           if (r0 >= live) break;

@@ -78,6 +78,32 @@ __device__ __forceinline__ void store_elems(T* p, int left, const float* v) {
   }
 }
 
+// N = kN elements of a row as they were loaded (a 16-byte vector, four registers, where rows begin at
+// vectors), and as floats when they are needed.
+template <typename T, bool VEC>
+struct RowVec {
+  static constexpr int kN = Elem<T>::kN;
+  uint4 u;
+  float f[VEC ? 1 : kN];
+  // the elements from p on, of which the first `left` exist; zeros if not live
+  __device__ __forceinline__ void load(const T* p, int left, bool live) {
+    if (VEC) {
+      u = live && left > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) f[VEC ? 0 : j] = live && j < left ? Elem<T>::get(p[j]) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void get(float* v) const {
+    if (VEC) {
+      Elem<T>::unpack(u, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) v[j] = f[VEC ? 0 : j];
+    }
+  }
+};
+
 // ---- e4m3 in blocks: a block's scale is its largest magnitude / 448, and a byte stands for scale times
 // its value.  A block that holds an infinity has an infinite scale, so all of it reads as NaN; a NaN
 // leaves the others as they are.
@@ -107,12 +133,9 @@ __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
 __device__ __forceinline__ uint32_t e4m3x4(const float* v) {
   return e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
 }
-// N = 4 or 8 bytes of a row, of quotients.
+// N = 4 or 8 bytes of a row.
 template <int N, bool VEC>
-__device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v) {
-  uint32_t w[N / 4];
-#pragma unroll
-  for (int j = 0; j < N / 4; ++j) w[j] = e4m3x4(v + 4 * j);
+__device__ __forceinline__ void store_bytes(uint8_t* p, int left, const uint32_t* w) {
   if (VEC) {
     if (N == 8) *(uint2*)p = make_uint2(w[0], w[N / 4 - 1]);
     else *(uint32_t*)p = w[0];
@@ -121,6 +144,14 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v)
     for (int j = 0; j < N; ++j)
       if (j < left) p[j] = (uint8_t)(w[j / 4] >> 8 * (j % 4));
   }
+}
+// The same of quotients.
+template <int N, bool VEC>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v) {
+  uint32_t w[N / 4];
+#pragma unroll
+  for (int j = 0; j < N / 4; ++j) w[j] = e4m3x4(v + 4 * j);
+  store_bytes<N, VEC>(p, left, w);
 }
 template <int N, bool VEC>
 __device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v, const BlockDiv& div) {

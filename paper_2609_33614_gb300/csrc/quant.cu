@@ -79,6 +79,8 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
 }
 
 // ---------------------------------------------------------------------------------- columns
+constexpr int kTilesOfBlock = 4;  // that a thread block takes of its rows: it finds them once
+
 // Block b of the experts' blocks of 128 rows: its rows in x, and where they go in the padded order.
 struct RowBlock {
   int row, n, padded;  // first row, number (0: none), first padded row
@@ -86,13 +88,22 @@ struct RowBlock {
 // By a full warp; the same in all lanes.  Offsets are held to [0, M].  Blocks past the experts' last
 // take the rows behind it: n is 0, and row the first of their 128 (M where there is none).
 __device__ RowBlock find_block(const int32_t* offsets, int E, int M, int b) {
+  constexpr int kRounds = kMaxExperts / 32;
   const int lane = threadIdx.x & 31;
+  int lo[kRounds], hi[kRounds];  // (one latency for all of them)
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    const int e = 32 * i + lane;
+    const bool in = e < E;
+    lo[i] = in && offsets ? offsets[e] : 0;
+    hi[i] = !in ? 0 : offsets ? offsets[e + 1] : M;
+  }
   int blocks = 0, padded = 0, end = 0;  // of the experts so far
-  for (int e0 = 0; e0 < E; e0 += 32) {
-    const int e = e0 + lane;
-    const int lo = e < E ? max(0, min(offsets ? offsets[e] : 0, M)) : 0;
-    const int hi = e < E ? max(lo, min(offsets ? offsets[e + 1] : M, M)) : 0;
-    const int c = (hi - lo + kBlock - 1) / kBlock, p = (hi - lo + 31) & ~31;
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    if (32 * i >= E) break;
+    const int l = max(0, min(lo[i], M)), h = 32 * i + lane < E ? max(l, min(hi[i], M)) : l;
+    const int c = (h - l + kBlock - 1) / kBlock, p = (h - l + 31) & ~31;
     int vc = c, vp = p;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -106,19 +117,18 @@ __device__ RowBlock find_block(const int32_t* offsets, int E, int M, int b) {
     const unsigned who = __ballot_sync(0xffffffffu, at >= 0 && at < c);
     if (who) {
       const int src = __ffs(who) - 1;
-      const RowBlock r{lo + at * kBlock, min(kBlock, hi - lo - at * kBlock),
-                       padded + vp - p + at * kBlock};
+      const RowBlock r{l + at * kBlock, min(kBlock, h - l - at * kBlock), padded + vp - p + at * kBlock};
       return RowBlock{__shfl_sync(0xffffffffu, r.row, src), __shfl_sync(0xffffffffu, r.n, src),
                       __shfl_sync(0xffffffffu, r.padded, src)};
     }
     blocks += __shfl_sync(0xffffffffu, vc, 31);
     padded += __shfl_sync(0xffffffffu, vp, 31);
-    end = max(end, (int)__reduce_max_sync(0xffffffffu, (unsigned)hi));
+    end = max(end, (int)__reduce_max_sync(0xffffffffu, (unsigned)h));
   }
   return RowBlock{(int)min((long long)M, end + (long long)(b - blocks) * kBlock), 0, 0};
 }
 
-// A tile of 128 rows and 128 columns at a time: thread (l, r) holds a vector of kSpan consecutive rows.
+// A tile of 128 rows and 128 columns at a time: thread (l, r) holds a vector of R consecutive rows.
 // ROWS: the rows' own blocks as well (q, scale), which the same tile holds whole.
 template <typename T, bool VEC, bool ROWS>
 __global__ void __launch_bounds__(kThreads)
@@ -152,40 +162,41 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
       }
     return;
   }
+  // (a tile's rows are kept as they were loaded, and the next tile's come while this one is taken)
+  RowVec<T, VEC> in[R];
+  auto load = [&](int i) {
+    const int c = i * kBlock + l * N;
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      in[k].load(x + (size_t)(rb.row + r + k) * K + c, K - c, r + k < rb.n && i < tiles);
+  };
+  load(blockIdx.y);
   for (int i = blockIdx.y; i < tiles; i += gridDim.y) {
     const int c = i * kBlock + l * N, left = K - c;
-    float v[R][N], top[N] = {};
+    float top[N] = {};
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (r + k < rb.n && left > 0) {
-        load_elems<T, N, VEC>(x + (size_t)(rb.row + r + k) * K + c, left, v[k]);
-      } else {
+      float v[N], t = 0.f;
+      in[k].get(v);
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[k][j] = 0.f;
+      for (int j = 0; j < N; ++j) {
+        top[j] = fmaxf(top[j], fabsf(v[j]));
+        t = fmaxf(t, fabsf(v[j]));
+      }
+      if (ROWS) {
+        const BlockDiv div(group_max<L>(t));
+        if (r + k >= rb.n) continue;
+        const size_t row = rb.row + r + k;
+        if (left > 0) store_e4m3<N, VEC>(q + row * K + c, left, v, div);
+        if (l == 0) scale[(size_t)i * M + row] = div.scale;
       }
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
 #pragma unroll
-      for (int k = 0; k < R; ++k) top[j] = fmaxf(top[j], fabsf(v[k][j]));
-#pragma unroll
       for (int o = 16; o >= L; o >>= 1)
         top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
       if (lane < L) s_top[warp][lane * N + j] = top[j];
-    }
-    if (ROWS) {
-#pragma unroll
-      for (int k = 0; k < R; ++k) {
-        float t = 0.f;
-#pragma unroll
-        for (int j = 0; j < N; ++j) t = fmaxf(t, fabsf(v[k][j]));
-        t = group_max<L>(t);
-        if (r + k >= rb.n) continue;
-        const size_t row = rb.row + r + k;
-        const BlockDiv div(t);
-        if (left > 0) store_e4m3<N, VEC>(q + row * K + c, left, v[k], div);
-        if (l == 0) scale[(size_t)i * M + row] = div.scale;
-      }
     }
     __syncthreads();
     if (threadIdx.x < kBlock) {
@@ -205,13 +216,21 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
       fs[j] = s_scale[l * N + j];
       fr[j] = s_recip[l * N + j];
     }
+    uint32_t w[R][N / 4];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (r + k >= out_rows || left <= 0) continue;
+      float v[N];
+      in[k].get(v);
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[k][j] = BlockDiv(fs[j], fr[j])(v[k][j]);
-      store_e4m3<N, VEC>(cq + (size_t)(rb.padded + r + k) * K + c, left, v[k]);
+      for (int j = 0; j < N; ++j) v[j] = BlockDiv(fs[j], fr[j])(v[j]);
+#pragma unroll
+      for (int j = 0; j < N / 4; ++j) w[k][j] = e4m3x4(v + 4 * j);
     }
+    load(i + gridDim.y);
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      if (r + k < out_rows && left > 0)
+        store_bytes<N, VEC>(cq + (size_t)(rb.padded + r + k) * K + c, left, w[k]);
   }
 }
 
@@ -230,20 +249,18 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
   const size_t e = blockIdx.z, at = e * n_rows * K;
   const int l = threadIdx.x % L, r = threadIdx.x / L * R;
   const int c = kb * kBlock + l * N, left = K - c, row0 = nb * kBlock + r;
-  float v[R][N], top = 0.f;
-#pragma unroll
-  for (int k = 0; k < R; ++k) {
-    if (row0 + k < n_rows && left > 0) {
-      load_elems<T, N, VEC>(w + at + (size_t)(row0 + k) * K + c, left, v[k]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) v[k][j] = 0.f;
-    }
-  }
+  RowVec<T, VEC> in[R];
+  float top = 0.f;
 #pragma unroll
   for (int k = 0; k < R; ++k)
+    in[k].load(w + at + (size_t)(row0 + k) * K + c, left, row0 + k < n_rows);
 #pragma unroll
-    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[k][j]));
+  for (int k = 0; k < R; ++k) {
+    float v[N];
+    in[k].get(v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[j]));
+  }
   top = group_max<32>(top);
   if (lane == 0) s_top[warp] = top;
   __syncthreads();
@@ -252,9 +269,12 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
   const BlockDiv div(top);
   if (threadIdx.x == 0) scale[(e * n_blocks + nb) * blocks + kb] = div.scale;
 #pragma unroll
-  for (int k = 0; k < R; ++k)
+  for (int k = 0; k < R; ++k) {
+    float v[N];
+    in[k].get(v);
     if (row0 + k < n_rows && left > 0)
-      store_e4m3<N, VEC>(q + at + (size_t)(row0 + k) * K + c, left, v[k], div);
+      store_e4m3<N, VEC>(q + at + (size_t)(row0 + k) * K + c, left, v, div);
+  }
 }
 
 // ----------------------------------------------------------------------------------- swiglu
@@ -369,7 +389,7 @@ extern "C" eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int
                      : (vec ? quant_columns_kernel<T, true, false>
                             : quant_columns_kernel<T, false, false>);
     // (one more block than the experts can have: the rows behind them)
-    return launch_pdl(kernel, dim3(blocks + 1, std::min(tiles, 65535)), dim3(kThreads), 0,
+    return launch_pdl(kernel, dim3(blocks + 1, (tiles + kTilesOfBlock - 1) / kTilesOfBlock), dim3(kThreads), 0,
                       (cudaStream_t)stream, (const T*)x, M, K, offsets, E, (int)padded, blocks, tiles,
                       (uint8_t*)q, scale, (uint8_t*)cq, cscale);
   }));

@@ -228,52 +228,74 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
   }
 }
 
-// y[t]: a warp takes N elements a lane of one token, all of its rows' loads before their use.
-template <typename T, int N>
+// y[t]: a warp takes a vector a lane of one token at a time, all of its rows' loads before their use, and
+// loads the next token's slots meanwhile.
+constexpr int kAhead = 8;  // rows
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(32 * kWarps)
 combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
                const float* __restrict__ weight, int tokens, int K, int d, int pieces,
                T* __restrict__ y) {
-  constexpr bool VEC = N > 1;
-  constexpr int kAhead = 8;  // rows
+  constexpr int N = Elem<T>::kN;
   pdl_wait();
   pdl_launch_dependents();
-  const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31, t = (int)(w / pieces);
-  const int c = ((int)(w % pieces) * 32 + lane) * N;
-  if (t >= tokens) return;
-  const int M = tokens * K;
-  int mine = lane < K ? slot[(size_t)t * K + lane] : -1;
-  if (mine >= M) mine = -1;
-  const float wt = lane < K && weight ? weight[(size_t)t * K + lane] : 1.0f;
-  float sum[N] = {};
-  for (int k0 = 0; k0 < K; k0 += kAhead) {
-    float v[kAhead][N];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
-      if (r >= 0 && c < d) load_elems<T, N, VEC>(rows + (size_t)r * d + c, d - c, v[k]);
+  const int lane = threadIdx.x & 31, M = tokens * K;
+  // units of (token, piece of its row), and the step between a warp's
+  const long long first = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int step = gridDim.x * kWarps, dt = step / pieces, dp = step - dt * pieces;
+  int nt = (int)(first / pieces), np = (int)(first - (long long)nt * pieces);
+  int next = -1;
+  float next_wt = 1.0f;
+  auto prefetch = [&] {
+    next = -1;
+    if (nt < tokens && lane < K) {
+      const size_t at = (size_t)nt * K + lane;
+      next = slot[at];
+      if (weight) next_wt = weight[at];
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
-      const float f = __shfl_sync(0xffffffffu, wt, (k0 + k) & 31);
-      if (r < 0) continue;
-#pragma unroll
-      for (int j = 0; j < N; ++j) sum[j] = fmaf(f, v[k][j], sum[j]);
+  };
+  prefetch();
+  while (nt < tokens) {
+    const int mine = next < M ? next : -1, t = nt, c = (np * 32 + lane) * N, left = d - c;
+    const float wt = next_wt;
+    nt += dt;
+    np += dp;
+    if (np >= pieces) {
+      np -= pieces;
+      ++nt;
     }
+    prefetch();
+    float sum[N] = {};
+    for (int k0 = 0; k0 < K; k0 += kAhead) {
+      RowVec<T, VEC> in[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+        in[k].load(rows + (size_t)max(r, 0) * d + c, left, r >= 0);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+        const float f = __shfl_sync(0xffffffffu, wt, (k0 + k) & 31);
+        float v[N];
+        in[k].get(v);
+        if (r < 0) continue;
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = fmaf(f, v[j], sum[j]);
+      }
+    }
+    if (left > 0) store_elems<T, N, VEC>(y + (size_t)t * d + c, left, sum);
   }
-  if (c < d) store_elems<T, N, VEC>(y + (size_t)t * d + c, d - c, sum);
 }
 
 // A block takes a token: its warps share the row, and add their parts of dw in their order.
-template <typename T, int N>
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(32 * kWarps)
 combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
                     const int32_t* __restrict__ slot, const int32_t* __restrict__ offsets,
                     const float* __restrict__ weight, int tokens, int K, int E, int d,
                     T* __restrict__ drows, float* __restrict__ dw) {
-  constexpr bool VEC = N > 1;
+  constexpr int N = Elem<T>::kN;
   __shared__ float s_part[kWarps][kMaxK];
   pdl_wait();
   pdl_launch_dependents();
@@ -283,33 +305,52 @@ combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
   if (mine >= M) mine = -1;
   const float wt = lane < K ? weight[(size_t)t * K + lane] : 0.f;
   float part = 0.f;  // lane k's: the warp's part of dw[t][k]
-  for (int c = threadIdx.x * N; c - lane * N < d; c += blockDim.x * N) {
-    float g[N];
-    const bool in = c < d;
-    if (in) load_elems<T, N, VEC>(dy + (size_t)t * d + c, d - c, g);
-    for (int k = 0; k < K; ++k) {
-      const int r = __shfl_sync(0xffffffffu, mine, k);
-      const float f = __shfl_sync(0xffffffffu, wt, k);
-      if (r < 0) continue;
-      float dot = 0.f;
-      if (in) {
+  for (int k0 = 0; k0 < K; k0 += kAhead) {
+    float dot[kAhead] = {};
+    for (int c = threadIdx.x * N; c - lane * N < d; c += blockDim.x * N) {
+      const int left = d - c;
+      RowVec<T, VEC> own, in[kAhead];
+      own.load(dy + (size_t)t * d + c, left, true);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+        in[k].load(rows + (size_t)max(r, 0) * d + c, left, r >= 0);
+      }
+      float g[N];
+      own.get(g);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+        const float f = __shfl_sync(0xffffffffu, wt, (k0 + k) & 31);
         float v[N], o[N];
-        load_elems<T, N, VEC>(rows + (size_t)r * d + c, d - c, v);
+        in[k].get(v);
+        if (r < 0 || left <= 0) continue;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          dot = fmaf(g[j], v[j], dot);
+          dot[k] = fmaf(g[j], v[j], dot[k]);
           o[j] = f * g[j];
         }
-        store_elems<T, N, VEC>(drows + (size_t)r * d + c, d - c, o);
+        store_elems<T, N, VEC>(drows + (size_t)r * d + c, left, o);
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      if (lane == k) part += dot;
+      if (k0 == 0 && left > 0) {
+        const float zero[N] = {};
+        for (long long r = (long long)used + t; r < M; r += tokens)
+          store_elems<T, N, VEC>(drows + (size_t)r * d + c, left, zero);
+      }
     }
-    const float zero[N] = {};
-    if (in)
-      for (long long r = (long long)used + t; r < M; r += tokens)
-        store_elems<T, N, VEC>(drows + (size_t)r * d + c, d - c, zero);
+    // lanes exchange the halves that they do not keep: lane l ends with the sum of the (l % 8)-th
+#pragma unroll
+    for (int h = kAhead / 2; h > 0; h >>= 1) {
+      const bool upper = lane & h;
+#pragma unroll
+      for (int i = 0; i < h; ++i) {
+        const float give = upper ? dot[i] : dot[i + h], keep = upper ? dot[i + h] : dot[i];
+        dot[i] = keep + __shfl_xor_sync(0xffffffffu, give, h);
+      }
+    }
+    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 8);
+    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 16);
+    if (lane / kAhead == k0 / kAhead) part = dot[0];
   }
   if (lane < K) s_part[warp][lane] = part;
   __syncthreads();
@@ -319,6 +360,8 @@ combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
     dw[(size_t)t * K + threadIdx.x] = s;
   }
 }
+
+constexpr unsigned kCombineBlocks = 152 * 4;
 
 int sort_chunks(int n) { return (n + kChunkLen - 1) / kChunkLen; }
 dim3 warp_grid(long long warps) { return dim3((unsigned)((warps + kWarps - 1) / kWarps)); }
@@ -428,10 +471,12 @@ extern "C" eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K,
     using X = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<X>::kN;
     const bool vec = d % N == 0 && !misaligned(rows, 16) && !misaligned(y, 16);
-    const int n = vec ? N : 1, pieces = (d + 32 * n - 1) / (32 * n);
-    return launch_pdl(vec ? combine_kernel<X, N> : combine_kernel<X, 1>,
-                      warp_grid((long long)T * pieces), dim3(32 * kWarps), 0, (cudaStream_t)stream,
-                      (const X*)rows, slot, w, T, K, d, pieces, (X*)y);
+    const int pieces = (d + 32 * N - 1) / (32 * N);
+    // (as many blocks as fit at a time, so that a warp has a next token)
+    const unsigned most = kCombineBlocks, all = warp_grid((long long)T * pieces).x;
+    return launch_pdl(vec ? combine_kernel<X, true> : combine_kernel<X, false>, dim3(std::min(most, all)),
+                      dim3(32 * kWarps), 0, (cudaStream_t)stream, (const X*)rows, slot, w, T, K, d,
+                      pieces, (X*)y);
   };
   return launched(fn, dtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr));
 }
@@ -456,8 +501,8 @@ extern "C" eat_status eat_expert_combine_grad(const void* dy, const void* rows, 
     constexpr int N = Elem<X>::kN;
     const bool vec =
         d % N == 0 && !misaligned(dy, 16) && !misaligned(rows, 16) && !misaligned(drows, 16);
-    const int per = vec ? N : 1, warps = std::min(kWarps, (d + 32 * per - 1) / (32 * per));
-    return launch_pdl(vec ? combine_grad_kernel<X, N> : combine_grad_kernel<X, 1>, dim3(T),
+    const int warps = std::min(kWarps, (d + 32 * N - 1) / (32 * N));
+    return launch_pdl(vec ? combine_grad_kernel<X, true> : combine_grad_kernel<X, false>, dim3(T),
                       dim3(32 * warps), 0, (cudaStream_t)stream, (const X*)dy, (const X*)rows, slot,
                       offsets, w, T, K, E, d, (X*)drows, dw);
   };

@@ -75,6 +75,26 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, WaitCt
     if (mbar_try_wait(bar, parity)) return true;
   return mbar_wait_slow(bar, parity, c, code, check_abort);
 }
+// The same without a call, for code that holds most of its registers across the wait (a call's convention
+// would move them).
+__device__ __forceinline__ bool mbar_wait_inline(uint64_t* bar, uint32_t parity, WaitCtx c,
+                                                 unsigned int code) {
+  if (mbar_try_wait(bar, parity)) return true;
+  unsigned long long t0 = 0, t;
+#pragma unroll 1
+  for (unsigned i = 1;; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (i % 64u != 0) continue;
+    if (*c.abort_flag) return false;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    if (t0 == 0) t0 = t;
+    if (t - t0 > kWaitLimitNs) {
+      *c.abort_flag = 1;
+      atomicOr(c.err, code);
+      return false;
+    }
+  }
+}
 // The same by all lanes of a warp, with one outcome for the whole warp.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, WaitCtx c,
                                           unsigned int code) {
