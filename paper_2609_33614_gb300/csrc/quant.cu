@@ -20,7 +20,6 @@ namespace eat {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 
 // 1 / (1 + exp(-g)): within 3 2^-23 + |g| 2^-24 of itself, far below what bf16 or e4m3 keep of it.
 __device__ __forceinline__ float sigmoid(float g) {
@@ -30,15 +29,15 @@ __device__ __forceinline__ float sigmoid(float g) {
 }
 
 // ------------------------------------------------------------------------------------- rows
-constexpr int kRows = 8;  // rows of a unit: their scales fill a sector of [blocks][M]
+constexpr int kMostRows = 8;  // of a unit: their scales fill a sector of [blocks][M]
 
 // A unit is kRows rows of one block of 128 columns, taken by as many lanes as the block has 16-byte
 // vectors.  GLU: the values are swiglu of rows of twice the length.
-template <typename T, bool VEC, bool GLU>
+template <typename T, bool VEC, bool GLU, int kRows>
 __global__ void __launch_bounds__(kThreads)
 quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __restrict__ q,
                   float* __restrict__ scale) {
-  constexpr int N = Elem<T>::kN, G = kBlock / N, U = GLU ? 4 : kRows;
+  constexpr int N = Elem<T>::kN, G = kBlock / N, U = GLU && kRows > 4 ? 4 : kRows;
   pdl_wait();
   pdl_launch_dependents();
   const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) / G;
@@ -79,7 +78,8 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
 }
 
 // ---------------------------------------------------------------------------------- columns
-constexpr int kTilesOfBlock = 4;  // that a thread block takes of its rows: it finds them once
+constexpr int kTileThreads = 512, kTileWarps = kTileThreads / 32;  // of a block that takes 128 x 128
+constexpr int kTilesOfBlock = 4;  // at most, of its rows: a thread block finds them once
 
 // Block b of the experts' blocks of 128 rows: its rows in x, and where they go in the padded order.
 struct RowBlock {
@@ -131,13 +131,13 @@ __device__ RowBlock find_block(const int32_t* offsets, int E, int M, int b) {
 // A tile of 128 rows and 128 columns at a time: thread (l, r) holds a vector of R consecutive rows.
 // ROWS: the rows' own blocks as well (q, scale), which the same tile holds whole.
 template <typename T, bool VEC, bool ROWS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kTileThreads, VEC ? 2 : 1)
 quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __restrict__ offsets,
                      int E, int padded_rows, int blocks, int tiles, uint8_t* __restrict__ q,
                      float* __restrict__ scale, uint8_t* __restrict__ cq,
                      float* __restrict__ cscale) {
-  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kThreads;
-  __shared__ float s_top[kWarps][kBlock];
+  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kTileThreads;
+  __shared__ float s_top[kTileWarps][kBlock];
   __shared__ float s_scale[kBlock], s_recip[kBlock];
   pdl_wait();
   pdl_launch_dependents();
@@ -202,7 +202,7 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
     if (threadIdx.x < kBlock) {
       float t = 0.f;
 #pragma unroll
-      for (int k = 0; k < kWarps; ++k) t = fmaxf(t, s_top[k][threadIdx.x]);
+      for (int k = 0; k < kTileWarps; ++k) t = fmaxf(t, s_top[k][threadIdx.x]);
       const BlockDiv div(t);
       s_scale[threadIdx.x] = div.scale;
       s_recip[threadIdx.x] = div.recip;
@@ -237,11 +237,11 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
 // ------------------------------------------------------------------------------------ tiles
 // A block takes a tile; thread: N columns of R consecutive rows.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kTileThreads, VEC ? 2 : 1)
 quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restrict__ q,
                    float* __restrict__ scale) {
-  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kThreads;
-  __shared__ float s_top[kWarps];
+  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kTileThreads;
+  __shared__ float s_top[kTileWarps];
   pdl_wait();
   pdl_launch_dependents();
   const int kb = blockIdx.x, blocks = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -265,7 +265,7 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
   if (lane == 0) s_top[warp] = top;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kWarps; ++k) top = fmaxf(top, s_top[k]);
+  for (int k = 0; k < kTileWarps; ++k) top = fmaxf(top, s_top[k]);
   const BlockDiv div(top);
   if (threadIdx.x == 0) scale[(e * n_blocks + nb) * blocks + kb] = div.scale;
 #pragma unroll
@@ -332,12 +332,19 @@ cudaError_t quant_rows(const void* x, int M, int K, int dtype, void* q, float* s
     using T = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<T>::kN;
     const int blocks = (K + kBlock - 1) / kBlock;
-    const long long units = (long long)((M + kRows - 1) / kRows) * blocks;
     const bool vec = K % N == 0 && !misaligned(x, 16) && !misaligned(q, N);
-    const long long threads = units * (kBlock / N);
-    return launch_pdl(vec ? quant_rows_kernel<T, true, GLU> : quant_rows_kernel<T, false, GLU>,
-                      dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st,
-                      (const T*)x, M, K, blocks, (uint8_t*)q, scale);
+    auto go = [&](auto rows) {
+      constexpr int R = decltype(rows)::value;
+      const long long threads = (long long)((M + R - 1) / R) * blocks * (kBlock / N);
+      return launch_pdl(vec ? quant_rows_kernel<T, true, GLU, R> : quant_rows_kernel<T, false, GLU, R>,
+                        dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st,
+                        (const T*)x, M, K, blocks, (uint8_t*)q, scale);
+    };
+    // Units of one row where longer ones would leave SMs without a block (8 rows of 14336, gated:
+    // MEASURED)
+    const long long units = (long long)((M + kMostRows - 1) / kMostRows) * blocks;
+    if (units * (kBlock / N) < 2LL * kThreads * num_sms()) return go(std::integral_constant<int, 1>());
+    return go(std::integral_constant<int, kMostRows>());
   });
 }
 
@@ -389,7 +396,10 @@ extern "C" eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int
                      : (vec ? quant_columns_kernel<T, true, false>
                             : quant_columns_kernel<T, false, false>);
     // (one more block than the experts can have: the rows behind them)
-    return launch_pdl(kernel, dim3(blocks + 1, (tiles + kTilesOfBlock - 1) / kTilesOfBlock), dim3(kThreads), 0,
+    // several tiles a block where there are blocks enough
+    const long long all = (long long)(blocks + 1) * tiles;
+    const int per = (int)std::max(1LL, std::min((long long)kTilesOfBlock, all / (4LL * num_sms())));
+    return launch_pdl(kernel, dim3(blocks + 1, (tiles + per - 1) / per), dim3(kTileThreads), 0,
                       (cudaStream_t)stream, (const T*)x, M, K, offsets, E, (int)padded, blocks, tiles,
                       (uint8_t*)q, scale, (uint8_t*)cq, cscale);
   }));
@@ -408,7 +418,7 @@ extern "C" eat_status eat_quant_tiles(const void* w, int32_t E, int32_t N, int32
     constexpr int V = Elem<T>::kN;
     const bool vec = K % V == 0 && !misaligned(w, 16) && !misaligned(q, V);
     return launch_pdl(vec ? quant_tiles_kernel<T, true> : quant_tiles_kernel<T, false>,
-                      dim3((K + kBlock - 1) / kBlock, (N + kBlock - 1) / kBlock, E), dim3(kThreads),
+                      dim3((K + kBlock - 1) / kBlock, (N + kBlock - 1) / kBlock, E), dim3(kTileThreads),
                       0, (cudaStream_t)stream, (const T*)w, N, K, (uint8_t*)q, scale);
   }));
 }

@@ -11,6 +11,7 @@
 // k and of the lanes, so the same inputs give the same bits; a value is rounded when it is stored.
 #include "elem.cuh"
 #include "op_checks.cuh"
+#include "tc_ptx.cuh"
 
 #include <algorithm>
 #include <type_traits>
@@ -20,32 +21,36 @@ namespace eat {
 namespace {
 
 // ------------------------------------------------------------------------------------- sort
-// A block sorts a chunk of consecutive selections; a warp takes kPer times 32 of them in order and
+// A block sorts a chunk of consecutive selections; a warp takes PER times 32 of them in order and
 // counts per expert as it goes (lanes of the same expert find each other by __match_any_sync), so a
 // selection's row is its expert's first + the chunks' and warps' before + its rank in the warp.
 constexpr int kSortThreads = 1024;
-constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kPer = 8;
+constexpr int kSortCtas = 8;   // of a cluster
+constexpr int kPer = 8;        // of a chunk of the calls that no cluster holds
 constexpr int kChunkLen = kSortThreads * kPer;
+constexpr int kClusterMost = kSortCtas * kSortThreads * 16;
 
-enum : int { kWhole = 0, kCount = 1, kAssign = 2 };
+// kCluster: the launch's one cluster holds all selections.  Otherwise chunk[c][e]: kCount writes the
+// chunks' counts, kAssign reads the sums of the chunks before, and total[e].
+enum : int { kCluster = 0, kCount = 1, kAssign = 2 };
 
-// chunk[c][e]: kCount writes the chunks' counts, kAssign reads the sums of the chunks before, and total[e].
-template <int MODE>
+template <int MODE, int PER>
 __global__ void __launch_bounds__(kSortThreads)
 sort_kernel(const int32_t* __restrict__ idx, int n, int K, int E, const uint8_t* __restrict__ mask,
             int32_t* chunk, const int32_t* __restrict__ total, int32_t* __restrict__ offsets,
             int32_t* __restrict__ slot) {
-  extern __shared__ int s_cnt[];  // [warps][E], then [E] first rows
-  int* const s_base = s_cnt + kSortWarps * E;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  for (int i = tid; i < kSortWarps * E; i += kSortThreads) s_cnt[i] = 0;
+  extern __shared__ int s_cnt[];  // [warps][E], then [E] first rows, [E] this CTA's counts
+  __shared__ int s_sum[kMaxExperts / 32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
+  int* const s_base = s_cnt + warps * E;
+  int* const s_mine = s_base + E;
+  for (int i = tid; i < warps * E; i += blockDim.x) s_cnt[i] = 0;
   pdl_wait();
   pdl_launch_dependents();
-  const int first = blockIdx.x * kChunkLen + warp * 32 * kPer + lane;
-  int ex[kPer], rank[kPer];
+  const int first = (blockIdx.x * warps + warp) * 32 * PER + lane;
+  int ex[PER], rank[PER];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const int at = first + 32 * i;
     int e = at < n ? idx[at] : -1;
     if (mask && at < n && !mask[at / K]) e = -1;
@@ -54,7 +59,7 @@ sort_kernel(const int32_t* __restrict__ idx, int n, int K, int E, const uint8_t*
   __syncthreads();
   int* const mine = s_cnt + warp * E;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const unsigned same = __match_any_sync(0xffffffffu, ex[i]);
     const int below = __popc(same & ((1u << lane) - 1u));
     int c = 0;
@@ -65,46 +70,80 @@ sort_kernel(const int32_t* __restrict__ idx, int n, int K, int E, const uint8_t*
     __syncwarp();
   }
   __syncthreads();
-  for (int e = tid; e < E; e += kSortThreads) {
+  for (int e = tid; e < E; e += blockDim.x) {
     int sum = 0;
-    for (int w = 0; w < kSortWarps; ++w) {
-      const int c = s_cnt[w * E + e];
-      s_cnt[w * E + e] = sum;
-      sum += c;
+    for (int w0 = 0; w0 < warps; w0 += 8) {
+      int c[8];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) c[w] = w0 + w < warps ? s_cnt[(w0 + w) * E + e] : 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        if (w0 + w < warps) s_cnt[(w0 + w) * E + e] = sum;
+        sum += c[w];
+      }
     }
     if (MODE == kCount) chunk[(size_t)blockIdx.x * E + e] = sum;
-    s_base[e] = MODE == kAssign ? total[e] : sum;
+    s_mine[e] = sum;
   }
   if (MODE == kCount) return;
-  __syncthreads();
-  if (warp == 0) {  // first rows of the experts
-    int before = 0;
-    for (int b = 0; b < E; b += 32) {
-      const int c = b + lane < E ? s_base[b + lane] : 0;
-      int v = c;
+  int before = 0;  // expert tid's: in the CTAs or chunks before this one
+  int all = 0;
+  if (MODE == kCluster) {
+    if (gridDim.x > 1) ptx::cluster_sync_all();
+    else __syncthreads();
+    if (tid < E) {
+      if (gridDim.x == 1) {
+        all = s_mine[tid];
+      } else {
+        int c[kSortCtas];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += u;
+        for (int r = 0; r < kSortCtas; ++r) {
+          c[r] = 0;
+          if (r < (int)gridDim.x)
+            asm volatile("ld.shared::cluster.s32 %0, [%1];"
+                         : "=r"(c[r])
+                         : "r"(ptx::map_rank(ptx::smem_u32(s_mine + tid), (uint32_t)r)));
+        }
+#pragma unroll
+        for (int r = 0; r < kSortCtas; ++r) {
+          if (r < (int)blockIdx.x) before += c[r];
+          all += c[r];
+        }
       }
-      if (b + lane < E) {
-        s_base[b + lane] = before + v - c;
-        if (blockIdx.x == 0) offsets[b + lane] = before + v - c;
-      }
-      before += __shfl_sync(0xffffffffu, v, 31);
     }
-    if (blockIdx.x == 0 && lane == 0) offsets[E] = before;
+    // (no CTA leaves while another may still read its counts)
+    if (gridDim.x > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  } else if (tid < E) {
+    all = total[tid];
+    before = chunk[(size_t)blockIdx.x * E + tid];
+  }
+  // first rows of the experts: scans of 32 of them, then of those sums (a block has at least E threads,
+  // or 256)
+  int v = all;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  if (lane == 31 && warp < kMaxExperts / 32) s_sum[warp] = v;
+  __syncthreads();
+  if (tid < E) {
+    int at = v - all;
+    for (int w = 0; w < warp; ++w) at += s_sum[w];
+    s_base[tid] = at + before;
+    if (blockIdx.x == 0) {
+      offsets[tid] = at;
+      if (tid == E - 1) offsets[E] = at + all;
+    }
   }
   __syncthreads();
-  if (MODE == kAssign) {
-    for (int e = tid; e < E; e += kSortThreads) s_base[e] += chunk[(size_t)blockIdx.x * E + e];
-    __syncthreads();
-  }
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const int at = first + 32 * i;
     if (at < n) slot[at] = ex[i] < 0 ? -1 : s_base[ex[i]] + mine[ex[i]] + rank[i];
   }
+  if (MODE == kCluster && gridDim.x > 1)
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // A warp per expert: chunk[c][e] becomes the sum of the chunks before c, total[e] the sum of all.
@@ -230,9 +269,10 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
 
 // y[t]: a warp takes a vector a lane of one token at a time, all of its rows' loads before their use, and
 // loads the next token's slots meanwhile.
-constexpr int kAhead = 8;  // rows
+constexpr int kAhead = 4;          // rows
+constexpr int kCombineBlocks = 6;  // of an SM
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, VEC ? kCombineBlocks : 1)
 combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
                const float* __restrict__ weight, int tokens, int K, int d, int pieces,
                T* __restrict__ y) {
@@ -338,7 +378,7 @@ combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
           store_elems<T, N, VEC>(drows + (size_t)r * d + c, left, zero);
       }
     }
-    // lanes exchange the halves that they do not keep: lane l ends with the sum of the (l % 8)-th
+    // lanes exchange the halves that they do not keep: lane l ends with the sum of the (l % kAhead)-th
 #pragma unroll
     for (int h = kAhead / 2; h > 0; h >>= 1) {
       const bool upper = lane & h;
@@ -348,8 +388,8 @@ combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
         dot[i] = keep + __shfl_xor_sync(0xffffffffu, give, h);
       }
     }
-    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 8);
-    dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 16);
+#pragma unroll
+    for (int o = kAhead; o < 32; o <<= 1) dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], o);
     if (lane / kAhead == k0 / kAhead) part = dot[0];
   }
   if (lane < K) s_part[warp][lane] = part;
@@ -360,8 +400,6 @@ combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
     dw[(size_t)t * K + threadIdx.x] = s;
   }
 }
-
-constexpr unsigned kCombineBlocks = 152 * 4;
 
 int sort_chunks(int n) { return (n + kChunkLen - 1) / kChunkLen; }
 dim3 warp_grid(long long warps) { return dim3((unsigned)((warps + kWarps - 1) / kWarps)); }
@@ -397,19 +435,30 @@ extern "C" eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, 
     return bad_arg(fn, "misaligned pointer");
   const cudaStream_t st = (cudaStream_t)stream;
   const int n = T * K, chunks = sort_chunks(n);
-  const size_t smem = (size_t)(kSortWarps + 1) * E * 4;  // at most 33 KB
-  if (chunks == 1)
-    return launched(fn, launch_pdl(sort_kernel<kWhole>, dim3(1), dim3(kSortThreads), smem, st, idx,
-                                   n, K, E, mask, (int32_t*)nullptr, (const int32_t*)nullptr,
-                                   offsets, slot));
+  auto smem = [&](int threads) { return (size_t)(threads / 32 + 2) * E * 4; };  // at most 35 KB
+  if (n <= kClusterMost) {
+    // One launch.  Two selections a thread in as many CTAs as that takes, up to a cluster's; more of them
+    // only where it holds no more threads (65528 selections of 64 experts: MEASURED)
+    const int per = n <= 2 * kSortCtas * kSortThreads ? 2 : n <= 8 * kSortCtas * kSortThreads ? 8 : 16;
+    const int ctas = (n + per * kSortThreads - 1) / (per * kSortThreads);
+    // (a small call's block has no warps that only add to its sums, but a thread for each expert)
+    const int need = ctas > 1 ? kSortThreads : (n + 2 * 32 - 1) / (2 * 32) * 32;
+    const int threads = std::max(need, (E + 31) / 32 * 32);
+    auto* kernel = per == 2   ? sort_kernel<kCluster, 2>
+                   : per == 8 ? sort_kernel<kCluster, 8>
+                              : sort_kernel<kCluster, 16>;
+    return launched(fn, launch_pdl_cluster(kernel, dim3(ctas), ctas, dim3(threads), smem(threads), st, idx,
+                                           n, K, E, mask, (int32_t*)nullptr, (const int32_t*)nullptr,
+                                           offsets, slot));
+  }
   int32_t *chunk = (int32_t*)work, *total = chunk + (size_t)chunks * E;
-  cudaError_t e = launch_pdl(sort_kernel<kCount>, dim3(chunks), dim3(kSortThreads), smem, st, idx, n,
+  cudaError_t e = launch_pdl(sort_kernel<kCount, kPer>, dim3(chunks), dim3(kSortThreads), smem(kSortThreads), st, idx, n,
                              K, E, mask, chunk, (const int32_t*)nullptr, (int32_t*)nullptr,
                              (int32_t*)nullptr);
   if (e == cudaSuccess)
     e = launch_pdl(sort_scan_kernel, dim3(E), dim3(32), 0, st, chunk, chunks, E, total);
   if (e == cudaSuccess)
-    e = launch_pdl(sort_kernel<kAssign>, dim3(chunks), dim3(kSortThreads), smem, st, idx, n, K, E,
+    e = launch_pdl(sort_kernel<kAssign, kPer>, dim3(chunks), dim3(kSortThreads), smem(kSortThreads), st, idx, n, K, E,
                    mask, chunk, (const int32_t*)total, offsets, slot);
   return launched(fn, e);
 }
@@ -472,8 +521,8 @@ extern "C" eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K,
     constexpr int N = Elem<X>::kN;
     const bool vec = d % N == 0 && !misaligned(rows, 16) && !misaligned(y, 16);
     const int pieces = (d + 32 * N - 1) / (32 * N);
-    // (as many blocks as fit at a time, so that a warp has a next token)
-    const unsigned most = kCombineBlocks, all = warp_grid((long long)T * pieces).x;
+    // (as many blocks as run at a time, so that a warp has a next token)
+    const unsigned most = (unsigned)(kCombineBlocks * num_sms()), all = warp_grid((long long)T * pieces).x;
     return launch_pdl(vec ? combine_kernel<X, true> : combine_kernel<X, false>, dim3(std::min(most, all)),
                       dim3(32 * kWarps), 0, (cudaStream_t)stream, (const X*)rows, slot, w, T, K, d,
                       pieces, (X*)y);
@@ -501,7 +550,10 @@ extern "C" eat_status eat_expert_combine_grad(const void* dy, const void* rows, 
     constexpr int N = Elem<X>::kN;
     const bool vec =
         d % N == 0 && !misaligned(dy, 16) && !misaligned(rows, 16) && !misaligned(drows, 16);
-    const int warps = std::min(kWarps, (d + 32 * N - 1) / (32 * N));
+    // Many tokens: two warps each, so that more tokens' loads are under way (8191 tokens x 8 of 2048:
+    // MEASURED); few: as many as the row has vectors for.
+    const int most = T >= 16 * num_sms() ? 2 : kWarps;
+    const int warps = std::min(most, (d + 32 * N - 1) / (32 * N));
     return launch_pdl(vec ? combine_grad_kernel<X, true> : combine_grad_kernel<X, false>, dim3(T),
                       dim3(32 * warps), 0, (cudaStream_t)stream, (const X*)dy, (const X*)rows, slot,
                       offsets, w, T, K, E, d, (X*)drows, dw);
