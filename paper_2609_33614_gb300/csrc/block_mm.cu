@@ -10,7 +10,7 @@
 // A k-block of 128 is four MMAs into an accumulator of its own in TMEM; the epilogue's warps read it,
 // multiply by the block's scales and add it to fp32 sums in registers while the next k-blocks run.  In
 // the 16x256b layout a thread has two neighbouring rows of the output for each of its columns, so a
-// scale's pair is one load and each packed multiply-add takes two elements.
+// scale's pair is one load.
 // Operands come by TMA as they lie (K-major, or MN-major where the sum runs over their rows): w serves
 // both directions, and the gradient reads both operands by rows.
 // Warps: 0 issues TMA, 1 owns TMEM and issues MMAs, 2 copies the blocks' scales into a ring and clears
@@ -122,11 +122,23 @@ __device__ __forceinline__ uint32_t bf16x2(uint64_t v) {
   const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
   return *(const uint32_t*)&b;
 }
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *(const uint32_t*)&v;
+}
 // Four 8 x 8 matrices of 16-bit values whose fragments the lanes hold, transposed into rows of 16 bytes.
 __device__ __forceinline__ void stmatrix_t(uint32_t dst, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(dst),
                "r"(a), "r"(b), "r"(c), "r"(d)
                : "memory");
+}
+
+// Operands landed and the accumulator free.  Both are asked at once: a wait that need not wait takes 180
+// cycles where its answer is waited for, and the accumulator's, which every k-block waits for, comes last.
+__device__ __forceinline__ bool both(uint64_t* full, uint32_t fp, uint64_t* tempty, uint32_t tp, WaitCtx wc) {
+  const bool f = mbar_test_wait(full, fp), t = mbar_test_wait(tempty, tp);
+  if (!f && !mbar_wait_inline(full, fp, wc, 8u)) return false;
+  return t || mbar_wait_inline(tempty, tp, wc, 4u);
 }
 
 // The experts of a call, in shared memory: rows row[e] .. end[e] - 1 (held to [0, M]) and the row tiles of
@@ -138,6 +150,112 @@ struct Experts {
 // k-blocks (the last of `tail` k; kGrad: from padded row k0, block b0).
 struct Tile {
   int e, row0, rows, c0, nkb, k0, b0, sums;
+};
+
+// By a full warp: fills ex for row tiles of up to NT rows.
+template <int MODE, int NT>
+__device__ __forceinline__ void list_experts(const Args& a, Experts& ex) {
+  const int lane = threadIdx.x & 31;
+  // prefix sums over the experts; what follows the last one is in [E]
+  int tiles = 0, padded = 0, blocks = 0;
+  const int cap = MODE == kGrad ? 1 << 30 : a.M;
+  for (int e0 = 0; e0 < a.E; e0 += 32) {
+    const int e = e0 + lane;
+    int lo = 0, hi = 0;
+    if (e < a.E) {
+      lo = a.offsets ? max(0, min(a.offsets[e], cap)) : 0;
+      hi = a.offsets ? max(lo, min(a.offsets[e + 1], cap)) : a.M;
+    }
+    const int n = hi - lo;
+    int vt = (n + NT - 1) / NT, vp = (n + 31) & ~31, vb = (n + kBlock - 1) / kBlock;
+    const int t = vt, p = vp, b = vb;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int ut = __shfl_up_sync(0xffffffffu, vt, o), up = __shfl_up_sync(0xffffffffu, vp, o),
+                ub = __shfl_up_sync(0xffffffffu, vb, o);
+      if (lane >= o) {
+        vt += ut;
+        vp += up;
+        vb += ub;
+      }
+    }
+    if (e < a.E) {
+      if (MODE == kGrad) {
+        // (offsets that are not those of the operands reach nothing outside of them)
+        const int k0 = padded + vp - p, b0 = blocks + vb - b;
+        const bool fits = k0 >= 0 && b0 >= 0 && (long long)k0 + p <= a.M && (long long)b0 + b <= a.blocks;
+        ex.row[e] = k0;
+        ex.end[e] = fits ? n : 0;
+        ex.tile0[e] = b0;
+      } else {
+        ex.row[e] = lo;
+        ex.end[e] = hi;
+        ex.tile0[e] = tiles + vt - t;
+      }
+    }
+    tiles += __shfl_sync(0xffffffffu, vt, 31);
+    padded += __shfl_sync(0xffffffffu, vp, 31);
+    blocks += __shfl_sync(0xffffffffu, vb, 31);
+  }
+  if (lane == 0) ex.tile0[a.E] = tiles;
+}
+
+// Tile u of x's rows, in the order (expert, columns, rows): tiles that read the same part of a matrix
+// follow each other.  The rows of an expert are cut into tiles of equal heights, a multiple of 16.
+template <int COLS>
+__device__ __forceinline__ Tile row_tile(const Args& a, const Experts& ex, int col_tiles, int inner,
+                                         long long u) {
+  Tile t;
+  int lo = 0, hi = a.E;  // the last expert whose tiles begin at or before u
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((long long)ex.tile0[mid] * col_tiles <= u) lo = mid;
+    else hi = mid;
+  }
+  t.e = lo;
+  const unsigned n = ex.end[lo] - ex.row[lo], count = ex.tile0[lo + 1] - ex.tile0[lo];
+  const unsigned v = (unsigned)(u - (long long)ex.tile0[lo] * col_tiles);
+  const unsigned h = ((n + count - 1) / count + 15) & ~15u;
+  const unsigned c = v / count, i = v - c * count;
+  t.row0 = ex.row[lo] + (int)(i * h);
+  t.rows = (int)min(h, n - i * h);
+  t.c0 = (int)c * COLS;
+  t.sums = inner;
+  t.k0 = t.b0 = 0;
+  t.nkb = (inner + kBlock - 1) / kBlock;
+  return t;
+}
+
+// The rows behind the last expert's, in pieces of 512 bytes of which every CTA takes its share: a warp
+// clears some whenever it has time.
+template <typename Out>
+struct Behind {
+  uint4* at = nullptr;
+  long long pieces = 0, piece = 0;
+  __device__ __forceinline__ Behind(const Args& a, const Experts& ex, int cols, bool any) {
+    if (!any || !a.offsets) return;
+    const int lane = threadIdx.x & 31;
+    int end = 0;
+    for (int e = lane; e < a.E; e += 32) end = max(end, ex.end[e]);
+    end = (int)__reduce_max_sync(0xffffffffu, (unsigned)end);
+    Out* const first = (Out*)a.out + (size_t)end * cols;
+    Out* const last = (Out*)a.out + (size_t)a.M * cols;
+    uint4* const begin = (uint4*)(((uintptr_t)first + 15) & ~(uintptr_t)15);
+    uint4* const stop = (uint4*)((uintptr_t)last & ~(uintptr_t)15);
+    if (blockIdx.x == 0) {  // what lies before and behind whole vectors
+      const long long n = last - first, head = min(n, (long long)((Out*)begin - first));
+      if (lane < head) first[lane] = Elem<Out>::put(0.f);
+      const long long tail = stop >= begin ? last - (Out*)stop : 0;
+      if (lane < tail) last[-1 - lane] = Elem<Out>::put(0.f);
+    }
+    at = begin + lane;
+    piece = blockIdx.x;
+    pieces = stop > begin ? ((long long)(stop - begin) + 31) / 32 : 0;
+    if (pieces > 0 && at + (pieces - 1) * 32 >= stop) --pieces;  // this lane has none in the last
+  }
+  __device__ __forceinline__ void clear(int n) {
+    for (; n > 0 && piece < pieces; --n, piece += gridDim.x) at[piece * 32] = make_uint4(0, 0, 0, 0);
+  }
 };
 
 template <int MODE, int NT, typename Out>
@@ -179,50 +297,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   if (warp == 1) tmem_alloc<false>(&tmem_slot, C::kTmemCols);
   pdl_wait();
   pdl_launch_dependents();
-  if (warp == 0) {
-    // prefix sums over the experts; what follows the last one is in [E]
-    int tiles = 0, padded = 0, blocks = 0;
-    const int cap = MODE == kGrad ? 1 << 30 : a.M;
-    for (int e0 = 0; e0 < a.E; e0 += 32) {
-      const int e = e0 + lane;
-      int lo = 0, hi = 0;
-      if (e < a.E) {
-        lo = a.offsets ? max(0, min(a.offsets[e], cap)) : 0;
-        hi = a.offsets ? max(lo, min(a.offsets[e + 1], cap)) : a.M;
-      }
-      const int n = hi - lo;
-      int vt = (n + NT - 1) / NT, vp = (n + 31) & ~31, vb = (n + kBlock - 1) / kBlock;
-      const int t = vt, p = vp, b = vb;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int ut = __shfl_up_sync(0xffffffffu, vt, o), up = __shfl_up_sync(0xffffffffu, vp, o),
-                  ub = __shfl_up_sync(0xffffffffu, vb, o);
-        if (lane >= o) {
-          vt += ut;
-          vp += up;
-          vb += ub;
-        }
-      }
-      if (e < a.E) {
-        if (MODE == kGrad) {
-          // (offsets that are not those of the operands reach nothing outside of them)
-          const int k0 = padded + vp - p, b0 = blocks + vb - b;
-          const bool fits = k0 >= 0 && b0 >= 0 && (long long)k0 + p <= a.M && (long long)b0 + b <= a.blocks;
-          ex.row[e] = k0;
-          ex.end[e] = fits ? n : 0;
-          ex.tile0[e] = b0;
-        } else {
-          ex.row[e] = lo;
-          ex.end[e] = hi;
-          ex.tile0[e] = tiles + vt - t;
-        }
-      }
-      tiles += __shfl_sync(0xffffffffu, vt, 31);
-      padded += __shfl_sync(0xffffffffu, vp, 31);
-      blocks += __shfl_sync(0xffffffffu, vb, 31);
-    }
-    if (lane == 0) ex.tile0[a.E] = tiles;
-  }
+  if (warp == 0) list_experts<MODE, NT>(a, ex);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -232,7 +307,6 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   const int col_tiles = (cols + kBlock - 1) / kBlock;
   const int n_tiles = (a.N + NT - 1) / NT;  // kGrad
   const long long units = (long long)(MODE == kGrad ? a.E * n_tiles : ex.tile0[a.E]) * col_tiles;
-  // Tiles in the order (expert, columns, rows): those that read the same part of a matrix follow each other.
   auto tile_at = [&](long long u) {
     Tile t;
     if (MODE == kGrad) {
@@ -247,22 +321,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       t.k0 = ex.row[t.e];
       t.b0 = ex.tile0[t.e];
     } else {
-      int lo = 0, hi = a.E;  // the last expert whose tiles begin at or before u
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((long long)ex.tile0[mid] * col_tiles <= u) lo = mid;
-        else hi = mid;
-      }
-      t.e = lo;
-      const int n = ex.end[lo] - ex.row[lo], count = ex.tile0[lo + 1] - ex.tile0[lo];
-      const int v = (int)(u - (long long)ex.tile0[lo] * col_tiles);
-      const int h = ((n + count - 1) / count + 15) & ~15;
-      const int i = v % count;
-      t.row0 = ex.row[lo] + i * h;
-      t.rows = min(h, n - i * h);
-      t.c0 = v / count * kBlock;
-      t.sums = inner;
-      t.k0 = t.b0 = 0;
+      return row_tile<kBlock>(a, ex, col_tiles, inner, u);
     }
     t.nkb = (t.sums + kBlock - 1) / kBlock;
     return t;
@@ -280,7 +339,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
         const Tile t = tile_at(u);
         for (int kb = 0; kb < t.nkb; ++kb) {
-          if (!mbar_wait(&empty[stage], phase ^ 1u, wc, 1u)) {
+          if (!mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
             ok = false;
             break;
           }
@@ -324,7 +383,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         const Tile t = tile_at(u);
         const uint32_t id = idesc(true, kBlock, (t.rows + 15) & ~15, MODE != kForward, MODE == kGrad);
         for (int kb = 0; kb < t.nkb; ++kb) {
-          if (!mbar_wait(&tempty[buf], bphase ^ 1u, wc, 4u) || !mbar_wait(&full[stage], phase, wc, 8u)) {
+          if (!both(&full[stage], phase, &tempty[buf], bphase ^ 1u, wc)) {
             ok = false;
             break;
           }
@@ -353,30 +412,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
     if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
   } else if (warp == 2) {
-    // The rows behind the last expert's, in pieces of 512 bytes of which every CTA takes its share.
-    uint4* zero = nullptr;
-    long long pieces = 0, piece = blockIdx.x;
-    if (MODE != kGrad && a.offsets) {
-      int end = 0;
-      for (int e = lane; e < a.E; e += 32) end = max(end, ex.end[e]);
-      end = (int)__reduce_max_sync(0xffffffffu, (unsigned)end);
-      Out* const first = (Out*)a.out + (size_t)end * cols;
-      Out* const last = (Out*)a.out + (size_t)a.M * cols;
-      zero = (uint4*)(((uintptr_t)first + 15) & ~(uintptr_t)15);
-      uint4* const stop = (uint4*)((uintptr_t)last & ~(uintptr_t)15);
-      pieces = stop > zero ? ((long long)(stop - zero) + 31) / 32 : 0;
-      if (blockIdx.x == 0) {  // what lies before and behind whole vectors
-        const long long n = last - first, head = min(n, (long long)((Out*)zero - first));
-        if (lane < head) first[lane] = Elem<Out>::put(0.f);
-        const long long tail = stop >= zero ? last - (Out*)stop : 0;
-        if (lane < tail) last[-1 - lane] = Elem<Out>::put(0.f);
-      }
-      zero += lane;
-      if (pieces > 0 && zero + (pieces - 1) * 32 >= stop) --pieces;  // this lane has none in the last
-    }
-    auto clear = [&](int n) {
-      for (; n > 0 && piece < pieces; --n, piece += gridDim.x) zero[piece * 32] = make_uint4(0, 0, 0, 0);
-    };
+    Behind<Out> behind(a, ex, cols, MODE != kGrad);
     // The copies of k-block i are issued kAhead before those of i - kAhead are handed over, which is once
     // the accumulator that goes with them is free: then so is the slot that comes kBufs before it.
     long long u = blockIdx.x;
@@ -429,9 +465,9 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (++copy == C::kSlots) copy = 0;
       }
       cp_async_commit();  // (one group an iteration, whether it holds a copy or not)
-      clear(8);
+      if (MODE != kGrad) behind.clear(8);
     }
-    clear(1 << 30);
+    if (MODE != kGrad) behind.clear(1 << 30);
     asm volatile("cp.async.wait_all;" ::: "memory");
   }
   } else {
@@ -445,7 +481,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     bool ok = true;
     for (long long u = blockIdx.x; u < units; u += gridDim.x) {
       const Tile t = tile_at(u);
-      // acc[g][2 h + p]: rows 8 g + 2 (lane % 4), + 1, column 16 h + 8 p + lane / 4 of the warp's
+      // acc[g][i]: rows 8 g + 2 (lane % 4), + 1, column 8 i + lane / 4 of the warp's
       uint64_t acc[C::kCols / 8][4];
 #pragma unroll
       for (int g = 0; g < C::kCols / 8; ++g)
@@ -567,7 +603,322 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   if (warp == 1) tmem_dealloc<false>(tmem_base, C::kTmemCols);
 }
 
+// ------------------------------------------------------------------------------ many rows an expert
+// On an SM pair (cta_group::2): up to 256 of x's rows (M, half of them each CTA's) x 256 columns (N).  A
+// thread owns a row of 128 columns, so a k-block's scales are one product a thread: its row's times the
+// columns' block's, loaded kLead k-blocks ahead.
+// Rows an expert has on average, above which its tiles are these (32 matrices of 2048 x 2048, 96 rows each:
+// 49.1 us, 47.1 with the kernel above; 128 rows: 47.1 and 51.2; 256: 59.4 and 65.5)
+constexpr int kWideRows = 112;
+
+struct Wide {
+  static constexpr int kRows = 256, kCols = 256;
+  static constexpr int kStage = 2 * kOperand, kStages = 6;
+  static constexpr int kEpiWarps = 8, kThreads = 32 * (kFirstEpi + kEpiWarps);
+  static constexpr int kOut = kEpiWarps * 32 * 64;
+  static constexpr int kSmem = 1024 + kStages * kStage + kOut;
+  static constexpr int kLead = 4;
+  static constexpr int kFewRegs = 88, kManyRegs = 208;  // as above
+};
+
+__device__ __forceinline__ void tma_load_pair_3d(void* dst, const CUtensorMap* map, uint32_t bar, int c0,
+                                                 int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+
+template <int MODE, typename Out>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Wide::kThreads, 1)
+wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+            const Args a) {
+  using C = Wide;
+  constexpr int S = C::kStages, L = C::kLead;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  __shared__ uint64_t full[S], empty[S], tfull[2], tempty[2], mma_done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  __shared__ unsigned int err_word;
+  __shared__ Experts ex;
+  volatile int* const abort_flag = &abort_word;
+  const WaitCtx wc{abort_flag, &err_word};
+
+  const uint32_t rank = cluster_rank();
+  const bool leader = rank == 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], 2 * C::kEpiWarps);  // the epilogue's warps of both CTAs (rank 0's)
+    }
+    mbar_init(&mma_done, 1);
+    abort_word = 0;
+    err_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&map_w);
+    prefetch_map(&map_x);
+  }
+  if (warp == 1) tmem_alloc<true>(&tmem_slot, 512);
+  pdl_wait();
+  pdl_launch_dependents();
+  if (warp == 0) list_experts<MODE, C::kRows>(a, ex);
+  tc_fence_before();
+  cluster_sync_all();  // both CTAs' barriers exist before either signals the other
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+
+  const int cols = MODE == kForward ? a.N : a.K, inner = MODE == kForward ? a.K : a.N;
+  const int col_tiles = (cols + C::kCols - 1) / C::kCols;
+  const long long units = (long long)ex.tile0[a.E] * col_tiles;
+  const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  auto tile_at = [&](long long u) { return row_tile<C::kCols>(a, ex, col_tiles, inner, u); };
+  // rows of a CTA: rank 0's half is a multiple of 16
+  auto half = [](int rows) { return min(rows, ((rows + 1) / 2 + 15) & ~15); };
+  const uint32_t full0 = map_rank(smem_u32(full), 0), tempty0 = map_rank(smem_u32(tempty), 0);
+
+  if (warp < kFirstEpi) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kFewRegs));
+    if (warp == 0) {
+      if (elect_one()) {
+        int stage = 0;
+        uint32_t phase = 0;
+        long long issued = 0;
+        bool ok = true;
+        for (long long u = first; ok && u < units; u += step) {
+          const Tile t = tile_at(u);
+          const int h = half(t.rows), box0 = (h + 31) / 32, box1 = (t.rows - h + 31) / 32;
+          const int boxes = leader ? box0 : box1, row0 = t.row0 + (leader ? 0 : h);
+          const int c0 = t.c0 + (int)rank * kBlock;
+          const uint32_t bytes = (uint32_t)(2 * kOperand + (box0 + box1) * 32 * kBlock);
+          for (int kb = 0; kb < t.nkb; ++kb) {
+            if (!mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
+              ok = false;
+              break;
+            }
+            uint8_t* const sa = smem + stage * C::kStage;
+            uint8_t* const sb = sa + kOperand;
+            const uint32_t bar = full0 + 8u * (uint32_t)stage;
+            if (leader) mbar_expect_tx(&full[stage], bytes);
+            const int k = kb * kBlock;
+            if (MODE == kForward) tma_load_pair_3d(sb, &map_w, bar, k, c0, t.e);
+            else tma_load_pair_3d(sb, &map_w, bar, c0, k, t.e);
+            for (int i = 0; i < boxes; ++i)
+              tma_load_pair(sa + i * 32 * kBlock, &map_x, bar, k, row0 + 32 * i);
+            ++issued;
+            if (++stage == S) {
+              stage = 0;
+              phase ^= 1u;
+            }
+          }
+        }
+        // rank 0: the copies of both CTAs still in flight land before the pair may exit
+        if (leader)
+          for (long long i = issued > S ? issued - S : 0; i < issued; ++i)
+            mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), wc, 2u, false);
+      }
+    } else if (warp == 1) {
+      if (leader && elect_one()) {
+        constexpr uint32_t id = idesc(true, C::kRows, C::kCols, false, MODE == kBack);
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, bphase = 0;
+        bool ok = true;
+        for (long long u = first; ok && u < units; u += step) {
+          const Tile t = tile_at(u);
+          for (int kb = 0; kb < t.nkb; ++kb) {
+            if (!both(&full[stage], phase, &tempty[buf], bphase ^ 1u, wc)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem + stage * C::kStage);
+            const uint64_t da = sdesc_k(sa);
+            const uint64_t db = MODE == kBack ? sdesc_mn8(sa + kOperand) : sdesc_k(sa + kOperand);
+            const uint32_t d = tmem_base + (uint32_t)(buf * C::kCols);
+            const int steps = (min(kBlock, inner - kb * kBlock) + 31) / 32;
+            for (int k = 0; k < steps; ++k)
+              mma<true, true>(d, da + 2 * k, db + k * (MODE == kBack ? 256 : 2), id, k > 0);
+            mma_commit<true>(&empty[stage]);
+            mma_commit<true>(&tfull[buf]);
+            if (++stage == S) {
+              stage = 0;
+              phase ^= 1u;
+            }
+            if (++buf == 2) {
+              buf = 0;
+              bphase ^= 1u;
+            }
+          }
+        }
+        mma_commit<true>(&mma_done);
+      }
+      if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+    } else if (warp == 2) {
+      Behind<Out> behind(a, ex, cols, true);
+      behind.clear(1 << 30);
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kManyRegs));
+    const int q = warp & 3, ch = (warp - kFirstEpi) >> 2;  // quarter of the rows, half of the columns
+    const uint32_t tq = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(ch * kBlock);
+    uint4* const box = (uint4*)(smem + S * C::kStage) + (warp - kFirstEpi) * 128;
+    const int nb = (a.N + kBlock - 1) / kBlock, kbs = (a.K + kBlock - 1) / kBlock;
+    int buf = 0;
+    uint32_t bphase = 0;
+    bool ok = true;
+    Tile t{};
+    float xs[L], ws[L];
+    const float *px = nullptr, *pw = nullptr;
+    int live = 0, row0 = 0;  // of this CTA's rows
+    size_t wstep = 0;
+    auto begin = [&](long long u) {  // the tile and its first scales
+      t = tile_at(u);
+      const int h = half(t.rows);
+      row0 = t.row0 + (leader ? 0 : h);
+      live = leader ? h : t.rows - h;
+      const int cb = min(t.c0 / kBlock + ch, (cols + kBlock - 1) / kBlock - 1);
+      px = a.xs + min(row0 + 32 * q + lane, a.M - 1);
+      pw = a.ws + (size_t)t.e * nb * kbs + (MODE == kForward ? (size_t)cb * kbs : (size_t)cb);
+      wstep = MODE == kForward ? 1 : (size_t)kbs;
+      // (the k-blocks behind the last are not used: they repeat it)
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        if (i > 0) {
+          px += i < t.nkb ? a.M : 0;
+          pw += i < t.nkb ? wstep : 0;
+        }
+        xs[i] = *px;
+        ws[i] = *pw;
+      }
+    };
+    bool ready = false;
+    if (first < units) begin(first);
+    for (long long u = first; u < units;) {
+      float acc[kBlock];
+#pragma unroll
+      for (int j = 0; j < kBlock; ++j) acc[j] = 0.f;
+      const bool mine = live > 32 * q && t.c0 + ch * kBlock < cols;  // of the warp's quarter and half
+      // What a k-block costs beside its products counts as much as they do (110 cycles a barrier whose
+      // answer is waited for, of 500): the next accumulator is asked for before this one is added, the
+      // scales' loads have no branch, and the loop is unrolled, so that a scale stays in the register that
+      // it is loaded into (a move would wait for it).
+      for (int kb0 = 0; ok && kb0 < t.nkb; kb0 += L) {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+          if (kb0 + i >= t.nkb) break;
+          if (!__all_sync(0xffffffffu, ready) &&
+              !__all_sync(0xffffffffu, mbar_wait_inline(&tfull[buf], bphase, wc, 32u))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t tb = tq + (uint32_t)(buf * C::kCols), free_bar = tempty0 + 8u * (uint32_t)buf;
+          buf ^= 1;
+          bphase ^= buf ^ 1u;
+          ready = mbar_test_wait(&tfull[buf], bphase);
+          if (mine) {
+            const float f = xs[i] * ws[i];
+#pragma unroll
+            for (int c = 0; c < kBlock; c += 32) {
+              uint32_t w[32];
+              tmem_ld16(tb + c, w);
+              tmem_ld16(tb + c + 16, w + 16);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) acc[c + j] = fmaf(__uint_as_float(w[j]), f, acc[c + j]);
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(free_bar);
+          const bool more = kb0 + i + L < t.nkb;
+          px += more ? a.M : 0;
+          pw += more ? wstep : 0;
+          xs[i] = *px;
+          ws[i] = *pw;
+        }
+      }
+      if (!ok) {
+#pragma unroll
+        for (int j = 0; j < kBlock; ++j) acc[j] = NAN;
+      }
+      // The warp's rows, 64 bytes of each at a time through shared memory (lane: row, then four lanes a row):
+      // pieces of 16 bytes whose place is exchanged by row.
+      const int last = live - 32 * q, col = t.c0 + ch * kBlock;
+      Out* const out = (Out*)a.out + (size_t)(row0 + 32 * q) * cols + col;
+      const bool store = mine;
+      u += step;
+      if (u < units) begin(u);  // (its scales come while this tile is stored)
+      if (!store) continue;
+      constexpr int kPer = 64 / sizeof(Out), kVec = 16 / sizeof(Out);
+#pragma unroll
+      for (int c = 0; c < kBlock; c += kPer) {
+        if (col + c >= cols) break;
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float* const v = acc + c + j * kVec;
+          uint4 p;
+          if (sizeof(Out) == 4)
+            p = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                           __float_as_uint(v[3]));
+          else
+            p = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4 % kVec], v[5 % kVec]),
+                           bf16x2(v[6 % kVec], v[7 % kVec]));
+          box[lane * 4 + (j ^ ((lane >> 1) & 3))] = p;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 8 * k + (lane >> 2), j = lane & 3, cc = c + j * kVec;
+          const uint4 v = box[r * 4 + (j ^ ((r >> 1) & 3))];
+          if (r >= last || col + cc >= cols) continue;
+          Out* const p = out + (size_t)r * cols + cc;
+          if (a.vec && col + cc + kVec <= cols) {
+            *(uint4*)p = v;
+          } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+              if (col + cc + i >= cols) break;
+              if (sizeof(Out) == 4) ((uint32_t*)p)[i] = w[i & 3];
+              else ((uint16_t*)p)[i] = (uint16_t)(w[i / 2 & 3] >> 16 * (i & 1));
+            }
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();  // neither CTA leaves while the other may still signal it
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc<true>(tmem_base, 512);
+}
+
 // -------------------------------------------------------------------------------- host side
+template <int MODE>
+cudaError_t run_wide(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, int out_dtype, int sms,
+                     cudaStream_t st) {
+  const int cols = MODE == kForward ? a.N : a.K;
+  const long long tiles = std::min((long long)a.M, (a.M + (long long)a.E * (Wide::kRows - 1)) / Wide::kRows) *
+                          ((cols + Wide::kCols - 1) / Wide::kCols);
+  const int pairs = (int)std::min<long long>(std::max(1, sms / 2), tiles);
+  auto go = [&](auto* kernel) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Wide::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kernel, dim3(2 * pairs), dim3(Wide::kThreads), Wide::kSmem, st, mw, mx, a);
+  };
+  return out_dtype == EAT_BF16 ? go(wide_kernel<MODE, __nv_bfloat16>) : go(wide_kernel<MODE, float>);
+}
+
 template <int MODE, int NT>
 cudaError_t run_nt(const CUtensorMap& ma, const CUtensorMap& mb, const Args& a, int out_dtype, int ctas,
                    cudaStream_t st) {
@@ -593,7 +944,8 @@ eat_status run(const char* fn, const void* x, const void* w, const Args& a, int 
   const int rows = MODE == kGrad ? a.N : (a.M + a.E - 1) / a.E;
   int nt = rows <= 16 ? 32 : rows <= 32 ? 64 : rows <= 64 ? 128 : 256;
   if (MODE == kGrad) nt = rows <= kBlock ? 128 : 256;  // (its operands come in columns of 128)
-  const int box = MODE == kGrad ? 32 : std::min(nt, 64);
+  const bool wide = MODE != kGrad && rows > kWideRows;
+  const int box = MODE == kGrad || wide ? 32 : std::min(nt, 64);
   CUtensorMap ma, mb;
   bool ok;
   if (MODE == kGrad)
@@ -602,6 +954,8 @@ eat_status run(const char* fn, const void* x, const void* w, const Args& a, int 
     ok = encode_bytes(&ma, 3, w, a.K, a.N, a.E, kBlock) &&
          encode_bytes(&mb, 2, x, MODE == kForward ? a.K : a.N, a.M, 1, box);
   if (!ok) return thread_fail(EAT_ERR_CUDA, "%s: tensor map", fn);
+  if constexpr (MODE != kGrad)
+    if (wide) return launched(fn, run_wide<MODE>(ma, mb, a, out_dtype, sms, st));
   const int cols = MODE == kForward ? a.N : a.K, col_tiles = (cols + kBlock - 1) / kBlock;
   const long long tiles =
       (MODE == kGrad ? (long long)a.E * ((a.N + nt - 1) / nt)

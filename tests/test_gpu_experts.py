@@ -241,7 +241,7 @@ def test_quant_rows_special():
 
 
 SPLITS = [[5], [0, 3, 0, 0, 130, 1], [128, 32, 33, 0, 257], [0, 0, 0], [31, 1, 127, 129, 0, 64] * 6,
-          [0] * 255 + [300], [1] * 256]
+          [0] * 255 + [300], [1] * 256, [300, 0, 17, 513, 1]]
 
 
 def _offsets(split):
