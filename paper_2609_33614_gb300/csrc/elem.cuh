@@ -54,19 +54,24 @@ struct Elem<__nv_bfloat16> {
   }
 };
 
-// N consecutive elements of a row as floats: in whole 16-byte vectors (N a multiple of kN, aligned), or
-// one by one, of which the first `left` exist (the others read as 0 and are not written).
-template <typename T, int N, bool VEC>
+// N elements of a row as floats: in whole 16-byte vectors (N a multiple of kN, aligned), or, where rows
+// begin anywhere, one by one and S apart (so that S lanes side by side read what lies side by side); of
+// the row's `left` > 0 from p on, those that do not exist read as 0 and are not written.
+template <typename T, int N, bool VEC, int S = 1>
 __device__ __forceinline__ void load_elems(const T* p, int left, float* v) {
   if (VEC) {
 #pragma unroll
     for (int j = 0; j < N; j += Elem<T>::kN) Elem<T>::unpack(*(const uint4*)(p + j), v + j);
   } else {
+    // (all loads, then their use: a load under a condition of its own would be waited for)
+    T t[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = j < left ? Elem<T>::get(p[j]) : 0.f;
+    for (int j = 0; j < N; ++j) t[j] = p[j * S < left ? j * S : 0];
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = j * S < left ? Elem<T>::get(t[j]) : 0.f;
   }
 }
-template <typename T, int N, bool VEC>
+template <typename T, int N, bool VEC, int S = 1>
 __device__ __forceinline__ void store_elems(T* p, int left, const float* v) {
   if (VEC) {
 #pragma unroll
@@ -74,24 +79,33 @@ __device__ __forceinline__ void store_elems(T* p, int left, const float* v) {
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (j < left) p[j] = Elem<T>::put(v[j]);
+      if (j * S < left) p[j * S] = Elem<T>::put(v[j]);
   }
 }
-
-// N = kN elements of a row as they were loaded (a 16-byte vector, four registers, where rows begin at
-// vectors), and as floats when they are needed.
+// Where lane l of S begins in a piece of S kN elements.
 template <typename T, bool VEC>
+__device__ __forceinline__ int lane_at(int l) {
+  return VEC ? l * Elem<T>::kN : l;
+}
+
+// kN elements of a row as they were loaded (a 16-byte vector, four registers, where rows begin at
+// vectors), and as floats when they are needed.
+template <typename T, bool VEC, int S>
 struct RowVec {
   static constexpr int kN = Elem<T>::kN;
   uint4 u;
-  float f[VEC ? 1 : kN];
-  // the elements from p on, of which the first `left` exist; zeros if not live
+  T f[VEC ? 1 : kN];
+  int n;  // of f
+  // the elements from p on, of which `left` exist; zeros if not live
   __device__ __forceinline__ void load(const T* p, int left, bool live) {
     if (VEC) {
       u = live && left > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
     } else {
+      n = live ? left : 0;
+      if (n > 0) {
 #pragma unroll
-      for (int j = 0; j < kN; ++j) f[VEC ? 0 : j] = live && j < left ? Elem<T>::get(p[j]) : 0.f;
+        for (int j = 0; j < kN; ++j) f[VEC ? 0 : j] = p[j * S < n ? j * S : 0];
+      }
     }
   }
   __device__ __forceinline__ void get(float* v) const {
@@ -99,7 +113,7 @@ struct RowVec {
       Elem<T>::unpack(u, v);
     } else {
 #pragma unroll
-      for (int j = 0; j < kN; ++j) v[j] = f[VEC ? 0 : j];
+      for (int j = 0; j < kN; ++j) v[j] = j * S < n ? Elem<T>::get(f[VEC ? 0 : j]) : 0.f;
     }
   }
 };
@@ -134,7 +148,7 @@ __device__ __forceinline__ uint32_t e4m3x4(const float* v) {
   return e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
 }
 // N = 4 or 8 bytes of a row.
-template <int N, bool VEC>
+template <int N, bool VEC, int S = 1>
 __device__ __forceinline__ void store_bytes(uint8_t* p, int left, const uint32_t* w) {
   if (VEC) {
     if (N == 8) *(uint2*)p = make_uint2(w[0], w[N / 4 - 1]);
@@ -142,23 +156,23 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, int left, const uint32_t
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (j < left) p[j] = (uint8_t)(w[j / 4] >> 8 * (j % 4));
+      if (j * S < left) p[j * S] = (uint8_t)(w[j / 4] >> 8 * (j % 4));
   }
 }
 // The same of quotients.
-template <int N, bool VEC>
+template <int N, bool VEC, int S = 1>
 __device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v) {
   uint32_t w[N / 4];
 #pragma unroll
   for (int j = 0; j < N / 4; ++j) w[j] = e4m3x4(v + 4 * j);
-  store_bytes<N, VEC>(p, left, w);
+  store_bytes<N, VEC, S>(p, left, w);
 }
-template <int N, bool VEC>
+template <int N, bool VEC, int S = 1>
 __device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v, const BlockDiv& div) {
   float t[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) t[j] = div(v[j]);
-  store_e4m3<N, VEC>(p, left, t);
+  store_e4m3<N, VEC, S>(p, left, t);
 }
 // The largest magnitude over groups of G lanes, in all of them.
 template <int G>

@@ -43,7 +43,7 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
   const long long unit = ((long long)blockIdx.x * kThreads + threadIdx.x) / G;
   const int kb = (int)(unit % blocks), l = threadIdx.x % G;
   const long long r0 = unit / blocks * kRows;
-  const int c = kb * kBlock + l * N, left = K - c;
+  const int c = kb * kBlock + lane_at<T, VEC>(l), left = K - c;
   const size_t pitch = GLU ? 2 * (size_t)K : (size_t)K;
   float s = 1.0f;  // lane l: of the l-th row
 #pragma unroll
@@ -53,8 +53,8 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
     for (int i = 0; i < U; ++i) {
       const long long r = r0 + i0 + i;
       if (r < M && left > 0) {
-        load_elems<T, N, VEC>(x + r * pitch + c, left, v[i]);
-        if (GLU) load_elems<T, N, VEC>(x + r * pitch + K + c, left, u[GLU ? i : 0]);
+        load_elems<T, N, VEC, G>(x + r * pitch + c, left, v[i]);
+        if (GLU) load_elems<T, N, VEC, G>(x + r * pitch + K + c, left, u[GLU ? i : 0]);
       }
     }
 #pragma unroll
@@ -65,12 +65,12 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           if (GLU) v[i][j] = v[i][j] * sigmoid(v[i][j]) * u[GLU ? i : 0][j];
-          if (VEC || j < left) top = fmaxf(top, fabsf(v[i][j]));
+          if (VEC || j * G < left) top = fmaxf(top, fabsf(v[i][j]));
         }
       }
       top = group_max<G>(top);
       const BlockDiv div(top);
-      if (r < M && left > 0) store_e4m3<N, VEC>(q + (size_t)r * K + c, left, v[i], div);
+      if (r < M && left > 0) store_e4m3<N, VEC, G>(q + (size_t)r * K + c, left, v[i], div);
       if (l == i0 + i) s = div.scale;
     }
   }
@@ -150,29 +150,29 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
   if (rb.n == 0) {  // rows behind the last expert's
     if (ROWS)
       for (int i = blockIdx.y; i < tiles; i += gridDim.y) {
-        const int c = i * kBlock + l * N, left = K - c;
+        const int c = i * kBlock + lane_at<T, VEC>(l), left = K - c;
         const float zero[N] = {};
 #pragma unroll
         for (int k = 0; k < R; ++k) {
           const int row = rb.row + r + k;
           if (row >= M) break;
-          if (left > 0) store_e4m3<N, VEC>(q + (size_t)row * K + c, left, zero);
+          if (left > 0) store_e4m3<N, VEC, L>(q + (size_t)row * K + c, left, zero);
           if (l == 0) scale[(size_t)i * M + row] = 1.0f;
         }
       }
     return;
   }
   // (a tile's rows are kept as they were loaded, and the next tile's come while this one is taken)
-  RowVec<T, VEC> in[R];
+  RowVec<T, VEC, L> in[R];
   auto load = [&](int i) {
-    const int c = i * kBlock + l * N;
+    const int c = i * kBlock + lane_at<T, VEC>(l);
 #pragma unroll
     for (int k = 0; k < R; ++k)
       in[k].load(x + (size_t)(rb.row + r + k) * K + c, K - c, r + k < rb.n && i < tiles);
   };
   load(blockIdx.y);
   for (int i = blockIdx.y; i < tiles; i += gridDim.y) {
-    const int c = i * kBlock + l * N, left = K - c;
+    const int c = i * kBlock + lane_at<T, VEC>(l), left = K - c;
     float top[N] = {};
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -187,7 +187,7 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
         const BlockDiv div(group_max<L>(t));
         if (r + k >= rb.n) continue;
         const size_t row = rb.row + r + k;
-        if (left > 0) store_e4m3<N, VEC>(q + row * K + c, left, v, div);
+        if (left > 0) store_e4m3<N, VEC, L>(q + row * K + c, left, v, div);
         if (l == 0) scale[(size_t)i * M + row] = div.scale;
       }
     }
@@ -196,7 +196,7 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
 #pragma unroll
       for (int o = 16; o >= L; o >>= 1)
         top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
-      if (lane < L) s_top[warp][lane * N + j] = top[j];
+      if (lane < L) s_top[warp][lane_at<T, VEC>(lane) + (VEC ? j : j * L)] = top[j];
     }
     __syncthreads();
     if (threadIdx.x < kBlock) {
@@ -213,8 +213,9 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
     float fs[N], fr[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      fs[j] = s_scale[l * N + j];
-      fr[j] = s_recip[l * N + j];
+      const int at = lane_at<T, VEC>(l) + (VEC ? j : j * L);
+      fs[j] = s_scale[at];
+      fr[j] = s_recip[at];
     }
     uint32_t w[R][N / 4];
 #pragma unroll
@@ -230,7 +231,7 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
 #pragma unroll
     for (int k = 0; k < R; ++k)
       if (r + k < out_rows && left > 0)
-        store_bytes<N, VEC>(cq + (size_t)(rb.padded + r + k) * K + c, left, w[k]);
+        store_bytes<N, VEC, L>(cq + (size_t)(rb.padded + r + k) * K + c, left, w[k]);
   }
 }
 
@@ -248,8 +249,8 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
   const int n_blocks = (n_rows + kBlock - 1) / kBlock, nb = blockIdx.y;
   const size_t e = blockIdx.z, at = e * n_rows * K;
   const int l = threadIdx.x % L, r = threadIdx.x / L * R;
-  const int c = kb * kBlock + l * N, left = K - c, row0 = nb * kBlock + r;
-  RowVec<T, VEC> in[R];
+  const int c = kb * kBlock + lane_at<T, VEC>(l), left = K - c, row0 = nb * kBlock + r;
+  RowVec<T, VEC, L> in[R];
   float top = 0.f;
 #pragma unroll
   for (int k = 0; k < R; ++k)
@@ -273,7 +274,7 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
     float v[N];
     in[k].get(v);
     if (row0 + k < n_rows && left > 0)
-      store_e4m3<N, VEC>(q + at + (size_t)(row0 + k) * K + c, left, v, div);
+      store_e4m3<N, VEC, L>(q + at + (size_t)(row0 + k) * K + c, left, v, div);
   }
 }
 
@@ -396,9 +397,10 @@ extern "C" eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int
                      : (vec ? quant_columns_kernel<T, true, false>
                             : quant_columns_kernel<T, false, false>);
     // (one more block than the experts can have: the rows behind them)
-    // several tiles a block where there are blocks enough
-    const long long all = (long long)(blocks + 1) * tiles;
-    const int per = (int)std::max(1LL, std::min((long long)kTilesOfBlock, all / (4LL * num_sms())));
+    // several tiles a block where there are more than run at a time (a block's life is mostly latency:
+    // 24 rows of 64 experts, 2048 columns: MEASURED)
+    const long long all = (long long)(blocks + 1) * tiles, run = 2LL * num_sms();
+    const int per = (int)std::min((long long)kTilesOfBlock, (all + run - 1) / run);
     return launch_pdl(kernel, dim3(blocks + 1, (tiles + per - 1) / per), dim3(kTileThreads), 0,
                       (cudaStream_t)stream, (const T*)x, M, K, offsets, E, (int)padded, blocks, tiles,
                       (uint8_t*)q, scale, (uint8_t*)cq, cscale);

@@ -225,7 +225,7 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
   pdl_launch_dependents();
   const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31, t = (int)(w / pieces);
-  const int c0 = (int)(w % pieces) * 32 * N * U + lane * N;
+  const int c0 = (int)(w % pieces) * 32 * N * U + lane / G * kBlock + lane_at<T, VEC>(lane % G);
   if (t >= tokens) return;
   const int M = tokens * K, used = rows_used(offsets, E, M);
   const int mine = lane < K ? slot[(size_t)t * K + lane] : -1;
@@ -234,7 +234,7 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
   for (int i = 0; i < U; ++i) {
     const int c = c0 + 32 * N * i;
     float top = 0.f;
-    if (c < d) load_elems<T, N, VEC>(x + (size_t)t * d + c, d - c, v[i]);
+    if (c < d) load_elems<T, N, VEC, G>(x + (size_t)t * d + c, d - c, v[i]);
     if (c < d)
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[i][j]));
@@ -251,7 +251,7 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
     for (int i = 0; i < U; ++i) {
       const int c = c0 + 32 * N * i;
       if (c >= d) continue;
-      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, v[i]);
+      store_e4m3<N, VEC, G>(q + (size_t)r * d + c, d - c, v[i]);
       if (lane % G == 0) scale[(size_t)(c / kBlock) * M + r] = s[i];
     }
   }
@@ -261,18 +261,18 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
     for (int i = 0; i < U; ++i) {
       const int c = c0 + 32 * N * i;
       if (c >= d) continue;
-      store_e4m3<N, VEC>(q + (size_t)r * d + c, d - c, zero);
+      store_e4m3<N, VEC, G>(q + (size_t)r * d + c, d - c, zero);
       if (lane % G == 0) scale[(size_t)(c / kBlock) * M + r] = 1.0f;
     }
   }
 }
 
-// y[t]: a warp takes a vector a lane of one token at a time, all of its rows' loads before their use, and
+// y[t]: a warp takes V vectors a lane of one token at a time, the loads of kAhead rows before their use, and
 // loads the next token's slots meanwhile.
-constexpr int kAhead = 4;          // rows
-constexpr int kCombineBlocks = 6;  // of an SM
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(32 * kWarps, VEC ? kCombineBlocks : 1)
+constexpr int kAhead = 4;  // rows
+constexpr int combine_blocks(int V) { return V == 2 ? 3 : 4; }  // of an SM
+template <typename T, bool VEC, int V>
+__global__ void __launch_bounds__(32 * kWarps, VEC ? combine_blocks(V) : 1)
 combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
                const float* __restrict__ weight, int tokens, int K, int d, int pieces,
                T* __restrict__ y) {
@@ -296,7 +296,8 @@ combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
   };
   prefetch();
   while (nt < tokens) {
-    const int mine = next < M ? next : -1, t = nt, c = (np * 32 + lane) * N, left = d - c;
+    const int mine = next < M ? next : -1, t = nt;
+    const int c = np * (32 * N * V) + lane_at<T, VEC>(lane), left = d - c;
     const float wt = next_wt;
     nt += dt;
     np += dp;
@@ -305,26 +306,34 @@ combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
       ++nt;
     }
     prefetch();
-    float sum[N] = {};
+    float sum[V][N] = {};
     for (int k0 = 0; k0 < K; k0 += kAhead) {
-      RowVec<T, VEC> in[kAhead];
+      RowVec<T, VEC, 32> in[kAhead][V];
+      int r[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
-        in[k].load(rows + (size_t)max(r, 0) * d + c, left, r >= 0);
+        r[k] = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+        const T* const p = rows + (size_t)max(r[k], 0) * d + c;
+#pragma unroll
+        for (int i = 0; i < V; ++i) in[k][i].load(p + i * 32 * N, left - i * 32 * N, r[k] >= 0);
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
         const float f = __shfl_sync(0xffffffffu, wt, (k0 + k) & 31);
-        float v[N];
-        in[k].get(v);
-        if (r < 0) continue;
+        if (r[k] < 0) continue;
 #pragma unroll
-        for (int j = 0; j < N; ++j) sum[j] = fmaf(f, v[j], sum[j]);
+        for (int i = 0; i < V; ++i) {
+          float v[N];
+          in[k][i].get(v);
+#pragma unroll
+          for (int j = 0; j < N; ++j) sum[i][j] = fmaf(f, v[j], sum[i][j]);
+        }
       }
     }
-    if (left > 0) store_elems<T, N, VEC>(y + (size_t)t * d + c, left, sum);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (left > i * 32 * N)
+        store_elems<T, N, VEC, 32>(y + (size_t)t * d + c + i * 32 * N, left - i * 32 * N, sum[i]);
   }
 }
 
@@ -347,35 +356,35 @@ combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ rows,
   float part = 0.f;  // lane k's: the warp's part of dw[t][k]
   for (int k0 = 0; k0 < K; k0 += kAhead) {
     float dot[kAhead] = {};
-    for (int c = threadIdx.x * N; c - lane * N < d; c += blockDim.x * N) {
-      const int left = d - c;
-      RowVec<T, VEC> own, in[kAhead];
+    for (int c0 = warp * 32 * N; c0 < d; c0 += blockDim.x * N) {
+      const int c = c0 + lane_at<T, VEC>(lane), left = d - c;
+      RowVec<T, VEC, 32> own, in[kAhead];
+      int r[kAhead];
       own.load(dy + (size_t)t * d + c, left, true);
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
-        in[k].load(rows + (size_t)max(r, 0) * d + c, left, r >= 0);
+        r[k] = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
+        in[k].load(rows + (size_t)max(r[k], 0) * d + c, left, r[k] >= 0);
       }
       float g[N];
       own.get(g);
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int r = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
         const float f = __shfl_sync(0xffffffffu, wt, (k0 + k) & 31);
+        if (r[k] < 0 || left <= 0) continue;
         float v[N], o[N];
         in[k].get(v);
-        if (r < 0 || left <= 0) continue;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           dot[k] = fmaf(g[j], v[j], dot[k]);
           o[j] = f * g[j];
         }
-        store_elems<T, N, VEC>(drows + (size_t)r * d + c, left, o);
+        store_elems<T, N, VEC, 32>(drows + (size_t)r[k] * d + c, left, o);
       }
       if (k0 == 0 && left > 0) {
         const float zero[N] = {};
         for (long long r = (long long)used + t; r < M; r += tokens)
-          store_elems<T, N, VEC>(drows + (size_t)r * d + c, left, zero);
+          store_elems<T, N, VEC, 32>(drows + (size_t)r * d + c, left, zero);
       }
     }
     // lanes exchange the halves that they do not keep: lane l ends with the sum of the (l % kAhead)-th
@@ -520,12 +529,21 @@ extern "C" eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K,
     using X = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<X>::kN;
     const bool vec = d % N == 0 && !misaligned(rows, 16) && !misaligned(y, 16);
-    const int pieces = (d + 32 * N - 1) / (32 * N);
-    // (as many blocks as run at a time, so that a warp has a next token)
-    const unsigned most = (unsigned)(kCombineBlocks * num_sms()), all = warp_grid((long long)T * pieces).x;
-    return launch_pdl(vec ? combine_kernel<X, true> : combine_kernel<X, false>, dim3(std::min(most, all)),
-                      dim3(32 * kWarps), 0, (cudaStream_t)stream, (const X*)rows, slot, w, T, K, d,
-                      pieces, (X*)y);
+    auto go = [&](auto two) {
+      constexpr int V = decltype(two)::value;
+      const int pieces = (d + 32 * N * V - 1) / (32 * N * V);
+      // (as many blocks as run at a time, so that a warp has a next token)
+      const unsigned most = (unsigned)(combine_blocks(V) * num_sms());
+      const unsigned all = warp_grid((long long)T * pieces).x;
+      return launch_pdl(vec ? combine_kernel<X, true, V> : combine_kernel<X, false, V>,
+                        dim3(std::min(most, all)), dim3(32 * kWarps), 0, (cudaStream_t)stream,
+                        (const X*)rows, slot, w, T, K, d, pieces, (X*)y);
+    };
+    // Two vectors a lane where that still leaves every SM its warps: half the steps that go with a row, not
+    // its elements (8191 tokens x 8 of 2048: MEASURED)
+    const bool two = vec && d > 32 * N &&
+                     (long long)T * ((d + 64 * N - 1) / (64 * N)) >= 16LL * kWarps * num_sms();
+    return two ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 1>());
   };
   return launched(fn, dtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr));
 }
