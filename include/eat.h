@@ -440,7 +440,8 @@ eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* st
  * selections of experts below e; slot [T, K]: the row of selection (t, k) among the sorted ones (those
  * of an expert in the order of t, then k), or -1.  A token may select an expert more than once.
  * work: eat_expert_sort_workspace(T, K, E) bytes of device memory, 16-byte aligned, whose contents do
- * not matter; the call may use it until it has finished on `stream`. */
+ * not matter; the call may use it until it has finished on `stream`.  0 bytes up to T K = 131072: work may
+ * then be NULL. */
 eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, int32_t E, const uint8_t* mask,
                            int32_t* offsets, int32_t* slot, void* work, void* stream);
 int64_t eat_expert_sort_workspace(int32_t T, int32_t K, int32_t E);
@@ -467,8 +468,9 @@ eat_status eat_expert_combine_grad(const void* dy, const void* rows, int32_t T, 
 
 /* e4m3 with a scale for each 128 elements of a row.  x [M, K] fp32 or bf16 (dtype); q [M, K] bytes;
  * scale [ceil(K / 128)][M] fp32: element k of row r is scale[k / 128][r] * (its byte), and the scale is
- * the largest magnitude / 448 (1, and bytes 0, where that is not above 1e-35).  A block that holds an
- * infinity reads as NaN; a NaN leaves the others of its block as they are.
+ * the largest magnitude / 448, to within 2^-23 of itself (1, and bytes 0, where that magnitude is not above
+ * 1e-35).  A byte is the fp32 quotient by the scale, rounded.  A block that holds an infinity reads as NaN;
+ * a NaN leaves the others of its block as they are.
  * 1 <= M <= 2^30, 1 <= K <= 65536. */
 eat_status eat_quant_rows(const void* x, int32_t M, int32_t K, int32_t dtype, void* q, float* scale,
                           void* stream);
@@ -500,7 +502,9 @@ eat_status eat_quant_tiles(const void* w, int32_t E, int32_t N, int32_t K, int32
  * y in ydtype, EAT_BF16 or EAT_F32.  Sums are fp32: those of a block of 128 on the tensor cores, scaled
  * and added to each other in order.  Rows of x behind an expert's own never reach its outputs.
  * K, and with transposed N, are multiples of 16 (EAT_ERR_UNSUPPORTED otherwise); N, K <= 65536; xq and
- * wq 16-byte aligned.  y overlaps no input. */
+ * wq 16-byte aligned.  y overlaps no input.
+ * Where a kernel gives up on a bounded wait (see EAT_ERR_STATE), the outputs that it has not finished are
+ * NaN; no handle keeps a state of it. */
 eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const float* ws,
                         const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
                         int32_t transposed, void* y, int32_t ydtype, void* stream);
@@ -509,7 +513,7 @@ eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const f
  * operands as eat_quant_columns makes them with the same offsets: gq [rows, N], gs [blocks][N], xq
  * [rows, K], xs [blocks][K], rows and blocks being eat_quant_columns_rows and _blocks.  Zeros for an
  * expert without rows.  offsets NULL with E = 1: one expert with `rows` rows (those that pad add
- * nothing).  N and K are multiples of 16; gq and xq 16-byte aligned. */
+ * nothing).  N and K are multiples of 16; gq and xq 16-byte aligned; dw overlaps no input; waits as above. */
 eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq, const float* xs,
                              const int32_t* offsets, int32_t E, int32_t rows, int32_t blocks,
                              int32_t N, int32_t K, void* dw, int32_t dtype, void* stream);

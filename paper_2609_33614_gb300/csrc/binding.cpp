@@ -289,10 +289,12 @@ PyObject* expert_sort(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t T32 = to_i32("T", T), K32 = to_i32("K", K);
     at::Tensor offsets = empty({std::min(std::max(E, 0), 256) + 1}, at::kInt, idx);
     at::Tensor slot = empty(idx.sizes(), at::kInt, idx);
-    at::Tensor work = empty({eat_expert_sort_workspace(T32, K32, E)}, at::kByte, idx);
+    const int64_t bytes = eat_expert_sort_workspace(T32, K32, E);
+    at::Tensor work;
+    if (bytes > 0) work = empty({bytes}, at::kByte, idx);
     ok(eat_expert_sort((const int32_t*)idx.const_data_ptr(), T32, K32, E, mask,
-                       (int32_t*)offsets.data_ptr(), (int32_t*)slot.data_ptr(), work.data_ptr(),
-                       stream_of(idx)));
+                       (int32_t*)offsets.data_ptr(), (int32_t*)slot.data_ptr(),
+                       bytes > 0 ? work.data_ptr() : nullptr, stream_of(idx)));
     return results(offsets, slot);
   });
 }

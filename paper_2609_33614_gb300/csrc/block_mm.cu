@@ -4,25 +4,32 @@
 //   y[r][k]  = the same with w as it lies, summed over n (transposed: the gradient to x)
 //   dw[n][k] = sum_b gs[b][n] xs[b][k] sum_{r in b} g[r][n] x[r][k], b the blocks of 128 rows of an expert
 //
-// A tile of the output is up to NT of its rows x 128 of its columns, as the transposed product: the 128
-// columns (w's; dw: x's) are the MMA's M, the rows (x's; dw: g's) its N.  So a matrix is read once for up
-// to NT rows of x, however few there are, and an expert's rows are cut into tiles of equal heights.
-// A k-block of 128 is four MMAs into an accumulator of its own in TMEM; the epilogue's warps read it,
-// multiply by the block's scales and add it to fp32 sums in registers while the next k-blocks run.  In
-// the 16x256b layout a thread has two neighbouring rows of the output for each of its columns, so a
-// scale's pair is one load.
+// A k-block of 128 is up to four MMAs into an accumulator of its own in TMEM; the epilogue's warps read it,
+// multiply by the block's scales and add it to fp32 sums in registers while the next k-blocks run.
+//   block_mm_kernel: a tile of the output is up to NT of its rows x 128 of its columns, as the transposed
+//      product: the 128 columns (w's; dw: x's) are the MMA's M, the rows (x's; dw: g's) its N.  So a matrix
+//      is read once for up to NT rows of x, however few there are, and an expert's rows are cut into
+//      tiles of equal heights.  In the 16x256b layout a thread has two neighbouring rows of the output for each
+//      of its columns, so a scale's pair is one load.  Bound: HBM with few rows an expert (1 token, 2 of 8
+//      matrices of 28672 x 4096: 41 us, 5.7 TB/s; 32 tokens, 8 of 64 of 2048 x 2048: 42 us, 6.4 TB/s); dw
+//      of 18432 rows, 64 matrices of 2048 x 2048: 230 us, of which writing dw is 79.
+//   wide_kernel: on SM pairs, 256 rows (M) x 256 columns (N), for many rows an expert: half the operand bytes
+//      from L2 for each MMA, and a k-block's scales are one product a thread.  Bound: the accumulator's way
+//      through TMEM (two buffers: an MMA of 530 cycles, then 500 of reading and adding, then the
+//      hand-over).  8192 x 2048 x 8192: 137 us, 2.0 PFLOP/s; 10240 rows, 60 matrices of 2816 x 2048: 113 us.
 // Operands come by TMA as they lie (K-major, or MN-major where the sum runs over their rows): w serves
 // both directions, and the gradient reads both operands by rows.
-// Warps: 0 issues TMA, 1 owns TMEM and issues MMAs, 2 copies the blocks' scales into a ring and clears
-// the rows behind the last expert's, the others drain TMEM.  Every wait is bounded; where one expires
-// the CTA's tiles that are not done become NaN, copies and MMAs land, TMEM is freed and the kernel ends.
+// Warps: 0 issues TMA, 1 owns TMEM and issues MMAs, 2 copies the blocks' scales into a ring (block_mm_kernel)
+// and clears the rows behind the last expert's, the others drain TMEM.  Every wait is bounded; where one
+// expires the CTA's tiles that are not done become NaN, copies and MMAs land, TMEM is freed and the kernel ends.
 #include "elem.cuh"
 #include "op_checks.cuh"
 #include "tc_ptx.cuh"
 
-#include <algorithm>
-
 #include "tensor_map.cuh"
+
+#include <algorithm>
+#include <atomic>
 
 namespace eat {
 
@@ -305,18 +312,19 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 
   const int cols = MODE == kForward ? a.N : a.K, inner = MODE == kForward ? a.K : a.N;
   const int col_tiles = (cols + kBlock - 1) / kBlock;
-  const int n_tiles = (a.N + NT - 1) / NT;  // kGrad
+  const int n_tiles = (a.N + NT - 1) / NT;  // kGrad, and their rows
+  const int grad_rows = ((a.N + n_tiles - 1) / n_tiles + 15) & ~15;
   const long long units = (long long)(MODE == kGrad ? a.E * n_tiles : ex.tile0[a.E]) * col_tiles;
   auto tile_at = [&](long long u) {
     Tile t;
     if (MODE == kGrad) {
-      const int per = n_tiles * col_tiles;
-      t.e = (int)(u / per);
-      const int v = (int)(u - (long long)t.e * per);
-      const int h = ((a.N + n_tiles - 1) / n_tiles + 15) & ~15;
-      t.row0 = v % n_tiles * h;
-      t.rows = max(0, min(h, a.N - t.row0));
-      t.c0 = v / n_tiles * kBlock;
+      // (below 2^25 tiles: 32-bit divisions)
+      const unsigned per = n_tiles * col_tiles, e = (unsigned)u / per, v = (unsigned)u - e * per;
+      const unsigned c = v / (unsigned)n_tiles, i = v - c * n_tiles;
+      t.e = (int)e;
+      t.row0 = (int)i * grad_rows;
+      t.rows = min(grad_rows, a.N - t.row0);
+      t.c0 = (int)c * kBlock;
       t.sums = ex.end[t.e];
       t.k0 = ex.row[t.e];
       t.b0 = ex.tile0[t.e];
@@ -328,148 +336,148 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   };
 
   if (warp < kFirstEpi) {
-  if constexpr (C::kFewRegs > 0)
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kFewRegs));
-  if (warp == 0) {
-    if (elect_one()) {
-      int stage = 0;
-      uint32_t phase = 0;
-      long long issued = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
-        const Tile t = tile_at(u);
-        for (int kb = 0; kb < t.nkb; ++kb) {
-          if (!mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
-            ok = false;
-            break;
-          }
-          uint8_t* const sa = smem + stage * C::kStage;
-          uint8_t* const sb = sa + kOperand;
-          uint64_t* const bar = &full[stage];
-          if (MODE == kGrad) {
-            const int k = t.k0 + kb * kBlock, boxes = (min(kBlock, t.sums - kb * kBlock) + 31) / 32;
-            const int chunks = (t.rows + kBlock - 1) / kBlock;
-            mbar_expect_tx(bar, (1 + chunks) * boxes * 32 * kBlock);
-            for (int i = 0; i < boxes; ++i) {
-              tma_load(sa + i * 32 * kBlock, &map_a, bar, t.c0, k + 32 * i);
-              for (int c = 0; c < chunks; ++c)
-                tma_load(sb + c * kOperand + i * 32 * kBlock, &map_b, bar, t.row0 + c * kBlock, k + 32 * i);
+    if constexpr (C::kFewRegs > 0)
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kFewRegs));
+    if (warp == 0) {
+      if (elect_one()) {
+        int stage = 0;
+        uint32_t phase = 0;
+        long long issued = 0;
+        bool ok = true;
+        for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+          const Tile t = tile_at(u);
+          for (int kb = 0; kb < t.nkb; ++kb) {
+            if (!mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
+              ok = false;
+              break;
             }
-          } else {
-            const int k = kb * kBlock, boxes = (t.rows + C::kBox - 1) / C::kBox;
-            mbar_expect_tx(bar, kOperand + boxes * C::kBox * kBlock);
-            if (MODE == kForward) tma_load_3d(sa, &map_a, bar, k, t.c0, t.e);
-            else tma_load_3d(sa, &map_a, bar, t.c0, k, t.e);
-            for (int i = 0; i < boxes; ++i)
-              tma_load(sb + i * C::kBox * kBlock, &map_b, bar, k, t.row0 + i * C::kBox);
-          }
-          ++issued;
-          if (++stage == S) {
-            stage = 0;
-            phase ^= 1u;
+            uint8_t* const sa = smem + stage * C::kStage;
+            uint8_t* const sb = sa + kOperand;
+            uint64_t* const bar = &full[stage];
+            if (MODE == kGrad) {
+              const int k = t.k0 + kb * kBlock, boxes = (min(kBlock, t.sums - kb * kBlock) + 31) / 32;
+              const int chunks = (t.rows + kBlock - 1) / kBlock;
+              mbar_expect_tx(bar, (1 + chunks) * boxes * 32 * kBlock);
+              for (int i = 0; i < boxes; ++i) {
+                tma_load(sa + i * 32 * kBlock, &map_a, bar, t.c0, k + 32 * i);
+                for (int c = 0; c < chunks; ++c)
+                  tma_load(sb + c * kOperand + i * 32 * kBlock, &map_b, bar, t.row0 + c * kBlock, k + 32 * i);
+              }
+            } else {
+              const int k = kb * kBlock, boxes = (t.rows + C::kBox - 1) / C::kBox;
+              mbar_expect_tx(bar, kOperand + boxes * C::kBox * kBlock);
+              if (MODE == kForward) tma_load_3d(sa, &map_a, bar, k, t.c0, t.e);
+              else tma_load_3d(sa, &map_a, bar, t.c0, k, t.e);
+              for (int i = 0; i < boxes; ++i)
+                tma_load(sb + i * C::kBox * kBlock, &map_b, bar, k, t.row0 + i * C::kBox);
+            }
+            ++issued;
+            if (++stage == S) {
+              stage = 0;
+              phase ^= 1u;
+            }
           }
         }
+        // copies in flight land before the CTA may exit
+        for (long long i = issued > S ? issued - S : 0; i < issued; ++i)
+          mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), wc, 2u, false);
       }
-      // copies in flight land before the CTA may exit
-      for (long long i = issued > S ? issued - S : 0; i < issued; ++i)
-        mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), wc, 2u, false);
-    }
-  } else if (warp == 1) {
-    if (elect_one()) {
-      int stage = 0, buf = 0;
-      uint32_t phase = 0, bphase = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
-        const Tile t = tile_at(u);
-        const uint32_t id = idesc(true, kBlock, (t.rows + 15) & ~15, MODE != kForward, MODE == kGrad);
-        for (int kb = 0; kb < t.nkb; ++kb) {
-          if (!both(&full[stage], phase, &tempty[buf], bphase ^ 1u, wc)) {
-            ok = false;
-            break;
+    } else if (warp == 1) {
+      if (elect_one()) {
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, bphase = 0;
+        bool ok = true;
+        for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+          const Tile t = tile_at(u);
+          const uint32_t id = idesc(true, kBlock, (t.rows + 15) & ~15, MODE != kForward, MODE == kGrad);
+          for (int kb = 0; kb < t.nkb; ++kb) {
+            if (!both(&full[stage], phase, &tempty[buf], bphase ^ 1u, wc)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem + stage * C::kStage);
+            const uint64_t da = MODE == kForward ? sdesc_k(sa) : sdesc_mn8(sa);
+            const uint64_t db = MODE == kGrad ? sdesc_mn8(sa + kOperand) : sdesc_k(sa + kOperand);
+            const uint32_t d = tmem_base + (uint32_t)(buf * NT);
+            const int steps = (min(kBlock, t.sums - kb * kBlock) + 31) / 32;
+            for (int k = 0; k < steps; ++k)
+              mma<false, true>(d, da + k * (MODE == kForward ? 2 : 256), db + k * (MODE == kGrad ? 256 : 2),
+                               id, k > 0);
+            mma_commit<false>(&empty[stage]);
+            mma_commit<false>(&tfull[buf]);
+            if (++stage == S) {
+              stage = 0;
+              phase ^= 1u;
+            }
+            if (++buf == B) {
+              buf = 0;
+              bphase ^= 1u;
+            }
           }
-          tc_fence_after();
-          const uint32_t sa = smem_u32(smem + stage * C::kStage);
-          const uint64_t da = MODE == kForward ? sdesc_k(sa) : sdesc_mn8(sa);
-          const uint64_t db = MODE == kGrad ? sdesc_mn8(sa + kOperand) : sdesc_k(sa + kOperand);
-          const uint32_t d = tmem_base + (uint32_t)(buf * NT);
-          const int steps = (min(kBlock, t.sums - kb * kBlock) + 31) / 32;
-          for (int k = 0; k < steps; ++k)
-            mma<false, true>(d, da + k * (MODE == kForward ? 2 : 256), db + k * (MODE == kGrad ? 256 : 2),
-                             id, k > 0);
-          mma_commit<false>(&empty[stage]);
-          mma_commit<false>(&tfull[buf]);
-          if (++stage == S) {
-            stage = 0;
-            phase ^= 1u;
-          }
+        }
+        mma_commit<false>(&mma_done);  // no MMA may run when TMEM is freed
+      }
+      if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+    } else if (warp == 2) {
+      Behind<Out> behind(a, ex, cols, MODE != kGrad);
+      // The copies of k-block i are issued kAhead before those of i - kAhead are handed over, which is once
+      // the accumulator that goes with them is free: then so is the slot that comes kBufs before it.
+      long long u = blockIdx.x;
+      Tile t{};
+      int kb = 0, copy = 0, buf = 0;
+      uint32_t bphase = 0;
+      auto next = [&] {  // the tile of the next k-block to copy; false behind the last
+        while (kb == t.nkb) {
+          if (u >= units) return false;
+          t = tile_at(u);
+          u += gridDim.x;
+          kb = 0;
+        }
+        return true;
+      };
+      const int nb = (a.N + kBlock - 1) / kBlock, kbs = (a.K + kBlock - 1) / kBlock;
+      int pending = 0;
+      for (int i = 0;; ++i) {
+        if (i >= kAhead) {
+          if (pending == 0) break;
+          cp_async_wait<kAhead - 1>();
+          __syncwarp();
+          if (!warp_wait(&tempty[buf], bphase ^ 1u, wc, 64u)) break;
+          if (lane == 0) mbar_arrive(&tfull[buf]);
+          --pending;
           if (++buf == B) {
             buf = 0;
             bphase ^= 1u;
           }
         }
-      }
-      mma_commit<false>(&mma_done);  // no MMA may run when TMEM is freed
-    }
-    if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
-  } else if (warp == 2) {
-    Behind<Out> behind(a, ex, cols, MODE != kGrad);
-    // The copies of k-block i are issued kAhead before those of i - kAhead are handed over, which is once
-    // the accumulator that goes with them is free: then so is the slot that comes kBufs before it.
-    long long u = blockIdx.x;
-    Tile t{};
-    int kb = 0, copy = 0, buf = 0;
-    uint32_t bphase = 0;
-    auto next = [&] {  // the tile of the next k-block to copy; false behind the last
-      while (kb == t.nkb) {
-        if (u >= units) return false;
-        t = tile_at(u);
-        u += gridDim.x;
-        kb = 0;
-      }
-      return true;
-    };
-    const int nb = (a.N + kBlock - 1) / kBlock, kbs = (a.K + kBlock - 1) / kBlock;
-    int pending = 0;
-    for (int i = 0;; ++i) {
-      if (i >= kAhead) {
-        if (pending == 0) break;
-        cp_async_wait<kAhead - 1>();
-        __syncwarp();
-        if (!warp_wait(&tempty[buf], bphase ^ 1u, wc, 64u)) break;
-        if (lane == 0) mbar_arrive(&tfull[buf]);
-        --pending;
-        if (++buf == B) {
-          buf = 0;
-          bphase ^= 1u;
-        }
-      }
-      if (next()) {
-        const uint32_t dst = smem_u32(s_scale + copy * C::kSlotFloats);
-        const float* rs =
-            (MODE == kGrad ? a.xs + (size_t)(t.b0 + kb) * a.N : a.xs + (size_t)kb * a.M) + t.row0;
+        if (next()) {
+          const uint32_t dst = smem_u32(s_scale + copy * C::kSlotFloats);
+          const float* rs =
+              (MODE == kGrad ? a.xs + (size_t)(t.b0 + kb) * a.N : a.xs + (size_t)kb * a.M) + t.row0;
 #pragma unroll
-        for (int j = 0; j < NT; j += 32)
-          if (j + lane < t.rows) cp_async4(dst + (j + lane) * 4, rs + j + lane);
-        if (MODE == kGrad) {
-          const float* cs = a.ws + (size_t)(t.b0 + kb) * a.K;
+          for (int j = 0; j < NT; j += 32)
+            if (j + lane < t.rows) cp_async4(dst + (j + lane) * 4, rs + j + lane);
+          if (MODE == kGrad) {
+            const float* cs = a.ws + (size_t)(t.b0 + kb) * a.K;
 #pragma unroll
-          for (int j = 0; j < kBlock; j += 32)
-            cp_async4(dst + (NT + j + lane) * 4, cs + min(t.c0 + j + lane, a.K - 1));
-        } else if (lane == 0) {
-          const size_t at = MODE == kForward ? ((size_t)t.e * nb + t.c0 / kBlock) * kbs + kb
-                                             : ((size_t)t.e * nb + kb) * kbs + t.c0 / kBlock;
-          cp_async4(dst + NT * 4, a.ws + at);
+            for (int j = 0; j < kBlock; j += 32)
+              cp_async4(dst + (NT + j + lane) * 4, cs + min(t.c0 + j + lane, a.K - 1));
+          } else if (lane == 0) {
+            const size_t at = MODE == kForward ? ((size_t)t.e * nb + t.c0 / kBlock) * kbs + kb
+                                               : ((size_t)t.e * nb + kb) * kbs + t.c0 / kBlock;
+            cp_async4(dst + NT * 4, a.ws + at);
+          }
+          ++kb;
+          ++pending;
+          if (++copy == C::kSlots) copy = 0;
         }
-        ++kb;
-        ++pending;
-        if (++copy == C::kSlots) copy = 0;
+        cp_async_commit();  // (one group an iteration, whether it holds a copy or not)
+        if (MODE != kGrad) behind.clear(8);
       }
-      cp_async_commit();  // (one group an iteration, whether it holds a copy or not)
-      if (MODE != kGrad) behind.clear(8);
+      if (MODE != kGrad) behind.clear(1 << 30);
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
-    if (MODE != kGrad) behind.clear(1 << 30);
-    asm volatile("cp.async.wait_all;" ::: "memory");
-  }
   } else {
     if constexpr (C::kManyRegs > 0)
       asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kManyRegs));
@@ -903,6 +911,18 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
 }
 
 // -------------------------------------------------------------------------------- host side
+// Whether a kernel was launched with the registers that its warps share out (setmaxnreg would wait for the
+// rest forever).  Once per kernel: it is a property of the code.
+template <typename K>
+cudaError_t shares_registers(K* kernel, int threads, int few, int many) {
+  cudaFuncAttributes at;
+  const cudaError_t e = cudaFuncGetAttributes(&at, kernel);
+  if (e != cudaSuccess || few == 0) return e;
+  const int first = 32 * kFirstEpi;
+  return at.numRegs * threads >= few * first + many * (threads - first) ? cudaSuccess
+                                                                      : cudaErrorInvalidKernelImage;
+}
+
 template <int MODE>
 cudaError_t run_wide(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, int out_dtype, int sms,
                      cudaStream_t st) {
@@ -911,8 +931,15 @@ cudaError_t run_wide(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a
                           ((cols + Wide::kCols - 1) / Wide::kCols);
   const int pairs = (int)std::min<long long>(std::max(1, sms / 2), tiles);
   auto go = [&](auto* kernel) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Wide::kSmem);
+    static std::atomic<bool> seen[2];
+    std::atomic<bool>& checked = seen[out_dtype == EAT_BF16];
+    cudaError_t e = cudaSuccess;
+    if (!checked.load(std::memory_order_relaxed)) {
+      e = shares_registers(kernel, Wide::kThreads, Wide::kFewRegs, Wide::kManyRegs);
+      if (e == cudaSuccess) checked.store(true, std::memory_order_relaxed);
+    }
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Wide::kSmem);
     if (e != cudaSuccess) return e;
     return launch_pdl(kernel, dim3(2 * pairs), dim3(Wide::kThreads), Wide::kSmem, st, mw, mx, a);
   };
@@ -924,8 +951,16 @@ cudaError_t run_nt(const CUtensorMap& ma, const CUtensorMap& mb, const Args& a, 
                    cudaStream_t st) {
   auto go = [&](auto* kernel) {
     // (the kernel's own limit, whatever the call: it cannot be lowered between this and the launch)
-    const cudaError_t e =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<NT>::kSmem);
+    using C = Cfg<NT>;
+    static std::atomic<bool> seen[2];  // (the two output types' kernels)
+    std::atomic<bool>& checked = seen[out_dtype == EAT_BF16];
+    cudaError_t e = cudaSuccess;
+    if (!checked.load(std::memory_order_relaxed)) {
+      e = shares_registers(kernel, C::kThreads, C::kFewRegs, C::kManyRegs);
+      if (e == cudaSuccess) checked.store(true, std::memory_order_relaxed);
+    }
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
     if (e != cudaSuccess) return e;
     return launch_pdl(kernel, dim3(ctas), dim3(Cfg<NT>::kThreads), Cfg<NT>::kSmem, st, ma, mb, a);
   };
@@ -996,6 +1031,9 @@ extern "C" eat_status eat_block_mm(const void* xq, const float* xs, const void* 
   if (misaligned(xq, 16) || misaligned(wq, 16) || misaligned(xs, 4) || misaligned(ws, 4) ||
       misaligned(offsets, 4) || misaligned(y, ydtype == EAT_BF16 ? 2 : 4))
     return bad_arg(fn, "misaligned pointer");
+  const size_t out = (size_t)M * (transposed ? K : N) * (ydtype == EAT_BF16 ? 2 : 4);
+  if (overlap(y, out, xq, (size_t)M * (transposed ? N : K)) || overlap(y, out, wq, (size_t)E * N * K))
+    return bad_arg(fn, "y overlaps xq or wq");
   const int vec = !misaligned(y, 16) && (transposed ? K : N) % 8 == 0;
   const Args a{xs, ws, offsets, E, M, N, K, 0, y, vec};
   const cudaStream_t st = (cudaStream_t)stream;
@@ -1015,6 +1053,9 @@ extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const v
   if (misaligned(gq, 16) || misaligned(xq, 16) || misaligned(gs, 4) || misaligned(xs, 4) ||
       misaligned(offsets, 4) || misaligned(dw, dtype == EAT_BF16 ? 2 : 4))
     return bad_arg(fn, "misaligned pointer");
+  const size_t out = (size_t)E * N * K * (dtype == EAT_BF16 ? 2 : 4);
+  if (overlap(dw, out, gq, (size_t)rows * N) || overlap(dw, out, xq, (size_t)rows * K))
+    return bad_arg(fn, "dw overlaps gq or xq");
   const Args a{gs, xs, offsets, E, rows, N, K, blocks, dw, !misaligned(dw, 16)};
   return run<kGrad>(fn, gq, xq, a, dtype, (cudaStream_t)stream);
 }

@@ -19,7 +19,7 @@ namespace eat {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 // 1 / (1 + exp(-g)): within 3 2^-23 + |g| 2^-24 of itself, far below what bf16 or e4m3 keep of it.
 __device__ __forceinline__ float sigmoid(float g) {
@@ -238,11 +238,11 @@ quant_columns_kernel(const T* __restrict__ x, int M, int K, const int32_t* __res
 // ------------------------------------------------------------------------------------ tiles
 // A block takes a tile; thread: N columns of R consecutive rows.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kTileThreads, VEC ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, VEC ? 3 : 1)
 quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restrict__ q,
                    float* __restrict__ scale) {
-  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kTileThreads;
-  __shared__ float s_top[kTileWarps];
+  constexpr int N = Elem<T>::kN, L = kBlock / N, R = kBlock * L / kThreads;
+  __shared__ float s_top[kWarps];
   pdl_wait();
   pdl_launch_dependents();
   const int kb = blockIdx.x, blocks = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -266,7 +266,7 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
   if (lane == 0) s_top[warp] = top;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kTileWarps; ++k) top = fmaxf(top, s_top[k]);
+  for (int k = 0; k < kWarps; ++k) top = fmaxf(top, s_top[k]);
   const BlockDiv div(top);
   if (threadIdx.x == 0) scale[(e * n_blocks + nb) * blocks + kb] = div.scale;
 #pragma unroll
@@ -342,7 +342,7 @@ cudaError_t quant_rows(const void* x, int M, int K, int dtype, void* q, float* s
                         (const T*)x, M, K, blocks, (uint8_t*)q, scale);
     };
     // Units of one row where longer ones would leave SMs without a block (8 rows of 14336, gated:
-    // MEASURED)
+    // 2.6 us, 9.4 with eight)
     const long long units = (long long)((M + kMostRows - 1) / kMostRows) * blocks;
     if (units * (kBlock / N) < 2LL * kThreads * num_sms()) return go(std::integral_constant<int, 1>());
     return go(std::integral_constant<int, kMostRows>());
@@ -360,6 +360,8 @@ extern "C" eat_status eat_quant_rows(const void* x, int32_t M, int32_t K, int32_
   if (!x || !q || !scale) return bad_arg(fn, "x, q and scale must be non-NULL");
   if (const char* why = bad_matrix(M, K, dtype)) return bad_arg(fn, why);
   if (misaligned(x, elem_bytes(dtype)) || misaligned(scale, 4)) return bad_arg(fn, "misaligned pointer");
+  const size_t n = (size_t)M * K;
+  if (overlap(q, n, x, n * elem_bytes(dtype))) return bad_arg(fn, "q overlaps x");
   return launched(fn, quant_rows<false>(x, M, K, dtype, q, scale, (cudaStream_t)stream));
 }
 
@@ -388,6 +390,9 @@ extern "C" eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int
   const long long padded = eat_quant_columns_rows(M, E);
   const int blocks = (int)eat_quant_columns_blocks(M, E), tiles = (K + kBlock - 1) / kBlock;
   if (padded > 1 << 30) return bad_arg(fn, "need at most 2^30 padded rows");
+  const size_t n = (size_t)M * K * elem_bytes(dtype);
+  if ((q && overlap(q, (size_t)M * K, x, n)) || overlap(cq, (size_t)padded * K, x, n))
+    return bad_arg(fn, "q or cq overlaps x");
   return launched(fn, by_type(dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<T>::kN;
@@ -397,8 +402,9 @@ extern "C" eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int
                      : (vec ? quant_columns_kernel<T, true, false>
                             : quant_columns_kernel<T, false, false>);
     // (one more block than the experts can have: the rows behind them)
-    // several tiles a block where there are more than run at a time (a block's life is mostly latency:
-    // 24 rows of 64 experts, 2048 columns: MEASURED)
+    // Several tiles a block where there are more than run at a time: a block's life is mostly latency, so a
+    // small call takes one each (two calls of 666 rows, 512 and 256 columns: 11 us, 26 with four a block of
+    // 256 threads), a large one shares what finding the rows costs.
     const long long all = (long long)(blocks + 1) * tiles, run = 2LL * num_sms();
     const int per = (int)std::min((long long)kTilesOfBlock, (all + run - 1) / run);
     return launch_pdl(kernel, dim3(blocks + 1, (tiles + per - 1) / per), dim3(kTileThreads), 0,
@@ -415,12 +421,14 @@ extern "C" eat_status eat_quant_tiles(const void* w, int32_t E, int32_t N, int32
   if (N < 1 || N > 65536) return bad_arg(fn, "need 1 <= N <= 65536");
   if (const char* why = bad_matrix(N, K, dtype)) return bad_arg(fn, why);
   if (misaligned(w, elem_bytes(dtype)) || misaligned(scale, 4)) return bad_arg(fn, "misaligned pointer");
+  const size_t n = (size_t)E * N * K;
+  if (overlap(q, n, w, n * elem_bytes(dtype))) return bad_arg(fn, "q overlaps w");
   return launched(fn, by_type(dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     constexpr int V = Elem<T>::kN;
     const bool vec = K % V == 0 && !misaligned(w, 16) && !misaligned(q, V);
     return launch_pdl(vec ? quant_tiles_kernel<T, true> : quant_tiles_kernel<T, false>,
-                      dim3((K + kBlock - 1) / kBlock, (N + kBlock - 1) / kBlock, E), dim3(kTileThreads),
+                      dim3((K + kBlock - 1) / kBlock, (N + kBlock - 1) / kBlock, E), dim3(kThreads),
                       0, (cudaStream_t)stream, (const T*)w, N, K, (uint8_t*)q, scale);
   }));
 }
@@ -437,6 +445,8 @@ extern "C" eat_status eat_swiglu(const void* gu, int32_t R, int32_t F, int32_t d
   const int eb = elem_bytes(dtype);
   if (misaligned(gu, eb) || misaligned(h, fp8 ? 1 : eb) || (fp8 && misaligned(scale, 4)))
     return bad_arg(fn, "misaligned pointer");
+  const size_t size = (size_t)R * F;
+  if (overlap(h, size * (fp8 ? 1 : eb), gu, 2 * size * eb)) return bad_arg(fn, "h overlaps gu");
   const cudaStream_t st = (cudaStream_t)stream;
   if (fp8) return launched(fn, quant_rows<true>(gu, R, F, dtype, h, scale, st));
   return launched(fn, by_type(dtype, [&](auto* tag) {
@@ -458,6 +468,9 @@ extern "C" eat_status eat_swiglu_grad(const void* gu, const void* dh, int32_t R,
   const int eb = elem_bytes(dtype);
   if (misaligned(gu, eb) || misaligned(dh, eb) || misaligned(dgu, eb))
     return bad_arg(fn, "misaligned pointer");
+  const size_t size = (size_t)R * F * eb;
+  if (overlap(dgu, 2 * size, dh, size) || (dgu != gu && overlap(dgu, 2 * size, gu, 2 * size)))
+    return bad_arg(fn, "dgu overlaps dh, or a part of gu");
   return launched(fn, by_type(dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<T>::kN;

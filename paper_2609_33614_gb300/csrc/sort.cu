@@ -430,16 +430,16 @@ using namespace eat;
 
 extern "C" int64_t eat_expert_sort_workspace(int32_t T, int32_t K, int32_t E) {
   if (T < 1 || K < 1 || K > kMaxK || E < 1 || E > kMaxExperts || (long long)T * K > 1 << 30) return 0;
-  return (int64_t)(sort_chunks(T * K) + 1) * E * 4;
+  return T * K <= kClusterMost ? 0 : (int64_t)(sort_chunks(T * K) + 1) * E * 4;
 }
 
 extern "C" eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, int32_t E,
                                       const uint8_t* mask, int32_t* offsets, int32_t* slot,
                                       void* work, void* stream) {
   const char* fn = "eat_expert_sort";
-  if (!idx || !offsets || !slot || !work)
-    return bad_arg(fn, "idx, offsets, slot and work must be non-NULL");
+  if (!idx || !offsets || !slot) return bad_arg(fn, "idx, offsets and slot must be non-NULL");
   if (const char* why = bad_rows(T, K, E, 1, EAT_F32)) return bad_arg(fn, why);
+  if (!work && eat_expert_sort_workspace(T, K, E) > 0) return bad_arg(fn, "a call of this size needs work");
   if (misaligned(idx, 4) || misaligned(offsets, 4) || misaligned(slot, 4) || misaligned(work, 16))
     return bad_arg(fn, "misaligned pointer");
   const cudaStream_t st = (cudaStream_t)stream;
@@ -447,7 +447,8 @@ extern "C" eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, 
   auto smem = [&](int threads) { return (size_t)(threads / 32 + 2) * E * 4; };  // at most 35 KB
   if (n <= kClusterMost) {
     // One launch.  Two selections a thread in as many CTAs as that takes, up to a cluster's; more of them
-    // only where it holds no more threads (65528 selections of 64 experts: MEASURED)
+    // only where it holds no more threads (65528 selections of 64 experts: 10.5 us, 25 in the three launches
+    // that larger calls take)
     const int per = n <= 2 * kSortCtas * kSortThreads ? 2 : n <= 8 * kSortCtas * kSortThreads ? 8 : 16;
     const int ctas = (n + per * kSortThreads - 1) / (per * kSortThreads);
     // (a small call's block has no warps that only add to its sums, but a thread for each expert)
@@ -461,13 +462,14 @@ extern "C" eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, 
                                            offsets, slot));
   }
   int32_t *chunk = (int32_t*)work, *total = chunk + (size_t)chunks * E;
-  cudaError_t e = launch_pdl(sort_kernel<kCount, kPer>, dim3(chunks), dim3(kSortThreads), smem(kSortThreads), st, idx, n,
+  const size_t bytes = smem(kSortThreads);
+  cudaError_t e = launch_pdl(sort_kernel<kCount, kPer>, dim3(chunks), dim3(kSortThreads), bytes, st, idx, n,
                              K, E, mask, chunk, (const int32_t*)nullptr, (int32_t*)nullptr,
                              (int32_t*)nullptr);
   if (e == cudaSuccess)
     e = launch_pdl(sort_scan_kernel, dim3(E), dim3(32), 0, st, chunk, chunks, E, total);
   if (e == cudaSuccess)
-    e = launch_pdl(sort_kernel<kAssign, kPer>, dim3(chunks), dim3(kSortThreads), smem(kSortThreads), st, idx, n, K, E,
+    e = launch_pdl(sort_kernel<kAssign, kPer>, dim3(chunks), dim3(kSortThreads), bytes, st, idx, n, K, E,
                    mask, chunk, (const int32_t*)total, offsets, slot);
   return launched(fn, e);
 }
@@ -488,6 +490,8 @@ extern "C" eat_status eat_expert_gather(const void* x, int32_t T, int32_t K, int
   if (misaligned(x, eb) || misaligned(rows, fp8 ? 1 : eb) || misaligned(slot, 4) ||
       misaligned(offsets, 4) || (fp8 && misaligned(scale, 4)))
     return bad_arg(fn, "misaligned pointer");
+  const size_t n = (size_t)T * d;
+  if (overlap(rows, n * K * (fp8 ? 1 : eb), x, n * eb)) return bad_arg(fn, "rows overlaps x");
   const cudaStream_t st = (cudaStream_t)stream;
   if (fp8) {
     auto run = [&](auto* tag) {
@@ -540,7 +544,7 @@ extern "C" eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K,
                         (const X*)rows, slot, w, T, K, d, pieces, (X*)y);
     };
     // Two vectors a lane where that still leaves every SM its warps: half the steps that go with a row, not
-    // its elements (8191 tokens x 8 of 2048: MEASURED)
+    // its elements (two calls of 8191 tokens x 8 of 2048: 117 us, 120 with one)
     const bool two = vec && d > 32 * N &&
                      (long long)T * ((d + 64 * N - 1) / (64 * N)) >= 16LL * kWarps * num_sms();
     return two ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 1>());
@@ -569,7 +573,7 @@ extern "C" eat_status eat_expert_combine_grad(const void* dy, const void* rows, 
     const bool vec =
         d % N == 0 && !misaligned(dy, 16) && !misaligned(rows, 16) && !misaligned(drows, 16);
     // Many tokens: two warps each, so that more tokens' loads are under way (8191 tokens x 8 of 2048:
-    // MEASURED); few: as many as the row has vectors for.
+    // 82 us, 107 with eight); few: as many as the row has vectors for.
     const int most = T >= 16 * num_sms() ? 2 : kWarps;
     const int warps = std::min(most, (d + 32 * N - 1) / (32 * N));
     return launch_pdl(vec ? combine_grad_kernel<X, true> : combine_grad_kernel<X, false>, dim3(T),

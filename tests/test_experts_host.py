@@ -25,7 +25,7 @@ CGRAD = dict(dy=1 << 20, rows=1 << 21, T=4, K=2, E=8, d=64, dtype=BF16, slot=A[0
 QROWS = dict(x=A[0], M=4, K=64, dtype=BF16, q=A[1], scale=A[2], stream=None)
 QCOLS = dict(x=A[0], M=4, K=64, dtype=BF16, offsets=A[1], E=2, q=A[2], scale=A[3], cq=A[4],
              cscale=A[5], stream=None)
-QTILES = dict(w=A[0], E=2, N=64, K=64, dtype=F32, q=A[1], scale=A[2], stream=None)
+QTILES = dict(w=1 << 20, E=2, N=64, K=64, dtype=F32, q=1 << 21, scale=A[2], stream=None)
 MM = dict(xq=1 << 20, xs=A[0], wq=1 << 21, ws=A[1], offsets=A[2], E=2, M=4, N=64, K=64, transposed=0,
           y=1 << 22, ydtype=BF16, stream=None)
 MGRAD = dict(gq=1 << 20, gs=A[0], xq=1 << 21, xs=A[1], offsets=A[2], E=2, rows=64, blocks=2, N=64,
@@ -36,7 +36,7 @@ UNS = eat.EAT_ERR_UNSUPPORTED
 
 CASES = [
     ("eat_expert_sort", SORT, [
-        (dict(idx=None), "non-NULL"), (dict(work=None), "non-NULL"), (dict(T=0), "T >= 1"),
+        (dict(idx=None), "non-NULL"), (dict(T=1 << 20, work=None), "needs work"), (dict(T=0), "T >= 1"),
         (dict(K=0), "K <= 16"), (dict(K=17), "K <= 16"), (dict(T=1 << 30, K=2), "2^30"),
         (dict(E=0), "E <= 256"), (dict(E=257), "E <= 256"), (dict(idx=A[0] + 2), "misaligned"),
         (dict(work=A[3] + 4), "misaligned")]),
@@ -44,7 +44,7 @@ CASES = [
         (dict(slot=None), "non-NULL"), (dict(rows=None), "non-NULL"), (dict(d=0), "d <= 65536"),
         (dict(d=65537), "d <= 65536"), (dict(dtype=FP8), "dtype"), (dict(rows_dtype=F32), "rows_dtype"),
         (dict(rows_dtype=FP8), "scale"), (dict(x=A[0] + 1), "misaligned"),
-        (dict(rows_dtype=FP8, scale=A[4] + 2), "misaligned")]),
+        (dict(rows_dtype=FP8, scale=A[4] + 2), "misaligned"), (dict(rows=A[0] + 256), "overlaps")]),
     ("eat_expert_combine", COMBINE, [
         (dict(y=None), "non-NULL"), (dict(T=-1), "T >= 1"), (dict(w=A[2] + 1), "misaligned"),
         (dict(y=(1 << 20) + 1024), "overlaps"), (dict(dtype=5), "dtype")]),
@@ -54,15 +54,18 @@ CASES = [
     ("eat_quant_rows", QROWS, [
         (dict(q=None), "non-NULL"), (dict(M=0), "rows"), (dict(M=(1 << 30) + 1), "rows"),
         (dict(K=0), "columns"), (dict(K=65537), "columns"), (dict(dtype=FP8), "dtype"),
-        (dict(x=A[0] + 1), "misaligned"), (dict(scale=A[2] + 2), "misaligned")]),
+        (dict(x=A[0] + 1), "misaligned"), (dict(scale=A[2] + 2), "misaligned"),
+        (dict(q=A[0] + 504), "overlaps")]),
     ("eat_quant_columns", QCOLS, [
+        (dict(q=A[0] + 16), "overlaps"), (dict(cq=A[0] - 128), "overlaps"),
         (dict(cq=None), "non-NULL"), (dict(scale=None), "together"), (dict(q=None), "together"),
         (dict(E=0), "E <= 256"), (dict(offsets=None), "offsets"), (dict(M=1 << 30), "padded"),
         (dict(offsets=A[1] + 2), "misaligned")]),
     ("eat_quant_tiles", QTILES, [
         (dict(w=None), "non-NULL"), (dict(N=0), "N <= 65536"), (dict(E=257), "E <= 256"),
-        (dict(w=A[0] + 2), "misaligned")]),
+        (dict(w=(1 << 20) + 2), "misaligned"), (dict(q=(1 << 20) + 32), "overlaps")]),
     ("eat_block_mm", MM, [
+        (dict(y=(1 << 20) + 32), "overlaps"), (dict(y=(1 << 21) - 64), "overlaps"),
         (dict(xs=None), "non-NULL"), (dict(y=None), "non-NULL"), (dict(M=0), "rows"),
         (dict(N=0), "N and K"), (dict(K=65537), "N and K"), (dict(offsets=None), "offsets"),
         (dict(ydtype=FP8), "dtype"), (dict(xq=(1 << 20) + 8), "misaligned"),
@@ -70,12 +73,15 @@ CASES = [
     ("eat_block_mm_grad", MGRAD, [
         (dict(gs=None), "non-NULL"), (dict(rows=0), "rows"), (dict(blocks=0), "blocks"),
         (dict(offsets=None), "offsets"), (dict(dtype=FP8), "dtype"),
-        (dict(xq=(1 << 21) + 8), "misaligned")]),
+        (dict(xq=(1 << 21) + 8), "misaligned"), (dict(dw=(1 << 20) + 64), "overlaps"),
+        (dict(dw=1 << 21), "overlaps")]),
     ("eat_swiglu", GLU, [
         (dict(h=None), "non-NULL"), (dict(F=0), "columns"), (dict(R=0), "rows"),
-        (dict(h_dtype=F32), "h_dtype"), (dict(h_dtype=FP8), "scale"), (dict(gu=A[0] + 1), "misaligned")]),
+        (dict(h_dtype=F32), "h_dtype"), (dict(h_dtype=FP8), "scale"), (dict(gu=A[0] + 1), "misaligned"),
+        (dict(h=A[0] + 512), "overlaps")]),
     ("eat_swiglu_grad", GLUGRAD, [
-        (dict(dh=None), "non-NULL"), (dict(dtype=FP8), "dtype"), (dict(dgu=A[2] + 1), "misaligned")]),
+        (dict(dh=None), "non-NULL"), (dict(dtype=FP8), "dtype"), (dict(dgu=A[2] + 1), "misaligned"),
+        (dict(dgu=A[1] - 64), "overlaps"), (dict(dgu=A[0] + 16), "overlaps")]),
 ]
 
 
@@ -95,8 +101,8 @@ def test_widths_that_are_not_supported(lib, fn, base, kw):
 
 
 def test_workspaces_and_padded_sizes(lib):
-    assert lib.eat_expert_sort_workspace(4096, 8, 64) > 0
-    assert lib.eat_expert_sort_workspace(0, 8, 64) == 0 == lib.eat_expert_sort_workspace(4, 17, 64)
+    assert lib.eat_expert_sort_workspace(16384, 8, 64) == 0 < lib.eat_expert_sort_workspace(16385, 8, 64)
+    assert lib.eat_expert_sort_workspace(0, 8, 64) == 0 == lib.eat_expert_sort_workspace(1 << 20, 17, 64)
     rows, blocks = lib.eat_quant_columns_rows, lib.eat_quant_columns_blocks
     assert (rows(1, 1), rows(32, 1), rows(33, 1), rows(2, 64)) == (32, 32, 64, 64)
     assert (blocks(1, 1), blocks(128, 1), blocks(129, 1), blocks(2, 64)) == (1, 1, 2, 2)

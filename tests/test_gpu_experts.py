@@ -73,7 +73,7 @@ def _sorted(idx, E, mask=None):
 
 
 SIZES = [(1, 1, 1), (1, 64, 8), (2, 3, 16), (5, 256, 2), (300, 8, 2), (1024, 60, 8), (1025, 64, 8),
-         (9001, 200, 5), (40000, 7, 3)]
+         (9001, 200, 5), (40000, 7, 3), (16384, 64, 8), (16385, 64, 8), (90001, 256, 3)]
 
 
 @pytest.mark.parametrize("masked", ["none", "some", "all"])
@@ -91,7 +91,7 @@ def test_sort(T, E, K, masked):
 @pytest.mark.parametrize("E", [1, 8, 256])
 def test_sort_all_to_one_expert(E):
     """The fullest expert, in one block and in several."""
-    for T, K in ((700, 4), (5000, 4)):
+    for T, K in ((700, 4), (5000, 4), (40000, 4)):
         idx = torch.full((T, K), E - 1, dtype=torch.int32, device="cuda")
         offsets, slot = eat.expert_sort(idx, E)
         assert offsets.tolist() == [0] * E + [T * K]
@@ -478,6 +478,13 @@ def test_swiglu_grad(R, F, off, dtype):
                      (dh.double() * gate * s).abs()], 1)
     tol = _u(dtype) * v.grad.abs() + (12 + gate.abs().repeat(1, 2)) * U32 * mag
     assert ((dgu.double() - v.grad).abs() <= tol + 1e-38).all()
+
+
+def test_swiglu_grad_in_place():
+    gu, dh = _randn(46, 33, 400).to(BF16), _randn(47, 33, 200).to(BF16)
+    want = eat.swiglu_grad(gu, dh)
+    eat.eat_swiglu_grad(gu, dh, 33, 200, eat.EAT_BF16, gu)
+    assert torch.equal(gu, want)
 
 
 def test_swiglu_grad_against_differences():
