@@ -12,11 +12,11 @@
 //      tiles of equal heights.  In the 16x256b layout a thread has two neighbouring rows of the output for each
 //      of its columns, so a scale's pair is one load.  Bound: HBM with few rows an expert (1 token, 2 of 8
 //      matrices of 28672 x 4096: 41 us, 5.7 TB/s; 32 tokens, 8 of 64 of 2048 x 2048: 42 us, 6.4 TB/s); dw
-//      of 18432 rows, 64 matrices of 2048 x 2048: 230 us, of which writing dw is 79.
+//      of 18432 rows, 64 matrices of 2048 x 2048: 205 us, of which writing dw is 79.
 //   wide_kernel: on SM pairs, 256 rows (M) x 256 columns (N), for many rows an expert: half the operand bytes
 //      from L2 for each MMA, and a k-block's scales are one product a thread.  Bound: the accumulator's way
 //      through TMEM (two buffers: an MMA of 530 cycles, then 500 of reading and adding, then the
-//      hand-over).  8192 x 2048 x 8192: 137 us, 2.0 PFLOP/s; 10240 rows, 60 matrices of 2816 x 2048: 113 us.
+//      hand-over).  8192 x 2048 x 8192: 137 us, 2.0 PFLOP/s; 10240 rows, 60 matrices of 2816 x 2048: 111 us.
 // Operands come by TMA as they lie (K-major, or MN-major where the sum runs over their rows): w serves
 // both directions, and the gradient reads both operands by rows.
 // Warps: 0 issues TMA, 1 owns TMEM and issues MMAs, 2 copies the blocks' scales into a ring (block_mm_kernel)
@@ -133,6 +133,17 @@ __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
   return *(const uint32_t*)&v;
 }
+// 16 bytes of a row that may begin anywhere, of which `left` elements exist.
+template <typename Out>
+__device__ __forceinline__ void store_some(Out* p, int left, uint4 v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 16 / (int)sizeof(Out); ++i) {
+    if (i >= left) break;
+    if (sizeof(Out) == 4) ((uint32_t*)p)[i] = w[i & 3];
+    else ((uint16_t*)p)[i] = (uint16_t)(w[i / 2 & 3] >> 16 * (i & 1));
+  }
+}
 // Four 8 x 8 matrices of 16-bit values whose fragments the lanes hold, transposed into rows of 16 bytes.
 __device__ __forceinline__ void stmatrix_t(uint32_t dst, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(dst),
@@ -213,10 +224,12 @@ template <int COLS>
 __device__ __forceinline__ Tile row_tile(const Args& a, const Experts& ex, int col_tiles, int inner,
                                          long long u) {
   Tile t;
-  int lo = 0, hi = a.E;  // the last expert whose tiles begin at or before u
+  // the last expert whose tiles begin at or before u (its first column's, so that the search compares ints)
+  const int q = u >> 32 ? (int)(u / col_tiles) : (int)((unsigned)u / (unsigned)col_tiles);
+  int lo = 0, hi = a.E;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if ((long long)ex.tile0[mid] * col_tiles <= u) lo = mid;
+    if (ex.tile0[mid] <= q) lo = mid;
     else hi = mid;
   }
   t.e = lo;
@@ -586,20 +599,23 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                        bf16x2(v[2]), bf16x2(v[3]));
           }
           __syncwarp();
+          const int c = 8 * (lane & 3);
+          uint4 v[kRows / 8];
 #pragma unroll
           for (int k = 0; k < kRows / 8; ++k) {
-            const int r = 8 * k + (lane >> 2), piece = lane & 3, c = 8 * piece;
-            const uint4 v = box[r * 4 + (piece ^ ((r >> 1) & 3))];
-            if (r0 + r >= live || col + c >= cols) continue;
-            Out* const p = out + (size_t)(r0 + r) * cols + c;
-            if (a.vec && col + c + 8 <= cols) {
-              *(uint4*)p = v;
-            } else {
-              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            const int r = 8 * k + (lane >> 2);
+            v[k] = box[r * 4 + ((lane & 3) ^ ((r >> 1) & 3))];
+          }
+          Out* p = out + (size_t)(r0 + (lane >> 2)) * cols + c;
+          const int rows = live - r0 - (lane >> 2);
+          if (a.vec && col + 32 <= cols) {
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (col + c + j < cols) ((uint16_t*)p)[j] = (uint16_t)(w[j / 2] >> 16 * (j & 1));
-            }
+            for (int k = 0; k < kRows / 8; ++k)
+              if (8 * k < rows) *(uint4*)(p + (size_t)(8 * k) * cols) = v[k];
+          } else {
+#pragma unroll
+            for (int k = 0; k < kRows / 8; ++k)
+              if (8 * k < rows) store_some(p + (size_t)(8 * k) * cols, cols - col - c, v[k]);
           }
         }
       }
@@ -616,7 +632,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // thread owns a row of 128 columns, so a k-block's scales are one product a thread: its row's times the
 // columns' block's, loaded kLead k-blocks ahead.
 // Rows an expert has on average, above which its tiles are these (32 matrices of 2048 x 2048, 96 rows each:
-// 49.1 us, 47.1 with the kernel above; 128 rows: 47.1 and 51.2; 256: 59.4 and 65.5)
+// 49 us, 45 with the kernel above; 128 rows: 47 and 51; 256: 57 and 65)
 constexpr int kWideRows = 112;
 
 struct Wide {
@@ -882,23 +898,22 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
           box[lane * 4 + (j ^ ((lane >> 1) & 3))] = p;
         }
         __syncwarp();
+        const int cc = c + (lane & 3) * kVec, rows = last - (lane >> 2);
+        uint4 v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int r = 8 * k + (lane >> 2), j = lane & 3, cc = c + j * kVec;
-          const uint4 v = box[r * 4 + (j ^ ((r >> 1) & 3))];
-          if (r >= last || col + cc >= cols) continue;
-          Out* const p = out + (size_t)r * cols + cc;
-          if (a.vec && col + cc + kVec <= cols) {
-            *(uint4*)p = v;
-          } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          const int r = 8 * k + (lane >> 2);
+          v[k] = box[r * 4 + ((lane & 3) ^ ((r >> 1) & 3))];
+        }
+        Out* p = out + (size_t)(lane >> 2) * cols + cc;
+        if (a.vec && col + c + kPer <= cols) {
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-              if (col + cc + i >= cols) break;
-              if (sizeof(Out) == 4) ((uint32_t*)p)[i] = w[i & 3];
-              else ((uint16_t*)p)[i] = (uint16_t)(w[i / 2 & 3] >> 16 * (i & 1));
-            }
-          }
+          for (int k = 0; k < 4; ++k)
+            if (8 * k < rows) *(uint4*)(p + (size_t)(8 * k) * cols) = v[k];
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (8 * k < rows) store_some(p + (size_t)(8 * k) * cols, cols - col - cc, v[k]);
         }
       }
     }
