@@ -433,7 +433,10 @@ eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* st
 /* ---- Experts of a router's choice: tokens sorted by expert and back, products in e4m3 -----------
  * What serving and training experts outside a layer handle takes, on the idx and w that eat_route
  * writes.  No handle; errors through eat_last_error(NULL).  Every output is a function of the inputs
- * alone: the same inputs give the same bits.  1 <= K <= 16, 1 <= E <= 256, T K <= 2^30, 1 <= d <= 65536. */
+ * alone: the same inputs give the same bits.  1 <= K <= 16, 1 <= E <= 256, T K <= 2^30, 1 <= d <= 65536.
+ * offsets [E + 1] and slot stay on the device; calls read them there.  Others than eat_expert_sort writes (not
+ * in order, beyond the rows) reach nothing outside of the call's buffers, but what the outputs then are is
+ * not defined. */
 
 /* Sorts the selections of idx [T, K] by expert.  Entries outside [0, E), and those of tokens whose mask
  * byte is 0 (mask [T] or NULL), select nothing.  offsets [E + 1]: offsets[e] is the number of
@@ -499,8 +502,8 @@ eat_status eat_quant_tiles(const void* w, int32_t E, int32_t N, int32_t K, int32
  * [E, N, K]: rows offsets[e] .. offsets[e + 1] - 1 of x by matrix e, zeros in the rows from offsets[E]
  * on; offsets NULL with E = 1: one matrix for all rows.
  *   x [M, K], xs [ceil(K / 128)][M], y [M, N]; transposed: x [M, N], xs [ceil(N / 128)][M], y [M, K].
- * y in ydtype, EAT_BF16 or EAT_F32.  Sums are fp32: those of a block of 128 on the tensor cores, scaled
- * and added to each other in order.  Rows of x behind an expert's own never reach its outputs.
+ * y in ydtype, EAT_BF16 or EAT_F32.  Sums are fp32: those of a block of 128 on the tensor cores, multiplied
+ * by the fp32 product of their two scales and added to each other in order.  Rows of x behind an expert's own never reach its outputs.
  * K, and with transposed N, are multiples of 16 (EAT_ERR_UNSUPPORTED otherwise); N, K <= 65536; xq and
  * wq 16-byte aligned.  y overlaps no input.
  * Where a kernel gives up on a bounded wait (see EAT_ERR_STATE), the outputs that it has not finished are

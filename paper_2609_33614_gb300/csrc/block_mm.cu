@@ -164,8 +164,8 @@ __device__ __forceinline__ bool both(uint64_t* full, uint32_t fp, uint64_t* temp
 struct Experts {
   int row[kMaxExperts], end[kMaxExperts], tile0[kMaxExperts + 1];
 };
-// One tile: `rows` output rows from row0 (x's rows, or dw's n), columns c0 .. c0 + 127 of expert e, nkb
-// k-blocks (the last of `tail` k; kGrad: from padded row k0, block b0).
+// One tile: `rows` output rows from row0 (x's rows, or dw's n), columns from c0 on, of expert e; its sums'
+// length and number of k-blocks (kGrad: from padded row k0, block b0).
 struct Tile {
   int e, row0, rows, c0, nkb, k0, b0, sums;
 };
@@ -175,7 +175,7 @@ template <int MODE, int NT>
 __device__ __forceinline__ void list_experts(const Args& a, Experts& ex) {
   const int lane = threadIdx.x & 31;
   // prefix sums over the experts; what follows the last one is in [E]
-  int tiles = 0, padded = 0, blocks = 0;
+  int tiles = 0, padded = 0, blocks = 0, before = 0;
   const int cap = MODE == kGrad ? 1 << 30 : a.M;
   for (int e0 = 0; e0 < a.E; e0 += 32) {
     const int e = e0 + lane;
@@ -184,6 +184,7 @@ __device__ __forceinline__ void list_experts(const Args& a, Experts& ex) {
       lo = a.offsets ? max(0, min(a.offsets[e], cap)) : 0;
       hi = a.offsets ? max(lo, min(a.offsets[e + 1], cap)) : a.M;
     }
+    in_order(lo, hi, before);
     const int n = hi - lo;
     int vt = (n + NT - 1) / NT, vp = (n + 31) & ~31, vb = (n + kBlock - 1) / kBlock;
     const int t = vt, p = vp, b = vb;

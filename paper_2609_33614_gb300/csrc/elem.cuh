@@ -174,6 +174,21 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, int left, const float* v,
   for (int j = 0; j < N; ++j) t[j] = div(v[j]);
   store_e4m3<N, VEC, S>(p, left, t);
 }
+// Rows [lo, hi) of the experts of 32 lanes, held to be in order and apart from each other whatever the
+// offsets say, so that they never add up to more than there are; before: the largest end so far.
+__device__ __forceinline__ void in_order(int& lo, int& hi, int& before) {
+  const int lane = threadIdx.x & 31;
+  int top = hi;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, top, o);
+    if (lane >= o) top = max(top, u);
+  }
+  const int prev = __shfl_up_sync(0xffffffffu, top, 1);
+  lo = max(lo, max(before, lane > 0 ? prev : 0));
+  hi = max(hi, lo);
+  before = max(before, __shfl_sync(0xffffffffu, top, 31));
+}
 // The largest magnitude over groups of G lanes, in all of them.
 template <int G>
 __device__ __forceinline__ float group_max(float v) {

@@ -98,11 +98,12 @@ __device__ RowBlock find_block(const int32_t* offsets, int E, int M, int b) {
     lo[i] = in && offsets ? offsets[e] : 0;
     hi[i] = !in ? 0 : offsets ? offsets[e + 1] : M;
   }
-  int blocks = 0, padded = 0, end = 0;  // of the experts so far
+  int blocks = 0, padded = 0, end = 0, before = 0;  // of the experts so far
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
     if (32 * i >= E) break;
-    const int l = max(0, min(lo[i], M)), h = 32 * i + lane < E ? max(l, min(hi[i], M)) : l;
+    int l = max(0, min(lo[i], M)), h = 32 * i + lane < E ? max(l, min(hi[i], M)) : l;
+    in_order(l, h, before);
     const int c = (h - l + kBlock - 1) / kBlock, p = (h - l + 31) & ~31;
     int vc = c, vp = p;
 #pragma unroll

@@ -418,6 +418,26 @@ def test_product_grad_of_all_rows(M, N, K):
     _check_product(dw, u.t() @ v, u.abs().t() @ v.abs(), -(-M // 128), BF16)
 
 
+def test_offsets_out_of_order_stay_in_the_buffers():
+    """Offsets that no sort makes: the calls end, and leave what lies behind their outputs alone."""
+    M, N, K = 96, 64, 128
+    x, w = _randn(36, M, K).to(BF16), _randn(37, 4, N, K).to(BF16)
+    (xq, xs), (wq, ws) = eat.quant_rows(x), eat.quant_tiles(w)
+    for bad in ([0, 90, 10, 200, 96], [-5, 96, 0, 96, 0], [1 << 30, -7, 50, 3, 1 << 30], [96] * 5):
+        o = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        y = torch.full((M + 8, N), 7.0, dtype=BF16, device="cuda")
+        eat.eat_block_mm(xq, xs, wq, ws, o, 4, M, N, K, 0, y, eat.EAT_BF16)
+        assert (y[M:] == 7).all()
+        rows, blocks = eat.eat_quant_columns_rows(M, 4), eat.eat_quant_columns_blocks(M, 4)
+        cq = torch.full((rows + 8, K), 7.0, device="cuda").to(E4M3)
+        cs = torch.full((blocks + 1, K), 7.0, device="cuda")
+        eat.eat_quant_columns(x, M, K, eat.EAT_BF16, o, 4, None, None, cq, cs)
+        assert (cq[rows:].float() == 7).all() and (cs[blocks:] == 7).all()
+        dw = torch.full((5, K, K), 7.0, device="cuda")
+        eat.eat_block_mm_grad(cq, cs, cq, cs, o, 4, rows, blocks, K, K, dw, eat.EAT_F32)
+        assert (dw[4] == 7).all()
+
+
 # -------------------------------------------------------------------------- gated activation
 GLU = [(1, 1, 0), (1, 16, 0), (3, 129, 0), (8, 14336, 0), (33, 1408, 0), (700, 256, 0), (5, 100, 1), (2, 65536, 0)]
 
