@@ -131,7 +131,7 @@ def _build_binding(force: bool = False) -> str:
     obj = os.path.join(BUILD, "binding.o")
     tmp = BINDING + ".tmp"
     # (torch's libraries are loaded before it; libeat.so is found in its own directory)
-    libs = ["-L" + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+    libs = ["-L" + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
             "-L" + PKG, "-l:libeat.so", "-Wl,-rpath,$ORIGIN"]
     for cmd in (cxx + flags + ["-I" + i for i in inc] + ["-c", src, "-o", obj],
                 cxx + ["-shared", "-o", tmp, obj] + libs):

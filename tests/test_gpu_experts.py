@@ -624,6 +624,61 @@ def test_layer_on_two_streams():
                 assert torch.equal(r[n], w[n]), n
 
 
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("N,K", [(65536, 128), (128, 65536)])
+def test_widest_products(N, K, transposed):
+    M, inner = 130, N if transposed else K
+    x, w = _randn(111, M, inner).to(BF16), _randn(112, N, K).to(BF16)
+    (xq, xs), (wq, ws) = eat.quant_rows(x), eat.quant_tiles(w)
+    a, b = _of_rows(xq, xs), _of_tiles(wq, ws)
+    b = b if transposed else b.t()
+    for rows in (M, 5):
+        y = eat.block_mm(xq[:rows], xs[:, :rows].contiguous(), wq, ws, transposed=transposed, dtype=F32)
+        _check_product(y, a[:rows] @ b, a[:rows].abs() @ b.abs(), -(-inner // 128), F32)
+
+
+def test_rows_far_into_a_buffer():
+    """Elements and bytes whose offsets pass 32 bits: the last rows as in a call of their own."""
+    T, d, n = 70000, 65536, 112  # (the last 112 rows are a block of columns)
+    x = torch.empty(T, d, dtype=BF16, device="cuda").normal_(generator=_gen(121))
+    idx = (torch.arange(T, device="cuda") % 2).to(torch.int32)[:, None].contiguous()
+    offsets, slot = eat.expert_sort(idx, 2)
+    rows = eat.expert_gather(x, slot, offsets)
+    assert torch.equal(rows[-3:], x[-5::2]) and torch.equal(rows[T // 2 - 2:T // 2], x[-4::2])
+    assert torch.equal(eat.expert_combine(rows, slot), x)
+    drows, dw = eat.expert_combine_grad(x, rows, slot, offsets, torch.ones(T, 1, device="cuda"))
+    assert torch.equal(drows[-3:], rows[-3:])
+    assert ((dw[-2:, 0] - x[-2:].double().square().sum(1)).abs() < 1e-3 * d).all()
+    del rows, drows
+    q, scale = eat.quant_rows(x)
+    q1, scale1 = eat.quant_rows(x[-n:])
+    assert torch.equal(q[-n:].view(torch.uint8), q1.view(torch.uint8))
+    assert torch.equal(scale[:, -n:], scale1)
+    w, wt = (eat.quant_tiles(_randn(s, 16, d).to(BF16)) for s in (122, 123))
+    y = eat.block_mm(q, scale, *w)
+    assert torch.equal(y[-130:], eat.block_mm(q[-130:], scale[:, -130:].contiguous(), *w))
+    _, _, cq, cscale = eat.quant_rows_columns(x)
+    c1, cs1 = eat.quant_columns(x[-n:])
+    assert torch.equal(cq[-n:].view(torch.uint8), c1[:n].view(torch.uint8))
+    assert torch.equal(cscale[-1], cs1[0])
+    gq, gs = eat.quant_columns(y)
+    dw = eat.block_mm_grad(gq, gs, cq, cscale)
+    assert dw.shape == (16, d) and dw.isfinite().all()
+    del cq, cscale
+    yq, ys = eat.quant_rows(y)
+    back = eat.block_mm(yq, ys, *wt, transposed=True)
+    assert torch.equal(back[-130:], eat.block_mm(yq[-130:], ys[:, -130:].contiguous(), *wt, transposed=True))
+    del back, q
+    gu = x.view(T // 2, 2 * d)
+    h = eat.swiglu(gu)
+    assert torch.equal(h[-3:], eat.swiglu(gu[-3:]))
+    dgu = eat.swiglu_grad(gu, h)
+    assert torch.equal(dgu[-3:], eat.swiglu_grad(gu[-3:], h[-3:]))
+    h8, s8 = eat.swiglu_fp8(gu)
+    h1, s1 = eat.swiglu_fp8(gu[-3:])
+    assert torch.equal(h8[-3:].view(torch.uint8), h1.view(torch.uint8)) and torch.equal(s8[:, -3:], s1)
+
+
 def test_routing_of_a_layer_feeds_the_sort():
     """idx and w as EatLayer.route writes them."""
     from paper_2609_33614_gb300 import workloads as W
