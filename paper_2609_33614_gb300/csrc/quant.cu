@@ -34,7 +34,7 @@ constexpr int kMostRows = 8;  // of a unit: their scales fill a sector of [block
 // A unit is kRows rows of one block of 128 columns, taken by as many lanes as the block has 16-byte
 // vectors.  GLU: the values are swiglu of rows of twice the length.
 template <typename T, bool VEC, bool GLU, int kRows>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, VEC ? 4 : 1)
 quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __restrict__ q,
                   float* __restrict__ scale) {
   constexpr int N = Elem<T>::kN, G = kBlock / N, U = GLU && kRows > 4 ? 4 : kRows;
@@ -48,29 +48,30 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
   float s = 1.0f;  // lane l: of the l-th row
 #pragma unroll
   for (int i0 = 0; i0 < kRows; i0 += U) {
-    float v[U][N], u[GLU ? U : 1][N];
+    // (kept as they were loaded until their row's turn: four blocks an SM)
+    RowVec<T, VEC, G> in[U], up[GLU ? U : 1];
+    const T* const p = x + (r0 + i0) * pitch + c;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const long long r = r0 + i0 + i;
-      if (r < M && left > 0) {
-        load_elems<T, N, VEC, G>(x + r * pitch + c, left, v[i]);
-        if (GLU) load_elems<T, N, VEC, G>(x + r * pitch + K + c, left, u[GLU ? i : 0]);
-      }
+      in[i].load(p + i * pitch, left, r0 + i0 + i < M);
+      if (GLU) up[GLU ? i : 0].load(p + i * pitch + K, left, r0 + i0 + i < M);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const long long r = r0 + i0 + i;
-      float top = 0.f;
-      if (r < M && left > 0) {
+      float v[N], top = 0.f;
+      in[i].get(v);
+      if (GLU) {
+        float u[N];
+        up[GLU ? i : 0].get(u);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          if (GLU) v[i][j] = v[i][j] * sigmoid(v[i][j]) * u[GLU ? i : 0][j];
-          if (VEC || j * G < left) top = fmaxf(top, fabsf(v[i][j]));
-        }
+        for (int j = 0; j < N; ++j) v[j] = v[j] * sigmoid(v[j]) * u[j];
       }
-      top = group_max<G>(top);
-      const BlockDiv div(top);
-      if (r < M && left > 0) store_e4m3<N, VEC, G>(q + (size_t)r * K + c, left, v[i], div);
+      // (elements that do not exist are 0)
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[j]));
+      const BlockDiv div(group_max<G>(top));
+      if (r < M && left > 0) store_e4m3<N, VEC, G>(q + (size_t)r * K + c, left, v, div);
       if (l == i0 + i) s = div.scale;
     }
   }
