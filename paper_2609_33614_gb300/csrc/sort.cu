@@ -267,12 +267,13 @@ gather_fp8_kernel(const T* __restrict__ x, const int32_t* __restrict__ slot,
   }
 }
 
-// y[t]: a warp takes V vectors a lane of one token at a time, the loads of kAhead rows before their use, and
-// loads the next token's slots meanwhile.
-constexpr int kAhead = 4;  // rows
-constexpr int combine_blocks(int V) { return V == 2 ? 3 : 4; }  // of an SM
-template <typename T, bool VEC, int V>
-__global__ void __launch_bounds__(32 * kWarps, VEC ? combine_blocks(V) : 1)
+// y[t]: a warp takes a vector a lane of one token at a time, the loads of kAhead rows before their use, and
+// loads the next token's slots meanwhile.  Bound: HBM (8191 tokens x 8 of 2048 bf16: 33 us, 5.2 TB/s; with
+// eight rows ahead 41, with two vectors a lane 36, as fewer warps fit).
+constexpr int kAhead = 4;          // rows
+constexpr int kCombineBlocks = 4;  // of an SM
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(32 * kWarps, VEC ? kCombineBlocks : 1)
 combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
                const float* __restrict__ weight, int tokens, int K, int d, int pieces,
                T* __restrict__ y) {
@@ -297,7 +298,7 @@ combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
   prefetch();
   while (nt < tokens) {
     const int mine = next < M ? next : -1, t = nt;
-    const int c = np * (32 * N * V) + lane_at<T, VEC>(lane), left = d - c;
+    const int c = np * (32 * N) + lane_at<T, VEC>(lane), left = d - c;
     const float wt = next_wt;
     nt += dt;
     np += dp;
@@ -306,34 +307,26 @@ combine_kernel(const T* __restrict__ rows, const int32_t* __restrict__ slot,
       ++nt;
     }
     prefetch();
-    float sum[V][N] = {};
+    float sum[N] = {};
     for (int k0 = 0; k0 < K; k0 += kAhead) {
-      RowVec<T, VEC, 32> in[kAhead][V];
+      RowVec<T, VEC, 32> in[kAhead];
       int r[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         r[k] = __shfl_sync(0xffffffffu, mine, (k0 + k) & 31);
-        const T* const p = rows + (size_t)max(r[k], 0) * d + c;
-#pragma unroll
-        for (int i = 0; i < V; ++i) in[k][i].load(p + i * 32 * N, left - i * 32 * N, r[k] >= 0);
+        in[k].load(rows + (size_t)max(r[k], 0) * d + c, left, r[k] >= 0);
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const float f = __shfl_sync(0xffffffffu, wt, (k0 + k) & 31);
         if (r[k] < 0) continue;
+        float v[N];
+        in[k].get(v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float v[N];
-          in[k][i].get(v);
-#pragma unroll
-          for (int j = 0; j < N; ++j) sum[i][j] = fmaf(f, v[j], sum[i][j]);
-        }
+        for (int j = 0; j < N; ++j) sum[j] = fmaf(f, v[j], sum[j]);
       }
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (left > i * 32 * N)
-        store_elems<T, N, VEC, 32>(y + (size_t)t * d + c + i * 32 * N, left - i * 32 * N, sum[i]);
+    if (left > 0) store_elems<T, N, VEC, 32>(y + (size_t)t * d + c, left, sum);
   }
 }
 
@@ -533,21 +526,13 @@ extern "C" eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K,
     using X = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<X>::kN;
     const bool vec = d % N == 0 && !misaligned(rows, 16) && !misaligned(y, 16);
-    auto go = [&](auto two) {
-      constexpr int V = decltype(two)::value;
-      const int pieces = (d + 32 * N * V - 1) / (32 * N * V);
-      // (as many blocks as run at a time, so that a warp has a next token)
-      const unsigned most = (unsigned)(combine_blocks(V) * num_sms());
-      const unsigned all = warp_grid((long long)T * pieces).x;
-      return launch_pdl(vec ? combine_kernel<X, true, V> : combine_kernel<X, false, V>,
-                        dim3(std::min(most, all)), dim3(32 * kWarps), 0, (cudaStream_t)stream,
-                        (const X*)rows, slot, w, T, K, d, pieces, (X*)y);
-    };
-    // Two vectors a lane where that still leaves every SM its warps: half the steps that go with a row, not
-    // its elements (two calls of 8191 tokens x 8 of 2048: 117 us, 120 with one)
-    const bool two = vec && d > 32 * N &&
-                     (long long)T * ((d + 64 * N - 1) / (64 * N)) >= 16LL * kWarps * num_sms();
-    return two ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 1>());
+    const int pieces = (d + 32 * N - 1) / (32 * N);
+    // (as many blocks as run at a time, so that a warp has a next token)
+    const unsigned most = (unsigned)(kCombineBlocks * num_sms());
+    const unsigned all = warp_grid((long long)T * pieces).x;
+    return launch_pdl(vec ? combine_kernel<X, true> : combine_kernel<X, false>, dim3(std::min(most, all)),
+                      dim3(32 * kWarps), 0, (cudaStream_t)stream, (const X*)rows, slot, w, T, K, d,
+                      pieces, (X*)y);
   };
   return launched(fn, dtype == EAT_BF16 ? run((__nv_bfloat16*)nullptr) : run((float*)nullptr));
 }
@@ -573,7 +558,7 @@ extern "C" eat_status eat_expert_combine_grad(const void* dy, const void* rows, 
     const bool vec =
         d % N == 0 && !misaligned(dy, 16) && !misaligned(rows, 16) && !misaligned(drows, 16);
     // Many tokens: two warps each, so that more tokens' loads are under way (8191 tokens x 8 of 2048:
-    // 82 us, 107 with eight); few: as many as the row has vectors for.
+    // 71 us, 107 with eight, cold); few: as many as the row has vectors for.
     const int most = T >= 16 * num_sms() ? 2 : kWarps;
     const int warps = std::min(most, (d + 32 * N - 1) / (32 * N));
     return launch_pdl(vec ? combine_grad_kernel<X, true> : combine_grad_kernel<X, false>, dim3(T),
