@@ -167,6 +167,29 @@ def test_combine_grad(T, E, K, d, off, dtype):
     assert torch.equal(again[0], drows) and torch.equal(again[1], dw)
 
 
+def test_combine_grad_against_differences():
+    """combine is linear in its rows and in its weights, so a step of any size gives the derivative; fp32
+    sums of K d terms are off by at most (K + d) 2^-24 of the magnitudes."""
+    T, E, K, d = 37, 5, 3, 68
+    offsets, slot, entry = _sorted(_idx(51, T, E, K), E)
+    n = len(entry)
+    rows, dy, w = _randn(52, T * K, d), _randn(53, T, d), torch.rand(T, K, generator=_gen(54), device="cuda")
+    e, ew = _randn(55, T * K, d), _randn(56, T, K)
+    drows, dw = eat.expert_combine_grad(dy, rows, slot, offsets, w)
+    y = eat.expert_combine(rows, slot, w).double()
+    for moved, grad, step in ((eat.expert_combine(rows + e, slot, w), drows[:n], e[:n]),
+                              (eat.expert_combine(rows, slot, w + ew), dw[slot >= 0], ew[slot >= 0])):
+        change = ((moved.double() - y) * dy.double()).sum()
+        want = (grad.double() * step.double()).sum()
+        mag = ((moved.double().abs() + y.abs()) * dy.double().abs()).sum()
+        assert (change - want).abs() <= 4 * (K + d) * U32 * mag
+    # and without weights it is gather's transpose
+    x, din = _randn(57, T, d), _randn(58, T * K, d)
+    a = (eat.expert_gather(x, slot, offsets).double()[:n] * din.double()[:n]).sum()
+    b = (eat.expert_combine(din, slot).double() * x.double()).sum()
+    assert (a - b).abs() <= (K + d) * U32 * (x.abs().max() * din.abs().sum()).double()
+
+
 # ------------------------------------------------------------------------------ e4m3 in blocks
 def _scales64(top):
     return torch.where(top > 1e-35, top / 448.0, 1.0)
@@ -622,6 +645,34 @@ def test_layer_on_two_streams():
         for r in g:
             for n in w:
                 assert torch.equal(r[n], w[n]), n
+
+
+@pytest.mark.parametrize("split", [[128], [128, 0, 256], [512, 128], [0, 128] * 40])
+def test_products_of_integers_are_exact(split):
+    """Powers of two up to 4, and 448 once in every row, column and tile of a block: the scales are 1, every
+    product and sum is a whole number below 2^24, and all three products come out exactly."""
+    E, M, N, K = len(split), sum(split), 256, 384
+
+    def whole(seed, *shape):
+        v = 2.0 ** torch.randint(0, 3, shape, generator=_gen(seed), device="cuda")
+        v *= torch.randint(-1, 2, shape, generator=_gen(seed + 1), device="cuda")
+        i, j = (torch.arange(n, device="cuda") % 128 for n in shape[-2:])
+        return torch.where(i[:, None] == j, 448.0, v).to(BF16)
+
+    x, g, w = whole(131, M, K), whole(133, M, N), whole(135, E, N, K)
+    o = _offsets(split)
+    (wq, ws), (xq, xs, xcq, xcs) = eat.quant_tiles(w), eat.quant_rows_columns(x, o)
+    gq, gs, gcq, gcs = eat.quant_rows_columns(g, o)
+    blocks = M // 128
+    assert (ws == 1).all() and (xs == 1).all() and (xcs[:blocks] == 1).all() and (gcs[:blocks] == 1).all()
+    y = eat.block_mm(xq, xs, wq, ws, offsets=o, dtype=F32)
+    dx = eat.block_mm(gq, gs, wq, ws, offsets=o, transposed=True, dtype=F32)
+    dw = eat.block_mm_grad(gcq, gcs, xcq, xcs, offsets=o, dtype=F32)
+    for e in range(E):
+        r = slice(o[e].item(), o[e + 1].item())
+        assert torch.equal(y[r].double(), x[r].double() @ w[e].double().t())
+        assert torch.equal(dx[r].double(), g[r].double() @ w[e].double())
+        assert torch.equal(dw[e].double(), g[r].double().t() @ x[r].double())
 
 
 @pytest.mark.parametrize("transposed", [False, True])
