@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(Cfg<NT>::kThreads, 1)
 block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const Args a) {
   using C = Cfg<NT>;
-  static_assert(MODE != kGrad || NT % kBlock == 0, "columns of 128 bytes");
+  static_assert(MODE != kGrad || C::kCols == kBlock, "columns of 128 bytes");
   constexpr int S = C::kStages, B = C::kBufs;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -632,10 +632,6 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // On an SM pair (cta_group::2): up to 256 of x's rows (M, half of them each CTA's) x 256 columns (N).  A
 // thread owns a row of 128 columns, so a k-block's scales are one product a thread: its row's times the
 // columns' block's, loaded kLead k-blocks ahead.
-// Rows an expert has on average, above which its tiles are these (32 matrices of 2048 x 2048, 96 rows each:
-// 49 us, 45 with the kernel above; 128 rows: 47 and 51; 256: 57 and 65)
-constexpr int kWideRows = 112;
-
 struct Wide {
   static constexpr int kRows = 256, kCols = 256;
   static constexpr int kStage = 2 * kOperand, kStages = 6;
@@ -991,11 +987,33 @@ eat_status run(const char* fn, const void* x, const void* w, const Args& a, int 
   cudaError_t e = cudaGetDevice(&device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (e != cudaSuccess) return launched(fn, e);
-  // rows of a tile at most: what an expert has on average, with room
-  const int rows = MODE == kGrad ? a.N : (a.M + a.E - 1) / a.E;
-  int nt = rows <= 16 ? 32 : rows <= 32 ? 64 : rows <= 64 ? 128 : 256;
-  if (MODE == kGrad) nt = rows <= kBlock ? 128 : 256;  // (its operands come in columns of 128)
-  const bool wide = MODE != kGrad && rows > kWideRows;
+  const int cols = MODE == kForward ? a.N : a.K, col_tiles = (cols + kBlock - 1) / kBlock;
+  // at most, for tiles of up to n rows
+  auto tiles_of = [&](int n) {
+    if (MODE == kGrad) return (long long)a.E * ((a.N + n - 1) / n) * col_tiles;
+    return std::min((long long)a.M, (a.M + (long long)a.E * (n - 1)) / n) * col_tiles;
+  };
+  // Rows of a tile: what an expert has on average, with room.  32 matrices of 2048 x 2048, 48 rows each: tiles
+  // of 64 28.4 us, 128 31.5, 256 36.0; 96 rows: 44.5, 38.7, 43.0, on pairs 43.5; 128 rows: 50.7, 40.7,
+  // 46.9, 44.8; 160 rows: 62.4, 48.0, 48.2, 45.7; 256 rows: 97.0, 69.4, 59.0, 55.1.
+  int nt = 256;  // (kGrad: its operands come in columns of 128, a warp's half)
+  bool wide = false;
+  if (MODE != kGrad) {
+    const int rows = (a.M + a.E - 1) / a.E;
+    nt = rows <= 16 ? 32 : rows <= 48 ? 64 : 128;
+    wide = rows > 144;
+    // Where tiles are few, the lowest that all run at the same time: a tile's time is mostly latency and its
+    // share of the epilogue (1000 rows, 512 x 2048: 32 to 64 rows 8.6 us, 128 10.1, 256 14.6, on pairs 13.3).
+    // Of 256 rows only short sums, as pairs start 1 us later and take less for each k-block (777 rows, 4096 x
+    // 1408: 11.7 us, on pairs 12.6; 531 rows, 4096 x 4096: 23.1 and 21.1).
+    const int nkb = ((MODE == kForward ? a.K : a.N) + kBlock - 1) / kBlock;
+    for (int n = 32; n <= (nkb <= 12 ? 256 : 128); n *= 2)
+      if (tiles_of(n) <= sms) {
+        nt = n;
+        wide = false;
+        break;
+      }
+  }
   const int box = MODE == kGrad || wide ? 32 : std::min(nt, 64);
   CUtensorMap ma, mb;
   bool ok;
@@ -1007,17 +1025,12 @@ eat_status run(const char* fn, const void* x, const void* w, const Args& a, int 
   if (!ok) return thread_fail(EAT_ERR_CUDA, "%s: tensor map", fn);
   if constexpr (MODE != kGrad)
     if (wide) return launched(fn, run_wide<MODE>(ma, mb, a, out_dtype, sms, st));
-  const int cols = MODE == kForward ? a.N : a.K, col_tiles = (cols + kBlock - 1) / kBlock;
-  const long long tiles =
-      (MODE == kGrad ? (long long)a.E * ((a.N + nt - 1) / nt)
-                     : (long long)std::min((long long)a.M, (a.M + (long long)a.E * (nt - 1)) / nt)) *
-      col_tiles;
-  const int ctas = (int)std::min<long long>(sms, tiles);
+  const int ctas = (int)std::min<long long>(sms, tiles_of(nt));
   if (nt == 256) e = run_nt<MODE, 256>(ma, mb, a, out_dtype, ctas, st);
-  else if (nt == 128) e = run_nt<MODE, 128>(ma, mb, a, out_dtype, ctas, st);
   else if constexpr (MODE != kGrad)
-    e = nt == 64 ? run_nt<MODE, 64>(ma, mb, a, out_dtype, ctas, st)
-                 : run_nt<MODE, 32>(ma, mb, a, out_dtype, ctas, st);
+    e = nt == 128  ? run_nt<MODE, 128>(ma, mb, a, out_dtype, ctas, st)
+        : nt == 64 ? run_nt<MODE, 64>(ma, mb, a, out_dtype, ctas, st)
+                   : run_nt<MODE, 32>(ma, mb, a, out_dtype, ctas, st);
   return launched(fn, e);
 }
 

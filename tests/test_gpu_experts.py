@@ -403,6 +403,29 @@ def test_product_of_experts(split, N, K, transposed, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("split,cols,inner", [
+    ([1500], 3008, 400), ([1500], 3008, 1680), ([2001], 2816, 272), ([90], 8192, 272), ([200], 8192, 144),
+    ([300, 0, 517, 513, 1], 2816, 272), ([0, 900, 17, 2, 400], 2832, 1616), ([100, 90, 130] * 4, 2048, 272),
+    ([40, 0, 55, 33] * 10, 2048, 144), ([700, 3] * 3, 2064, 1552)])
+def test_products_of_every_tile(split, cols, inner, transposed, dtype):
+    """Enough tiles of each kind: few and many rows an expert, short and long sums."""
+    E, R = len(split), sum(split)
+    M, N, K = R + 7, *((inner, cols) if transposed else (cols, inner))
+    x, w = _randn(141, M, inner).to(BF16), _randn(142, E, N, K).to(BF16)
+    x[R:] = NAN
+    offsets = _offsets(split)
+    (xq, xs), (wq, ws) = eat.quant_rows(x), eat.quant_tiles(w)
+    y = eat.block_mm(xq, xs, wq, ws, offsets=offsets, transposed=transposed, dtype=dtype)
+    a, b = _of_rows(xq, xs), _of_tiles(wq, ws)
+    for e in range(E):
+        r = slice(offsets[e].item(), offsets[e + 1].item())
+        m = b[e] if transposed else b[e].t()
+        _check_product(y[r], a[r] @ m, a[r].abs() @ m.abs(), -(-inner // 128), dtype)
+    assert (y[R:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("split", range(len(SPLITS)))
 @pytest.mark.parametrize("N,K", [(16, 16), (256, 128), (80, 272), (512, 400)])
 def test_product_grad(split, N, K, dtype):
@@ -707,7 +730,8 @@ def test_rows_far_into_a_buffer():
     assert torch.equal(scale[:, -n:], scale1)
     w, wt = (eat.quant_tiles(_randn(s, 16, d).to(BF16)) for s in (122, 123))
     y = eat.block_mm(q, scale, *w)
-    assert torch.equal(y[-130:], eat.block_mm(q[-130:], scale[:, -130:].contiguous(), *w))
+    a, b = _of_rows(q[-130:], scale[:, -130:]), _of_tiles(*w).t()
+    _check_product(y[-130:], a @ b, a.abs() @ b.abs(), d // 128, BF16)
     _, _, cq, cscale = eat.quant_rows_columns(x)
     c1, cs1 = eat.quant_columns(x[-n:])
     assert torch.equal(cq[T - n:].view(torch.uint8), c1.view(torch.uint8))  # (both padded to 128 rows)
@@ -718,7 +742,8 @@ def test_rows_far_into_a_buffer():
     del cq, cscale
     yq, ys = eat.quant_rows(y)
     back = eat.block_mm(yq, ys, *wt, transposed=True)
-    assert torch.equal(back[-130:], eat.block_mm(yq[-130:], ys[:, -130:].contiguous(), *wt, transposed=True))
+    a, b = _of_rows(yq[-130:], ys[:, -130:]), _of_tiles(*wt)
+    _check_product(back[-130:], a @ b, a.abs() @ b.abs(), 1, BF16)
     del back, q
     gu = x.view(T // 2, 2 * d)
     h = eat.swiglu(gu)
