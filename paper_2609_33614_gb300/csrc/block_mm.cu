@@ -1076,7 +1076,9 @@ extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const v
   const char* fn = "eat_block_mm_grad";
   if (!gq || !gs || !xq || !xs || !dw) return bad_arg(fn, "gq, gs, xq, xs and dw must be non-NULL");
   if (const char* why = bad_shape(E, rows, N, K, offsets, dtype)) return bad_arg(fn, why);
-  if (blocks < 1) return bad_arg(fn, "need blocks >= 1");
+  // (eat_quant_columns makes no others; an expert whose rows or blocks are not all there would count as empty)
+  if (rows % 32) return bad_arg(fn, "rows must be a multiple of 32");
+  if (blocks < (rows + kBlock - 1) / kBlock) return bad_arg(fn, "need blocks >= rows / 128");
   if (N % 16 || K % 16)
     return thread_fail(EAT_ERR_UNSUPPORTED, "%s: N and K must be multiples of 16", fn);
   if (misaligned(gq, 16) || misaligned(xq, 16) || misaligned(gs, 4) || misaligned(xs, 4) ||

@@ -1,0 +1,37 @@
+"""Block-scaled products and sorted rows: calls that the C entry points refuse, host only."""
+import pytest
+
+from paper_2609_33614_gb300 import build, eat
+from test_experts_host import BF16, MGRAD
+
+BAD = eat.EAT_ERR_INVALID_ARG
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return eat.lib()
+
+
+def _refused(lib, fn, args, word):
+    assert getattr(lib, fn)(*args) == BAD
+    text = lib.eat_last_error(None).decode()
+    assert text.startswith(fn) and word in text, text
+
+
+@pytest.mark.parametrize("rows,blocks,word", [
+    (100, 1, "multiple of 32"), (1, 1, "multiple of 32"), (33, 8, "multiple of 32"),
+    (256, 1, "blocks"), (160, 1, "blocks"), (64, 0, "blocks"), (64, -3, "blocks"), (1 << 30, 7, "blocks")])
+@pytest.mark.parametrize("offsets,E", [(None, 1), (1 << 16, 2)])
+def test_operands_of_a_weights_gradient_that_are_not_all_there(lib, rows, blocks, word, offsets, E):
+    """Rows or blocks that eat_quant_columns_rows and _blocks never give: an expert that reaches beyond them
+    would add nothing to dw."""
+    _refused(lib, "eat_block_mm_grad",
+             {**MGRAD, "rows": rows, "blocks": blocks, "offsets": offsets, "E": E}.values(), word)
+
+
+def test_every_operand_of_quant_columns_has_the_rows_and_blocks(lib):
+    for E in (1, 2, 7, 64, 256):
+        for M in list(range(1, 700)) + [4095, 4096, 70001, (1 << 30) - 31 * 256]:
+            rows, blocks = lib.eat_quant_columns_rows(M, E), lib.eat_quant_columns_blocks(M, E)
+            assert rows % 32 == 0 and blocks >= -(-rows // 128) >= 1
