@@ -512,6 +512,15 @@ eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const f
                         const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
                         int32_t transposed, void* y, int32_t ydtype, void* stream);
 
+/* Diagnostic of the waits: eat_block_mm with waits that give up after limit_ns (1 ms .. 1 s; a wait is for a
+ * step of the call, whose whole time it does not bound).  Codes of those that gave up (as in
+ * eat_get_counters; 64: the scales' warp waiting for a free accumulator) are ORed into *status, a device
+ * word. */
+eat_status eat_block_mm_selftest(const void* xq, const float* xs, const void* wq, const float* ws,
+                                 const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
+                                 int32_t transposed, void* y, int32_t ydtype, int64_t limit_ns,
+                                 uint32_t* status, void* stream);
+
 /* dw [E, N, K] (dtype: EAT_BF16 or EAT_F32) = for each expert the sum over its rows of g^T x, of
  * operands as eat_quant_columns makes them with the same offsets: gq [rows, N], gs [blocks][N], xq
  * [rows, K], xs [blocks][K], rows and blocks being eat_quant_columns_rows and _blocks (rows a multiple of 32,

@@ -46,6 +46,8 @@ struct Args {
   int blocks;      // kGrad: rows of the scales
   void* out;
   int vec;         // rows of the output begin at multiples of 16 bytes
+  unsigned long long limit_ns;  // of a wait
+  unsigned int* status;         // device word that takes the codes of the waits that gave up, or null
 };
 
 constexpr int kOperand = kBlock * kBlock;  // bytes of 128 rows of a k-block
@@ -279,6 +281,11 @@ struct Behind {
   }
 };
 
+// By one thread, after the CTA's last wait.
+__device__ __forceinline__ void report(const Args& a, const volatile unsigned int& err) {
+  if (a.status && err) atomicOr(a.status, err);
+}
+
 template <int MODE, int NT, typename Out>
 __global__ void __launch_bounds__(Cfg<NT>::kThreads, 1)
 block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -296,7 +303,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   __shared__ unsigned int err_word;
   __shared__ Experts ex;
   volatile int* const abort_flag = &abort_word;
-  const WaitCtx wc{abort_flag, &err_word};
+  const WaitCtx wc{abort_flag, &err_word, a.limit_ns};
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -432,6 +439,8 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
         mma_commit<false>(&mma_done);  // no MMA may run when TMEM is freed
       }
+      // (the whole warp: the wait's limit counts from the last MMA's issue, whichever lane issues)
+      __syncwarp();
       if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
     } else if (warp == 2) {
       Behind<Out> behind(a, ex, cols, MODE != kGrad);
@@ -625,6 +634,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (threadIdx.x == 0) report(a, err_word);
   if (warp == 1) tmem_dealloc<false>(tmem_base, C::kTmemCols);
 }
 
@@ -665,7 +675,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   __shared__ unsigned int err_word;
   __shared__ Experts ex;
   volatile int* const abort_flag = &abort_word;
-  const WaitCtx wc{abort_flag, &err_word};
+  const WaitCtx wc{abort_flag, &err_word, a.limit_ns};
 
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
@@ -779,7 +789,8 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
         }
         mma_commit<true>(&mma_done);
       }
-      if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+      __syncwarp();
+      if (leader && lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
     } else if (warp == 2) {
       Behind<Out> behind(a, ex, cols, true);
       behind.clear(1 << 30);
@@ -917,8 +928,15 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   }
   tc_fence_before();
   __syncthreads();
+  // Rank 1 issues no MMA, so its wait for the pair's last one begins where its own tiles are done: from the
+  // kernel's begin its limit would bound the whole call, not a step (5e5 rows of 65536 x 65536 take longer).
+  if (!leader && warp == 1) {
+    if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+    __syncwarp();
+  }
   cluster_sync_all();  // neither CTA leaves while the other may still signal it
   tc_fence_after();
+  if (threadIdx.x == 0) report(a, err_word);
   if (warp == 1) tmem_dealloc<true>(tmem_base, 512);
 }
 
@@ -1049,10 +1067,17 @@ const char* bad_shape(int32_t E, int32_t M, int32_t N, int32_t K, const void* of
 
 using namespace eat;
 
-extern "C" eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const float* ws,
-                                   const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
-                                   int32_t transposed, void* y, int32_t ydtype, void* stream) {
-  const char* fn = "eat_block_mm";
+namespace {
+
+// A call's waits, and the word that takes the codes of those that gave up.
+struct Waits {
+  unsigned long long limit_ns = ptx::kWaitLimitNs;
+  unsigned int* status = nullptr;
+};
+
+eat_status product(const char* fn, const void* xq, const float* xs, const void* wq, const float* ws,
+                   const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K, int32_t transposed,
+                   void* y, int32_t ydtype, const Waits& waits, void* stream) {
   if (!xq || !xs || !wq || !ws || !y) return bad_arg(fn, "xq, xs, wq, ws and y must be non-NULL");
   if (const char* why = bad_shape(E, M, N, K, offsets, ydtype)) return bad_arg(fn, why);
   if (K % 16 || (transposed && N % 16))
@@ -1064,9 +1089,29 @@ extern "C" eat_status eat_block_mm(const void* xq, const float* xs, const void* 
   if (overlap(y, out, xq, (size_t)M * (transposed ? N : K)) || overlap(y, out, wq, (size_t)E * N * K))
     return bad_arg(fn, "y overlaps xq or wq");
   const int vec = !misaligned(y, 16) && (transposed ? K : N) % 8 == 0;
-  const Args a{xs, ws, offsets, E, M, N, K, 0, y, vec};
+  const Args a{xs, ws, offsets, E, M, N, K, 0, y, vec, waits.limit_ns, waits.status};
   const cudaStream_t st = (cudaStream_t)stream;
   return transposed ? run<kBack>(fn, xq, wq, a, ydtype, st) : run<kForward>(fn, xq, wq, a, ydtype, st);
+}
+
+}  // namespace
+
+extern "C" eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const float* ws,
+                                   const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
+                                   int32_t transposed, void* y, int32_t ydtype, void* stream) {
+  return product("eat_block_mm", xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, Waits{}, stream);
+}
+
+extern "C" eat_status eat_block_mm_selftest(const void* xq, const float* xs, const void* wq,
+                                            const float* ws, const int32_t* offsets, int32_t E, int32_t M,
+                                            int32_t N, int32_t K, int32_t transposed, void* y,
+                                            int32_t ydtype, int64_t limit_ns, uint32_t* status,
+                                            void* stream) {
+  const char* fn = "eat_block_mm_selftest";
+  if (limit_ns < 1000000 || limit_ns > 1000000000) return bad_arg(fn, "limit_ns must be in [1e6, 1e9]");
+  if (!status || misaligned(status, 4)) return bad_arg(fn, "status must be a device word");
+  return product(fn, xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype,
+                 Waits{(unsigned long long)limit_ns, status}, stream);
 }
 
 extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq,
@@ -1087,6 +1132,6 @@ extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const v
   const size_t out = (size_t)E * N * K * (dtype == EAT_BF16 ? 2 : 4);
   if (overlap(dw, out, gq, (size_t)rows * N) || overlap(dw, out, xq, (size_t)rows * K))
     return bad_arg(fn, "dw overlaps gq or xq");
-  const Args a{gs, xs, offsets, E, rows, N, K, blocks, dw, !misaligned(dw, 16)};
+  const Args a{gs, xs, offsets, E, rows, N, K, blocks, dw, !misaligned(dw, 16), ptx::kWaitLimitNs, nullptr};
   return run<kGrad>(fn, gq, xq, a, dtype, (cudaStream_t)stream);
 }

@@ -55,24 +55,25 @@ __device__ __forceinline__ bool elect_one() {
 }
 
 // Where a CTA's waits report that they gave up: the CTA's abort flag (shared memory), which makes
-// its other roles give up too, and the handle's status word.
+// its other roles give up too, and a status word; and after how long they do.
 struct WaitCtx {
   volatile int* abort_flag;
   unsigned int* err;
+  unsigned long long limit_ns = kWaitLimitNs;
 };
 
 // Bounded wait on the phase with the given parity; false when it gave up: because another role
-// raised the abort flag (check_abort), or after kWaitLimitNs (then it raises the flag itself and
+// raised the abort flag (check_abort), or after limit_ns (then it raises the flag itself and
 // records `code`).  The first polls are inlined; only a longer wait pays for the call and the clock.
 static __device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity, WaitCtx c,
-                                            unsigned int code, bool check_abort) {
+                                                   unsigned int code, bool check_abort) {
   unsigned long long t0, t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
   for (;;) {
     if (mbar_try_wait(bar, parity)) return true;
     if (check_abort && *c.abort_flag) return false;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    if (t - t0 > kWaitLimitNs) {
+    if (t - t0 > c.limit_ns) {
       *c.abort_flag = 1;
       atomicOr(c.err, code);
       return false;
@@ -99,7 +100,7 @@ __device__ __forceinline__ bool mbar_wait_inline(uint64_t* bar, uint32_t parity,
     if (*c.abort_flag) return false;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     if (t0 == 0) t0 = t;
-    if (t - t0 > kWaitLimitNs) {
+    if (t - t0 > c.limit_ns) {
       *c.abort_flag = 1;
       atomicOr(c.err, code);
       return false;

@@ -111,6 +111,8 @@ _SIGS = {
     "eat_quant_tiles": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp]),
     "eat_block_mm": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp,
                              c_i32, c_vp]),
+    "eat_block_mm_selftest": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                      c_vp, c_i32, c_i64, c_vp, c_vp]),
     "eat_block_mm_grad": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
                                   c_vp, c_i32, c_vp]),
     "eat_swiglu": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_i32, c_vp, c_vp]),
@@ -403,6 +405,13 @@ def eat_quant_tiles(w, E, N, K, dtype, q, scale, stream=None):
 def eat_block_mm(xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, stream=None):
     _check(lib().eat_block_mm(_ptr(xq), _ptr(xs), _ptr(wq), _ptr(ws), _ptr(offsets), E, M, N, K,
                               int(transposed), _ptr(y), ydtype, _stream(stream)))
+
+
+def eat_block_mm_selftest(xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, limit_ns, status,
+                          stream=None):
+    _check(lib().eat_block_mm_selftest(_ptr(xq), _ptr(xs), _ptr(wq), _ptr(ws), _ptr(offsets), E, M, N, K,
+                                       int(transposed), _ptr(y), ydtype, limit_ns, _ptr(status),
+                                       _stream(stream)))
 
 
 def eat_block_mm_grad(gq, gs, xq, xs, offsets, E, rows, blocks, N, K, dw, dtype, stream=None):

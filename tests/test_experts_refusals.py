@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2609_33614_gb300 import build, eat
-from test_experts_host import BF16, MGRAD
+from test_experts_host import A, MGRAD, MM
 
 BAD = eat.EAT_ERR_INVALID_ARG
 
@@ -35,3 +35,12 @@ def test_every_operand_of_quant_columns_has_the_rows_and_blocks(lib):
         for M in list(range(1, 700)) + [4095, 4096, 70001, (1 << 30) - 31 * 256]:
             rows, blocks = lib.eat_quant_columns_rows(M, E), lib.eat_quant_columns_blocks(M, E)
             assert rows % 32 == 0 and blocks >= -(-rows // 128) >= 1
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(limit_ns=999_999), "limit_ns"), (dict(limit_ns=10 ** 9 + 1), "limit_ns"), (dict(status=None), "status"),
+    (dict(status=A[6] + 2), "status"), (dict(xs=None), "non-NULL"), (dict(K=65537), "N and K")])
+def test_selftest_of_the_waits(lib, kw, word):
+    args = {n: v for n, v in MM.items() if n != "stream"}
+    args.update(limit_ns=10 ** 6, status=A[6], stream=None)
+    _refused(lib, "eat_block_mm_selftest", {**args, **kw}.values(), word)
