@@ -430,6 +430,10 @@ eat_status eat_head_reset(eat_head* h, void* stream);
  * nothing arrives on gives up after limit_ns (1 us .. 1 s) and sets the head's device status word. */
 eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* stream);
 
+/* Diagnostic: the waits of the handle's later calls give up after limit_ns (1 ms .. 1 s; a wait is for a step of
+ * a call, whose whole time it does not bound), or with 0 after the usual two seconds. */
+eat_status eat_head_selftest_wait_limit(eat_head* h, int64_t limit_ns);
+
 /* ---- Experts of a router's choice: tokens sorted by expert and back, products in e4m3 -----------
  * What serving and training experts outside a layer handle takes, on the idx and w that eat_route
  * writes.  No handle; errors through eat_last_error(NULL).  Every output is a function of the inputs

@@ -17,6 +17,7 @@
 
 #include "ffn_tc.cuh"
 #include "op_checks.cuh"
+#include "tc_ptx.cuh"
 
 #include <algorithm>
 #include <cstring>
@@ -27,7 +28,7 @@ struct eat_head {
   bool w8 = false;
   int device = 0, num_sms = 0, max_pairs = 1;
   char* mem = nullptr;
-  eat::HeadStatus st{};
+  eat::HeadStatus st{nullptr, nullptr, eat::ptx::kWaitLimitNs};
   unsigned int* mirror_host = nullptr;
   bool failed = false;
   CUtensorMap w128, w64, w16, x64, e64;
@@ -604,6 +605,15 @@ eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* st
   if (on_device != EAT_OK) return on_device;
   return launched(fn, tc_selftest_bounded_wait((unsigned long long)limit_ns, h->st.err,
                                                (cudaStream_t)stream));
+}
+
+eat_status eat_head_selftest_wait_limit(eat_head* h, int64_t limit_ns) {
+  const char* fn = "eat_head_selftest_wait_limit";
+  if (!h) return bad_arg(fn, "null handle");
+  if (limit_ns != 0 && (limit_ns < 1000000LL || limit_ns > 1000000000LL))
+    return bad_arg(fn, "need 1 ms <= limit_ns <= 1 s, or 0");
+  h->st.limit_ns = limit_ns ? (unsigned long long)limit_ns : ptx::kWaitLimitNs;
+  return EAT_OK;
 }
 
 eat_status eat_head_nll(eat_head* h, const void* x, const float* x_scale, int32_t T,

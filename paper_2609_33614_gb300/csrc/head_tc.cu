@@ -129,7 +129,7 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
   __shared__ float s_max[C::kEpiWarps][C::kChunk];
   __shared__ int s_last;
   volatile int* abort_flag = &abort_word;
-  const WaitCtx wc{abort_flag, a.st.err};
+  const WaitCtx wc{abort_flag, a.st.err, a.st.limit_ns};
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -249,6 +249,8 @@ small_kernel(const __grid_constant__ CUtensorMap map_w128, const __grid_constant
       }
       mma_commit<false>(&mma_done);  // no MMA may run when TMEM is freed
     }
+    // (the whole warp: the wait's limit counts from the last MMA's issue, whichever lane issues)
+    __syncwarp();
     if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
   } else if (warp == C::kDotWarp) {
     target_logits<W8>(a, blockIdx.x, gridDim.x, lane);  // beside the MMAs
@@ -501,7 +503,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   __shared__ int abort_word;
   __shared__ float s_ws[W8 ? C::kEpiWarps : 1][W8 ? 128 : 1];
   volatile int* abort_flag = &abort_word;
-  const WaitCtx wc{abort_flag, status.err};
+  const WaitCtx wc{abort_flag, status.err, status.limit_ns};
 
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
@@ -684,7 +686,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       }
       mma_commit<true>(&mma_done);
     }
-    if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+    __syncwarp();
+    if (leader && lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
   } else if (MODE == kNll && warp == C::kDotWarp) {
     target_logits<W8>(p, blockIdx.x, gridDim.x, lane);  // beside the MMAs
   } else {
@@ -901,6 +904,12 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   }
   tc_fence_before();
   __syncthreads();
+  // Rank 1 issues no MMA, so its wait for the pair's last one begins where its own tiles are done: from the
+  // kernel's begin its limit would bound the whole launch, not a step.
+  if (!leader && warp == 1) {
+    if (lane == 0) mbar_wait(&mma_done, 0u, wc, 16u, false);
+    __syncwarp();
+  }
   cluster_sync_all();  // neither CTA leaves while the other may still signal it
   tc_fence_after();
   if (warp == 1) tmem_dealloc<true>(tmem_base, 512);

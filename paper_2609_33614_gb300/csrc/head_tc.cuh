@@ -30,6 +30,7 @@ __host__ __device__ __forceinline__ int head_rows(int n) { return n + head_lo(n)
 struct HeadStatus {
   unsigned int* err;     // device status word
   unsigned int* mirror;  // device address of its host-mapped copy
+  unsigned long long limit_ns;  // of a kernel's wait
 };
 
 // Loss of up to kHeadSmallT tokens.  part: each CTA's maximum and sum of exp2 relative to it of the base-2

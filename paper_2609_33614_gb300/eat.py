@@ -96,6 +96,7 @@ _SIGS = {
     "eat_head_nll_grad": (c_i32, [c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
     "eat_head_reset": (c_i32, [c_vp, c_vp]),
     "eat_head_selftest_expire_wait": (c_i32, [c_vp, c_i64, c_vp]),
+    "eat_head_selftest_wait_limit": (c_i32, [c_vp, c_i64]),
     "eat_expert_sort": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp]),
     "eat_expert_sort_workspace": (c_i64, [c_i32, c_i32, c_i32]),
     "eat_expert_gather": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32,
@@ -354,6 +355,10 @@ def eat_head_reset(h, stream=None):
 
 def eat_head_selftest_expire_wait(h, limit_ns: int, stream=None):
     _check(lib().eat_head_selftest_expire_wait(h, limit_ns, _stream(stream)))
+
+
+def eat_head_selftest_wait_limit(h, limit_ns: int):
+    _check(lib().eat_head_selftest_wait_limit(h, limit_ns))
 
 
 def eat_expert_sort(idx, T, K, E, mask, offsets, slot, work, stream=None):

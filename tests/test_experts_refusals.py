@@ -44,3 +44,7 @@ def test_selftest_of_the_waits(lib, kw, word):
     args = {n: v for n, v in MM.items() if n != "stream"}
     args.update(limit_ns=10 ** 6, status=A[6], stream=None)
     _refused(lib, "eat_block_mm_selftest", {**args, **kw}.values(), word)
+
+
+def test_a_null_handle_has_no_limit_of_its_waits(lib):
+    _refused(lib, "eat_head_selftest_wait_limit", (None, 10 ** 6), "null handle")
