@@ -516,15 +516,6 @@ eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const f
                         const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
                         int32_t transposed, void* y, int32_t ydtype, void* stream);
 
-/* Diagnostic of the waits: eat_block_mm with waits that give up after limit_ns (1 ms .. 1 s; a wait is for a
- * step of the call, whose whole time it does not bound).  Codes of those that gave up (as in
- * eat_get_counters; 64: the scales' warp waiting for a free accumulator) are ORed into *status, a device
- * word. */
-eat_status eat_block_mm_selftest(const void* xq, const float* xs, const void* wq, const float* ws,
-                                 const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
-                                 int32_t transposed, void* y, int32_t ydtype, int64_t limit_ns,
-                                 uint32_t* status, void* stream);
-
 /* dw [E, N, K] (dtype: EAT_BF16 or EAT_F32) = for each expert the sum over its rows of g^T x, of
  * operands as eat_quant_columns makes them with the same offsets: gq [rows, N], gs [blocks][N], xq
  * [rows, K], xs [blocks][K], rows and blocks being eat_quant_columns_rows and _blocks (rows a multiple of 32,
@@ -534,6 +525,21 @@ eat_status eat_block_mm_selftest(const void* xq, const float* xs, const void* wq
 eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq, const float* xs,
                              const int32_t* offsets, int32_t E, int32_t rows, int32_t blocks,
                              int32_t N, int32_t K, void* dw, int32_t dtype, void* stream);
+
+/* Diagnostics of the waits: eat_block_mm and eat_block_mm_grad with waits that give up after limit_ns (1 ms ..
+ * 1 s; a wait is for a step of the call, whose whole time it does not bound).  cta >= 0: the copies of that
+ * thread block end after `copies` of its k-blocks, so that waits for more expire: its outputs (on SM pairs:
+ * the pair's) that need them are NaN, all others right, and the kernel returns.  The codes of the waits that
+ * gave up (as in eat_get_counters; 64: the scales' warp waiting for a free accumulator) are ORed into *status,
+ * a device word.  No fault, trap or hang is involved. */
+eat_status eat_block_mm_selftest(const void* xq, const float* xs, const void* wq, const float* ws,
+                                 const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
+                                 int32_t transposed, void* y, int32_t ydtype, int64_t limit_ns, int32_t cta,
+                                 int64_t copies, uint32_t* status, void* stream);
+eat_status eat_block_mm_grad_selftest(const void* gq, const float* gs, const void* xq, const float* xs,
+                                      const int32_t* offsets, int32_t E, int32_t rows, int32_t blocks,
+                                      int32_t N, int32_t K, void* dw, int32_t dtype, int64_t limit_ns,
+                                      int32_t cta, int64_t copies, uint32_t* status, void* stream);
 
 /* The gated activation between an expert's two products: rows gu [R, 2 F] = [gate | up], fp32 or bf16
  * (dtype): h = gate / (1 + exp(-gate)) * up, in dtype, or (h_dtype EAT_FP8_E4M3) e4m3 with scale

@@ -39,6 +39,15 @@ using namespace ptx;
 
 enum : int { kForward = 0, kBack = 1, kGrad = 2 };
 
+// A call's bounded waits: their limit, and for the tests of what follows when one expires a CTA whose copies
+// end after so many k-blocks, and a device word that takes the codes of the waits that gave up (or null).
+struct Waits {
+  unsigned long long limit_ns = kWaitLimitNs;
+  int held_cta = -1;
+  long long held_after = 0;
+  unsigned int* status = nullptr;
+};
+
 struct Args {
   const float *xs, *ws;  // kGrad: g's and x's
   const int32_t* offsets;
@@ -46,8 +55,7 @@ struct Args {
   int blocks;      // kGrad: rows of the scales
   void* out;
   int vec;         // rows of the output begin at multiples of 16 bytes
-  unsigned long long limit_ns;  // of a wait
-  unsigned int* status;         // device word that takes the codes of the waits that gave up, or null
+  Waits waits;
 };
 
 constexpr int kOperand = kBlock * kBlock;  // bytes of 128 rows of a k-block
@@ -283,7 +291,7 @@ struct Behind {
 
 // By one thread, after the CTA's last wait.
 __device__ __forceinline__ void report(const Args& a, const volatile unsigned int& err) {
-  if (a.status && err) atomicOr(a.status, err);
+  if (a.waits.status && err) atomicOr(a.waits.status, err);
 }
 
 template <int MODE, int NT, typename Out>
@@ -303,7 +311,7 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   __shared__ unsigned int err_word;
   __shared__ Experts ex;
   volatile int* const abort_flag = &abort_word;
-  const WaitCtx wc{abort_flag, &err_word, a.limit_ns};
+  const WaitCtx wc{abort_flag, &err_word, a.waits.limit_ns};
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -364,11 +372,12 @@ block_mm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         int stage = 0;
         uint32_t phase = 0;
         long long issued = 0;
+        const long long held = (int)blockIdx.x == a.waits.held_cta ? a.waits.held_after : -1;
         bool ok = true;
         for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
           const Tile t = tile_at(u);
           for (int kb = 0; kb < t.nkb; ++kb) {
-            if (!mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
+            if (issued == held || !mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
               ok = false;
               break;
             }
@@ -675,7 +684,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
   __shared__ unsigned int err_word;
   __shared__ Experts ex;
   volatile int* const abort_flag = &abort_word;
-  const WaitCtx wc{abort_flag, &err_word, a.limit_ns};
+  const WaitCtx wc{abort_flag, &err_word, a.waits.limit_ns};
 
   const uint32_t rank = cluster_rank();
   const bool leader = rank == 0;
@@ -721,6 +730,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
         int stage = 0;
         uint32_t phase = 0;
         long long issued = 0;
+        const long long held = (int)blockIdx.x == a.waits.held_cta ? a.waits.held_after : -1;
         bool ok = true;
         for (long long u = first; ok && u < units; u += step) {
           const Tile t = tile_at(u);
@@ -729,7 +739,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ C
           const int c0 = t.c0 + (int)rank * kBlock;
           const uint32_t bytes = (uint32_t)(2 * kOperand + (box0 + box1) * 32 * kBlock);
           for (int kb = 0; kb < t.nkb; ++kb) {
-            if (!mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
+            if (issued == held || !mbar_wait_inline(&empty[stage], phase ^ 1u, wc, 1u)) {
               ok = false;
               break;
             }
@@ -1069,12 +1079,6 @@ using namespace eat;
 
 namespace {
 
-// A call's waits, and the word that takes the codes of those that gave up.
-struct Waits {
-  unsigned long long limit_ns = ptx::kWaitLimitNs;
-  unsigned int* status = nullptr;
-};
-
 eat_status product(const char* fn, const void* xq, const float* xs, const void* wq, const float* ws,
                    const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K, int32_t transposed,
                    void* y, int32_t ydtype, const Waits& waits, void* stream) {
@@ -1089,36 +1093,14 @@ eat_status product(const char* fn, const void* xq, const float* xs, const void* 
   if (overlap(y, out, xq, (size_t)M * (transposed ? N : K)) || overlap(y, out, wq, (size_t)E * N * K))
     return bad_arg(fn, "y overlaps xq or wq");
   const int vec = !misaligned(y, 16) && (transposed ? K : N) % 8 == 0;
-  const Args a{xs, ws, offsets, E, M, N, K, 0, y, vec, waits.limit_ns, waits.status};
+  const Args a{xs, ws, offsets, E, M, N, K, 0, y, vec, waits};
   const cudaStream_t st = (cudaStream_t)stream;
   return transposed ? run<kBack>(fn, xq, wq, a, ydtype, st) : run<kForward>(fn, xq, wq, a, ydtype, st);
 }
 
-}  // namespace
-
-extern "C" eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const float* ws,
-                                   const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
-                                   int32_t transposed, void* y, int32_t ydtype, void* stream) {
-  return product("eat_block_mm", xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, Waits{}, stream);
-}
-
-extern "C" eat_status eat_block_mm_selftest(const void* xq, const float* xs, const void* wq,
-                                            const float* ws, const int32_t* offsets, int32_t E, int32_t M,
-                                            int32_t N, int32_t K, int32_t transposed, void* y,
-                                            int32_t ydtype, int64_t limit_ns, uint32_t* status,
-                                            void* stream) {
-  const char* fn = "eat_block_mm_selftest";
-  if (limit_ns < 1000000 || limit_ns > 1000000000) return bad_arg(fn, "limit_ns must be in [1e6, 1e9]");
-  if (!status || misaligned(status, 4)) return bad_arg(fn, "status must be a device word");
-  return product(fn, xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype,
-                 Waits{(unsigned long long)limit_ns, status}, stream);
-}
-
-extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq,
-                                        const float* xs, const int32_t* offsets, int32_t E,
-                                        int32_t rows, int32_t blocks, int32_t N, int32_t K, void* dw,
-                                        int32_t dtype, void* stream) {
-  const char* fn = "eat_block_mm_grad";
+eat_status product_grad(const char* fn, const void* gq, const float* gs, const void* xq, const float* xs,
+                        const int32_t* offsets, int32_t E, int32_t rows, int32_t blocks, int32_t N,
+                        int32_t K, void* dw, int32_t dtype, const Waits& waits, void* stream) {
   if (!gq || !gs || !xq || !xs || !dw) return bad_arg(fn, "gq, gs, xq, xs and dw must be non-NULL");
   if (const char* why = bad_shape(E, rows, N, K, offsets, dtype)) return bad_arg(fn, why);
   // (eat_quant_columns makes no others; an expert whose rows or blocks are not all there would count as empty)
@@ -1132,6 +1114,52 @@ extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const v
   const size_t out = (size_t)E * N * K * (dtype == EAT_BF16 ? 2 : 4);
   if (overlap(dw, out, gq, (size_t)rows * N) || overlap(dw, out, xq, (size_t)rows * K))
     return bad_arg(fn, "dw overlaps gq or xq");
-  const Args a{gs, xs, offsets, E, rows, N, K, blocks, dw, !misaligned(dw, 16), ptx::kWaitLimitNs, nullptr};
+  const Args a{gs, xs, offsets, E, rows, N, K, blocks, dw, !misaligned(dw, 16), waits};
   return run<kGrad>(fn, gq, xq, a, dtype, (cudaStream_t)stream);
+}
+
+// (copies that nothing waits for have landed long before a millisecond is over)
+const char* bad_waits(int64_t limit_ns, int32_t cta, int64_t copies, const void* status) {
+  if (limit_ns < 1000000 || limit_ns > 1000000000) return "limit_ns must be in [1e6, 1e9]";
+  if (cta >= 0 && copies < 0) return "copies must not be negative";
+  if (!status || misaligned(status, 4)) return "status must be a device word";
+  return nullptr;
+}
+
+}  // namespace
+
+extern "C" eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const float* ws,
+                                   const int32_t* offsets, int32_t E, int32_t M, int32_t N, int32_t K,
+                                   int32_t transposed, void* y, int32_t ydtype, void* stream) {
+  return product("eat_block_mm", xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, Waits{}, stream);
+}
+
+extern "C" eat_status eat_block_mm_selftest(const void* xq, const float* xs, const void* wq,
+                                            const float* ws, const int32_t* offsets, int32_t E, int32_t M,
+                                            int32_t N, int32_t K, int32_t transposed, void* y,
+                                            int32_t ydtype, int64_t limit_ns, int32_t cta, int64_t copies,
+                                            uint32_t* status, void* stream) {
+  const char* fn = "eat_block_mm_selftest";
+  if (const char* why = bad_waits(limit_ns, cta, copies, status)) return bad_arg(fn, why);
+  return product(fn, xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype,
+                 Waits{(unsigned long long)limit_ns, cta, copies, status}, stream);
+}
+
+extern "C" eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq,
+                                        const float* xs, const int32_t* offsets, int32_t E,
+                                        int32_t rows, int32_t blocks, int32_t N, int32_t K, void* dw,
+                                        int32_t dtype, void* stream) {
+  return product_grad("eat_block_mm_grad", gq, gs, xq, xs, offsets, E, rows, blocks, N, K, dw, dtype, Waits{},
+                      stream);
+}
+
+extern "C" eat_status eat_block_mm_grad_selftest(const void* gq, const float* gs, const void* xq,
+                                                 const float* xs, const int32_t* offsets, int32_t E,
+                                                 int32_t rows, int32_t blocks, int32_t N, int32_t K, void* dw,
+                                                 int32_t dtype, int64_t limit_ns, int32_t cta,
+                                                 int64_t copies, uint32_t* status, void* stream) {
+  const char* fn = "eat_block_mm_grad_selftest";
+  if (const char* why = bad_waits(limit_ns, cta, copies, status)) return bad_arg(fn, why);
+  return product_grad(fn, gq, gs, xq, xs, offsets, E, rows, blocks, N, K, dw, dtype,
+                      Waits{(unsigned long long)limit_ns, cta, copies, status}, stream);
 }

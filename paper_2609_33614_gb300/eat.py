@@ -113,7 +113,9 @@ _SIGS = {
     "eat_block_mm": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp,
                              c_i32, c_vp]),
     "eat_block_mm_selftest": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
-                                      c_vp, c_i32, c_i64, c_vp, c_vp]),
+                                      c_vp, c_i32, c_i64, c_i32, c_i64, c_vp, c_vp]),
+    "eat_block_mm_grad_selftest": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32,
+                                           c_i32, c_vp, c_i32, c_i64, c_i32, c_i64, c_vp, c_vp]),
     "eat_block_mm_grad": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
                                   c_vp, c_i32, c_vp]),
     "eat_swiglu": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_i32, c_vp, c_vp]),
@@ -413,15 +415,22 @@ def eat_block_mm(xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, str
 
 
 def eat_block_mm_selftest(xq, xs, wq, ws, offsets, E, M, N, K, transposed, y, ydtype, limit_ns, status,
-                          stream=None):
+                          cta=-1, copies=0, stream=None):
     _check(lib().eat_block_mm_selftest(_ptr(xq), _ptr(xs), _ptr(wq), _ptr(ws), _ptr(offsets), E, M, N, K,
-                                       int(transposed), _ptr(y), ydtype, limit_ns, _ptr(status),
-                                       _stream(stream)))
+                                       int(transposed), _ptr(y), ydtype, limit_ns, cta, copies,
+                                       _ptr(status), _stream(stream)))
 
 
 def eat_block_mm_grad(gq, gs, xq, xs, offsets, E, rows, blocks, N, K, dw, dtype, stream=None):
     _check(lib().eat_block_mm_grad(_ptr(gq), _ptr(gs), _ptr(xq), _ptr(xs), _ptr(offsets), E, rows,
                                    blocks, N, K, _ptr(dw), dtype, _stream(stream)))
+
+
+def eat_block_mm_grad_selftest(gq, gs, xq, xs, offsets, E, rows, blocks, N, K, dw, dtype, limit_ns, status,
+                               cta=-1, copies=0, stream=None):
+    _check(lib().eat_block_mm_grad_selftest(_ptr(gq), _ptr(gs), _ptr(xq), _ptr(xs), _ptr(offsets), E, rows,
+                                            blocks, N, K, _ptr(dw), dtype, limit_ns, cta, copies,
+                                            _ptr(status), _stream(stream)))
 
 
 def eat_swiglu(gu, R, F, dtype, h, h_dtype, scale=None, stream=None):

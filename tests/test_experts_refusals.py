@@ -37,13 +37,15 @@ def test_every_operand_of_quant_columns_has_the_rows_and_blocks(lib):
             assert rows % 32 == 0 and blocks >= -(-rows // 128) >= 1
 
 
+@pytest.mark.parametrize("fn,base", [("eat_block_mm_selftest", MM), ("eat_block_mm_grad_selftest", MGRAD)])
 @pytest.mark.parametrize("kw,word", [
     (dict(limit_ns=999_999), "limit_ns"), (dict(limit_ns=10 ** 9 + 1), "limit_ns"), (dict(status=None), "status"),
-    (dict(status=A[6] + 2), "status"), (dict(xs=None), "non-NULL"), (dict(K=65537), "N and K")])
-def test_selftest_of_the_waits(lib, kw, word):
-    args = {n: v for n, v in MM.items() if n != "stream"}
-    args.update(limit_ns=10 ** 6, status=A[6], stream=None)
-    _refused(lib, "eat_block_mm_selftest", {**args, **kw}.values(), word)
+    (dict(status=A[6] + 2), "status"), (dict(copies=-1), "copies"), (dict(xs=None), "non-NULL"),
+    (dict(K=65537), "N and K")])
+def test_selftests_of_the_waits(lib, fn, base, kw, word):
+    args = {n: v for n, v in base.items() if n != "stream"}
+    args.update(limit_ns=10 ** 6, cta=0, copies=1, status=A[6], stream=None)
+    _refused(lib, fn, {**args, **kw}.values(), word)
 
 
 def test_a_null_handle_has_no_limit_of_its_waits(lib):
