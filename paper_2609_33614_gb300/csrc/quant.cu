@@ -21,11 +21,45 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
-// 1 / (1 + exp(-g)): within 3 2^-23 + |g| 2^-24 of itself, far below what bf16 or e4m3 keep of it.
+// 1 / (1 + exp(-g)) for g >= kFarGate, where the exponential is finite.  CUDA's tables give expf 2 units in the last
+// place and __expf 2 + |1.173 g|, so it is within 3 2^-23 of itself in fp32; of bf16 operands within
+// (4 + 1.173 |g|) 2^-23, below 2^-16, far less than what bf16 or e4m3 keep of it.
+template <typename T>
 __device__ __forceinline__ float sigmoid(float g) {
+  if (sizeof(T) == 4) return __frcp_rn(1.0f + expf(-g));
   float r;
   asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-g)));
   return r;
+}
+// Below it exp(-g) would overflow long before gate * sigmoid * up is 0 (-89: -2e-37 up).  There the sigmoid is exp(g)
+// to within 2^-92 of itself, and exp(g / 2), which each of two factors takes, is a normal number down to -174.
+constexpr float kFarGate = -64.0f;
+template <typename T>
+__device__ __forceinline__ float far_root(float g) {
+  return sizeof(T) == 4 ? expf(0.5f * g) : __expf(0.5f * g);
+}
+// Whether any of a thread's gates is (as a rule none: one test for all of them).
+template <int N>
+__device__ __forceinline__ bool any_far(const float* g) {
+  float lo = g[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) lo = fminf(lo, g[j]);
+  return lo < kFarGate;
+}
+// v = swiglu of g and u
+template <typename T, int N>
+__device__ __forceinline__ void swiglu_values(const float* g, const float* u, float* v) {
+  const bool far = any_far<N>(g);
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = g[j] * sigmoid<T>(g[j]) * u[j];
+  if (far) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (g[j] < kFarGate) {
+        const float h = far_root<T>(g[j]);
+        v[j] = (g[j] * h) * (u[j] * h);
+      }
+  }
 }
 
 // ------------------------------------------------------------------------------------- rows
@@ -60,12 +94,13 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
     for (int i = 0; i < U; ++i) {
       const long long r = r0 + i0 + i;
       float v[N], top = 0.f;
-      in[i].get(v);
-      if (GLU) {
-        float u[N];
+      if (!GLU) {
+        in[i].get(v);
+      } else {
+        float g[N], u[N];
+        in[i].get(g);
         up[GLU ? i : 0].get(u);
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = v[j] * sigmoid(v[j]) * u[j];
+        swiglu_values<T, N>(g, u, v);
       }
       // (elements that do not exist are 0)
 #pragma unroll
@@ -309,8 +344,7 @@ swiglu_kernel(const T* __restrict__ gu, const T* __restrict__ dh, long long n, i
   load_elems<T, N, VEC, 32>(gu + g0, left, g);
   load_elems<T, N, VEC, 32>(gu + g0 + F, left, u);
   if (!GRAD) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) o[j] = g[j] * sigmoid(g[j]) * u[j];
+    swiglu_values<T, N>(g, u, o);
     store_elems<T, N, VEC, 32>(out + at, left, o);
     return;
   }
@@ -318,9 +352,18 @@ swiglu_kernel(const T* __restrict__ gu, const T* __restrict__ dh, long long n, i
   load_elems<T, N, VEC, 32>(dh + at, left, d);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const float s = sigmoid(g[j]);
+    const float s = sigmoid<T>(g[j]);
     o[j] = d[j] * u[j] * s * fmaf(g[j], 1.0f - s, 1.0f);
     du[j] = d[j] * g[j] * s;
+  }
+  if (any_far<N>(g)) {  // (there 1 - s is 1)
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (g[j] < kFarGate) {
+        const float h = far_root<T>(g[j]), dr = d[j] * h;
+        o[j] = dr * (u[j] * h) * (g[j] + 1.0f);
+        du[j] = dr * (g[j] * h);
+      }
   }
   store_elems<T, N, VEC, 32>(out + g0, left, o);
   store_elems<T, N, VEC, 32>(out + g0 + F, left, du);
