@@ -46,7 +46,8 @@ __device__ __forceinline__ bool any_far(const float* g) {
   for (int j = 1; j < N; ++j) lo = fminf(lo, g[j]);
   return lo < kFarGate;
 }
-// v = swiglu of g and u
+// v = swiglu of g and u.  (One test for all: a branch an element made the e4m3 form of 16383 x 1408 31 -> 37 us.  The
+// gradient, which holds more registers, tests each: 41 -> 39.8 us.)
 template <typename T, int N>
 __device__ __forceinline__ void swiglu_values(const float* g, const float* u, float* v) {
   const bool far = any_far<N>(g);
@@ -352,18 +353,15 @@ swiglu_kernel(const T* __restrict__ gu, const T* __restrict__ dh, long long n, i
   load_elems<T, N, VEC, 32>(dh + at, left, d);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const float s = sigmoid<T>(g[j]);
-    o[j] = d[j] * u[j] * s * fmaf(g[j], 1.0f - s, 1.0f);
-    du[j] = d[j] * g[j] * s;
-  }
-  if (any_far<N>(g)) {  // (there 1 - s is 1)
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (g[j] < kFarGate) {
-        const float h = far_root<T>(g[j]), dr = d[j] * h;
-        o[j] = dr * (u[j] * h) * (g[j] + 1.0f);
-        du[j] = dr * (g[j] * h);
-      }
+    if (__builtin_expect(g[j] < kFarGate, 0)) {  // (there 1 - s is 1)
+      const float h = far_root<T>(g[j]), dr = d[j] * h;
+      o[j] = dr * (u[j] * h) * (g[j] + 1.0f);
+      du[j] = dr * (g[j] * h);
+    } else {
+      const float s = sigmoid<T>(g[j]);
+      o[j] = d[j] * u[j] * s * fmaf(g[j], 1.0f - s, 1.0f);
+      du[j] = d[j] * g[j] * s;
+    }
   }
   store_elems<T, N, VEC, 32>(out + g0, left, o);
   store_elems<T, N, VEC, 32>(out + g0 + F, left, du);
