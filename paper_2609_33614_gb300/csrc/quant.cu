@@ -317,12 +317,13 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
 }
 
 // ----------------------------------------------------------------------------------- swiglu
+// The gradient may be written over gu: a thread loads all that it needs before it stores, and stores where it alone
+// loads (gu and out may be one array, so neither is __restrict__).
 // A vector a thread; where rows begin anywhere a warp takes 32 vectors' elements of one row, lanes side by side
 // (32000 x 721 bf16: 33 us, gradient 47; one element a thread, with a division for each, took over twice that).
 template <typename T, bool VEC, bool GRAD>
 __global__ void __launch_bounds__(kThreads)
-swiglu_kernel(const T* __restrict__ gu, const T* __restrict__ dh, long long n, int F,
-              T* __restrict__ out) {
+swiglu_kernel(const T* gu, const T* __restrict__ dh, long long n, int F, T* out) {
   constexpr int N = Elem<T>::kN;
   pdl_wait();
   pdl_launch_dependents();
