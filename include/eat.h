@@ -438,6 +438,8 @@ eat_status eat_head_selftest_wait_limit(eat_head* h, int64_t limit_ns);
  * What serving and training experts outside a layer handle takes, on the idx and w that eat_route
  * writes.  No handle; errors through eat_last_error(NULL).  Every output is a function of the inputs
  * alone: the same inputs give the same bits.  1 <= K <= 16, 1 <= E <= 256, T K <= 2^30, 1 <= d <= 65536.
+ * An output (or work) that overlaps an input or another output is refused (EAT_ERR_INVALID_ARG); only
+ * eat_swiglu_grad may write over its rows.
  * offsets [E + 1] and slot stay on the device; calls read them there.  Others than eat_expert_sort writes (not
  * in order, beyond the rows) reach nothing outside of the call's buffers, but what the outputs then are is
  * not defined. */

@@ -1090,8 +1090,13 @@ eat_status product(const char* fn, const void* xq, const float* xs, const void* 
       misaligned(offsets, 4) || misaligned(y, ydtype == EAT_BF16 ? 2 : 4))
     return bad_arg(fn, "misaligned pointer");
   const size_t out = (size_t)M * (transposed ? K : N) * (ydtype == EAT_BF16 ? 2 : 4);
-  if (overlap(y, out, xq, (size_t)M * (transposed ? N : K)) || overlap(y, out, wq, (size_t)E * N * K))
-    return bad_arg(fn, "y overlaps xq or wq");
+  const int inner = transposed ? N : K;
+  if (overlaps({{y, out}}, {{xq, (size_t)M * inner},
+                            {xs, 4 * (size_t)blocks_of(inner) * M},
+                            {wq, (size_t)E * N * K},
+                            {ws, 4 * (size_t)E * blocks_of(N) * blocks_of(K)},
+                            {offsets, 4 * (size_t)(E + 1)}}))
+    return bad_arg(fn, "y overlaps another array");
   const int vec = !misaligned(y, 16) && (transposed ? K : N) % 8 == 0;
   const Args a{xs, ws, offsets, E, M, N, K, 0, y, vec, waits};
   const cudaStream_t st = (cudaStream_t)stream;
@@ -1112,8 +1117,12 @@ eat_status product_grad(const char* fn, const void* gq, const float* gs, const v
       misaligned(offsets, 4) || misaligned(dw, dtype == EAT_BF16 ? 2 : 4))
     return bad_arg(fn, "misaligned pointer");
   const size_t out = (size_t)E * N * K * (dtype == EAT_BF16 ? 2 : 4);
-  if (overlap(dw, out, gq, (size_t)rows * N) || overlap(dw, out, xq, (size_t)rows * K))
-    return bad_arg(fn, "dw overlaps gq or xq");
+  if (overlaps({{dw, out}}, {{gq, (size_t)rows * N},
+                             {gs, 4 * (size_t)blocks * N},
+                             {xq, (size_t)rows * K},
+                             {xs, 4 * (size_t)blocks * K},
+                             {offsets, 4 * (size_t)(E + 1)}}))
+    return bad_arg(fn, "dw overlaps another array");
   const Args a{gs, xs, offsets, E, rows, N, K, blocks, dw, !misaligned(dw, 16), waits};
   return run<kGrad>(fn, gq, xq, a, dtype, (cudaStream_t)stream);
 }

@@ -122,6 +122,7 @@ struct RowVec {
 // its value.  A block that holds an infinity has an infinite scale, so all of it reads as NaN; a NaN
 // leaves the others as they are.
 constexpr int kBlock = 128;  // elements of a block along its axis
+constexpr long long blocks_of(long long n) { return (n + kBlock - 1) / kBlock; }
 
 // (within 2^-23 of the quotient)
 __device__ __forceinline__ float block_scale(float top) {

@@ -421,7 +421,8 @@ extern "C" eat_status eat_quant_rows(const void* x, int32_t M, int32_t K, int32_
   if (const char* why = bad_matrix(M, K, dtype)) return bad_arg(fn, why);
   if (misaligned(x, elem_bytes(dtype)) || misaligned(scale, 4)) return bad_arg(fn, "misaligned pointer");
   const size_t n = (size_t)M * K;
-  if (overlap(q, n, x, n * elem_bytes(dtype))) return bad_arg(fn, "q overlaps x");
+  if (overlaps({{q, n}, {scale, 4 * (size_t)blocks_of(K) * M}}, {{x, n * elem_bytes(dtype)}}))
+    return bad_arg(fn, "q or scale overlaps another array");
   return launched(fn, quant_rows<false>(x, M, K, dtype, q, scale, (cudaStream_t)stream));
 }
 
@@ -451,8 +452,12 @@ extern "C" eat_status eat_quant_columns(const void* x, int32_t M, int32_t K, int
   const int blocks = (int)eat_quant_columns_blocks(M, E), tiles = (K + kBlock - 1) / kBlock;
   if (padded > 1 << 30) return bad_arg(fn, "need at most 2^30 padded rows");
   const size_t n = (size_t)M * K * elem_bytes(dtype);
-  if ((q && overlap(q, (size_t)M * K, x, n)) || overlap(cq, (size_t)padded * K, x, n))
-    return bad_arg(fn, "q or cq overlaps x");
+  if (overlaps({{q, (size_t)M * K},
+                {scale, 4 * (size_t)tiles * M},
+                {cq, (size_t)padded * K},
+                {cscale, 4 * (size_t)blocks * K}},
+               {{x, n}, {offsets, 4 * (size_t)(E + 1)}}))
+    return bad_arg(fn, "an output overlaps another array");
   return launched(fn, by_type(dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<T>::kN;
@@ -482,7 +487,8 @@ extern "C" eat_status eat_quant_tiles(const void* w, int32_t E, int32_t N, int32
   if (const char* why = bad_matrix(N, K, dtype)) return bad_arg(fn, why);
   if (misaligned(w, elem_bytes(dtype)) || misaligned(scale, 4)) return bad_arg(fn, "misaligned pointer");
   const size_t n = (size_t)E * N * K;
-  if (overlap(q, n, w, n * elem_bytes(dtype))) return bad_arg(fn, "q overlaps w");
+  if (overlaps({{q, n}, {scale, 4 * (size_t)E * blocks_of(N) * blocks_of(K)}}, {{w, n * elem_bytes(dtype)}}))
+    return bad_arg(fn, "q or scale overlaps another array");
   return launched(fn, by_type(dtype, [&](auto* tag) {
     using T = std::remove_pointer_t<decltype(tag)>;
     constexpr int V = Elem<T>::kN;
@@ -506,7 +512,9 @@ extern "C" eat_status eat_swiglu(const void* gu, int32_t R, int32_t F, int32_t d
   if (misaligned(gu, eb) || misaligned(h, fp8 ? 1 : eb) || (fp8 && misaligned(scale, 4)))
     return bad_arg(fn, "misaligned pointer");
   const size_t size = (size_t)R * F;
-  if (overlap(h, size * (fp8 ? 1 : eb), gu, 2 * size * eb)) return bad_arg(fn, "h overlaps gu");
+  if (overlaps({{h, size * (fp8 ? 1 : eb)}, {fp8 ? scale : nullptr, 4 * (size_t)blocks_of(F) * R}},
+               {{gu, 2 * size * eb}}))
+    return bad_arg(fn, "h or scale overlaps another array");
   const cudaStream_t st = (cudaStream_t)stream;
   if (fp8) return launched(fn, quant_rows<true>(gu, R, F, dtype, h, scale, st));
   return launched(fn, by_type(dtype, [&](auto* tag) {

@@ -435,6 +435,12 @@ extern "C" eat_status eat_expert_sort(const int32_t* idx, int32_t T, int32_t K, 
   if (!work && eat_expert_sort_workspace(T, K, E) > 0) return bad_arg(fn, "a call of this size needs work");
   if (misaligned(idx, 4) || misaligned(offsets, 4) || misaligned(slot, 4) || misaligned(work, 16))
     return bad_arg(fn, "misaligned pointer");
+  const size_t bytes_n = 4 * (size_t)T * K;
+  if (overlaps({{offsets, 4 * (size_t)(E + 1)},
+                {slot, bytes_n},
+                {work, (size_t)eat_expert_sort_workspace(T, K, E)}},
+               {{idx, bytes_n}, {mask, (size_t)T}}))
+    return bad_arg(fn, "an output or work overlaps another array");
   const cudaStream_t st = (cudaStream_t)stream;
   const int n = T * K, chunks = sort_chunks(n);
   auto smem = [&](int threads) { return (size_t)(threads / 32 + 2) * E * 4; };  // at most 35 KB
@@ -484,7 +490,9 @@ extern "C" eat_status eat_expert_gather(const void* x, int32_t T, int32_t K, int
       misaligned(offsets, 4) || (fp8 && misaligned(scale, 4)))
     return bad_arg(fn, "misaligned pointer");
   const size_t n = (size_t)T * d;
-  if (overlap(rows, n * K * (fp8 ? 1 : eb), x, n * eb)) return bad_arg(fn, "rows overlaps x");
+  if (overlaps({{rows, n * K * (fp8 ? 1 : eb)}, {fp8 ? scale : nullptr, 4 * (size_t)blocks_of(d) * T * K}},
+               {{x, n * eb}, {slot, 4 * (size_t)T * K}, {offsets, 4 * (size_t)(E + 1)}}))
+    return bad_arg(fn, "rows or scale overlaps another array");
   const cudaStream_t st = (cudaStream_t)stream;
   if (fp8) {
     auto run = [&](auto* tag) {
@@ -520,8 +528,9 @@ extern "C" eat_status eat_expert_combine(const void* rows, int32_t T, int32_t K,
   const int eb = dtype == EAT_BF16 ? 2 : 4;
   if (misaligned(rows, eb) || misaligned(y, eb) || misaligned(slot, 4) || misaligned(w, 4))
     return bad_arg(fn, "misaligned pointer");
-  if (overlap(rows, (size_t)T * K * d * eb, y, (size_t)T * d * eb))
-    return bad_arg(fn, "y overlaps rows");
+  const size_t sel = (size_t)T * K;
+  if (overlaps({{y, (size_t)T * d * eb}}, {{rows, sel * d * eb}, {slot, 4 * sel}, {w, 4 * sel}}))
+    return bad_arg(fn, "y overlaps rows, slot or w");
   auto run = [&](auto* tag) {
     using X = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<X>::kN;
@@ -549,9 +558,13 @@ extern "C" eat_status eat_expert_combine_grad(const void* dy, const void* rows, 
   if (misaligned(dy, eb) || misaligned(rows, eb) || misaligned(drows, eb) || misaligned(slot, 4) ||
       misaligned(offsets, 4) || misaligned(w, 4) || misaligned(dw, 4))
     return bad_arg(fn, "misaligned pointer");
-  const size_t n = (size_t)T * K * d * eb;
-  if (overlap(drows, n, rows, n) || overlap(drows, n, dy, n / K))
-    return bad_arg(fn, "drows overlaps rows or dy");
+  const size_t sel = (size_t)T * K, n = sel * d * eb;
+  if (overlaps({{drows, n}, {dw, 4 * sel}}, {{rows, n},
+                                             {dy, n / K},
+                                             {slot, 4 * sel},
+                                             {offsets, 4 * (size_t)(E + 1)},
+                                             {w, 4 * sel}}))
+    return bad_arg(fn, "drows or dw overlaps another array");
   auto run = [&](auto* tag) {
     using X = std::remove_pointer_t<decltype(tag)>;
     constexpr int N = Elem<X>::kN;

@@ -2,7 +2,8 @@
 import pytest
 
 from paper_2609_33614_gb300 import build, eat
-from test_experts_host import A, MGRAD, MM
+from test_experts_host import (A, BF16, CGRAD, COMBINE, F32, FP8, GATHER, GLU, GLUGRAD, MGRAD, MM, QCOLS, QROWS,
+                               QTILES, SORT)
 
 BAD = eat.EAT_ERR_INVALID_ARG
 
@@ -50,3 +51,41 @@ def test_selftests_of_the_waits(lib, fn, base, kw, word):
 
 def test_a_null_handle_has_no_limit_of_its_waits(lib):
     _refused(lib, "eat_head_selftest_wait_limit", (None, 10 ** 6), "null handle")
+
+
+BIG = 1 << 30  # apart from every other stand-in
+# the last element of the array that the output's first one lies on, or the other way round
+OVERLAPS = [
+    ("eat_expert_sort", SORT, [
+        dict(offsets=A[0] + 28), dict(slot=A[0] - 28), dict(slot=A[1] + 32), dict(mask=A[2] + 28),
+        dict(mask=BIG + 3, offsets=BIG), dict(T=1 << 20, idx=1 << 26, slot=1 << 27, work=(1 << 26) + 16),
+        dict(T=1 << 20, idx=1 << 26, slot=1 << 27, work=(1 << 27) + (1 << 23) - 16)]),
+    ("eat_expert_gather", GATHER, [
+        dict(rows=A[1] + 28), dict(rows=A[2] + 32), dict(rows_dtype=FP8, scale=A[0] + 508),
+        dict(rows_dtype=FP8, scale=A[3] + 508), dict(rows_dtype=FP8, scale=A[1] - 28),
+        dict(rows_dtype=FP8, scale=A[2] - 28)]),
+    ("eat_expert_combine", COMBINE, [dict(y=A[1] + 28), dict(w=(1 << 21) + 1020), dict(y=(1 << 20) + 2044)]),
+    ("eat_expert_combine_grad", CGRAD, [
+        dict(drows=A[0] + 28), dict(drows=A[1] + 32), dict(drows=A[2] + 28), dict(dw=A[2]), dict(dw=A[0] - 28),
+        dict(dw=A[1] + 32), dict(dw=(1 << 22) + 1020), dict(dw=(1 << 20) + 508), dict(dw=(1 << 21) + 1020)]),
+    ("eat_quant_rows", QROWS, [dict(scale=A[0] + 508), dict(scale=A[1] + 252), dict(q=A[2] + 15)]),
+    ("eat_quant_columns", QCOLS, [
+        dict(scale=A[0] + 508), dict(cscale=A[0] + 508), dict(cq=A[1] + 11), dict(q=A[1] + 11),
+        dict(scale=A[2] + 252), dict(cscale=A[4] + 4092), dict(cq=A[2] + 255), dict(cscale=A[3] + 12),
+        dict(q=None, scale=None, cscale=A[4])]),
+    ("eat_quant_tiles", QTILES, [dict(scale=(1 << 20) + 32764), dict(scale=(1 << 21) + 8188)]),
+    ("eat_block_mm", MM, [
+        dict(y=A[0] + 12), dict(y=A[1] + 4), dict(y=A[2] + 8), dict(xs=(1 << 22) + 508), dict(ws=(1 << 22) + 508),
+        dict(offsets=(1 << 22) + 508), dict(y=(1 << 20) + 254), dict(transposed=1, y=A[0] + 12)]),
+    ("eat_block_mm_grad", MGRAD, [
+        dict(dw=A[0] + 508), dict(dw=A[1] + 508), dict(dw=A[2] + 8), dict(gs=(1 << 22) + 16380),
+        dict(xs=(1 << 22) + 16380), dict(offsets=(1 << 22) + 16380)]),
+    ("eat_swiglu", GLU, [
+        dict(h_dtype=FP8, scale=A[0] + 1020), dict(h_dtype=FP8, scale=A[1] + 252), dict(h=A[0] + 1022)]),
+    ("eat_swiglu_grad", GLUGRAD, [dict(dgu=A[0] + 1022), dict(dgu=A[1] + 510)]),
+]
+
+
+@pytest.mark.parametrize("fn,base,kw", [(f, b, k) for f, b, cs in OVERLAPS for k in cs])
+def test_an_output_that_overlaps_another_array(lib, fn, base, kw):
+    _refused(lib, fn, {**base, **kw}.values(), "overlaps")
