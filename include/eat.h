@@ -521,9 +521,10 @@ eat_status eat_block_mm(const void* xq, const float* xs, const void* wq, const f
 /* dw [E, N, K] (dtype: EAT_BF16 or EAT_F32) = for each expert the sum over its rows of g^T x, of
  * operands as eat_quant_columns makes them with the same offsets: gq [rows, N], gs [blocks][N], xq
  * [rows, K], xs [blocks][K], rows and blocks being eat_quant_columns_rows and _blocks (rows a multiple of 32,
- * blocks at least rows / 128).  Zeros for an
- * expert without rows.  offsets NULL with E = 1: one expert with `rows` rows (those that pad add
- * nothing).  N and K are multiples of 16; gq and xq 16-byte aligned; dw overlaps no input; waits as above. */
+ * blocks at least rows / 128).  Zeros for an expert without rows; NaN for one whose rows or blocks, as the
+ * offsets have them, do not lie within the operands.  offsets NULL with E = 1: one expert with `rows` rows
+ * (those that pad add nothing).  N and K are multiples of 16; gq and xq 16-byte aligned; dw overlaps no
+ * input; waits as above. */
 eat_status eat_block_mm_grad(const void* gq, const float* gs, const void* xq, const float* xs,
                              const int32_t* offsets, int32_t E, int32_t rows, int32_t blocks,
                              int32_t N, int32_t K, void* dw, int32_t dtype, void* stream);

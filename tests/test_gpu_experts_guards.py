@@ -149,6 +149,20 @@ def test_outputs_of_a_sorted_step(T, K, E, d, off, dtype):
     G.check()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_weights_gradient_of_an_expert_that_is_not_all_there(dtype):
+    """Offsets of more rows than the operands have: NaN, where zeros would pass for a gradient."""
+    g, x = _randn(1, 100, 48), _randn(2, 100, 272)
+    made = torch.tensor([0, 60, 60, 100], device="cuda", dtype=torch.int32)
+    (gq, gs), (xq, xs) = eat.quant_columns(g, made), eat.quant_columns(x, made)
+    want = eat.block_mm_grad(gq, gs, xq, xs, offsets=made, dtype=dtype)
+    assert want.isfinite().all() and (want[1] == 0).all()
+    for other, whole in (([0, 60, 60, 400], 2), ([0, 60, 2000, 2000], 1)):
+        dw = eat.block_mm_grad(gq, gs, xq, xs, offsets=torch.tensor(other, device="cuda", dtype=torch.int32), dtype=dtype)
+        assert torch.equal(dw[:whole], want[:whole]) and dw[whole].isnan().all()
+        assert (dw[whole + 1:] == 0).all()  # (without rows)
+
+
 def test_weights_gradient_of_rows_far_into_a_buffer():
     """The last block of rows, whose bytes begin beyond 2^32, is all that g is not 0 in."""
     T, d, N, n = 70000, 65536, 16, 112
