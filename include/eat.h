@@ -318,6 +318,10 @@ eat_status eat_selftest_bounded_wait(int64_t limit_ns, uint32_t* status_out);
  * EAT_ERR_STATE until eat_reset_accounts.  No fault, trap or hang is involved. */
 eat_status eat_selftest_expire_wait(eat_handle* h, int64_t limit_ns, void* stream);
 
+/* Diagnostic: the waits of the handle's later calls give up after limit_ns (1 ms .. 1 s; a wait is for a step of
+ * a call, whose whole time it does not bound), or with 0 after the usual two seconds. */
+eat_status eat_selftest_wait_limit(eat_handle* h, int64_t limit_ns);
+
 /* ---- Operators around the layer: norm, vocabulary head, balance loss --------------------------
  * They need no layer handle.  Errors are reported through eat_last_error(NULL). */
 
@@ -430,8 +434,7 @@ eat_status eat_head_reset(eat_head* h, void* stream);
  * nothing arrives on gives up after limit_ns (1 us .. 1 s) and sets the head's device status word. */
 eat_status eat_head_selftest_expire_wait(eat_head* h, int64_t limit_ns, void* stream);
 
-/* Diagnostic: the waits of the handle's later calls give up after limit_ns (1 ms .. 1 s; a wait is for a step of
- * a call, whose whole time it does not bound), or with 0 after the usual two seconds. */
+/* As eat_selftest_wait_limit. */
 eat_status eat_head_selftest_wait_limit(eat_head* h, int64_t limit_ns);
 
 /* ---- Experts of a router's choice: tokens sorted by expert and back, products in e4m3 -----------

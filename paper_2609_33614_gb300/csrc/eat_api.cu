@@ -61,6 +61,7 @@ struct eat_handle {
   int stage_i = 0;
   void* xperm = nullptr;  // [Tmax*K, d] gathered token rows (tensor-core path)
   unsigned int* status = nullptr;  // device status word: bounded waits that expired
+  unsigned long long limit_ns = eat::kWaitLimitNs;  // of a kernel's wait
   // host-mapped copy of the status word, written by the account kernel of every forward call
   // (the host pointer is read by the entry points without a synchronisation)
   unsigned int* mirror_host = nullptr;
@@ -297,6 +298,7 @@ eat_status run_forward(eat_handle* h, const void* x, int T, int ppl_sign, void* 
   c.sact = h->sact;
   c.sout = h->sout;
   c.status = h->status;
+  c.limit_ns = h->limit_ns;
   const bool side = shared_on_side_stream(h, T, tile_rows);
   // large calls on SM pairs: the shared experts' units follow the routed ones in the same launches
   c.fold_shared = !side && h->backend == 1 && tc_folds_shared(h->tc, T);
@@ -886,6 +888,14 @@ eat_status eat_selftest_expire_wait(eat_handle* h, int64_t limit_ns, void* strea
   const cudaError_t e =
       tc_selftest_bounded_wait((unsigned long long)limit_ns, h->status, (cudaStream_t)stream);
   if (e != cudaSuccess) return cuda_fail(h, e, "self-test launch");
+  return EAT_OK;
+}
+
+eat_status eat_selftest_wait_limit(eat_handle* h, int64_t limit_ns) {
+  if (!h) return fail(nullptr, EAT_ERR_INVALID_ARG, "null handle");
+  if (limit_ns != 0 && (limit_ns < 1000000LL || limit_ns > 1000000000LL))
+    return fail(h, EAT_ERR_INVALID_ARG, "need 1 ms <= limit_ns <= 1 s, or 0");
+  h->limit_ns = limit_ns ? (unsigned long long)limit_ns : kWaitLimitNs;
   return EAT_OK;
 }
 

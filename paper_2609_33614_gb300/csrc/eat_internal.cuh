@@ -20,6 +20,9 @@ __device__ __forceinline__ void pdl_launch_dependents() {
 
 bool pdl_enabled();
 
+// After which a tensor-core kernel's wait, for a step of its work, gives up.
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+
 // Unique id of the context current on this thread; false if there is none or the driver cannot tell.
 // (After cudaDeviceReset the device's next context has another one.)
 bool current_context_id(unsigned long long* id);

@@ -39,7 +39,6 @@ constexpr int kBK = 64;                   // 64 bf16 = 128 B: one 128B-swizzle r
 constexpr int kBK8 = 128;                 // 128 e4m3 = 128 B: the same row for fp8 layers
 constexpr int kNumBN = 4;
 constexpr int kBNs[kNumBN] = {16, 32, 64, 128};  // single-SM token tiles; SM pairs load 128 per CTA
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 constexpr int kSmemBudget = 220 * 1024;
 
 // -------------------------------------------------------------------------------- PTX wrappers
@@ -86,7 +85,7 @@ __device__ __forceinline__ bool elect_one() {
 }
 
 // Bounded wait on the phase with the given parity.  Returns false when it gave up: because another
-// role raised the CTA's abort flag (check_abort), or after kWaitLimitNs (then it raises the flag and
+// role raised the CTA's abort flag (check_abort), or after limit_ns (then it raises the flag and
 // records `code` in the device status word).  The first polls are inlined (a phase that is there
 // costs 75 clocks instead of the 260 of a call); only a longer wait takes the call with the clock.
 __device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity,
@@ -106,7 +105,7 @@ __device__ __noinline__ bool mbar_wait_slow(uint64_t* bar, uint32_t parity,
 }
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
                                           unsigned int* err, unsigned int code, bool check_abort,
-                                          unsigned long long limit_ns = kWaitLimitNs) {
+                                          unsigned long long limit_ns) {
 #pragma unroll 1
   for (int i = 0; i < 8; ++i)
     if (mbar_try_wait(bar, parity)) return true;
@@ -116,8 +115,9 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
 // The bounded wait by all lanes of a warp, with one outcome for the whole warp (a lane that gave
 // up makes every lane give up), so warp-synchronous code after it never sees diverged lanes.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
-                                          unsigned int* err, unsigned int code) {
-  const bool ok = mbar_wait(bar, parity, abort_flag, err, code, true);
+                                          unsigned int* err, unsigned int code,
+                                          unsigned long long limit_ns) {
+  const bool ok = mbar_wait(bar, parity, abort_flag, err, code, true, limit_ns);
   return __all_sync(0xffffffffu, ok);
 }
 
@@ -303,6 +303,7 @@ struct TcArgs {
   int stream_a;              // every weight byte is read once: evict it from L2 first
   int gate_first;            // 16-row interleaved gate/up A tile: the gate rows come first
   unsigned int* err;
+  unsigned long long limit_ns;  // of a wait
 };
 
 struct Unit {
@@ -510,7 +511,7 @@ tc_ffn_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__
           const int nk = min(C::kKPS, w.kb1 - kb);
           uint8_t* st = smem + stage * C::kStageBytes;
           if (issued >= pre) {  // (the first `pre` stages: A already in flight, stage unused)
-            if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, args.err, 1u, true)) {
+            if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, args.err, 1u, true, args.limit_ns)) {
               ok = false;
               break;
             }
@@ -533,7 +534,7 @@ tc_ffn_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__
       // let the copies still in flight land before the CTA may exit
       const long long first = issued > S ? issued - S : 0;
       for (long long i = first; i < issued; ++i)
-        mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), abort_flag, args.err, 2u, false);
+        mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), abort_flag, args.err, 2u, false, args.limit_ns);
     }
   } else if (warp == 1) {
     if (elect_one()) {
@@ -546,7 +547,7 @@ tc_ffn_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__
       for (Unit w; ok && it_u.next(args, w); ++local) {
         const int buf = local & 1;
         const uint32_t tph = (uint32_t)((local >> 1) & 1);
-        if (!mbar_wait(&tempty[buf], tph ^ 1u, abort_flag, args.err, 4u, true)) {
+        if (!mbar_wait(&tempty[buf], tph ^ 1u, abort_flag, args.err, 4u, true, args.limit_ns)) {
           ok = false;
           break;
         }
@@ -561,7 +562,7 @@ tc_ffn_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__
                                           : idesc_e4m3(n_mma);
         for (int kb = w.kb0; kb < w.kb1; kb += C::kKPS) {
           const int nk = min(C::kKPS, w.kb1 - kb);
-          if (!mbar_wait(&full[stage], phase, abort_flag, args.err, 8u, true)) {
+          if (!mbar_wait(&full[stage], phase, abort_flag, args.err, 8u, true, args.limit_ns)) {
             ok = false;
             break;
           }
@@ -607,7 +608,7 @@ tc_ffn_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__
       }
       // no MMA may still be running when TMEM is freed
       mma_commit(mma_done);
-      mbar_wait(mma_done, 0u, abort_flag, args.err, 16u, false);
+      mbar_wait(mma_done, 0u, abort_flag, args.err, 16u, false, args.limit_ns);
     }
   } else {
     // ------------------------------------------------- epilogue (warps 2 .. 2 + kEpiWarps - 1)
@@ -632,7 +633,7 @@ tc_ffn_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant__
       }
       const int buf = local & 1;
       const uint32_t tph = (uint32_t)((local >> 1) & 1);
-      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u)) break;
+      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u, args.limit_ns)) break;
       tc_fence_after();
       const uint32_t tbase = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * C::kAccCols);
       const int f = w.m0 + row;
@@ -968,7 +969,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
             w.slot0 - w.g * b_shift + (int)rank * (W8 && !IL ? args.b_lo_rows : n / 2);
         for (int kb = w.kb0; kb < w.kb1; kb += C::kKPS) {
           const int nk = min(C::kKPS, w.kb1 - kb);  // k-blocks of this stage
-          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, args.err, 1u, true)) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, args.err, 1u, true, args.limit_ns)) {
             ok = false;
             break;
           }
@@ -1005,7 +1006,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
       if (leader) {
         const long long first = issued > S ? issued - S : 0;
         for (long long i = first; i < issued; ++i)
-          mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), abort_flag, args.err, 2u, false);
+          mbar_wait(&full[i % S], (uint32_t)((i / S) & 1), abort_flag, args.err, 2u, false, args.limit_ns);
       }
     }
   } else if (warp == 1) {
@@ -1020,7 +1021,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
         unit_at(u, w);
         const int buf = local & 1;
         const uint32_t tph = (uint32_t)((local >> 1) & 1);
-        if (!mbar_wait(&tempty[buf], tph ^ 1u, abort_flag, args.err, 4u, true)) {
+        if (!mbar_wait(&tempty[buf], tph ^ 1u, abort_flag, args.err, 4u, true, args.limit_ns)) {
           ok = false;
           break;
         }
@@ -1031,7 +1032,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
                                     : idesc_e4m3_pair(2 * pair_n8(w.nrows));
         for (int kb = w.kb0; kb < w.kb1; kb += C::kKPS) {
           const int nk = min(C::kKPS, w.kb1 - kb);
-          if (!mbar_wait(&full[stage], phase, abort_flag, args.err, 8u, true)) {
+          if (!mbar_wait(&full[stage], phase, abort_flag, args.err, 8u, true, args.limit_ns)) {
             ok = false;
             break;
           }
@@ -1064,7 +1065,8 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
       // no MMA may still be running when either CTA frees its TMEM
       mma_commit_pair(mma_done);
     }
-    if (lane == 0) mbar_wait(mma_done, 0u, abort_flag, args.err, 16u, false);
+    __syncwarp();
+    if (leader && lane == 0) mbar_wait(mma_done, 0u, abort_flag, args.err, 16u, false, args.limit_ns);
   } else if (IL4) {
     // ------------------------------ epilogue, gate/up interleaved in 16-row groups (warps 2..9)
     // Warp w drains TMEM lane quarter q = w % 4 for the token columns [128 ch, 128 ch + 128),
@@ -1084,7 +1086,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
       const bool mine_is_gate = lo == gate_first;
       const int buf = local & 1;
       const uint32_t tph = (uint32_t)((local >> 1) & 1);
-      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u)) break;
+      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u, args.limit_ns)) break;
       tc_fence_after();
       const uint32_t tbase =
           tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * C::kAccCols);
@@ -1152,7 +1154,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
       const int M = sh ? args_s.M : args.M;
       const int buf = local & 1;
       const uint32_t tph = (uint32_t)((local >> 1) & 1);
-      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u)) break;
+      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u, args.limit_ns)) break;
       tc_fence_after();
       const uint32_t tbase =
           tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * C::kAccCols);
@@ -1173,7 +1175,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
           mine_out[j * 32 + lane] = __uint_as_float(is_gate ? v1[j] : v0[j]);
         __syncwarp();
         if (lane == 0) mbar_arrive(&xb[b]);
-        if (!warp_wait(&xb[b], (uint32_t)((chunk >> 1) & 1), abort_flag, args.err, 128u)) {
+        if (!warp_wait(&xb[b], (uint32_t)((chunk >> 1) & 1), abort_flag, args.err, 128u, args.limit_ns)) {
           ok = false;
           break;
         }
@@ -1213,7 +1215,7 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
       const long long sstride = sh ? args_s.split_stride : args.split_stride;
       const int buf = local & 1;
       const uint32_t tph = (uint32_t)((local >> 1) & 1);
-      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u)) break;
+      if (!warp_wait(&tfull[buf], tph, abort_flag, args.err, 32u, args.limit_ns)) break;
       tc_fence_after();
       const uint32_t tbase =
           tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * C::kAccCols);
@@ -1261,6 +1263,12 @@ tc_pair_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
   }
   tc_fence_before();
   __syncthreads();
+  // Rank 1 issues no MMA, so its wait for the pair's last one begins where its own tiles are done: from the
+  // kernel's begin its limit would bound the whole launch, not a step.
+  if (!leader && warp == 1) {
+    if (lane == 0) mbar_wait(mma_done, 0u, abort_flag, args.err, 16u, false, args.limit_ns);
+    __syncwarp();
+  }
   cluster_sync_all();  // neither CTA leaves while the other may still signal it
   tc_fence_after();
   if (warp == 1) tmem_dealloc_pair(tmem_base, C::kTmemCols);
@@ -1795,6 +1803,7 @@ cudaError_t tc_launch_up(const TcLayer& L, const TcCall& c, bool shared, cudaStr
   a.kb_per_split = a.kblocks;
   a.a_rows_per_group = a.M;
   a.err = c.status;
+  a.limit_ns = c.limit_ns;
   a.stream_a = streams_weights(c.T);
   // the group layout is two or more launches old unless nothing was copied in between (then the
   // permute is the previous launch)
@@ -1929,6 +1938,7 @@ cudaError_t tc_launch_down(const TcLayer& L, const TcCall& c, bool shared, int n
   a.kb_per_split = (a.kblocks + n_split - 1) / n_split;
   a.a_rows_per_group = L.d;
   a.err = c.status;
+  a.limit_ns = c.limit_ns;
   a.stream_a = streams_weights(c.T);
   a.prefetch_a = 1;  // the group layout is the permute's, two or more launches back
   if (L.w8) {

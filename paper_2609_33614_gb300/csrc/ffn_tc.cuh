@@ -51,6 +51,7 @@ struct TcCall {
   void* sact = nullptr;            // [S*T, Fs] bf16
   void* sout = nullptr;            // [S*T, d] bf16
   unsigned int* status = nullptr;  // device status word (bounded-wait failures)
+  unsigned long long limit_ns = kWaitLimitNs;  // of a kernel's wait
   bool fold_shared = false;        // the routed launches also run the shared experts (SM pairs)
 };
 

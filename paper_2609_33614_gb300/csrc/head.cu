@@ -17,7 +17,6 @@
 
 #include "ffn_tc.cuh"
 #include "op_checks.cuh"
-#include "tc_ptx.cuh"
 
 #include <algorithm>
 #include <cstring>
@@ -28,7 +27,7 @@ struct eat_head {
   bool w8 = false;
   int device = 0, num_sms = 0, max_pairs = 1;
   char* mem = nullptr;
-  eat::HeadStatus st{nullptr, nullptr, eat::ptx::kWaitLimitNs};
+  eat::HeadStatus st{nullptr, nullptr, eat::kWaitLimitNs};
   unsigned int* mirror_host = nullptr;
   bool failed = false;
   CUtensorMap w128, w64, w16, x64, e64;
@@ -612,7 +611,7 @@ eat_status eat_head_selftest_wait_limit(eat_head* h, int64_t limit_ns) {
   if (!h) return bad_arg(fn, "null handle");
   if (limit_ns != 0 && (limit_ns < 1000000LL || limit_ns > 1000000000LL))
     return bad_arg(fn, "need 1 ms <= limit_ns <= 1 s, or 0");
-  h->st.limit_ns = limit_ns ? (unsigned long long)limit_ns : ptx::kWaitLimitNs;
+  h->st.limit_ns = limit_ns ? (unsigned long long)limit_ns : kWaitLimitNs;
   return EAT_OK;
 }
 

@@ -9,8 +9,6 @@
 namespace eat {
 namespace ptx {
 
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;
-
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
   return (uint32_t)__cvta_generic_to_shared(p);
 }

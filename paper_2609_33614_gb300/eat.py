@@ -81,6 +81,7 @@ _SIGS = {
     "eat_ffn_backend": (c_i32, [c_vp]),
     "eat_selftest_bounded_wait": (c_i32, [c_i64, ctypes.POINTER(ctypes.c_uint32)]),
     "eat_selftest_expire_wait": (c_i32, [c_vp, c_i64, c_vp]),
+    "eat_selftest_wait_limit": (c_i32, [c_vp, c_i64]),
     "eat_rms_norm": (c_i32, [c_vp, c_vp, c_i32, c_i32, c_i32, c_vp, c_dbl, c_vp, c_vp, c_i32, c_vp,
                              c_vp]),
     "eat_rms_norm_grad": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_vp, c_dbl, c_vp, c_vp, c_vp, c_vp,
@@ -301,6 +302,10 @@ def eat_selftest_bounded_wait(limit_ns: int) -> int:
 
 def eat_selftest_expire_wait(h, limit_ns: int, stream=None):
     _check(lib().eat_selftest_expire_wait(h, limit_ns, _stream(stream)), h)
+
+
+def eat_selftest_wait_limit(h, limit_ns: int):
+    _check(lib().eat_selftest_wait_limit(h, limit_ns), h)
 
 
 def eat_rms_norm(x, residual, T, d, xdtype, gamma, eps, h, y, ydtype, y_scale=None, stream=None):
