@@ -22,11 +22,11 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 // 1 / (1 + exp(-g)) for g >= kFarGate, where the exponential is finite.  CUDA's tables give expf 2 units in the last
-// place and __expf 2 + |1.173 g|, so it is within 3 2^-23 of itself in fp32; of bf16 operands within
+// place and __expf 2 + |1.173 g|, so that it is within 3 2^-23 of itself (EXACT: fp32 results), or within
 // (4 + 1.173 |g|) 2^-23, below 2^-16, far less than what bf16 or e4m3 keep of it.
-template <typename T>
+template <bool EXACT>
 __device__ __forceinline__ float sigmoid(float g) {
-  if (sizeof(T) == 4) return __frcp_rn(1.0f + expf(-g));
+  if (EXACT) return __frcp_rn(1.0f + expf(-g));
   float r;
   asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-g)));
   return r;
@@ -34,33 +34,18 @@ __device__ __forceinline__ float sigmoid(float g) {
 // Below it exp(-g) would overflow long before gate * sigmoid * up is 0 (-89: -2e-37 up).  There the sigmoid is exp(g)
 // to within 2^-92 of itself, and exp(g / 2), which each of two factors takes, is a normal number down to -174.
 constexpr float kFarGate = -64.0f;
-template <typename T>
+template <bool EXACT>
 __device__ __forceinline__ float far_root(float g) {
-  return sizeof(T) == 4 ? expf(0.5f * g) : __expf(0.5f * g);
+  return EXACT ? expf(0.5f * g) : __expf(0.5f * g);
 }
-// Whether any of a thread's gates is (as a rule none: one test for all of them).
+// Whether any of a thread's gates is: as a rule none, so that there is one test for all of them.  (Without a
+// branch, both forms at once, 16383 x 1408 bf16 took 24.7 for 20.9 us and its gradient 34.7 for 28.8.)
 template <int N>
 __device__ __forceinline__ bool any_far(const float* g) {
   float lo = g[0];
 #pragma unroll
   for (int j = 1; j < N; ++j) lo = fminf(lo, g[j]);
   return lo < kFarGate;
-}
-// v = swiglu of g and u.  (One test for all: a branch an element made the e4m3 form of 16383 x 1408 31 -> 37 us.  The
-// gradient, which holds more registers, tests each: 41 -> 39.8 us.)
-template <typename T, int N>
-__device__ __forceinline__ void swiglu_values(const float* g, const float* u, float* v) {
-  const bool far = any_far<N>(g);
-#pragma unroll
-  for (int j = 0; j < N; ++j) v[j] = g[j] * sigmoid<T>(g[j]) * u[j];
-  if (far) {
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (g[j] < kFarGate) {
-        const float h = far_root<T>(g[j]);
-        v[j] = (g[j] * h) * (u[j] * h);
-      }
-  }
 }
 
 // ------------------------------------------------------------------------------------- rows
@@ -101,7 +86,16 @@ quant_rows_kernel(const T* __restrict__ x, int M, int K, int blocks, uint8_t* __
         float g[N], u[N];
         in[i].get(g);
         up[GLU ? i : 0].get(u);
-        swiglu_values<T, N>(g, u, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = g[j] * sigmoid<false>(g[j]) * u[j];
+        if (any_far<N>(g)) {
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (g[j] < kFarGate) {
+              const float h = far_root<false>(g[j]);
+              v[j] = (g[j] * h) * (u[j] * h);
+            }
+        }
       }
       // (elements that do not exist are 0)
 #pragma unroll
@@ -319,8 +313,25 @@ quant_tiles_kernel(const T* __restrict__ w, int n_rows, int K, uint8_t* __restri
 // ----------------------------------------------------------------------------------- swiglu
 // The gradient may be written over gu: a thread loads all that it needs before it stores, and stores where it alone
 // loads (gu and out may be one array, so neither is __restrict__).
+template <typename T, bool VEC>
+__device__ __forceinline__ bool any_far(const RowVec<T, VEC, 32>& v, const float* g) {
+  if (VEC && sizeof(T) == 2) {
+    // (of 16-bit words the largest is the lowest gate, if one is negative; a NaN may count as far)
+    const unsigned m = __vmaxu2(__vmaxu2(v.u.x, v.u.y), __vmaxu2(v.u.z, v.u.w));
+    return (m & 0xffff) > 0xc280 || m > 0xc280ffffu;
+  }
+  return any_far<Elem<T>::kN>(g);
+}
+// Loaded here, whatever path uses it.
+template <typename T, bool VEC>
+__device__ __forceinline__ void loaded(RowVec<T, VEC, 32>& v) {
+  if (VEC) asm volatile("" : "+r"(v.u.x), "+r"(v.u.y), "+r"(v.u.z), "+r"(v.u.w));
+}
+
 // A vector a thread; where rows begin anywhere a warp takes 32 vectors' elements of one row, lanes side by side
-// (32000 x 721 bf16: 33 us, gradient 47; one element a thread, with a division for each, took over twice that).
+// (32000 x 721 bf16: 28.8 us, gradient 43.2; one element a thread, with a division for each, took over twice that).
+// Bound: HBM, or the L2 that holds what was written (16383 x 1408 bf16: 20.9 us, gradient 28.8; fp32 38.5 and 60,
+// of which expf and the rounded reciprocal are 2 of the first).
 template <typename T, bool VEC, bool GRAD>
 __global__ void __launch_bounds__(kThreads)
 swiglu_kernel(const T* gu, const T* __restrict__ dh, long long n, int F, T* out) {
@@ -342,27 +353,54 @@ swiglu_kernel(const T* gu, const T* __restrict__ dh, long long n, int F, T* out)
   }
   const int left = F - c;
   const size_t at = (size_t)r * F + c, g0 = (size_t)r * 2 * F + c;
+  constexpr bool EXACT = sizeof(T) == 4;
+  RowVec<T, VEC, 32> rg, ru, rd;
   float g[N], u[N], o[N];
-  load_elems<T, N, VEC, 32>(gu + g0, left, g);
-  load_elems<T, N, VEC, 32>(gu + g0 + F, left, u);
+  if (VEC || GRAD) {
+    rg.load(gu + g0, left, true);
+    ru.load(gu + g0 + F, left, true);
+  } else {
+    load_elems<T, N, VEC, 32>(gu + g0, left, g);
+    load_elems<T, N, VEC, 32>(gu + g0 + F, left, u);
+  }
+  if (GRAD) rd.load(dh + at, left, true);
+  if (VEC) {  // all loads are under way before the branch (else the gradient takes 32 us for 29)
+    loaded(ru);
+    if (GRAD) loaded(rd);
+  }
+  if (VEC || GRAD) rg.get(g);
+  if (any_far(rg, g)) {  // a path of its own, which holds no registers of the other
+#pragma unroll 1
+    for (int j = 0; j < N; ++j) {
+      const int c_j = VEC ? j : 32 * j;
+      if (c_j >= left) break;
+      const float gj = Elem<T>::get(gu[g0 + c_j]), uj = Elem<T>::get(gu[g0 + F + c_j]);
+      const bool f = gj < kFarGate;
+      const float h = far_root<EXACT>(f ? gj : 0.0f), s = sigmoid<EXACT>(f ? 0.0f : gj);
+      if (!GRAD) {
+        out[at + c_j] = Elem<T>::put(f ? (gj * h) * (uj * h) : gj * s * uj);
+      } else {
+        const float dj = Elem<T>::get(dh[at + c_j]);  // (1 - the sigmoid is 1 far below 0)
+        out[g0 + c_j] = Elem<T>::put(f ? (dj * h) * (uj * h) * (gj + 1.0f) : dj * uj * s * fmaf(gj, 1.0f - s, 1.0f));
+        out[g0 + F + c_j] = Elem<T>::put(f ? (dj * h) * (gj * h) : dj * gj * s);
+      }
+    }
+    return;
+  }
+  if (VEC || GRAD) ru.get(u);
   if (!GRAD) {
-    swiglu_values<T, N>(g, u, o);
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = g[j] * sigmoid<EXACT>(g[j]) * u[j];
     store_elems<T, N, VEC, 32>(out + at, left, o);
     return;
   }
   float d[N], du[N];
-  load_elems<T, N, VEC, 32>(dh + at, left, d);
+  rd.get(d);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    if (__builtin_expect(g[j] < kFarGate, 0)) {  // (there 1 - s is 1)
-      const float h = far_root<T>(g[j]), dr = d[j] * h;
-      o[j] = dr * (u[j] * h) * (g[j] + 1.0f);
-      du[j] = dr * (g[j] * h);
-    } else {
-      const float s = sigmoid<T>(g[j]);
-      o[j] = d[j] * u[j] * s * fmaf(g[j], 1.0f - s, 1.0f);
-      du[j] = d[j] * g[j] * s;
-    }
+    const float s = sigmoid<EXACT>(g[j]);
+    o[j] = d[j] * u[j] * s * fmaf(g[j], 1.0f - s, 1.0f);
+    du[j] = d[j] * g[j] * s;
   }
   store_elems<T, N, VEC, 32>(out + g0, left, o);
   store_elems<T, N, VEC, 32>(out + g0 + F, left, du);

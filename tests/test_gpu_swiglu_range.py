@@ -26,11 +26,12 @@ def _inputs(dtype, F, scale):
 
 
 def _units(dtype, gate):
-    """Of a sigmoid: (its exponential, the sum and the reciprocal), or of the two roots far below 0."""
+    """Of a sigmoid: its exponential, the sum and the reciprocal; far below 0 two roots of the exponential, each of
+    half the argument."""
     x = gate.double().abs()
     if dtype == F32:
-        return torch.where(gate < -63, 8.0, 6.0)
-    return torch.where(gate < -63, 2 * (4 + 1.173 * x), 4 + 2.346 * x + 3)
+        return 8.0 + 0 * x  # 4 + 1 + 1, or 2 * 4
+    return 8.0 + 2.346 * x  # 2 (2 + 1.173 x) + 1 + 2, or 2 * 2 (2 + 0.587 x)
 
 
 def _bound(dtype):
@@ -87,4 +88,26 @@ def test_e4m3_blocks_of_far_gates(dtype, F):
     assert (s != 1).all()
     t = want / s
     step = torch.maximum(t.abs() * 2.0 ** -4, torch.full_like(t, 2.0 ** -10))
-    assert ((q.double() - t).abs() <= step + (_units(dtype, gate) + 6) * U32 * t.abs()).all()
+    # (e4m3 of fp32 rows takes bf16's exponential too)
+    assert ((q.double() - t).abs() <= step + (_units(BF16, gate) + 6) * U32 * t.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("F", [1024, 1001])
+def test_far_gates_leave_their_neighbours_alone(dtype, F):
+    """Bits of an element do not depend on the gates beside it, nor on where the rows begin."""
+    gate, up = _inputs(dtype, F, 1.0)
+    gate = (gate.float() / 2).to(dtype)  # none below -64
+    dh = _inputs(dtype, F, 1.0)[1]
+    mixed = gate.clone()
+    mixed[:, ::5] = -80.0
+    near = torch.ones(F, dtype=torch.bool, device="cuda")
+    near[::5] = False
+    h, want = eat.swiglu(torch.cat([mixed, up], 1)), eat.swiglu(torch.cat([gate, up], 1))
+    d, dwant = eat.swiglu_grad(torch.cat([mixed, up], 1), dh), eat.swiglu_grad(torch.cat([gate, up], 1), dh)
+    assert torch.equal(h[:, near], want[:, near])
+    assert torch.equal(d[:, near.repeat(2)], dwant[:, near.repeat(2)])
+    buf = torch.zeros(3 * 2 * F + 8, dtype=dtype, device="cuda")
+    moved = buf[1:1 + 6 * F].view(3, 2 * F)
+    moved.copy_(torch.cat([mixed, up], 1))
+    assert torch.equal(eat.swiglu(moved), h) and torch.equal(eat.swiglu_grad(moved, dh), d)
