@@ -16,11 +16,13 @@
 //   wide_kernel: on SM pairs, 256 rows (M) x 256 columns (N), for many rows an expert: half the operand bytes
 //      from L2 for each MMA, and a k-block's scales are one product a thread.  Bound: the accumulator's way
 //      through TMEM (two buffers: an MMA of 530 cycles, then 500 of reading and adding, then the
-//      hand-over).  8192 x 2048 x 8192: 137 us, 2.0 PFLOP/s; 10240 rows, 60 matrices of 2816 x 2048: 111 us.
+//      hand-over).  8192 x 2048 x 8192: 137 us, 2.0 PFLOP/s; 60 matrices of 2816 x 2048, 170 rows
+//      each: 97 us; a router's 10240 rows, 30 to 500 each: 122.
 // Operands come by TMA as they lie (K-major, or MN-major where the sum runs over their rows): w serves
 // both directions, and the gradient reads both operands by rows.
 // Warps: 0 issues TMA, 1 owns TMEM and issues MMAs, 2 copies the blocks' scales into a ring (block_mm_kernel)
-// and clears the rows behind the last expert's, the others drain TMEM.  Every wait is bounded; where one
+// and clears the rows behind the last expert's, 3 has no role (registers are shared out by fours), the others
+// drain TMEM.  Every wait is bounded; where one
 // expires the CTA's tiles that are not done become NaN, copies and MMAs land, TMEM is freed and the kernel ends.
 #include "elem.cuh"
 #include "op_checks.cuh"
@@ -1034,7 +1036,9 @@ eat_status run(const char* fn, const void* x, const void* w, const Args& a, int 
     // Where tiles are few, the lowest that all run at the same time: a tile's time is mostly latency and its
     // share of the epilogue (1000 rows, 512 x 2048: 32 to 64 rows 8.6 us, 128 10.1, 256 14.6, on pairs 13.3).
     // Of 256 rows only short sums, as pairs start 1 us later and take less for each k-block (777 rows, 4096 x
-    // 1408: 11.7 us, on pairs 12.6; 531 rows, 4096 x 4096: 23.1 and 21.1).
+    // 1408: 11.7 us, on pairs 12.6; 531 rows, 4096 x 4096: 23.1 and 21.1; between 11 and 32 k-blocks nothing was
+    // measured).  M counts the rows behind the last expert's too: with 60 % of them live the best tile of 160 and
+    // 192 rows of 64 experts is 4 to 5 % faster than this rule's.
     const int nkb = ((MODE == kForward ? a.K : a.N) + kBlock - 1) / kBlock;
     for (int n = 32; n <= (nkb <= 12 ? 256 : 128); n *= 2)
       if (tiles_of(n) <= sms) {

@@ -571,7 +571,7 @@ extern "C" eat_status eat_expert_combine_grad(const void* dy, const void* rows, 
     const bool vec =
         d % N == 0 && !misaligned(dy, 16) && !misaligned(rows, 16) && !misaligned(drows, 16);
     // Many tokens: two warps each, so that more tokens' loads are under way (8191 tokens x 8 of 2048:
-    // 71 us, 107 with eight, cold); few: as many as the row has vectors for.
+    // 71 us, 107 with eight, cold; no other size was measured); few: as many as the row has vectors for.
     const int most = T >= 16 * num_sms() ? 2 : kWarps;
     const int warps = std::min(most, (d + 32 * N - 1) / (32 * N));
     return launch_pdl(vec ? combine_grad_kernel<X, true> : combine_grad_kernel<X, false>, dim3(T),
